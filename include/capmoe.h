@@ -270,6 +270,65 @@ int capmoe_grouped_ffn_segments(const void* x_rows, const int32_t* seg_begin, co
                                 const void* w_down, void* h_ws, void* y_rows, int64_t rows,
                                 int32_t* dev_status, void* stream);
 
+/* ---------------------------------------------------------------- grouped products and their gradients
+ * The products inside stage 5 as calls of their own, over the same expert-major rows: expert e owns the
+ * rows [expert_offsets[e], expert_offsets[e+1]) of matrices with `rows` allocated rows (offsets
+ * non-decreasing, at most `rows`; larger or negative ones are clamped).  Rows behind the last expert's are
+ * neither read into a result nor written.
+ *   capmoe_grouped_mm      y[r]  = W[e] x[r]                    x [rows,d], w [E,n,d] -> y [rows,n]
+ *   capmoe_grouped_mm_dx   dx[r] = W[e]^T dy[r]                 dy [rows,n], w [E,n,d] -> dx [rows,d]
+ *   capmoe_grouped_mm_dw   dW[e] = sum over e's rows of dy[r] x[r]^T   -> dw [E,n,d] in out_dtype (`dtype`, or
+ *                          CAPMOE_F32 for bf16 inputs); zeros for an expert without rows, the whole of dw is
+ *                          written.  ws: capmoe_grouped_mm_dw_workspace_bytes(E) bytes.
+ *   capmoe_grouped_ffn_backward   gradients of stage 5 (SwiGLU) from x_perm and dy_perm [A_max,d], the gradient
+ *                          of y_perm; the hidden activations are recomputed: g = W_g x, u = W_u x,
+ *                          dh = W_d^T dy, p = 1/(1+exp(-g)), h = g p u, dg = dh u p (1 + g (1-p)), du = dh g p;
+ *                          dx = W_g^T dg + W_u^T du, dW_g = sum dg x^T, dW_u = sum du x^T, dW_d = sum dy h^T.
+ *                          dx_perm [A_max,d], dw_gate/dw_up [E,F,d], dw_down [E,d,F], all in `dtype`.
+ *                          dg, du and h are rounded to `dtype` before the products that read them.
+ *                          ws: capmoe_ffn_backward_workspace_bytes(A_max,E,F,dtype) bytes.
+ * bf16 with d and n (F) multiples of 8 runs on tensor cores (TMA-fed tiles, fp32 accumulators); fp32 and other
+ * sizes run plain fp32-FMA kernels.  dev_status as in capmoe_grouped_ffn.  E <= 256, rows < 2^31. */
+int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n, int dtype,
+                      void* y, int64_t rows, int32_t* dev_status, void* stream);
+int capmoe_grouped_mm_dx(const void* dy_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n, int dtype,
+                         void* dx, int64_t rows, int32_t* dev_status, void* stream);
+int capmoe_grouped_mm_dw_workspace_bytes(int E, size_t* bytes);
+int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, const int32_t* expert_offsets, int E, int d, int n,
+                         int dtype, int out_dtype, void* dw, int64_t rows, void* ws, size_t ws_bytes, int32_t* dev_status,
+                         void* stream);
+int capmoe_ffn_backward_workspace_bytes(int64_t A_max, int E, int F, int dtype, size_t* bytes);
+int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_perm, const int32_t* expert_offsets, int E, int d, int F,
+                                int dtype, const void* w_gate, const void* w_up, const void* w_down, void* dx_perm,
+                                void* dw_gate, void* dw_up, void* dw_down, int64_t A_max, void* ws, size_t ws_bytes,
+                                int32_t* dev_status, void* stream);
+
+/* ---------------------------------------------------------------- 8-bit expert products
+ * e4m3 codes (the bit patterns of 8-bit floats with 4 exponent and 3 mantissa bits, finite up to 448) with one
+ * power-of-two scale per 128 columns of an activation row or per 128 x 128 block of a weight matrix (the last
+ * blocks of a row or column may be smaller):  value = code * 2^(s - 127), s the uint8 scale, s = 255 a NaN.
+ *   capmoe_quantize_rows     x [rows,d] -> q [rows,d], scale [rows, ceil(d/128)]; with n_rows (device int32, e.g.
+ *                            expert_offsets + E) only the rows below *n_rows are read and written
+ *   capmoe_quantize_weights  w [E,n,d] -> q [E,n,d], scale [E, ceil(n/128), ceil(d/128)]
+ * The scale is the smallest 2^e (e >= -127) with max|block| <= 448 * 2^e, 1 for a block of zeros; codes are
+ * rounded to nearest even.  A block that holds a NaN or an infinity becomes NaN as a whole.
+ *   capmoe_grouped_mm_fp8    y[r] = W[e] x[r] from codes and scales, fp32 accumulation, y [rows,n] bf16
+ *   capmoe_grouped_ffn_fp8   stage 5 with 8-bit weights: x_perm [A_max,d] bf16 is quantised, then
+ *                            h = silu(W_g x) * (W_u x) in fp32, h quantised, y_perm [A_max,d] bf16 = W_d h.
+ *                            ws: capmoe_ffn_fp8_workspace_bytes(A_max,d,F) bytes, contents undefined afterwards.
+ * d and n (F) multiples of 16 run on the tensor cores' block-scaled 8-bit products; other sizes run plain
+ * fp32-FMA kernels.  Rows, offsets and dev_status as for the grouped products above. */
+int capmoe_quantize_rows(const void* x, const int32_t* n_rows, int64_t rows, int d, int dtype, void* q, void* scale,
+                         void* stream);
+int capmoe_quantize_weights(const void* w, int E, int n, int d, int dtype, void* q, void* scale, void* stream);
+int capmoe_grouped_mm_fp8(const void* x_q, const void* x_scale, const int32_t* expert_offsets, const void* w_q,
+                          const void* w_scale, int E, int d, int n, void* y, int64_t rows, int32_t* dev_status, void* stream);
+int capmoe_ffn_fp8_workspace_bytes(int64_t A_max, int d, int F, size_t* bytes);
+int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_offsets, int E, int d, int F, const void* wg_q,
+                           const void* wg_scale, const void* wu_q, const void* wu_scale, const void* wd_q,
+                           const void* wd_scale, void* y_perm, int64_t A_max, void* ws, size_t ws_bytes, int32_t* dev_status,
+                           void* stream);
+
 /* ---------------------------------------------------------------- expert parallelism
  * The paper's deployment (experimental set-up: data parallel over the tokens, expert parallel over
  * the experts) with the capacity applied "within each local device" (Capacity-Aware Token Drop

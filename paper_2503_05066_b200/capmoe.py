@@ -30,7 +30,10 @@ EXPORTS = ["capmoe_capacity", "capmoe_max_rows", "capmoe_device_max_rows", "capm
            "capmoe_rows_from_mask", "capmoe_permute", "capmoe_grouped_ffn",
            "capmoe_combine", "capmoe_layer_forward", "capmoe_layer_forward_host", "capmoe_debug_wait_probe",
            "capmoe_grouped_ffn_segments", "capmoe_debug_ffn_variant", "capmoe_ep_plan", "capmoe_ep_forward_dispatch", "capmoe_ep_forward_experts", "capmoe_ep_forward_combine", "capmoe_ep_segments", "capmoe_ep_dispatch",
-           "capmoe_ep_combine", "capmoe_debug_read_probe", "capmoe_debug_check_indices"]
+           "capmoe_ep_combine", "capmoe_debug_read_probe", "capmoe_debug_check_indices",
+           "capmoe_grouped_mm", "capmoe_grouped_mm_dx", "capmoe_grouped_mm_dw_workspace_bytes", "capmoe_grouped_mm_dw",
+           "capmoe_ffn_backward_workspace_bytes", "capmoe_grouped_ffn_backward", "capmoe_quantize_rows",
+           "capmoe_quantize_weights", "capmoe_grouped_mm_fp8", "capmoe_ffn_fp8_workspace_bytes", "capmoe_grouped_ffn_fp8"]
 
 
 class CapmoeError(RuntimeError):
@@ -407,6 +410,218 @@ def grouped_ffn_segments(x_rows, seg_begin, seg_end, w_gate, w_up, w_down, w_mod
     return y_rows
 
 
+# ----------------------------------------------------------------------------- grouped products
+def _need(ok: bool, where: str, what: str):
+    if not ok:
+        raise CapmoeError(EINVAL, f"{where}: {what}")
+
+
+def _same_device(where: str, *tensors):
+    """All tensors on the current CUDA device: the library launches there and nowhere else."""
+    tensors = [t for t in tensors if t is not None]
+    for t in tensors:
+        _need(t.is_cuda, where, f"CUDA tensors expected, got one on {t.device}")
+    here = torch.cuda.current_device()
+    for t in tensors:
+        _need(t.device.index == here, where, f"tensors must be on the current device cuda:{here}, got {t.device}")
+
+
+def _bytes(fn, *args) -> int:
+    out = ctypes.c_size_t(0)
+    _check(getattr(lib(), fn)(*args, ctypes.byref(out)), fn)
+    return out.value
+
+
+def _experts(where: str, offsets) -> int:
+    _need(offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.numel() >= 2, where, "offsets must be int32 [E+1]")
+    return offsets.numel() - 1
+
+
+def _out(where: str, t, shape, dtype, like):
+    if t is None:
+        return torch.empty(shape, device=like.device, dtype=dtype)
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype, where, f"output must be {dtype} {tuple(shape)}")
+    return t
+
+
+def _status(where: str, dev_status):
+    if dev_status is not None:
+        _need(dev_status.dtype == torch.int32 and dev_status.numel() >= FFN_STATUS_WORDS, where,
+              f"dev_status must be int32 [{FFN_STATUS_WORDS}]")
+    return _ptr(dev_status)
+
+
+def grouped_mm(x_rows, offsets, w, y=None, dev_status=None, stream=None):
+    """y[r] = W[e] x[r] for the rows r of every expert e.  x_rows [rows,d], w [E,n,d] -> y [rows,n]; rows behind
+    offsets[E] are left as they are (undefined in a y made here)."""
+    where = "capmoe_grouped_mm"
+    E = _experts(where, offsets)
+    _need(x_rows.dim() == 2 and w.dim() == 3 and w.shape[0] == E and w.shape[2] == x_rows.shape[1] and w.dtype == x_rows.dtype,
+          where, "x_rows [rows,d] and w [E,n,d] of one dtype expected")
+    rows, d = x_rows.shape
+    n = w.shape[1]
+    y = _out(where, y, (rows, n), x_rows.dtype, x_rows)
+    _same_device(where, x_rows, offsets, w, y, dev_status)
+    _check(lib().capmoe_grouped_mm(_ptr(x_rows), _ptr(offsets), _ptr(w), E, int(d), int(n), _dt(x_rows), _ptr(y), _i64(rows),
+                                   _status(where, dev_status), _stream(stream)), where)
+    return y
+
+
+def grouped_mm_dx(dy_rows, offsets, w, dx=None, dev_status=None, stream=None):
+    """Gradient of grouped_mm's rows: dx[r] = W[e]^T dy[r].  dy_rows [rows,n], w [E,n,d] -> dx [rows,d]."""
+    where = "capmoe_grouped_mm_dx"
+    E = _experts(where, offsets)
+    _need(dy_rows.dim() == 2 and w.dim() == 3 and w.shape[0] == E and w.shape[1] == dy_rows.shape[1] and
+          w.dtype == dy_rows.dtype, where, "dy_rows [rows,n] and w [E,n,d] of one dtype expected")
+    rows, n = dy_rows.shape
+    d = w.shape[2]
+    dx = _out(where, dx, (rows, d), dy_rows.dtype, dy_rows)
+    _same_device(where, dy_rows, offsets, w, dx, dev_status)
+    _check(lib().capmoe_grouped_mm_dx(_ptr(dy_rows), _ptr(offsets), _ptr(w), E, int(d), int(n), _dt(dy_rows), _ptr(dx),
+                                      _i64(rows), _status(where, dev_status), _stream(stream)), where)
+    return dx
+
+
+def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, dev_status=None, stream=None):
+    """Gradient of grouped_mm's weights: dW[e] = sum over e's rows of dy[r] x[r]^T, zeros for an expert without rows.
+    -> dw [E,n,d] in the rows' dtype, or out_dtype (float32)."""
+    where = "capmoe_grouped_mm_dw"
+    E = _experts(where, offsets)
+    _need(dy_rows.dim() == 2 and x_rows.dim() == 2 and dy_rows.shape[0] == x_rows.shape[0] and dy_rows.dtype == x_rows.dtype,
+          where, "dy_rows [rows,n] and x_rows [rows,d] of one dtype expected")
+    rows, n = dy_rows.shape
+    d = x_rows.shape[1]
+    out_dtype = out_dtype or (dw.dtype if dw is not None else x_rows.dtype)
+    dw = _out(where, dw, (E, n, d), out_dtype, x_rows)
+    if ws is None:
+        ws = torch.empty((_bytes("capmoe_grouped_mm_dw_workspace_bytes", E),), device=x_rows.device, dtype=torch.uint8)
+    _same_device(where, dy_rows, x_rows, offsets, dw, ws, dev_status)
+    _check(lib().capmoe_grouped_mm_dw(_ptr(dy_rows), _ptr(x_rows), _ptr(offsets), E, int(d), int(n), _dt(x_rows), _dt(dw),
+                                      _ptr(dw), _i64(rows), _ptr(ws), ctypes.c_size_t(ws.numel()), _status(where, dev_status),
+                                      _stream(stream)), where)
+    return dw
+
+
+def ffn_backward_workspace_bytes(A_max: int, E: int, F: int, dtype) -> int:
+    return _bytes("capmoe_ffn_backward_workspace_bytes", _i64(A_max), int(E), int(F), _dt(dtype))
+
+
+def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None, dw=None, ws=None, dev_status=None,
+                         stream=None):
+    """Gradients of grouped_ffn from its input and the gradient of its output (the hidden activations are recomputed).
+    -> (dx [A_max,d], dw_gate [E,F,d], dw_up [E,F,d], dw_down [E,d,F]); `dw` may hand in the last three."""
+    where = "capmoe_grouped_ffn_backward"
+    E = _experts(where, offsets)
+    _need(x_perm.dim() == 2 and x_perm.shape == dy_perm.shape and w_gate.dim() == 3 and w_gate.shape[0] == E and
+          w_gate.shape[2] == x_perm.shape[1] and w_up.shape == w_gate.shape and
+          tuple(w_down.shape) == (E, w_gate.shape[2], w_gate.shape[1]), where,
+          "x_perm, dy_perm [A_max,d], w_gate, w_up [E,F,d], w_down [E,d,F] expected")
+    _need(len({t.dtype for t in (x_perm, dy_perm, w_gate, w_up, w_down)}) == 1, where, "one dtype expected")
+    A_max, d = x_perm.shape
+    F = w_gate.shape[1]
+    dx = _out(where, dx, (A_max, d), x_perm.dtype, x_perm)
+    dwg, dwu, dwd = (None, None, None) if dw is None else dw
+    dwg = _out(where, dwg, (E, F, d), x_perm.dtype, x_perm)
+    dwu = _out(where, dwu, (E, F, d), x_perm.dtype, x_perm)
+    dwd = _out(where, dwd, (E, d, F), x_perm.dtype, x_perm)
+    if ws is None:
+        ws = torch.empty((ffn_backward_workspace_bytes(A_max, E, F, x_perm.dtype),), device=x_perm.device, dtype=torch.uint8)
+    _same_device(where, x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx, dwg, dwu, dwd, ws, dev_status)
+    _check(lib().capmoe_grouped_ffn_backward(_ptr(x_perm), _ptr(dy_perm), _ptr(offsets), E, int(d), int(F), _dt(x_perm),
+                                             _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(dwd),
+                                             _i64(A_max), _ptr(ws), ctypes.c_size_t(ws.numel()), _status(where, dev_status),
+                                             _stream(stream)), where)
+    return dx, dwg, dwu, dwd
+
+
+# ----------------------------------------------------------------------------- 8-bit expert products
+FP8, SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
+QBLOCK = 128                # columns of a row (rows and columns of a weight) that share one power-of-two scale
+
+
+def _blocks(v: int) -> int:
+    return (v + QBLOCK - 1) // QBLOCK
+
+
+def quantize_rows(x, offsets=None, out=None, stream=None):
+    """x [rows,d] (float32 or bfloat16) -> (q [rows,d] float8_e4m3fn, scale [rows, ceil(d/128)] float8_e8m0fnu), one
+    power-of-two scale per 128 columns.  With offsets [E+1] only the rows below offsets[E] are quantised."""
+    where = "capmoe_quantize_rows"
+    _need(x.dim() == 2, where, "x [rows,d] expected")
+    rows, d = x.shape
+    q, scale = (None, None) if out is None else out
+    q = _out(where, q, (rows, d), FP8, x)
+    scale = _out(where, scale, (rows, _blocks(d)), SCALE, x)
+    _same_device(where, x, offsets, q, scale)
+    n_rows = ctypes.c_void_p(0) if offsets is None else ctypes.c_void_p(offsets.data_ptr() + 4 * _experts(where, offsets))
+    _check(lib().capmoe_quantize_rows(_ptr(x), n_rows, _i64(rows), int(d), _dt(x), _ptr(q), _ptr(scale), _stream(stream)), where)
+    return q, scale
+
+
+def quantize_weights(w, out=None, stream=None):
+    """w [E,n,d] -> (q [E,n,d] float8_e4m3fn, scale [E, ceil(n/128), ceil(d/128)] float8_e8m0fnu), one scale per
+    128 x 128 block."""
+    where = "capmoe_quantize_weights"
+    _need(w.dim() == 3, where, "w [E,n,d] expected")
+    E, n, d = w.shape
+    q, scale = (None, None) if out is None else out
+    q = _out(where, q, (E, n, d), FP8, w)
+    scale = _out(where, scale, (E, _blocks(n), _blocks(d)), SCALE, w)
+    _same_device(where, w, q, scale)
+    _check(lib().capmoe_quantize_weights(_ptr(w), int(E), int(n), int(d), _dt(w), _ptr(q), _ptr(scale), _stream(stream)), where)
+    return q, scale
+
+
+def _coded(where: str, q, scale, shape, tall: int):
+    want = tuple(shape[:-2]) + (_blocks(shape[-2]) if tall > 1 else shape[-2], _blocks(shape[-1]))
+    _need(q.dtype == FP8 and tuple(q.shape) == tuple(shape) and scale.dtype == SCALE and tuple(scale.shape) == want, where,
+          f"float8_e4m3fn {tuple(shape)} with float8_e8m0fnu scales {want} expected")
+
+
+def grouped_mm_fp8(x_q, x_scale, offsets, w_q, w_scale, y=None, dev_status=None, stream=None):
+    """grouped_mm from 8-bit rows (quantize_rows) and weights (quantize_weights) -> y [rows,n] bfloat16."""
+    where = "capmoe_grouped_mm_fp8"
+    E = _experts(where, offsets)
+    _need(x_q.dim() == 2 and w_q.dim() == 3, where, "x_q [rows,d], w_q [E,n,d] expected")
+    rows, d = x_q.shape
+    n = w_q.shape[1]
+    _coded(where, x_q, x_scale, (rows, d), 1)
+    _coded(where, w_q, w_scale, (E, n, d), QBLOCK)
+    y = _out(where, y, (rows, n), torch.bfloat16, x_q)
+    _same_device(where, x_q, x_scale, offsets, w_q, w_scale, y, dev_status)
+    _check(lib().capmoe_grouped_mm_fp8(_ptr(x_q), _ptr(x_scale), _ptr(offsets), _ptr(w_q), _ptr(w_scale), E, int(d), int(n),
+                                       _ptr(y), _i64(rows), _status(where, dev_status), _stream(stream)), where)
+    return y
+
+
+def ffn_fp8_workspace_bytes(A_max: int, d: int, F: int) -> int:
+    return _bytes("capmoe_ffn_fp8_workspace_bytes", _i64(A_max), int(d), int(F))
+
+
+def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None, dev_status=None, stream=None):
+    """grouped_ffn with 8-bit weights, each a (q, scale) pair of quantize_weights; x_perm [A_max,d] bfloat16 and the
+    hidden rows are quantised on the way -> y_perm [A_max,d] bfloat16."""
+    where = "capmoe_grouped_ffn_fp8"
+    E = _experts(where, offsets)
+    _need(x_perm.dim() == 2 and x_perm.dtype == torch.bfloat16 and w_gate[0].dim() == 3, where,
+          "x_perm [A_max,d] bfloat16 and (q, scale) weights expected")
+    A_max, d = x_perm.shape
+    F = w_gate[0].shape[1]
+    _coded(where, *w_gate, (E, F, d), QBLOCK)
+    _coded(where, *w_up, (E, F, d), QBLOCK)
+    _coded(where, *w_down, (E, d, F), QBLOCK)
+    y_perm = _out(where, y_perm, (A_max, d), torch.bfloat16, x_perm)
+    if ws is None:
+        ws = torch.empty((ffn_fp8_workspace_bytes(A_max, d, F),), device=x_perm.device, dtype=torch.uint8)
+    _same_device(where, x_perm, offsets, *w_gate, *w_up, *w_down, y_perm, ws, dev_status)
+    _check(lib().capmoe_grouped_ffn_fp8(_ptr(x_perm), _ptr(offsets), E, int(d), int(F), _ptr(w_gate[0]), _ptr(w_gate[1]),
+                                        _ptr(w_up[0]), _ptr(w_up[1]), _ptr(w_down[0]), _ptr(w_down[1]), _ptr(y_perm),
+                                        _i64(A_max), _ptr(ws), ctypes.c_size_t(ws.numel()), _status(where, dev_status),
+                                        _stream(stream)), where)
+    return y_perm
+
+
+# ----------------------------------------------------------------------------- expert parallelism
 def ep_plan(slot_row, topk_idx, offsets, E: int, C_local: int, D: int = 1, token_group=None, stream=None):
     """-> (slot_row_ep [N,slots], bad [1]): rows of the [E][C_local] space of an expert-parallel rank."""
     N, slots = slot_row.shape

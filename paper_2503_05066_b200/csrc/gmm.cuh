@@ -1,0 +1,41 @@
+// Internal interface of the grouped products (grouped_mm.cu and the tensor-core files behind it).
+#pragma once
+#include "common.cuh"
+
+namespace capmoe {
+
+constexpr int GMM_MAX_E = 256;               // segments per call (the kernels keep their bounds in shared memory)
+constexpr int QBLOCK = 128;                  // columns (and, for weights, rows) that share one scale
+constexpr int Q_NAN_SCALE = 255;             // scale code of a block that holds a NaN or an infinity
+
+// Rows [seg[e], seg[e+1]) of expert e, clamped to the rows that were allocated.
+struct Segments { const int32_t* offsets; int E; int rows; };
+
+__device__ __forceinline__ int seg_at(const Segments& s, int e) {
+  const int v = s.offsets[e];
+  return v < 0 ? 0 : v > s.rows ? s.rows : v;
+}
+
+// Scale code of a block whose largest magnitude has these fp32 bits: 127 + e with the smallest e such
+// that 448 * 2^e is not below it (448 = 1.75 * 2^8 is the largest e4m3 value), at least 2^-127; an
+// all-zero block has e = 0, and one with a NaN or an infinity the code of a NaN.
+__device__ __forceinline__ uint32_t scale_code(uint32_t amax_bits) {
+  if (amax_bits >= 0x7f800000u) return Q_NAN_SCALE;
+  if (amax_bits == 0u) return 127u;
+  const int c = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return (uint32_t)(c < 0 ? 0 : c);
+}
+// 2^-e of a scale code below 255 (a normal number: codes go up to 247), and 2^e.
+__device__ __forceinline__ float inv_scale(uint32_t code) { return __uint_as_float((254u - code) << 23); }
+__device__ __forceinline__ float scale_value(uint32_t code) {
+  if (code == (uint32_t)Q_NAN_SCALE) return __uint_as_float(0x7fffffffu);
+  return code ? __uint_as_float(code << 23) : __uint_as_float(0x00400000u);
+}
+// Two floats to two e4m3 codes (a in the low byte), round to nearest even; |a|, |b| <= 448 after scaling.
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+}  // namespace capmoe

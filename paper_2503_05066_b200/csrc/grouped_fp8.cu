@@ -1,0 +1,307 @@
+// 8-bit form of the grouped products: e4m3 values with one power-of-two scale per 128 columns of an
+// activation row, or per 128 x 128 block of a weight matrix.
+//   scale 2^e, e the smallest with max|block| <= 448 * 2^e;  q = e4m3(v * 2^-e), round to nearest even
+// The product with a power of two is exact, so a value has one rounding, its own to e4m3 (at most 2^-4 of
+// it), and the codes do not depend on how a division rounds.  A block that holds a NaN or an infinity
+// becomes NaN as a whole.
+// This file: the two quantisers, the host side, and the plain-FMA kernels for sizes the tensor-core
+// kernels do not take.
+#include "gmm_simt.cuh"
+
+namespace capmoe {
+namespace {
+
+constexpr int QN = 256;                    // threads of the quantisers
+
+// eight consecutive elements from p; with VEC they are 16-byte loads, else the first `left` are read
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else if constexpr (VEC) {
+    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ uint32_t amax_bits8(const float (&v)[8]) {
+  uint32_t m = 0;                          // of non-negative floats the larger has the larger pattern; NaN is above all
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(uint8_t* p, int left, const float (&v)[8], uint32_t code) {
+  uint32_t lo, hi;
+  if (code == (uint32_t)Q_NAN_SCALE) {
+    lo = hi = 0x7f7f7f7fu;
+  } else {
+    const float f = inv_scale(code);
+    lo = to_e4m3x2(v[0] * f, v[1] * f) | (to_e4m3x2(v[2] * f, v[3] * f) << 16);
+    hi = to_e4m3x2(v[4] * f, v[5] * f) | (to_e4m3x2(v[6] * f, v[7] * f) << 16);
+  }
+  if constexpr (VEC) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = (uint8_t)((i < 4 ? lo >> (8 * i) : hi >> (8 * (i - 4))) & 0xffu);
+  }
+}
+
+// Rows: half a warp per block of 128 columns, QROW_U blocks per half-warp in flight.
+constexpr int QROW_U = 4;
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(QN)
+k_quantize_rows(const T* __restrict__ x, const int32_t* __restrict__ n_rows, int64_t rows, int d, uint8_t* __restrict__ q,
+                uint8_t* __restrict__ scale) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  const int lane = threadIdx.x & 31, sub = lane & 15;
+  const int nb = (d + QBLOCK - 1) / QBLOCK, per_row = (nb + 2 * QROW_U - 1) / (2 * QROW_U);
+  const int64_t unit = (int64_t)blockIdx.x * (QN / 32) + (threadIdx.x >> 5);
+  const int64_t r = unit / per_row;
+  if (r >= rows || (n_rows && r >= *n_rows)) return;
+  const int b0 = (int)(unit - r * per_row) * 2 * QROW_U + (lane >> 4);
+  float v[QROW_U][8];
+#pragma unroll
+  for (int u = 0; u < QROW_U; ++u) {
+    const int c = (b0 + 2 * u) * QBLOCK + sub * 8;
+    if (c < d) load8<T, VEC>(x + r * d + c, d - c, v[u]);
+    else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < QROW_U; ++u) {
+    const int b = b0 + 2 * u, c = b * QBLOCK + sub * 8;
+    uint32_t m = amax_bits8(v[u]);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const uint32_t code = scale_code(m);
+    if (c < d) store8<VEC>(q + r * d + c, d - c, v[u], code);
+    if (sub == 0 && b < nb) scale[r * nb + b] = (uint8_t)code;
+  }
+}
+
+// Weights: one CTA per 128 x 128 block, the whole block in registers (eight passes of 16 rows).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(QN)
+k_quantize_weights(const T* __restrict__ w, int n, int d, uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ uint32_t part[QN / 32];
+  const int db = (d + QBLOCK - 1) / QBLOCK, nb = (n + QBLOCK - 1) / QBLOCK;
+  const int64_t blk = blockIdx.x;
+  const int jb = (int)(blk % db), ib = (int)(blk / db % nb);
+  const int64_t e = blk / db / nb;
+  const int c = jb * QBLOCK + (threadIdx.x & 15) * 8, r0 = ib * QBLOCK + (threadIdx.x >> 4);
+  const int64_t base = e * n * d;
+  float v[8][8];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 16 * i;
+    if (r < n && c < d) load8<T, VEC>(w + base + (int64_t)r * d + c, d - c, v[i]);
+    else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+    }
+    m = max(m, amax_bits8(v[i]));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < QN / 32; ++i) m = max(m, part[i]);
+  const uint32_t code = scale_code(m);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 16 * i;
+    if (r < n && c < d) store8<VEC>(q + base + (int64_t)r * d + c, d - c, v[i], code);
+  }
+  if (threadIdx.x == 0) scale[blk] = (uint8_t)code;
+}
+
+// y = x W^T from codes; SWIGLU: silu(x W_g^T) * (x W_u^T)
+template <typename TO, bool SWIGLU>
+__global__ void __launch_bounds__(SN)
+k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const uint8_t* __restrict__ w0,
+         const uint8_t* __restrict__ s0, const uint8_t* __restrict__ w1, const uint8_t* __restrict__ s1, TO* __restrict__ out,
+         Segments sg, int K, int Nout) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ SimtTile sm;
+  RowTile t;
+  if (!find_row_tile(sg, blockIdx.x, t)) return;
+  const int col0 = blockIdx.y * ST, kb = (K + QBLOCK - 1) / QBLOCK, nb = (Nout + QBLOCK - 1) / QBLOCK;
+  const Coded<1> la{xq + (int64_t)t.row0 * K, xs + (int64_t)t.row0 * kb, K, kb};
+  const int64_t wo = ((int64_t)t.e * Nout + col0) * K, so = ((int64_t)t.e * nb + col0 / QBLOCK) * kb;
+  float acc[4][4], up[4][4];
+  clear_acc(acc);
+  // (a 64-column tile lies inside one block of 128 weight rows: one row of scales serves it)
+  tile_product(la, Coded<QBLOCK>{w0 + wo, s0 + so, K, kb}, t.rows, Nout - col0, K, sm, acc);
+  if (SWIGLU) {
+    clear_acc(up);
+    tile_product(la, Coded<QBLOCK>{w1 + wo, s1 + so, K, kb}, t.rows, Nout - col0, K, sm, up);
+  }
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = ty * 4 + i, c = col0 + tx * 4 + j;
+      float v = acc[i][j];
+      if (SWIGLU) v = v / (1.0f + expf(-v)) * up[i][j];
+      if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<TO>(v);
+    }
+}
+
+template <typename T>
+int quantize_rows_run(const void* x, const int32_t* n_rows, int64_t rows, int d, void* q, void* scale, cudaStream_t st) {
+  const int64_t units = rows * ceil_div(ceil_div(d, QBLOCK), 2 * QROW_U);
+  const int64_t grid = ceil_div(units, QN / 32);
+  if (grid >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
+  // 16-byte loads of eight columns need rows that start on 16 bytes; the codes' rows then start on 8
+  const bool vec = d % 8 == 0;
+  const int rc = note_cuda(vec ? launch_chained(k_quantize_rows<T, true>, (unsigned)grid, QN, 0, st, (const T*)x, n_rows, rows, d,
+                                                (uint8_t*)q, (uint8_t*)scale)
+                               : launch_chained(k_quantize_rows<T, false>, (unsigned)grid, QN, 0, st, (const T*)x, n_rows, rows,
+                                                d, (uint8_t*)q, (uint8_t*)scale));
+  count_launch(1);
+  return rc;
+}
+
+template <typename T>
+int quantize_weights_run(const void* w, int E, int n, int d, void* q, void* scale, cudaStream_t st) {
+  const int64_t grid = (int64_t)E * ceil_div(n, QBLOCK) * ceil_div(d, QBLOCK);
+  if (grid >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
+  const int rc = note_cuda(d % 8 == 0 ? launch_chained(k_quantize_weights<T, true>, (unsigned)grid, QN, 0, st, (const T*)w, n, d,
+                                                       (uint8_t*)q, (uint8_t*)scale)
+                                      : launch_chained(k_quantize_weights<T, false>, (unsigned)grid, QN, 0, st, (const T*)w, n, d,
+                                                       (uint8_t*)q, (uint8_t*)scale));
+  count_launch(1);
+  return rc;
+}
+
+template <class... KArgs, class... Args>
+int launch_tiles(void (*kernel)(KArgs...), const Segments& sg, int cols, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(ceil_div(sg.rows, ST) + sg.E), (unsigned)ceil_div(cols, ST));
+  cfg.blockDim = dim3(SN);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const int rc = note_cuda(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
+  count_launch(1);
+  return rc;
+}
+
+int check_shape(const int32_t* offsets, int E, int d, int n, int64_t rows) {
+  if (E < 1 || d < 1 || n < 1 || rows < 0 || !offsets) return CAPMOE_EINVAL;
+  if (E > GMM_MAX_E || rows >= ((int64_t)1 << 31) || ceil_div(d, ST) > 65535 || ceil_div(n, ST) > 65535)
+    return CAPMOE_EUNSUPPORTED;
+  return CAPMOE_OK;
+}
+template <class... P>
+bool usable(P... p) {
+  return ((p != nullptr && aligned16(p)) && ...);
+}
+
+// Workspace of the 8-bit FFN: codes and scales of x and of the hidden rows, and (sizes without a
+// tensor-core kernel) the hidden rows in fp32.
+struct FfnWs { size_t xq, xs, hq, hs, h, total; };
+FfnWs ffn_ws(int64_t A_max, int d, int F) {
+  auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+  const size_t A = (size_t)A_max;
+  FfnWs w;
+  w.xq = 0;
+  w.xs = w.xq + up(A * d);
+  w.hq = w.xs + up(A * ceil_div(d, QBLOCK));
+  w.hs = w.hq + up(A * F);
+  w.h = w.hs + up(A * ceil_div(F, QBLOCK));
+  w.total = w.h + up(A * F * 4) + 256;
+  return w;
+}
+
+}  // namespace
+}  // namespace capmoe
+
+using namespace capmoe;
+
+extern "C" int capmoe_quantize_rows(const void* x, const int32_t* n_rows, int64_t rows, int d, int dtype, void* q, void* scale,
+                                    void* stream) {
+  if (rows < 0 || d < 1) return CAPMOE_EINVAL;
+  if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
+  if (rows >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
+  if (rows == 0) return CAPMOE_OK;
+  if (!usable(x, q) || !scale) return CAPMOE_EINVAL;
+  if (dtype == CAPMOE_F32) return quantize_rows_run<float>(x, n_rows, rows, d, q, scale, as_stream(stream));
+  return quantize_rows_run<__nv_bfloat16>(x, n_rows, rows, d, q, scale, as_stream(stream));
+}
+
+extern "C" int capmoe_quantize_weights(const void* w, int E, int n, int d, int dtype, void* q, void* scale, void* stream) {
+  if (E < 1 || n < 1 || d < 1) return CAPMOE_EINVAL;
+  if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
+  if (!usable(w, q) || !scale) return CAPMOE_EINVAL;
+  if (dtype == CAPMOE_F32) return quantize_weights_run<float>(w, E, n, d, q, scale, as_stream(stream));
+  return quantize_weights_run<__nv_bfloat16>(w, E, n, d, q, scale, as_stream(stream));
+}
+
+extern "C" int capmoe_grouped_mm_fp8(const void* x_q, const void* x_scale, const int32_t* expert_offsets, const void* w_q,
+                                     const void* w_scale, int E, int d, int n, void* y, int64_t rows, int32_t* dev_status,
+                                     void* stream) {
+  const int rc = check_shape(expert_offsets, E, d, n, rows);
+  if (rc != CAPMOE_OK || rows == 0) return rc;
+  if (!usable(x_q, w_q, y) || !x_scale || !w_scale) return CAPMOE_EINVAL;
+  const Segments sg{expert_offsets, E, (int)rows};
+  (void)dev_status;
+  const uint8_t* none = nullptr;
+  return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, n, as_stream(stream), (const uint8_t*)x_q, (const uint8_t*)x_scale,
+                      (const uint8_t*)w_q, (const uint8_t*)w_scale, none, none, (__nv_bfloat16*)y, sg, d, n);
+}
+
+extern "C" int capmoe_ffn_fp8_workspace_bytes(int64_t A_max, int d, int F, size_t* bytes) {
+  if (!bytes || A_max < 0 || d < 1 || F < 1) return CAPMOE_EINVAL;
+  *bytes = ffn_ws(A_max, d, F).total;
+  return CAPMOE_OK;
+}
+
+extern "C" int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_offsets, int E, int d, int F, const void* wg_q,
+                                      const void* wg_scale, const void* wu_q, const void* wu_scale, const void* wd_q,
+                                      const void* wd_scale, void* y_perm, int64_t A_max, void* ws, size_t ws_bytes,
+                                      int32_t* dev_status, void* stream) {
+  int rc = check_shape(expert_offsets, E, d, F, A_max);
+  if (rc != CAPMOE_OK || A_max == 0) return rc;
+  if (!usable(x_perm, wg_q, wu_q, wd_q, y_perm, ws) || !wg_scale || !wu_scale || !wd_scale) return CAPMOE_EINVAL;
+  const FfnWs w = ffn_ws(A_max, d, F);
+  if (ws_bytes < w.total) return CAPMOE_EWORKSPACE;
+  const Segments sg{expert_offsets, E, (int)A_max};
+  (void)dev_status;
+  cudaStream_t st = as_stream(stream);
+  uint8_t* b = (uint8_t*)ws;
+  rc = quantize_rows_run<__nv_bfloat16>(x_perm, expert_offsets + E, A_max, d, b + w.xq, b + w.xs, st);
+  if (rc != CAPMOE_OK) return rc;
+  float* h = (float*)(b + w.h);
+  rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, b + w.xq, b + w.xs, (const uint8_t*)wg_q, (const uint8_t*)wg_scale,
+                    (const uint8_t*)wu_q, (const uint8_t*)wu_scale, h, sg, d, F);
+  if (rc != CAPMOE_OK) return rc;
+  rc = quantize_rows_run<float>(h, expert_offsets + E, A_max, F, b + w.hq, b + w.hs, st);
+  if (rc != CAPMOE_OK) return rc;
+  const uint8_t* none = nullptr;
+  return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, d, st, b + w.hq, b + w.hs, (const uint8_t*)wd_q,
+                      (const uint8_t*)wd_scale, none, none, (__nv_bfloat16*)y_perm, sg, F, d);
+}

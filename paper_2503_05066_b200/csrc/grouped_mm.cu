@@ -1,0 +1,285 @@
+// Grouped products of expert-major rows with per-expert weights, and their gradients: host side, and the
+// plain-FMA kernels for fp32 storage and for sizes the tensor-core kernels do not take.
+//   forward    y[r]   = W[e] x[r]
+//   dx         dx[r]  = W[e]^T dy[r]
+//   dw         dW[e]  = sum over the rows r of expert e of dy[r] x[r]^T
+//   backward of the SwiGLU FFN: g = W_g x, u = W_u x, dh = W_d^T dy, p = sigmoid(g), then
+//              dg = dh u p (1 + g (1 - p)), du = dh g p, h = g p u and the products of those with x, dy and
+//              the weights.
+// All sums are fp32; one rounding to the storage type at each stored matrix.
+#include "gmm_simt.cuh"
+
+namespace capmoe {
+namespace {
+
+enum { DIR_FWD = 0, DIR_DX = 1 };
+
+template <typename T, int DIR>
+__global__ void __launch_bounds__(SN)
+k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out, Segments sg, int K, int Nout) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ SimtTile sm;
+  RowTile t;
+  if (!find_row_tile(sg, blockIdx.x, t)) return;
+  const int col0 = blockIdx.y * ST;
+  const T* We = W + (int64_t)t.e * Nout * K;
+  float acc[4][4];
+  clear_acc(acc);
+  const Dense<T, true> la{A + (int64_t)t.row0 * K, K};
+  if (DIR == DIR_FWD) tile_product(la, Dense<T, true>{We + (int64_t)col0 * K, K}, t.rows, Nout - col0, K, sm, acc);
+  else tile_product(la, Dense<T, false>{We + col0, Nout}, t.rows, Nout - col0, K, sm, acc);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = ty * 4 + i, c = col0 + tx * 4 + j;
+      if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<T>(acc[i][j]);
+    }
+}
+
+// Up to three weight gradients of one set of segments in one launch (blockIdx.z = product * E + expert):
+// product p is P[p]^T Q[p] with P [rows, M[p]] and Q [rows, N[p]].
+template <typename T, typename TO>
+struct DwSet { const T* P[3]; const T* Q[3]; TO* out[3]; int M[3], N[3]; };
+
+template <typename T, typename TO>
+__global__ void __launch_bounds__(SN) k_mm_dw(DwSet<T, TO> s, Segments sg) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ SimtTile sm;
+  const int p = blockIdx.z / sg.E, e = blockIdx.z - p * sg.E;
+  const int M = s.M[p], N = s.N[p];
+  const int r0 = blockIdx.x * ST, c0 = blockIdx.y * ST;
+  if (r0 >= M || c0 >= N) return;
+  const int begin = seg_at(sg, e), n = seg_at(sg, e + 1) - begin;
+  float acc[4][4];
+  clear_acc(acc);
+  tile_product(Dense<T, false>{s.P[p] + (int64_t)begin * M + r0, M}, Dense<T, false>{s.Q[p] + (int64_t)begin * N + c0, N},
+               M - r0, N - c0, n, sm, acc);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = r0 + ty * 4 + i, c = c0 + tx * 4 + j;
+      if (r < M && c < N) s.out[p][((int64_t)e * M + r) * N + c] = from_float<TO>(acc[i][j]);
+    }
+}
+
+// dg, du and h of the SwiGLU backward pass: three products over d with the elementwise part in registers.
+template <typename T>
+__global__ void __launch_bounds__(SN)
+k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __restrict__ wg, const T* __restrict__ wu,
+                  const T* __restrict__ wd, T* __restrict__ dg, T* __restrict__ du, T* __restrict__ h, Segments sg, int d,
+                  int F) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ SimtTile sm;
+  RowTile t;
+  if (!find_row_tile(sg, blockIdx.x, t)) return;
+  const int col0 = blockIdx.y * ST, cols = F - col0;
+  const int64_t we = (int64_t)t.e * F * d;
+  const Dense<T, true> lx{x + (int64_t)t.row0 * d, d}, ldy{dy + (int64_t)t.row0 * d, d};
+  float g[4][4], u[4][4], dh[4][4];
+  clear_acc(g); clear_acc(u); clear_acc(dh);
+  tile_product(lx, Dense<T, true>{wg + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, g);
+  tile_product(lx, Dense<T, true>{wu + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, u);
+  tile_product(ldy, Dense<T, false>{wd + we + col0, F}, t.rows, cols, d, sm, dh);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = ty * 4 + i, c = col0 + tx * 4 + j;
+      if (r >= t.rows || c >= F) continue;
+      const float p = 1.0f / (1.0f + expf(-g[i][j]));
+      const float a = g[i][j] * p;
+      const int64_t o = (int64_t)(t.row0 + r) * F + c;
+      dg[o] = from_float<T>(dh[i][j] * u[i][j] * (p + a * (1.0f - p)));
+      du[o] = from_float<T>(dh[i][j] * a);
+      h[o] = from_float<T>(a * u[i][j]);
+    }
+}
+
+// dx = dg W_g + du W_u (weights [E, F, d])
+template <typename T>
+__global__ void __launch_bounds__(SN)
+k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __restrict__ wg, const T* __restrict__ wu,
+             T* __restrict__ dx, Segments sg, int d, int F) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ SimtTile sm;
+  RowTile t;
+  if (!find_row_tile(sg, blockIdx.x, t)) return;
+  const int col0 = blockIdx.y * ST;
+  const int64_t we = (int64_t)t.e * F * d + col0;
+  float acc[4][4];
+  clear_acc(acc);
+  tile_product(Dense<T, true>{dg + (int64_t)t.row0 * F, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, F, sm, acc);
+  tile_product(Dense<T, true>{du + (int64_t)t.row0 * F, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, F, sm, acc);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = ty * 4 + i, c = col0 + tx * 4 + j;
+      if (r < t.rows && c < d) dx[(int64_t)(t.row0 + r) * d + c] = from_float<T>(acc[i][j]);
+    }
+}
+
+int launched(cudaError_t err) {
+  count_launch(1);
+  return note_cuda(err);
+}
+
+template <class... KArgs, class... Args>
+int launch_tiles(void (*kernel)(KArgs...), dim3 grid, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(SN);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return launched(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
+}
+
+dim3 row_grid(const Segments& sg, int cols) {       // every segment rounds up to whole tiles
+  return dim3((unsigned)(ceil_div(sg.rows, ST) + sg.E), (unsigned)ceil_div(cols, ST));
+}
+
+template <typename T, int DIR>
+int rows_simt(const void* a, const void* w, void* out, const Segments& sg, int K, int Nout, cudaStream_t st) {
+  return launch_tiles(k_mm_rows<T, DIR>, row_grid(sg, Nout), st, (const T*)a, (const T*)w, (T*)out, sg, K, Nout);
+}
+
+template <typename T, typename TO>
+int dw_simt(const DwSet<T, TO>& s, int count, const Segments& sg, cudaStream_t st) {
+  int M = 0, N = 0;
+  for (int p = 0; p < count; ++p) { M = s.M[p] > M ? s.M[p] : M; N = s.N[p] > N ? s.N[p] : N; }
+  return launch_tiles(k_mm_dw<T, TO>, dim3((unsigned)ceil_div(M, ST), (unsigned)ceil_div(N, ST), (unsigned)(count * sg.E)), st,
+                      s, sg);
+}
+
+template <typename T>
+int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
+                  const void* wd, void* dx, void* dwg, void* dwu, void* dwd, void* ws, cudaStream_t st) {
+  T* dg = (T*)ws;
+  T* du = dg + (int64_t)sg.rows * F;
+  T* h = du + (int64_t)sg.rows * F;
+  int rc = launch_tiles(k_ffn_grad_hidden<T>, row_grid(sg, F), st, (const T*)x, (const T*)dy, (const T*)wg, (const T*)wu,
+                        (const T*)wd, dg, du, h, sg, d, F);
+  if (rc != CAPMOE_OK) return rc;
+  rc = launch_tiles(k_ffn_grad_x<T>, row_grid(sg, d), st, (const T*)dg, (const T*)du, (const T*)wg, (const T*)wu, (T*)dx, sg,
+                    d, F);
+  if (rc != CAPMOE_OK) return rc;
+  DwSet<T, T> s = {{dg, du, (const T*)dy}, {(const T*)x, (const T*)x, h}, {(T*)dwg, (T*)dwu, (T*)dwd}, {F, F, d}, {d, d, F}};
+  return dw_simt(s, 3, sg, st);
+}
+
+// Checks common to the grouped products.  CAPMOE_OK, or the status to return before anything is enqueued.
+int check_shape(const int32_t* offsets, int E, int d, int n, int dtype, int64_t rows) {
+  if (E < 1 || d < 1 || n < 1 || rows < 0 || !offsets) return CAPMOE_EINVAL;
+  if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
+  if (E > GMM_MAX_E || rows >= ((int64_t)1 << 31) || ceil_div(d, ST) > 65535 || ceil_div(n, ST) > 65535)
+    return CAPMOE_EUNSUPPORTED;
+  return CAPMOE_OK;
+}
+template <class... P>
+bool usable(P... p) {                       // every pointer there and 16-byte aligned
+  return ((p != nullptr && aligned16(p)) && ...);
+}
+size_t align256(size_t b) { return (b + 255) / 256 * 256; }
+
+}  // namespace
+}  // namespace capmoe
+
+using namespace capmoe;
+
+extern "C" int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n,
+                                 int dtype, void* y, int64_t rows, int32_t* dev_status, void* stream) {
+  const int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
+  if (rc != CAPMOE_OK || rows == 0) return rc;
+  if (!usable(x_rows, w, y)) return CAPMOE_EINVAL;
+  const Segments sg{expert_offsets, E, (int)rows};
+  (void)dev_status;
+  if (dtype == CAPMOE_F32) return rows_simt<float, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
+  return rows_simt<__nv_bfloat16, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
+}
+
+extern "C" int capmoe_grouped_mm_dx(const void* dy_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n,
+                                    int dtype, void* dx, int64_t rows, int32_t* dev_status, void* stream) {
+  const int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
+  if (rc != CAPMOE_OK || rows == 0) return rc;
+  if (!usable(dy_rows, w, dx)) return CAPMOE_EINVAL;
+  const Segments sg{expert_offsets, E, (int)rows};
+  (void)dev_status;
+  if (dtype == CAPMOE_F32) return rows_simt<float, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
+  return rows_simt<__nv_bfloat16, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
+}
+
+extern "C" int capmoe_grouped_mm_dw_workspace_bytes(int E, size_t* bytes) {
+  if (!bytes || E < 1) return CAPMOE_EINVAL;
+  *bytes = 256;
+  return CAPMOE_OK;
+}
+
+extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, const int32_t* expert_offsets, int E, int d,
+                                    int n, int dtype, int out_dtype, void* dw, int64_t rows, void* ws, size_t ws_bytes,
+                                    int32_t* dev_status, void* stream) {
+  const int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
+  if (rc != CAPMOE_OK) return rc;
+  if (out_dtype != CAPMOE_F32 && out_dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
+  if (dtype == CAPMOE_F32 && out_dtype != CAPMOE_F32) return CAPMOE_EUNSUPPORTED;
+  if (!usable(dw)) return CAPMOE_EINVAL;
+  if (rows == 0) return note_cuda(cudaMemsetAsync(dw, 0, (size_t)E * n * d * elt_size(out_dtype), as_stream(stream)));
+  if (!usable(dy_rows, x_rows, ws)) return CAPMOE_EINVAL;
+  size_t need = 0;
+  capmoe_grouped_mm_dw_workspace_bytes(E, &need);
+  if (ws_bytes < need) return CAPMOE_EWORKSPACE;
+  const Segments sg{expert_offsets, E, (int)rows};
+  (void)dev_status;
+  cudaStream_t st = as_stream(stream);
+  if (dtype == CAPMOE_F32)
+    return dw_simt(DwSet<float, float>{{(const float*)dy_rows}, {(const float*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
+  using B = __nv_bfloat16;
+  if (out_dtype == CAPMOE_F32)
+    return dw_simt(DwSet<B, float>{{(const B*)dy_rows}, {(const B*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
+  return dw_simt(DwSet<B, B>{{(const B*)dy_rows}, {(const B*)x_rows}, {(B*)dw}, {n}, {d}}, 1, sg, st);
+}
+
+extern "C" int capmoe_ffn_backward_workspace_bytes(int64_t A_max, int E, int F, int dtype, size_t* bytes) {
+  if (!bytes || A_max < 0 || E < 1 || F < 1) return CAPMOE_EINVAL;
+  if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
+  *bytes = align256((size_t)A_max * (size_t)F * elt_size(dtype) * 3) + 256;
+  return CAPMOE_OK;
+}
+
+extern "C" int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_perm, const int32_t* expert_offsets, int E,
+                                           int d, int F, int dtype, const void* w_gate, const void* w_up,
+                                           const void* w_down, void* dx_perm, void* dw_gate, void* dw_up, void* dw_down,
+                                           int64_t A_max, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  int rc = check_shape(expert_offsets, E, d, F, dtype, A_max);
+  if (rc != CAPMOE_OK) return rc;
+  if (!usable(dw_gate, dw_up, dw_down)) return CAPMOE_EINVAL;
+  cudaStream_t st = as_stream(stream);
+  if (A_max == 0) {
+    for (void* dw : {dw_gate, dw_up, dw_down})
+      if ((rc = note_cuda(cudaMemsetAsync(dw, 0, (size_t)E * F * d * elt_size(dtype), st))) != CAPMOE_OK) return rc;
+    return CAPMOE_OK;
+  }
+  if (!usable(x_perm, dy_perm, w_gate, w_up, w_down, dx_perm, ws)) return CAPMOE_EINVAL;
+  size_t need = 0;
+  capmoe_ffn_backward_workspace_bytes(A_max, E, F, dtype, &need);
+  if (ws_bytes < need) return CAPMOE_EWORKSPACE;
+  const Segments sg{expert_offsets, E, (int)A_max};
+  (void)dev_status;
+  if (dtype == CAPMOE_F32)
+    return ffn_grad_simt<float>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws, st);
+  return ffn_grad_simt<__nv_bfloat16>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws,
+                                      st);
+}
