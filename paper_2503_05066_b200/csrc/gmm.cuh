@@ -38,4 +38,16 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
   return r;
 }
 
+// Tensor-core kernels (gmm_tc.cu): bf16 with rows of whole 16-byte vectors.  All matrices 16-byte aligned, map_ws
+// 128-byte aligned with gmm_tc_map_bytes(E, lists) bytes (dw: 2 lists, ffn_grad: 5).
+bool gmm_tc_supported(int E, int d, int n, int dtype);
+size_t gmm_tc_map_bytes(int E, int lists);
+int gmm_tc_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, cudaStream_t st);
+int gmm_tc_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, cudaStream_t st);
+int gmm_tc_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws,
+              int32_t* dev_status, cudaStream_t st);
+int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
+                    const void* wd, void* dx, void* dwg, void* dwu, void* dwd, void* map_ws, void* hidden, int32_t* dev_status,
+                    cudaStream_t st);
+
 }  // namespace capmoe

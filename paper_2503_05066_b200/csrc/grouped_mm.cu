@@ -194,6 +194,7 @@ bool usable(P... p) {                       // every pointer there and 16-byte a
   return ((p != nullptr && aligned16(p)) && ...);
 }
 size_t align256(size_t b) { return (b + 255) / 256 * 256; }
+void* align256(void* p) { return (void*)align256((size_t)p); }
 
 }  // namespace
 }  // namespace capmoe
@@ -206,7 +207,7 @@ extern "C" int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offse
   if (rc != CAPMOE_OK || rows == 0) return rc;
   if (!usable(x_rows, w, y)) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
-  (void)dev_status;
+  if (gmm_tc_supported(E, d, n, dtype)) return gmm_tc_fwd(x_rows, sg, w, d, n, y, dev_status, as_stream(stream));
   if (dtype == CAPMOE_F32) return rows_simt<float, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
   return rows_simt<__nv_bfloat16, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
 }
@@ -217,14 +218,14 @@ extern "C" int capmoe_grouped_mm_dx(const void* dy_rows, const int32_t* expert_o
   if (rc != CAPMOE_OK || rows == 0) return rc;
   if (!usable(dy_rows, w, dx)) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
-  (void)dev_status;
+  if (gmm_tc_supported(E, d, n, dtype)) return gmm_tc_dx(dy_rows, sg, w, d, n, dx, dev_status, as_stream(stream));
   if (dtype == CAPMOE_F32) return rows_simt<float, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
   return rows_simt<__nv_bfloat16, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
 }
 
 extern "C" int capmoe_grouped_mm_dw_workspace_bytes(int E, size_t* bytes) {
   if (!bytes || E < 1) return CAPMOE_EINVAL;
-  *bytes = 256;
+  *bytes = gmm_tc_map_bytes(E, 2) + 256;                     // 256: to align the maps
   return CAPMOE_OK;
 }
 
@@ -242,8 +243,9 @@ extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, con
   capmoe_grouped_mm_dw_workspace_bytes(E, &need);
   if (ws_bytes < need) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)rows};
-  (void)dev_status;
   cudaStream_t st = as_stream(stream);
+  if (gmm_tc_supported(E, d, n, dtype))
+    return gmm_tc_dw(dy_rows, x_rows, sg, d, n, out_dtype == CAPMOE_F32, dw, align256(ws), dev_status, st);
   if (dtype == CAPMOE_F32)
     return dw_simt(DwSet<float, float>{{(const float*)dy_rows}, {(const float*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
   using B = __nv_bfloat16;
@@ -255,7 +257,7 @@ extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, con
 extern "C" int capmoe_ffn_backward_workspace_bytes(int64_t A_max, int E, int F, int dtype, size_t* bytes) {
   if (!bytes || A_max < 0 || E < 1 || F < 1) return CAPMOE_EINVAL;
   if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
-  *bytes = align256((size_t)A_max * (size_t)F * elt_size(dtype) * 3) + 256;
+  *bytes = (size_t)A_max * (size_t)F * elt_size(dtype) * 3 + align256(gmm_tc_map_bytes(E, 5)) + 256;
   return CAPMOE_OK;
 }
 
@@ -277,7 +279,10 @@ extern "C" int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_pe
   capmoe_ffn_backward_workspace_bytes(A_max, E, F, dtype, &need);
   if (ws_bytes < need) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)A_max};
-  (void)dev_status;
+  uint8_t* maps = (uint8_t*)align256(ws);
+  if (gmm_tc_supported(E, d, F, dtype))
+    return gmm_tc_ffn_grad(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, maps,
+                           maps + align256(gmm_tc_map_bytes(E, 5)), dev_status, st);
   if (dtype == CAPMOE_F32)
     return ffn_grad_simt<float>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws, st);
   return ffn_grad_simt<__nv_bfloat16>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws,
