@@ -50,4 +50,12 @@ int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, in
                     const void* wd, void* dx, void* dwg, void* dwu, void* dwd, void* map_ws, void* hidden, int32_t* dev_status,
                     cudaStream_t st);
 
+// Block-scaled 8-bit kernels (gmm_fp8_tc.cu): d and n (F) multiples of 16.  `sched`: a zeroed tile counter or NULL.
+bool gmm8_tc_supported(int d, int n);
+int gmm8_tc(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
+            int32_t* dev_status, int32_t* sched, cudaStream_t st);
+int gmm8_tc_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                   const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+                   int32_t* sched, cudaStream_t st);
+
 }  // namespace capmoe

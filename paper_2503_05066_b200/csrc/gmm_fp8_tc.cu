@@ -1,0 +1,406 @@
+// 8-bit grouped products on tcgen05's block-scaled MMA (kind::mxf8f6f4): e4m3 codes, power-of-two scales per 128
+// columns of a row and per 128 x 128 block of a weight, applied by the tensor cores, fp32 accumulation.
+//   PLAIN    y[r]   = W[e] x[r]                                    bf16
+//   SWIGLU   h[r]   = silu(W_g[e] x[r]) * (W_u[e] x[r])            quantised: codes and scales
+// Persistent kernel over CTA pairs, 256 x 256 tiles, the structure of k_gmm2 with one more warp that stages scale words
+// (see gmm_tc.cuh).  SWIGLU puts 128 gate and 128 up columns of the same hidden columns into a tile, which is one
+// block of 128 hidden columns per row: its largest magnitude meets between the two threads that share a row, and the
+// hidden row leaves the kernel as codes, never as fp32.
+// Tensor memory: two accumulators of 256 columns and three groups of scales do not fit 512 columns, so the
+// accumulators overlap by 64 columns ([0,256) and [192,448)); an epilogue reads the shared columns first and lets the
+// next tile's MMAs start then, with most of its own columns still to convert.
+// What bounds it: the tensor pipe.
+#include "gmm.cuh"
+#include "gmm_tc.cuh"
+
+namespace capmoe {
+namespace {
+
+enum { PLAIN = 0, SWIGLU = 1 };
+constexpr int NST8 = 6;
+constexpr int STAGE8 = 2 * A_BYTES;                       // 128 rows of A, 128 rows of B: 32 KB
+constexpr int STG8_OFF = NST8 * STAGE8;
+constexpr int SF_OFF = STG8_OFF + EPI_WARPS * STG_WARP_BYTES;
+constexpr int SF_SLOT = 3 * SF_CHUNK;                     // A rows, B rows 0..127, B rows 128..255
+constexpr int TAIL8 = SF_OFF + SF_RING * SF_SLOT;
+constexpr int SMEM8 = TAIL8 + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + 2 * 2 * 128 * 4;
+static_assert(SMEM8 <= 227 * 1024, "shared memory of a thread block");
+constexpr int ACC_STEP = 192;                             // columns between the two accumulators
+constexpr int OVERLAP = 64;
+
+struct F8Args {
+  Segments sg;
+  int K, Nout;
+  const uint8_t *xs, *s0, *s1;      // scales of the rows, of W (W_g) and of W_u
+  void* out;                        // bf16 y, or codes of h
+  uint8_t* out_scale;               // SWIGLU
+  int32_t* dev_status;
+  int32_t* sched;
+};
+struct F8Maps { CUtensorMap a, b0, b1, o; };
+
+template <int EPI>
+__global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ F8Maps mp, const __grid_constant__ F8Args ar) {
+  constexpr int N_TILE = EPI == SWIGLU ? 128 : 256, BM2 = 2 * BM;
+  allow_next_kernel();
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (tiles - raw);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen + TAIL8);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 52);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* offs = reinterpret_cast<int*>(gen + TAIL8 + 512);
+  int* ends = offs + (GMM_MAX_E + 1);
+  int* tile_start = ends + (GMM_MAX_E + 1);
+  uint32_t* row_max = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 4);   // [2 tiles][2 halves][128 rows]
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_ctarank();
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * (uint32_t)s; };                 // 0..5
+  auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(8 + s); };
+  auto tfull_bar = [&](int b) { return bar0 + 8u * (uint32_t)(16 + b); };
+  auto tempty_bar = [&](int b) { return bar0 + 8u * (uint32_t)(18 + b); };
+  auto shared_bar = [&](int b) { return bar0 + 8u * (uint32_t)(20 + b); };        // the overlap columns have been read
+  auto sfull_bar = [&](int r) { return bar0 + 8u * (uint32_t)(24 + r); };
+  auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(28 + r); };
+  const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
+
+  if (tid == 0) {
+    for (int s = 0; s < NST8; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull_bar(b), 1);
+      mbar_init(tempty_bar(b), 2 * EPI_WARPS * 32);
+      mbar_init(shared_bar(b), EPI_WARPS * 32);                 // one half of the warps of each CTA
+    }
+    for (int r = 0; r < SF_RING; ++r) { mbar_init(sfull_bar(r), 2); mbar_init(sempty_bar(r), 1); }
+    for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), TQ_READERS_F8); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  wait_for_previous_kernel();
+  const int E = ar.sg.E;
+  for (int i = tid; i < E; i += F8_THREADS) { offs[i] = seg_at(ar.sg, i); ends[i] = max(offs[i], seg_at(ar.sg, i + 1)); }
+  __syncthreads();
+  if (warp == 0) {
+    const int n_blocks = (ar.Nout + N_TILE - 1) / N_TILE;
+    int carry = 0;
+    for (int e0 = 0; e0 < E; e0 += 32) {
+      const int e = e0 + lane;
+      const int mine = e < E ? ((ends[e] - offs[e] + BM2 - 1) / BM2) * n_blocks : 0;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
+      if (e < E) tile_start[e] = carry + upto - mine;
+      carry += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) tile_start[E] = carry;
+  }
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const int tile_hi = tile_start[E];
+  const bool dyn = ar.sched != nullptr;
+  auto next_tile = [&](int j, bool whole_warp) -> int {
+    if (!dyn) { const int tile = pair + j * npairs; return tile < tile_hi ? tile : -1; }
+    return tq.get(j, whole_warp);
+  };
+  auto locate = [&](int tile, int& cursor, Tile& t) {
+    return locate_tile(tile, cursor, tile_start, offs, ends, E, N_TILE, BM2, t);
+  };
+  const int num_kb = (ar.K + QBLOCK - 1) / QBLOCK;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer (both CTAs)
+    if (elect_one()) {
+      int cursor = 0, s = 0;
+      uint32_t ph = 0;
+      Tile t;
+      bool ok = true;
+      const bool scheduler = dyn && rank == 0;
+      int cur = -1, claim = 0;
+      if (scheduler) {
+        cur = atomicAdd(ar.sched, 1);
+        if (cur >= tile_hi) cur = -1;
+        ok = tq.put(0, cur);
+        if (ok && cur >= 0) claim = atomicAdd(ar.sched, 1);
+      }
+      const int pub_kb = num_kb / 2;
+      for (int j = 0; ok; ++j) {
+        const int tile = scheduler ? cur : next_tile(j, false);
+        if (tile < 0 || !locate(tile, cursor, t)) break;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (scheduler && kb == pub_kb) {
+            cur = claim < tile_hi ? claim : -1;
+            if (!tq.put(j + 1, cur)) { ok = false; break; }
+            if (cur >= 0) claim = atomicAdd(ar.sched, 1);
+          }
+          if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t bar = full_bar(s) & PEER_MASK;
+          if (rank == 0) mbar_expect_tx(full_bar(s), 2 * STAGE8);
+          const uint32_t a_dst = tiles + (uint32_t)s * STAGE8;
+          tma2_load_2d(a_dst, &mp.a, kb * QBLOCK, t.row0 + (int)rank * BM, bar);
+          if (EPI == SWIGLU) tma2_load_3d(a_dst + A_BYTES, rank == 0 ? &mp.b0 : &mp.b1, kb * QBLOCK, t.n0, t.e, bar);
+          else tma2_load_3d(a_dst + A_BYTES, &mp.b0, kb * QBLOCK, t.n0 + (int)rank * 128, t.e, bar);
+          if (++s == NST8) { s = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (leader CTA only)
+    if (rank == 0 && elect_one()) {
+      int cursor = 0, s = 0, r = 0;
+      uint32_t it = 0, ph = 0, rph = 0;
+      const uint32_t idesc0 = f8_idesc(256);
+      const uint64_t a0 = umma_desc(tiles), b0 = umma_desc(tiles + A_BYTES);
+      uint64_t off = 0;
+      Tile t;
+      bool ok = true;
+      for (int j = 0; ok; ++j, ++it) {
+        const int tile = next_tile(j, false);
+        if (tile < 0 || !locate(tile, cursor, t)) break;
+        const uint32_t b = it & 1u, use = it >> 1;
+        // this accumulator has been converted, and the one before it has been read where the two overlap
+        if (!mbar_wait(tempty_bar(b), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        if (it > 0 && !mbar_wait(shared_bar(b ^ 1u), ((it - 1) >> 1) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d = tmem_base + b * (uint32_t)ACC_STEP;
+        uint32_t sf = 0;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if ((kb & 3) == 0) {
+            if (!mbar_wait(sfull_bar(r), rph, abort_flag)) { ok = false; break; }
+            fence_acquire_cluster();
+            tc_fence_after();
+            sf = tmem_base + (uint32_t)(SF_TMEM + r * SF_COLS);
+            const uint32_t src = tiles + SF_OFF + (uint32_t)(r * SF_SLOT);
+            copy_scales(sf + 8u, src);                          // A rows
+            copy_scales(sf, src + SF_CHUNK);                    // B rows 0..127
+            copy_scales(sf + 4u, src + 2 * SF_CHUNK);           // B rows 128..255
+          }
+          if (!mbar_wait(full_bar(s), ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t idesc = idesc0 | f8_scale_byte(kb);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma2_f8(d, a0 + off + 2 * k, b0 + off + 2 * k, idesc, sf + 8u, sf, (kb | k) != 0 ? 1u : 0u);
+          umma2_commit_both(empty_bar(s));
+          if ((kb & 3) == 3 || kb == num_kb - 1) {              // the group's last k-block: its words may be replaced
+            umma2_commit_both(sempty_bar(r));
+            if (++r == SF_RING) { r = 0; rph ^= 1u; }
+          }
+          off += (uint64_t)(STAGE8 >> 4);
+          if (++s == NST8) { s = 0; ph ^= 1u; off = 0; }
+        }
+        if (ok) umma2_commit_both(tfull_bar(b));
+      }
+    }
+  } else if (warp == 2 + EPI_WARPS) {
+    // ------------------------------------------------------------ scales (both CTAs)
+    int cursor = 0, r = 0;
+    uint32_t rph = 0;
+    Tile t;
+    bool ok = true;
+    const int nb = num_kb, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
+    const bool words = (nb & 3) == 0 &&                          // rows of scales start on words
+                       (((uintptr_t)ar.xs | (uintptr_t)ar.s0 | (uintptr_t)ar.s1) & 3u) == 0;
+    for (int j = 0; ok; ++j) {
+      const int tile = next_tile(j, true);
+      if (tile < 0 || !locate(tile, cursor, t)) break;
+      const uint8_t* rows[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = min(t.row0 + (int)rank * BM + lane + 32 * i, ar.sg.rows - 1);   // rows past the tile: any scale
+        rows[i] = ar.xs + (int64_t)row * nb;
+      }
+      const int blk = t.n0 / QBLOCK;
+      const uint8_t* w0 = ar.s0 + ((int64_t)t.e * wb + blk) * nb;
+      const uint8_t* w1 = EPI == SWIGLU ? ar.s1 + ((int64_t)t.e * wb + blk) * nb
+                                        : ar.s0 + ((int64_t)t.e * wb + min(blk + 1, wb - 1)) * nb;
+      for (int k = 0; k < nb; k += 4) {
+        uint32_t a[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = scale_word(rows[i], k, nb, words);
+        const uint32_t b = scale_word(w0, k, nb, words), c = scale_word(w1, k, nb, words);
+        bool free_slot = mbar_wait(sempty_bar(r), rph ^ 1u, abort_flag);
+        free_slot = __all_sync(0xffffffffu, free_slot);
+        if (!free_slot) { ok = false; break; }
+        const uint32_t dst = tiles + SF_OFF + (uint32_t)(r * SF_SLOT);
+        put_words(dst, lane, a[0], a[1], a[2], a[3]);
+        put_words(dst + SF_CHUNK, lane, b, b, b, b);
+        put_words(dst + 2 * SF_CHUNK, lane, c, c, c, c);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_release_cluster(sfull_bar(r) & PEER_MASK);
+        if (++r == SF_RING) { r = 0; rph ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue (both CTAs, own 128 rows)
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    int cursor = 0;
+    uint32_t it = 0;
+    Tile t;
+    uint8_t* stg = gen + STG8_OFF + (warp - 2) * STG_WARP_BYTES;
+    for (int j = 0;; ++j, ++it) {
+      const int tile = next_tile(j, true);
+      if (tile < 0 || !locate(tile, cursor, t)) break;
+      const uint32_t b = it & 1u, use = it >> 1;
+      bool ready = mbar_wait(tfull_bar(b), use & 1u, abort_flag);
+      ready = __all_sync(0xffffffffu, ready);
+      if (EPI == SWIGLU) ready = group_all(1 + quarter, 64, ready);   // the two threads of a row stop together
+      if (!ready) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * (uint32_t)ACC_STEP;
+      const int warp_row0 = (int)rank * BM + quarter * 32;
+      const bool full_rows = warp_row0 + 32 <= t.rows, row_ok = warp_row0 + lane < t.rows;
+      const int row = t.row0 + warp_row0;
+      // the overlap is the last 64 columns of accumulator 0 and the first 64 of accumulator 1
+      const bool mine_shared = half == (b == 0 ? 1 : 0);
+      if constexpr (EPI == PLAIN) {
+        __nv_bfloat16* orow = reinterpret_cast<__nv_bfloat16*>(ar.out) + (int64_t)(row + lane) * ar.Nout + t.n0;
+        const int first = half * 128 + (half == 1 && b == 0 ? 64 : 0);          // 64 columns at a time, shared ones first
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
+          const int c0 = q == 0 ? first : first ^ 64;
+          uint32_t g[2][32];
+          tmem_ld32(taddr + (uint32_t)c0, g[0]);
+          tmem_ld32(taddr + (uint32_t)(c0 + 32), g[1]);
+          tmem_ld_wait();
+          if (q == 0 && mine_shared) {
+            tc_fence_before();
+            mbar_arrive_cluster(shared_bar(b) & PEER_MASK);
+          }
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const int c = c0 + 32 * v;
+            if (t.n0 + c >= ar.Nout) break;
+            uint32_t packed[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) packed[i] = pack_bf16(__uint_as_float(g[v][2 * i]), __uint_as_float(g[v][2 * i + 1]));
+            store_piece(packed, full_rows, row_ok, stg, &mp.o, t.n0 + c, row, orow + c, ar.Nout - (t.n0 + c));
+          }
+        }
+        tc_fence_before();
+        mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
+      } else {
+        // hidden columns half * 64 .. + 63 of the tile: gate there, up 128 columns further on
+        float h[64];
+        uint32_t top = 0;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          uint32_t g[32], u[32];
+          tmem_ld32(taddr + (uint32_t)(half * 64 + 32 * v), g);
+          tmem_ld32(taddr + (uint32_t)(128 + half * 64 + 32 * v), u);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float gv = __uint_as_float(g[i]);
+            h[32 * v + i] = __fdividef(gv, 1.0f + __expf(-gv)) * __uint_as_float(u[i]);
+            top = max(top, __float_as_uint(h[32 * v + i]) & 0x7fffffffu);
+          }
+        }
+        tc_fence_before();
+        if (mine_shared) mbar_arrive_cluster(shared_bar(b) & PEER_MASK);
+        mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
+        uint32_t* rm = row_max + b * 256 + quarter * 32 + lane;
+        rm[half * 128] = top;
+        group_sync(1 + quarter, 64);
+        top = max(top, rm[(half ^ 1) * 128]);
+        const uint32_t code = scale_code(top);
+        uint32_t packed[16];
+        if (code == (uint32_t)Q_NAN_SCALE) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) packed[i] = 0x7f7f7f7fu;
+        } else {
+          const float f = inv_scale(code);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            packed[i] = to_e4m3x2(h[4 * i] * f, h[4 * i + 1] * f) | (to_e4m3x2(h[4 * i + 2] * f, h[4 * i + 3] * f) << 16);
+        }
+        const int c = t.n0 + half * 64;
+        if (half == 0 && row_ok)
+          ar.out_scale[(int64_t)(row + lane) * ((ar.Nout + QBLOCK - 1) / QBLOCK) + t.n0 / QBLOCK] = (uint8_t)code;
+        if (c < ar.Nout)                                        // 64 codes are the 64 bytes of a piece's row
+          store_piece(packed, full_rows, row_ok, stg, &mp.o, c, row,
+                      reinterpret_cast<__nv_bfloat16*>(reinterpret_cast<uint8_t*>(ar.out) + (int64_t)(row + lane) * ar.Nout + c),
+                      (ar.Nout - c) / 2);
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+
+  // ------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+  if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
+}
+
+template <int EPI>
+int launch(const F8Maps& mp, const F8Args& ar, cudaStream_t st) {
+  const int pairs = sm_count() / 2;
+  if (pairs < 1) return CAPMOE_EUNSUPPORTED;
+  cudaError_t err = cudaFuncSetAttribute(k_gmm8<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM8);
+  if (err != cudaSuccess) return note_cuda(err);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(F8_THREADS);
+  cfg.dynamicSmemBytes = SMEM8;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  err = cudaLaunchKernelEx(&cfg, k_gmm8<EPI>, mp, ar);
+  count_launch(1);
+  return note_cuda(err);
+}
+
+}  // namespace
+
+bool gmm8_tc_supported(int d, int n) { return d % 16 == 0 && n % 16 == 0; }
+
+int gmm8_tc(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
+            int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+  F8Maps mp = {};
+  F8Args ar = {};
+  if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wq, d, n, sg.E, 128) ||
+      !make_store_map(&mp.o, y, n, sg.rows))
+    return note_cuda(cudaErrorInvalidValue);
+  ar.sg = sg; ar.K = d; ar.Nout = n; ar.xs = xs; ar.s0 = ws; ar.out = y; ar.dev_status = dev_status; ar.sched = sched;
+  return launch<PLAIN>(mp, ar, st);
+}
+
+int gmm8_tc_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                   const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+                   int32_t* sched, cudaStream_t st) {
+  F8Maps mp = {};
+  F8Args ar = {};
+  if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wg, d, F, sg.E, 128) ||
+      !make_map_u8(&mp.b1, wu, d, F, sg.E, 128) || !make_store_map_u8(&mp.o, hq, F, sg.rows))
+    return note_cuda(cudaErrorInvalidValue);
+  ar.sg = sg; ar.K = d; ar.Nout = F; ar.xs = xs; ar.s0 = wgs; ar.s1 = wus; ar.out = hq; ar.out_scale = hs;
+  ar.dev_status = dev_status; ar.sched = sched;
+  return launch<SWIGLU>(mp, ar, st);
+}
+
+}  // namespace capmoe

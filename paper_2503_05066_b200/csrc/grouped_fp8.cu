@@ -233,7 +233,7 @@ FfnWs ffn_ws(int64_t A_max, int d, int F) {
   w.hq = w.xs + up(A * ceil_div(d, QBLOCK));
   w.hs = w.hq + up(A * F);
   w.h = w.hs + up(A * ceil_div(F, QBLOCK));
-  w.total = w.h + up(A * F * 4) + 256;
+  w.total = w.h + (gmm8_tc_supported(d, F) ? 0 : up(A * F * 4)) + 256;
   return w;
 }
 
@@ -268,7 +268,12 @@ extern "C" int capmoe_grouped_mm_fp8(const void* x_q, const void* x_scale, const
   if (rc != CAPMOE_OK || rows == 0) return rc;
   if (!usable(x_q, w_q, y) || !x_scale || !w_scale) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
-  (void)dev_status;
+  if (gmm8_tc_supported(d, n)) {
+    const int rc2 = dev_status ? clear_words(dev_status + 1, 1, nullptr, 0, as_stream(stream)) : CAPMOE_OK;
+    if (rc2 != CAPMOE_OK) return rc2;
+    return gmm8_tc((const uint8_t*)x_q, (const uint8_t*)x_scale, sg, (const uint8_t*)w_q, (const uint8_t*)w_scale, d, n, y,
+                   dev_status, dev_status ? dev_status + 1 : nullptr, as_stream(stream));
+  }
   const uint8_t* none = nullptr;
   return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, n, as_stream(stream), (const uint8_t*)x_q, (const uint8_t*)x_scale,
                       (const uint8_t*)w_q, (const uint8_t*)w_scale, none, none, (__nv_bfloat16*)y, sg, d, n);
@@ -290,11 +295,19 @@ extern "C" int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_
   const FfnWs w = ffn_ws(A_max, d, F);
   if (ws_bytes < w.total) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)A_max};
-  (void)dev_status;
   cudaStream_t st = as_stream(stream);
   uint8_t* b = (uint8_t*)ws;
+  const bool tc = gmm8_tc_supported(d, F);
+  if (tc && dev_status && (rc = clear_words(dev_status + 1, 2, nullptr, 0, st)) != CAPMOE_OK) return rc;
   rc = quantize_rows_run<__nv_bfloat16>(x_perm, expert_offsets + E, A_max, d, b + w.xq, b + w.xs, st);
   if (rc != CAPMOE_OK) return rc;
+  if (tc) {
+    rc = gmm8_tc_swiglu(b + w.xq, b + w.xs, sg, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
+                        (const uint8_t*)wu_scale, d, F, b + w.hq, b + w.hs, dev_status, dev_status ? dev_status + 1 : nullptr, st);
+    if (rc != CAPMOE_OK) return rc;
+    return gmm8_tc(b + w.hq, b + w.hs, sg, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, F, d, y_perm, dev_status,
+                   dev_status ? dev_status + 2 : nullptr, st);
+  }
   float* h = (float*)(b + w.h);
   rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, b + w.xq, b + w.xs, (const uint8_t*)wg_q, (const uint8_t*)wg_scale,
                     (const uint8_t*)wu_q, (const uint8_t*)wu_scale, h, sg, d, F);

@@ -135,6 +135,23 @@ def test_product_without_a_status_block(cm):
     _mm(cm, COUNTS["longer"], 384, 320, status=False)
 
 
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_scales_need_no_alignment(cm, shift):
+    """Scales are bytes: a scale tensor may start anywhere."""
+    counts, d, n = [40, 0, 150], 1024, 256
+    off = R.offsets_of(counts)
+    x, w = _normal((190, d), 1.0, BF16, 21), _normal((3, n, d), 0.05, BF16, 22)
+    (xq, xs), (wq, ws) = cm.quantize_rows(x), cm.quantize_weights(w)
+
+    def moved(s):
+        raw = torch.zeros(s.numel() + 4, device="cuda", dtype=torch.uint8)
+        raw[shift:shift + s.numel()] = s.view(torch.uint8).reshape(-1)
+        return raw[shift:shift + s.numel()].view(cm.SCALE).view(s.shape)
+
+    y = cm.grouped_mm_fp8(xq, xs, off, wq, ws)
+    assert torch.equal(cm.grouped_mm_fp8(xq, moved(xs), off, wq, moved(ws)), y)
+
+
 def test_a_nan_row_stays_a_row(cm):
     counts = [40, 0, 90]
     off = R.offsets_of(counts)
