@@ -109,6 +109,8 @@ def lib():
         L.capmoe_status_str.restype = ctypes.c_char_p
         L.capmoe_last_cuda_error.restype = ctypes.c_char_p
         L.capmoe_launch_count.restype = ctypes.c_uint64
+        for name, types in _ARGTYPES.items():
+            getattr(L, name).argtypes = types
         _lib = L
     return _lib
 
@@ -411,19 +413,46 @@ def grouped_ffn_segments(x_rows, seg_begin, seg_end, w_gate, w_up, w_down, w_mod
 
 
 # ----------------------------------------------------------------------------- grouped products
-def _need(ok: bool, where: str, what: str):
-    if not ok:
-        raise CapmoeError(EINVAL, f"{where}: {what}")
+# A decode step makes these calls every few microseconds, so they are written for little time on the host: argument
+# types are declared once (ints and addresses then pass without ctypes objects), messages are built only on failure.
+_V, _I, _L, _S = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+_ARGTYPES = {
+    "capmoe_grouped_mm": [_V, _V, _V, _I, _I, _I, _I, _V, _L, _V, _V],
+    "capmoe_grouped_mm_dx": [_V, _V, _V, _I, _I, _I, _I, _V, _L, _V, _V],
+    "capmoe_grouped_mm_dw": [_V, _V, _V, _I, _I, _I, _I, _I, _V, _L, _V, _S, _V, _V],
+    "capmoe_grouped_ffn_backward": [_V, _V, _V, _I, _I, _I, _I, _V, _V, _V, _V, _V, _V, _V, _L, _V, _S, _V, _V],
+    "capmoe_quantize_rows": [_V, _V, _L, _I, _I, _V, _V, _V],
+    "capmoe_quantize_weights": [_V, _I, _I, _I, _I, _V, _V, _V],
+    "capmoe_grouped_mm_fp8": [_V, _V, _V, _V, _V, _I, _I, _I, _V, _L, _V, _V],
+    "capmoe_grouped_ffn_fp8": [_V, _V, _I, _I, _I, _V, _V, _V, _V, _V, _V, _V, _L, _V, _S, _V, _V],
+}
 
 
-def _same_device(where: str, *tensors):
-    """All tensors on the current CUDA device: the library launches there and nowhere else."""
-    tensors = [t for t in tensors if t is not None]
-    for t in tensors:
-        _need(t.is_cuda, where, f"CUDA tensors expected, got one on {t.device}")
-    here = torch.cuda.current_device()
-    for t in tensors:
-        _need(t.device.index == here, where, f"tensors must be on the current device cuda:{here}, got {t.device}")
+def _refuse(where: str, what: str, status: int = EINVAL):
+    raise CapmoeError(status, f"{where}: {what}")
+
+
+def _run(name: str, stream, like, *args):
+    """Calls entry point `name` with `args` and the stream; tensors among the arguments pass as their addresses."""
+    here = like.get_device()
+    raw = []
+    for v in args:
+        if isinstance(v, torch.Tensor):
+            if v.get_device() != here or here < 0:
+                _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
+            assert v.is_contiguous(), "capmoe tensors must be contiguous"
+            v = v.data_ptr()
+        raw.append(v)
+    if here != torch.cuda.current_device():
+        _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
+    fn = getattr(lib(), name)
+    if stream is None:
+        raw.append(torch._C._cuda_getCurrentRawStream(here))
+    else:
+        raw.append(stream.cuda_stream)
+    rc = fn(*raw)
+    if rc != OK:
+        raise CapmoeError(rc, name)
 
 
 def _bytes(fn, *args) -> int:
@@ -433,22 +462,23 @@ def _bytes(fn, *args) -> int:
 
 
 def _experts(where: str, offsets) -> int:
-    _need(offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.numel() >= 2, where, "offsets must be int32 [E+1]")
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2:
+        _refuse(where, "offsets must be int32 [E+1]")
     return offsets.numel() - 1
 
 
 def _out(where: str, t, shape, dtype, like):
     if t is None:
         return torch.empty(shape, device=like.device, dtype=dtype)
-    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype, where, f"output must be {dtype} {tuple(shape)}")
+    if t.shape != shape or t.dtype != dtype:
+        _refuse(where, f"output must be {dtype} {tuple(shape)}")
     return t
 
 
 def _status(where: str, dev_status):
-    if dev_status is not None:
-        _need(dev_status.dtype == torch.int32 and dev_status.numel() >= FFN_STATUS_WORDS, where,
-              f"dev_status must be int32 [{FFN_STATUS_WORDS}]")
-    return _ptr(dev_status)
+    if dev_status is not None and (dev_status.dtype != torch.int32 or dev_status.numel() < FFN_STATUS_WORDS):
+        _refuse(where, f"dev_status must be int32 [{FFN_STATUS_WORDS}]")
+    return dev_status
 
 
 def grouped_mm(x_rows, offsets, w, y=None, dev_status=None, stream=None):
@@ -456,14 +486,12 @@ def grouped_mm(x_rows, offsets, w, y=None, dev_status=None, stream=None):
     offsets[E] are left as they are (undefined in a y made here)."""
     where = "capmoe_grouped_mm"
     E = _experts(where, offsets)
-    _need(x_rows.dim() == 2 and w.dim() == 3 and w.shape[0] == E and w.shape[2] == x_rows.shape[1] and w.dtype == x_rows.dtype,
-          where, "x_rows [rows,d] and w [E,n,d] of one dtype expected")
+    if x_rows.dim() != 2 or w.dim() != 3 or w.shape[0] != E or w.shape[2] != x_rows.shape[1] or w.dtype != x_rows.dtype:
+        _refuse(where, "x_rows [rows,d] and w [E,n,d] of one dtype expected")
     rows, d = x_rows.shape
     n = w.shape[1]
     y = _out(where, y, (rows, n), x_rows.dtype, x_rows)
-    _same_device(where, x_rows, offsets, w, y, dev_status)
-    _check(lib().capmoe_grouped_mm(_ptr(x_rows), _ptr(offsets), _ptr(w), E, int(d), int(n), _dt(x_rows), _ptr(y), _i64(rows),
-                                   _status(where, dev_status), _stream(stream)), where)
+    _run(where, stream, x_rows, x_rows, offsets, w, E, d, n, _dt(x_rows), y, rows, _status(where, dev_status))
     return y
 
 
@@ -471,14 +499,12 @@ def grouped_mm_dx(dy_rows, offsets, w, dx=None, dev_status=None, stream=None):
     """Gradient of grouped_mm's rows: dx[r] = W[e]^T dy[r].  dy_rows [rows,n], w [E,n,d] -> dx [rows,d]."""
     where = "capmoe_grouped_mm_dx"
     E = _experts(where, offsets)
-    _need(dy_rows.dim() == 2 and w.dim() == 3 and w.shape[0] == E and w.shape[1] == dy_rows.shape[1] and
-          w.dtype == dy_rows.dtype, where, "dy_rows [rows,n] and w [E,n,d] of one dtype expected")
+    if dy_rows.dim() != 2 or w.dim() != 3 or w.shape[0] != E or w.shape[1] != dy_rows.shape[1] or w.dtype != dy_rows.dtype:
+        _refuse(where, "dy_rows [rows,n] and w [E,n,d] of one dtype expected")
     rows, n = dy_rows.shape
     d = w.shape[2]
     dx = _out(where, dx, (rows, d), dy_rows.dtype, dy_rows)
-    _same_device(where, dy_rows, offsets, w, dx, dev_status)
-    _check(lib().capmoe_grouped_mm_dx(_ptr(dy_rows), _ptr(offsets), _ptr(w), E, int(d), int(n), _dt(dy_rows), _ptr(dx),
-                                      _i64(rows), _status(where, dev_status), _stream(stream)), where)
+    _run(where, stream, dy_rows, dy_rows, offsets, w, E, d, n, _dt(dy_rows), dx, rows, _status(where, dev_status))
     return dx
 
 
@@ -487,18 +513,15 @@ def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, de
     -> dw [E,n,d] in the rows' dtype, or out_dtype (float32)."""
     where = "capmoe_grouped_mm_dw"
     E = _experts(where, offsets)
-    _need(dy_rows.dim() == 2 and x_rows.dim() == 2 and dy_rows.shape[0] == x_rows.shape[0] and dy_rows.dtype == x_rows.dtype,
-          where, "dy_rows [rows,n] and x_rows [rows,d] of one dtype expected")
+    if (dy_rows.dim() != 2 or x_rows.dim() != 2 or dy_rows.shape[0] != x_rows.shape[0] or dy_rows.dtype != x_rows.dtype):
+        _refuse(where, "dy_rows [rows,n] and x_rows [rows,d] of one dtype expected")
     rows, n = dy_rows.shape
     d = x_rows.shape[1]
-    out_dtype = out_dtype or (dw.dtype if dw is not None else x_rows.dtype)
-    dw = _out(where, dw, (E, n, d), out_dtype, x_rows)
+    dw = _out(where, dw, (E, n, d), out_dtype or (dw.dtype if dw is not None else x_rows.dtype), x_rows)
     if ws is None:
         ws = torch.empty((_bytes("capmoe_grouped_mm_dw_workspace_bytes", E),), device=x_rows.device, dtype=torch.uint8)
-    _same_device(where, dy_rows, x_rows, offsets, dw, ws, dev_status)
-    _check(lib().capmoe_grouped_mm_dw(_ptr(dy_rows), _ptr(x_rows), _ptr(offsets), E, int(d), int(n), _dt(x_rows), _dt(dw),
-                                      _ptr(dw), _i64(rows), _ptr(ws), ctypes.c_size_t(ws.numel()), _status(where, dev_status),
-                                      _stream(stream)), where)
+    _run(where, stream, x_rows, dy_rows, x_rows, offsets, E, d, n, _dt(x_rows), _dt(dw), dw, rows, ws,
+         ws.numel() * ws.element_size(), _status(where, dev_status))
     return dw
 
 
@@ -512,25 +535,24 @@ def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None
     -> (dx [A_max,d], dw_gate [E,F,d], dw_up [E,F,d], dw_down [E,d,F]); `dw` may hand in the last three."""
     where = "capmoe_grouped_ffn_backward"
     E = _experts(where, offsets)
-    _need(x_perm.dim() == 2 and x_perm.shape == dy_perm.shape and w_gate.dim() == 3 and w_gate.shape[0] == E and
-          w_gate.shape[2] == x_perm.shape[1] and w_up.shape == w_gate.shape and
-          tuple(w_down.shape) == (E, w_gate.shape[2], w_gate.shape[1]), where,
-          "x_perm, dy_perm [A_max,d], w_gate, w_up [E,F,d], w_down [E,d,F] expected")
-    _need(len({t.dtype for t in (x_perm, dy_perm, w_gate, w_up, w_down)}) == 1, where, "one dtype expected")
+    if (x_perm.dim() != 2 or x_perm.shape != dy_perm.shape or w_gate.dim() != 3 or w_gate.shape[0] != E or
+            w_gate.shape[2] != x_perm.shape[1] or w_up.shape != w_gate.shape or
+            w_down.shape != (E, w_gate.shape[2], w_gate.shape[1])):
+        _refuse(where, "x_perm, dy_perm [A_max,d], w_gate, w_up [E,F,d], w_down [E,d,F] expected")
+    dtype = x_perm.dtype
+    if dy_perm.dtype != dtype or w_gate.dtype != dtype or w_up.dtype != dtype or w_down.dtype != dtype:
+        _refuse(where, "one dtype expected")
     A_max, d = x_perm.shape
     F = w_gate.shape[1]
-    dx = _out(where, dx, (A_max, d), x_perm.dtype, x_perm)
+    dx = _out(where, dx, (A_max, d), dtype, x_perm)
     dwg, dwu, dwd = (None, None, None) if dw is None else dw
-    dwg = _out(where, dwg, (E, F, d), x_perm.dtype, x_perm)
-    dwu = _out(where, dwu, (E, F, d), x_perm.dtype, x_perm)
-    dwd = _out(where, dwd, (E, d, F), x_perm.dtype, x_perm)
+    dwg = _out(where, dwg, (E, F, d), dtype, x_perm)
+    dwu = _out(where, dwu, (E, F, d), dtype, x_perm)
+    dwd = _out(where, dwd, (E, d, F), dtype, x_perm)
     if ws is None:
-        ws = torch.empty((ffn_backward_workspace_bytes(A_max, E, F, x_perm.dtype),), device=x_perm.device, dtype=torch.uint8)
-    _same_device(where, x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx, dwg, dwu, dwd, ws, dev_status)
-    _check(lib().capmoe_grouped_ffn_backward(_ptr(x_perm), _ptr(dy_perm), _ptr(offsets), E, int(d), int(F), _dt(x_perm),
-                                             _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(dwd),
-                                             _i64(A_max), _ptr(ws), ctypes.c_size_t(ws.numel()), _status(where, dev_status),
-                                             _stream(stream)), where)
+        ws = torch.empty((ffn_backward_workspace_bytes(A_max, E, F, dtype),), device=x_perm.device, dtype=torch.uint8)
+    _run(where, stream, x_perm, x_perm, dy_perm, offsets, E, d, F, _dt(dtype), w_gate, w_up, w_down, dx, dwg, dwu, dwd, A_max, ws,
+         ws.numel() * ws.element_size(), _status(where, dev_status))
     return dx, dwg, dwu, dwd
 
 
@@ -547,14 +569,18 @@ def quantize_rows(x, offsets=None, out=None, stream=None):
     """x [rows,d] (float32 or bfloat16) -> (q [rows,d] float8_e4m3fn, scale [rows, ceil(d/128)] float8_e8m0fnu), one
     power-of-two scale per 128 columns.  With offsets [E+1] only the rows below offsets[E] are quantised."""
     where = "capmoe_quantize_rows"
-    _need(x.dim() == 2, where, "x [rows,d] expected")
+    if x.dim() != 2:
+        _refuse(where, "x [rows,d] expected")
     rows, d = x.shape
     q, scale = (None, None) if out is None else out
     q = _out(where, q, (rows, d), FP8, x)
     scale = _out(where, scale, (rows, _blocks(d)), SCALE, x)
-    _same_device(where, x, offsets, q, scale)
-    n_rows = ctypes.c_void_p(0) if offsets is None else ctypes.c_void_p(offsets.data_ptr() + 4 * _experts(where, offsets))
-    _check(lib().capmoe_quantize_rows(_ptr(x), n_rows, _i64(rows), int(d), _dt(x), _ptr(q), _ptr(scale), _stream(stream)), where)
+    n_rows = None
+    if offsets is not None:
+        n_rows = offsets.data_ptr() + 4 * _experts(where, offsets)
+        if offsets.get_device() != x.get_device():
+            _refuse(where, "offsets must be on x's device")
+    _run(where, stream, x, x, n_rows, rows, d, _dt(x), q, scale)
     return q, scale
 
 
@@ -562,35 +588,34 @@ def quantize_weights(w, out=None, stream=None):
     """w [E,n,d] -> (q [E,n,d] float8_e4m3fn, scale [E, ceil(n/128), ceil(d/128)] float8_e8m0fnu), one scale per
     128 x 128 block."""
     where = "capmoe_quantize_weights"
-    _need(w.dim() == 3, where, "w [E,n,d] expected")
+    if w.dim() != 3:
+        _refuse(where, "w [E,n,d] expected")
     E, n, d = w.shape
     q, scale = (None, None) if out is None else out
     q = _out(where, q, (E, n, d), FP8, w)
     scale = _out(where, scale, (E, _blocks(n), _blocks(d)), SCALE, w)
-    _same_device(where, w, q, scale)
-    _check(lib().capmoe_quantize_weights(_ptr(w), int(E), int(n), int(d), _dt(w), _ptr(q), _ptr(scale), _stream(stream)), where)
+    _run(where, stream, w, w, E, n, d, _dt(w), q, scale)
     return q, scale
 
 
 def _coded(where: str, q, scale, shape, tall: int):
-    want = tuple(shape[:-2]) + (_blocks(shape[-2]) if tall > 1 else shape[-2], _blocks(shape[-1]))
-    _need(q.dtype == FP8 and tuple(q.shape) == tuple(shape) and scale.dtype == SCALE and tuple(scale.shape) == want, where,
-          f"float8_e4m3fn {tuple(shape)} with float8_e8m0fnu scales {want} expected")
+    want = (*shape[:-2], _blocks(shape[-2]) if tall > 1 else shape[-2], _blocks(shape[-1]))
+    if q.dtype != FP8 or q.shape != shape or scale.dtype != SCALE or scale.shape != want:
+        _refuse(where, f"float8_e4m3fn {tuple(shape)} with float8_e8m0fnu scales {want} expected")
 
 
 def grouped_mm_fp8(x_q, x_scale, offsets, w_q, w_scale, y=None, dev_status=None, stream=None):
     """grouped_mm from 8-bit rows (quantize_rows) and weights (quantize_weights) -> y [rows,n] bfloat16."""
     where = "capmoe_grouped_mm_fp8"
     E = _experts(where, offsets)
-    _need(x_q.dim() == 2 and w_q.dim() == 3, where, "x_q [rows,d], w_q [E,n,d] expected")
+    if x_q.dim() != 2 or w_q.dim() != 3:
+        _refuse(where, "x_q [rows,d], w_q [E,n,d] expected")
     rows, d = x_q.shape
     n = w_q.shape[1]
     _coded(where, x_q, x_scale, (rows, d), 1)
     _coded(where, w_q, w_scale, (E, n, d), QBLOCK)
     y = _out(where, y, (rows, n), torch.bfloat16, x_q)
-    _same_device(where, x_q, x_scale, offsets, w_q, w_scale, y, dev_status)
-    _check(lib().capmoe_grouped_mm_fp8(_ptr(x_q), _ptr(x_scale), _ptr(offsets), _ptr(w_q), _ptr(w_scale), E, int(d), int(n),
-                                       _ptr(y), _i64(rows), _status(where, dev_status), _stream(stream)), where)
+    _run(where, stream, x_q, x_q, x_scale, offsets, w_q, w_scale, E, d, n, y, rows, _status(where, dev_status))
     return y
 
 
@@ -603,8 +628,8 @@ def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None,
     hidden rows are quantised on the way -> y_perm [A_max,d] bfloat16."""
     where = "capmoe_grouped_ffn_fp8"
     E = _experts(where, offsets)
-    _need(x_perm.dim() == 2 and x_perm.dtype == torch.bfloat16 and w_gate[0].dim() == 3, where,
-          "x_perm [A_max,d] bfloat16 and (q, scale) weights expected")
+    if x_perm.dim() != 2 or x_perm.dtype != torch.bfloat16 or w_gate[0].dim() != 3:
+        _refuse(where, "x_perm [A_max,d] bfloat16 and (q, scale) weights expected")
     A_max, d = x_perm.shape
     F = w_gate[0].shape[1]
     _coded(where, *w_gate, (E, F, d), QBLOCK)
@@ -613,11 +638,8 @@ def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None,
     y_perm = _out(where, y_perm, (A_max, d), torch.bfloat16, x_perm)
     if ws is None:
         ws = torch.empty((ffn_fp8_workspace_bytes(A_max, d, F),), device=x_perm.device, dtype=torch.uint8)
-    _same_device(where, x_perm, offsets, *w_gate, *w_up, *w_down, y_perm, ws, dev_status)
-    _check(lib().capmoe_grouped_ffn_fp8(_ptr(x_perm), _ptr(offsets), E, int(d), int(F), _ptr(w_gate[0]), _ptr(w_gate[1]),
-                                        _ptr(w_up[0]), _ptr(w_up[1]), _ptr(w_down[0]), _ptr(w_down[1]), _ptr(y_perm),
-                                        _i64(A_max), _ptr(ws), ctypes.c_size_t(ws.numel()), _status(where, dev_status),
-                                        _stream(stream)), where)
+    _run(where, stream, x_perm, x_perm, offsets, E, d, F, *w_gate, *w_up, *w_down, y_perm, A_max, ws,
+         ws.numel() * ws.element_size(), _status(where, dev_status))
     return y_perm
 
 

@@ -38,6 +38,15 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
   return r;
 }
 
+// Whether a call runs the short-segment kernels (gmm_short.cu): average segment below `limit` rows, unless
+// capmoe_debug_ffn_variant forces one form.
+inline bool use_short(const Segments& sg, int64_t limit) {
+  const int v = ffn_variant();
+  if (v == FFN_SHORT) return true;
+  if (v == FFN_PAIR) return false;
+  return (int64_t)sg.rows < limit * sg.E;
+}
+
 // Tensor-core kernels (gmm_tc.cu): bf16 with rows of whole 16-byte vectors.  All matrices 16-byte aligned, map_ws
 // 128-byte aligned with gmm_tc_map_bytes(E, lists) bytes (dw: 2 lists, ffn_grad: 5).
 bool gmm_tc_supported(int E, int d, int n, int dtype);
@@ -49,6 +58,21 @@ int gmm_tc_dw(const void* dy, const void* x, const Segments& sg, int d, int n, b
 int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
                     const void* wd, void* dx, void* dwg, void* dwu, void* dwd, void* map_ws, void* hidden, int32_t* dev_status,
                     cudaStream_t st);
+
+// The same products with the weights on the M side (gmm_short.cu).  `sched`: a zeroed tile counter or NULL.
+int gmm_short_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
+                  cudaStream_t st);
+int gmm_short_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
+                 cudaStream_t st);
+int gmm_short_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
+                     const void* wd, void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st);
+int gmm_short_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
+                  int32_t* dev_status, int32_t* sched, cudaStream_t st);
+int gmm8_short(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n,
+               void* y, int32_t* dev_status, int32_t* sched, cudaStream_t st);
+int gmm8_short_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                      const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+                      int32_t* sched, cudaStream_t st);
 
 // Block-scaled 8-bit kernels (gmm_fp8_tc.cu): d and n (F) multiples of 16.  `sched`: a zeroed tile counter or NULL.
 bool gmm8_tc_supported(int d, int n);

@@ -16,6 +16,9 @@
 namespace capmoe {
 namespace {
 
+// rows per expert on average below which gmm_short.cu takes over
+constexpr int64_t SHORT_LIMIT = 256, SHORT_LIMIT_SWIGLU = 256;
+
 enum { PLAIN = 0, SWIGLU = 1 };
 constexpr int NST8 = 6;
 constexpr int STAGE8 = 2 * A_BYTES;                       // 128 rows of A, 128 rows of B: 32 KB
@@ -381,6 +384,7 @@ bool gmm8_tc_supported(int d, int n) { return d % 16 == 0 && n % 16 == 0; }
 
 int gmm8_tc(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
             int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+  if (use_short(sg, SHORT_LIMIT)) return gmm8_short(xq, xs, sg, wq, ws, d, n, y, dev_status, sched, st);
   F8Maps mp = {};
   F8Args ar = {};
   if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wq, d, n, sg.E, 128) ||
@@ -393,6 +397,8 @@ int gmm8_tc(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint
 int gmm8_tc_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                    const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
                    int32_t* sched, cudaStream_t st) {
+  if (use_short(sg, SHORT_LIMIT_SWIGLU))
+    return gmm8_short_swiglu(xq, xs, sg, wg, wgs, wu, wus, d, F, hq, hs, dev_status, sched, st);
   F8Maps mp = {};
   F8Args ar = {};
   if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wg, d, F, sg.E, 128) ||

@@ -1,0 +1,528 @@
+// Grouped products for short segments, in bf16 and in 8 bits: the operand roles of gmm_tc.cu / gmm_fp8_tc.cu
+// exchanged.  The weights are the M side (256 weight rows per CTA pair, 128 per CTA), the tokens the N side, which the
+// MMA takes in steps of 16, so an expert with a few rows pays for 16 of them and one with a few hundred for at most 15
+// more than it has; a segment longer than a tile is cut into equal token blocks.
+//   T_FWD   y^T  = W[e] x^T             T_DX  dx^T = W[e]^T dy^T (weights MN-major)      T_DX2  over both FFN weights
+//   T_HID   dg, du, h of the SwiGLU backward pass (three accumulators)
+//   T_F8    8-bit T_FWD                 T_F8SW  8-bit gate/up with SwiGLU, hidden rows quantised
+// One token's row of an output is one column of an accumulator: a warp's 32 lanes hold 32 neighbouring output columns
+// of it and store them as one run of 64 (8-bit: 32) bytes.  In T_F8SW a CTA's 128 weight rows are exactly one block
+// of 128 hidden columns, whose maximum is taken per token over the lanes (redux) and the four warps (shared memory).
+// A stage holds the weights of one k-block and `tb` token rows per CTA; `tb` follows the average segment so that short
+// segments leave the ring to the weights, which is what a decode step has to stream.  What bounds it: HBM for few rows
+// per expert, else the tensor pipe and the L2 traffic of the weights (once per token block).
+// Tensor memory: accumulators of `tt` columns, two sets of them when they fit, so that an epilogue overlaps the next
+// tile's MMAs.
+#include "gmm.cuh"
+#include "gmm_tc.cuh"
+
+namespace capmoe {
+namespace {
+
+enum Kind { T_FWD = 0, T_DX, T_DX2, T_HID, T_F8, T_F8SW };
+
+template <int KIND>
+struct ShapeT {
+  static constexpr bool FP8 = KIND == T_F8 || KIND == T_F8SW;
+  static constexpr int NACC = KIND == T_HID ? 3 : KIND == T_F8SW ? 2 : 1;     // accumulators = weight tiles per stage
+  static constexpr int NX = KIND == T_HID ? 2 : 1;                             // token tiles per stage
+  static constexpr int KE = FP8 ? 128 : 64;                                    // reduction steps per k-block: 128 bytes
+  static constexpr int EW = KIND == T_HID || KIND == T_F8SW ? 16 : 8;          // epilogue warps
+  static constexpr int THREADS = 64 + EW * 32 + (FP8 ? 32 : 0);
+  static constexpr int READERS = 2 + 2 * EW + (FP8 ? 2 : 0);                   // of the tile queue
+  static constexpr int COLS = FP8 ? SF_TMEM : 512;                             // tensor-memory columns for accumulators
+  static constexpr int SF_SLOT = 4 * SF_CHUNK;                                 // tokens 0..127, 128..255, weights, second weights
+  static constexpr int RING = (FP8 ? 212 : 216) * 1024;
+  static constexpr int SF_OFF = RING;
+  static constexpr int TAIL = RING + (FP8 ? SF_RING * SF_SLOT : 0);
+  static constexpr int RED = KIND == T_F8SW ? 2 * 4 * 4 * 32 * 4 : 0;
+  static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + RED;
+  static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
+};
+constexpr int MAX_NST = 12;
+
+struct TMaps { CUtensorMap x0, x1, w0, w1, w2; };
+struct TArgs {
+  Segments sg;
+  int K, Nout;
+  int tb, tt, bufs, nst;            // token rows per CTA and stage, tokens per tile, accumulator sets, stages
+  void* out[3];
+  const uint8_t *xs, *s0, *s1;      // 8-bit: scales of the rows, of W (W_g) and of W_u
+  uint8_t* out_scale;
+  int32_t* dev_status;
+  int32_t* sched;
+};
+
+struct STile { int e, row0, rows, nt, w0; };   // segment, first token row, tokens, MMA N, first weight row
+
+template <int KIND>
+__global__ void __launch_bounds__(ShapeT<KIND>::THREADS, 1)
+k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
+  using S = ShapeT<KIND>;
+  constexpr bool FP8 = S::FP8, W_MN = KIND == T_DX || KIND == T_DX2;
+  constexpr int EW = S::EW, NACC = S::NACC;
+  allow_next_kernel();
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (tiles - raw);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen + S::TAIL);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 52);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* offs = reinterpret_cast<int*>(gen + S::TAIL + 512);
+  int* ends = offs + (GMM_MAX_E + 1);
+  int* tile_start = ends + (GMM_MAX_E + 1);
+  uint32_t* red = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 4);       // T_F8SW: [2][4 warp groups][4][32]
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_ctarank();
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * (uint32_t)s; };                 // MAX_NST each
+  auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(MAX_NST + s); };
+  auto tfull_bar = [&](int b) { return bar0 + 8u * (uint32_t)(24 + b); };
+  auto tempty_bar = [&](int b) { return bar0 + 8u * (uint32_t)(26 + b); };
+  auto sfull_bar = [&](int r) { return bar0 + 8u * (uint32_t)(28 + r); };
+  auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(32 + r); };
+  const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
+  const int nst = ar.nst, tt = ar.tt, bufs = ar.bufs;
+  const uint32_t x_bytes = (uint32_t)ar.tb * 128u;
+  const uint32_t stage = (uint32_t)(NACC * A_BYTES) + (uint32_t)S::NX * x_bytes;
+
+  if (tid == 0) {
+    for (int s = 0; s < nst; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * EW * 32); }
+    for (int r = 0; r < SF_RING; ++r) { mbar_init(sfull_bar(r), 2); mbar_init(sempty_bar(r), 1); }
+    for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), S::READERS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  wait_for_previous_kernel();
+  const int E = ar.sg.E;
+  for (int i = tid; i < E; i += S::THREADS) { offs[i] = seg_at(ar.sg, i); ends[i] = max(offs[i], seg_at(ar.sg, i + 1)); }
+  __syncthreads();
+  const int w_blocks = (ar.Nout + 255) >> 8;
+  if (warp == 0) {
+    int carry = 0;
+    for (int e0 = 0; e0 < E; e0 += 32) {
+      const int e = e0 + lane;
+      const int mine = e < E ? (ends[e] - offs[e] + tt - 1) / tt * w_blocks : 0;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
+      if (e < E) tile_start[e] = carry + upto - mine;
+      carry += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) tile_start[E] = carry;
+  }
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const int tile_hi = tile_start[E];
+  const bool dyn = ar.sched != nullptr;
+  auto next_tile = [&](int j, bool whole_warp) -> int {
+    if (!dyn) { const int tile = pair + j * npairs; return tile < tile_hi ? tile : -1; }
+    return tq.get(j, whole_warp);
+  };
+  // Tiles of a segment: token block fastest (pairs side by side share a weight tile through L2), then weight block.
+  auto locate = [&](int tile, int& cursor, STile& t) -> bool {
+    while (cursor < E && tile >= tile_start[cursor + 1]) ++cursor;
+    if (cursor >= E) return false;
+    const int local = tile - tile_start[cursor], cnt = ends[cursor] - offs[cursor];
+    const int ntb = (cnt + tt - 1) / tt;
+    const int per = ((cnt + ntb - 1) / ntb + 15) & ~15;              // equal token blocks of whole MMA steps
+    const int wb = local / ntb, tbk = local - wb * ntb;
+    t.e = cursor;
+    t.row0 = offs[cursor] + tbk * per;
+    t.rows = max(0, min(per, cnt - tbk * per));                      // (rounding may leave the last block empty)
+    t.nt = max(16, (t.rows + 15) & ~15);
+    t.w0 = wb * 256;
+    return true;
+  };
+  const int kbs = (ar.K + S::KE - 1) / S::KE;
+  const int num_kb = kbs * (KIND == T_DX2 ? 2 : 1);
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer (both CTAs)
+    if (elect_one()) {
+      int cursor = 0, s = 0;
+      uint32_t ph = 0;
+      STile t;
+      bool ok = true;
+      const bool scheduler = dyn && rank == 0;
+      int cur = -1, claim = 0;
+      if (scheduler) {
+        cur = atomicAdd(ar.sched, 1);
+        if (cur >= tile_hi) cur = -1;
+        ok = tq.put(0, cur);
+        if (ok && cur >= 0) claim = atomicAdd(ar.sched, 1);
+      }
+      const int pub_kb = num_kb / 2;
+      for (int j = 0; ok; ++j) {
+        const int tile = scheduler ? cur : next_tile(j, false);
+        if (tile < 0 || !locate(tile, cursor, t)) break;
+        const int w = t.w0 + (int)rank * BM;                     // this CTA's 128 weight rows
+        const int x = t.row0 + (int)rank * (t.nt >> 1);          // and its half of the tokens
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (scheduler && kb == pub_kb) {
+            cur = claim < tile_hi ? claim : -1;
+            if (!tq.put(j + 1, cur)) { ok = false; break; }
+            if (cur >= 0) claim = atomicAdd(ar.sched, 1);
+          }
+          if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t bar = full_bar(s) & PEER_MASK;
+          if (rank == 0) mbar_expect_tx(full_bar(s), 2u * stage);
+          const uint32_t w_dst = tiles + (uint32_t)s * stage, x_dst = w_dst + (uint32_t)(NACC * A_BYTES);
+          if constexpr (KIND == T_FWD || KIND == T_F8) {
+            tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
+            tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
+          } else if constexpr (KIND == T_F8SW) {
+            tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
+            tma2_load_3d(w_dst + A_BYTES, &mp.w1, kb * S::KE, w, t.e, bar);
+            tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
+          } else if constexpr (KIND == T_HID) {
+            tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
+            tma2_load_3d(w_dst + A_BYTES, &mp.w1, kb * S::KE, w, t.e, bar);
+            tma2_load_3d(w_dst + 2 * A_BYTES, &mp.w2, w, kb * S::KE, t.e, bar);
+            tma2_load_3d(w_dst + 2 * A_BYTES + 8192u, &mp.w2, w + 64, kb * S::KE, t.e, bar);
+            tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
+            tma2_load_2d(x_dst + x_bytes, &mp.x1, kb * S::KE, x, bar);
+          } else {
+            const bool second = KIND == T_DX2 && kb >= kbs;
+            const int k = (second ? kb - kbs : kb) * S::KE;
+            tma2_load_3d(w_dst, second ? &mp.w1 : &mp.w0, w, k, t.e, bar);
+            tma2_load_3d(w_dst + 8192u, second ? &mp.w1 : &mp.w0, w + 64, k, t.e, bar);
+            tma2_load_2d(x_dst, second ? &mp.x1 : &mp.x0, k, x, bar);
+          }
+          if (++s == nst) { s = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (leader CTA only)
+    if (rank == 0 && elect_one()) {
+      int cursor = 0, s = 0, r = 0, b = 0;
+      uint32_t ph = 0, rph = 0, bph = 0;
+      const uint64_t w0 = W_MN ? umma_desc_mn(tiles) : umma_desc(tiles);
+      const uint64_t x0 = umma_desc(tiles + (uint32_t)(NACC * A_BYTES));
+      const uint64_t w2 = umma_desc_mn(tiles + 2 * A_BYTES);
+      const uint64_t x_step = (uint64_t)(x_bytes >> 4), stage_step = (uint64_t)(stage >> 4);
+      uint64_t off = 0;
+      STile t;
+      bool ok = true;
+      for (int j = 0; ok; ++j) {
+        const int tile = next_tile(j, false);
+        if (tile < 0 || !locate(tile, cursor, t)) break;
+        const uint32_t idesc = FP8 ? f8_idesc(t.nt) : pair_idesc(t.nt, W_MN, false), idesc2 = pair_idesc(t.nt, true, false);
+        if (!mbar_wait(tempty_bar(b), bph ^ 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(b * NACC * tt);
+        uint32_t sf = 0;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (FP8 && (kb & 3) == 0) {
+            if (!mbar_wait(sfull_bar(r), rph, abort_flag)) { ok = false; break; }
+            fence_acquire_cluster();
+            tc_fence_after();
+            sf = tmem_base + (uint32_t)(SF_TMEM + r * SF_COLS);
+            const uint32_t src = tiles + (uint32_t)(S::SF_OFF + r * S::SF_SLOT);
+            copy_scales(sf, src);
+            if (t.nt > 128) copy_scales(sf + 4u, src + SF_CHUNK);
+            copy_scales(sf + 8u, src + 2 * SF_CHUNK);
+            if (KIND == T_F8SW) copy_scales(sf + 12u, src + 3 * SF_CHUNK);
+          }
+          if (!mbar_wait(full_bar(s), ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t acc = (kb | k) != 0 ? 1u : 0u;
+            const uint64_t xd = x0 + off + 2 * k;
+            if constexpr (FP8) {
+              const uint32_t id = idesc | f8_scale_byte(kb);
+              umma2_f8(d, w0 + off + 2 * k, xd, id, sf + 8u, sf, acc);
+              if (KIND == T_F8SW)
+                umma2_f8(d + (uint32_t)tt, w0 + off + (uint64_t)((A_BYTES >> 4) + 2 * k), xd, id, sf + 12u, sf, acc);
+            } else {
+              umma2(d, w0 + off + (W_MN ? 128 : 2) * k, xd, idesc, acc);
+              if (KIND == T_HID) {
+                umma2(d + (uint32_t)tt, w0 + off + (uint64_t)((A_BYTES >> 4) + 2 * k), xd, idesc, acc);
+                umma2(d + (uint32_t)(2 * tt), w2 + off + 128 * k, xd + x_step, idesc2, acc);
+              }
+            }
+          }
+          umma2_commit_both(empty_bar(s));
+          if (FP8 && ((kb & 3) == 3 || kb == num_kb - 1)) {
+            umma2_commit_both(sempty_bar(r));
+            if (++r == SF_RING) { r = 0; rph ^= 1u; }
+          }
+          off += stage_step;
+          if (++s == nst) { s = 0; ph ^= 1u; off = 0; }
+        }
+        if (ok) umma2_commit_both(tfull_bar(b));
+        if (++b == bufs) { b = 0; bph ^= 1u; }
+      }
+    }
+  } else if (FP8 && warp == 2 + EW) {
+    // ------------------------------------------------------------ scales (both CTAs)
+    int cursor = 0, r = 0;
+    uint32_t rph = 0;
+    STile t;
+    bool ok = true;
+    const int nb = kbs, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
+    const bool words = (nb & 3) == 0 && (((uintptr_t)ar.xs | (uintptr_t)ar.s0 | (uintptr_t)ar.s1) & 3u) == 0;
+    for (int j = 0; ok; ++j) {
+      const int tile = next_tile(j, true);
+      if (tile < 0 || !locate(tile, cursor, t)) break;
+      const int64_t blk = (int64_t)t.e * wb + min(t.w0 / QBLOCK + (int)rank, wb - 1);
+      for (int k = 0; k < nb; k += 4) {
+        uint32_t a[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          a[i] = 0x7f7f7f7fu;
+          if (32 * i < t.nt)                                    // the same for the whole warp
+            a[i] = scale_word(ar.xs + (int64_t)min(t.row0 + lane + 32 * i, ar.sg.rows - 1) * nb, k, nb, words);
+        }
+        const uint32_t g = scale_word(ar.s0 + blk * nb, k, nb, words);
+        const uint32_t u = KIND == T_F8SW ? scale_word(ar.s1 + blk * nb, k, nb, words) : 0u;
+        bool free_slot = mbar_wait(sempty_bar(r), rph ^ 1u, abort_flag);
+        free_slot = __all_sync(0xffffffffu, free_slot);
+        if (!free_slot) { ok = false; break; }
+        const uint32_t dst = tiles + (uint32_t)(S::SF_OFF + r * S::SF_SLOT);
+        put_words(dst, lane, a[0], a[1], a[2], a[3]);
+        if (t.nt > 128) put_words(dst + SF_CHUNK, lane, a[4], a[5], a[6], a[7]);
+        put_words(dst + 2 * SF_CHUNK, lane, g, g, g, g);
+        if (KIND == T_F8SW) put_words(dst + 3 * SF_CHUNK, lane, u, u, u, u);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_release_cluster(sfull_bar(r) & PEER_MASK);
+        if (++r == SF_RING) { r = 0; rph ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue (both CTAs, own 128 weight rows)
+    const int quarter = warp & 3, sub = (warp - 2) >> 2;         // lane quarter; this warp's share of the token chunks
+    int cursor = 0, b = 0;
+    uint32_t bph = 0, flip = 0;
+    STile t;
+    for (int j = 0;; ++j) {
+      const int tile = next_tile(j, true);
+      if (tile < 0 || !locate(tile, cursor, t)) break;
+      bool ready = mbar_wait(tfull_bar(b), bph, abort_flag);
+      ready = __all_sync(0xffffffffu, ready);
+      if (KIND == T_F8SW) ready = group_all(1 + sub, 128, ready);    // the four warps of a token chunk stop together
+      if (!ready) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * NACC * tt);
+      const int col0 = t.w0 + (int)rank * BM;                    // first output column of this CTA
+      const int col = col0 + quarter * 32 + lane;                // this thread's
+      const bool col_ok = col < ar.Nout;
+      if (col0 < ar.Nout) {                                      // (all of a CTA's warps agree)
+#pragma unroll 1
+        for (int c = sub * 32; c < t.nt; c += EW * 8) {          // 32 tokens at a time
+          const int n = min(32, t.rows - c);                     // tokens that exist (may be negative: none)
+          const int64_t o = (int64_t)(t.row0 + c) * ar.Nout + col;
+          uint32_t g[32];
+          tmem_ld32(taddr + (uint32_t)c, g);
+          if constexpr (KIND == T_HID) {
+            uint32_t u[32], h[32];
+            tmem_ld32(taddr + (uint32_t)(tt + c), u);
+            tmem_ld32(taddr + (uint32_t)(2 * tt + c), h);
+            tmem_ld_wait();
+            __nv_bfloat16 *og = (__nv_bfloat16*)ar.out[0] + o, *ou = (__nv_bfloat16*)ar.out[1] + o,
+                          *oh = (__nv_bfloat16*)ar.out[2] + o;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float gv = __uint_as_float(g[i]), uv = __uint_as_float(u[i]), dv = __uint_as_float(h[i]);
+              const float p = __fdividef(1.0f, 1.0f + __expf(-gv));
+              const float a = gv * p;
+              if (i < n && col_ok) {
+                og[(int64_t)i * ar.Nout] = __float2bfloat16_rn(dv * uv * (p + a * (1.0f - p)));
+                ou[(int64_t)i * ar.Nout] = __float2bfloat16_rn(dv * a);
+                oh[(int64_t)i * ar.Nout] = __float2bfloat16_rn(a * uv);
+              }
+            }
+          } else if constexpr (KIND == T_F8SW) {
+            uint32_t u[32];
+            tmem_ld32(taddr + (uint32_t)(tt + c), u);
+            tmem_ld_wait();
+            uint32_t mine = 0;                                   // lane i: largest magnitude of token c + i in this warp
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float gv = __uint_as_float(g[i]);
+              const float h = __fdividef(gv, 1.0f + __expf(-gv)) * __uint_as_float(u[i]);
+              g[i] = __float_as_uint(h);
+              const uint32_t m = __reduce_max_sync(0xffffffffu, g[i] & 0x7fffffffu);
+              mine = lane == i ? m : mine;
+            }
+            uint32_t* rd = red + ((flip * 4 + (uint32_t)sub) * 4) * 32;
+            rd[quarter * 32 + lane] = mine;
+            group_sync(1 + sub, 128);
+            const uint32_t code = scale_code(max(max(rd[lane], rd[32 + lane]), max(rd[64 + lane], rd[96 + lane])));
+            flip ^= 1u;                                          // the next chunk writes the other copy
+            if (quarter == 0 && lane < n)
+              ar.out_scale[(int64_t)(t.row0 + c + lane) * ((ar.Nout + QBLOCK - 1) / QBLOCK) + col0 / QBLOCK] = (uint8_t)code;
+            uint8_t* oq = (uint8_t*)ar.out[0] + o;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const uint32_t ci = __shfl_sync(0xffffffffu, code, i);
+              const uint32_t q = ci == (uint32_t)Q_NAN_SCALE ? 0x7fu : to_e4m3x2(__uint_as_float(g[i]) * inv_scale(ci), 0.f) & 0xffu;
+              if (i < n && col_ok) oq[(int64_t)i * ar.Nout] = (uint8_t)q;
+            }
+          } else {
+            tmem_ld_wait();
+            __nv_bfloat16* oy = (__nv_bfloat16*)ar.out[0] + o;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i < n && col_ok) oy[(int64_t)i * ar.Nout] = __float2bfloat16_rn(__uint_as_float(g[i]));
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
+      if (++b == bufs) { b = 0; bph ^= 1u; }
+    }
+  }
+
+  // ------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+  if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
+}
+
+// Token rows per CTA and stage for segments of `avg` rows on average: twice the average fits a tile of two CTAs, in
+// steps of 16 rows, at least 16 and at most what `tt_max` columns allow.
+int token_rows(int64_t avg, int tt_max) {
+  int64_t tb = (avg + 15) / 16 * 16;
+  if (tb < 16) tb = 16;
+  if (tb > tt_max / 2) tb = tt_max / 2;
+  return (int)tb;
+}
+
+// Sets the tile geometry of a launch; tt_max as for token_rows.
+template <int KIND>
+void geometry(TArgs& ar, int tt_max) {
+  using S = ShapeT<KIND>;
+  ar.tb = token_rows(ar.sg.rows / ar.sg.E, tt_max);
+  ar.tt = 2 * ar.tb;
+  ar.bufs = 2 * S::NACC * ar.tt <= S::COLS ? 2 : 1;
+  const int stage = S::NACC * A_BYTES + S::NX * ar.tb * 128;
+  ar.nst = S::RING / stage < MAX_NST ? S::RING / stage : MAX_NST;
+}
+
+template <int KIND>
+int launch(const TMaps& mp, const TArgs& ar, cudaStream_t st) {
+  using S = ShapeT<KIND>;
+  const int pairs = sm_count() / 2;
+  if (pairs < 1) return CAPMOE_EUNSUPPORTED;
+  cudaError_t err = cudaFuncSetAttribute(k_gmm_t<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+  if (err != cudaSuccess) return note_cuda(err);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(S::THREADS);
+  cfg.dynamicSmemBytes = S::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  err = cudaLaunchKernelEx(&cfg, k_gmm_t<KIND>, mp, ar);
+  count_launch(1);
+  return note_cuda(err);
+}
+
+bool map2(CUtensorMap* m, const void* p, int64_t cols, int64_t rows, uint32_t box_rows) {
+  return make_map(m, p, (uint64_t)cols, (uint64_t)rows, 0, box_rows);
+}
+bool map3(CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t batch, uint32_t box_rows) {
+  return make_map(m, p, (uint64_t)cols, (uint64_t)rows, (uint64_t)batch, box_rows);
+}
+
+}  // namespace
+
+int gmm_short_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
+                  cudaStream_t st) {
+  TMaps mp = {};
+  TArgs ar = {};
+  ar.sg = sg; ar.K = d; ar.Nout = n; ar.out[0] = y; ar.dev_status = dev_status; ar.sched = sched;
+  geometry<T_FWD>(ar, 256);
+  if (!map2(&mp.x0, x, d, sg.rows, (uint32_t)ar.tb) || !map3(&mp.w0, w, d, n, sg.E, BM)) return note_cuda(cudaErrorInvalidValue);
+  return launch<T_FWD>(mp, ar, st);
+}
+
+int gmm_short_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
+                 cudaStream_t st) {
+  TMaps mp = {};
+  TArgs ar = {};
+  ar.sg = sg; ar.K = n; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = sched;
+  geometry<T_DX>(ar, 256);
+  if (!map2(&mp.x0, dy, n, sg.rows, (uint32_t)ar.tb) || !map3(&mp.w0, w, d, n, sg.E, BK)) return note_cuda(cudaErrorInvalidValue);
+  return launch<T_DX>(mp, ar, st);
+}
+
+int gmm_short_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
+                     const void* wd, void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+  TMaps mp = {};
+  TArgs ar = {};
+  ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = dg; ar.out[1] = du; ar.out[2] = h; ar.dev_status = dev_status; ar.sched = sched;
+  geometry<T_HID>(ar, 160);
+  if (!map2(&mp.x0, x, d, sg.rows, (uint32_t)ar.tb) || !map2(&mp.x1, dy, d, sg.rows, (uint32_t)ar.tb) ||
+      !map3(&mp.w0, wg, d, F, sg.E, BM) || !map3(&mp.w1, wu, d, F, sg.E, BM) || !map3(&mp.w2, wd, F, d, sg.E, BK))
+    return note_cuda(cudaErrorInvalidValue);
+  return launch<T_HID>(mp, ar, st);
+}
+
+int gmm_short_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
+                  int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+  TMaps mp = {};
+  TArgs ar = {};
+  ar.sg = sg; ar.K = F; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = sched;
+  geometry<T_DX2>(ar, 256);
+  if (!map2(&mp.x0, dg, F, sg.rows, (uint32_t)ar.tb) || !map2(&mp.x1, du, F, sg.rows, (uint32_t)ar.tb) ||
+      !map3(&mp.w0, wg, d, F, sg.E, BK) || !map3(&mp.w1, wu, d, F, sg.E, BK))
+    return note_cuda(cudaErrorInvalidValue);
+  return launch<T_DX2>(mp, ar, st);
+}
+
+int gmm8_short(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n,
+               void* y, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+  TMaps mp = {};
+  TArgs ar = {};
+  ar.sg = sg; ar.K = d; ar.Nout = n; ar.out[0] = y; ar.xs = xs; ar.s0 = ws; ar.dev_status = dev_status; ar.sched = sched;
+  geometry<T_F8>(ar, 224);
+  if (!make_map_u8(&mp.x0, xq, d, sg.rows, 0, (uint32_t)ar.tb) || !make_map_u8(&mp.w0, wq, d, n, sg.E, BM))
+    return note_cuda(cudaErrorInvalidValue);
+  return launch<T_F8>(mp, ar, st);
+}
+
+int gmm8_short_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                      const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+                      int32_t* sched, cudaStream_t st) {
+  TMaps mp = {};
+  TArgs ar = {};
+  ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = hq; ar.out_scale = hs; ar.xs = xs; ar.s0 = wgs; ar.s1 = wus;
+  ar.dev_status = dev_status; ar.sched = sched;
+  geometry<T_F8SW>(ar, 224);
+  if (!make_map_u8(&mp.x0, xq, d, sg.rows, 0, (uint32_t)ar.tb) || !make_map_u8(&mp.w0, wg, d, F, sg.E, BM) ||
+      !make_map_u8(&mp.w1, wu, d, F, sg.E, BM))
+    return note_cuda(cudaErrorInvalidValue);
+  return launch<T_F8SW>(mp, ar, st);
+}
+
+}  // namespace capmoe

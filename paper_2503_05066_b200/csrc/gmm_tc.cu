@@ -21,6 +21,8 @@
 namespace capmoe {
 namespace {
 
+constexpr int64_t SHORT_LIMIT = 1024;        // rows per expert on average below which gmm_short.cu takes over
+
 enum Kind { FWD = 0, DX = 1, DX2 = 2, DW = 3, HID = 4 };
 
 struct GmmMaps { CUtensorMap a0, a1, b0, b1, b2, o0, o1, o2; };
@@ -439,6 +441,10 @@ bool gmm_tc_supported(int E, int d, int n, int dtype) {
 size_t gmm_tc_map_bytes(int E, int lists) { return (size_t)lists * E * sizeof(CUtensorMap); }
 
 int gmm_tc_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, cudaStream_t st) {
+  if (use_short(sg, SHORT_LIMIT)) {
+    const int rc0 = begin_counters(dev_status, 1, st);
+    return rc0 != CAPMOE_OK ? rc0 : gmm_short_fwd(x, sg, w, d, n, y, dev_status, counter(dev_status, 0), st);
+  }
   GmmMaps mp = {};
   GmmArgs ar = {};
   if (!map2(&mp.a0, x, d, sg.rows, BM) || !map3(&mp.b0, w, d, n, sg.E, 128) || !make_store_map(&mp.o0, y, n, sg.rows))
@@ -450,6 +456,10 @@ int gmm_tc_fwd(const void* x, const Segments& sg, const void* w, int d, int n, v
 }
 
 int gmm_tc_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, cudaStream_t st) {
+  if (use_short(sg, SHORT_LIMIT)) {
+    const int rc0 = begin_counters(dev_status, 1, st);
+    return rc0 != CAPMOE_OK ? rc0 : gmm_short_dx(dy, sg, w, d, n, dx, dev_status, counter(dev_status, 0), st);
+  }
   GmmMaps mp = {};
   GmmArgs ar = {};
   if (!map2(&mp.a0, dy, n, sg.rows, BM) || !map3(&mp.b0, w, d, n, sg.E, 64) || !make_store_map(&mp.o0, dx, d, sg.rows))
@@ -505,9 +515,12 @@ int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, in
   a1.dev_status = a2.dev_status = a3.dev_status = dev_status;
   a1.sched = counter(dev_status, 0); a2.sched = counter(dev_status, 1); a3.sched = counter(dev_status, 2);
   a1.K = d; a1.Nout = F; a1.out[0] = dg; a1.out[1] = du; a1.out[2] = h;
-  if ((rc = launch<HID, B>(m1, a1, st)) != CAPMOE_OK) return rc;
   a3.K = F; a3.Nout = d; a3.out[0] = dx;
-  if ((rc = launch<DX2, B>(m3, a3, st)) != CAPMOE_OK) return rc;
+  const bool brief = use_short(sg, SHORT_LIMIT);
+  rc = brief ? gmm_short_hidden(x, dy, sg, d, F, wg, wu, wd, dg, du, h, dev_status, a1.sched, st) : launch<HID, B>(m1, a1, st);
+  if (rc != CAPMOE_OK) return rc;
+  rc = brief ? gmm_short_dx2(dg, du, sg, d, F, wg, wu, dx, dev_status, a3.sched, st) : launch<DX2, B>(m3, a3, st);
+  if (rc != CAPMOE_OK) return rc;
   a2.count = 3;
   a2.out[0] = dwg; a2.out[1] = dwu; a2.out[2] = dwd;
   a2.M[0] = a2.M[1] = F; a2.M[2] = d;

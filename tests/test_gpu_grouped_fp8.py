@@ -130,6 +130,21 @@ def test_product_long_and_many_segments(cm, name, d, n):
     _mm(cm, COUNTS[name], d, n)
 
 
+@pytest.fixture
+def forced(cm):
+    yield lambda name: cm.debug_ffn_variant(name)
+    cm.debug_ffn_variant("auto")
+
+
+@pytest.mark.parametrize("form", ["pair", "short"])
+@pytest.mark.parametrize("d,n", [(256, 512), (144, 272), (1936, 400), (400, 48)])
+@pytest.mark.parametrize("name", ["few", "borders", "longer", "many"])
+def test_product_in_both_forms(cm, forced, name, d, n, form):
+    forced(form)
+    _mm(cm, COUNTS[name], d, n)
+    _mm(cm, COUNTS[name], d, n, status=False)
+
+
 def test_product_without_a_status_block(cm):
     _mm(cm, COUNTS["borders"], 384, 320, status=False)
     _mm(cm, COUNTS["longer"], 384, 320, status=False)
@@ -162,9 +177,14 @@ def test_a_nan_row_stays_a_row(cm):
     assert bool(nan[77].all()) and int(nan.sum()) == 128 and bool(torch.isfinite(y[:77].float()).all())
 
 
-@pytest.mark.parametrize("counts,d,F", [([1], 128, 128), ([0, 0], 128, 128), ([3, 0, 70, 129, 1], 256, 192), ([65, 64, 17], 144, 80),
-                                        ([5, 9, 0, 33], 33, 45), ([300, 0, 513], 256, 320), ([1] * 60, 256, 384), ([1100, 1400], 384, 256)])
-def test_ffn(cm, counts, d, F):
+FFN_CASES = [([1], 128, 128), ([0, 0], 128, 128), ([3, 0, 70, 129, 1], 256, 192), ([65, 64, 17], 144, 80),
+                                        ([5, 9, 0, 33], 33, 45), ([300, 0, 513], 256, 320), ([1] * 60, 256, 384), ([1100, 1400], 384, 256)]
+
+
+@pytest.mark.parametrize("form", ["auto", "pair", "short"])
+@pytest.mark.parametrize("counts,d,F", FFN_CASES)
+def test_ffn(cm, forced, counts, d, F, form):
+    forced(form)
     off = R.offsets_of(counts)
     A, E = sum(counts), len(counts)
     rows = A + 3
