@@ -24,7 +24,8 @@ constexpr int NST8 = 6;
 constexpr int STAGE8 = 2 * A_BYTES;                       // 128 rows of A, 128 rows of B: 32 KB
 constexpr int STG8_OFF = NST8 * STAGE8;
 constexpr int SF_OFF = STG8_OFF + EPI_WARPS * STG_WARP_BYTES;
-constexpr int SF_SLOT = 3 * SF_CHUNK;                     // A rows, B rows 0..127, B rows 128..255
+constexpr int SF_GROUP = 3 * SF_CHUNK;                    // A rows, B rows 0..127, B rows 128..255
+constexpr int SF_SLOT = SF_GROUPS * SF_GROUP;
 constexpr int TAIL8 = SF_OFF + SF_RING * SF_SLOT;
 constexpr int SMEM8 = TAIL8 + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + 2 * 2 * 128 * 4;
 static_assert(SMEM8 <= 227 * 1024, "shared memory of a thread block");
@@ -67,7 +68,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
   auto tempty_bar = [&](int b) { return bar0 + 8u * (uint32_t)(18 + b); };
   auto shared_bar = [&](int b) { return bar0 + 8u * (uint32_t)(20 + b); };        // the overlap columns have been read
   auto sfull_bar = [&](int r) { return bar0 + 8u * (uint32_t)(24 + r); };
-  auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(28 + r); };
+  auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(26 + r); };
+  auto gfree_bar = [&](int g) { return bar0 + 8u * (uint32_t)(28 + g); };
   const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
 
   if (tid == 0) {
@@ -78,6 +80,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
       mbar_init(shared_bar(b), EPI_WARPS * 32);                 // one half of the warps of each CTA
     }
     for (int r = 0; r < SF_RING; ++r) { mbar_init(sfull_bar(r), 2); mbar_init(sempty_bar(r), 1); }
+    for (int g = 0; g < SF_GROUPS; ++g) mbar_init(gfree_bar(g), 1);
     for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), TQ_READERS_F8); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -163,8 +166,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (rank == 0 && elect_one()) {
-      int cursor = 0, s = 0, r = 0;
-      uint32_t it = 0, ph = 0, rph = 0;
+      int cursor = 0, s = 0, r = 0, g = 0;
+      uint32_t it = 0, ph = 0, rph = 0, gph = 0;
       const uint32_t idesc0 = f8_idesc(256);
       const uint64_t a0 = umma_desc(tiles), b0 = umma_desc(tiles + A_BYTES);
       uint64_t off = 0;
@@ -181,12 +184,12 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
         const uint32_t d = tmem_base + b * (uint32_t)ACC_STEP;
         uint32_t sf = 0;
         for (int kb = 0; kb < num_kb; ++kb) {
+          if ((kb & 15) == 0 && !mbar_wait_cluster(sfull_bar(r), rph, abort_flag)) { ok = false; break; }
           if ((kb & 3) == 0) {
-            if (!mbar_wait(sfull_bar(r), rph, abort_flag)) { ok = false; break; }
-            fence_acquire_cluster();
+            if (!mbar_wait(gfree_bar(g), gph ^ 1u, abort_flag)) { ok = false; break; }   // its last MMAs are done
             tc_fence_after();
-            sf = tmem_base + (uint32_t)(SF_TMEM + r * SF_COLS);
-            const uint32_t src = tiles + SF_OFF + (uint32_t)(r * SF_SLOT);
+            sf = tmem_base + (uint32_t)(SF_TMEM + g * SF_COLS);
+            const uint32_t src = tiles + SF_OFF + (uint32_t)(r * SF_SLOT + ((kb >> 2) & 3) * SF_GROUP);
             copy_scales(sf + 8u, src);                          // A rows
             copy_scales(sf, src + SF_CHUNK);                    // B rows 0..127
             copy_scales(sf + 4u, src + 2 * SF_CHUNK);           // B rows 128..255
@@ -198,7 +201,12 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
           for (int k = 0; k < 4; ++k)
             umma2_f8(d, a0 + off + 2 * k, b0 + off + 2 * k, idesc, sf + 8u, sf, (kb | k) != 0 ? 1u : 0u);
           umma2_commit_both(empty_bar(s));
-          if ((kb & 3) == 3 || kb == num_kb - 1) {              // the group's last k-block: its words may be replaced
+          const bool last = kb == num_kb - 1;
+          if ((kb & 3) == 3 || last) {
+            umma2_commit_own(gfree_bar(g));
+            if (++g == SF_GROUPS) { g = 0; gph ^= 1u; }
+          }
+          if ((kb & 15) == 15 || last) {
             umma2_commit_both(sempty_bar(r));
             if (++r == SF_RING) { r = 0; rph ^= 1u; }
           }
@@ -215,8 +223,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
     Tile t;
     bool ok = true;
     const int nb = num_kb, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
-    const bool words = (nb & 3) == 0 &&                          // rows of scales start on words
-                       (((uintptr_t)ar.xs | (uintptr_t)ar.s0 | (uintptr_t)ar.s1) & 3u) == 0;
+    const int loads = scale_loads(nb, ar.xs, ar.s0, ar.s1);
     for (int j = 0; ok; ++j) {
       const int tile = next_tile(j, true);
       if (tile < 0 || !locate(tile, cursor, t)) break;
@@ -230,18 +237,22 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
       const uint8_t* w0 = ar.s0 + ((int64_t)t.e * wb + blk) * nb;
       const uint8_t* w1 = EPI == SWIGLU ? ar.s1 + ((int64_t)t.e * wb + blk) * nb
                                         : ar.s0 + ((int64_t)t.e * wb + min(blk + 1, wb - 1)) * nb;
-      for (int k = 0; k < nb; k += 4) {
-        uint32_t a[4];
+      for (int k = 0; ok && k < nb; k += 16) {
+        uint4 a[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = scale_word(rows[i], k, nb, words);
-        const uint32_t b = scale_word(w0, k, nb, words), c = scale_word(w1, k, nb, words);
+        for (int i = 0; i < 4; ++i) a[i] = scale_words(rows[i], k, nb, loads);
+        const uint4 b = scale_words(w0, k, nb, loads), c = scale_words(w1, k, nb, loads);
         bool free_slot = mbar_wait(sempty_bar(r), rph ^ 1u, abort_flag);
         free_slot = __all_sync(0xffffffffu, free_slot);
         if (!free_slot) { ok = false; break; }
-        const uint32_t dst = tiles + SF_OFF + (uint32_t)(r * SF_SLOT);
-        put_words(dst, lane, a[0], a[1], a[2], a[3]);
-        put_words(dst + SF_CHUNK, lane, b, b, b, b);
-        put_words(dst + 2 * SF_CHUNK, lane, c, c, c, c);
+#pragma unroll
+        for (int g = 0; g < SF_GROUPS; ++g) {
+          const uint32_t dst = tiles + SF_OFF + (uint32_t)(r * SF_SLOT + g * SF_GROUP);
+          const uint32_t bw = word_of(b, g), cw = word_of(c, g);
+          put_words(dst, lane, word_of(a[0], g), word_of(a[1], g), word_of(a[2], g), word_of(a[3], g));
+          put_words(dst + SF_CHUNK, lane, bw, bw, bw, bw);
+          put_words(dst + 2 * SF_CHUNK, lane, cw, cw, cw, cw);
+        }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive_release_cluster(sfull_bar(r) & PEER_MASK);

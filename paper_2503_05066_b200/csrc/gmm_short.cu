@@ -31,8 +31,9 @@ struct ShapeT {
   static constexpr int THREADS = 64 + EW * 32 + (FP8 ? 32 : 0);
   static constexpr int READERS = 2 + 2 * EW + (FP8 ? 2 : 0);                   // of the tile queue
   static constexpr int COLS = FP8 ? SF_TMEM : 512;                             // tensor-memory columns for accumulators
-  static constexpr int SF_SLOT = 4 * SF_CHUNK;                                 // tokens 0..127, 128..255, weights, second weights
-  static constexpr int RING = (FP8 ? 212 : 216) * 1024;
+  static constexpr int SF_GROUP = 4 * SF_CHUNK;                                // tokens 0..127, 128..255, weights, second weights
+  static constexpr int SF_SLOT = SF_GROUPS * SF_GROUP;
+  static constexpr int RING = (FP8 ? 202 : 216) * 1024;
   static constexpr int SF_OFF = RING;
   static constexpr int TAIL = RING + (FP8 ? SF_RING * SF_SLOT : 0);
   static constexpr int RED = KIND == T_F8SW ? 2 * 4 * 4 * 32 * 4 : 0;
@@ -45,6 +46,7 @@ struct TMaps { CUtensorMap x0, x1, w0, w1, w2; };
 struct TArgs {
   Segments sg;
   int K, Nout;
+  int wide;                         // MN-major weights: one box per k-block
   int tb, tt, bufs, nst;            // token rows per CTA and stage, tokens per tile, accumulator sets, stages
   void* out[3];
   const uint8_t *xs, *s0, *s1;      // 8-bit: scales of the rows, of W (W_g) and of W_u
@@ -82,7 +84,8 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   auto tfull_bar = [&](int b) { return bar0 + 8u * (uint32_t)(24 + b); };
   auto tempty_bar = [&](int b) { return bar0 + 8u * (uint32_t)(26 + b); };
   auto sfull_bar = [&](int r) { return bar0 + 8u * (uint32_t)(28 + r); };
-  auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(32 + r); };
+  auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(30 + r); };
+  auto gfree_bar = [&](int g) { return bar0 + 8u * (uint32_t)(32 + g); };
   const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
   const int nst = ar.nst, tt = ar.tt, bufs = ar.bufs;
   const uint32_t x_bytes = (uint32_t)ar.tb * 128u;
@@ -92,6 +95,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     for (int s = 0; s < nst; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * EW * 32); }
     for (int r = 0; r < SF_RING; ++r) { mbar_init(sfull_bar(r), 2); mbar_init(sempty_bar(r), 1); }
+    for (int g = 0; g < SF_GROUPS; ++g) mbar_init(gfree_bar(g), 1);
     for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), S::READERS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -192,15 +196,13 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
           } else if constexpr (KIND == T_HID) {
             tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
             tma2_load_3d(w_dst + A_BYTES, &mp.w1, kb * S::KE, w, t.e, bar);
-            tma2_load_3d(w_dst + 2 * A_BYTES, &mp.w2, w, kb * S::KE, t.e, bar);
-            tma2_load_3d(w_dst + 2 * A_BYTES + 8192u, &mp.w2, w + 64, kb * S::KE, t.e, bar);
+            load_mn(w_dst + 2 * A_BYTES, &mp.w2, ar.wide, w, kb * S::KE, t.e, bar);
             tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
             tma2_load_2d(x_dst + x_bytes, &mp.x1, kb * S::KE, x, bar);
           } else {
             const bool second = KIND == T_DX2 && kb >= kbs;
             const int k = (second ? kb - kbs : kb) * S::KE;
-            tma2_load_3d(w_dst, second ? &mp.w1 : &mp.w0, w, k, t.e, bar);
-            tma2_load_3d(w_dst + 8192u, second ? &mp.w1 : &mp.w0, w + 64, k, t.e, bar);
+            load_mn(w_dst, second ? &mp.w1 : &mp.w0, ar.wide, w, k, t.e, bar);
             tma2_load_2d(x_dst, second ? &mp.x1 : &mp.x0, k, x, bar);
           }
           if (++s == nst) { s = 0; ph ^= 1u; }
@@ -210,8 +212,8 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (rank == 0 && elect_one()) {
-      int cursor = 0, s = 0, r = 0, b = 0;
-      uint32_t ph = 0, rph = 0, bph = 0;
+      int cursor = 0, s = 0, r = 0, b = 0, g = 0;
+      uint32_t ph = 0, rph = 0, bph = 0, gph = 0;
       const uint64_t w0 = W_MN ? umma_desc_mn(tiles) : umma_desc(tiles);
       const uint64_t x0 = umma_desc(tiles + (uint32_t)(NACC * A_BYTES));
       const uint64_t w2 = umma_desc_mn(tiles + 2 * A_BYTES);
@@ -228,12 +230,12 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
         const uint32_t d = tmem_base + (uint32_t)(b * NACC * tt);
         uint32_t sf = 0;
         for (int kb = 0; kb < num_kb; ++kb) {
+          if (FP8 && (kb & 15) == 0 && !mbar_wait_cluster(sfull_bar(r), rph, abort_flag)) { ok = false; break; }
           if (FP8 && (kb & 3) == 0) {
-            if (!mbar_wait(sfull_bar(r), rph, abort_flag)) { ok = false; break; }
-            fence_acquire_cluster();
+            if (!mbar_wait(gfree_bar(g), gph ^ 1u, abort_flag)) { ok = false; break; }   // its last MMAs are done
             tc_fence_after();
-            sf = tmem_base + (uint32_t)(SF_TMEM + r * SF_COLS);
-            const uint32_t src = tiles + (uint32_t)(S::SF_OFF + r * S::SF_SLOT);
+            sf = tmem_base + (uint32_t)(SF_TMEM + g * SF_COLS);
+            const uint32_t src = tiles + (uint32_t)(S::SF_OFF + r * S::SF_SLOT + ((kb >> 2) & 3) * S::SF_GROUP);
             copy_scales(sf, src);
             if (t.nt > 128) copy_scales(sf + 4u, src + SF_CHUNK);
             copy_scales(sf + 8u, src + 2 * SF_CHUNK);
@@ -259,7 +261,12 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
             }
           }
           umma2_commit_both(empty_bar(s));
-          if (FP8 && ((kb & 3) == 3 || kb == num_kb - 1)) {
+          const bool last = kb == num_kb - 1;
+          if (FP8 && ((kb & 3) == 3 || last)) {
+            umma2_commit_own(gfree_bar(g));
+            if (++g == SF_GROUPS) { g = 0; gph ^= 1u; }
+          }
+          if (FP8 && ((kb & 15) == 15 || last)) {
             umma2_commit_both(sempty_bar(r));
             if (++r == SF_RING) { r = 0; rph ^= 1u; }
           }
@@ -277,29 +284,33 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     STile t;
     bool ok = true;
     const int nb = kbs, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
-    const bool words = (nb & 3) == 0 && (((uintptr_t)ar.xs | (uintptr_t)ar.s0 | (uintptr_t)ar.s1) & 3u) == 0;
+    const int loads = scale_loads(nb, ar.xs, ar.s0, ar.s1);
     for (int j = 0; ok; ++j) {
       const int tile = next_tile(j, true);
       if (tile < 0 || !locate(tile, cursor, t)) break;
       const int64_t blk = (int64_t)t.e * wb + min(t.w0 / QBLOCK + (int)rank, wb - 1);
-      for (int k = 0; k < nb; k += 4) {
-        uint32_t a[8];
+      for (int k = 0; ok && k < nb; k += 16) {
+        uint4 a[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          a[i] = 0x7f7f7f7fu;
+          a[i] = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
           if (32 * i < t.nt)                                    // the same for the whole warp
-            a[i] = scale_word(ar.xs + (int64_t)min(t.row0 + lane + 32 * i, ar.sg.rows - 1) * nb, k, nb, words);
+            a[i] = scale_words(ar.xs + (int64_t)min(t.row0 + lane + 32 * i, ar.sg.rows - 1) * nb, k, nb, loads);
         }
-        const uint32_t g = scale_word(ar.s0 + blk * nb, k, nb, words);
-        const uint32_t u = KIND == T_F8SW ? scale_word(ar.s1 + blk * nb, k, nb, words) : 0u;
+        const uint4 g4 = scale_words(ar.s0 + blk * nb, k, nb, loads);
+        const uint4 u4 = KIND == T_F8SW ? scale_words(ar.s1 + blk * nb, k, nb, loads) : g4;
         bool free_slot = mbar_wait(sempty_bar(r), rph ^ 1u, abort_flag);
         free_slot = __all_sync(0xffffffffu, free_slot);
         if (!free_slot) { ok = false; break; }
-        const uint32_t dst = tiles + (uint32_t)(S::SF_OFF + r * S::SF_SLOT);
-        put_words(dst, lane, a[0], a[1], a[2], a[3]);
-        if (t.nt > 128) put_words(dst + SF_CHUNK, lane, a[4], a[5], a[6], a[7]);
-        put_words(dst + 2 * SF_CHUNK, lane, g, g, g, g);
-        if (KIND == T_F8SW) put_words(dst + 3 * SF_CHUNK, lane, u, u, u, u);
+#pragma unroll
+        for (int g = 0; g < SF_GROUPS; ++g) {
+          const uint32_t dst = tiles + (uint32_t)(S::SF_OFF + r * S::SF_SLOT + g * S::SF_GROUP);
+          const uint32_t gw = word_of(g4, g), uw = word_of(u4, g);
+          put_words(dst, lane, word_of(a[0], g), word_of(a[1], g), word_of(a[2], g), word_of(a[3], g));
+          if (t.nt > 128) put_words(dst + SF_CHUNK, lane, word_of(a[4], g), word_of(a[5], g), word_of(a[6], g), word_of(a[7], g));
+          put_words(dst + 2 * SF_CHUNK, lane, gw, gw, gw, gw);
+          if (KIND == T_F8SW) put_words(dst + 3 * SF_CHUNK, lane, uw, uw, uw, uw);
+        }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive_release_cluster(sfull_bar(r) & PEER_MASK);
@@ -472,7 +483,8 @@ int gmm_short_dx(const void* dy, const Segments& sg, const void* w, int d, int n
   TArgs ar = {};
   ar.sg = sg; ar.K = n; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_DX>(ar, 256);
-  if (!map2(&mp.x0, dy, n, sg.rows, (uint32_t)ar.tb) || !map3(&mp.w0, w, d, n, sg.E, BK)) return note_cuda(cudaErrorInvalidValue);
+  if (!map2(&mp.x0, dy, n, sg.rows, (uint32_t)ar.tb) || !make_mn_map(&mp.w0, w, d, n, sg.E)) return note_cuda(cudaErrorInvalidValue);
+  ar.wide = mn_wide(d);
   return launch<T_DX>(mp, ar, st);
 }
 
@@ -483,8 +495,9 @@ int gmm_short_hidden(const void* x, const void* dy, const Segments& sg, int d, i
   ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = dg; ar.out[1] = du; ar.out[2] = h; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_HID>(ar, 160);
   if (!map2(&mp.x0, x, d, sg.rows, (uint32_t)ar.tb) || !map2(&mp.x1, dy, d, sg.rows, (uint32_t)ar.tb) ||
-      !map3(&mp.w0, wg, d, F, sg.E, BM) || !map3(&mp.w1, wu, d, F, sg.E, BM) || !map3(&mp.w2, wd, F, d, sg.E, BK))
+      !map3(&mp.w0, wg, d, F, sg.E, BM) || !map3(&mp.w1, wu, d, F, sg.E, BM) || !make_mn_map(&mp.w2, wd, F, d, sg.E))
     return note_cuda(cudaErrorInvalidValue);
+  ar.wide = mn_wide(F);
   return launch<T_HID>(mp, ar, st);
 }
 
@@ -495,8 +508,9 @@ int gmm_short_dx2(const void* dg, const void* du, const Segments& sg, int d, int
   ar.sg = sg; ar.K = F; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_DX2>(ar, 256);
   if (!map2(&mp.x0, dg, F, sg.rows, (uint32_t)ar.tb) || !map2(&mp.x1, du, F, sg.rows, (uint32_t)ar.tb) ||
-      !map3(&mp.w0, wg, d, F, sg.E, BK) || !map3(&mp.w1, wu, d, F, sg.E, BK))
+      !make_mn_map(&mp.w0, wg, d, F, sg.E) || !make_mn_map(&mp.w1, wu, d, F, sg.E))
     return note_cuda(cudaErrorInvalidValue);
+  ar.wide = mn_wide(d);
   return launch<T_DX2>(mp, ar, st);
 }
 

@@ -32,6 +32,7 @@ struct GmmArgs {
   void* out[3];                // o0..o2 as plain pointers, for pieces that do not fill a box
   int count, M[3], N[3];       // DW: products, their sizes
   int ia[3], ib[3];            // DW: which of the per-expert map lists holds A and B
+  int wide_a, wide_b;          // MN-major operands: one box per k-block (DW: a bit per product)
   const CUtensorMap* maps;     // DW: [lists][E]
   int32_t* dev_status;
   int32_t* sched;
@@ -60,11 +61,11 @@ struct Shape {
   static constexpr int A_TILES = KIND == HID ? 2 : 1;
   static constexpr int B_BYTES_CTA = KIND == HID ? 3 * 64 * BK * 2 : 128 * BK * 2;
   static constexpr int STAGE = A_TILES * A_BYTES + B_BYTES_CTA;      // 32 KB / 56 KB
-  static constexpr int NST = KIND == HID ? 3 : 6;
-  static constexpr int STG_PIECES = KIND == HID ? 3 : 1;
+  static constexpr int NST = KIND == HID ? 3 : 5;
+  static constexpr int STG = KIND == HID ? 3 * STG_WARP_BYTES : WIDE_BYTES;   // staging per epilogue warp
   static constexpr int N_TILE = KIND == HID ? 128 : 256;
   static constexpr int STG_OFF = NST * STAGE;
-  static constexpr int TAIL = STG_OFF + STG_PIECES * EPI_WARPS * STG_WARP_BYTES;
+  static constexpr int TAIL = STG_OFF + EPI_WARPS * STG;
   static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16;
   static constexpr int BUFS = KIND == HID ? 1 : 2;                   // accumulators of 256 columns, or three of 128
 };
@@ -227,14 +228,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
             const bool second = KIND == DX2 && kb >= half_kb;
             const int k = (second ? kb - half_kb : kb) * BK, n = t.n0 + (int)rank * 128;
             tma2_load_2d(a_dst, second ? &mp.a1 : ma, k, m0, bar);
-            tma2_load_3d(b_dst, second ? &mp.b1 : mb, n, k, t.e, bar);
-            tma2_load_3d(b_dst + 8192u, second ? &mp.b1 : mb, n + 64, k, t.e, bar);
+            load_mn(b_dst, second ? &mp.b1 : mb, ar.wide_b, n, k, t.e, bar);
           } else if constexpr (KIND == DW) {
             const int r = offs[t.e] + kb * BK, n = t.n0 + (int)rank * 128;
-            tma2_load_2d(a_dst, ma, m0, r, bar);
-            tma2_load_2d(a_dst + 8192u, ma, m0 + 64, r, bar);
-            tma2_load_2d(b_dst, mb, n, r, bar);
-            tma2_load_2d(b_dst + 8192u, mb, n + 64, r, bar);
+            load_mn(a_dst, ma, (ar.wide_a >> t.p) & 1, m0, r, bar);
+            load_mn(b_dst, mb, (ar.wide_b >> t.p) & 1, n, r, bar);
           } else {
             const int n = t.n0 + (int)rank * 64;
             tma2_load_2d(a_dst, &mp.a0, kb * BK, m0, bar);
@@ -291,7 +289,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
     int cursor = 0;
     uint32_t it = 0;
     GTile t;
-    uint8_t* stg = gen + S::STG_OFF + (warp - 2) * S::STG_PIECES * STG_WARP_BYTES;
+    uint8_t* stg = gen + S::STG_OFF + (warp - 2) * S::STG;
     for (int j = 0;; ++j, ++it) {
       const int tile = next_tile(j, true);
       if (tile < 0 || !locate(tile, cursor, t)) break;
@@ -337,37 +335,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
           }
           const int64_t o = (row + lane) * Nout + t.n0 + c;
           const int left = Nout - (t.n0 + c);
-          store_piece(pg, full_rows, row_ok, stg, &mp.o0, t.n0 + c, (int)row, (__nv_bfloat16*)ar.out[0] + o, left);
-          store_piece2(pu, full_rows, row_ok, stg + STG_WARP_BYTES, &mp.o1, t.n0 + c, (int)row, (__nv_bfloat16*)ar.out[1] + o, left);
-          store_piece2(phd, full_rows, row_ok, stg + 2 * STG_WARP_BYTES, &mp.o2, t.n0 + c, (int)row,
+          put_piece(pg, true, full_rows, row_ok, stg, &mp.o0, t.n0 + c, (int)row, (__nv_bfloat16*)ar.out[0] + o, left);
+          put_piece(pu, false, full_rows, row_ok, stg + STG_WARP_BYTES, &mp.o1, t.n0 + c, (int)row, (__nv_bfloat16*)ar.out[1] + o, left);
+          put_piece(phd, false, full_rows, row_ok, stg + 2 * STG_WARP_BYTES, &mp.o2, t.n0 + c, (int)row,
                        (__nv_bfloat16*)ar.out[2] + o, left);
         }
       } else {
+        constexpr int PC = 128 / (int)sizeof(TO);               // columns of a piece
 #pragma unroll 1
-        for (int c = half * 128; c < half * 128 + 128; c += 32) {
+        for (int c = half * 128; c < half * 128 + 128; c += PC) {
           if (t.n0 + c >= Nout) break;
-          uint32_t g[32];
+          uint32_t g[PC], w[32];
           if (empty_sum) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = 0u;
+            for (int i = 0; i < PC; ++i) g[i] = 0u;
           } else {
-            tmem_ld32(taddr + (uint32_t)c, g);
+#pragma unroll
+            for (int i = 0; i < PC; i += 32) tmem_ld32(taddr + (uint32_t)(c + i), g + i);
             tmem_ld_wait();
           }
-          if constexpr (sizeof(TO) == 2) {
-            uint32_t packed[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) packed[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
-            store_piece(packed, full_rows, row_ok, stg, mo, t.n0 + c, (int)row, (__nv_bfloat16*)orow + c, Nout - (t.n0 + c));
-          } else {
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {                       // boxes of 16 fp32 columns: the same 64-byte rows
-              const int left = Nout - (t.n0 + c + 16 * v);
-              if (left <= 0) break;
-              store_piece(g + 16 * v, full_rows, row_ok, stg, mo, t.n0 + c + 16 * v, (int)row,
-                          reinterpret_cast<__nv_bfloat16*>(orow + c + 16 * v), 2 * left);
-            }
-          }
+          for (int i = 0; i < 32; ++i)
+            w[i] = sizeof(TO) == 2 ? pack_bf16(__uint_as_float(g[2 * i % PC]), __uint_as_float(g[(2 * i + 1) % PC])) : g[i];
+          put_wide(w, full_rows, row_ok, stg, mo, t.n0 + c, (int)row, orow + c, (Nout - (t.n0 + c)) * (int)sizeof(TO));
         }
       }
       tc_fence_before();
@@ -447,7 +437,7 @@ int gmm_tc_fwd(const void* x, const Segments& sg, const void* w, int d, int n, v
   }
   GmmMaps mp = {};
   GmmArgs ar = {};
-  if (!map2(&mp.a0, x, d, sg.rows, BM) || !map3(&mp.b0, w, d, n, sg.E, 128) || !make_store_map(&mp.o0, y, n, sg.rows))
+  if (!map2(&mp.a0, x, d, sg.rows, BM) || !map3(&mp.b0, w, d, n, sg.E, 128) || !make_wide_map(&mp.o0, y, n, sg.rows, 2))
     return note_cuda(cudaErrorInvalidValue);
   const int rc = begin_counters(dev_status, 1, st);
   if (rc != CAPMOE_OK) return rc;
@@ -462,11 +452,11 @@ int gmm_tc_dx(const void* dy, const Segments& sg, const void* w, int d, int n, v
   }
   GmmMaps mp = {};
   GmmArgs ar = {};
-  if (!map2(&mp.a0, dy, n, sg.rows, BM) || !map3(&mp.b0, w, d, n, sg.E, 64) || !make_store_map(&mp.o0, dx, d, sg.rows))
+  if (!map2(&mp.a0, dy, n, sg.rows, BM) || !make_mn_map(&mp.b0, w, d, n, sg.E) || !make_wide_map(&mp.o0, dx, d, sg.rows, 2))
     return note_cuda(cudaErrorInvalidValue);
   const int rc = begin_counters(dev_status, 1, st);
   if (rc != CAPMOE_OK) return rc;
-  ar.sg = sg; ar.K = n; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = counter(dev_status, 0);
+  ar.sg = sg; ar.K = n; ar.Nout = d; ar.out[0] = dx; ar.wide_b = mn_wide(d); ar.dev_status = dev_status; ar.sched = counter(dev_status, 0);
   return launch<DX, __nv_bfloat16>(mp, ar, st);
 }
 
@@ -475,13 +465,14 @@ int gmm_tc_dw(const void* dy, const void* x, const Segments& sg, int d, int n, b
   GmmMaps mp = {};
   GmmArgs ar = {};
   BaseMaps base = {};
-  if (!map2(&base.m[0], dy, n, sg.rows, BK) || !map2(&base.m[1], x, d, sg.rows, BK) ||
-      !(out_f32 ? make_store_map_f32(&mp.o0, dw, d, (uint64_t)sg.E * n) : make_store_map(&mp.o0, dw, d, (uint64_t)sg.E * n)))
+  if (!make_mn_map(&base.m[0], dy, n, sg.rows, 0) || !make_mn_map(&base.m[1], x, d, sg.rows, 0) ||
+      !make_wide_map(&mp.o0, dw, d, (uint64_t)sg.E * n, out_f32 ? 4 : 2))
     return note_cuda(cudaErrorInvalidValue);
   int rc = begin_counters(dev_status, 1, st);
   if (rc == CAPMOE_OK) rc = segment_maps(base, 2, sg, ws, st);
   if (rc != CAPMOE_OK) return rc;
   ar.sg = sg; ar.out[0] = dw; ar.count = 1; ar.M[0] = n; ar.N[0] = d; ar.ia[0] = 0; ar.ib[0] = 1;
+  ar.wide_a = mn_wide(n); ar.wide_b = mn_wide(d);
   ar.maps = (const CUtensorMap*)ws; ar.dev_status = dev_status; ar.sched = counter(dev_status, 0);
   return out_f32 ? launch<DW, float>(mp, ar, st) : launch<DW, __nv_bfloat16>(mp, ar, st);
 }
@@ -500,12 +491,12 @@ int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, in
   if (!map2(&m1.a0, x, d, R, BM) || !map2(&m1.a1, dy, d, R, BM) || !map3(&m1.b0, wg, d, F, sg.E, 64) ||
       !map3(&m1.b1, wu, d, F, sg.E, 64) || !map3(&m1.b2, wd, F, d, sg.E, 64) || !make_store_map(&m1.o0, dg, F, R) ||
       !make_store_map(&m1.o1, du, F, R) || !make_store_map(&m1.o2, h, F, R) ||
-      !map2(&base.m[0], dg, F, R, BK) || !map2(&base.m[1], du, F, R, BK) || !map2(&base.m[2], dy, d, R, BK) ||
-      !map2(&base.m[3], x, d, R, BK) || !map2(&base.m[4], h, F, R, BK) ||
-      !make_store_map(&m2.o0, dwg, d, (uint64_t)sg.E * F) || !make_store_map(&m2.o1, dwu, d, (uint64_t)sg.E * F) ||
-      !make_store_map(&m2.o2, dwd, F, (uint64_t)sg.E * d) ||
-      !map2(&m3.a0, dg, F, R, BM) || !map2(&m3.a1, du, F, R, BM) || !map3(&m3.b0, wg, d, F, sg.E, 64) ||
-      !map3(&m3.b1, wu, d, F, sg.E, 64) || !make_store_map(&m3.o0, dx, d, R))
+      !make_mn_map(&base.m[0], dg, F, R, 0) || !make_mn_map(&base.m[1], du, F, R, 0) || !make_mn_map(&base.m[2], dy, d, R, 0) ||
+      !make_mn_map(&base.m[3], x, d, R, 0) || !make_mn_map(&base.m[4], h, F, R, 0) ||
+      !make_wide_map(&m2.o0, dwg, d, (uint64_t)sg.E * F, 2) || !make_wide_map(&m2.o1, dwu, d, (uint64_t)sg.E * F, 2) ||
+      !make_wide_map(&m2.o2, dwd, F, (uint64_t)sg.E * d, 2) ||
+      !map2(&m3.a0, dg, F, R, BM) || !map2(&m3.a1, du, F, R, BM) || !make_mn_map(&m3.b0, wg, d, F, sg.E) ||
+      !make_mn_map(&m3.b1, wu, d, F, sg.E) || !make_wide_map(&m3.o0, dx, d, R, 2))
     return note_cuda(cudaErrorInvalidValue);
   int rc = begin_counters(dev_status, 3, st);
   if (rc == CAPMOE_OK) rc = segment_maps(base, MAP_LISTS, sg, map_ws, st);
@@ -515,7 +506,7 @@ int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, in
   a1.dev_status = a2.dev_status = a3.dev_status = dev_status;
   a1.sched = counter(dev_status, 0); a2.sched = counter(dev_status, 1); a3.sched = counter(dev_status, 2);
   a1.K = d; a1.Nout = F; a1.out[0] = dg; a1.out[1] = du; a1.out[2] = h;
-  a3.K = F; a3.Nout = d; a3.out[0] = dx;
+  a3.K = F; a3.Nout = d; a3.out[0] = dx; a3.wide_b = mn_wide(d);
   const bool brief = use_short(sg, SHORT_LIMIT);
   rc = brief ? gmm_short_hidden(x, dy, sg, d, F, wg, wu, wd, dg, du, h, dev_status, a1.sched, st) : launch<HID, B>(m1, a1, st);
   if (rc != CAPMOE_OK) return rc;
@@ -527,6 +518,8 @@ int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, in
   a2.N[0] = a2.N[1] = d; a2.N[2] = F;
   a2.ia[0] = 0; a2.ia[1] = 1; a2.ia[2] = 2;
   a2.ib[0] = a2.ib[1] = 3; a2.ib[2] = 4;
+  a2.wide_a = (mn_wide(F) ? 3 : 0) | (mn_wide(d) ? 4 : 0);
+  a2.wide_b = (mn_wide(d) ? 3 : 0) | (mn_wide(F) ? 4 : 0);
   a2.maps = (const CUtensorMap*)map_ws;
   return launch<DW, B>(m2, a2, st);
 }

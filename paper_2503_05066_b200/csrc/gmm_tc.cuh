@@ -23,12 +23,49 @@ __device__ __forceinline__ uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
          ((uint32_t)((2 * BM) >> 4) << 24);
 }
 
-// store_piece for the second and third piece of a chunk: the wait for this warp's earlier stores, made by the
-// first piece, covers their staging buffers too.
-__device__ __forceinline__ void store_piece2(const uint32_t* packed, bool full_rows, bool row_ok, uint8_t* stg,
-                                             const CUtensorMap* map_out, int col, int row0_of_warp, __nv_bfloat16* orow_c,
-                                             int cols_left) {
+// all but the newest N groups of this thread have finished reading their shared-memory source
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+
+// A wide piece of an output: 32 rows of 128 bytes (64 bf16 or 32 fp32 columns), lane r holding row r as 32 words.  With all
+// 32 rows inside the segment it goes out as one TMA box (128-byte swizzle) from a 4 KB buffer of the warp, else row by
+// row.  `bytes_left`: of the output row from this piece on, a multiple of 16.  Against 64-byte pieces this halves the
+// proxy fences and store instructions, which cost about 400 cycles a piece and bound short reductions.
+constexpr int WIDE_BYTES = 32 * 128;
+__device__ __forceinline__ void put_wide(const uint32_t* w, bool full_rows, bool row_ok, uint8_t* stg, const CUtensorMap* map_out,
+                                         int col, int row0_of_warp, void* orow_c, int bytes_left) {
   const int lane = threadIdx.x & 31;
+  if (full_rows) {
+    if (lane == 0) bulk_wait_read<0>();                        // the previous piece has left the buffer
+    __syncwarp();
+    const uint32_t base = smem_u32(stg) + (uint32_t)lane * 128u;
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)((v ^ (lane & 7)) * 16)), "r"(w[4 * v]),
+                   "r"(w[4 * v + 1]), "r"(w[4 * v + 2]), "r"(w[4 * v + 3])
+                   : "memory");
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_2d(map_out, col, row0_of_warp, smem_u32(stg));
+      bulk_commit();
+    }
+  } else if (row_ok) {
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+      if (v * 16 + 16 <= bytes_left)
+        reinterpret_cast<uint4*>(orow_c)[v] = make_uint4(w[4 * v], w[4 * v + 1], w[4 * v + 2], w[4 * v + 3]);
+  }
+}
+
+// The same for one of several 64-byte pieces with a 2 KB buffer each; `wait` for the first of a chunk.
+__device__ __forceinline__ void put_piece(const uint32_t* packed, bool wait, bool full_rows, bool row_ok, uint8_t* stg,
+                                          const CUtensorMap* map_out, int col, int row0_of_warp, __nv_bfloat16* orow_c,
+                                          int cols_left) {
+  const int lane = threadIdx.x & 31;
+  if (full_rows && wait) {
+    if (lane == 0) bulk_wait_read<0>();
+    __syncwarp();
+  }
   if (full_rows) {
     const uint32_t base = smem_u32(stg) + (uint32_t)lane * 64u;
 #pragma unroll
@@ -51,17 +88,59 @@ __device__ __forceinline__ void store_piece2(const uint32_t* packed, bool full_r
   }
 }
 
-// fp32 matrix [rows, cols] as 32-row x 16-column boxes (64-byte rows, as the bf16 boxes of 32 columns)
-bool make_store_map_f32(CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows) {
+__device__ __forceinline__ void tma2_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+      : "memory");
+}
+
+// Output matrix [rows, cols] (elements of 4 or 2 bytes) in boxes of 32 rows x 128 bytes, 128-byte swizzle
+bool make_wide_map(CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, int elt) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[2] = {cols, rows};
-  cuuint64_t strides[1] = {cols * 4};
-  cuuint32_t box[2] = {16, 32};
+  cuuint64_t strides[1] = {cols * (uint64_t)elt};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / elt), 32};
   cuuint32_t estr[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+  return fn(m, elt == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// MN-major operand: bf16 [rows, cols] or [batch, rows, cols], the reduction along the rows.  When the columns are whole
+// blocks of 64 the map splits them, (64, rows, cols / 64 [, batch]), and one box brings 128 columns by 64 rows in the order
+// the MMA descriptor wants; otherwise boxes of 64 columns.  mn_wide tells which.
+bool mn_wide(int64_t cols) { return cols % 64 == 0; }
+bool make_mn_map(CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t batch) {
+  if (!mn_wide((int64_t)cols)) return make_map(m, base, cols, rows, batch, BK);
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4] = {64, rows, cols / 64, batch};
+  cuuint64_t strides[3] = {cols * 2, 128, cols * rows * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)BK, 2, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, batch > 0 ? 4 : 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// 128 columns from c on (a multiple of 64) by 64 reduction steps from k on
+__device__ __forceinline__ void load_mn(uint32_t dst, const CUtensorMap* m, bool wide, int c, int k, uint32_t bar) {
+  if (wide) {
+    tma2_load_3d(dst, m, 0, k, c >> 6, bar);
+  } else {
+    tma2_load_2d(dst, m, c, k, bar);
+    tma2_load_2d(dst + 8192u, m, c + 64, k, bar);
+  }
+}
+__device__ __forceinline__ void load_mn(uint32_t dst, const CUtensorMap* m, bool wide, int c, int k, int e, uint32_t bar) {
+  if (wide) {
+    tma2_load_4d(dst, m, 0, k, c >> 6, e, bar);
+  } else {
+    tma2_load_3d(dst, m, c, k, e, bar);
+    tma2_load_3d(dst + 8192u, m, c + 64, k, e, bar);
+  }
 }
 
 }  // namespace
@@ -77,7 +156,12 @@ namespace {
 // group"), and the four MMAs of a k-block name the same byte.  128 rows of scales are 32 lanes x 4 columns (row r in
 // lane r % 32, column r / 32), copied by tcgen05.cp from 512 bytes of shared memory with row r's word at
 // (r % 32) * 16 + (r / 32) * 4, and repeated for the four lane quarters.
-constexpr int SF_RING = 3;                  // scale groups in flight
+// Shared memory holds them in slots of four groups (16 k-blocks, one 16-byte load per row): the hand-over from the warp
+// that stages them to the MMA thread, a fence and a release across the pair, takes about 1300 cycles, more than a
+// group of a decode step lasts (one group per slot: 41 us for a decode step's product, 8-bit, of 166 MB of weights).
+// Tensor memory holds four groups; a barrier per group says when its MMAs are done.
+constexpr int SF_RING = 2;                  // slots
+constexpr int SF_GROUPS = 4;                // groups per slot, and in tensor memory
 constexpr int SF_CHUNK = 512;               // bytes of shared memory for 128 rows
 constexpr int SF_COLS = 16;                 // tensor-memory columns per group (12 used)
 constexpr int SF_TMEM = 448;                // first column of the scales
@@ -108,20 +192,55 @@ __device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t saddr) {
   d |= (uint64_t)1 << 46;
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
 }
+// arrives on this CTA's barrier once the MMAs and copies issued so far are done
+__device__ __forceinline__ void umma2_commit_own(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void fence_acquire_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
-
-// Four scale bytes s[0..3] of a row of nb scales from position k on; those behind the row count as 2^0 (their codes are
-// zeros that TMA filled in).
-__device__ __forceinline__ uint32_t scale_word(const uint8_t* row, int k, int nb, bool words) {
-  if (words) return *reinterpret_cast<const uint32_t*>(row + k);
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w |= (k + i < nb ? (uint32_t)row[k + i] : 127u) << (8 * i);
-  return w;
+// mbar_wait for a barrier that the peer CTA arrives on with release semantics (acquire at cluster scope; a separate
+// fence on the MMA thread costs about a microsecond per scale group)
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
+}
+
+// Scale bytes k .. k + 15 of a row of nb (four scale groups), in one 16-byte load where the rows start on 16 bytes, as
+// words where they start on words.  Bytes behind the row count as 2^0: their codes are zeros that TMA filled in.
+enum { SCALES_16 = 0, SCALES_4 = 1, SCALES_1 = 2 };
+__device__ __forceinline__ int scale_loads(int nb, const void* p, const void* q, const void* r) {
+  const uintptr_t a = (uintptr_t)nb | (uintptr_t)p | (uintptr_t)q | (uintptr_t)r;
+  return (a & 15u) == 0 ? SCALES_16 : (a & 3u) == 0 ? SCALES_4 : SCALES_1;
+}
+__device__ __forceinline__ uint4 scale_words(const uint8_t* row, int k, int nb, int loads) {
+  if (loads == SCALES_16) return *reinterpret_cast<const uint4*>(row + k);
+  uint32_t w[4];
+  if (loads == SCALES_4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = k + 4 * i < nb ? *reinterpret_cast<const uint32_t*>(row + k + 4 * i) : 0x7f7f7f7fu;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[i] |= (k + 4 * i + j < nb ? (uint32_t)row[k + 4 * i + j] : 127u) << (8 * j);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ void put_words(uint32_t saddr, int lane, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr + (uint32_t)lane * 16u), "r"(a), "r"(b), "r"(c), "r"(d)
                : "memory");

@@ -139,21 +139,20 @@ __global__ void __launch_bounds__(SN)
 k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const uint8_t* __restrict__ w0,
          const uint8_t* __restrict__ s0, const uint8_t* __restrict__ w1, const uint8_t* __restrict__ s1, TO* __restrict__ out,
          Segments sg, int K, int Nout) {
-  allow_next_kernel();
   wait_for_previous_kernel();
-  __shared__ SimtTile sm;
+  __shared__ SimtTile<ST> sm;
   RowTile t;
-  if (!find_row_tile(sg, blockIdx.x, t)) return;
+  if (!find_row_tile<ST>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST, kb = (K + QBLOCK - 1) / QBLOCK, nb = (Nout + QBLOCK - 1) / QBLOCK;
   const Coded<1> la{xq + (int64_t)t.row0 * K, xs + (int64_t)t.row0 * kb, K, kb};
   const int64_t wo = ((int64_t)t.e * Nout + col0) * K, so = ((int64_t)t.e * nb + col0 / QBLOCK) * kb;
   float acc[4][4], up[4][4];
   clear_acc(acc);
   // (a 64-column tile lies inside one block of 128 weight rows: one row of scales serves it)
-  tile_product(la, Coded<QBLOCK>{w0 + wo, s0 + so, K, kb}, t.rows, Nout - col0, K, sm, acc);
+  tile_product<ST>(la, Coded<QBLOCK>{w0 + wo, s0 + so, K, kb}, t.rows, Nout - col0, K, sm, acc);
   if (SWIGLU) {
     clear_acc(up);
-    tile_product(la, Coded<QBLOCK>{w1 + wo, s1 + so, K, kb}, t.rows, Nout - col0, K, sm, up);
+    tile_product<ST>(la, Coded<QBLOCK>{w1 + wo, s1 + so, K, kb}, t.rows, Nout - col0, K, sm, up);
   }
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
