@@ -5,9 +5,11 @@
 //   T_FWD   y^T  = W[e] x^T             T_DX  dx^T = W[e]^T dy^T (weights MN-major)      T_DX2  over both FFN weights
 //   T_HID   dg, du, h of the SwiGLU backward pass (three accumulators)
 //   T_F8    8-bit T_FWD                 T_F8SW  8-bit gate/up with SwiGLU, hidden rows quantised
-// One token's row of an output is one column of an accumulator: a warp's 32 lanes hold 32 neighbouring output columns
-// of it and store them as one run of 64 (8-bit: 32) bytes.  In T_F8SW a CTA's 128 weight rows are exactly one block
-// of 128 hidden columns, whose maximum is taken per token over the lanes (redux) and the four warps (shared memory).
+// One token's row of an output is one column of an accumulator.  The epilogue reads 8 x 8 fragments, which stmatrix
+// writes transposed to shared memory, so that whole 64-byte runs of a token's row leave the warp.  (Two-byte stores
+// straight from the accumulator's columns took 15,000 cycles for a 128-token tile of T_HID, half as long as its MMAs.)
+// In T_F8SW a CTA's 128 weight rows are exactly one block of 128 hidden columns, whose maximum is taken per token over
+// the lanes (shuffles) and the four warps (shared memory).
 // A stage holds the weights of one k-block and `tb` token rows per CTA; `tb` follows the average segment so that short
 // segments leave the ring to the weights, which is what a decode step has to stream.  What bounds it: HBM for few rows
 // per expert, else the tensor pipe and the L2 traffic of the weights (once per token block).
@@ -27,16 +29,17 @@ struct ShapeT {
   static constexpr int NACC = KIND == T_HID ? 3 : KIND == T_F8SW ? 2 : 1;     // accumulators = weight tiles per stage
   static constexpr int NX = KIND == T_HID ? 2 : 1;                             // token tiles per stage
   static constexpr int KE = FP8 ? 128 : 64;                                    // reduction steps per k-block: 128 bytes
-  static constexpr int EW = KIND == T_HID || KIND == T_F8SW ? 16 : 8;          // epilogue warps
+  static constexpr int EW = 8;                                                 // epilogue warps
   static constexpr int THREADS = 64 + EW * 32 + (FP8 ? 32 : 0);
   static constexpr int READERS = 2 + 2 * EW + (FP8 ? 2 : 0);                   // of the tile queue
   static constexpr int COLS = FP8 ? SF_TMEM : 512;                             // tensor-memory columns for accumulators
   static constexpr int SF_GROUP = 4 * SF_CHUNK;                                // tokens 0..127, 128..255, weights, second weights
   static constexpr int SF_SLOT = SF_GROUPS * SF_GROUP;
-  static constexpr int RING = (FP8 ? 202 : 216) * 1024;
-  static constexpr int SF_OFF = RING;
-  static constexpr int TAIL = RING + (FP8 ? SF_RING * SF_SLOT : 0);
-  static constexpr int RED = KIND == T_F8SW ? 2 * 4 * 4 * 32 * 4 : 0;
+  static constexpr int RING = (FP8 ? 186 : 204) * 1024;
+  static constexpr int STG_OFF = RING;                                         // 2 KB per epilogue warp
+  static constexpr int SF_OFF = RING + EW * STG_WARP_BYTES;
+  static constexpr int TAIL = SF_OFF + (FP8 ? SF_RING * SF_SLOT : 0);
+  static constexpr int RED = KIND == T_F8SW ? 2 * 2 * 4 * 32 * 4 : 0;
   static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + RED;
   static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
 };
@@ -74,7 +77,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   int* offs = reinterpret_cast<int*>(gen + S::TAIL + 512);
   int* ends = offs + (GMM_MAX_E + 1);
   int* tile_start = ends + (GMM_MAX_E + 1);
-  uint32_t* red = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 4);       // T_F8SW: [2][4 warp groups][4][32]
+  uint32_t* red = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 4);       // T_F8SW: [2][2 warp groups][4][32]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank();
@@ -323,6 +326,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     int cursor = 0, b = 0;
     uint32_t bph = 0, flip = 0;
     STile t;
+    const uint32_t stg = tiles + (uint32_t)(S::STG_OFF + (warp - 2) * STG_WARP_BYTES);
     for (int j = 0;; ++j) {
       const int tile = next_tile(j, true);
       if (tile < 0 || !locate(tile, cursor, t)) break;
@@ -333,66 +337,115 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * NACC * tt);
       const int col0 = t.w0 + (int)rank * BM;                    // first output column of this CTA
-      const int col = col0 + quarter * 32 + lane;                // this thread's
-      const bool col_ok = col < ar.Nout;
+      const int wcol = col0 + quarter * 32, cols = ar.Nout - wcol;   // this warp's 32, and how many exist from there on
       if (col0 < ar.Nout) {                                      // (all of a CTA's warps agree)
 #pragma unroll 1
         for (int c = sub * 32; c < t.nt; c += EW * 8) {          // 32 tokens at a time
-          const int n = min(32, t.rows - c);                     // tokens that exist (may be negative: none)
-          const int64_t o = (int64_t)(t.row0 + c) * ar.Nout + col;
-          uint32_t g[32];
-          tmem_ld32(taddr + (uint32_t)c, g);
+          const int n = t.rows - c;                              // tokens that exist from here on (may be negative)
+          const int64_t o = (int64_t)(t.row0 + c) * ar.Nout + wcol;
+          const uint32_t ta = taddr + (uint32_t)c;
           if constexpr (KIND == T_HID) {
-            uint32_t u[32], h[32];
-            tmem_ld32(taddr + (uint32_t)(tt + c), u);
-            tmem_ld32(taddr + (uint32_t)(2 * tt + c), h);
-            tmem_ld_wait();
-            __nv_bfloat16 *og = (__nv_bfloat16*)ar.out[0] + o, *ou = (__nv_bfloat16*)ar.out[1] + o,
-                          *oh = (__nv_bfloat16*)ar.out[2] + o;
+            uint32_t pg[2][8], pu[2][8], ph[2][8];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float gv = __uint_as_float(g[i]), uv = __uint_as_float(u[i]), dv = __uint_as_float(h[i]);
-              const float p = __fdividef(1.0f, 1.0f + __expf(-gv));
-              const float a = gv * p;
-              if (i < n && col_ok) {
-                og[(int64_t)i * ar.Nout] = __float2bfloat16_rn(dv * uv * (p + a * (1.0f - p)));
-                ou[(int64_t)i * ar.Nout] = __float2bfloat16_rn(dv * a);
-                oh[(int64_t)i * ar.Nout] = __float2bfloat16_rn(a * uv);
+            for (int hf = 0; hf < 2; ++hf) {                     // 16 lanes at a time
+              uint32_t g[16], u[16], h[16];
+              tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16), g);
+              tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16) + (uint32_t)tt, u);
+              tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16) + (uint32_t)(2 * tt), h);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float dg[2], du[2], hh[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                  const float gv = __uint_as_float(g[2 * i + q]), uv = __uint_as_float(u[2 * i + q]), dv = __uint_as_float(h[2 * i + q]);
+                  const float p = __fdividef(1.0f, 1.0f + __expf(-gv));
+                  const float a = gv * p;
+                  dg[q] = dv * uv * (p + a * (1.0f - p));
+                  du[q] = dv * a;
+                  hh[q] = a * uv;
+                }
+                pg[hf][i] = pack_bf16(dg[0], dg[1]);
+                pu[hf][i] = pack_bf16(du[0], du[1]);
+                ph[hf][i] = pack_bf16(hh[0], hh[1]);
               }
             }
-          } else if constexpr (KIND == T_F8SW) {
-            uint32_t u[32];
-            tmem_ld32(taddr + (uint32_t)(tt + c), u);
-            tmem_ld_wait();
-            uint32_t mine = 0;                                   // lane i: largest magnitude of token c + i in this warp
+            auto put = [&](const uint32_t (&p)[2][8], void* out) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float gv = __uint_as_float(g[i]);
-              const float h = __fdividef(gv, 1.0f + __expf(-gv)) * __uint_as_float(u[i]);
-              g[i] = __float_as_uint(h);
-              const uint32_t m = __reduce_max_sync(0xffffffffu, g[i] & 0x7fffffffu);
-              mine = lane == i ? m : mine;
+              for (int i = 0; i < 4; ++i) put_frag(stg, i, p[0][2 * i], p[0][2 * i + 1], p[1][2 * i], p[1][2 * i + 1]);
+              flush_tokens(stg, (__nv_bfloat16*)out + o, ar.Nout, n, cols);
+            };
+            put(pg, ar.out[0]);
+            put(pu, ar.out[1]);
+            put(ph, ar.out[2]);
+          } else if constexpr (KIND == T_F8SW) {
+            uint32_t h[2][16];
+            uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};          // largest magnitude of tokens 8j + 2(lane % 4) and the next
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              uint32_t u[16];
+              tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16), h[hf]);
+              tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16) + (uint32_t)tt, u);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float gv = __uint_as_float(h[hf][i]);
+                h[hf][i] = __float_as_uint(__fdividef(gv, 1.0f + __expf(-gv)) * __uint_as_float(u[i]));
+                uint32_t& m = top[(i >> 2) * 2 + (i & 1)];
+                m = max(m, h[hf][i] & 0x7fffffffu);
+              }
             }
-            uint32_t* rd = red + ((flip * 4 + (uint32_t)sub) * 4) * 32;
-            rd[quarter * 32 + lane] = mine;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int x = 4; x < 32; x <<= 1) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+            uint32_t* rd = red + ((flip * 2 + (uint32_t)sub) * 4) * 32;
+            if (lane < 4) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) rd[quarter * 32 + (i >> 1) * 8 + 2 * lane + (i & 1)] = top[i];
+            }
             group_sync(1 + sub, 128);
-            const uint32_t code = scale_code(max(max(rd[lane], rd[32 + lane]), max(rd[64 + lane], rd[96 + lane])));
             flip ^= 1u;                                          // the next chunk writes the other copy
             if (quarter == 0 && lane < n)
-              ar.out_scale[(int64_t)(t.row0 + c + lane) * ((ar.Nout + QBLOCK - 1) / QBLOCK) + col0 / QBLOCK] = (uint8_t)code;
-            uint8_t* oq = (uint8_t*)ar.out[0] + o;
+              ar.out_scale[(int64_t)(t.row0 + c + lane) * ((ar.Nout + QBLOCK - 1) / QBLOCK) + col0 / QBLOCK] =
+                  (uint8_t)scale_code(max(max(rd[lane], rd[32 + lane]), max(rd[64 + lane], rd[96 + lane])));
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const uint32_t ci = __shfl_sync(0xffffffffu, code, i);
-              const uint32_t q = ci == (uint32_t)Q_NAN_SCALE ? 0x7fu : to_e4m3x2(__uint_as_float(g[i]) * inv_scale(ci), 0.f) & 0xffu;
-              if (i < n && col_ok) oq[(int64_t)i * ar.Nout] = (uint8_t)q;
+            for (int i = 0; i < 4; ++i) {
+              float f[2];
+              bool bad[2];
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {
+                const int at = 8 * i + 2 * (lane & 3) + q;
+                const uint32_t code = scale_code(max(max(rd[at], rd[32 + at]), max(rd[64 + at], rd[96 + at])));
+                bad[q] = code == (uint32_t)Q_NAN_SCALE;
+                f[q] = bad[q] ? 0.f : inv_scale(code);
+              }
+              uint32_t p[4];                                     // lanes 0-7, 8-15, 16-23, 24-31
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t* v = &h[k >> 1][4 * i + 2 * (k & 1)];
+                const uint32_t q2 = to_e4m3x2(__uint_as_float(v[0]) * f[0], __uint_as_float(v[1]) * f[1]);
+                p[k] = (bad[0] ? 0x7fu : q2 & 0xffu) | (bad[1] ? 0x7f0000u : (q2 & 0xff00u) << 8);
+              }
+              put_frag(stg, i, p[0], p[1], p[2], p[3]);
             }
+            flush_tokens_u8(stg, (uint8_t*)ar.out[0] + o, ar.Nout, n, cols);
           } else {
+            uint32_t g[2][16];
+            tmem_ld_frag(ta, g[0]);
+            tmem_ld_frag(ta + (16u << 16), g[1]);
             tmem_ld_wait();
-            __nv_bfloat16* oy = (__nv_bfloat16*)ar.out[0] + o;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i < n && col_ok) oy[(int64_t)i * ar.Nout] = __float2bfloat16_rn(__uint_as_float(g[i]));
+            for (int i = 0; i < 4; ++i) {
+              uint32_t p[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t* v = &g[k >> 1][4 * i + 2 * (k & 1)];
+                p[k] = pack_bf16(__uint_as_float(v[0]), __uint_as_float(v[1]));
+              }
+              put_frag(stg, i, p[0], p[1], p[2], p[3]);
+            }
+            flush_tokens(stg, (__nv_bfloat16*)ar.out[0] + o, ar.Nout, n, cols);
           }
         }
       }

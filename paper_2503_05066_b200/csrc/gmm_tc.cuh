@@ -88,6 +88,64 @@ __device__ __forceinline__ void put_piece(const uint32_t* packed, bool wait, boo
   }
 }
 
+// ---- transposing epilogue: accumulator lanes are output columns, accumulator columns are output rows (tokens)
+// 16 lanes x 32 columns of the accumulator as 8 x 8 fragments: of columns 8j .. 8j+7, thread t gets lane t/4, columns
+// 8j + 2(t%4) and the next (r[4j], r[4j+1]), and the same of lane t/4 + 8 (r[4j+2], r[4j+3]).
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// A warp's buffer: 32 tokens x 64 bytes (32 columns of 16 bits), 16-byte chunks swizzled.  Four 8 x 8 fragments of 16-bit
+// values, lanes 0..31 of tokens 8j .. 8j+7, written transposed.
+__device__ __forceinline__ void put_frag(uint32_t stg, int j, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t row = (uint32_t)(8 * j + (lane & 7)), chunk = (uint32_t)(lane >> 3);
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+               ::"r"(stg + row * 64u + ((chunk ^ ((row >> 1) & 3u)) << 4)), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ uint4 get_chunk(uint32_t stg, uint32_t row, uint32_t chunk) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(stg + row * 64u + ((chunk ^ ((row >> 1) & 3u)) << 4))
+               : "memory");
+  return v;
+}
+// The buffer's first n tokens to global memory, four lanes per token (whole 64-byte runs); `out`: first token, first of the
+// warp's columns; `cols`: columns that exist from there on (a multiple of 8; may be zero or negative).
+__device__ __forceinline__ void flush_tokens(uint32_t stg, __nv_bfloat16* out, int64_t ld, int n, int cols) {
+  const int lane = threadIdx.x & 31, chunk = lane & 3;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 8 * i + (lane >> 2);
+    const uint4 v = get_chunk(stg, (uint32_t)row, (uint32_t)chunk);
+    if (row < n && chunk * 8 < cols) *reinterpret_cast<uint4*>(out + (int64_t)row * ld + chunk * 8) = v;
+  }
+  __syncwarp();
+}
+// The same for 8-bit values, one in the low byte of each 16: two lanes per token, 16 columns each.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x6420); }
+__device__ __forceinline__ void flush_tokens_u8(uint32_t stg, uint8_t* out, int64_t ld, int n, int cols) {
+  const int lane = threadIdx.x & 31, part = lane & 1;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = 16 * i + (lane >> 1);
+    const uint4 a = get_chunk(stg, (uint32_t)row, (uint32_t)(2 * part)), b = get_chunk(stg, (uint32_t)row, (uint32_t)(2 * part + 1));
+    if (row < n && part * 16 < cols)
+      *reinterpret_cast<uint4*>(out + (int64_t)row * ld + part * 16) =
+          make_uint4(low_bytes(a.x, a.y), low_bytes(a.z, a.w), low_bytes(b.x, b.y), low_bytes(b.z, b.w));
+  }
+  __syncwarp();
+}
+
 __device__ __forceinline__ void tma2_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
