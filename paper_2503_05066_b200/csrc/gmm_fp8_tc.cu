@@ -27,10 +27,9 @@ constexpr int SF_OFF = STG8_OFF + EPI_WARPS * STG_WARP_BYTES;
 constexpr int SF_GROUP = 3 * SF_CHUNK;                    // A rows, B rows 0..127, B rows 128..255
 constexpr int SF_SLOT = SF_GROUPS * SF_GROUP;
 constexpr int TAIL8 = SF_OFF + SF_RING * SF_SLOT;
-constexpr int SMEM8 = TAIL8 + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + 2 * 2 * 128 * 4;
+constexpr int SMEM8 = TAIL8 + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + 2 * 2 * 128 * 4 + TR_BYTES;
 static_assert(SMEM8 <= 227 * 1024, "shared memory of a thread block");
 constexpr int ACC_STEP = 192;                             // columns between the two accumulators
-constexpr int OVERLAP = 64;
 
 struct F8Args {
   Segments sg;
@@ -57,7 +56,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
   int* offs = reinterpret_cast<int*>(gen + TAIL8 + 512);
   int* ends = offs + (GMM_MAX_E + 1);
   int* tile_start = ends + (GMM_MAX_E + 1);
-  uint32_t* row_max = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 4);   // [2 tiles][2 halves][128 rows]
+  uint32_t* row_max = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 1);   // (16-byte aligned) [2 tiles][2 halves][128 rows]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank();
@@ -70,7 +69,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
   auto sfull_bar = [&](int r) { return bar0 + 8u * (uint32_t)(24 + r); };
   auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(26 + r); };
   auto gfree_bar = [&](int g) { return bar0 + 8u * (uint32_t)(28 + g); };
-  const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
+  const TileRing ring{bar0 + 8u * RING_BAR, smem_u32(row_max + 512), rank, abort_flag};
 
   if (tid == 0) {
     for (int s = 0; s < NST8; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -81,7 +80,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
     }
     for (int r = 0; r < SF_RING; ++r) { mbar_init(sfull_bar(r), 2); mbar_init(sempty_bar(r), 1); }
     for (int g = 0; g < SF_GROUPS; ++g) mbar_init(gfree_bar(g), 1);
-    for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), TQ_READERS_F8); }
+    ring.init(2 + (rank == 0 ? 1 : 0) + EPI_WARPS);             // TMA thread, scales, MMA thread, epilogue warps
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -117,41 +116,24 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
 
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int tile_hi = tile_start[E];
-  const bool dyn = ar.sched != nullptr;
-  auto next_tile = [&](int j, bool whole_warp) -> int {
-    if (!dyn) { const int tile = pair + j * npairs; return tile < tile_hi ? tile : -1; }
-    return tq.get(j, whole_warp);
-  };
-  auto locate = [&](int tile, int& cursor, Tile& t) {
-    return locate_tile(tile, cursor, tile_start, offs, ends, E, N_TILE, BM2, t);
+  auto get_tile = [&](int j, bool whole_warp, Tile& t) -> bool {
+    int4 a, b;
+    if (!ring.get(j, whole_warp, a, b)) return false;
+    t.e = a.x; t.row0 = a.y; t.rows = a.z; t.n0 = a.w;
+    return true;
   };
   const int num_kb = (ar.K + QBLOCK - 1) / QBLOCK;
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
     if (elect_one()) {
-      int cursor = 0, s = 0;
+      int s = 0;
       uint32_t ph = 0;
       Tile t;
       bool ok = true;
-      const bool scheduler = dyn && rank == 0;
-      int cur = -1, claim = 0;
-      if (scheduler) {
-        cur = atomicAdd(ar.sched, 1);
-        if (cur >= tile_hi) cur = -1;
-        ok = tq.put(0, cur);
-        if (ok && cur >= 0) claim = atomicAdd(ar.sched, 1);
-      }
-      const int pub_kb = num_kb / 2;
       for (int j = 0; ok; ++j) {
-        const int tile = scheduler ? cur : next_tile(j, false);
-        if (tile < 0 || !locate(tile, cursor, t)) break;
+        if (!get_tile(j, false, t)) break;
         for (int kb = 0; kb < num_kb; ++kb) {
-          if (scheduler && kb == pub_kb) {
-            cur = claim < tile_hi ? claim : -1;
-            if (!tq.put(j + 1, cur)) { ok = false; break; }
-            if (cur >= 0) claim = atomicAdd(ar.sched, 1);
-          }
           if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
           const uint32_t bar = full_bar(s) & PEER_MASK;
           if (rank == 0) mbar_expect_tx(full_bar(s), 2 * STAGE8);
@@ -166,7 +148,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (rank == 0 && elect_one()) {
-      int cursor = 0, s = 0, r = 0, g = 0;
+      int s = 0, r = 0, g = 0;
       uint32_t it = 0, ph = 0, rph = 0, gph = 0;
       const uint32_t idesc0 = f8_idesc(256);
       const uint64_t a0 = umma_desc(tiles), b0 = umma_desc(tiles + A_BYTES);
@@ -174,8 +156,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
       Tile t;
       bool ok = true;
       for (int j = 0; ok; ++j, ++it) {
-        const int tile = next_tile(j, false);
-        if (tile < 0 || !locate(tile, cursor, t)) break;
+        if (!get_tile(j, false, t)) break;
         const uint32_t b = it & 1u, use = it >> 1;
         // this accumulator has been converted, and the one before it has been read where the two overlap
         if (!mbar_wait(tempty_bar(b), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -218,15 +199,14 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
     }
   } else if (warp == 2 + EPI_WARPS) {
     // ------------------------------------------------------------ scales (both CTAs)
-    int cursor = 0, r = 0;
+    int r = 0;
     uint32_t rph = 0;
     Tile t;
     bool ok = true;
     const int nb = num_kb, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
     const int loads = scale_loads(nb, ar.xs, ar.s0, ar.s1);
     for (int j = 0; ok; ++j) {
-      const int tile = next_tile(j, true);
-      if (tile < 0 || !locate(tile, cursor, t)) break;
+      if (!get_tile(j, true, t)) break;
       const uint8_t* rows[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -259,16 +239,24 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
         if (++r == SF_RING) { r = 0; rph ^= 1u; }
       }
     }
+  } else if (warp == 3 + EPI_WARPS) {
+    // ------------------------------------------------------------ scheduler (both CTAs)
+    if (elect_one()) {
+      int cursor = 0;
+      ring.run(pair, npairs, tile_hi, ar.sched, [&](int tile, int4& a, int4&) {
+        Tile q;
+        locate_tile(tile, cursor, tile_start, offs, ends, E, N_TILE, BM2, q);
+        a = make_int4(q.e, q.row0, q.rows, q.n0);
+      });
+    }
   } else {
     // ------------------------------------------------------------ epilogue (both CTAs, own 128 rows)
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    int cursor = 0;
     uint32_t it = 0;
     Tile t;
     uint8_t* stg = gen + STG8_OFF + (warp - 2) * STG_WARP_BYTES;
     for (int j = 0;; ++j, ++it) {
-      const int tile = next_tile(j, true);
-      if (tile < 0 || !locate(tile, cursor, t)) break;
+      if (!get_tile(j, true, t)) break;
       const uint32_t b = it & 1u, use = it >> 1;
       bool ready = mbar_wait(tfull_bar(b), use & 1u, abort_flag);
       ready = __all_sync(0xffffffffu, ready);

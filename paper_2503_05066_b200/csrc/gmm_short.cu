@@ -30,8 +30,8 @@ struct ShapeT {
   static constexpr int NX = KIND == T_HID ? 2 : 1;                             // token tiles per stage
   static constexpr int KE = FP8 ? 128 : 64;                                    // reduction steps per k-block: 128 bytes
   static constexpr int EW = 8;                                                 // epilogue warps
-  static constexpr int THREADS = 64 + EW * 32 + (FP8 ? 32 : 0);
-  static constexpr int READERS = 2 + 2 * EW + (FP8 ? 2 : 0);                   // of the tile queue
+  static constexpr int THREADS = 64 + EW * 32 + 32 + (FP8 ? 32 : 0);           // roles, scheduler, scales
+  static constexpr int READERS = 1 + EW + (FP8 ? 1 : 0);                       // of the tile ring, and the leader's MMA thread
   static constexpr int COLS = FP8 ? SF_TMEM : 512;                             // tensor-memory columns for accumulators
   static constexpr int SF_GROUP = 4 * SF_CHUNK;                                // tokens 0..127, 128..255, weights, second weights
   static constexpr int SF_SLOT = SF_GROUPS * SF_GROUP;
@@ -40,7 +40,7 @@ struct ShapeT {
   static constexpr int SF_OFF = RING + EW * STG_WARP_BYTES;
   static constexpr int TAIL = SF_OFF + (FP8 ? SF_RING * SF_SLOT : 0);
   static constexpr int RED = KIND == T_F8SW ? 2 * 2 * 4 * 32 * 4 : 0;
-  static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + RED;
+  static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + RED + TR_BYTES;
   static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
 };
 constexpr int MAX_NST = 12;
@@ -77,7 +77,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   int* offs = reinterpret_cast<int*>(gen + S::TAIL + 512);
   int* ends = offs + (GMM_MAX_E + 1);
   int* tile_start = ends + (GMM_MAX_E + 1);
-  uint32_t* red = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 4);       // T_F8SW: [2][2 warp groups][4][32]
+  uint32_t* red = reinterpret_cast<uint32_t*>(tile_start + (GMM_MAX_E + 1) + 1);       // (16-byte aligned) T_F8SW: [2][2 warp groups][4][32]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank();
@@ -89,7 +89,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   auto sfull_bar = [&](int r) { return bar0 + 8u * (uint32_t)(28 + r); };
   auto sempty_bar = [&](int r) { return bar0 + 8u * (uint32_t)(30 + r); };
   auto gfree_bar = [&](int g) { return bar0 + 8u * (uint32_t)(32 + g); };
-  const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
+  const TileRing ring{bar0 + 8u * RING_BAR, smem_u32(red) + S::RED, rank, abort_flag};
   const int nst = ar.nst, tt = ar.tt, bufs = ar.bufs;
   const uint32_t x_bytes = (uint32_t)ar.tb * 128u;
   const uint32_t stage = (uint32_t)(NACC * A_BYTES) + (uint32_t)S::NX * x_bytes;
@@ -99,7 +99,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * EW * 32); }
     for (int r = 0; r < SF_RING; ++r) { mbar_init(sfull_bar(r), 2); mbar_init(sempty_bar(r), 1); }
     for (int g = 0; g < SF_GROUPS; ++g) mbar_init(gfree_bar(g), 1);
-    for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), S::READERS); }
+    ring.init(S::READERS + (rank == 0 ? 1 : 0));
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -135,24 +135,10 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
 
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int tile_hi = tile_start[E];
-  const bool dyn = ar.sched != nullptr;
-  auto next_tile = [&](int j, bool whole_warp) -> int {
-    if (!dyn) { const int tile = pair + j * npairs; return tile < tile_hi ? tile : -1; }
-    return tq.get(j, whole_warp);
-  };
-  // Tiles of a segment: token block fastest (pairs side by side share a weight tile through L2), then weight block.
-  auto locate = [&](int tile, int& cursor, STile& t) -> bool {
-    while (cursor < E && tile >= tile_start[cursor + 1]) ++cursor;
-    if (cursor >= E) return false;
-    const int local = tile - tile_start[cursor], cnt = ends[cursor] - offs[cursor];
-    const int ntb = (cnt + tt - 1) / tt;
-    const int per = ((cnt + ntb - 1) / ntb + 15) & ~15;              // equal token blocks of whole MMA steps
-    const int wb = local / ntb, tbk = local - wb * ntb;
-    t.e = cursor;
-    t.row0 = offs[cursor] + tbk * per;
-    t.rows = max(0, min(per, cnt - tbk * per));                      // (rounding may leave the last block empty)
-    t.nt = max(16, (t.rows + 15) & ~15);
-    t.w0 = wb * 256;
+  auto get_tile = [&](int j, bool whole_warp, STile& t) -> bool {
+    int4 a, b;
+    if (!ring.get(j, whole_warp, a, b)) return false;
+    t.e = a.x; t.row0 = a.y; t.rows = a.z; t.nt = a.w; t.w0 = b.x;
     return true;
   };
   const int kbs = (ar.K + S::KE - 1) / S::KE;
@@ -161,30 +147,15 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
     if (elect_one()) {
-      int cursor = 0, s = 0;
+      int s = 0;
       uint32_t ph = 0;
       STile t;
       bool ok = true;
-      const bool scheduler = dyn && rank == 0;
-      int cur = -1, claim = 0;
-      if (scheduler) {
-        cur = atomicAdd(ar.sched, 1);
-        if (cur >= tile_hi) cur = -1;
-        ok = tq.put(0, cur);
-        if (ok && cur >= 0) claim = atomicAdd(ar.sched, 1);
-      }
-      const int pub_kb = num_kb / 2;
       for (int j = 0; ok; ++j) {
-        const int tile = scheduler ? cur : next_tile(j, false);
-        if (tile < 0 || !locate(tile, cursor, t)) break;
+        if (!get_tile(j, false, t)) break;
         const int w = t.w0 + (int)rank * BM;                     // this CTA's 128 weight rows
         const int x = t.row0 + (int)rank * (t.nt >> 1);          // and its half of the tokens
         for (int kb = 0; kb < num_kb; ++kb) {
-          if (scheduler && kb == pub_kb) {
-            cur = claim < tile_hi ? claim : -1;
-            if (!tq.put(j + 1, cur)) { ok = false; break; }
-            if (cur >= 0) claim = atomicAdd(ar.sched, 1);
-          }
           if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
           const uint32_t bar = full_bar(s) & PEER_MASK;
           if (rank == 0) mbar_expect_tx(full_bar(s), 2u * stage);
@@ -215,7 +186,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (rank == 0 && elect_one()) {
-      int cursor = 0, s = 0, r = 0, b = 0, g = 0;
+      int s = 0, r = 0, b = 0, g = 0;
       uint32_t ph = 0, rph = 0, bph = 0, gph = 0;
       const uint64_t w0 = W_MN ? umma_desc_mn(tiles) : umma_desc(tiles);
       const uint64_t x0 = umma_desc(tiles + (uint32_t)(NACC * A_BYTES));
@@ -225,8 +196,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
       STile t;
       bool ok = true;
       for (int j = 0; ok; ++j) {
-        const int tile = next_tile(j, false);
-        if (tile < 0 || !locate(tile, cursor, t)) break;
+        if (!get_tile(j, false, t)) break;
         const uint32_t idesc = FP8 ? f8_idesc(t.nt) : pair_idesc(t.nt, W_MN, false), idesc2 = pair_idesc(t.nt, true, false);
         if (!mbar_wait(tempty_bar(b), bph ^ 1u, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -280,17 +250,32 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
         if (++b == bufs) { b = 0; bph ^= 1u; }
       }
     }
-  } else if (FP8 && warp == 2 + EW) {
+  } else if (warp == 2 + EW) {
+    // ------------------------------------------------------------ scheduler (both CTAs)
+    // Tiles of a segment: token block fastest (pairs side by side share a weight tile through L2), then weight block.
+    if (elect_one()) {
+      int cursor = 0;
+      ring.run(pair, npairs, tile_hi, ar.sched, [&](int tile, int4& a, int4& b) {
+        while (tile >= tile_start[cursor + 1]) ++cursor;
+        const int local = tile - tile_start[cursor], cnt = ends[cursor] - offs[cursor];
+        const int ntb = (cnt + tt - 1) / tt;
+        const int per = ((cnt + ntb - 1) / ntb + 15) & ~15;              // equal token blocks of whole MMA steps
+        const int wb = local / ntb, r0 = (local - wb * ntb) * per;
+        const int rows = min(per, cnt - r0);                             // at least one: (ntb - 1) * per < cnt
+        a = make_int4(cursor, offs[cursor] + r0, rows, (rows + 15) & ~15);
+        b = make_int4(wb * 256, 0, 0, 0);
+      });
+    }
+  } else if (FP8 && warp == 3 + EW) {
     // ------------------------------------------------------------ scales (both CTAs)
-    int cursor = 0, r = 0;
+    int r = 0;
     uint32_t rph = 0;
     STile t;
     bool ok = true;
     const int nb = kbs, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
     const int loads = scale_loads(nb, ar.xs, ar.s0, ar.s1);
     for (int j = 0; ok; ++j) {
-      const int tile = next_tile(j, true);
-      if (tile < 0 || !locate(tile, cursor, t)) break;
+      if (!get_tile(j, true, t)) break;
       const int64_t blk = (int64_t)t.e * wb + min(t.w0 / QBLOCK + (int)rank, wb - 1);
       for (int k = 0; ok && k < nb; k += 16) {
         uint4 a[8];
@@ -323,13 +308,12 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   } else {
     // ------------------------------------------------------------ epilogue (both CTAs, own 128 weight rows)
     const int quarter = warp & 3, sub = (warp - 2) >> 2;         // lane quarter; this warp's share of the token chunks
-    int cursor = 0, b = 0;
+    int b = 0;
     uint32_t bph = 0, flip = 0;
     STile t;
     const uint32_t stg = tiles + (uint32_t)(S::STG_OFF + (warp - 2) * STG_WARP_BYTES);
     for (int j = 0;; ++j) {
-      const int tile = next_tile(j, true);
-      if (tile < 0 || !locate(tile, cursor, t)) break;
+      if (!get_tile(j, true, t)) break;
       bool ready = mbar_wait(tfull_bar(b), bph, abort_flag);
       ready = __all_sync(0xffffffffu, ready);
       if (KIND == T_F8SW) ready = group_all(1 + sub, 128, ready);    // the four warps of a token chunk stop together

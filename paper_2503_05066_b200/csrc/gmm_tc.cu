@@ -66,15 +66,18 @@ struct Shape {
   static constexpr int N_TILE = KIND == HID ? 128 : 256;
   static constexpr int STG_OFF = NST * STAGE;
   static constexpr int TAIL = STG_OFF + EPI_WARPS * STG;
-  static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16;
+  static constexpr int SMEM = TAIL + 1024 + 512 + 3 * (GMM_MAX_E + 1) * 4 + 16 + TR_BYTES;
   static constexpr int BUFS = KIND == HID ? 1 : 2;                   // accumulators of 256 columns, or three of 128
 };
 static_assert(Shape<HID>::SMEM <= 227 * 1024 && Shape<FWD>::SMEM <= 227 * 1024, "shared memory of a thread block");
 
-struct GTile { int e, row0, rows, n0, p, num_kb; };      // rows: valid rows of the tile from row0 (DW: of the output)
+// rows: valid rows of the tile from row0 (DW: of the output); k0: first row of the expert
+struct GTile { int e, row0, rows, n0, p, num_kb, k0; };
+
+constexpr int GMM_THREADS = TC_THREADS + 32;             // one more warp: the scheduler
 
 template <int KIND, typename TO>
-__global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ GmmMaps mp, const __grid_constant__ GmmArgs ar) {
+__global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm2(const __grid_constant__ GmmMaps mp, const __grid_constant__ GmmArgs ar) {
   using S = Shape<KIND>;
   constexpr int NST = S::NST, N_TILE = S::N_TILE, BM2 = 2 * BM;
   constexpr bool A_MN = KIND == DW, B_MN = KIND == DX || KIND == DX2 || KIND == DW;
@@ -84,7 +87,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
   const uint32_t tiles = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (tiles - raw);
   uint64_t* bars = reinterpret_cast<uint64_t*>(gen + S::TAIL);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 52);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* offs = reinterpret_cast<int*>(gen + S::TAIL + 512);
   int* ends = offs + (GMM_MAX_E + 1);
@@ -97,13 +100,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
   auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(MAX_STAGES + s); };
   auto tfull_bar = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MAX_STAGES + b); };
   auto tempty_bar = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MAX_STAGES + 2 + b); };
-  const TileQueue<true> tq{bar0 + 8u * 40u, bar0 + 8u * 44u, bar0 + 8u * 48u, rank, abort_flag};
+  const TileRing ring{bar0 + 8u * RING_BAR, smem_u32(tile_start + (GMM_MAX_E + 1) + 1) /* 3 * 257 + 1 ints: 16-byte aligned */,
+                      rank, abort_flag};
 
   // set-up that touches no global memory comes before the wait for the previous kernel
   if (tid == 0) {
     for (int s = 0; s < NST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int b = 0; b < S::BUFS; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * EPI_WARPS * 32); }
-    for (int i = 0; i < TQ; ++i) { mbar_init(tq.full(i), 1); mbar_init(tq.empty(i), TQ_READERS_PAIR); }
+    ring.init(1 + (rank == 0 ? 1 : 0) + EPI_WARPS);             // TMA thread, MMA thread, epilogue warps
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -114,7 +118,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
   }
   wait_for_previous_kernel();
   const int E = ar.sg.E;
-  for (int i = tid; i < E; i += TC_THREADS) { offs[i] = seg_at(ar.sg, i); ends[i] = max(offs[i], seg_at(ar.sg, i + 1)); }
+  for (int i = tid; i < E; i += GMM_THREADS) { offs[i] = seg_at(ar.sg, i); ends[i] = max(offs[i], seg_at(ar.sg, i + 1)); }
   __syncthreads();
   int per_e = 0;                                                // DW: tiles of one expert
   if (KIND == DW)
@@ -142,66 +146,24 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
 
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int tile_hi = KIND == DW ? E * per_e : tile_start[E];
-  const bool dyn = ar.sched != nullptr;
-  auto next_tile = [&](int j, bool whole_warp) -> int {         // every role but the scheduler
-    if (!dyn) { const int tile = pair + j * npairs; return tile < tile_hi ? tile : -1; }
-    return tq.get(j, whole_warp);
-  };
-  auto locate = [&](int tile, int& cursor, GTile& t) -> bool {
-    if (KIND == DW) {
-      t.e = tile / per_e;
-      if (t.e >= E) return false;
-      int local = tile - t.e * per_e;
-      t.p = 0;
-      int nmb = (ar.M[0] + 255) >> 8;
-      while (t.p + 1 < ar.count) {
-        const int here = nmb * ((ar.N[t.p] + 255) >> 8);
-        if (local < here) break;
-        local -= here;
-        ++t.p;
-        nmb = (ar.M[t.p] + 255) >> 8;
-      }
-      const int nb = local / nmb, mb = local - nb * nmb;
-      t.row0 = mb * BM2;
-      t.rows = min(BM2, ar.M[t.p] - t.row0);
-      t.n0 = nb * 256;
-      t.num_kb = (ends[t.e] - offs[t.e] + BK - 1) / BK;
-      return true;
-    }
-    Tile q;
-    if (!locate_tile(tile, cursor, tile_start, offs, ends, E, N_TILE, BM2, q)) return false;
-    t.e = q.e; t.row0 = q.row0; t.rows = q.rows; t.n0 = q.n0; t.p = 0;
-    t.num_kb = (ar.K + BK - 1) / BK * (KIND == DX2 ? 2 : 1);
+  auto get_tile = [&](int j, bool whole_warp, GTile& t) -> bool {
+    int4 a, b;
+    if (!ring.get(j, whole_warp, a, b)) return false;
+    t.e = a.x; t.row0 = a.y; t.rows = a.z; t.n0 = a.w;
+    t.p = b.x; t.num_kb = b.y; t.k0 = b.z;
     return true;
   };
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
     if (elect_one()) {
-      int cursor = 0, s = 0;
+      int s = 0;
       uint32_t ph = 0;
       GTile t;
       bool ok = true;
-      // The leader's producer is the pair's scheduler; it publishes the next tile halfway through the
-      // loads of the current one and asks the counter for the one after (see k_ffn_tc2).
-      const bool scheduler = dyn && rank == 0;
-      int cur = -1, claim = 0;
-      if (scheduler) {
-        cur = atomicAdd(ar.sched, 1);
-        if (cur >= tile_hi) cur = -1;
-        ok = tq.put(0, cur);
-        if (ok && cur >= 0) claim = atomicAdd(ar.sched, 1);
-      }
       int mapped = -1;                                          // DW: expert whose maps were last acquired
       for (int j = 0; ok; ++j) {
-        const int tile = scheduler ? cur : next_tile(j, false);
-        if (tile < 0 || !locate(tile, cursor, t)) break;
-        auto publish = [&]() {
-          cur = claim < tile_hi ? claim : -1;
-          if (!tq.put(j + 1, cur)) { ok = false; return; }
-          if (cur >= 0) claim = atomicAdd(ar.sched, 1);
-        };
-        const int pub_kb = t.num_kb / 2;
+        if (!get_tile(j, false, t)) break;
         const CUtensorMap *ma = &mp.a0, *mb = &mp.b0;
         if (KIND == DW) {
           ma = ar.maps + (size_t)ar.ia[t.p] * E + t.e;
@@ -214,7 +176,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
         }
         const int half_kb = KIND == DX2 ? t.num_kb / 2 : t.num_kb;
         for (int kb = 0; kb < t.num_kb; ++kb) {
-          if (scheduler && kb == pub_kb) { publish(); if (!ok) break; }
           if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
           const uint32_t bar = full_bar(s) & PEER_MASK;         // the leader's barrier counts both CTAs' bytes
           if (rank == 0) mbar_expect_tx(full_bar(s), 2 * S::STAGE);
@@ -230,7 +191,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
             tma2_load_2d(a_dst, second ? &mp.a1 : ma, k, m0, bar);
             load_mn(b_dst, second ? &mp.b1 : mb, ar.wide_b, n, k, t.e, bar);
           } else if constexpr (KIND == DW) {
-            const int r = offs[t.e] + kb * BK, n = t.n0 + (int)rank * 128;
+            const int r = t.k0 + kb * BK, n = t.n0 + (int)rank * 128;
             load_mn(a_dst, ma, (ar.wide_a >> t.p) & 1, m0, r, bar);
             load_mn(b_dst, mb, (ar.wide_b >> t.p) & 1, n, r, bar);
           } else {
@@ -243,13 +204,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
           }
           if (++s == NST) { s = 0; ph ^= 1u; }
         }
-        if (scheduler && ok && t.num_kb == 0) publish();
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (rank == 0 && elect_one()) {
-      int cursor = 0, s = 0;
+      int s = 0;
       uint32_t it = 0, ph = 0;
       const uint32_t i0 = pair_idesc(256, A_MN, B_MN), i1 = pair_idesc(128, false, true);
       const uint64_t a0 = A_MN ? umma_desc_mn(tiles) : umma_desc(tiles);
@@ -261,8 +221,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
       GTile t;
       bool ok = true;
       for (int j = 0; ok; ++j, ++it) {
-        const int tile = next_tile(j, false);
-        if (tile < 0 || !locate(tile, cursor, t)) break;
+        if (!get_tile(j, false, t)) break;
         const uint32_t b = S::BUFS == 2 ? it & 1u : 0u, use = S::BUFS == 2 ? it >> 1 : it;
         if (!mbar_wait(tempty_bar(b), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -283,16 +242,39 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_gmm2(const __grid_constant__ 
         if (ok) umma2_commit_both(tfull_bar(b));
       }
     }
+  } else if (warp == 2 + EPI_WARPS) {
+    // ------------------------------------------------------------ scheduler (both CTAs)
+    if (elect_one()) {
+      int cursor = 0;
+      ring.run(pair, npairs, tile_hi, ar.sched, [&](int tile, int4& a, int4& b) {
+        if (KIND == DW) {
+          const int e = tile / per_e;
+          int local = tile - e * per_e, p = 0, nmb = (ar.M[0] + 255) >> 8;
+          while (p + 1 < ar.count) {
+            const int here = nmb * ((ar.N[p] + 255) >> 8);
+            if (local < here) break;
+            local -= here;
+            nmb = (ar.M[++p] + 255) >> 8;
+          }
+          const int nb = local / nmb, m0 = (local - nb * nmb) * BM2;
+          a = make_int4(e, m0, min(BM2, ar.M[p] - m0), nb * 256);
+          b = make_int4(p, (ends[e] - offs[e] + BK - 1) / BK, offs[e], 0);
+        } else {
+          Tile q;
+          locate_tile(tile, cursor, tile_start, offs, ends, E, N_TILE, BM2, q);
+          a = make_int4(q.e, q.row0, q.rows, q.n0);
+          b = make_int4(0, (ar.K + BK - 1) / BK * (KIND == DX2 ? 2 : 1), 0, 0);
+        }
+      });
+    }
   } else {
     // ------------------------------------------------------------ epilogue (both CTAs, own 128 rows)
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    int cursor = 0;
     uint32_t it = 0;
     GTile t;
     uint8_t* stg = gen + S::STG_OFF + (warp - 2) * S::STG;
     for (int j = 0;; ++j, ++it) {
-      const int tile = next_tile(j, true);
-      if (tile < 0 || !locate(tile, cursor, t)) break;
+      if (!get_tile(j, true, t)) break;
       const uint32_t b = S::BUFS == 2 ? it & 1u : 0u, use = S::BUFS == 2 ? it >> 1 : it;
       bool ready = mbar_wait(tfull_bar(b), use & 1u, abort_flag);
       ready = __all_sync(0xffffffffu, ready);
@@ -386,7 +368,7 @@ int launch(const GmmMaps& mp, const GmmArgs& ar, cudaStream_t st) {
   if (err != cudaSuccess) return note_cuda(err);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
-  cfg.blockDim = dim3(TC_THREADS);
+  cfg.blockDim = dim3(GMM_THREADS);
   cfg.dynamicSmemBytes = Shape<KIND>::SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];

@@ -201,6 +201,84 @@ __device__ __forceinline__ void load_mn(uint32_t dst, const CUtensorMap* m, bool
   }
 }
 
+// ---------------------------------------------------------------- tile ring
+// One thread of its own warp (the scheduler) picks a CTA's tiles, works out where they lie and hands each on as a record of
+// eight ints through a ring in shared memory; the other roles only read records.  The first tile of a pair is its
+// index; with a counter the further ones are claimed from it by the leader's scheduler, which passes them to the
+// peer's through a two-deep mailbox.  Decoding a tile and claiming the next takes about 1300 cycles; inside the TMA
+// thread that was a quarter of a weight-gradient tile's time.
+// Four records: one each for epilogue, MMAs and loads, and one ahead.
+constexpr int TR = 4;
+constexpr int TR_BYTES = TR * 32;
+struct TileRing {
+  uint32_t bar0;                     // barriers: full[TR], empty[TR], xfull[2], xempty[2] (leader's used), then two ints
+  uint32_t rec0;                     // records
+  uint32_t rank;
+  volatile int* abort_flag;
+  __device__ __forceinline__ uint32_t full(int j) const { return bar0 + 8u * (uint32_t)(j & (TR - 1)); }
+  __device__ __forceinline__ uint32_t empty(int j) const { return bar0 + 8u * (uint32_t)(TR + (j & (TR - 1))); }
+  __device__ __forceinline__ uint32_t xfull(int q) const { return bar0 + 8u * (uint32_t)(2 * TR + (q & 1)); }
+  __device__ __forceinline__ uint32_t xempty(int q) const { return bar0 + 8u * (uint32_t)(2 * TR + 2 + (q & 1)); }
+  __device__ __forceinline__ uint32_t xval(int q) const { return bar0 + 8u * (uint32_t)(2 * TR + 4) + 4u * (uint32_t)(q & 1); }
+  __device__ __forceinline__ void init(int readers) const {
+    for (int i = 0; i < TR; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), (uint32_t)readers); }
+    for (int q = 0; q < 2; ++q) { mbar_init(xfull(q), 1); mbar_init(xempty(q), 1); }
+  }
+  // Record j for one thread or one whole warp; false when there is no further tile or a wait ran out.
+  __device__ __forceinline__ bool get(int j, bool whole_warp, int4& a, int4& b) const {
+    bool ok = mbar_wait(full(j), ((uint32_t)j / TR) & 1u, abort_flag);
+    if (whole_warp) ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return false;
+    const uint32_t r = rec0 + 32u * (uint32_t)(j & (TR - 1));
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w) : "r"(r) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(r + 16u) : "memory");
+    if (whole_warp) __syncwarp();
+    if (!whole_warp || (threadIdx.x & 31) == 0) mbar_arrive(empty(j));
+    return a.x >= 0;
+  }
+  __device__ __forceinline__ bool put(int j, const int4& a, const int4& b) const {
+    if (!mbar_wait(empty(j), (((uint32_t)j / TR) & 1u) ^ 1u, abort_flag)) return false;
+    const uint32_t r = rec0 + 32u * (uint32_t)(j & (TR - 1));
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(r), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(r + 16u), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+    mbar_arrive(full(j));
+    return true;
+  }
+  // The scheduler thread of either CTA.  decode(tile, a, b) fills the record of a tile below tile_hi; a.x >= 0.
+  template <class Decode>
+  __device__ __forceinline__ void run(int pair, int npairs, int tile_hi, int32_t* counter, const Decode& decode) const {
+    int claim = 0;
+    const bool leader = rank == 0;
+    if (counter && leader && pair < tile_hi) claim = atomicAdd(counter, 1);
+    for (int j = 0;; ++j) {
+      int tile = pair + j * npairs;
+      if (counter && j > 0) {
+        const int q = j - 1;
+        const uint32_t use = (uint32_t)q >> 1;
+        if (leader) {
+          tile = npairs + claim;
+          if (tile < tile_hi) claim = atomicAdd(counter, 1);
+          if (!mbar_wait(xempty(q), (use & 1u) ^ 1u, abort_flag)) return;
+          const uint32_t pfull = peer_addr(xfull(q));
+          asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(pfull), "r"(4u) : "memory");
+          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];"
+                       ::"r"(peer_addr(xval(q))), "r"((uint32_t)tile), "r"(pfull)
+                       : "memory");
+        } else {
+          if (!mbar_wait(xfull(q), use & 1u, abort_flag)) return;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tile) : "r"(xval(q)) : "memory");
+          mbar_arrive_cluster(xempty(q) & PEER_MASK);
+        }
+      }
+      int4 a = make_int4(-1, 0, 0, 0), b = make_int4(0, 0, 0, 0);
+      const bool any = tile < tile_hi;
+      if (any) decode(tile, a, b);
+      if (!put(j, a, b) || !any) return;
+    }
+  }
+};
+constexpr int RING_BAR = 36;              // first of the ring's barriers in a kernel's barrier block
+
 }  // namespace
 }  // namespace capmoe
 
@@ -223,8 +301,7 @@ constexpr int SF_GROUPS = 4;                // groups per slot, and in tensor me
 constexpr int SF_CHUNK = 512;               // bytes of shared memory for 128 rows
 constexpr int SF_COLS = 16;                 // tensor-memory columns per group (12 used)
 constexpr int SF_TMEM = 448;                // first column of the scales
-constexpr int F8_THREADS = TC_THREADS + 32; // one more warp: it stages the scales
-constexpr int TQ_READERS_F8 = TQ_READERS_PAIR + 2;
+constexpr int F8_THREADS = TC_THREADS + 64; // two more warps: scales and scheduler
 
 __device__ __forceinline__ uint32_t f8_idesc(int n) {     // D = fp32, A = B = e4m3, K-major, ue8m0 scales, M = 256
   return (1u << 23) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
