@@ -469,7 +469,7 @@ def _experts(where: str, offsets) -> int:
 
 def _out(where: str, t, shape, dtype, like):
     if t is None:
-        return torch.empty(shape, device=like.device, dtype=dtype)
+        return like.new_empty(shape, dtype=dtype)
     if t.shape != shape or t.dtype != dtype:
         _refuse(where, f"output must be {dtype} {tuple(shape)}")
     return t
@@ -573,7 +573,7 @@ def quantize_rows(x, offsets=None, out=None, stream=None):
         _refuse(where, "x [rows,d] expected")
     rows, d = x.shape
     q, scale = (None, None) if out is None else out
-    q = _out(where, q, (rows, d), FP8, x)
+    q = torch.empty_like(x, dtype=FP8) if q is None else _out(where, q, (rows, d), FP8, x)
     scale = _out(where, scale, (rows, _blocks(d)), SCALE, x)
     n_rows = None
     if offsets is not None:

@@ -1,10 +1,14 @@
 // Plain-FMA tile product shared by the grouped products' fp32, odd-size and 8-bit fallback kernels:
 // C[TM, 64] += A[TM, K] B[64, K]^T with fp32 accumulation, operands read through small loader types that
-// hide storage type, major order and block scales.  256 threads, each a TM/16 x 4 micro-tile.  fp32 operands are
-// fetched element by element with cp.async into a ring of four k-steps (rows need no alignment, and the copies
-// transpose on the way); other types go through registers, one k-step ahead.
-// The fp32 layers this serves have a few hundred tiles at most, one or two per SM, so latency, not FMA rate, is what
-// these kernels fight: deep prefetch, and TM = 32 where 64-row tiles would leave SMs without one.
+// hide storage type, major order and block scales.
+// 256 threads in four groups of 64; each group multiplies its quarter of every k-step over the whole tile, a thread
+// with a TM/8 x 8 micro-tile (rows and columns 8 apart), and the four partial tiles are added in shared memory at the
+// end, in a fixed order.  Shared memory, not the FMA pipe, is what a plain-FMA tile product runs into (a 16-byte load
+// takes four cycles of it whatever its lanes share), so the micro-tile is as large as registers allow: with 4 x 4 ones
+// and 256 of them side by side a 1024-row product (250 x 515, 7 experts) took 24.5 us.
+// An operand is staged as it lies in memory: [index][k] when k is contiguous, [k][index] otherwise.  fp32 operands come
+// in by cp.async, three k-steps ahead, in 16-byte pieces when their rows start on 16 bytes, else in 4-byte ones; other
+// types go through registers, one k-step ahead.  TM = 32 where 64-row tiles would leave SMs without one.
 #pragma once
 #include "gmm.cuh"
 
@@ -14,7 +18,6 @@ namespace {
 constexpr int ST = 64;        // tile columns (and rows, or half of them)
 constexpr int SK = 16;        // k-step
 constexpr int SN = 256;       // threads
-constexpr int SROW = ST + 4;  // row of a staged operand: 16-byte aligned, shifted by four banks
 constexpr int SDEPTH = 4;     // k-steps in the ring
 
 // element (i, k) of an operand stored with k contiguous (KMAJ) or i contiguous
@@ -43,76 +46,161 @@ struct Coded {
   }
 };
 
-template <int TM> struct alignas(16) SimtTile { float a[SDEPTH][SK][TM + 4], b[SDEPTH][SK][SROW]; };
+// floats of one k-step of an operand of W rows (columns): [W][SK + 4] or [SK][W + 4]; both row pitches are odd multiples
+// of 16 bytes
+template <int W> constexpr int staged() { return W * (SK + 4) > SK * (W + 4) ? W * (SK + 4) : SK * (W + 4); }
+template <int TM> struct alignas(16) SimtTile { float a[SDEPTH][staged<TM>()], b[SDEPTH][staged<ST>()]; };
 
-__device__ __forceinline__ void copy4(float* dst, const float* src, bool there) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
-               "r"(there ? 4 : 0)
-               : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const float* src, int valid) {    // valid: bytes that exist, the rest is zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const float* src, int valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
 }
 
+// A thread's share of staging an fp32 operand of W rows (columns), n of which exist: source addresses are worked out once
+// and advance by a k-step (the copies' address arithmetic cost twice the FMAs' instructions when done per copy).
+template <int W, class L>
+struct Stager {
+  static constexpr int N4 = W * SK / SN;           // 4-byte copies per thread and step
+  const float* src[N4];
+  uint32_t dst0, size;                             // size: 4-byte form: bit e = copy e is inside; 16-byte form: bytes inside
+  int64_t step_len;
+  int k, K;                                        // this thread's first k of the step in hand; end of the reduction
+  bool vec, idle;
+  __device__ __forceinline__ Stager(const L& l, int n, int K_, const float* ring) : K(K_) {
+    const int tid = threadIdx.x;
+    vec = l.ld % 4 == 0 && ((uintptr_t)l.p & 15u) == 0;
+    step_len = L::k_fast ? SK : SK * l.ld;
+    size = 0;
+    if (vec) {                                     // one 16-byte piece, by the first W * 4 threads
+      const int i = L::k_fast ? tid / (SK / 4) : tid % (W / 4) * 4;
+      k = L::k_fast ? tid % (SK / 4) * 4 : tid / (W / 4);
+      idle = tid >= W * SK / 4;
+      dst0 = (uint32_t)__cvta_generic_to_shared(ring) + 4u * (uint32_t)(L::k_fast ? i * (SK + 4) + k : k * (W + 4) + i);
+      const int in = L::k_fast ? (i < n ? 4 : 0) : n - i;
+      size = in <= 0 ? 0u : in >= 4 ? 16u : 4u * (uint32_t)in;
+      src[0] = size && !idle ? l.ptr(i, k) : l.p;
+      if (!size) step_len = 0;
+    } else {
+      const int i0 = L::k_fast ? tid / SK : tid % W;
+      k = L::k_fast ? tid % SK : tid / W;
+      idle = false;
+      dst0 = (uint32_t)__cvta_generic_to_shared(ring) + 4u * (uint32_t)(L::k_fast ? i0 * (SK + 4) + k : k * (W + 4) + i0);
+#pragma unroll
+      for (int e = 0; e < N4; ++e) {
+        const int i = L::k_fast ? i0 + e * (SN / SK) : i0, kk = L::k_fast ? k : k + e * (SN / W);
+        const bool in = i < n;
+        size |= (uint32_t)in << e;
+        src[e] = in ? l.ptr(i, kk) : l.p;
+      }
+      if (!L::k_fast && !size) step_len = 0;
+    }
+  }
+  // copies the step in hand into the ring's buffer at byte offset `off` and moves on
+  __device__ __forceinline__ void step(uint32_t off) {
+    if (vec) {
+      if (!idle) {
+        const int left = K - k;
+        const uint32_t valid = L::k_fast ? (left <= 0 ? 0u : min(size, 4u * (uint32_t)min(left, 4))) : left > 0 ? size : 0u;
+        copy16(dst0 + off, src[0], (int)valid);
+        src[0] += step_len;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N4; ++e) {
+        const bool in = ((size >> e) & 1u) && k + (L::k_fast ? 0 : e * (SN / W)) < K;
+        copy4(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * (SN / SK) * (SK + 4) : e * (SN / W) * (W + 4)), src[e], in ? 4 : 0);
+        if (!L::k_fast || ((size >> e) & 1u)) src[e] += step_len;
+      }
+    }
+    k += SK;
+  }
+};
+
+// Result element (i, j) of a thread, i < TM/16, j < 4: row and column in the tile
+__device__ __forceinline__ int out_row(int i) { return (int)(threadIdx.x >> 4) + 16 * i; }
+__device__ __forceinline__ int out_col(int j) { return (int)(threadIdx.x & 15) * 4 + j; }
+constexpr int CROW = ST + 8;                        // row of a partial tile
+
+// acc += A B^T over the tile; result elements at out_row / out_col
 template <int TM, class LA, class LB>
 __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int rows, int cols, int K, SimtTile<TM>& sm,
                                              float (&acc)[TM / 16][4]) {
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  constexpr int NA = TM * SK / SN, NB = ST * SK / SN;
+  const int tid = threadIdx.x, tx = tid & 7, ty = (tid >> 3) & 7, group = tid >> 6;
+  constexpr int R = TM / 8;
   constexpr bool ring = LA::direct && LB::direct;
+  static_assert(sizeof(SimtTile<TM>) >= 2 * TM * CROW * sizeof(float), "two partial tiles fit the staging buffers");
   if (K <= 0) return;
   const int steps = (K + SK - 1) / SK;
-  auto a_k = [&](int x) { return LA::k_fast ? x % SK : x / TM; };
-  auto a_i = [&](int x) { return LA::k_fast ? x / SK : x % TM; };
-  auto b_k = [&](int x) { return LB::k_fast ? x % SK : x / ST; };
-  auto b_i = [&](int x) { return LB::k_fast ? x / SK : x % ST; };
+  float part[R][8];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[i][j] = 0.f;
   auto multiply = [&](int buf) {
+    const float *A = sm.a[buf], *B = sm.b[buf];
+    const int k0 = group * 4;
+    float a[R][4];
+    if constexpr (LA::k_fast) {
 #pragma unroll
-    for (int kk = 0; kk < SK; ++kk) {
-      float av[TM / 16];
-      if constexpr (TM == 64) {
-        const float4 a = *reinterpret_cast<const float4*>(&sm.a[buf][kk][ty * 4]);
-        av[0] = a.x; av[1] = a.y; av[2] = a.z; av[3] = a.w;
-      } else {
-        const float2 a = *reinterpret_cast<const float2*>(&sm.a[buf][kk][ty * 2]);
-        av[0] = a.x; av[1] = a.y;
+      for (int i = 0; i < R; ++i) {
+        const float4 f = *reinterpret_cast<const float4*>(A + (ty + 8 * i) * (SK + 4) + k0);
+        a[i][0] = f.x; a[i][1] = f.y; a[i][2] = f.z; a[i][3] = f.w;
       }
-      const float4 b = *reinterpret_cast<const float4*>(&sm.b[buf][kk][tx * 4]);
-      const float bv[4] = {b.x, b.y, b.z, b.w};
+    } else {
 #pragma unroll
-      for (int i = 0; i < TM / 16; ++i)
+      for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
+        for (int i = 0; i < R; ++i) a[i][kk] = A[(k0 + kk) * (TM + 4) + ty + 8 * i];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float b[4];
+      if constexpr (LB::k_fast) {
+        const float4 f = *reinterpret_cast<const float4*>(B + (tx + 8 * j) * (SK + 4) + k0);
+        b[0] = f.x; b[1] = f.y; b[2] = f.z; b[3] = f.w;
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) b[kk] = B[(k0 + kk) * (ST + 4) + tx + 8 * j];
+      }
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int i = 0; i < R; ++i) part[i][j] = fmaf(a[i][kk], b[kk], part[i][j]);
     }
   };
   __syncthreads();                                  // an earlier product may still read the buffers
   if constexpr (ring) {
-    auto issue = [&](int step) {
-      if (step < steps) {
-        const int k0 = step * SK, buf = step % SDEPTH;
-#pragma unroll
-        for (int i = 0; i < NA; ++i) {
-          const int x = tid + i * SN, k = a_k(x), r = a_i(x);
-          const bool there = r < rows && k0 + k < K;
-          copy4(&sm.a[buf][k][r], there ? la.ptr(r, k0 + k) : la.p, there);
-        }
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          const int x = tid + i * SN, k = b_k(x), c = b_i(x);
-          const bool there = c < cols && k0 + k < K;
-          copy4(&sm.b[buf][k][c], there ? lb.ptr(c, k0 + k) : lb.p, there);
-        }
+    Stager<TM, LA> sa(la, rows, K, sm.a[0]);
+    Stager<ST, LB> sb(lb, cols, K, sm.b[0]);
+    uint32_t buf = 0;                               // ring buffer of the next step to copy
+    int left = steps;                               // steps not yet copied
+    auto issue = [&]() {
+      if (left > 0) {
+        sa.step(buf * (uint32_t)sizeof(sm.a[0]));
+        sb.step(buf * (uint32_t)sizeof(sm.b[0]));
+        --left;
+        buf = buf + 1 == SDEPTH ? 0 : buf + 1;
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (int s = 0; s < SDEPTH - 1; ++s) issue(s);
+    for (int s = 0; s < SDEPTH - 1; ++s) issue();
     for (int step = 0; step < steps; ++step) {
       asm volatile("cp.async.wait_group %0;" ::"n"(SDEPTH - 2) : "memory");
       __syncthreads();                              // this step is in; the buffer of the step before it has been read
-      issue(step + SDEPTH - 1);
+      issue();
       multiply(step % SDEPTH);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
   } else {
+    constexpr int NA = TM * SK / SN, NB = ST * SK / SN;
     float ra[NA], rb[NB];
+    auto a_k = [&](int x) { return LA::k_fast ? x % SK : x / TM; };
+    auto a_i = [&](int x) { return LA::k_fast ? x / SK : x % TM; };
+    auto b_k = [&](int x) { return LB::k_fast ? x % SK : x / ST; };
+    auto b_i = [&](int x) { return LB::k_fast ? x / SK : x % ST; };
     auto fetch = [&](int k0) {
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
@@ -127,9 +215,15 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
     };
     auto put = [&](int buf) {
 #pragma unroll
-      for (int i = 0; i < NA; ++i) sm.a[buf][a_k(tid + i * SN)][a_i(tid + i * SN)] = ra[i];
+      for (int i = 0; i < NA; ++i) {
+        const int x = tid + i * SN;
+        sm.a[buf][LA::k_fast ? a_i(x) * (SK + 4) + a_k(x) : a_k(x) * (TM + 4) + a_i(x)] = ra[i];
+      }
 #pragma unroll
-      for (int i = 0; i < NB; ++i) sm.b[buf][b_k(tid + i * SN)][b_i(tid + i * SN)] = rb[i];
+      for (int i = 0; i < NB; ++i) {
+        const int x = tid + i * SN;
+        sm.b[buf][LB::k_fast ? b_i(x) * (SK + 4) + b_k(x) : b_k(x) * (ST + 4) + b_i(x)] = rb[i];
+      }
     };
     fetch(0);
     put(0);
@@ -140,6 +234,28 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
       if (step + 1 < steps) put((step + 1) & 1);    // last read two steps ago, before the previous barrier
       __syncthreads();
     }
+  }
+  // ((group 2 + group 0) + (group 3 + group 1)), in the staging buffers
+  __syncthreads();
+  float* C = &sm.a[0][0] + (group & 1) * TM * CROW;
+#pragma unroll
+  for (int turn = 1; turn >= 0; --turn) {
+    if ((group >> 1) == turn) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float& c = C[(ty + 8 * i) * CROW + tx + 8 * j];
+          c = turn ? part[i][j] : c + part[i][j];
+        }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < TM / 16; ++i) {
+    const float* c0 = &sm.a[0][0] + out_row(i) * CROW + out_col(0);
+    const float4 p = *reinterpret_cast<const float4*>(c0), q = *reinterpret_cast<const float4*>(c0 + TM * CROW);
+    acc[i][0] += p.x + q.x; acc[i][1] += p.y + q.y; acc[i][2] += p.z + q.z; acc[i][3] += p.w + q.w;
   }
 }
 

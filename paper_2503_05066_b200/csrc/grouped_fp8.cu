@@ -13,40 +13,53 @@ namespace {
 
 constexpr int QN = 256;                    // threads of the quantisers
 
-// eight consecutive elements from p; with VEC they are 16-byte loads, else the first `left` are read
+// Eight consecutive elements of a row, kept as they are stored until they are used (half the registers of fp32 for bf16,
+// so more loads in flight): 16-byte loads with VEC, else the first `left` one by one.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+struct Eight {
+  uint32_t w[sizeof(T) * 2];
+  __device__ __forceinline__ void load(const T* p, int left) {
+    if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+        w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+      }
+    } else {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) * 2; ++i)
+        w[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : (__float_as_uint(v[2 * i % 8]) >> 16) | (__float_as_uint(v[(2 * i + 1) % 8]) & 0xffff0000u);
     }
-  } else if constexpr (VEC) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
   }
-}
-__device__ __forceinline__ uint32_t amax_bits8(const float (&v)[8]) {
-  uint32_t m = 0;                          // of non-negative floats the larger has the larger pattern; NaN is above all
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  return m;
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(uint8_t* p, int left, const float (&v)[8], uint32_t code) {
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) w[i] = 0u;
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float((i & 1) ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
+  // bit pattern of the largest magnitude: of non-negative floats the larger has the larger pattern; NaN is above all
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(at(i)) & 0x7fffffffu);
+    return m;
+  }
+};
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(uint8_t* p, int left, const Eight<T, VEC>& v, uint32_t code) {
   uint32_t lo, hi;
   if (code == (uint32_t)Q_NAN_SCALE) {
     lo = hi = 0x7f7f7f7fu;
   } else {
     const float f = inv_scale(code);
-    lo = to_e4m3x2(v[0] * f, v[1] * f) | (to_e4m3x2(v[2] * f, v[3] * f) << 16);
-    hi = to_e4m3x2(v[4] * f, v[5] * f) | (to_e4m3x2(v[6] * f, v[7] * f) << 16);
+    lo = to_e4m3x2(v.at(0) * f, v.at(1) * f) | (to_e4m3x2(v.at(2) * f, v.at(3) * f) << 16);
+    hi = to_e4m3x2(v.at(4) * f, v.at(5) * f) | (to_e4m3x2(v.at(6) * f, v.at(7) * f) << 16);
   }
   if constexpr (VEC) {
     *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
@@ -57,45 +70,46 @@ __device__ __forceinline__ void store8(uint8_t* p, int left, const float (&v)[8]
   }
 }
 
-// Rows: half a warp per block of 128 columns, QROW_U blocks per half-warp in flight.
+// Rows: half a warp per block of 128 columns, QROW_U blocks per half-warp in flight.  Bound by HBM (3 bytes per bf16
+// element).  The grid is no larger than what is resident and walks the rows that exist, so that *n_rows is read once per
+// warp and not in front of every load.
 constexpr int QROW_U = 4;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(QN)
-k_quantize_rows(const T* __restrict__ x, const int32_t* __restrict__ n_rows, int64_t rows, int d, uint8_t* __restrict__ q,
+k_quantize_rows(const T* __restrict__ x, const int32_t* __restrict__ n_rows, int rows, int d, int per_row, uint8_t* __restrict__ q,
                 uint8_t* __restrict__ scale) {
   allow_next_kernel();
   wait_for_previous_kernel();
   const int lane = threadIdx.x & 31, sub = lane & 15;
-  const int nb = (d + QBLOCK - 1) / QBLOCK, per_row = (nb + 2 * QROW_U - 1) / (2 * QROW_U);
-  const int64_t unit = (int64_t)blockIdx.x * (QN / 32) + (threadIdx.x >> 5);
-  const int64_t r = unit / per_row;
-  if (r >= rows || (n_rows && r >= *n_rows)) return;
-  const int b0 = (int)(unit - r * per_row) * 2 * QROW_U + (lane >> 4);
-  float v[QROW_U][8];
+  const int nb = (d + QBLOCK - 1) / QBLOCK;
+  if (n_rows) rows = min(rows, max(*n_rows, 0));
+  const int64_t units = (int64_t)rows * per_row, step = (int64_t)gridDim.x * (QN / 32);
+  for (int64_t unit = (int64_t)blockIdx.x * (QN / 32) + (threadIdx.x >> 5); unit < units; unit += step) {
+    const int64_t r = per_row == 1 ? unit : unit / per_row;
+    const int b0 = (int)(unit - r * per_row) * 2 * QROW_U + (lane >> 4);
+    Eight<T, VEC> v[QROW_U];
 #pragma unroll
-  for (int u = 0; u < QROW_U; ++u) {
-    const int c = (b0 + 2 * u) * QBLOCK + sub * 8;
-    if (c < d) load8<T, VEC>(x + r * d + c, d - c, v[u]);
-    else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+    for (int u = 0; u < QROW_U; ++u) {
+      const int c = (b0 + 2 * u) * QBLOCK + sub * 8;
+      if (c < d) v[u].load(x + r * d + c, d - c);
+      else v[u].clear();
     }
-  }
 #pragma unroll
-  for (int u = 0; u < QROW_U; ++u) {
-    const int b = b0 + 2 * u, c = b * QBLOCK + sub * 8;
-    uint32_t m = amax_bits8(v[u]);
+    for (int u = 0; u < QROW_U; ++u) {
+      const int b = b0 + 2 * u, c = b * QBLOCK + sub * 8;
+      uint32_t m = v[u].top();
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const uint32_t code = scale_code(m);
-    if (c < d) store8<VEC>(q + r * d + c, d - c, v[u], code);
-    if (sub == 0 && b < nb) scale[r * nb + b] = (uint8_t)code;
+      for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const uint32_t code = scale_code(m);
+      if (c < d) store8(q + r * d + c, d - c, v[u], code);
+      if (sub == 0 && b < nb) scale[r * nb + b] = (uint8_t)code;
+    }
   }
 }
 
-// Weights: one CTA per 128 x 128 block, the whole block in registers (eight passes of 16 rows).
+// Weights: one CTA per 128 x 128 block, the whole block in registers (eight passes of 16 rows).  Bound by HBM.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(QN)
+__global__ void __launch_bounds__(QN, sizeof(T) == 2 ? 3 : 2)
 k_quantize_weights(const T* __restrict__ w, int n, int d, uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
   allow_next_kernel();
   wait_for_previous_kernel();
@@ -106,20 +120,17 @@ k_quantize_weights(const T* __restrict__ w, int n, int d, uint8_t* __restrict__ 
   const int64_t e = blk / db / nb;
   const int c = jb * QBLOCK + (threadIdx.x & 15) * 8, r0 = ib * QBLOCK + (threadIdx.x >> 4);
   const int64_t base = e * n * d;
-  float v[8][8];
-  uint32_t m = 0;
+  Eight<T, VEC> v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = r0 + 16 * i;
-    if (r < n && c < d) load8<T, VEC>(w + base + (int64_t)r * d + c, d - c, v[i]);
-    else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
-    }
-    m = max(m, amax_bits8(v[i]));
+    if (r < n && c < d) v[i].load(w + base + (int64_t)r * d + c, d - c);
+    else v[i].clear();
   }
+  uint32_t m = 0;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int i = 0; i < 8; ++i) m = max(m, v[i].top());
+  m = __reduce_max_sync(0xffffffffu, m);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
   __syncthreads();
 #pragma unroll
@@ -128,14 +139,14 @@ k_quantize_weights(const T* __restrict__ w, int n, int d, uint8_t* __restrict__ 
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = r0 + 16 * i;
-    if (r < n && c < d) store8<VEC>(q + base + (int64_t)r * d + c, d - c, v[i], code);
+    if (r < n && c < d) store8(q + base + (int64_t)r * d + c, d - c, v[i], code);
   }
   if (threadIdx.x == 0) scale[blk] = (uint8_t)code;
 }
 
 // y = x W^T from codes; SWIGLU: silu(x W_g^T) * (x W_u^T)
 template <typename TO, bool SWIGLU>
-__global__ void __launch_bounds__(SN)
+__global__ void __launch_bounds__(SN, 2)
 k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const uint8_t* __restrict__ w0,
          const uint8_t* __restrict__ s0, const uint8_t* __restrict__ w1, const uint8_t* __restrict__ s1, TO* __restrict__ out,
          Segments sg, int K, int Nout) {
@@ -154,12 +165,11 @@ k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const u
     clear_acc(up);
     tile_product<ST>(la, Coded<QBLOCK>{w1 + wo, s1 + so, K, kb}, t.rows, Nout - col0, K, sm, up);
   }
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = ty * 4 + i, c = col0 + tx * 4 + j;
+      const int r = out_row(i), c = col0 + out_col(j);
       float v = acc[i][j];
       if (SWIGLU) v = v / (1.0f + expf(-v)) * up[i][j];
       if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<TO>(v);
@@ -168,15 +178,14 @@ k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const u
 
 template <typename T>
 int quantize_rows_run(const void* x, const int32_t* n_rows, int64_t rows, int d, void* q, void* scale, cudaStream_t st) {
-  const int64_t units = rows * ceil_div(ceil_div(d, QBLOCK), 2 * QROW_U);
-  const int64_t grid = ceil_div(units, QN / 32);
-  if (grid >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
+  const int per_row = (int)ceil_div(ceil_div(d, QBLOCK), 2 * QROW_U);
+  const int64_t want = ceil_div(rows * per_row, QN / 32), most = (int64_t)sm_count() * 6;
+  const unsigned grid = (unsigned)(want < most ? want : most);
   // 16-byte loads of eight columns need rows that start on 16 bytes; the codes' rows then start on 8
-  const bool vec = d % 8 == 0;
-  const int rc = note_cuda(vec ? launch_chained(k_quantize_rows<T, true>, (unsigned)grid, QN, 0, st, (const T*)x, n_rows, rows, d,
-                                                (uint8_t*)q, (uint8_t*)scale)
-                               : launch_chained(k_quantize_rows<T, false>, (unsigned)grid, QN, 0, st, (const T*)x, n_rows, rows,
-                                                d, (uint8_t*)q, (uint8_t*)scale));
+  const int rc = note_cuda(d % 8 == 0 ? launch_chained(k_quantize_rows<T, true>, grid, QN, 0, st, (const T*)x, n_rows, (int)rows, d,
+                                                       per_row, (uint8_t*)q, (uint8_t*)scale)
+                                      : launch_chained(k_quantize_rows<T, false>, grid, QN, 0, st, (const T*)x, n_rows, (int)rows, d,
+                                                       per_row, (uint8_t*)q, (uint8_t*)scale));
   count_launch(1);
   return rc;
 }

@@ -15,7 +15,7 @@ namespace {
 enum { DIR_FWD = 0, DIR_DX = 1 };
 
 template <typename T, int DIR, int TM>
-__global__ void __launch_bounds__(SN)
+__global__ void __launch_bounds__(SN, 2)
 k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out, Segments sg, int K, int Nout) {
   wait_for_previous_kernel();
   __shared__ SimtTile<TM> sm;
@@ -29,12 +29,11 @@ k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out,
   const Dense<T, true> la{A + (int64_t)t.row0 * K, K};
   if (DIR == DIR_FWD) tile_product<TM>(la, Dense<T, true>{We + (int64_t)col0 * K, K}, t.rows, Nout - col0, K, sm, acc);
   else tile_product<TM>(la, Dense<T, false>{We + col0, Nout}, t.rows, Nout - col0, K, sm, acc);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = ty * R + i, c = col0 + tx * 4 + j;
+      const int r = out_row(i), c = col0 + out_col(j);
       if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<T>(acc[i][j]);
     }
 }
@@ -45,7 +44,7 @@ template <typename T, typename TO>
 struct DwSet { const T* P[3]; const T* Q[3]; TO* out[3]; int M[3], N[3]; };
 
 template <typename T, typename TO, int TM>
-__global__ void __launch_bounds__(SN) k_mm_dw(DwSet<T, TO> s, Segments sg) {
+__global__ void __launch_bounds__(SN, 2) k_mm_dw(DwSet<T, TO> s, Segments sg) {
   wait_for_previous_kernel();
   __shared__ SimtTile<TM> sm;
   const int p = blockIdx.z / sg.E, e = blockIdx.z - p * sg.E;
@@ -58,19 +57,18 @@ __global__ void __launch_bounds__(SN) k_mm_dw(DwSet<T, TO> s, Segments sg) {
   clear_acc(acc);
   tile_product<TM>(Dense<T, false>{s.P[p] + (int64_t)begin * M + r0, M}, Dense<T, false>{s.Q[p] + (int64_t)begin * N + c0, N},
                M - r0, N - c0, n, sm, acc);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = r0 + ty * R + i, c = c0 + tx * 4 + j;
+      const int r = r0 + out_row(i), c = c0 + out_col(j);
       if (r < M && c < N) s.out[p][((int64_t)e * M + r) * N + c] = from_float<TO>(acc[i][j]);
     }
 }
 
 // dg, du and h of the SwiGLU backward pass: three products over d with the elementwise part in registers.
 template <typename T, int TM>
-__global__ void __launch_bounds__(SN)
+__global__ void __launch_bounds__(SN, 2)
 k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __restrict__ wg, const T* __restrict__ wu,
                   const T* __restrict__ wd, T* __restrict__ dg, T* __restrict__ du, T* __restrict__ h, Segments sg, int d,
                   int F) {
@@ -87,12 +85,11 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
   tile_product<TM>(lx, Dense<T, true>{wg + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, g);
   tile_product<TM>(lx, Dense<T, true>{wu + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, u);
   tile_product<TM>(ldy, Dense<T, false>{wd + we + col0, F}, t.rows, cols, d, sm, dh);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = ty * R + i, c = col0 + tx * 4 + j;
+      const int r = out_row(i), c = col0 + out_col(j);
       if (r >= t.rows || c >= F) continue;
       const float p = 1.0f / (1.0f + expf(-g[i][j]));
       const float a = g[i][j] * p;
@@ -105,7 +102,7 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
 
 // dx = dg W_g + du W_u (weights [E, F, d])
 template <typename T, int TM>
-__global__ void __launch_bounds__(SN)
+__global__ void __launch_bounds__(SN, 2)
 k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __restrict__ wg, const T* __restrict__ wu,
              T* __restrict__ dx, Segments sg, int d, int F) {
   wait_for_previous_kernel();
@@ -119,12 +116,11 @@ k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __rest
   clear_acc(acc);
   tile_product<TM>(Dense<T, true>{dg + (int64_t)t.row0 * F, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, F, sm, acc);
   tile_product<TM>(Dense<T, true>{du + (int64_t)t.row0 * F, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, F, sm, acc);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = ty * R + i, c = col0 + tx * 4 + j;
+      const int r = out_row(i), c = col0 + out_col(j);
       if (r < t.rows && c < d) dx[(int64_t)(t.row0 + r) * d + c] = from_float<T>(acc[i][j]);
     }
 }
