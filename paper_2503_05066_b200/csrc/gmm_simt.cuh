@@ -1,24 +1,36 @@
 // Plain-FMA tile product shared by the grouped products' fp32, odd-size and 8-bit fallback kernels:
 // C[TM, 64] += A[TM, K] B[64, K]^T with fp32 accumulation, operands read through small loader types that
 // hide storage type, major order and block scales.
-// 256 threads in four groups of 64; each group multiplies its quarter of every k-step over the whole tile, a thread
-// with a TM/8 x 8 micro-tile (rows and columns 8 apart), and the four partial tiles are added in shared memory at the
+// A block is G groups of 64 threads; a k-step is 4 G long and each group multiplies its four of it over the whole tile, a
+// thread with a TM/8 x 8 micro-tile (rows and columns 8 apart); the partial tiles are added in shared memory at the
 // end, in a fixed order.  Shared memory, not the FMA pipe, is what a plain-FMA tile product runs into (a 16-byte load
-// takes four cycles of it whatever its lanes share), so the micro-tile is as large as registers allow: with 4 x 4 ones
-// and 256 of them side by side a 1024-row product (250 x 515, 7 experts) took 24.5 us.
+// takes four cycles of it whatever its lanes share), so the micro-tile is as large as registers allow.
+// The fp32 layers this serves have a few hundred tiles at most.  G = 4, two blocks to an SM, hides one block's latency
+// behind the other; when the tiles do not outnumber the SMs, G = 8 gives a tile a whole SM: of 124 blocks that could
+// share an SM the hardware puts two on some and none on others.  (1024 rows, 7 experts, 250 x 515 weights: y 15.5 us
+// with G = 4, 18.4 with 8; dx, 124 tiles, 31 and 18; with 4 x 4 micro-tiles they took 24 and 32.)
 // An operand is staged as it lies in memory: [index][k] when k is contiguous, [k][index] otherwise.  fp32 operands come
-// in by cp.async, three k-steps ahead, in 16-byte pieces when their rows start on 16 bytes, else in 4-byte ones; other
-// types go through registers, one k-step ahead.  TM = 32 where 64-row tiles would leave SMs without one.
+// in by cp.async, two or three k-steps ahead, in 16-byte pieces when their rows start on 16 bytes, else in 4-byte ones;
+// other types go through registers, one k-step ahead.  TM = 32 where 64-row tiles would leave SMs without one.
 #pragma once
 #include "gmm.cuh"
 
 namespace capmoe {
 namespace {
 
-constexpr int ST = 64;        // tile columns (and rows, or half of them)
-constexpr int SK = 16;        // k-step
-constexpr int SN = 256;       // threads
-constexpr int SDEPTH = 4;     // k-steps in the ring
+constexpr int ST = 64;        // tile columns
+// Geometry of a block: TM tile rows, G thread groups
+template <int TM_, int G_>
+struct Geo {
+  static constexpr int TM = TM_, G = G_;
+  static constexpr int SK = 4 * G;                  // k-step
+  static constexpr int SN = 64 * G;                 // threads
+  static constexpr int DEPTH = G == 8 ? 3 : 4;      // k-steps in the ring
+  static constexpr int R = TM * ST / SN / 4;        // result elements of a thread: R x 4
+  // floats of one k-step of an operand of W rows (columns): [W][SK + 4] or [SK][W + 4]; both row pitches are odd multiples
+  // of 16 bytes
+  static constexpr int staged(int W) { return W * (SK + 4) > SK * (W + 4) ? W * (SK + 4) : SK * (W + 4); }
+};
 
 // element (i, k) of an operand stored with k contiguous (KMAJ) or i contiguous
 template <typename T, bool KMAJ>
@@ -46,10 +58,7 @@ struct Coded {
   }
 };
 
-// floats of one k-step of an operand of W rows (columns): [W][SK + 4] or [SK][W + 4]; both row pitches are odd multiples
-// of 16 bytes
-template <int W> constexpr int staged() { return W * (SK + 4) > SK * (W + 4) ? W * (SK + 4) : SK * (W + 4); }
-template <int TM> struct alignas(16) SimtTile { float a[SDEPTH][staged<TM>()], b[SDEPTH][staged<ST>()]; };
+template <class GE> struct alignas(16) SimtTile { float a[GE::DEPTH][GE::staged(GE::TM)], b[GE::DEPTH][GE::staged(ST)]; };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const float* src, int valid) {    // valid: bytes that exist, the rest is zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
@@ -60,8 +69,9 @@ __device__ __forceinline__ void copy4(uint32_t dst, const float* src, int valid)
 
 // A thread's share of staging an fp32 operand of W rows (columns), n of which exist: source addresses are worked out once
 // and advance by a k-step (the copies' address arithmetic cost twice the FMAs' instructions when done per copy).
-template <int W, class L>
+template <class GE, int W, class L>
 struct Stager {
+  static constexpr int SK = GE::SK, SN = GE::SN;
   static constexpr int N4 = W * SK / SN;           // 4-byte copies per thread and step
   const float* src[N4];
   uint32_t dst0, size;                             // size: 4-byte form: bit e = copy e is inside; 16-byte form: bytes inside
@@ -118,19 +128,20 @@ struct Stager {
   }
 };
 
-// Result element (i, j) of a thread, i < TM/16, j < 4: row and column in the tile
-__device__ __forceinline__ int out_row(int i) { return (int)(threadIdx.x >> 4) + 16 * i; }
+// Result element (i, j) of a thread, i < R, j < 4: row and column in the tile
+template <class GE> __device__ __forceinline__ int out_row(int i) { return (int)(threadIdx.x >> 4) + (GE::SN / 16) * i; }
 __device__ __forceinline__ int out_col(int j) { return (int)(threadIdx.x & 15) * 4 + j; }
 constexpr int CROW = ST + 8;                        // row of a partial tile
 
 // acc += A B^T over the tile; result elements at out_row / out_col
-template <int TM, class LA, class LB>
-__device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int rows, int cols, int K, SimtTile<TM>& sm,
-                                             float (&acc)[TM / 16][4]) {
+template <class GE, class LA, class LB>
+__device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int rows, int cols, int K, SimtTile<GE>& sm,
+                                             float (&acc)[GE::R][4]) {
+  constexpr int TM = GE::TM, SK = GE::SK, SN = GE::SN, SDEPTH = GE::DEPTH;
   const int tid = threadIdx.x, tx = tid & 7, ty = (tid >> 3) & 7, group = tid >> 6;
   constexpr int R = TM / 8;
   constexpr bool ring = LA::direct && LB::direct;
-  static_assert(sizeof(SimtTile<TM>) >= 2 * TM * CROW * sizeof(float), "two partial tiles fit the staging buffers");
+  static_assert(sizeof(SimtTile<GE>) >= 2 * TM * CROW * sizeof(float), "two partial tiles fit the staging buffers");
   if (K <= 0) return;
   const int steps = (K + SK - 1) / SK;
   float part[R][8];
@@ -172,8 +183,8 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
   };
   __syncthreads();                                  // an earlier product may still read the buffers
   if constexpr (ring) {
-    Stager<TM, LA> sa(la, rows, K, sm.a[0]);
-    Stager<ST, LB> sb(lb, cols, K, sm.b[0]);
+    Stager<GE, TM, LA> sa(la, rows, K, sm.a[0]);
+    Stager<GE, ST, LB> sb(lb, cols, K, sm.b[0]);
     uint32_t buf = 0;                               // ring buffer of the next step to copy
     int left = steps;                               // steps not yet copied
     auto issue = [&]() {
@@ -235,25 +246,25 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
       __syncthreads();
     }
   }
-  // ((group 2 + group 0) + (group 3 + group 1)), in the staging buffers
+  // the even and the odd groups, one after the other from the last to the first, in the staging buffers, then both sums
   __syncthreads();
   float* C = &sm.a[0][0] + (group & 1) * TM * CROW;
 #pragma unroll
-  for (int turn = 1; turn >= 0; --turn) {
+  for (int turn = SN / 128 - 1; turn >= 0; --turn) {
     if ((group >> 1) == turn) {
 #pragma unroll
       for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           float& c = C[(ty + 8 * i) * CROW + tx + 8 * j];
-          c = turn ? part[i][j] : c + part[i][j];
+          c = turn == SN / 128 - 1 ? part[i][j] : c + part[i][j];
         }
     }
     __syncthreads();
   }
 #pragma unroll
-  for (int i = 0; i < TM / 16; ++i) {
-    const float* c0 = &sm.a[0][0] + out_row(i) * CROW + out_col(0);
+  for (int i = 0; i < GE::R; ++i) {
+    const float* c0 = &sm.a[0][0] + out_row<GE>(i) * CROW + out_col(0);
     const float4 p = *reinterpret_cast<const float4*>(c0), q = *reinterpret_cast<const float4*>(c0 + TM * CROW);
     acc[i][0] += p.x + q.x; acc[i][1] += p.y + q.y; acc[i][2] += p.z + q.z; acc[i][3] += p.w + q.w;
   }
@@ -267,12 +278,19 @@ __device__ __forceinline__ void clear_acc(float (&acc)[R][4]) {
     for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
 }
 
+template <class GE>
+__device__ __forceinline__ SimtTile<GE>& simt_tile() {
+  extern __shared__ __align__(16) uint8_t simt_smem[];
+  return *reinterpret_cast<SimtTile<GE>*>(simt_smem);
+}
+
 // The row tile that block `slot` of a launch works on: segments in order, ceil(rows / TM) tiles each.
 // Returns false when the slot lies behind the last tile.  All threads call it.
 struct RowTile { int e, row0, rows; };
-template <int TM>
+template <class GE>
 __device__ __forceinline__ bool find_row_tile(const Segments& sg, int slot, RowTile& t) {
-  __shared__ int warp_sum[SN / 32], found[3];
+  constexpr int TM = GE::TM;
+  __shared__ int warp_sum[GE::SN / 32], found[3];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int begin = 0, n = 0;
   if (tid < sg.E) { begin = seg_at(sg, tid); n = max(0, seg_at(sg, tid + 1) - begin); }

@@ -11,6 +11,7 @@
 namespace capmoe {
 namespace {
 
+using G8 = Geo<ST, 8>;                     // block of the fallback product
 constexpr int QN = 256;                    // threads of the quantisers
 
 // Eight consecutive elements of a row, kept as they are stored until they are used (half the registers of fp32 for bf16,
@@ -146,30 +147,31 @@ k_quantize_weights(const T* __restrict__ w, int n, int d, uint8_t* __restrict__ 
 
 // y = x W^T from codes; SWIGLU: silu(x W_g^T) * (x W_u^T)
 template <typename TO, bool SWIGLU>
-__global__ void __launch_bounds__(SN, 2)
+__global__ void __launch_bounds__(G8::SN)
 k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const uint8_t* __restrict__ w0,
          const uint8_t* __restrict__ s0, const uint8_t* __restrict__ w1, const uint8_t* __restrict__ s1, TO* __restrict__ out,
          Segments sg, int K, int Nout) {
   wait_for_previous_kernel();
-  __shared__ SimtTile<ST> sm;
+  SimtTile<G8>& sm = simt_tile<G8>();
   RowTile t;
-  if (!find_row_tile<ST>(sg, blockIdx.x, t)) return;
+  if (!find_row_tile<G8>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST, kb = (K + QBLOCK - 1) / QBLOCK, nb = (Nout + QBLOCK - 1) / QBLOCK;
   const Coded<1> la{xq + (int64_t)t.row0 * K, xs + (int64_t)t.row0 * kb, K, kb};
   const int64_t wo = ((int64_t)t.e * Nout + col0) * K, so = ((int64_t)t.e * nb + col0 / QBLOCK) * kb;
-  float acc[4][4], up[4][4];
+  constexpr int R = G8::R;
+  float acc[R][4], up[R][4];
   clear_acc(acc);
   // (a 64-column tile lies inside one block of 128 weight rows: one row of scales serves it)
-  tile_product<ST>(la, Coded<QBLOCK>{w0 + wo, s0 + so, K, kb}, t.rows, Nout - col0, K, sm, acc);
+  tile_product<G8>(la, Coded<QBLOCK>{w0 + wo, s0 + so, K, kb}, t.rows, Nout - col0, K, sm, acc);
   if (SWIGLU) {
     clear_acc(up);
-    tile_product<ST>(la, Coded<QBLOCK>{w1 + wo, s1 + so, K, kb}, t.rows, Nout - col0, K, sm, up);
+    tile_product<G8>(la, Coded<QBLOCK>{w1 + wo, s1 + so, K, kb}, t.rows, Nout - col0, K, sm, up);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = out_row(i), c = col0 + out_col(j);
+      const int r = out_row<G8>(i), c = col0 + out_col(j);
       float v = acc[i][j];
       if (SWIGLU) v = v / (1.0f + expf(-v)) * up[i][j];
       if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<TO>(v);
@@ -204,9 +206,12 @@ int quantize_weights_run(const void* w, int E, int n, int d, void* q, void* scal
 
 template <class... KArgs, class... Args>
 int launch_tiles(void (*kernel)(KArgs...), const Segments& sg, int cols, cudaStream_t st, Args... args) {
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SimtTile<G8>));
+  if (err != cudaSuccess) return note_cuda(err);
   cudaLaunchConfig_t cfg = {};
+  cfg.dynamicSmemBytes = sizeof(SimtTile<G8>);
   cfg.gridDim = dim3((unsigned)(ceil_div(sg.rows, ST) + sg.E), (unsigned)ceil_div(cols, ST));
-  cfg.blockDim = dim3(SN);
+  cfg.blockDim = dim3(G8::SN);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

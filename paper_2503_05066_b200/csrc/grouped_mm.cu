@@ -14,26 +14,26 @@ namespace {
 
 enum { DIR_FWD = 0, DIR_DX = 1 };
 
-template <typename T, int DIR, int TM>
-__global__ void __launch_bounds__(SN, 2)
+template <typename T, int DIR, class GE>
+__global__ void __launch_bounds__(GE::SN, 8 / GE::G)
 k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out, Segments sg, int K, int Nout) {
   wait_for_previous_kernel();
-  __shared__ SimtTile<TM> sm;
+  SimtTile<GE>& sm = simt_tile<GE>();
   RowTile t;
-  if (!find_row_tile<TM>(sg, blockIdx.x, t)) return;
+  if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST;
   const T* We = W + (int64_t)t.e * Nout * K;
-  constexpr int R = TM / 16;
+  constexpr int R = GE::R;
   float acc[R][4];
   clear_acc(acc);
   const Dense<T, true> la{A + (int64_t)t.row0 * K, K};
-  if (DIR == DIR_FWD) tile_product<TM>(la, Dense<T, true>{We + (int64_t)col0 * K, K}, t.rows, Nout - col0, K, sm, acc);
-  else tile_product<TM>(la, Dense<T, false>{We + col0, Nout}, t.rows, Nout - col0, K, sm, acc);
+  if (DIR == DIR_FWD) tile_product<GE>(la, Dense<T, true>{We + (int64_t)col0 * K, K}, t.rows, Nout - col0, K, sm, acc);
+  else tile_product<GE>(la, Dense<T, false>{We + col0, Nout}, t.rows, Nout - col0, K, sm, acc);
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = out_row(i), c = col0 + out_col(j);
+      const int r = out_row<GE>(i), c = col0 + out_col(j);
       if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<T>(acc[i][j]);
     }
 }
@@ -43,53 +43,53 @@ k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out,
 template <typename T, typename TO>
 struct DwSet { const T* P[3]; const T* Q[3]; TO* out[3]; int M[3], N[3]; };
 
-template <typename T, typename TO, int TM>
-__global__ void __launch_bounds__(SN, 2) k_mm_dw(DwSet<T, TO> s, Segments sg) {
+template <typename T, typename TO, class GE>
+__global__ void __launch_bounds__(GE::SN, 8 / GE::G) k_mm_dw(DwSet<T, TO> s, Segments sg) {
   wait_for_previous_kernel();
-  __shared__ SimtTile<TM> sm;
+  SimtTile<GE>& sm = simt_tile<GE>();
   const int p = blockIdx.z / sg.E, e = blockIdx.z - p * sg.E;
   const int M = s.M[p], N = s.N[p];
-  const int r0 = blockIdx.x * TM, c0 = blockIdx.y * ST;
+  const int r0 = blockIdx.x * GE::TM, c0 = blockIdx.y * ST;
   if (r0 >= M || c0 >= N) return;
   const int begin = seg_at(sg, e), n = seg_at(sg, e + 1) - begin;
-  constexpr int R = TM / 16;
+  constexpr int R = GE::R;
   float acc[R][4];
   clear_acc(acc);
-  tile_product<TM>(Dense<T, false>{s.P[p] + (int64_t)begin * M + r0, M}, Dense<T, false>{s.Q[p] + (int64_t)begin * N + c0, N},
+  tile_product<GE>(Dense<T, false>{s.P[p] + (int64_t)begin * M + r0, M}, Dense<T, false>{s.Q[p] + (int64_t)begin * N + c0, N},
                M - r0, N - c0, n, sm, acc);
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = r0 + out_row(i), c = c0 + out_col(j);
+      const int r = r0 + out_row<GE>(i), c = c0 + out_col(j);
       if (r < M && c < N) s.out[p][((int64_t)e * M + r) * N + c] = from_float<TO>(acc[i][j]);
     }
 }
 
 // dg, du and h of the SwiGLU backward pass: three products over d with the elementwise part in registers.
-template <typename T, int TM>
-__global__ void __launch_bounds__(SN, 2)
+template <typename T, class GE>
+__global__ void __launch_bounds__(GE::SN, 8 / GE::G)
 k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __restrict__ wg, const T* __restrict__ wu,
                   const T* __restrict__ wd, T* __restrict__ dg, T* __restrict__ du, T* __restrict__ h, Segments sg, int d,
                   int F) {
   wait_for_previous_kernel();
-  __shared__ SimtTile<TM> sm;
+  SimtTile<GE>& sm = simt_tile<GE>();
   RowTile t;
-  if (!find_row_tile<TM>(sg, blockIdx.x, t)) return;
+  if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST, cols = F - col0;
   const int64_t we = (int64_t)t.e * F * d;
   const Dense<T, true> lx{x + (int64_t)t.row0 * d, d}, ldy{dy + (int64_t)t.row0 * d, d};
-  constexpr int R = TM / 16;
+  constexpr int R = GE::R;
   float g[R][4], u[R][4], dh[R][4];
   clear_acc(g); clear_acc(u); clear_acc(dh);
-  tile_product<TM>(lx, Dense<T, true>{wg + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, g);
-  tile_product<TM>(lx, Dense<T, true>{wu + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, u);
-  tile_product<TM>(ldy, Dense<T, false>{wd + we + col0, F}, t.rows, cols, d, sm, dh);
+  tile_product<GE>(lx, Dense<T, true>{wg + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, g);
+  tile_product<GE>(lx, Dense<T, true>{wu + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, u);
+  tile_product<GE>(ldy, Dense<T, false>{wd + we + col0, F}, t.rows, cols, d, sm, dh);
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = out_row(i), c = col0 + out_col(j);
+      const int r = out_row<GE>(i), c = col0 + out_col(j);
       if (r >= t.rows || c >= F) continue;
       const float p = 1.0f / (1.0f + expf(-g[i][j]));
       const float a = g[i][j] * p;
@@ -101,26 +101,26 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
 }
 
 // dx = dg W_g + du W_u (weights [E, F, d])
-template <typename T, int TM>
-__global__ void __launch_bounds__(SN, 2)
+template <typename T, class GE>
+__global__ void __launch_bounds__(GE::SN, 8 / GE::G)
 k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __restrict__ wg, const T* __restrict__ wu,
              T* __restrict__ dx, Segments sg, int d, int F) {
   wait_for_previous_kernel();
-  __shared__ SimtTile<TM> sm;
+  SimtTile<GE>& sm = simt_tile<GE>();
   RowTile t;
-  if (!find_row_tile<TM>(sg, blockIdx.x, t)) return;
+  if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST;
   const int64_t we = (int64_t)t.e * F * d + col0;
-  constexpr int R = TM / 16;
+  constexpr int R = GE::R;
   float acc[R][4];
   clear_acc(acc);
-  tile_product<TM>(Dense<T, true>{dg + (int64_t)t.row0 * F, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, F, sm, acc);
-  tile_product<TM>(Dense<T, true>{du + (int64_t)t.row0 * F, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, F, sm, acc);
+  tile_product<GE>(Dense<T, true>{dg + (int64_t)t.row0 * F, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, F, sm, acc);
+  tile_product<GE>(Dense<T, true>{du + (int64_t)t.row0 * F, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, F, sm, acc);
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = out_row(i), c = col0 + out_col(j);
+      const int r = out_row<GE>(i), c = col0 + out_col(j);
       if (r < t.rows && c < d) dx[(int64_t)(t.row0 + r) * d + c] = from_float<T>(acc[i][j]);
     }
 }
@@ -133,11 +133,14 @@ int launched(cudaError_t err) {
 // These kernels do not let their successor start early (no allow_next_kernel): its blocks would be handed to the SMs
 // that happen to have room, several to each, and stay there (a 1024-row fp32 product of 120 blocks, launched back to
 // back: 63 us that way, 25 without).
-template <class... KArgs, class... Args>
+template <class GE, class... KArgs, class... Args>
 int launch_tiles(void (*kernel)(KArgs...), dim3 grid, cudaStream_t st, Args... args) {
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SimtTile<GE>));
+  if (err != cudaSuccess) return note_cuda(err);
   cudaLaunchConfig_t cfg = {};
+  cfg.dynamicSmemBytes = sizeof(SimtTile<GE>);
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(SN);
+  cfg.blockDim = dim3(GE::SN);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -150,47 +153,65 @@ int launch_tiles(void (*kernel)(KArgs...), dim3 grid, cudaStream_t st, Args... a
 dim3 row_grid(const Segments& sg, int cols, int tm) {       // every segment rounds up to whole tiles
   return dim3((unsigned)(ceil_div(sg.rows, tm) + sg.E), (unsigned)ceil_div(cols, ST));
 }
-// Rows per tile: 32 while 64-row tiles would not give every SM two (measured on a 1024-row fp32 layer, 256 x 512, of 8
-// experts: the gradient of its rows 45 us with 64-row tiles, 72 of them, against 36 with 32-row ones).
-bool low_tiles(int64_t tiles64) { return tiles64 < 2 * sm_count(); }
+// Geometry by the number of 64 x 64 tiles: above two per SM, 64-row tiles; else 32-row ones, whose block gets an SM to
+// itself when they do not outnumber the SMs (see gmm_simt.cuh; the bound on the tiles counts the segments' ragged ends
+// once each, so a few more may run).
+enum Size { LARGE, MEDIUM, SMALL };
+Size size_of(int64_t tiles64) { return tiles64 >= 2 * sm_count() ? LARGE : 2 * tiles64 > sm_count() ? MEDIUM : SMALL; }
+using Large = Geo<64, 4>;
+using Medium = Geo<32, 4>;
+using Small = Geo<32, 8>;
 
+template <typename T, int DIR, class GE>
+int rows_run(const T* a, const T* w, T* out, const Segments& sg, int K, int Nout, cudaStream_t st) {
+  return launch_tiles<GE>(k_mm_rows<T, DIR, GE>, row_grid(sg, Nout, GE::TM), st, a, w, out, sg, K, Nout);
+}
 template <typename T, int DIR>
 int rows_simt(const void* a, const void* w, void* out, const Segments& sg, int K, int Nout, cudaStream_t st) {
-  const T *A = (const T*)a, *W = (const T*)w;
-  if (low_tiles(ceil_div(sg.rows, ST) * ceil_div(Nout, ST)))
-    return launch_tiles(k_mm_rows<T, DIR, 32>, row_grid(sg, Nout, 32), st, A, W, (T*)out, sg, K, Nout);
-  return launch_tiles(k_mm_rows<T, DIR, 64>, row_grid(sg, Nout, 64), st, A, W, (T*)out, sg, K, Nout);
+  const Size z = size_of(ceil_div(sg.rows, ST) * ceil_div(Nout, ST));
+  auto run = z == LARGE ? rows_run<T, DIR, Large> : z == MEDIUM ? rows_run<T, DIR, Medium> : rows_run<T, DIR, Small>;
+  return run((const T*)a, (const T*)w, (T*)out, sg, K, Nout, st);
 }
 
+template <typename T, typename TO, class GE>
+int dw_run(const DwSet<T, TO>& s, int M, int N, unsigned z, const Segments& sg, cudaStream_t st) {
+  return launch_tiles<GE>(k_mm_dw<T, TO, GE>, dim3((unsigned)ceil_div(M, GE::TM), (unsigned)ceil_div(N, ST), z), st, s, sg);
+}
 template <typename T, typename TO>
 int dw_simt(const DwSet<T, TO>& s, int count, const Segments& sg, cudaStream_t st) {
   int M = 0, N = 0;
-  for (int p = 0; p < count; ++p) { M = s.M[p] > M ? s.M[p] : M; N = s.N[p] > N ? s.N[p] : N; }
-  const unsigned z = (unsigned)(count * sg.E), y = (unsigned)ceil_div(N, ST);
-  if (low_tiles(ceil_div(M, ST) * y * z))
-    return launch_tiles(k_mm_dw<T, TO, 32>, dim3((unsigned)ceil_div(M, 32), y, z), st, s, sg);
-  return launch_tiles(k_mm_dw<T, TO, 64>, dim3((unsigned)ceil_div(M, 64), y, z), st, s, sg);
+  int64_t tiles = 0;
+  for (int p = 0; p < count; ++p) {
+    M = s.M[p] > M ? s.M[p] : M;
+    N = s.N[p] > N ? s.N[p] : N;
+    tiles += ceil_div(s.M[p], ST) * ceil_div(s.N[p], ST) * sg.E;
+  }
+  const Size z = size_of(tiles);
+  auto run = z == LARGE ? dw_run<T, TO, Large> : z == MEDIUM ? dw_run<T, TO, Medium> : dw_run<T, TO, Small>;
+  return run(s, M, N, (unsigned)(count * sg.E), sg, st);
 }
 
-template <typename T, int TM>
-int ffn_grad_rows(const T* x, const T* dy, const Segments& sg, int d, int F, const T* wg, const T* wu, const T* wd, T* dg, T* du,
-                  T* h, T* dx, cudaStream_t st) {
-  const int rc = launch_tiles(k_ffn_grad_hidden<T, TM>, row_grid(sg, F, TM), st, x, dy, wg, wu, wd, dg, du, h, sg, d, F);
-  if (rc != CAPMOE_OK) return rc;
-  return launch_tiles(k_ffn_grad_x<T, TM>, row_grid(sg, d, TM), st, (const T*)dg, (const T*)du, wg, wu, dx, sg, d, F);
+template <typename T, class GE>
+int hidden_run(const T* x, const T* dy, const T* wg, const T* wu, const T* wd, T* dg, T* du, T* h, const Segments& sg, int d, int F,
+               cudaStream_t st) {
+  return launch_tiles<GE>(k_ffn_grad_hidden<T, GE>, row_grid(sg, F, GE::TM), st, x, dy, wg, wu, wd, dg, du, h, sg, d, F);
 }
-
+template <typename T, class GE>
+int dx2_run(const T* dg, const T* du, const T* wg, const T* wu, T* dx, const Segments& sg, int d, int F, cudaStream_t st) {
+  return launch_tiles<GE>(k_ffn_grad_x<T, GE>, row_grid(sg, d, GE::TM), st, dg, du, wg, wu, dx, sg, d, F);
+}
 template <typename T>
-int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
-                  const void* wd, void* dx, void* dwg, void* dwu, void* dwd, void* ws, cudaStream_t st) {
+int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int F, const void* w_gate, const void* w_up,
+                  const void* w_down, void* dx, void* dwg, void* dwu, void* dwd, void* ws, cudaStream_t st) {
   T* dg = (T*)ws;
   T* du = dg + (int64_t)sg.rows * F;
   T* h = du + (int64_t)sg.rows * F;
-  const bool low = low_tiles(ceil_div(sg.rows, ST) * ceil_div(F < d ? F : d, ST));
-  const int rc = low ? ffn_grad_rows<T, 32>((const T*)x, (const T*)dy, sg, d, F, (const T*)wg, (const T*)wu, (const T*)wd, dg, du,
-                                            h, (T*)dx, st)
-                     : ffn_grad_rows<T, 64>((const T*)x, (const T*)dy, sg, d, F, (const T*)wg, (const T*)wu, (const T*)wd, dg, du,
-                                            h, (T*)dx, st);
+  const T *wg = (const T*)w_gate, *wu = (const T*)w_up, *wd = (const T*)w_down;
+  const Size zh = size_of(ceil_div(sg.rows, ST) * ceil_div(F, ST)), zx = size_of(ceil_div(sg.rows, ST) * ceil_div(d, ST));
+  auto hidden = zh == LARGE ? hidden_run<T, Large> : zh == MEDIUM ? hidden_run<T, Medium> : hidden_run<T, Small>;
+  auto dx2 = zx == LARGE ? dx2_run<T, Large> : zx == MEDIUM ? dx2_run<T, Medium> : dx2_run<T, Small>;
+  int rc = hidden((const T*)x, (const T*)dy, wg, wu, wd, dg, du, h, sg, d, F, st);
+  if (rc == CAPMOE_OK) rc = dx2(dg, du, wg, wu, (T*)dx, sg, d, F, st);
   if (rc != CAPMOE_OK) return rc;
   DwSet<T, T> s = {{dg, du, (const T*)dy}, {(const T*)x, (const T*)x, h}, {(T*)dwg, (T*)dwu, (T*)dwd}, {F, F, d}, {d, d, F}};
   return dw_simt(s, 3, sg, st);
