@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcapmoe.so")
 SOURCES = ["api.cu", "route.cu", "drop.cu", "drop_cluster.cu", "drop_parallel.cu", "variants.cu", "permute_combine.cu", "ffn_simt.cu", "ffn_tc.cu", "ffn_tc_t.cu",
-           "grouped_mm.cu", "grouped_fp8.cu", "gmm_tc.cu", "gmm_fp8_tc.cu", "gmm_short.cu"]
+           "grouped_mm.cu", "grouped_fp8.cu", "gmm_rows.cu", "gmm_dw.cu", "gmm_swiglu8.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

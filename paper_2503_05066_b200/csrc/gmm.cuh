@@ -38,8 +38,8 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
   return r;
 }
 
-// Whether a call runs the short-segment kernels (gmm_short.cu): average segment below `limit` rows, unless
-// capmoe_debug_ffn_variant forces one form.
+// Whether the 8-bit gate/up product takes its tokens on the N side (gmm_rows.cu): average segment below `limit` rows,
+// unless capmoe_debug_ffn_variant forces one form.
 inline bool use_short(const Segments& sg, int64_t limit) {
   const int v = ffn_variant();
   if (v == FFN_SHORT) return true;
@@ -47,39 +47,44 @@ inline bool use_short(const Segments& sg, int64_t limit) {
   return (int64_t)sg.rows < limit * sg.E;
 }
 
-// Tensor-core kernels (gmm_tc.cu): bf16 with rows of whole 16-byte vectors.  All matrices 16-byte aligned, map_ws
-// 128-byte aligned with gmm_tc_map_bytes(E, lists) bytes (dw: 2 lists, ffn_grad: 5).
-bool gmm_tc_supported(int E, int d, int n, int dtype);
-size_t gmm_tc_map_bytes(int E, int lists);
-int gmm_tc_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, cudaStream_t st);
-int gmm_tc_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, cudaStream_t st);
-int gmm_tc_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws,
-              int32_t* dev_status, cudaStream_t st);
-int gmm_tc_ffn_grad(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
-                    const void* wd, void* dx, void* dwg, void* dwu, void* dwd, void* map_ws, void* hidden, int32_t* dev_status,
-                    cudaStream_t st);
-
-// The same products with the weights on the M side (gmm_short.cu).  `sched`: a zeroed tile counter or NULL.
-int gmm_short_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
-                  cudaStream_t st);
-int gmm_short_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
-                 cudaStream_t st);
-int gmm_short_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
-                     const void* wd, void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st);
-int gmm_short_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
-                  int32_t* dev_status, int32_t* sched, cudaStream_t st);
-int gmm8_short(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n,
-               void* y, int32_t* dev_status, int32_t* sched, cudaStream_t st);
-int gmm8_short_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
-                      const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+// Tensor-core kernels.  All matrices 16-byte aligned, `sched` a zeroed tile counter or NULL.
+// bf16 (gmm_rows.cu, gmm_dw.cu): rows of whole 16-byte vectors; dw's E * n (E * d) rows are 32-bit coordinates.  map_ws is
+// 128-byte aligned with gmm_dw_map_bytes(E, lists) bytes (gmm_dw: 2 lists, gmm_dw_ffn_maps: 5).
+inline bool gmm_supported(int E, int d, int n, int dtype) {
+  const int64_t lim = (int64_t)1 << 31;
+  return dtype == CAPMOE_BF16 && d % 8 == 0 && n % 8 == 0 && (int64_t)E * n < lim && (int64_t)E * d < lim;
+}
+int gmm_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
+            cudaStream_t st);
+int gmm_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
+           cudaStream_t st);
+int gmm_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu, const void* wd,
+               void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st);
+int gmm_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
+            int32_t* dev_status, int32_t* sched, cudaStream_t st);
+size_t gmm_dw_map_bytes(int E, int lists);
+int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws,
+           int32_t* dev_status, int32_t* sched, cudaStream_t st);
+// the FFN's three weight gradients: the maps first (they need the addresses only, so they can be made ahead)
+int gmm_dw_ffn_maps(const void* dg, const void* du, const void* dy, const void* x, const void* h, const Segments& sg, int d, int F,
+                    void* map_ws, cudaStream_t st);
+int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd, const void* map_ws, int32_t* dev_status,
+               int32_t* sched, cudaStream_t st);
+// 8-bit (gmm_rows.cu, gmm_swiglu8.cu): d and n (F) multiples of 16; xs_ld, hs_ld: bytes from one row's scales to the next's
+inline bool gmm8_supported(int d, int n) { return d % 16 == 0 && n % 16 == 0; }
+int gmm8(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
+         int32_t* dev_status, int32_t* sched, cudaStream_t st);
+int gmm8_swiglu(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
+                int32_t* sched, cudaStream_t st);
+int gmm8_swiglu_short(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                      const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
                       int32_t* sched, cudaStream_t st);
 
-// Block-scaled 8-bit kernels (gmm_fp8_tc.cu): d and n (F) multiples of 16.  `sched`: a zeroed tile counter or NULL.
-bool gmm8_tc_supported(int d, int n);
-int gmm8_tc(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
-            int32_t* dev_status, int32_t* sched, cudaStream_t st);
-int gmm8_tc_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
-                   const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
-                   int32_t* sched, cudaStream_t st);
+// Tile counters in the caller's status block, one per launch of a call: cleared by begin_counters, slot i by counter_at.
+inline int32_t* counter_at(int32_t* dev_status, int i) { return dev_status ? dev_status + 1 + i : nullptr; }
+inline int begin_counters(int32_t* dev_status, int n, cudaStream_t st) {
+  return dev_status ? clear_words(dev_status + 1, n, nullptr, 0, st) : CAPMOE_OK;
+}
 
 }  // namespace capmoe

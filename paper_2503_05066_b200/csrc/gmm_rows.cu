@@ -1,10 +1,14 @@
-// Grouped products for short segments, in bf16 and in 8 bits: the operand roles of gmm_tc.cu / gmm_fp8_tc.cu
-// exchanged.  The weights are the M side (256 weight rows per CTA pair, 128 per CTA), the tokens the N side, which the
-// MMA takes in steps of 16, so an expert with a few rows pays for 16 of them and one with a few hundred for at most 15
-// more than it has; a segment longer than a tile is cut into equal token blocks.
-//   T_FWD   y^T  = W[e] x^T             T_DX  dx^T = W[e]^T dy^T (weights MN-major)      T_DX2  over both FFN weights
-//   T_HID   dg, du, h of the SwiGLU backward pass (three accumulators)
+// Grouped products over expert rows on tcgen05, in bf16 and in 8 bits (kind::mxf8f6f4, see gmm_tc.cuh): persistent,
+// warp-specialised kernels over CTA pairs (cta_group::2), TMA-fed operand rings, fp32 accumulators in tensor memory.  The
+// WEIGHTS are the M side (256 weight rows per pair, 128 per CTA), the tokens the N side, which the MMA takes in steps of
+// 16, so an expert with a few rows pays for 16 of them and one with a few hundred for at most 15 more than it has; a
+// segment longer than a tile is cut into equal token blocks.  (With the tokens on the M side, 256 to a tile, the same
+// products were 2 % faster at best, at 2000 rows per expert and more, and up to half as fast below 300.)
+//   T_FWD   y^T  = W[e] x^T             T_DX  dx^T = W[e]^T dy^T         T_DX2  dx^T = W_g[e]^T dg^T + W_u[e]^T du^T
+//   T_HID   dg, du, h of the SwiGLU FFN's backward pass: g, u and dh of a tile side by side in tensor memory, the
+//           elementwise part in the epilogue, so that g, u and dh are never rounded or written
 //   T_F8    8-bit T_FWD                 T_F8SW  8-bit gate/up with SwiGLU, hidden rows quantised
+// Weights whose output index is contiguous (W^T) are MN-major operands, loaded as they lie (make_mn_map).
 // One token's row of an output is one column of an accumulator.  The epilogue reads 8 x 8 fragments, which stmatrix
 // writes transposed to shared memory, so that whole 64-byte runs of a token's row leave the warp.  (Two-byte stores
 // straight from the accumulator's columns took 15,000 cycles for a 128-token tile of T_HID, half as long as its MMAs.)
@@ -12,7 +16,8 @@
 // the lanes (shuffles) and the four warps (shared memory).
 // A stage holds the weights of one k-block and `tb` token rows per CTA; `tb` follows the average segment so that short
 // segments leave the ring to the weights, which is what a decode step has to stream.  What bounds it: HBM for few rows
-// per expert, else the tensor pipe and the L2 traffic of the weights (once per token block).
+// per expert (a decode step's 332 MB of bf16 weights: 55 us, 0.92 of the copy bandwidth), else the tensor pipe and the L2
+// traffic of the weights, once per token block.
 // Tensor memory: accumulators of `tt` columns, two sets of them when they fit, so that an epilogue overlaps the next
 // tile's MMAs.
 #include "gmm.cuh"
@@ -54,6 +59,7 @@ struct TArgs {
   void* out[3];
   const uint8_t *xs, *s0, *s1;      // 8-bit: scales of the rows, of W (W_g) and of W_u
   uint8_t* out_scale;
+  int64_t xs_ld, os_ld;             // bytes between rows of xs and of out_scale
   int32_t* dev_status;
   int32_t* sched;
 };
@@ -62,7 +68,7 @@ struct STile { int e, row0, rows, nt, w0; };   // segment, first token row, toke
 
 template <int KIND>
 __global__ void __launch_bounds__(ShapeT<KIND>::THREADS, 1)
-k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
+k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   using S = ShapeT<KIND>;
   constexpr bool FP8 = S::FP8, W_MN = KIND == T_DX || KIND == T_DX2;
   constexpr int EW = S::EW, NACC = S::NACC;
@@ -273,7 +279,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     STile t;
     bool ok = true;
     const int nb = kbs, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
-    const int loads = scale_loads(nb, ar.xs, ar.s0, ar.s1);
+    const bool xa = scales_aligned(ar.xs_ld, ar.xs), ga = scales_aligned(nb, ar.s0), ua = scales_aligned(nb, ar.s1);
     for (int j = 0; ok; ++j) {
       if (!get_tile(j, true, t)) break;
       const int64_t blk = (int64_t)t.e * wb + min(t.w0 / QBLOCK + (int)rank, wb - 1);
@@ -283,10 +289,10 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
         for (int i = 0; i < 8; ++i) {
           a[i] = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
           if (32 * i < t.nt)                                    // the same for the whole warp
-            a[i] = scale_words(ar.xs + (int64_t)min(t.row0 + lane + 32 * i, ar.sg.rows - 1) * nb, k, nb, loads);
+            a[i] = scale_words(ar.xs + (int64_t)min(t.row0 + lane + 32 * i, ar.sg.rows - 1) * ar.xs_ld, k, nb, xa);
         }
-        const uint4 g4 = scale_words(ar.s0 + blk * nb, k, nb, loads);
-        const uint4 u4 = KIND == T_F8SW ? scale_words(ar.s1 + blk * nb, k, nb, loads) : g4;
+        const uint4 g4 = scale_words(ar.s0 + blk * nb, k, nb, ga);
+        const uint4 u4 = KIND == T_F8SW ? scale_words(ar.s1 + blk * nb, k, nb, ua) : g4;
         bool free_slot = mbar_wait(sempty_bar(r), rph ^ 1u, abort_flag);
         free_slot = __all_sync(0xffffffffu, free_slot);
         if (!free_slot) { ok = false; break; }
@@ -391,7 +397,7 @@ k_gmm_t(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
             group_sync(1 + sub, 128);
             flip ^= 1u;                                          // the next chunk writes the other copy
             if (quarter == 0 && lane < n)
-              ar.out_scale[(int64_t)(t.row0 + c + lane) * ((ar.Nout + QBLOCK - 1) / QBLOCK) + col0 / QBLOCK] =
+              ar.out_scale[(int64_t)(t.row0 + c + lane) * ar.os_ld + col0 / QBLOCK] =
                   (uint8_t)scale_code(max(max(rd[lane], rd[32 + lane]), max(rd[64 + lane], rd[96 + lane])));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -476,7 +482,7 @@ int launch(const TMaps& mp, const TArgs& ar, cudaStream_t st) {
   using S = ShapeT<KIND>;
   const int pairs = sm_count() / 2;
   if (pairs < 1) return CAPMOE_EUNSUPPORTED;
-  cudaError_t err = cudaFuncSetAttribute(k_gmm_t<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+  cudaError_t err = cudaFuncSetAttribute(k_gmm_rows<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
   if (err != cudaSuccess) return note_cuda(err);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
@@ -490,7 +496,7 @@ int launch(const TMaps& mp, const TArgs& ar, cudaStream_t st) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  err = cudaLaunchKernelEx(&cfg, k_gmm_t<KIND>, mp, ar);
+  err = cudaLaunchKernelEx(&cfg, k_gmm_rows<KIND>, mp, ar);
   count_launch(1);
   return note_cuda(err);
 }
@@ -504,7 +510,7 @@ bool map3(CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t bat
 
 }  // namespace
 
-int gmm_short_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
+int gmm_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
                   cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
@@ -514,7 +520,7 @@ int gmm_short_fwd(const void* x, const Segments& sg, const void* w, int d, int n
   return launch<T_FWD>(mp, ar, st);
 }
 
-int gmm_short_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
+int gmm_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
                  cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
@@ -525,7 +531,7 @@ int gmm_short_dx(const void* dy, const Segments& sg, const void* w, int d, int n
   return launch<T_DX>(mp, ar, st);
 }
 
-int gmm_short_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
+int gmm_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
                      const void* wd, void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
@@ -538,7 +544,7 @@ int gmm_short_hidden(const void* x, const void* dy, const Segments& sg, int d, i
   return launch<T_HID>(mp, ar, st);
 }
 
-int gmm_short_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
+int gmm_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
                   int32_t* dev_status, int32_t* sched, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
@@ -551,23 +557,23 @@ int gmm_short_dx2(const void* dg, const void* du, const Segments& sg, int d, int
   return launch<T_DX2>(mp, ar, st);
 }
 
-int gmm8_short(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n,
+int gmm8(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n,
                void* y, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
-  ar.sg = sg; ar.K = d; ar.Nout = n; ar.out[0] = y; ar.xs = xs; ar.s0 = ws; ar.dev_status = dev_status; ar.sched = sched;
+  ar.sg = sg; ar.K = d; ar.Nout = n; ar.out[0] = y; ar.xs = xs; ar.xs_ld = xs_ld; ar.s0 = ws; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_F8>(ar, 224);
   if (!make_map_u8(&mp.x0, xq, d, sg.rows, 0, (uint32_t)ar.tb) || !make_map_u8(&mp.w0, wq, d, n, sg.E, BM))
     return note_cuda(cudaErrorInvalidValue);
   return launch<T_F8>(mp, ar, st);
 }
 
-int gmm8_short_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
-                      const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+int gmm8_swiglu_short(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                      const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
                       int32_t* sched, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
-  ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = hq; ar.out_scale = hs; ar.xs = xs; ar.s0 = wgs; ar.s1 = wus;
+  ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = hq; ar.out_scale = hs; ar.os_ld = hs_ld; ar.xs = xs; ar.xs_ld = xs_ld; ar.s0 = wgs; ar.s1 = wus;
   ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_F8SW>(ar, 224);
   if (!make_map_u8(&mp.x0, xq, d, sg.rows, 0, (uint32_t)ar.tb) || !make_map_u8(&mp.w0, wg, d, F, sg.E, BM) ||

@@ -1,25 +1,25 @@
-// 8-bit grouped products on tcgen05's block-scaled MMA (kind::mxf8f6f4): e4m3 codes, power-of-two scales per 128
-// columns of a row and per 128 x 128 block of a weight, applied by the tensor cores, fp32 accumulation.
-//   PLAIN    y[r]   = W[e] x[r]                                    bf16
-//   SWIGLU   h[r]   = silu(W_g[e] x[r]) * (W_u[e] x[r])            quantised: codes and scales
-// Persistent kernel over CTA pairs, 256 x 256 tiles, the structure of k_gmm2 with one more warp that stages scale words
-// (see gmm_tc.cuh).  SWIGLU puts 128 gate and 128 up columns of the same hidden columns into a tile, which is one
-// block of 128 hidden columns per row: its largest magnitude meets between the two threads that share a row, and the
-// hidden row leaves the kernel as codes, never as fp32.
-// Tensor memory: two accumulators of 256 columns and three groups of scales do not fit 512 columns, so the
+// Gate and up products of the 8-bit FFN on tcgen05's block-scaled MMA (kind::mxf8f6f4): e4m3 codes, power-of-two scales
+// per 128 columns of a row and per 128 x 128 block of a weight, applied by the tensor cores, fp32 accumulation.
+//   h[r] = silu(W_g[e] x[r]) * (W_u[e] x[r]), quantised: codes and scales
+// Persistent kernel over CTA pairs, tiles of 256 tokens by 128 hidden columns, the structure of k_gmm_dw (gmm_tc.cu) with
+// one more warp that stages scale words (see gmm_tc.cuh).  A tile puts 128 gate and 128 up columns of the same hidden
+// columns side by side, which is one block of 128 hidden columns per row: its largest magnitude meets between the two
+// threads that share a row, and the hidden row leaves the kernel as codes, never as fp32.
+// Tensor memory: two accumulators of 256 columns and four groups of scales do not fit 512 columns, so the
 // accumulators overlap by 64 columns ([0,256) and [192,448)); an epilogue reads the shared columns first and lets the
-// next tile's MMAs start then, with most of its own columns still to convert.
-// What bounds it: the tensor pipe.
+// next tile's MMAs start then, with most of its own columns still to convert.  (With the tokens on the N side, as in
+// gmm_rows.cu, gate and up would fill the 448 columns at 224 tokens, and an epilogue could not overlap the next tile.)
+// What bounds it: the tensor pipe; the scale copies take about 10 % of it.
 #include "gmm.cuh"
 #include "gmm_tc.cuh"
 
 namespace capmoe {
 namespace {
 
-// rows per expert on average below which gmm_short.cu takes over
-constexpr int64_t SHORT_LIMIT = 256, SHORT_LIMIT_SWIGLU = 256;
+// Allocated rows per expert on average below which gmm_rows.cu takes over (60 experts, 2048 x 1408, whole FFN: 144 us
+// against 155 at 136 rows, 205 against 207 at 273, 387 against 342 at 546).
+constexpr int64_t SHORT_LIMIT = 300;
 
-enum { PLAIN = 0, SWIGLU = 1 };
 constexpr int NST8 = 6;
 constexpr int STAGE8 = 2 * A_BYTES;                       // 128 rows of A, 128 rows of B: 32 KB
 constexpr int STG8_OFF = NST8 * STAGE8;
@@ -34,17 +34,16 @@ constexpr int ACC_STEP = 192;                             // columns between the
 struct F8Args {
   Segments sg;
   int K, Nout;
-  const uint8_t *xs, *s0, *s1;      // scales of the rows, of W (W_g) and of W_u
-  void* out;                        // bf16 y, or codes of h
-  uint8_t* out_scale;               // SWIGLU
+  const uint8_t *xs, *s0, *s1;      // scales of the rows, of W_g and of W_u
+  uint8_t *out, *out_scale;         // codes and scales of h
+  int64_t xs_ld, os_ld;             // bytes between rows of xs and of out_scale
   int32_t* dev_status;
   int32_t* sched;
 };
 struct F8Maps { CUtensorMap a, b0, b1, o; };
 
-template <int EPI>
-__global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ F8Maps mp, const __grid_constant__ F8Args ar) {
-  constexpr int N_TILE = EPI == SWIGLU ? 128 : 256, BM2 = 2 * BM;
+__global__ void __launch_bounds__(F8_THREADS, 1) k_gmm_swiglu8(const __grid_constant__ F8Maps mp, const __grid_constant__ F8Args ar) {
+  constexpr int N_TILE = 128, BM2 = 2 * BM;
   allow_next_kernel();
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -139,8 +138,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
           if (rank == 0) mbar_expect_tx(full_bar(s), 2 * STAGE8);
           const uint32_t a_dst = tiles + (uint32_t)s * STAGE8;
           tma2_load_2d(a_dst, &mp.a, kb * QBLOCK, t.row0 + (int)rank * BM, bar);
-          if (EPI == SWIGLU) tma2_load_3d(a_dst + A_BYTES, rank == 0 ? &mp.b0 : &mp.b1, kb * QBLOCK, t.n0, t.e, bar);
-          else tma2_load_3d(a_dst + A_BYTES, &mp.b0, kb * QBLOCK, t.n0 + (int)rank * 128, t.e, bar);
+          tma2_load_3d(a_dst + A_BYTES, rank == 0 ? &mp.b0 : &mp.b1, kb * QBLOCK, t.n0, t.e, bar);
           if (++s == NST8) { s = 0; ph ^= 1u; }
         }
       }
@@ -204,24 +202,23 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
     Tile t;
     bool ok = true;
     const int nb = num_kb, wb = (ar.Nout + QBLOCK - 1) / QBLOCK;
-    const int loads = scale_loads(nb, ar.xs, ar.s0, ar.s1);
+    const bool xa = scales_aligned(ar.xs_ld, ar.xs), ga = scales_aligned(nb, ar.s0), ua = scales_aligned(nb, ar.s1);
     for (int j = 0; ok; ++j) {
       if (!get_tile(j, true, t)) break;
       const uint8_t* rows[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = min(t.row0 + (int)rank * BM + lane + 32 * i, ar.sg.rows - 1);   // rows past the tile: any scale
-        rows[i] = ar.xs + (int64_t)row * nb;
+        rows[i] = ar.xs + (int64_t)row * ar.xs_ld;
       }
       const int blk = t.n0 / QBLOCK;
       const uint8_t* w0 = ar.s0 + ((int64_t)t.e * wb + blk) * nb;
-      const uint8_t* w1 = EPI == SWIGLU ? ar.s1 + ((int64_t)t.e * wb + blk) * nb
-                                        : ar.s0 + ((int64_t)t.e * wb + min(blk + 1, wb - 1)) * nb;
+      const uint8_t* w1 = ar.s1 + ((int64_t)t.e * wb + blk) * nb;
       for (int k = 0; ok && k < nb; k += 16) {
         uint4 a[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = scale_words(rows[i], k, nb, loads);
-        const uint4 b = scale_words(w0, k, nb, loads), c = scale_words(w1, k, nb, loads);
+        for (int i = 0; i < 4; ++i) a[i] = scale_words(rows[i], k, nb, xa);
+        const uint4 b = scale_words(w0, k, nb, ga), c = scale_words(w1, k, nb, ua);
         bool free_slot = mbar_wait(sempty_bar(r), rph ^ 1u, abort_flag);
         free_slot = __all_sync(0xffffffffu, free_slot);
         if (!free_slot) { ok = false; break; }
@@ -260,7 +257,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
       const uint32_t b = it & 1u, use = it >> 1;
       bool ready = mbar_wait(tfull_bar(b), use & 1u, abort_flag);
       ready = __all_sync(0xffffffffu, ready);
-      if (EPI == SWIGLU) ready = group_all(1 + quarter, 64, ready);   // the two threads of a row stop together
+      ready = group_all(1 + quarter, 64, ready);   // the two threads of a row stop together
       if (!ready) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * (uint32_t)ACC_STEP;
@@ -269,33 +266,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
       const int row = t.row0 + warp_row0;
       // the overlap is the last 64 columns of accumulator 0 and the first 64 of accumulator 1
       const bool mine_shared = half == (b == 0 ? 1 : 0);
-      if constexpr (EPI == PLAIN) {
-        __nv_bfloat16* orow = reinterpret_cast<__nv_bfloat16*>(ar.out) + (int64_t)(row + lane) * ar.Nout + t.n0;
-        const int first = half * 128 + (half == 1 && b == 0 ? 64 : 0);          // 64 columns at a time, shared ones first
-#pragma unroll 1
-        for (int q = 0; q < 2; ++q) {
-          const int c0 = q == 0 ? first : first ^ 64;
-          uint32_t g[2][32];
-          tmem_ld32(taddr + (uint32_t)c0, g[0]);
-          tmem_ld32(taddr + (uint32_t)(c0 + 32), g[1]);
-          tmem_ld_wait();
-          if (q == 0 && mine_shared) {
-            tc_fence_before();
-            mbar_arrive_cluster(shared_bar(b) & PEER_MASK);
-          }
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const int c = c0 + 32 * v;
-            if (t.n0 + c >= ar.Nout) break;
-            uint32_t packed[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) packed[i] = pack_bf16(__uint_as_float(g[v][2 * i]), __uint_as_float(g[v][2 * i + 1]));
-            store_piece(packed, full_rows, row_ok, stg, &mp.o, t.n0 + c, row, orow + c, ar.Nout - (t.n0 + c));
-          }
-        }
-        tc_fence_before();
-        mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
-      } else {
+      {
         // hidden columns half * 64 .. + 63 of the tile: gate there, up 128 columns further on
         float h[64];
         uint32_t top = 0;
@@ -332,10 +303,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
         }
         const int c = t.n0 + half * 64;
         if (half == 0 && row_ok)
-          ar.out_scale[(int64_t)(row + lane) * ((ar.Nout + QBLOCK - 1) / QBLOCK) + t.n0 / QBLOCK] = (uint8_t)code;
+          ar.out_scale[(int64_t)(row + lane) * ar.os_ld + t.n0 / QBLOCK] = (uint8_t)code;
         if (c < ar.Nout)                                        // 64 codes are the 64 bytes of a piece's row
           store_piece(packed, full_rows, row_ok, stg, &mp.o, c, row,
-                      reinterpret_cast<__nv_bfloat16*>(reinterpret_cast<uint8_t*>(ar.out) + (int64_t)(row + lane) * ar.Nout + c),
+                      reinterpret_cast<__nv_bfloat16*>(ar.out + (int64_t)(row + lane) * ar.Nout + c),
                       (ar.Nout - c) / 2);
       }
     }
@@ -354,11 +325,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm8(const __grid_constant__ 
   if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
 }
 
-template <int EPI>
 int launch(const F8Maps& mp, const F8Args& ar, cudaStream_t st) {
   const int pairs = sm_count() / 2;
   if (pairs < 1) return CAPMOE_EUNSUPPORTED;
-  cudaError_t err = cudaFuncSetAttribute(k_gmm8<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM8);
+  cudaError_t err = cudaFuncSetAttribute(k_gmm_swiglu8, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM8);
   if (err != cudaSuccess) return note_cuda(err);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
@@ -372,40 +342,27 @@ int launch(const F8Maps& mp, const F8Args& ar, cudaStream_t st) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  err = cudaLaunchKernelEx(&cfg, k_gmm8<EPI>, mp, ar);
+  err = cudaLaunchKernelEx(&cfg, k_gmm_swiglu8, mp, ar);
   count_launch(1);
   return note_cuda(err);
 }
 
 }  // namespace
 
-bool gmm8_tc_supported(int d, int n) { return d % 16 == 0 && n % 16 == 0; }
-
-int gmm8_tc(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
-            int32_t* dev_status, int32_t* sched, cudaStream_t st) {
-  if (use_short(sg, SHORT_LIMIT)) return gmm8_short(xq, xs, sg, wq, ws, d, n, y, dev_status, sched, st);
-  F8Maps mp = {};
-  F8Args ar = {};
-  if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wq, d, n, sg.E, 128) ||
-      !make_store_map(&mp.o, y, n, sg.rows))
-    return note_cuda(cudaErrorInvalidValue);
-  ar.sg = sg; ar.K = d; ar.Nout = n; ar.xs = xs; ar.s0 = ws; ar.out = y; ar.dev_status = dev_status; ar.sched = sched;
-  return launch<PLAIN>(mp, ar, st);
-}
-
-int gmm8_tc_swiglu(const uint8_t* xq, const uint8_t* xs, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
-                   const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int32_t* dev_status,
+int gmm8_swiglu(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
+                   const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
                    int32_t* sched, cudaStream_t st) {
-  if (use_short(sg, SHORT_LIMIT_SWIGLU))
-    return gmm8_short_swiglu(xq, xs, sg, wg, wgs, wu, wus, d, F, hq, hs, dev_status, sched, st);
+  if (use_short(sg, SHORT_LIMIT))
+    return gmm8_swiglu_short(xq, xs, xs_ld, sg, wg, wgs, wu, wus, d, F, hq, hs, hs_ld, dev_status, sched, st);
   F8Maps mp = {};
   F8Args ar = {};
   if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wg, d, F, sg.E, 128) ||
       !make_map_u8(&mp.b1, wu, d, F, sg.E, 128) || !make_store_map_u8(&mp.o, hq, F, sg.rows))
     return note_cuda(cudaErrorInvalidValue);
-  ar.sg = sg; ar.K = d; ar.Nout = F; ar.xs = xs; ar.s0 = wgs; ar.s1 = wus; ar.out = hq; ar.out_scale = hs;
+  ar.sg = sg; ar.K = d; ar.Nout = F; ar.xs = xs; ar.xs_ld = xs_ld; ar.s0 = wgs; ar.s1 = wus; ar.out = hq;
+  ar.out_scale = hs; ar.os_ld = hs_ld;
   ar.dev_status = dev_status; ar.sched = sched;
-  return launch<SWIGLU>(mp, ar, st);
+  return launch(mp, ar, st);
 }
 
 }  // namespace capmoe

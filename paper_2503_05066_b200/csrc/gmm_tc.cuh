@@ -352,28 +352,20 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
   return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
 }
 
-// Scale bytes k .. k + 15 of a row of nb (four scale groups), in one 16-byte load where the rows start on 16 bytes, as
-// words where they start on words.  Bytes behind the row count as 2^0: their codes are zeros that TMA filled in.
-enum { SCALES_16 = 0, SCALES_4 = 1, SCALES_1 = 2 };
-__device__ __forceinline__ int scale_loads(int nb, const void* p, const void* q, const void* r) {
-  const uintptr_t a = (uintptr_t)nb | (uintptr_t)p | (uintptr_t)q | (uintptr_t)r;
-  return (a & 15u) == 0 ? SCALES_16 : (a & 3u) == 0 ? SCALES_4 : SCALES_1;
-}
-__device__ __forceinline__ uint4 scale_words(const uint8_t* row, int k, int nb, int loads) {
-  if (loads == SCALES_16) return *reinterpret_cast<const uint4*>(row + k);
-  uint32_t w[4];
-  if (loads == SCALES_4) {
+// Scale bytes k .. k + 15 of a row of nb (four scale groups): one 16-byte load where rows start on 16 bytes, else the
+// aligned words that hold a byte of the row, shifted into place.  Bytes behind the row are whatever lies there: no k-block
+// asks for them.
+__device__ __forceinline__ bool scales_aligned(int64_t ld, const void* p) { return (((uintptr_t)ld | (uintptr_t)p) & 15u) == 0; }
+__device__ __forceinline__ uint4 scale_words(const uint8_t* row, int k, int nb, bool aligned) {
+  if (aligned) return *reinterpret_cast<const uint4*>(row + k);
+  const uintptr_t at = (uintptr_t)(row + k), end = (uintptr_t)(row + nb);
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~(uintptr_t)3);
+  const uint32_t shift = (uint32_t)(at & 3u) * 8u;
+  uint32_t v[5];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = k + 4 * i < nb ? *reinterpret_cast<const uint32_t*>(row + k + 4 * i) : 0x7f7f7f7fu;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[i] |= (k + 4 * i + j < nb ? (uint32_t)row[k + 4 * i + j] : 127u) << (8 * j);
-    }
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int i = 0; i < 5; ++i) v[i] = (uintptr_t)(w + i) < end ? w[i] : 0u;
+  return make_uint4(__funnelshift_r(v[0], v[1], shift), __funnelshift_r(v[1], v[2], shift), __funnelshift_r(v[2], v[3], shift),
+                    __funnelshift_r(v[3], v[4], shift));
 }
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ void put_words(uint32_t saddr, int lane, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {

@@ -39,28 +39,41 @@ struct Eight {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) * 2; ++i) w[i] = 0u;
   }
-  __device__ __forceinline__ float at(int i) const {
-    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-    else return __uint_as_float((i & 1) ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-  }
   // bit pattern of the largest magnitude: of non-negative floats the larger has the larger pattern; NaN is above all
   __device__ __forceinline__ uint32_t top() const {
-    uint32_t m = 0;
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
+      const __nv_bfloat162 m2 = __hmax2_nan(__hmax2_nan(__habs2(h[0]), __habs2(h[1])), __hmax2_nan(__habs2(h[2]), __habs2(h[3])));
+      const uint32_t m = *reinterpret_cast<const uint32_t*>(&m2);
+      return max(m << 16, m & 0xffff0000u);
+    } else {
+      uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(at(i)) & 0x7fffffffu);
-    return m;
+      for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+      return m;
+    }
+  }
+  // codes of elements 2i (low byte) and 2i + 1 under scale code `code` (a power of two: exact in bf16 as in fp32, but for
+  // results below 2^-126, which become zero codes either way)
+  __device__ __forceinline__ uint32_t codes(int i, uint32_t code) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t f = (254u - code) << 7, f2 = f | f << 16;
+      const __nv_bfloat162 p = __hmul2(reinterpret_cast<const __nv_bfloat162*>(w)[i], *reinterpret_cast<const __nv_bfloat162*>(&f2));
+      const uint32_t q = *reinterpret_cast<const uint32_t*>(&p);
+      return to_e4m3x2(__uint_as_float(q << 16), __uint_as_float(q & 0xffff0000u));
+    } else {
+      const float f = inv_scale(code);
+      return to_e4m3x2(__uint_as_float(w[2 * i]) * f, __uint_as_float(w[2 * i + 1]) * f);
+    }
   }
 };
 
 template <typename T, bool VEC>
 __device__ __forceinline__ void store8(uint8_t* p, int left, const Eight<T, VEC>& v, uint32_t code) {
-  uint32_t lo, hi;
-  if (code == (uint32_t)Q_NAN_SCALE) {
-    lo = hi = 0x7f7f7f7fu;
-  } else {
-    const float f = inv_scale(code);
-    lo = to_e4m3x2(v.at(0) * f, v.at(1) * f) | (to_e4m3x2(v.at(2) * f, v.at(3) * f) << 16);
-    hi = to_e4m3x2(v.at(4) * f, v.at(5) * f) | (to_e4m3x2(v.at(6) * f, v.at(7) * f) << 16);
+  uint32_t lo = 0x7f7f7f7fu, hi = 0x7f7f7f7fu;
+  if (code != (uint32_t)Q_NAN_SCALE) {
+    lo = v.codes(0, code) | (v.codes(1, code) << 16);
+    hi = v.codes(2, code) | (v.codes(3, code) << 16);
   }
   if constexpr (VEC) {
     *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
@@ -71,40 +84,40 @@ __device__ __forceinline__ void store8(uint8_t* p, int left, const Eight<T, VEC>
   }
 }
 
-// Rows: half a warp per block of 128 columns, QROW_U blocks per half-warp in flight.  Bound by HBM (3 bytes per bf16
-// element).  The grid is no larger than what is resident and walks the rows that exist, so that *n_rows is read once per
-// warp and not in front of every load.
+// Rows: half a warp per block of 128 columns, a warp per QROW_U pairs of blocks, all of them in flight.  Bound by HBM (3
+// bytes per bf16 element) and, close behind, by instructions: bf16 is searched and scaled two at a time.
+// (A grid that fits the GPU once and walks the rows was slower: 41 us against 35 for 15,000 rows of 4096.)
 constexpr int QROW_U = 4;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(QN)
-k_quantize_rows(const T* __restrict__ x, const int32_t* __restrict__ n_rows, int rows, int d, int per_row, uint8_t* __restrict__ q,
-                uint8_t* __restrict__ scale) {
+k_quantize_rows(const T* __restrict__ x, const int32_t* __restrict__ n_rows, int rows, int d, uint32_t per_row, uint8_t* __restrict__ q,
+                uint8_t* __restrict__ scale, int64_t scale_ld) {
   allow_next_kernel();
   wait_for_previous_kernel();
   const int lane = threadIdx.x & 31, sub = lane & 15;
   const int nb = (d + QBLOCK - 1) / QBLOCK;
-  if (n_rows) rows = min(rows, max(*n_rows, 0));
-  const int64_t units = (int64_t)rows * per_row, step = (int64_t)gridDim.x * (QN / 32);
-  for (int64_t unit = (int64_t)blockIdx.x * (QN / 32) + (threadIdx.x >> 5); unit < units; unit += step) {
-    const int64_t r = per_row == 1 ? unit : unit / per_row;
-    const int b0 = (int)(unit - r * per_row) * 2 * QROW_U + (lane >> 4);
-    Eight<T, VEC> v[QROW_U];
+  const uint32_t unit = blockIdx.x * (QN / 32) + (threadIdx.x >> 5);
+  const uint32_t row = unit / per_row;
+  if (n_rows) rows = min(rows, *n_rows);
+  if ((int64_t)row >= rows) return;
+  const int64_t r = row;
+  const int b0 = (int)(unit - row * per_row) * 2 * QROW_U + (lane >> 4);
+  Eight<T, VEC> v[QROW_U];
 #pragma unroll
-    for (int u = 0; u < QROW_U; ++u) {
-      const int c = (b0 + 2 * u) * QBLOCK + sub * 8;
-      if (c < d) v[u].load(x + r * d + c, d - c);
-      else v[u].clear();
-    }
+  for (int u = 0; u < QROW_U; ++u) {
+    const int c = (b0 + 2 * u) * QBLOCK + sub * 8;
+    if (c < d) v[u].load(x + r * d + c, d - c);
+    else v[u].clear();
+  }
 #pragma unroll
-    for (int u = 0; u < QROW_U; ++u) {
-      const int b = b0 + 2 * u, c = b * QBLOCK + sub * 8;
-      uint32_t m = v[u].top();
+  for (int u = 0; u < QROW_U; ++u) {
+    const int b = b0 + 2 * u, c = b * QBLOCK + sub * 8;
+    uint32_t m = v[u].top();
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const uint32_t code = scale_code(m);
-      if (c < d) store8(q + r * d + c, d - c, v[u], code);
-      if (sub == 0 && b < nb) scale[r * nb + b] = (uint8_t)code;
-    }
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const uint32_t code = scale_code(m);
+    if (c < d) store8(q + r * d + c, d - c, v[u], code);
+    if (sub == 0 && b < nb) scale[r * scale_ld + b] = (uint8_t)code;
   }
 }
 
@@ -179,15 +192,15 @@ k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const u
 }
 
 template <typename T>
-int quantize_rows_run(const void* x, const int32_t* n_rows, int64_t rows, int d, void* q, void* scale, cudaStream_t st) {
-  const int per_row = (int)ceil_div(ceil_div(d, QBLOCK), 2 * QROW_U);
-  const int64_t want = ceil_div(rows * per_row, QN / 32), most = (int64_t)sm_count() * 6;
-  const unsigned grid = (unsigned)(want < most ? want : most);
+int quantize_rows_run(const void* x, const int32_t* n_rows, int64_t rows, int d, void* q, void* scale, int64_t scale_ld, cudaStream_t st) {
+  const uint32_t per_row = (uint32_t)ceil_div(ceil_div(d, QBLOCK), 2 * QROW_U);
+  if (rows * per_row >= ((int64_t)1 << 32) - QN) return CAPMOE_EUNSUPPORTED;
+  const unsigned grid = (unsigned)ceil_div(rows * per_row, QN / 32);
   // 16-byte loads of eight columns need rows that start on 16 bytes; the codes' rows then start on 8
   const int rc = note_cuda(d % 8 == 0 ? launch_chained(k_quantize_rows<T, true>, grid, QN, 0, st, (const T*)x, n_rows, (int)rows, d,
-                                                       per_row, (uint8_t*)q, (uint8_t*)scale)
+                                                       per_row, (uint8_t*)q, (uint8_t*)scale, scale_ld)
                                       : launch_chained(k_quantize_rows<T, false>, grid, QN, 0, st, (const T*)x, n_rows, (int)rows, d,
-                                                       per_row, (uint8_t*)q, (uint8_t*)scale));
+                                                       per_row, (uint8_t*)q, (uint8_t*)scale, scale_ld));
   count_launch(1);
   return rc;
 }
@@ -235,18 +248,22 @@ bool usable(P... p) {
 }
 
 // Workspace of the 8-bit FFN: codes and scales of x and of the hidden rows, and (sizes without a
-// tensor-core kernel) the hidden rows in fp32.
-struct FfnWs { size_t xq, xs, hq, hs, h, total; };
+// tensor-core kernel) the hidden rows in fp32.  Rows of scales start on 16 bytes (one load for 16 of them: with packed rows
+// of 11 the down product of 43,000 rows took 100 us more), except where the fallback product reads them.
+struct FfnWs { size_t xq, xs, hq, hs, h, total; int64_t xs_ld, hs_ld; };
 FfnWs ffn_ws(int64_t A_max, int d, int F) {
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   const size_t A = (size_t)A_max;
   FfnWs w;
+  const int64_t pad = gmm8_supported(d, F) ? 16 : 1;
+  w.xs_ld = ceil_div(ceil_div(d, QBLOCK), pad) * pad;
+  w.hs_ld = ceil_div(ceil_div(F, QBLOCK), pad) * pad;
   w.xq = 0;
   w.xs = w.xq + up(A * d);
-  w.hq = w.xs + up(A * ceil_div(d, QBLOCK));
+  w.hq = w.xs + up(A * w.xs_ld);
   w.hs = w.hq + up(A * F);
-  w.h = w.hs + up(A * ceil_div(F, QBLOCK));
-  w.total = w.h + (gmm8_tc_supported(d, F) ? 0 : up(A * F * 4)) + 256;
+  w.h = w.hs + up(A * w.hs_ld);
+  w.total = w.h + (gmm8_supported(d, F) ? 0 : up(A * F * 4)) + 256;
   return w;
 }
 
@@ -262,8 +279,8 @@ extern "C" int capmoe_quantize_rows(const void* x, const int32_t* n_rows, int64_
   if (rows >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
   if (rows == 0) return CAPMOE_OK;
   if (!usable(x, q) || !scale) return CAPMOE_EINVAL;
-  if (dtype == CAPMOE_F32) return quantize_rows_run<float>(x, n_rows, rows, d, q, scale, as_stream(stream));
-  return quantize_rows_run<__nv_bfloat16>(x, n_rows, rows, d, q, scale, as_stream(stream));
+  if (dtype == CAPMOE_F32) return quantize_rows_run<float>(x, n_rows, rows, d, q, scale, ceil_div(d, QBLOCK), as_stream(stream));
+  return quantize_rows_run<__nv_bfloat16>(x, n_rows, rows, d, q, scale, ceil_div(d, QBLOCK), as_stream(stream));
 }
 
 extern "C" int capmoe_quantize_weights(const void* w, int E, int n, int d, int dtype, void* q, void* scale, void* stream) {
@@ -277,15 +294,14 @@ extern "C" int capmoe_quantize_weights(const void* w, int E, int n, int d, int d
 extern "C" int capmoe_grouped_mm_fp8(const void* x_q, const void* x_scale, const int32_t* expert_offsets, const void* w_q,
                                      const void* w_scale, int E, int d, int n, void* y, int64_t rows, int32_t* dev_status,
                                      void* stream) {
-  const int rc = check_shape(expert_offsets, E, d, n, rows);
+  int rc = check_shape(expert_offsets, E, d, n, rows);
   if (rc != CAPMOE_OK || rows == 0) return rc;
   if (!usable(x_q, w_q, y) || !x_scale || !w_scale) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
-  if (gmm8_tc_supported(d, n)) {
-    const int rc2 = dev_status ? clear_words(dev_status + 1, 1, nullptr, 0, as_stream(stream)) : CAPMOE_OK;
-    if (rc2 != CAPMOE_OK) return rc2;
-    return gmm8_tc((const uint8_t*)x_q, (const uint8_t*)x_scale, sg, (const uint8_t*)w_q, (const uint8_t*)w_scale, d, n, y,
-                   dev_status, dev_status ? dev_status + 1 : nullptr, as_stream(stream));
+  if (gmm8_supported(d, n)) {
+    if ((rc = begin_counters(dev_status, 1, as_stream(stream))) != CAPMOE_OK) return rc;
+    return gmm8((const uint8_t*)x_q, (const uint8_t*)x_scale, ceil_div(d, QBLOCK), sg, (const uint8_t*)w_q, (const uint8_t*)w_scale, d, n, y,
+                dev_status, counter_at(dev_status, 0), as_stream(stream));
   }
   const uint8_t* none = nullptr;
   return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, n, as_stream(stream), (const uint8_t*)x_q, (const uint8_t*)x_scale,
@@ -310,22 +326,22 @@ extern "C" int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_
   const Segments sg{expert_offsets, E, (int)A_max};
   cudaStream_t st = as_stream(stream);
   uint8_t* b = (uint8_t*)ws;
-  const bool tc = gmm8_tc_supported(d, F);
-  if (tc && dev_status && (rc = clear_words(dev_status + 1, 2, nullptr, 0, st)) != CAPMOE_OK) return rc;
-  rc = quantize_rows_run<__nv_bfloat16>(x_perm, expert_offsets + E, A_max, d, b + w.xq, b + w.xs, st);
+  const bool tc = gmm8_supported(d, F);
+  if (tc && (rc = begin_counters(dev_status, 2, st)) != CAPMOE_OK) return rc;
+  rc = quantize_rows_run<__nv_bfloat16>(x_perm, expert_offsets + E, A_max, d, b + w.xq, b + w.xs, w.xs_ld, st);
   if (rc != CAPMOE_OK) return rc;
   if (tc) {
-    rc = gmm8_tc_swiglu(b + w.xq, b + w.xs, sg, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
-                        (const uint8_t*)wu_scale, d, F, b + w.hq, b + w.hs, dev_status, dev_status ? dev_status + 1 : nullptr, st);
+    rc = gmm8_swiglu(b + w.xq, b + w.xs, w.xs_ld, sg, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
+                        (const uint8_t*)wu_scale, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(dev_status, 0), st);
     if (rc != CAPMOE_OK) return rc;
-    return gmm8_tc(b + w.hq, b + w.hs, sg, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, F, d, y_perm, dev_status,
-                   dev_status ? dev_status + 2 : nullptr, st);
+    return gmm8(b + w.hq, b + w.hs, w.hs_ld, sg, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, F, d, y_perm, dev_status,
+                counter_at(dev_status, 1), st);
   }
   float* h = (float*)(b + w.h);
   rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, b + w.xq, b + w.xs, (const uint8_t*)wg_q, (const uint8_t*)wg_scale,
                     (const uint8_t*)wu_q, (const uint8_t*)wu_scale, h, sg, d, F);
   if (rc != CAPMOE_OK) return rc;
-  rc = quantize_rows_run<float>(h, expert_offsets + E, A_max, F, b + w.hq, b + w.hs, st);
+  rc = quantize_rows_run<float>(h, expert_offsets + E, A_max, F, b + w.hq, b + w.hs, w.hs_ld, st);
   if (rc != CAPMOE_OK) return rc;
   const uint8_t* none = nullptr;
   return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, d, st, b + w.hq, b + w.hs, (const uint8_t*)wd_q,

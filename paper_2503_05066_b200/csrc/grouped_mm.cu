@@ -239,36 +239,42 @@ using namespace capmoe;
 
 extern "C" int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n,
                                  int dtype, void* y, int64_t rows, int32_t* dev_status, void* stream) {
-  const int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
+  int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
   if (rc != CAPMOE_OK || rows == 0) return rc;
   if (!usable(x_rows, w, y)) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
-  if (gmm_tc_supported(E, d, n, dtype)) return gmm_tc_fwd(x_rows, sg, w, d, n, y, dev_status, as_stream(stream));
+  if (gmm_supported(E, d, n, dtype)) {
+    if ((rc = begin_counters(dev_status, 1, as_stream(stream))) != CAPMOE_OK) return rc;
+    return gmm_fwd(x_rows, sg, w, d, n, y, dev_status, counter_at(dev_status, 0), as_stream(stream));
+  }
   if (dtype == CAPMOE_F32) return rows_simt<float, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
   return rows_simt<__nv_bfloat16, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
 }
 
 extern "C" int capmoe_grouped_mm_dx(const void* dy_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n,
                                     int dtype, void* dx, int64_t rows, int32_t* dev_status, void* stream) {
-  const int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
+  int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
   if (rc != CAPMOE_OK || rows == 0) return rc;
   if (!usable(dy_rows, w, dx)) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
-  if (gmm_tc_supported(E, d, n, dtype)) return gmm_tc_dx(dy_rows, sg, w, d, n, dx, dev_status, as_stream(stream));
+  if (gmm_supported(E, d, n, dtype)) {
+    if ((rc = begin_counters(dev_status, 1, as_stream(stream))) != CAPMOE_OK) return rc;
+    return gmm_dx(dy_rows, sg, w, d, n, dx, dev_status, counter_at(dev_status, 0), as_stream(stream));
+  }
   if (dtype == CAPMOE_F32) return rows_simt<float, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
   return rows_simt<__nv_bfloat16, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
 }
 
 extern "C" int capmoe_grouped_mm_dw_workspace_bytes(int E, size_t* bytes) {
   if (!bytes || E < 1) return CAPMOE_EINVAL;
-  *bytes = gmm_tc_map_bytes(E, 2) + 256;                     // 256: to align the maps
+  *bytes = gmm_dw_map_bytes(E, 2) + 256;                     // 256: to align the maps
   return CAPMOE_OK;
 }
 
 extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, const int32_t* expert_offsets, int E, int d,
                                     int n, int dtype, int out_dtype, void* dw, int64_t rows, void* ws, size_t ws_bytes,
                                     int32_t* dev_status, void* stream) {
-  const int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
+  int rc = check_shape(expert_offsets, E, d, n, dtype, rows);
   if (rc != CAPMOE_OK) return rc;
   if (out_dtype != CAPMOE_F32 && out_dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
   if (dtype == CAPMOE_F32 && out_dtype != CAPMOE_F32) return CAPMOE_EUNSUPPORTED;
@@ -280,8 +286,10 @@ extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, con
   if (ws_bytes < need) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)rows};
   cudaStream_t st = as_stream(stream);
-  if (gmm_tc_supported(E, d, n, dtype))
-    return gmm_tc_dw(dy_rows, x_rows, sg, d, n, out_dtype == CAPMOE_F32, dw, align256(ws), dev_status, st);
+  if (gmm_supported(E, d, n, dtype)) {
+    if ((rc = begin_counters(dev_status, 1, st)) != CAPMOE_OK) return rc;
+    return gmm_dw(dy_rows, x_rows, sg, d, n, out_dtype == CAPMOE_F32, dw, align256(ws), dev_status, counter_at(dev_status, 0), st);
+  }
   if (dtype == CAPMOE_F32)
     return dw_simt(DwSet<float, float>{{(const float*)dy_rows}, {(const float*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
   using B = __nv_bfloat16;
@@ -293,7 +301,7 @@ extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, con
 extern "C" int capmoe_ffn_backward_workspace_bytes(int64_t A_max, int E, int F, int dtype, size_t* bytes) {
   if (!bytes || A_max < 0 || E < 1 || F < 1) return CAPMOE_EINVAL;
   if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
-  *bytes = (size_t)A_max * (size_t)F * elt_size(dtype) * 3 + align256(gmm_tc_map_bytes(E, 5)) + 256;
+  *bytes = (size_t)A_max * (size_t)F * elt_size(dtype) * 3 + align256(gmm_dw_map_bytes(E, 5)) + 256;
   return CAPMOE_OK;
 }
 
@@ -315,10 +323,18 @@ extern "C" int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_pe
   capmoe_ffn_backward_workspace_bytes(A_max, E, F, dtype, &need);
   if (ws_bytes < need) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)A_max};
-  uint8_t* maps = (uint8_t*)align256(ws);
-  if (gmm_tc_supported(E, d, F, dtype))
-    return gmm_tc_ffn_grad(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, maps,
-                           maps + align256(gmm_tc_map_bytes(E, 5)), dev_status, st);
+  if (gmm_supported(E, d, F, dtype)) {
+    uint8_t* maps = (uint8_t*)align256(ws);
+    __nv_bfloat16* dg = (__nv_bfloat16*)(maps + align256(gmm_dw_map_bytes(E, 5)));
+    __nv_bfloat16 *du = dg + A_max * F, *h = du + A_max * F;
+    rc = begin_counters(dev_status, 3, st);
+    if (rc == CAPMOE_OK) rc = gmm_dw_ffn_maps(dg, du, dy_perm, x_perm, h, sg, d, F, maps, st);
+    if (rc == CAPMOE_OK)
+      rc = gmm_hidden(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dg, du, h, dev_status, counter_at(dev_status, 0), st);
+    if (rc == CAPMOE_OK) rc = gmm_dx2(dg, du, sg, d, F, w_gate, w_up, dx_perm, dev_status, counter_at(dev_status, 1), st);
+    if (rc != CAPMOE_OK) return rc;
+    return gmm_dw_ffn(sg, d, F, dw_gate, dw_up, dw_down, maps, dev_status, counter_at(dev_status, 2), st);
+  }
   if (dtype == CAPMOE_F32)
     return ffn_grad_simt<float>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws, st);
   return ffn_grad_simt<__nv_bfloat16>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws,

@@ -63,6 +63,16 @@ def test_quantize_borders(cm):
     assert s.view(torch.uint8)[0, 0] == 127 and s.view(torch.uint8)[1, 0] == 128 and s.view(torch.uint8)[8, 0] == 0
 
 
+def test_quantize_smallest_bf16_numbers(cm):
+    """Maxima and values below the smallest normal number, and blocks whose scale is clamped at 2^-127."""
+    x = torch.zeros((4, 256), device="cuda", dtype=BF16)
+    for i, top in enumerate((2.0 ** -118, 2.0 ** -126, 2.0 ** -133, 1.0)):
+        x[i] = (torch.linspace(-1, 1, 256, device="cuda", dtype=torch.float64) * top).to(BF16)
+    x[3, 1::2] = (torch.linspace(-1, 1, 128, device="cuda", dtype=torch.float64) * 2.0 ** -127).to(BF16)
+    q, s = cm.quantize_rows(x)
+    assert R.same_codes(q, s, R.quantized(x.double(), 1))
+
+
 def test_quantize_largest_numbers(cm):
     x = torch.zeros((3, 128), device="cuda", dtype=F32)
     x[:, ::3] = torch.tensor([3.4e38, -3.0e38, 2.0 ** 127], device="cuda")[:, None]
@@ -124,7 +134,7 @@ def test_product(cm, name, d, n):
     _mm(cm, COUNTS[name], d, n)
 
 
-@pytest.mark.parametrize("d,n", [(256, 512), (144, 272), (1936, 400)])
+@pytest.mark.parametrize("d,n", [(256, 512), (144, 272), (1936, 400), (400, 48)])
 @pytest.mark.parametrize("name", ["long", "longer", "many"])
 def test_product_long_and_many_segments(cm, name, d, n):
     _mm(cm, COUNTS[name], d, n)
@@ -134,15 +144,6 @@ def test_product_long_and_many_segments(cm, name, d, n):
 def forced(cm):
     yield lambda name: cm.debug_ffn_variant(name)
     cm.debug_ffn_variant("auto")
-
-
-@pytest.mark.parametrize("form", ["pair", "short"])
-@pytest.mark.parametrize("d,n", [(256, 512), (144, 272), (1936, 400), (400, 48)])
-@pytest.mark.parametrize("name", ["few", "borders", "longer", "many"])
-def test_product_in_both_forms(cm, forced, name, d, n, form):
-    forced(form)
-    _mm(cm, COUNTS[name], d, n)
-    _mm(cm, COUNTS[name], d, n, status=False)
 
 
 def test_product_without_a_status_block(cm):

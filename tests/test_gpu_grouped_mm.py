@@ -88,26 +88,10 @@ def test_products_and_gradients(cm, name, d, n, dtype):
     _check_all(cm, COUNTS[name], d, n, dtype)
 
 
-@pytest.mark.parametrize("d,n", [(256, 512), (136, 72), (1032, 264), (250, 515)])
+@pytest.mark.parametrize("d,n", [(256, 512), (136, 72), (1032, 264), (320, 1032), (250, 515)])
 @pytest.mark.parametrize("name", ["long", "longer", "many"])
 def test_long_and_many_segments(cm, name, d, n):
     _check_all(cm, COUNTS[name], d, n, BF16)
-
-
-@pytest.fixture
-def forced(cm):
-    """Forces one tensor-core form for a test."""
-    yield lambda name: cm.debug_ffn_variant(name)
-    cm.debug_ffn_variant("auto")
-
-
-@pytest.mark.parametrize("form", ["pair", "short"])
-@pytest.mark.parametrize("d,n", [(256, 512), (136, 72), (320, 1032)])
-@pytest.mark.parametrize("name", ["few", "borders", "longer", "many"])
-def test_both_forms(cm, forced, name, d, n, form):
-    forced(form)
-    _check_all(cm, COUNTS[name], d, n, BF16)
-    _check_all(cm, COUNTS[name], d, n, BF16, status=False)
 
 
 def test_many_segments_fp32(cm):
@@ -173,17 +157,10 @@ def _check_ffn_gradient(cm, counts, d, F, dtype):
             R.close(got[k][e], *ref[k])
 
 
-@pytest.mark.parametrize("form", ["pair", "short"])
-@pytest.mark.parametrize("counts,d,F", [([3, 0, 70, 129, 1], 128, 192), ([65, 64, 17], 136, 72), ([300, 0, 513, 41], 256, 320),
-                                        ([1] * 30, 64, 264)])
-def test_ffn_gradient_in_both_forms(cm, forced, counts, d, F, form):
-    forced(form)
-    _check_ffn_gradient(cm, counts, d, F, BF16)
-
-
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("counts,d,F", [([1], 64, 64), ([0, 0], 64, 64), ([3, 0, 70, 129, 1], 128, 192), ([65, 64, 17], 136, 72),
-                                        ([5, 9, 0, 33], 33, 45), ([300, 0, 513], 256, 320)])
+                                        ([5, 9, 0, 33], 33, 45), ([300, 0, 513], 256, 320), ([1] * 30, 64, 264),
+                                        ([1200, 0, 33], 136, 192)])
 def test_ffn_gradient(cm, counts, d, F, dtype):
     _check_ffn_gradient(cm, counts, d, F, dtype)
 
