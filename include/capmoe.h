@@ -287,6 +287,7 @@ int capmoe_grouped_ffn_segments(const void* x_rows, const int32_t* seg_begin, co
  *                          dx_perm [A_max,d], dw_gate/dw_up [E,F,d], dw_down [E,d,F], all in `dtype`.
  *                          dg, du and h are rounded to `dtype` before the products that read them.
  *                          ws: capmoe_ffn_backward_workspace_bytes(A_max,E,F,dtype) bytes.
+ * Outputs and workspace overlap neither each other nor an input.
  * bf16 with d and n (F) multiples of 8 runs on tensor cores (TMA-fed tiles, fp32 accumulators); fp32 and other
  * sizes run plain fp32-FMA kernels.  dev_status as in capmoe_grouped_ffn.  E <= 256, rows < 2^31. */
 int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n, int dtype,
@@ -414,7 +415,8 @@ int capmoe_ep_forward_combine(const capmoe_ep_rank* P, void* stream);
 /* Which tensor-core kernel capmoe_grouped_ffn* and the layer forward use for bf16 shapes, for the whole
  * process: 0 = chosen from the shape (the default), 1 = CTA pairs with 256-token tiles, 2 = one CTA per
  * 128-token tile, 3 = the short-segment form (256 weight rows x up to 256 tokens per pair, tokens in
- * steps of 16), 4 = that form for the down GEMM only, behind the gate/up kernel the shape selects.  All compute the same thing (Eq. 2's experts); tests force each on the same inputs.
+ * steps of 16), 4 = that form for the down GEMM only, behind the gate/up kernel the shape selects.  For the gate/up product of
+ * capmoe_grouped_ffn_fp8, 1 and 3 choose between tokens on the M side and on the N side of the MMA.  All compute the same thing (Eq. 2's experts); tests force each on the same inputs.
  * A variant the device cannot run (fewer than two SMs per straggler group) returns
  * CAPMOE_EUNSUPPORTED at the next FFN call.  Not stream-ordered: set it while no FFN call is being issued. */
 int capmoe_debug_ffn_variant(int variant);

@@ -282,3 +282,44 @@ def test_guard_bands(cm):
         torch.cuda.synchronize()
         for raw in raws:
             assert bool((raw[:G] == 0xA5).all()) and bool((raw[-G:] == 0xA5).all())
+
+
+def test_two_streams_at_once_give_what_one_gives(cm):
+    counts = [300, 0, 77, 1200, 5, 640]
+    off = R.offsets_of(counts)
+    A = sum(counts)
+    x = _normal((A, 512), 1.0, BF16, 40)
+    w = [cm.quantize_weights(_normal(s, 0.08, BF16, 41 + i)) for i, s in enumerate(((6, 768, 512), (6, 768, 512), (6, 512, 768)))]
+
+    def calls(st):
+        q = cm.quantize_rows(x, off)
+        return cm.grouped_mm_fp8(*q, off, *w[0], dev_status=st), cm.grouped_ffn_fp8(x, off, *w, dev_status=st)
+
+    want = calls(_block(cm))
+    torch.cuda.synchronize()
+    streams, blocks = [torch.cuda.Stream() for _ in range(3)], [_block(cm) for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = []
+        for s, b in zip(streams, blocks):
+            with torch.cuda.stream(s):
+                got.append(calls(b))
+        torch.cuda.synchronize()
+        for g in got:
+            assert torch.equal(g[0], want[0]) and torch.equal(g[1], want[1])
+    assert all(int(b[0]) == 0 for b in blocks)
+
+
+def test_matrices_past_32_bit_offsets(cm):
+    rows, d = 1_100_000, 2048
+    x = torch.empty((rows, d), device="cuda", dtype=BF16)
+    x[:] = _normal((1, d), 1.0, BF16, 50)
+    x[-400:] = _normal((400, d), 1.0, BF16, 51)
+    q, s = cm.quantize_rows(x)
+    assert R.same_codes(q[-400:], s[-400:], R.quantized(x[-400:].double(), 1))
+    assert R.same_codes(q[rows // 2:][:8], s[rows // 2:][:8], R.quantized(x[rows // 2:][:8].double(), 1))
+    wq, ws = cm.quantize_weights(_normal((2, 64, d), 0.05, BF16, 52))
+    off = R.offsets_of([rows - 400, 400])
+    y = cm.grouped_mm_fp8(q, s, off, wq, ws)
+    for e, r in ((0, slice(rows - 500, rows - 400)), (1, slice(rows - 400, rows))):
+        R.close(y[r], *R.product(R.decoded(q[r], s[r], 1), R.decoded(wq[e], ws[e], 128), BF16))

@@ -40,7 +40,7 @@ COUNTS = {
     "many": [(7 * e) % 23 for e in range(256)],
 }
 # (d, n): whole tiles, multiples of 64 and of 8 that leave ragged tiles, and sizes with no 16-byte rows
-SIZES = [(256, 512), (64, 64), (192, 320), (136, 72), (8, 264), (520, 24), (33, 65), (250, 515), (1, 7), (7, 1)]
+SIZES = [(256, 512), (64, 64), (192, 320), (136, 72), (8, 264), (520, 24), (33, 65), (250, 515), (1, 7), (7, 1), (64, 33), (33, 64)]
 
 
 def _case(counts, d, n, dtype, spare=5):
@@ -302,3 +302,78 @@ def test_guard_bands(cm):
         for raw in raws:
             assert bool((raw[:G] == 7).all()) and bool((raw[-G:] == 7).all())
             assert not bool((raw[G:-G] == 7).all())
+
+
+def _at(t, shift):
+    """The tensor's values in memory that starts `shift` bytes behind an allocation's start."""
+    raw = torch.zeros(t.numel() * t.element_size() + shift, device="cuda", dtype=torch.uint8)
+    v = raw[shift:].view(t.dtype).view(t.shape)
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("dtype,d,n", [(BF16, 136, 72), (BF16, 33, 65), (F32, 64, 96), (F32, 33, 65)])
+def test_buffers_that_start_on_16_bytes(cm, dtype, d, n):
+    counts = [70, 0, 5, 200]
+    off, A, rows, x, dy, w = _case(counts, d, n, dtype)
+    want = cm.grouped_mm(x, off, w)[:A], cm.grouped_mm_dx(dy, off, w)[:A], cm.grouped_mm_dw(dy, x, off)
+    x2, dy2, w2 = _at(x, 16), _at(dy, 48), _at(w, 16)
+    ws = torch.empty(1 << 16, device="cuda", dtype=torch.uint8)[16:]
+    got = (cm.grouped_mm(x2, off, w2, y=_at(torch.zeros((rows, n), device="cuda", dtype=dtype), 16))[:A],
+           cm.grouped_mm_dx(dy2, off, w2, dx=_at(torch.zeros((rows, d), device="cuda", dtype=dtype), 80))[:A],
+           cm.grouped_mm_dw(dy2, x2, off, dw=_at(torch.zeros((4, n, d), device="cuda", dtype=dtype), 16), ws=ws))
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+def test_misaligned_buffers_are_refused(cm):
+    off = R.offsets_of([3, 4])
+    x, w = _normal((7, 64), 1.0, BF16, 1), _normal((2, 32, 64), 0.1, BF16, 2)
+    with pytest.raises(cm.CapmoeError) as err:
+        cm.grouped_mm(_at(x, 8), off, w)
+    assert err.value.status == cm.EINVAL
+
+
+def test_two_streams_at_once_give_what_one_gives(cm):
+    """Calls that overlap on the GPU, each with its own status block and workspace; the tiles are handed out differently
+    every time and every result is the same bits."""
+    counts = [300, 0, 77, 1200, 5, 640]
+    off, A, rows, x, dy, w = _case(counts, 512, 768, BF16)
+    wd, dyx = _normal((6, 512, 768), 0.1, BF16, 30), _rows((rows, 512), A, 1.0, BF16, 31)
+
+    def calls(st):
+        return [cm.grouped_mm(x, off, w, dev_status=st)[:A], cm.grouped_mm_dx(dy, off, w, dev_status=st)[:A],
+                cm.grouped_mm_dw(dy, x, off, dev_status=st),
+                *(t[:A] if i == 0 else t for i, t in enumerate(cm.grouped_ffn_backward(x, dyx, off, w, w, wd, dev_status=st)))]
+
+    want = calls(_block(cm))
+    torch.cuda.synchronize()
+    streams, blocks = [torch.cuda.Stream() for _ in range(3)], [_block(cm) for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = []
+        for s, b in zip(streams, blocks):
+            with torch.cuda.stream(s):
+                got.append(calls(b))
+        torch.cuda.synchronize()
+        for g in got:
+            assert all(torch.equal(a, b) for a, b in zip(want, g))
+    assert all(int(b[0]) == 0 for b in blocks)
+
+
+def test_matrices_past_32_bit_offsets(cm):
+    """More than 2^31 elements in the rows of one side."""
+    rows, d, n = 1_100_000, 64, 2048
+    counts = [rows - 300, 0, 300]
+    off = R.offsets_of(counts)
+    x, w = _normal((rows, d), 1.0, BF16, 1), _normal((3, n, d), 0.1, BF16, 2)
+    y = cm.grouped_mm(x, off, w)
+    at = torch.tensor([0, 1, rows // 2, rows - 301, rows - 300, rows - 1], device="cuda")
+    for e, r in ((0, at[:4]), (2, at[4:])):
+        R.close(y[r], *R.product(x[r].double(), w[e].double(), BF16))
+    dx = cm.grouped_mm_dx(y, off, w)
+    for e, r in ((0, at[:4]), (2, at[4:])):
+        R.close(dx[r], *R.product(y[r].double(), w[e].double().T, BF16))
+    dw = cm.grouped_mm_dw(y, x, off)
+    R.close(dw[2], *R.product(y[-300:].double().T, x[-300:].double().T, BF16))
+    assert bool((dw[1] == 0).all()) and bool(torch.isfinite(dw.float()).all())
