@@ -441,16 +441,12 @@ def _run(name: str, stream, like, *args):
             if v.get_device() != here or here < 0:
                 _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
             assert v.is_contiguous(), "capmoe tensors must be contiguous"
-            v = v.data_ptr()
-        raw.append(v)
-    if here != torch.cuda.current_device():
+            raw.append(v.data_ptr())
+        else:
+            raw.append(v)
+    if here != torch._C._cuda_getDevice():
         _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
-    fn = getattr(lib(), name)
-    if stream is None:
-        raw.append(torch._C._cuda_getCurrentRawStream(here))
-    else:
-        raw.append(stream.cuda_stream)
-    rc = fn(*raw)
+    rc = getattr(_lib or lib(), name)(*raw, torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream)
     if rc != OK:
         raise CapmoeError(rc, name)
 

@@ -49,19 +49,23 @@ inline bool use_short(const Segments& sg, int64_t limit) {
 
 // Tensor-core kernels.  All matrices 16-byte aligned, `sched` a zeroed tile counter or NULL.
 // bf16 (gmm_rows.cu, gmm_dw.cu): rows of whole 16-byte vectors; dw's E * n (E * d) rows are 32-bit coordinates.  map_ws is
-// 128-byte aligned with gmm_dw_map_bytes(E, lists) bytes (gmm_dw: 2 lists, gmm_dw_ffn_maps: 5).
+// 128-byte aligned with gmm_dw_map_bytes(E, lists) bytes (gmm_dw: 2 lists, gmm_dw_ffn_maps: 5).  gmm_dw clears its counter itself.
 inline bool gmm_supported(int E, int d, int n, int dtype) {
   const int64_t lim = (int64_t)1 << 31;
   return dtype == CAPMOE_BF16 && d % 8 == 0 && n % 8 == 0 && (int64_t)E * n < lim && (int64_t)E * d < lim;
 }
+// `early`: the caller vouches that offsets and weights were final before the previous kernel on the stream started its work,
+// because that kernel is this library's own, of the same call, and lets its successor start only after its own wait for
+// what came before (wait_for_previous_kernel, then allow_next_kernel); the counter was cleared before that one.  The kernel then fetches its first weights while
+// the previous one, which makes the token rows, still runs: 4 us of a decode step's launch.
 int gmm_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
-            cudaStream_t st);
+            bool early, cudaStream_t st);
 int gmm_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
-           cudaStream_t st);
+           bool early, cudaStream_t st);
 int gmm_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu, const void* wd,
-               void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st);
+               void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st);
 int gmm_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
-            int32_t* dev_status, int32_t* sched, cudaStream_t st);
+            int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st);
 size_t gmm_dw_map_bytes(int E, int lists);
 int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws,
            int32_t* dev_status, int32_t* sched, cudaStream_t st);
@@ -73,18 +77,24 @@ int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd
 // 8-bit (gmm_rows.cu, gmm_swiglu8.cu): d and n (F) multiples of 16; xs_ld, hs_ld: bytes from one row's scales to the next's
 inline bool gmm8_supported(int d, int n) { return d % 16 == 0 && n % 16 == 0; }
 int gmm8(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,
-         int32_t* dev_status, int32_t* sched, cudaStream_t st);
+         int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st);
 int gmm8_swiglu(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                 const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
-                int32_t* sched, cudaStream_t st);
+                int32_t* sched, bool early, cudaStream_t st);
 int gmm8_swiglu_short(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                       const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
-                      int32_t* sched, cudaStream_t st);
+                      int32_t* sched, bool early, cudaStream_t st);
 
 // Tile counters in the caller's status block, one per launch of a call: cleared by begin_counters, slot i by counter_at.
+// Row products of up to 64 allocated rows per expert do without: every tile streams the same weight bytes, so fixed lists
+// are as even, and the launch that clears the counter costs 3 us (8-bit product of a decode step, 310 rows of 60 experts:
+// 33.7 us without, 36.8 with).
 inline int32_t* counter_at(int32_t* dev_status, int i) { return dev_status ? dev_status + 1 + i : nullptr; }
 inline int begin_counters(int32_t* dev_status, int n, cudaStream_t st) {
   return dev_status ? clear_words(dev_status + 1, n, nullptr, 0, st) : CAPMOE_OK;
+}
+inline int32_t* counters_of(const Segments& sg, int32_t* dev_status) {
+  return (int64_t)sg.rows > (int64_t)64 * sg.E ? dev_status : nullptr;
 }
 
 }  // namespace capmoe

@@ -30,10 +30,11 @@ struct DwArgs {
 // Tensor maps: list l, expert e = the base map of matrix l with its row count set to the end of e's rows.
 constexpr int MAP_LISTS = 5;
 struct BaseMaps { CUtensorMap m[MAP_LISTS]; };
-__global__ void __launch_bounds__(GMM_MAX_E) k_segment_maps(const __grid_constant__ BaseMaps base, Segments sg, CUtensorMap* maps) {
-  allow_next_kernel();
+__global__ void __launch_bounds__(GMM_MAX_E) k_segment_maps(const __grid_constant__ BaseMaps base, Segments sg, CUtensorMap* maps, int32_t* counter) {
   wait_for_previous_kernel();
+  allow_next_kernel();                       // in this order: an early successor reads what came before (gmm.cuh)
   const int e = threadIdx.x, l = blockIdx.x;
+  if (counter && e == 0 && l == 0) *counter = 0;
   if (e >= sg.E) return;
   CUtensorMap* to = maps + (size_t)l * sg.E + e;
   const uint4* src = reinterpret_cast<const uint4*>(&base.m[l]);
@@ -276,8 +277,9 @@ int launch(const DwMaps& mp, const DwArgs& ar, cudaStream_t st) {
   return note_cuda(err);
 }
 
-int segment_maps(const BaseMaps& base, int lists, const Segments& sg, void* ws, cudaStream_t st) {
-  const int rc = note_cuda(launch_chained(k_segment_maps, (unsigned)lists, GMM_MAX_E, 0, st, base, sg, (CUtensorMap*)ws));
+// `counter`: a word to clear on the way, or NULL
+int segment_maps(const BaseMaps& base, int lists, const Segments& sg, void* ws, int32_t* counter, cudaStream_t st) {
+  const int rc = note_cuda(launch_chained(k_segment_maps, (unsigned)lists, GMM_MAX_E, 0, st, base, sg, (CUtensorMap*)ws, counter));
   count_launch(1);
   return rc;
 }
@@ -294,7 +296,7 @@ int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool
   if (!make_mn_map(&base.m[0], dy, n, sg.rows, 0) || !make_mn_map(&base.m[1], x, d, sg.rows, 0) ||
       !make_wide_map(&mp.o0, dw, d, (uint64_t)sg.E * n, out_f32 ? 4 : 2))
     return note_cuda(cudaErrorInvalidValue);
-  const int rc = segment_maps(base, 2, sg, map_ws, st);
+  const int rc = segment_maps(base, 2, sg, map_ws, sched, st);
   if (rc != CAPMOE_OK) return rc;
   ar.sg = sg; ar.out[0] = dw; ar.count = 1; ar.M[0] = n; ar.N[0] = d; ar.ia[0] = 0; ar.ib[0] = 1;
   ar.wide_a = mn_wide(n); ar.wide_b = mn_wide(d);
@@ -309,7 +311,7 @@ int gmm_dw_ffn_maps(const void* dg, const void* du, const void* dy, const void* 
   if (!make_mn_map(&base.m[0], dg, F, R, 0) || !make_mn_map(&base.m[1], du, F, R, 0) || !make_mn_map(&base.m[2], dy, d, R, 0) ||
       !make_mn_map(&base.m[3], x, d, R, 0) || !make_mn_map(&base.m[4], h, F, R, 0))
     return note_cuda(cudaErrorInvalidValue);
-  return segment_maps(base, MAP_LISTS, sg, map_ws, st);
+  return segment_maps(base, MAP_LISTS, sg, map_ws, nullptr, st);
 }
 
 int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd, const void* map_ws, int32_t* dev_status,

@@ -54,6 +54,7 @@ struct TMaps { CUtensorMap x0, x1, w0, w1, w2; };
 struct TArgs {
   Segments sg;
   int K, Nout;
+  int early;                        // offsets and weights are final before the previous kernel ends (gmm.cuh)
   int wide;                         // MN-major weights: one box per k-block
   int tb, tt, bufs, nst;            // token rows per CTA and stage, tokens per tile, accumulator sets, stages
   void* out[3];
@@ -72,7 +73,6 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
   using S = ShapeT<KIND>;
   constexpr bool FP8 = S::FP8, W_MN = KIND == T_DX || KIND == T_DX2;
   constexpr int EW = S::EW, NACC = S::NACC;
-  allow_next_kernel();
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t tiles = (raw + 1023u) & ~1023u;
@@ -114,7 +114,8 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  wait_for_previous_kernel();
+  if (!ar.early) wait_for_previous_kernel();
+  allow_next_kernel();
   const int E = ar.sg.E;
   for (int i = tid; i < E; i += S::THREADS) { offs[i] = seg_at(ar.sg, i); ends[i] = max(offs[i], seg_at(ar.sg, i + 1)); }
   __syncthreads();
@@ -157,34 +158,48 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
       uint32_t ph = 0;
       STile t;
       bool ok = true;
+      // In an early start the first ring's weights are fetched while the previous kernel, which makes the token rows, still
+      // runs; their token rows follow when it has ended.
+      int fetched = 0;
+      bool waited = !ar.early;
+      auto load_weights = [&](int kb, int w, int e, uint32_t w_dst, uint32_t bar) {
+        if (rank == 0) mbar_expect_tx(bar, 2u * stage);           // (the leader's own address)
+        if constexpr (KIND == T_FWD || KIND == T_F8) {
+          tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, e, bar);
+        } else if constexpr (KIND == T_F8SW || KIND == T_HID) {
+          tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, e, bar);
+          tma2_load_3d(w_dst + A_BYTES, &mp.w1, kb * S::KE, w, e, bar);
+          if (KIND == T_HID) load_mn(w_dst + 2 * A_BYTES, &mp.w2, ar.wide, w, kb * S::KE, e, bar);
+        } else {
+          const bool second = KIND == T_DX2 && kb >= kbs;
+          load_mn(w_dst, second ? &mp.w1 : &mp.w0, ar.wide, w, (second ? kb - kbs : kb) * S::KE, e, bar);
+        }
+      };
+      auto load_tokens = [&](int kb, int x, uint32_t x_dst, uint32_t bar) {
+        const bool second = KIND == T_DX2 && kb >= kbs;
+        tma2_load_2d(x_dst, second ? &mp.x1 : &mp.x0, (second ? kb - kbs : kb) * S::KE, x, bar);
+        if (KIND == T_HID) tma2_load_2d(x_dst + x_bytes, &mp.x1, kb * S::KE, x, bar);
+      };
       for (int j = 0; ok; ++j) {
         if (!get_tile(j, false, t)) break;
         const int w = t.w0 + (int)rank * BM;                     // this CTA's 128 weight rows
         const int x = t.row0 + (int)rank * (t.nt >> 1);          // and its half of the tokens
+        if (!waited) {                                           // first tile of an early start
+          fetched = min(nst, num_kb);
+          for (int kb = 0; kb < fetched; ++kb) load_weights(kb, w, t.e, tiles + (uint32_t)kb * stage, full_bar(kb) & PEER_MASK);
+          wait_for_previous_kernel();
+          waited = true;
+        }
         for (int kb = 0; kb < num_kb; ++kb) {
-          if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
           const uint32_t bar = full_bar(s) & PEER_MASK;
-          if (rank == 0) mbar_expect_tx(full_bar(s), 2u * stage);
-          const uint32_t w_dst = tiles + (uint32_t)s * stage, x_dst = w_dst + (uint32_t)(NACC * A_BYTES);
-          if constexpr (KIND == T_FWD || KIND == T_F8) {
-            tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
-            tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
-          } else if constexpr (KIND == T_F8SW) {
-            tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
-            tma2_load_3d(w_dst + A_BYTES, &mp.w1, kb * S::KE, w, t.e, bar);
-            tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
-          } else if constexpr (KIND == T_HID) {
-            tma2_load_3d(w_dst, &mp.w0, kb * S::KE, w, t.e, bar);
-            tma2_load_3d(w_dst + A_BYTES, &mp.w1, kb * S::KE, w, t.e, bar);
-            load_mn(w_dst + 2 * A_BYTES, &mp.w2, ar.wide, w, kb * S::KE, t.e, bar);
-            tma2_load_2d(x_dst, &mp.x0, kb * S::KE, x, bar);
-            tma2_load_2d(x_dst + x_bytes, &mp.x1, kb * S::KE, x, bar);
+          const uint32_t w_dst = tiles + (uint32_t)s * stage;
+          if (fetched > 0) {
+            --fetched;
           } else {
-            const bool second = KIND == T_DX2 && kb >= kbs;
-            const int k = (second ? kb - kbs : kb) * S::KE;
-            load_mn(w_dst, second ? &mp.w1 : &mp.w0, ar.wide, w, k, t.e, bar);
-            tma2_load_2d(x_dst, second ? &mp.x1 : &mp.x0, k, x, bar);
+            if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
+            load_weights(kb, w, t.e, w_dst, bar);
           }
+          load_tokens(kb, x, w_dst + (uint32_t)(NACC * A_BYTES), bar);
           if (++s == nst) { s = 0; ph ^= 1u; }
         }
       }
@@ -274,6 +289,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     }
   } else if (FP8 && warp == 3 + EW) {
     // ------------------------------------------------------------ scales (both CTAs)
+    if (ar.early) wait_for_previous_kernel();
     int r = 0;
     uint32_t rph = 0;
     STile t;
@@ -313,6 +329,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
     }
   } else {
     // ------------------------------------------------------------ epilogue (both CTAs, own 128 weight rows)
+    if (ar.early) wait_for_previous_kernel();
     const int quarter = warp & 3, sub = (warp - 2) >> 2;         // lane quarter; this warp's share of the token chunks
     int b = 0;
     uint32_t bph = 0, flip = 0;
@@ -478,7 +495,8 @@ void geometry(TArgs& ar, int tt_max) {
 }
 
 template <int KIND>
-int launch(const TMaps& mp, const TArgs& ar, cudaStream_t st) {
+int launch(const TMaps& mp, TArgs& ar, bool early, cudaStream_t st) {
+  ar.early = early;
   using S = ShapeT<KIND>;
   const int pairs = sm_count() / 2;
   if (pairs < 1) return CAPMOE_EUNSUPPORTED;
@@ -511,28 +529,28 @@ bool map3(CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t bat
 }  // namespace
 
 int gmm_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
-                  cudaStream_t st) {
+                  bool early, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
   ar.sg = sg; ar.K = d; ar.Nout = n; ar.out[0] = y; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_FWD>(ar, 256);
   if (!map2(&mp.x0, x, d, sg.rows, (uint32_t)ar.tb) || !map3(&mp.w0, w, d, n, sg.E, BM)) return note_cuda(cudaErrorInvalidValue);
-  return launch<T_FWD>(mp, ar, st);
+  return launch<T_FWD>(mp, ar, early, st);
 }
 
 int gmm_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,
-                 cudaStream_t st) {
+                 bool early, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
   ar.sg = sg; ar.K = n; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_DX>(ar, 256);
   if (!map2(&mp.x0, dy, n, sg.rows, (uint32_t)ar.tb) || !make_mn_map(&mp.w0, w, d, n, sg.E)) return note_cuda(cudaErrorInvalidValue);
   ar.wide = mn_wide(d);
-  return launch<T_DX>(mp, ar, st);
+  return launch<T_DX>(mp, ar, early, st);
 }
 
 int gmm_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, const void* wg, const void* wu,
-                     const void* wd, void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+                     const void* wd, void* dg, void* du, void* h, int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
   ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = dg; ar.out[1] = du; ar.out[2] = h; ar.dev_status = dev_status; ar.sched = sched;
@@ -541,11 +559,11 @@ int gmm_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, 
       !map3(&mp.w0, wg, d, F, sg.E, BM) || !map3(&mp.w1, wu, d, F, sg.E, BM) || !make_mn_map(&mp.w2, wd, F, d, sg.E))
     return note_cuda(cudaErrorInvalidValue);
   ar.wide = mn_wide(F);
-  return launch<T_HID>(mp, ar, st);
+  return launch<T_HID>(mp, ar, early, st);
 }
 
 int gmm_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
-                  int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+                  int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
   ar.sg = sg; ar.K = F; ar.Nout = d; ar.out[0] = dx; ar.dev_status = dev_status; ar.sched = sched;
@@ -554,23 +572,23 @@ int gmm_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, co
       !make_mn_map(&mp.w0, wg, d, F, sg.E) || !make_mn_map(&mp.w1, wu, d, F, sg.E))
     return note_cuda(cudaErrorInvalidValue);
   ar.wide = mn_wide(d);
-  return launch<T_DX2>(mp, ar, st);
+  return launch<T_DX2>(mp, ar, early, st);
 }
 
 int gmm8(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n,
-               void* y, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+               void* y, int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
   ar.sg = sg; ar.K = d; ar.Nout = n; ar.out[0] = y; ar.xs = xs; ar.xs_ld = xs_ld; ar.s0 = ws; ar.dev_status = dev_status; ar.sched = sched;
   geometry<T_F8>(ar, 224);
   if (!make_map_u8(&mp.x0, xq, d, sg.rows, 0, (uint32_t)ar.tb) || !make_map_u8(&mp.w0, wq, d, n, sg.E, BM))
     return note_cuda(cudaErrorInvalidValue);
-  return launch<T_F8>(mp, ar, st);
+  return launch<T_F8>(mp, ar, early, st);
 }
 
 int gmm8_swiglu_short(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                       const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
-                      int32_t* sched, cudaStream_t st) {
+                      int32_t* sched, bool early, cudaStream_t st) {
   TMaps mp = {};
   TArgs ar = {};
   ar.sg = sg; ar.K = d; ar.Nout = F; ar.out[0] = hq; ar.out_scale = hs; ar.os_ld = hs_ld; ar.xs = xs; ar.xs_ld = xs_ld; ar.s0 = wgs; ar.s1 = wus;
@@ -579,7 +597,7 @@ int gmm8_swiglu_short(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const
   if (!make_map_u8(&mp.x0, xq, d, sg.rows, 0, (uint32_t)ar.tb) || !make_map_u8(&mp.w0, wg, d, F, sg.E, BM) ||
       !make_map_u8(&mp.w1, wu, d, F, sg.E, BM))
     return note_cuda(cudaErrorInvalidValue);
-  return launch<T_F8SW>(mp, ar, st);
+  return launch<T_F8SW>(mp, ar, early, st);
 }
 
 }  // namespace capmoe

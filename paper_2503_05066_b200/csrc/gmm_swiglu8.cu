@@ -351,9 +351,9 @@ int launch(const F8Maps& mp, const F8Args& ar, cudaStream_t st) {
 
 int gmm8_swiglu(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                    const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
-                   int32_t* sched, cudaStream_t st) {
+                   int32_t* sched, bool early, cudaStream_t st) {
   if (use_short(sg, SHORT_LIMIT))
-    return gmm8_swiglu_short(xq, xs, xs_ld, sg, wg, wgs, wu, wus, d, F, hq, hs, hs_ld, dev_status, sched, st);
+    return gmm8_swiglu_short(xq, xs, xs_ld, sg, wg, wgs, wu, wus, d, F, hq, hs, hs_ld, dev_status, sched, early, st);
   F8Maps mp = {};
   F8Args ar = {};
   if (!make_map_u8(&mp.a, xq, d, sg.rows, 0, BM) || !make_map_u8(&mp.b0, wg, d, F, sg.E, 128) ||

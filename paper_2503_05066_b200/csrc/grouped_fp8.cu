@@ -92,8 +92,8 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(QN)
 k_quantize_rows(const T* __restrict__ x, const int32_t* __restrict__ n_rows, int rows, int d, uint32_t per_row, uint8_t* __restrict__ q,
                 uint8_t* __restrict__ scale, int64_t scale_ld) {
-  allow_next_kernel();
   wait_for_previous_kernel();
+  allow_next_kernel();                       // in this order: an early successor reads what came before (gmm.cuh)
   const int lane = threadIdx.x & 31, sub = lane & 15;
   const int nb = (d + QBLOCK - 1) / QBLOCK;
   const uint32_t unit = blockIdx.x * (QN / 32) + (threadIdx.x >> 5);
@@ -299,9 +299,10 @@ extern "C" int capmoe_grouped_mm_fp8(const void* x_q, const void* x_scale, const
   if (!usable(x_q, w_q, y) || !x_scale || !w_scale) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
   if (gmm8_supported(d, n)) {
-    if ((rc = begin_counters(dev_status, 1, as_stream(stream))) != CAPMOE_OK) return rc;
+    int32_t* counters = counters_of(sg, dev_status);
+    if ((rc = begin_counters(counters, 1, as_stream(stream))) != CAPMOE_OK) return rc;
     return gmm8((const uint8_t*)x_q, (const uint8_t*)x_scale, ceil_div(d, QBLOCK), sg, (const uint8_t*)w_q, (const uint8_t*)w_scale, d, n, y,
-                dev_status, counter_at(dev_status, 0), as_stream(stream));
+                dev_status, counter_at(counters, 0), false, as_stream(stream));
   }
   const uint8_t* none = nullptr;
   return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, n, as_stream(stream), (const uint8_t*)x_q, (const uint8_t*)x_scale,
@@ -327,15 +328,16 @@ extern "C" int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_
   cudaStream_t st = as_stream(stream);
   uint8_t* b = (uint8_t*)ws;
   const bool tc = gmm8_supported(d, F);
-  if (tc && (rc = begin_counters(dev_status, 2, st)) != CAPMOE_OK) return rc;
+  int32_t* counters = counters_of(sg, dev_status);
+  if (tc && (rc = begin_counters(counters, 2, st)) != CAPMOE_OK) return rc;
   rc = quantize_rows_run<__nv_bfloat16>(x_perm, expert_offsets + E, A_max, d, b + w.xq, b + w.xs, w.xs_ld, st);
   if (rc != CAPMOE_OK) return rc;
   if (tc) {
     rc = gmm8_swiglu(b + w.xq, b + w.xs, w.xs_ld, sg, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
-                        (const uint8_t*)wu_scale, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(dev_status, 0), st);
+                        (const uint8_t*)wu_scale, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(counters, 0), true, st);
     if (rc != CAPMOE_OK) return rc;
     return gmm8(b + w.hq, b + w.hs, w.hs_ld, sg, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, F, d, y_perm, dev_status,
-                counter_at(dev_status, 1), st);
+                counter_at(counters, 1), true, st);
   }
   float* h = (float*)(b + w.h);
   rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, b + w.xq, b + w.xs, (const uint8_t*)wg_q, (const uint8_t*)wg_scale,

@@ -244,8 +244,9 @@ extern "C" int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offse
   if (!usable(x_rows, w, y)) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
   if (gmm_supported(E, d, n, dtype)) {
-    if ((rc = begin_counters(dev_status, 1, as_stream(stream))) != CAPMOE_OK) return rc;
-    return gmm_fwd(x_rows, sg, w, d, n, y, dev_status, counter_at(dev_status, 0), as_stream(stream));
+    int32_t* counters = counters_of(sg, dev_status);
+    if ((rc = begin_counters(counters, 1, as_stream(stream))) != CAPMOE_OK) return rc;
+    return gmm_fwd(x_rows, sg, w, d, n, y, dev_status, counter_at(counters, 0), false, as_stream(stream));
   }
   if (dtype == CAPMOE_F32) return rows_simt<float, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
   return rows_simt<__nv_bfloat16, DIR_FWD>(x_rows, w, y, sg, d, n, as_stream(stream));
@@ -258,8 +259,9 @@ extern "C" int capmoe_grouped_mm_dx(const void* dy_rows, const int32_t* expert_o
   if (!usable(dy_rows, w, dx)) return CAPMOE_EINVAL;
   const Segments sg{expert_offsets, E, (int)rows};
   if (gmm_supported(E, d, n, dtype)) {
-    if ((rc = begin_counters(dev_status, 1, as_stream(stream))) != CAPMOE_OK) return rc;
-    return gmm_dx(dy_rows, sg, w, d, n, dx, dev_status, counter_at(dev_status, 0), as_stream(stream));
+    int32_t* counters = counters_of(sg, dev_status);
+    if ((rc = begin_counters(counters, 1, as_stream(stream))) != CAPMOE_OK) return rc;
+    return gmm_dx(dy_rows, sg, w, d, n, dx, dev_status, counter_at(counters, 0), false, as_stream(stream));
   }
   if (dtype == CAPMOE_F32) return rows_simt<float, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
   return rows_simt<__nv_bfloat16, DIR_DX>(dy_rows, w, dx, sg, n, d, as_stream(stream));
@@ -286,10 +288,8 @@ extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, con
   if (ws_bytes < need) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)rows};
   cudaStream_t st = as_stream(stream);
-  if (gmm_supported(E, d, n, dtype)) {
-    if ((rc = begin_counters(dev_status, 1, st)) != CAPMOE_OK) return rc;
+  if (gmm_supported(E, d, n, dtype))
     return gmm_dw(dy_rows, x_rows, sg, d, n, out_dtype == CAPMOE_F32, dw, align256(ws), dev_status, counter_at(dev_status, 0), st);
-  }
   if (dtype == CAPMOE_F32)
     return dw_simt(DwSet<float, float>{{(const float*)dy_rows}, {(const float*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
   using B = __nv_bfloat16;
@@ -330,8 +330,8 @@ extern "C" int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_pe
     rc = begin_counters(dev_status, 3, st);
     if (rc == CAPMOE_OK) rc = gmm_dw_ffn_maps(dg, du, dy_perm, x_perm, h, sg, d, F, maps, st);
     if (rc == CAPMOE_OK)
-      rc = gmm_hidden(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dg, du, h, dev_status, counter_at(dev_status, 0), st);
-    if (rc == CAPMOE_OK) rc = gmm_dx2(dg, du, sg, d, F, w_gate, w_up, dx_perm, dev_status, counter_at(dev_status, 1), st);
+      rc = gmm_hidden(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dg, du, h, dev_status, counter_at(dev_status, 0), true, st);
+    if (rc == CAPMOE_OK) rc = gmm_dx2(dg, du, sg, d, F, w_gate, w_up, dx_perm, dev_status, counter_at(dev_status, 1), true, st);
     if (rc != CAPMOE_OK) return rc;
     return gmm_dw_ffn(sg, d, F, dw_gate, dw_up, dw_down, maps, dev_status, counter_at(dev_status, 2), st);
   }
