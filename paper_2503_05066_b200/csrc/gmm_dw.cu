@@ -218,6 +218,12 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
       TO* orow = reinterpret_cast<TO*>(ar.out[t.p]) + (row + lane) * Nout + t.n0;
       {
         constexpr int PC = 128 / (int)sizeof(TO);               // columns of a piece
+        bool held = true;
+        auto release = [&]() {                                  // this warp has read its last columns
+          tc_fence_before();
+          mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);       // the leader waits for both CTAs' epilogues
+          held = false;
+        };
 #pragma unroll 1
         for (int c = half * 128; c < half * 128 + 128; c += PC) {
           if (t.n0 + c >= Nout) break;
@@ -230,14 +236,14 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
             for (int i = 0; i < PC; i += 32) tmem_ld32(taddr + (uint32_t)(c + i), g + i);
             tmem_ld_wait();
           }
+          if (held && (c + PC >= half * 128 + 128 || t.n0 + c + PC >= Nout)) release();
 #pragma unroll
           for (int i = 0; i < 32; ++i)
             w[i] = sizeof(TO) == 2 ? pack_bf16(__uint_as_float(g[2 * i % PC]), __uint_as_float(g[(2 * i + 1) % PC])) : g[i];
           put_wide(w, full_rows, row_ok, stg, mo, t.n0 + c, (int)row, orow + c, (Nout - (t.n0 + c)) * (int)sizeof(TO));
         }
+        if (held) release();
       }
-      tc_fence_before();
-      mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);           // the leader waits for both CTAs' epilogues
     }
     if (lane == 0) bulk_wait_all();                              // this lane's stores have landed before the CTA ends
   }

@@ -344,6 +344,13 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * NACC * tt);
       const int col0 = t.w0 + (int)rank * BM;                    // first output column of this CTA
+      // the accumulators go back to the MMA thread as soon as this warp has read its last columns
+      bool held = true;
+      auto release = [&]() {
+        tc_fence_before();
+        mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);          // the leader waits for both CTAs' epilogues
+        held = false;
+      };
       const int wcol = col0 + quarter * 32, cols = ar.Nout - wcol;   // this warp's 32, and how many exist from there on
       if (col0 < ar.Nout) {                                      // (all of a CTA's warps agree)
 #pragma unroll 1
@@ -351,6 +358,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
           const int n = t.rows - c;                              // tokens that exist from here on (may be negative)
           const int64_t o = (int64_t)(t.row0 + c) * ar.Nout + wcol;
           const uint32_t ta = taddr + (uint32_t)c;
+          const bool last = c + EW * 8 >= t.nt;
           if constexpr (KIND == T_HID) {
             uint32_t pg[2][8], pu[2][8], ph[2][8];
 #pragma unroll
@@ -360,6 +368,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
               tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16) + (uint32_t)tt, u);
               tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16) + (uint32_t)(2 * tt), h);
               tmem_ld_wait();
+              if (last && hf == 1) release();
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 float dg[2], du[2], hh[2];
@@ -394,6 +403,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
               tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16), h[hf]);
               tmem_ld_frag(ta + ((uint32_t)(16 * hf) << 16) + (uint32_t)tt, u);
               tmem_ld_wait();
+              if (last && hf == 1) release();
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 const float gv = __uint_as_float(h[hf][i]);
@@ -442,6 +452,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
             tmem_ld_frag(ta, g[0]);
             tmem_ld_frag(ta + (16u << 16), g[1]);
             tmem_ld_wait();
+            if (last) release();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t p[4];
@@ -456,8 +467,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
           }
         }
       }
-      tc_fence_before();
-      mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
+      if (held) release();
       if (++b == bufs) { b = 0; bph ^= 1u; }
     }
   }
