@@ -132,7 +132,7 @@ int launched(cudaError_t err) {
 
 // These kernels do not let their successor start early (no allow_next_kernel): its blocks would be handed to the SMs
 // that happen to have room, several to each, and stay there (a 1024-row fp32 product of 120 blocks, launched back to
-// back: 63 us that way, 25 without).
+// back: 63 us that way, 25 without); letting it start when the sums are done changes nothing.
 template <class GE, class... KArgs, class... Args>
 int launch_tiles(void (*kernel)(KArgs...), dim3 grid, cudaStream_t st, Args... args) {
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SimtTile<GE>));
@@ -157,7 +157,9 @@ dim3 row_grid(const Segments& sg, int cols, int tm) {       // every segment rou
 // itself when they do not outnumber the SMs (see gmm_simt.cuh; the bound on the tiles counts the segments' ragged ends
 // once each, so a few more may run).
 enum Size { LARGE, MEDIUM, SMALL };
-Size size_of(int64_t tiles64) { return tiles64 >= 2 * sm_count() ? LARGE : 2 * tiles64 > sm_count() ? MEDIUM : SMALL; }
+Size size_of(int64_t tiles64, int large = 2) {
+  return tiles64 >= large * sm_count() ? LARGE : 2 * tiles64 > sm_count() ? MEDIUM : SMALL;
+}
 using Large = Geo<64, 4>;
 using Medium = Geo<32, 4>;
 using Small = Geo<32, 8>;
@@ -186,7 +188,7 @@ int dw_simt(const DwSet<T, TO>& s, int count, const Segments& sg, cudaStream_t s
     N = s.N[p] > N ? s.N[p] : N;
     tiles += ceil_div(s.M[p], ST) * ceil_div(s.N[p], ST) * sg.E;
   }
-  const Size z = size_of(tiles);
+  const Size z = size_of(tiles, 1);         // short sums: one wave of 64-row tiles, two to an SM, is the fastest
   auto run = z == LARGE ? dw_run<T, TO, Large> : z == MEDIUM ? dw_run<T, TO, Medium> : dw_run<T, TO, Small>;
   return run(s, M, N, (unsigned)(count * sg.E), sg, st);
 }
