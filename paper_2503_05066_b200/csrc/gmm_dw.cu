@@ -167,10 +167,8 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
           if (!mbar_wait(full_bar(s), ph, abort_flag)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
-          for (int k = 0; k < BK / UMMA_K; ++k) {
-            // 16 reduction steps: 16 rows of 128 bytes
+          for (int k = 0; k < BK / UMMA_K; ++k)                 // 16 reduction steps: 16 rows of 128 bytes
             umma2(d, a0 + off + 128 * k, b0 + off + 128 * k, idesc, (kb | k) != 0 ? 1u : 0u);
-          }
           umma2_commit_both(empty_bar(s));                      // both CTAs may refill this stage
           off += (uint64_t)(DW_STAGE >> 4);
           if (++s == DW_NST) { s = 0; ph ^= 1u; off = 0; }
@@ -216,34 +214,32 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
       const int64_t row = (int64_t)t.e * ar.M[t.p] + t.row0 + warp_row0;
       const CUtensorMap* mo = t.p == 0 ? &mp.o0 : t.p == 1 ? &mp.o1 : &mp.o2;
       TO* orow = reinterpret_cast<TO*>(ar.out[t.p]) + (row + lane) * Nout + t.n0;
-      {
-        constexpr int PC = 128 / (int)sizeof(TO);               // columns of a piece
-        bool held = true;
-        auto release = [&]() {                                  // this warp has read its last columns
-          tc_fence_before();
-          mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);       // the leader waits for both CTAs' epilogues
-          held = false;
-        };
+      constexpr int PC = 128 / (int)sizeof(TO);               // columns of a piece
+      bool held = true;
+      auto release = [&]() {                                  // this warp has read its last columns
+        tc_fence_before();
+        mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);       // the leader waits for both CTAs' epilogues
+        held = false;
+      };
 #pragma unroll 1
-        for (int c = half * 128; c < half * 128 + 128; c += PC) {
-          if (t.n0 + c >= Nout) break;
-          uint32_t g[PC], w[32];
-          if (empty_sum) {
+      for (int c = half * 128; c < half * 128 + 128; c += PC) {
+        if (t.n0 + c >= Nout) break;
+        uint32_t g[PC], w[32];
+        if (empty_sum) {
 #pragma unroll
-            for (int i = 0; i < PC; ++i) g[i] = 0u;
-          } else {
+          for (int i = 0; i < PC; ++i) g[i] = 0u;
+        } else {
 #pragma unroll
-            for (int i = 0; i < PC; i += 32) tmem_ld32(taddr + (uint32_t)(c + i), g + i);
-            tmem_ld_wait();
-          }
-          if (held && (c + PC >= half * 128 + 128 || t.n0 + c + PC >= Nout)) release();
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            w[i] = sizeof(TO) == 2 ? pack_bf16(__uint_as_float(g[2 * i % PC]), __uint_as_float(g[(2 * i + 1) % PC])) : g[i];
-          put_wide(w, full_rows, row_ok, stg, mo, t.n0 + c, (int)row, orow + c, (Nout - (t.n0 + c)) * (int)sizeof(TO));
+          for (int i = 0; i < PC; i += 32) tmem_ld32(taddr + (uint32_t)(c + i), g + i);
+          tmem_ld_wait();
         }
-        if (held) release();
+        if (held && (c + PC >= half * 128 + 128 || t.n0 + c + PC >= Nout)) release();
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          w[i] = sizeof(TO) == 2 ? pack_bf16(__uint_as_float(g[2 * i % PC]), __uint_as_float(g[(2 * i + 1) % PC])) : g[i];
+        put_wide(w, full_rows, row_ok, stg, mo, t.n0 + c, (int)row, orow + c, (Nout - (t.n0 + c)) * (int)sizeof(TO));
       }
+      if (held) release();
     }
     if (lane == 0) bulk_wait_all();                              // this lane's stores have landed before the CTA ends
   }

@@ -1,7 +1,7 @@
 // Gate and up products of the 8-bit FFN on tcgen05's block-scaled MMA (kind::mxf8f6f4): e4m3 codes, power-of-two scales
 // per 128 columns of a row and per 128 x 128 block of a weight, applied by the tensor cores, fp32 accumulation.
 //   h[r] = silu(W_g[e] x[r]) * (W_u[e] x[r]), quantised: codes and scales
-// Persistent kernel over CTA pairs, tiles of 256 tokens by 128 hidden columns, the structure of k_gmm_dw (gmm_tc.cu) with
+// Persistent kernel over CTA pairs, tiles of 256 tokens by 128 hidden columns, the structure of k_gmm_dw (gmm_dw.cu) with
 // one more warp that stages scale words (see gmm_tc.cuh).  A tile puts 128 gate and 128 up columns of the same hidden
 // columns side by side, which is one block of 128 hidden columns per row: its largest magnitude meets between the two
 // threads that share a row, and the hidden row leaves the kernel as codes, never as fp32.
@@ -266,49 +266,47 @@ __global__ void __launch_bounds__(F8_THREADS, 1) k_gmm_swiglu8(const __grid_cons
       const int row = t.row0 + warp_row0;
       // the overlap is the last 64 columns of accumulator 0 and the first 64 of accumulator 1
       const bool mine_shared = half == (b == 0 ? 1 : 0);
-      {
-        // hidden columns half * 64 .. + 63 of the tile: gate there, up 128 columns further on
-        float h[64];
-        uint32_t top = 0;
+      // hidden columns half * 64 .. + 63 of the tile: gate there, up 128 columns further on
+      float h[64];
+      uint32_t top = 0;
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          uint32_t g[32], u[32];
-          tmem_ld32(taddr + (uint32_t)(half * 64 + 32 * v), g);
-          tmem_ld32(taddr + (uint32_t)(128 + half * 64 + 32 * v), u);
-          tmem_ld_wait();
+      for (int v = 0; v < 2; ++v) {
+        uint32_t g[32], u[32];
+        tmem_ld32(taddr + (uint32_t)(half * 64 + 32 * v), g);
+        tmem_ld32(taddr + (uint32_t)(128 + half * 64 + 32 * v), u);
+        tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float gv = __uint_as_float(g[i]);
-            h[32 * v + i] = __fdividef(gv, 1.0f + __expf(-gv)) * __uint_as_float(u[i]);
-            top = max(top, __float_as_uint(h[32 * v + i]) & 0x7fffffffu);
-          }
+        for (int i = 0; i < 32; ++i) {
+          const float gv = __uint_as_float(g[i]);
+          h[32 * v + i] = __fdividef(gv, 1.0f + __expf(-gv)) * __uint_as_float(u[i]);
+          top = max(top, __float_as_uint(h[32 * v + i]) & 0x7fffffffu);
         }
-        tc_fence_before();
-        if (mine_shared) mbar_arrive_cluster(shared_bar(b) & PEER_MASK);
-        mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
-        uint32_t* rm = row_max + b * 256 + quarter * 32 + lane;
-        rm[half * 128] = top;
-        group_sync(1 + quarter, 64);
-        top = max(top, rm[(half ^ 1) * 128]);
-        const uint32_t code = scale_code(top);
-        uint32_t packed[16];
-        if (code == (uint32_t)Q_NAN_SCALE) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) packed[i] = 0x7f7f7f7fu;
-        } else {
-          const float f = inv_scale(code);
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            packed[i] = to_e4m3x2(h[4 * i] * f, h[4 * i + 1] * f) | (to_e4m3x2(h[4 * i + 2] * f, h[4 * i + 3] * f) << 16);
-        }
-        const int c = t.n0 + half * 64;
-        if (half == 0 && row_ok)
-          ar.out_scale[(int64_t)(row + lane) * ar.os_ld + t.n0 / QBLOCK] = (uint8_t)code;
-        if (c < ar.Nout)                                        // 64 codes are the 64 bytes of a piece's row
-          store_piece(packed, full_rows, row_ok, stg, &mp.o, c, row,
-                      reinterpret_cast<__nv_bfloat16*>(ar.out + (int64_t)(row + lane) * ar.Nout + c),
-                      (ar.Nout - c) / 2);
       }
+      tc_fence_before();
+      if (mine_shared) mbar_arrive_cluster(shared_bar(b) & PEER_MASK);
+      mbar_arrive_cluster(tempty_bar(b) & PEER_MASK);
+      uint32_t* rm = row_max + b * 256 + quarter * 32 + lane;
+      rm[half * 128] = top;
+      group_sync(1 + quarter, 64);
+      top = max(top, rm[(half ^ 1) * 128]);
+      const uint32_t code = scale_code(top);
+      uint32_t packed[16];
+      if (code == (uint32_t)Q_NAN_SCALE) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) packed[i] = 0x7f7f7f7fu;
+      } else {
+        const float f = inv_scale(code);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          packed[i] = to_e4m3x2(h[4 * i] * f, h[4 * i + 1] * f) | (to_e4m3x2(h[4 * i + 2] * f, h[4 * i + 3] * f) << 16);
+      }
+      const int c = t.n0 + half * 64;
+      if (half == 0 && row_ok)
+        ar.out_scale[(int64_t)(row + lane) * ar.os_ld + t.n0 / QBLOCK] = (uint8_t)code;
+      if (c < ar.Nout)                                        // 64 codes are the 64 bytes of a piece's row
+        store_piece(packed, full_rows, row_ok, stg, &mp.o, c, row,
+                    reinterpret_cast<__nv_bfloat16*>(ar.out + (int64_t)(row + lane) * ar.Nout + c),
+                    (ar.Nout - c) / 2);
     }
     if (lane == 0) bulk_wait_all();
   }

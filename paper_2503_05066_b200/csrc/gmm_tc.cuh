@@ -1,4 +1,5 @@
-// Additions to tc_common.cuh for the grouped products: MN-major operand descriptors, fp32 store boxes.
+// Additions to tc_common.cuh for the grouped products: MN-major operands, the wide and the transposing epilogue, the tile
+// ring with its scheduler, and what the block-scaled 8-bit MMAs need.
 #pragma once
 #include "tc_common.cuh"
 
@@ -23,9 +24,6 @@ __device__ __forceinline__ uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
          ((uint32_t)((2 * BM) >> 4) << 24);
 }
 
-// all but the newest N groups of this thread have finished reading their shared-memory source
-template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-
 // A wide piece of an output: 32 rows of 128 bytes (64 bf16 or 32 fp32 columns), lane r holding row r as 32 words.  With all
 // 32 rows inside the segment it goes out as one TMA box (128-byte swizzle) from a 4 KB buffer of the warp, else row by
 // row.  `bytes_left`: of the output row from this piece on, a multiple of 16.  Against 64-byte pieces this halves the
@@ -35,7 +33,7 @@ __device__ __forceinline__ void put_wide(const uint32_t* w, bool full_rows, bool
                                          int col, int row0_of_warp, void* orow_c, int bytes_left) {
   const int lane = threadIdx.x & 31;
   if (full_rows) {
-    if (lane == 0) bulk_wait_read<0>();                        // the previous piece has left the buffer
+    if (lane == 0) bulk_wait_read_all();                       // the previous piece has left the buffer
     __syncwarp();
     const uint32_t base = smem_u32(stg) + (uint32_t)lane * 128u;
 #pragma unroll
@@ -54,37 +52,6 @@ __device__ __forceinline__ void put_wide(const uint32_t* w, bool full_rows, bool
     for (int v = 0; v < 8; ++v)
       if (v * 16 + 16 <= bytes_left)
         reinterpret_cast<uint4*>(orow_c)[v] = make_uint4(w[4 * v], w[4 * v + 1], w[4 * v + 2], w[4 * v + 3]);
-  }
-}
-
-// The same for one of several 64-byte pieces with a 2 KB buffer each; `wait` for the first of a chunk.
-__device__ __forceinline__ void put_piece(const uint32_t* packed, bool wait, bool full_rows, bool row_ok, uint8_t* stg,
-                                          const CUtensorMap* map_out, int col, int row0_of_warp, __nv_bfloat16* orow_c,
-                                          int cols_left) {
-  const int lane = threadIdx.x & 31;
-  if (full_rows && wait) {
-    if (lane == 0) bulk_wait_read<0>();
-    __syncwarp();
-  }
-  if (full_rows) {
-    const uint32_t base = smem_u32(stg) + (uint32_t)lane * 64u;
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)((v ^ ((lane >> 1) & 3)) * 16)),
-                   "r"(packed[4 * v]), "r"(packed[4 * v + 1]), "r"(packed[4 * v + 2]), "r"(packed[4 * v + 3])
-                   : "memory");
-    fence_proxy_async();
-    __syncwarp();
-    if (lane == 0) {
-      tma_store_2d(map_out, col, row0_of_warp, smem_u32(stg));
-      bulk_commit();
-    }
-  } else if (row_ok) {
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-      if (v * 8 + 8 <= cols_left)
-        *reinterpret_cast<uint4*>(orow_c + v * 8) =
-            make_uint4(packed[4 * v], packed[4 * v + 1], packed[4 * v + 2], packed[4 * v + 3]);
   }
 }
 
