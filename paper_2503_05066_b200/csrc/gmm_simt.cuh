@@ -1,7 +1,7 @@
 // Plain-FMA tile product shared by the grouped products' fp32, odd-size and 8-bit fallback kernels:
 // C[TM, 64] += A[TM, K] B[64, K]^T with fp32 accumulation, operands read through small loader types that
 // hide storage type, major order and block scales.
-// A block is G groups of 64 threads; a k-step is 4 G long and each group multiplies its four of it over the whole tile, a
+// A block is G groups of 64 threads; a k-step is KG G long and each group multiplies its KG of it over the whole tile, a
 // thread with a TM/8 x 8 micro-tile (rows and columns 8 apart); the partial tiles are added in shared memory at the
 // end, in a fixed order.  Shared memory, not the FMA pipe, is what a plain-FMA tile product runs into (a 16-byte load
 // takes four cycles of it whatever its lanes share), so the micro-tile is as large as registers allow.
@@ -23,9 +23,10 @@ constexpr int ST = 64;        // tile columns
 template <int TM_, int G_>
 struct Geo {
   static constexpr int TM = TM_, G = G_;
-  static constexpr int SK = 4 * G;                  // k-step
+  static constexpr int KG = TM == 64 ? 4 : 8;       // a group's part of a k-step (eight spill the large micro-tile)
+  static constexpr int SK = KG * G;                 // k-step
   static constexpr int SN = 64 * G;                 // threads
-  static constexpr int DEPTH = G == 8 ? 3 : 4;      // k-steps in the ring
+  static constexpr int DEPTH = TM == 64 ? 4 : 3;    // k-steps in the ring
   static constexpr int R = TM * ST / SN / 4;        // result elements of a thread: R x 4
   // floats of one k-step of an operand of W rows (columns): [W][SK + 4] or [SK][W + 4]; both row pitches are odd multiples
   // of 16 bytes
@@ -73,8 +74,10 @@ template <class GE, int W, class L>
 struct Stager {
   static constexpr int SK = GE::SK, SN = GE::SN;
   static constexpr int N4 = W * SK / SN;           // 4-byte copies per thread and step
+  static constexpr int N16 = (N4 + 3) / 4;         // 16-byte copies (of the first threads only if N4 < 4)
+  static constexpr int V = SK / 4;                 // 16-byte pieces of a k-step of one row, k contiguous
   const float* src[N4];
-  uint32_t dst0, size;                             // size: 4-byte form: bit e = copy e is inside; 16-byte form: bytes inside
+  uint32_t dst0, size;                             // size: per copy, 4-byte form a bit, 16-byte form the bytes inside (8 bits)
   int64_t step_len;
   int k, K;                                        // this thread's first k of the step in hand; end of the reduction
   bool vec, idle;
@@ -83,20 +86,20 @@ struct Stager {
     vec = l.ld % 4 == 0 && ((uintptr_t)l.p & 15u) == 0;
     step_len = L::k_fast ? SK : SK * l.ld;
     size = 0;
-    if (vec) {                                     // one 16-byte piece, by the first W * 4 threads
-      const int i = L::k_fast ? tid / (SK / 4) : tid % (W / 4) * 4;
-      k = L::k_fast ? tid % (SK / 4) * 4 : tid / (W / 4);
-      idle = tid >= W * SK / 4;
-      dst0 = (uint32_t)__cvta_generic_to_shared(ring) + 4u * (uint32_t)(L::k_fast ? i * (SK + 4) + k : k * (W + 4) + i);
-      const int in = L::k_fast ? (i < n ? 4 : 0) : n - i;
-      size = in <= 0 ? 0u : in >= 4 ? 16u : 4u * (uint32_t)in;
-      src[0] = size && !idle ? l.ptr(i, k) : l.p;
-      if (!size) step_len = 0;
+    idle = vec && tid >= W * SK / 4;
+    const int i0 = vec ? (L::k_fast ? tid / V : tid % (W / 4) * 4) : (L::k_fast ? tid / SK : tid % W);
+    k = vec ? (L::k_fast ? tid % V * 4 : tid / (W / 4)) : (L::k_fast ? tid % SK : tid / W);
+    dst0 = (uint32_t)__cvta_generic_to_shared(ring) + 4u * (uint32_t)(L::k_fast ? i0 * (SK + 4) + k : k * (W + 4) + i0);
+    if (vec) {
+#pragma unroll
+      for (int e = 0; e < N16; ++e) {
+        const int i = L::k_fast ? i0 + e * (SN / V) : i0, kk = L::k_fast ? k : k + e * (SN / (W / 4));
+        const int in = idle ? 0 : L::k_fast ? (i < n ? 4 : 0) : n - i;
+        const uint32_t bytes = in <= 0 ? 0u : in >= 4 ? 16u : 4u * (uint32_t)in;
+        size |= bytes << (8 * e);
+        src[e] = bytes ? l.ptr(i, kk) : l.p;
+      }
     } else {
-      const int i0 = L::k_fast ? tid / SK : tid % W;
-      k = L::k_fast ? tid % SK : tid / W;
-      idle = false;
-      dst0 = (uint32_t)__cvta_generic_to_shared(ring) + 4u * (uint32_t)(L::k_fast ? i0 * (SK + 4) + k : k * (W + 4) + i0);
 #pragma unroll
       for (int e = 0; e < N4; ++e) {
         const int i = L::k_fast ? i0 + e * (SN / SK) : i0, kk = L::k_fast ? k : k + e * (SN / W);
@@ -104,24 +107,27 @@ struct Stager {
         size |= (uint32_t)in << e;
         src[e] = in ? l.ptr(i, kk) : l.p;
       }
-      if (!L::k_fast && !size) step_len = 0;
     }
   }
   // copies the step in hand into the ring's buffer at byte offset `off` and moves on
   __device__ __forceinline__ void step(uint32_t off) {
     if (vec) {
       if (!idle) {
-        const int left = K - k;
-        const uint32_t valid = L::k_fast ? (left <= 0 ? 0u : min(size, 4u * (uint32_t)min(left, 4))) : left > 0 ? size : 0u;
-        copy16(dst0 + off, src[0], (int)valid);
-        src[0] += step_len;
+#pragma unroll
+        for (int e = 0; e < N16; ++e) {
+          const uint32_t bytes = (size >> (8 * e)) & 255u;
+          const int left = K - (L::k_fast ? k : k + e * (SN / (W / 4)));
+          const uint32_t valid = L::k_fast ? (left <= 0 ? 0u : min(bytes, 4u * (uint32_t)min(left, 4))) : left > 0 ? bytes : 0u;
+          copy16(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * (SN / V) * (SK + 4) : e * (SN / (W / 4)) * (W + 4)), src[e], (int)valid);
+          if (bytes) src[e] += step_len;
+        }
       }
     } else {
 #pragma unroll
       for (int e = 0; e < N4; ++e) {
         const bool in = ((size >> e) & 1u) && k + (L::k_fast ? 0 : e * (SN / W)) < K;
         copy4(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * (SN / SK) * (SK + 4) : e * (SN / W) * (W + 4)), src[e], in ? 4 : 0);
-        if (!L::k_fast || ((size >> e) & 1u)) src[e] += step_len;
+        if ((size >> e) & 1u) src[e] += step_len;
       }
     }
     k += SK;
@@ -151,34 +157,36 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
     for (int j = 0; j < 8; ++j) part[i][j] = 0.f;
   auto multiply = [&](int buf) {
     const float *A = sm.a[buf], *B = sm.b[buf];
-    const int k0 = group * 4;
-    float a[R][4];
-    if constexpr (LA::k_fast) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const float4 f = *reinterpret_cast<const float4*>(A + (ty + 8 * i) * (SK + 4) + k0);
-        a[i][0] = f.x; a[i][1] = f.y; a[i][2] = f.z; a[i][3] = f.w;
-      }
-    } else {
+    for (int k0 = group * GE::KG; k0 < group * GE::KG + GE::KG; k0 += 4) {
+      float a[R][4];
+      if constexpr (LA::k_fast) {
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-        for (int i = 0; i < R; ++i) a[i][kk] = A[(k0 + kk) * (TM + 4) + ty + 8 * i];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float b[4];
-      if constexpr (LB::k_fast) {
-        const float4 f = *reinterpret_cast<const float4*>(B + (tx + 8 * j) * (SK + 4) + k0);
-        b[0] = f.x; b[1] = f.y; b[2] = f.z; b[3] = f.w;
+        for (int i = 0; i < R; ++i) {
+          const float4 f = *reinterpret_cast<const float4*>(A + (ty + 8 * i) * (SK + 4) + k0);
+          a[i][0] = f.x; a[i][1] = f.y; a[i][2] = f.z; a[i][3] = f.w;
+        }
       } else {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) b[kk] = B[(k0 + kk) * (ST + 4) + tx + 8 * j];
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int i = 0; i < R; ++i) a[i][kk] = A[(k0 + kk) * (TM + 4) + ty + 8 * i];
       }
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
+      for (int j = 0; j < 8; ++j) {
+        float b[4];
+        if constexpr (LB::k_fast) {
+          const float4 f = *reinterpret_cast<const float4*>(B + (tx + 8 * j) * (SK + 4) + k0);
+          b[0] = f.x; b[1] = f.y; b[2] = f.z; b[3] = f.w;
+        } else {
 #pragma unroll
-        for (int i = 0; i < R; ++i) part[i][j] = fmaf(a[i][kk], b[kk], part[i][j]);
+          for (int kk = 0; kk < 4; ++kk) b[kk] = B[(k0 + kk) * (ST + 4) + tx + 8 * j];
+        }
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int i = 0; i < R; ++i) part[i][j] = fmaf(a[i][kk], b[kk], part[i][j]);
+      }
     }
   };
   __syncthreads();                                  // an earlier product may still read the buffers
