@@ -415,6 +415,8 @@ def grouped_ffn_segments(x_rows, seg_begin, seg_end, w_gate, w_up, w_down, w_mod
 # ----------------------------------------------------------------------------- grouped products
 # A decode step makes these calls every few microseconds, so they are written for little time on the host: argument
 # types are declared once (ints and addresses then pass without ctypes objects), messages are built only on failure.
+# `stream=s` is the call under torch.cuda.stream(s): outputs and workspaces made here then belong to s, so that their
+# memory is neither still in use by another stream's kernels when the call writes it nor handed on before it is done.
 _V, _I, _L, _S = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
 _ARGTYPES = {
     "capmoe_grouped_mm": [_V, _V, _V, _I, _I, _I, _I, _V, _L, _V, _V],
@@ -432,8 +434,8 @@ def _refuse(where: str, what: str, status: int = EINVAL):
     raise CapmoeError(status, f"{where}: {what}")
 
 
-def _run(name: str, stream, like, *args):
-    """Calls entry point `name` with `args` and the stream; tensors among the arguments pass as their addresses."""
+def _run(name: str, like, *args):
+    """Calls entry point `name` with `args` and the current stream; tensors among the arguments pass as their addresses."""
     here = like.get_device()
     raw = []
     for v in args:
@@ -446,7 +448,7 @@ def _run(name: str, stream, like, *args):
             raw.append(v)
     if here != torch._C._cuda_getDevice():
         _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
-    rc = getattr(_lib or lib(), name)(*raw, torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream)
+    rc = getattr(_lib or lib(), name)(*raw, torch._C._cuda_getCurrentRawStream(here))
     if rc != OK:
         raise CapmoeError(rc, name)
 
@@ -481,26 +483,32 @@ def grouped_mm(x_rows, offsets, w, y=None, dev_status=None, stream=None):
     """y[r] = W[e] x[r] for the rows r of every expert e.  x_rows [rows,d], w [E,n,d] -> y [rows,n]; rows behind
     offsets[E] are left as they are (undefined in a y made here)."""
     where = "capmoe_grouped_mm"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grouped_mm(x_rows, offsets, w, y, dev_status)
     E = _experts(where, offsets)
     if x_rows.dim() != 2 or w.dim() != 3 or w.shape[0] != E or w.shape[2] != x_rows.shape[1] or w.dtype != x_rows.dtype:
         _refuse(where, "x_rows [rows,d] and w [E,n,d] of one dtype expected")
     rows, d = x_rows.shape
     n = w.shape[1]
     y = _out(where, y, (rows, n), x_rows.dtype, x_rows)
-    _run(where, stream, x_rows, x_rows, offsets, w, E, d, n, _dt(x_rows), y, rows, _status(where, dev_status))
+    _run(where, x_rows, x_rows, offsets, w, E, d, n, _dt(x_rows), y, rows, _status(where, dev_status))
     return y
 
 
 def grouped_mm_dx(dy_rows, offsets, w, dx=None, dev_status=None, stream=None):
     """Gradient of grouped_mm's rows: dx[r] = W[e]^T dy[r].  dy_rows [rows,n], w [E,n,d] -> dx [rows,d]."""
     where = "capmoe_grouped_mm_dx"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grouped_mm_dx(dy_rows, offsets, w, dx, dev_status)
     E = _experts(where, offsets)
     if dy_rows.dim() != 2 or w.dim() != 3 or w.shape[0] != E or w.shape[1] != dy_rows.shape[1] or w.dtype != dy_rows.dtype:
         _refuse(where, "dy_rows [rows,n] and w [E,n,d] of one dtype expected")
     rows, n = dy_rows.shape
     d = w.shape[2]
     dx = _out(where, dx, (rows, d), dy_rows.dtype, dy_rows)
-    _run(where, stream, dy_rows, dy_rows, offsets, w, E, d, n, _dt(dy_rows), dx, rows, _status(where, dev_status))
+    _run(where, dy_rows, dy_rows, offsets, w, E, d, n, _dt(dy_rows), dx, rows, _status(where, dev_status))
     return dx
 
 
@@ -508,6 +516,9 @@ def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, de
     """Gradient of grouped_mm's weights: dW[e] = sum over e's rows of dy[r] x[r]^T, zeros for an expert without rows.
     -> dw [E,n,d] in the rows' dtype, or out_dtype (float32)."""
     where = "capmoe_grouped_mm_dw"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grouped_mm_dw(dy_rows, x_rows, offsets, dw, out_dtype, ws, dev_status)
     E = _experts(where, offsets)
     if (dy_rows.dim() != 2 or x_rows.dim() != 2 or dy_rows.shape[0] != x_rows.shape[0] or dy_rows.dtype != x_rows.dtype):
         _refuse(where, "dy_rows [rows,n] and x_rows [rows,d] of one dtype expected")
@@ -516,7 +527,7 @@ def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, de
     dw = _out(where, dw, (E, n, d), out_dtype or (dw.dtype if dw is not None else x_rows.dtype), x_rows)
     if ws is None:
         ws = torch.empty((_bytes("capmoe_grouped_mm_dw_workspace_bytes", E),), device=x_rows.device, dtype=torch.uint8)
-    _run(where, stream, x_rows, dy_rows, x_rows, offsets, E, d, n, _dt(x_rows), _dt(dw), dw, rows, ws,
+    _run(where, x_rows, dy_rows, x_rows, offsets, E, d, n, _dt(x_rows), _dt(dw), dw, rows, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return dw
 
@@ -530,6 +541,9 @@ def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None
     """Gradients of grouped_ffn from its input and the gradient of its output (the hidden activations are recomputed).
     -> (dx [A_max,d], dw_gate [E,F,d], dw_up [E,F,d], dw_down [E,d,F]); `dw` may hand in the last three."""
     where = "capmoe_grouped_ffn_backward"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx, dw, ws, dev_status)
     E = _experts(where, offsets)
     if (x_perm.dim() != 2 or x_perm.shape != dy_perm.shape or w_gate.dim() != 3 or w_gate.shape[0] != E or
             w_gate.shape[2] != x_perm.shape[1] or w_up.shape != w_gate.shape or
@@ -547,7 +561,7 @@ def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None
     dwd = _out(where, dwd, (E, d, F), dtype, x_perm)
     if ws is None:
         ws = torch.empty((ffn_backward_workspace_bytes(A_max, E, F, dtype),), device=x_perm.device, dtype=torch.uint8)
-    _run(where, stream, x_perm, x_perm, dy_perm, offsets, E, d, F, _dt(dtype), w_gate, w_up, w_down, dx, dwg, dwu, dwd, A_max, ws,
+    _run(where, x_perm, x_perm, dy_perm, offsets, E, d, F, _dt(dtype), w_gate, w_up, w_down, dx, dwg, dwu, dwd, A_max, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return dx, dwg, dwu, dwd
 
@@ -565,6 +579,9 @@ def quantize_rows(x, offsets=None, out=None, stream=None):
     """x [rows,d] (float32 or bfloat16) -> (q [rows,d] float8_e4m3fn, scale [rows, ceil(d/128)] float8_e8m0fnu), one
     power-of-two scale per 128 columns.  With offsets [E+1] only the rows below offsets[E] are quantised."""
     where = "capmoe_quantize_rows"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantize_rows(x, offsets, out)
     if x.dim() != 2:
         _refuse(where, "x [rows,d] expected")
     rows, d = x.shape
@@ -576,7 +593,8 @@ def quantize_rows(x, offsets=None, out=None, stream=None):
         n_rows = offsets.data_ptr() + 4 * _experts(where, offsets)
         if offsets.get_device() != x.get_device():
             _refuse(where, "offsets must be on x's device")
-    _run(where, stream, x, x, n_rows, rows, d, _dt(x), q, scale)
+        assert offsets.is_contiguous(), "capmoe tensors must be contiguous"
+    _run(where, x, x, n_rows, rows, d, _dt(x), q, scale)
     return q, scale
 
 
@@ -584,13 +602,16 @@ def quantize_weights(w, out=None, stream=None):
     """w [E,n,d] -> (q [E,n,d] float8_e4m3fn, scale [E, ceil(n/128), ceil(d/128)] float8_e8m0fnu), one scale per
     128 x 128 block."""
     where = "capmoe_quantize_weights"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantize_weights(w, out)
     if w.dim() != 3:
         _refuse(where, "w [E,n,d] expected")
     E, n, d = w.shape
     q, scale = (None, None) if out is None else out
     q = _out(where, q, (E, n, d), FP8, w)
     scale = _out(where, scale, (E, _blocks(n), _blocks(d)), SCALE, w)
-    _run(where, stream, w, w, E, n, d, _dt(w), q, scale)
+    _run(where, w, w, E, n, d, _dt(w), q, scale)
     return q, scale
 
 
@@ -603,6 +624,9 @@ def _coded(where: str, q, scale, shape, tall: int):
 def grouped_mm_fp8(x_q, x_scale, offsets, w_q, w_scale, y=None, dev_status=None, stream=None):
     """grouped_mm from 8-bit rows (quantize_rows) and weights (quantize_weights) -> y [rows,n] bfloat16."""
     where = "capmoe_grouped_mm_fp8"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grouped_mm_fp8(x_q, x_scale, offsets, w_q, w_scale, y, dev_status)
     E = _experts(where, offsets)
     if x_q.dim() != 2 or w_q.dim() != 3:
         _refuse(where, "x_q [rows,d], w_q [E,n,d] expected")
@@ -611,7 +635,7 @@ def grouped_mm_fp8(x_q, x_scale, offsets, w_q, w_scale, y=None, dev_status=None,
     _coded(where, x_q, x_scale, (rows, d), 1)
     _coded(where, w_q, w_scale, (E, n, d), QBLOCK)
     y = _out(where, y, (rows, n), torch.bfloat16, x_q)
-    _run(where, stream, x_q, x_q, x_scale, offsets, w_q, w_scale, E, d, n, y, rows, _status(where, dev_status))
+    _run(where, x_q, x_q, x_scale, offsets, w_q, w_scale, E, d, n, y, rows, _status(where, dev_status))
     return y
 
 
@@ -623,6 +647,9 @@ def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None,
     """grouped_ffn with 8-bit weights, each a (q, scale) pair of quantize_weights; x_perm [A_max,d] bfloat16 and the
     hidden rows are quantised on the way -> y_perm [A_max,d] bfloat16."""
     where = "capmoe_grouped_ffn_fp8"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm, ws, dev_status)
     E = _experts(where, offsets)
     if x_perm.dim() != 2 or x_perm.dtype != torch.bfloat16 or w_gate[0].dim() != 3:
         _refuse(where, "x_perm [A_max,d] bfloat16 and (q, scale) weights expected")
@@ -634,7 +661,7 @@ def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None,
     y_perm = _out(where, y_perm, (A_max, d), torch.bfloat16, x_perm)
     if ws is None:
         ws = torch.empty((ffn_fp8_workspace_bytes(A_max, d, F),), device=x_perm.device, dtype=torch.uint8)
-    _run(where, stream, x_perm, x_perm, offsets, E, d, F, *w_gate, *w_up, *w_down, y_perm, A_max, ws,
+    _run(where, x_perm, x_perm, offsets, E, d, F, *w_gate, *w_up, *w_down, y_perm, A_max, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return y_perm
 

@@ -54,10 +54,11 @@ inline bool gmm_supported(int E, int d, int n, int dtype) {
   const int64_t lim = (int64_t)1 << 31;
   return dtype == CAPMOE_BF16 && d % 8 == 0 && n % 8 == 0 && (int64_t)E * n < lim && (int64_t)E * d < lim;
 }
-// `early`: the caller vouches that offsets and weights were final before the previous kernel on the stream started its work,
-// because that kernel is this library's own, of the same call, and lets its successor start only after its own wait for
-// what came before (wait_for_previous_kernel, then allow_next_kernel); the counter was cleared before that one.  The kernel then fetches its first weights while
-// the previous one, which makes the token rows, still runs: 4 us of a decode step's launch.
+// `early`: the caller vouches that offsets, weights and the cleared counter were final before any kernel of this call that
+// may still run began its work: the call's first kernel lets its successor start only after its own wait for what came
+// before (wait_for_previous_kernel, then allow_next_kernel), the ones between may be early themselves.  The kernel then
+// fetches its first weights while the previous one, which makes the token rows, still runs (8-bit FFN of a decode step,
+// 310 rows of 60 experts, with tile counters: 96 us, 102 without).
 int gmm_fwd(const void* x, const Segments& sg, const void* w, int d, int n, void* y, int32_t* dev_status, int32_t* sched,
             bool early, cudaStream_t st);
 int gmm_dx(const void* dy, const Segments& sg, const void* w, int d, int n, void* dx, int32_t* dev_status, int32_t* sched,

@@ -323,3 +323,29 @@ def test_matrices_past_32_bit_offsets(cm):
     y = cm.grouped_mm_fp8(q, s, off, wq, ws)
     for e, r in ((0, slice(rows - 500, rows - 400)), (1, slice(rows - 400, rows))):
         R.close(y[r], *R.product(R.decoded(q[r], s[r], 1), R.decoded(wq[e], ws[e], 128), BF16))
+
+
+def test_a_call_on_another_stream_keeps_its_workspace(cm):
+    """The call is queued behind 10 ms of waiting on its own stream; meanwhile the current stream takes memory of the
+    workspace's size and writes to it.  Workspaces made inside a call belong to the call's stream, so nothing changes."""
+    counts, d, F = [70, 0, 5, 200], 256, 384
+    off = R.offsets_of(counts)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rand = lambda *s, dtype: torch.randn(s, device="cuda", generator=g).mul_(0.3).to(dtype)
+    x8, w8 = rand(275, d, dtype=torch.bfloat16), [cm.quantize_weights(rand(4, *s, dtype=torch.bfloat16)) for s in ((F, d), (F, d), (d, F))]
+    x, dy = rand(275, d, dtype=torch.float32), rand(275, d, dtype=torch.float32)
+    w = [rand(4, *s, dtype=torch.float32) for s in ((F, d), (F, d), (d, F))]
+    for need, call in ((cm.ffn_fp8_workspace_bytes(275, d, F), lambda **kw: (cm.grouped_ffn_fp8(x8, off, *w8, **kw),)),
+                       (cm.ffn_backward_workspace_bytes(275, 4, F, torch.float32),
+                        lambda **kw: cm.grouped_ffn_backward(x, dy, off, *w, **kw))):
+        want = call()
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = call(stream=side)
+        taken = [torch.full((need,), 0x5a, device="cuda", dtype=torch.uint8) for _ in range(8)]
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
+        del taken

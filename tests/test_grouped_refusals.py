@@ -128,3 +128,8 @@ def test_binding_checks_shapes_and_types(cm):
     with pytest.raises(cm.CapmoeError) as err:
         cm.quantize_rows(torch.zeros((2, 8), dtype=torch.float16), out=(torch.zeros((2, 8)).to(cm.FP8), torch.ones((2, 1)).to(cm.SCALE)))
     assert err.value.status in (cm.EUNSUPPORTED, cm.EINVAL)
+
+
+def test_strided_offsets_are_refused(cm):
+    with pytest.raises(AssertionError, match="contiguous"):
+        cm.quantize_rows(torch.zeros((4, 64)), offsets=torch.zeros(10, dtype=torch.int32)[::2])
