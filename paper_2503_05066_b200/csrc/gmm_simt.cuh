@@ -3,12 +3,13 @@
 // hide storage type, major order and block scales.
 // A block is G groups of 64 threads; a k-step is KG G long and each group multiplies its KG of it over the whole tile, a
 // thread with a TM/8 x 8 micro-tile (rows and columns 8 apart); the partial tiles are added in shared memory at the
-// end, in a fixed order.  Shared memory, not the FMA pipe, is what a plain-FMA tile product runs into (a 16-byte load
-// takes four cycles of it whatever its lanes share), so the micro-tile is as large as registers allow.
+// end, in a fixed order.  What bounds it is latency: a k-step of two resident blocks takes about 2000 cycles, 1024 of them
+// FMA issue, in a call that lasts 8 of those and 6000 cycles around them.  Micro-tiles of 8 x 8 for 32-row tiles too (a
+// warp per group, a third fewer shared-memory reads) changed nothing or cost up to 8 %, packed pairs of FMAs 30 %.
 // The fp32 layers this serves have a few hundred tiles at most.  G = 4, two blocks to an SM, hides one block's latency
 // behind the other; when the tiles do not outnumber the SMs, G = 8 gives a tile a whole SM: of 124 blocks that could
-// share an SM the hardware puts two on some and none on others.  (1024 rows, 7 experts, 250 x 515 weights: y 15.5 us
-// with G = 4, 18.4 with 8; dx, 124 tiles, 31 and 18; with 4 x 4 micro-tiles they took 24 and 32.)
+// share an SM the hardware puts two on some and none on others.  (1034 rows, 7 experts, 250 x 515 weights: y 14.1 us
+// with G = 4, 17.5 with 8; dx, 124 tiles, 28.4 and 17.7; with 64-row tiles 24.9 and 30.7.)
 // An operand is staged as it lies in memory: [index][k] when k is contiguous, [k][index] otherwise.  fp32 operands come
 // in by cp.async, two or three k-steps ahead, in 16-byte pieces when their rows start on 16 bytes, else in 4-byte ones;
 // other types go through registers, one k-step ahead.  TM = 32 where 64-row tiles would leave SMs without one.
