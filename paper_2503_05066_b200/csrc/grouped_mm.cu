@@ -24,17 +24,19 @@ k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out,
   const int col0 = blockIdx.y * ST;
   const T* We = W + (int64_t)t.e * Nout * K;
   constexpr int R = GE::R;
-  float acc[R][4];
-  clear_acc(acc);
-  const Dense<T, true> la{A + (int64_t)t.row0 * K, K};
-  if (DIR == DIR_FWD) tile_product<GE>(la, Dense<T, true>{We + (int64_t)col0 * K, K}, t.rows, Nout - col0, K, sm, acc);
-  else tile_product<GE>(la, Dense<T, false>{We + col0, Nout}, t.rows, Nout - col0, K, sm, acc);
+  const Share k = share_of(K);
+  float acc[1][R][4];
+  clear_acc(acc[0]);
+  const Dense<T, true> la{A + (int64_t)t.row0 * K + k.k0, K};
+  if (DIR == DIR_FWD) tile_product<GE>(la, Dense<T, true>{We + (int64_t)col0 * K + k.k0, K}, t.rows, Nout - col0, k.len, sm, acc[0]);
+  else tile_product<GE>(la, Dense<T, false>{We + (int64_t)k.k0 * Nout + col0, Nout}, t.rows, Nout - col0, k.len, sm, acc[0]);
+  if (!join_shares(sm, acc)) return;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = out_row<GE>(i), c = col0 + out_col(j);
-      if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<T>(acc[i][j]);
+      if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<T>(acc[0][i][j]);
     }
 }
 
@@ -78,25 +80,28 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
   if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST, cols = F - col0;
   const int64_t we = (int64_t)t.e * F * d;
-  const Dense<T, true> lx{x + (int64_t)t.row0 * d, d}, ldy{dy + (int64_t)t.row0 * d, d};
+  const Share k = share_of(d);
+  const int64_t at = (int64_t)t.row0 * d + k.k0, wat = we + (int64_t)col0 * d + k.k0;
   constexpr int R = GE::R;
-  float g[R][4], u[R][4], dh[R][4];
-  clear_acc(g); clear_acc(u); clear_acc(dh);
-  tile_product<GE>(lx, Dense<T, true>{wg + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, g);
-  tile_product<GE>(lx, Dense<T, true>{wu + we + (int64_t)col0 * d, d}, t.rows, cols, d, sm, u);
-  tile_product<GE>(ldy, Dense<T, false>{wd + we + col0, F}, t.rows, cols, d, sm, dh);
+  float acc[3][R][4];                               // g, u, dh
+  clear_acc(acc[0]); clear_acc(acc[1]); clear_acc(acc[2]);
+  tile_product<GE>(Dense<T, true>{x + at, d}, Dense<T, true>{wg + wat, d}, t.rows, cols, k.len, sm, acc[0]);
+  tile_product<GE>(Dense<T, true>{x + at, d}, Dense<T, true>{wu + wat, d}, t.rows, cols, k.len, sm, acc[1]);
+  tile_product<GE>(Dense<T, true>{dy + at, d}, Dense<T, false>{wd + we + (int64_t)k.k0 * F + col0, F}, t.rows, cols, k.len, sm, acc[2]);
+  if (!join_shares(sm, acc)) return;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = out_row<GE>(i), c = col0 + out_col(j);
       if (r >= t.rows || c >= F) continue;
-      const float p = 1.0f / (1.0f + expf(-g[i][j]));
-      const float a = g[i][j] * p;
+      const float gv = acc[0][i][j], uv = acc[1][i][j], dhv = acc[2][i][j];
+      const float p = 1.0f / (1.0f + expf(-gv));
+      const float a = gv * p;
       const int64_t o = (int64_t)(t.row0 + r) * F + c;
-      dg[o] = from_float<T>(dh[i][j] * u[i][j] * (p + a * (1.0f - p)));
-      du[o] = from_float<T>(dh[i][j] * a);
-      h[o] = from_float<T>(a * u[i][j]);
+      dg[o] = from_float<T>(dhv * uv * (p + a * (1.0f - p)));
+      du[o] = from_float<T>(dhv * a);
+      h[o] = from_float<T>(a * uv);
     }
 }
 
@@ -110,18 +115,20 @@ k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __rest
   RowTile t;
   if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
   const int col0 = blockIdx.y * ST;
-  const int64_t we = (int64_t)t.e * F * d + col0;
+  const Share k = share_of(F);
+  const int64_t at = (int64_t)t.row0 * F + k.k0, we = (int64_t)t.e * F * d + (int64_t)k.k0 * d + col0;
   constexpr int R = GE::R;
-  float acc[R][4];
-  clear_acc(acc);
-  tile_product<GE>(Dense<T, true>{dg + (int64_t)t.row0 * F, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, F, sm, acc);
-  tile_product<GE>(Dense<T, true>{du + (int64_t)t.row0 * F, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, F, sm, acc);
+  float acc[1][R][4];
+  clear_acc(acc[0]);
+  tile_product<GE>(Dense<T, true>{dg + at, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, k.len, sm, acc[0]);
+  tile_product<GE>(Dense<T, true>{du + at, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, k.len, sm, acc[0]);
+  if (!join_shares(sm, acc)) return;
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = out_row<GE>(i), c = col0 + out_col(j);
-      if (r < t.rows && c < d) dx[(int64_t)(t.row0 + r) * d + c] = from_float<T>(acc[i][j]);
+      if (r < t.rows && c < d) dx[(int64_t)(t.row0 + r) * d + c] = from_float<T>(acc[0][i][j]);
     }
 }
 
@@ -134,7 +141,7 @@ int launched(cudaError_t err) {
 // that happen to have room, several to each, and stay there (a 1024-row fp32 product of 120 blocks, launched back to
 // back: 63 us that way, 25 without); letting it start when the sums are done changes nothing.
 template <class GE, class... KArgs, class... Args>
-int launch_tiles(void (*kernel)(KArgs...), dim3 grid, cudaStream_t st, Args... args) {
+int launch_tiles(void (*kernel)(KArgs...), dim3 grid, int split, cudaStream_t st, Args... args) {
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SimtTile<GE>));
   if (err != cudaSuccess) return note_cuda(err);
   cudaLaunchConfig_t cfg = {};
@@ -142,42 +149,57 @@ int launch_tiles(void (*kernel)(KArgs...), dim3 grid, cudaStream_t st, Args... a
   cfg.gridDim = grid;
   cfg.blockDim = dim3(GE::SN);
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;           // the blocks that share a reduction
+  attr[1].val.clusterDim.x = 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = (unsigned)split;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = split > 1 ? 2 : 1;
   return launched(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
 }
 
-dim3 row_grid(const Segments& sg, int cols, int tm) {       // every segment rounds up to whole tiles
-  return dim3((unsigned)(ceil_div(sg.rows, tm) + sg.E), (unsigned)ceil_div(cols, ST));
+dim3 row_grid(const Segments& sg, int cols, int tm, int split) {       // every segment rounds up to whole tiles
+  return dim3((unsigned)(ceil_div(sg.rows, tm) + sg.E), (unsigned)ceil_div(cols, ST), (unsigned)split);
 }
-// Geometry by the number of 64 x 64 tiles: from `large` per SM on, 64-row tiles; else 32-row ones, whose block gets an SM
-// to itself when they do not outnumber the SMs (see gmm_simt.cuh; the bound on the tiles counts the segments' ragged ends
-// once each, so a few more may run).
+// Geometry by the number of tiles: from `large` 64 x 64 ones per SM on, those; else 32-row ones, whose block gets an SM to
+// itself when they do not outnumber the SMs (see gmm_simt.cuh; FFN gradients of 236 rows of 45 experts, 41 x 415: 74 us
+// with two blocks to an SM, 90 with one).
 enum Size { LARGE, MEDIUM, SMALL };
-Size size_of(int64_t tiles64, int large = 2) {
-  return tiles64 >= large * sm_count() ? LARGE : 2 * tiles64 > sm_count() ? MEDIUM : SMALL;
+Size size_of(int64_t tiles64, int64_t tiles32, int large = 2) {
+  return tiles64 >= large * sm_count() ? LARGE : tiles32 > sm_count() ? MEDIUM : SMALL;
+}
+// Row products: the number of 32-row tiles, taking three quarters of the segments that can have rows to have some, each
+// ending in half a tile; and, while those would leave half of the SMs without one, into how many parts of at least
+// SPLIT_MIN steps the reduction is split.
+struct Plan { Size size; int split; };
+constexpr int SPLIT_MIN = 32;
+Plan plan_rows(const Segments& sg, int cols, int K) {
+  const int64_t used = ((sg.E < sg.rows ? sg.E : sg.rows) * 3 + 3) / 4, nc = ceil_div(cols, ST);
+  const int64_t t32 = ceil_div(sg.rows, 32) + used / 2, tiles32 = (t32 > used ? t32 : used) * nc;
+  Plan p = {size_of(ceil_div(sg.rows, ST) * nc, tiles32), 1};
+  if (p.size == SMALL)
+    while (p.split < 8 && tiles32 * p.split * 2 <= sm_count() && K >= p.split * 2 * SPLIT_MIN) p.split *= 2;
+  return p;
 }
 using Large = Geo<64, 4>;
 using Medium = Geo<32, 4>;
 using Small = Geo<32, 8>;
 
 template <typename T, int DIR, class GE>
-int rows_run(const T* a, const T* w, T* out, const Segments& sg, int K, int Nout, cudaStream_t st) {
-  return launch_tiles<GE>(k_mm_rows<T, DIR, GE>, row_grid(sg, Nout, GE::TM), st, a, w, out, sg, K, Nout);
+int rows_run(const T* a, const T* w, T* out, const Segments& sg, int K, int Nout, int split, cudaStream_t st) {
+  return launch_tiles<GE>(k_mm_rows<T, DIR, GE>, row_grid(sg, Nout, GE::TM, split), split, st, a, w, out, sg, K, Nout);
 }
 template <typename T, int DIR>
 int rows_simt(const void* a, const void* w, void* out, const Segments& sg, int K, int Nout, cudaStream_t st) {
-  const Size z = size_of(ceil_div(sg.rows, ST) * ceil_div(Nout, ST));
-  auto run = z == LARGE ? rows_run<T, DIR, Large> : z == MEDIUM ? rows_run<T, DIR, Medium> : rows_run<T, DIR, Small>;
-  return run((const T*)a, (const T*)w, (T*)out, sg, K, Nout, st);
+  const Plan p = plan_rows(sg, Nout, K);
+  auto run = p.size == LARGE ? rows_run<T, DIR, Large> : p.size == MEDIUM ? rows_run<T, DIR, Medium> : rows_run<T, DIR, Small>;
+  return run((const T*)a, (const T*)w, (T*)out, sg, K, Nout, p.split, st);
 }
 
 template <typename T, typename TO, class GE>
 int dw_run(const DwSet<T, TO>& s, int M, int N, unsigned z, const Segments& sg, cudaStream_t st) {
-  return launch_tiles<GE>(k_mm_dw<T, TO, GE>, dim3((unsigned)ceil_div(M, GE::TM), (unsigned)ceil_div(N, ST), z), st, s, sg);
+  return launch_tiles<GE>(k_mm_dw<T, TO, GE>, dim3((unsigned)ceil_div(M, GE::TM), (unsigned)ceil_div(N, ST), z), 1, st, s, sg);
 }
 template <typename T, typename TO>
 int dw_simt(const DwSet<T, TO>& s, int count, const Segments& sg, cudaStream_t st) {
@@ -189,19 +211,20 @@ int dw_simt(const DwSet<T, TO>& s, int count, const Segments& sg, cudaStream_t s
     tiles += ceil_div(s.M[p], ST) * ceil_div(s.N[p], ST) * sg.E;
   }
   // short sums: 64-row tiles from one per SM on (871 rows of 8 experts, 512 x 256: 12.5 us, 14.3 with 32-row tiles)
-  const Size z = size_of(tiles, 1);
+  const Size z = size_of(tiles, 2 * tiles, 1);
   auto run = z == LARGE ? dw_run<T, TO, Large> : z == MEDIUM ? dw_run<T, TO, Medium> : dw_run<T, TO, Small>;
   return run(s, M, N, (unsigned)(count * sg.E), sg, st);
 }
 
 template <typename T, class GE>
 int hidden_run(const T* x, const T* dy, const T* wg, const T* wu, const T* wd, T* dg, T* du, T* h, const Segments& sg, int d, int F,
-               cudaStream_t st) {
-  return launch_tiles<GE>(k_ffn_grad_hidden<T, GE>, row_grid(sg, F, GE::TM), st, x, dy, wg, wu, wd, dg, du, h, sg, d, F);
+               int split, cudaStream_t st) {
+  return launch_tiles<GE>(k_ffn_grad_hidden<T, GE>, row_grid(sg, F, GE::TM, split), split, st, x, dy, wg, wu, wd, dg, du, h, sg, d, F);
 }
 template <typename T, class GE>
-int dx2_run(const T* dg, const T* du, const T* wg, const T* wu, T* dx, const Segments& sg, int d, int F, cudaStream_t st) {
-  return launch_tiles<GE>(k_ffn_grad_x<T, GE>, row_grid(sg, d, GE::TM), st, dg, du, wg, wu, dx, sg, d, F);
+int dx2_run(const T* dg, const T* du, const T* wg, const T* wu, T* dx, const Segments& sg, int d, int F, int split,
+            cudaStream_t st) {
+  return launch_tiles<GE>(k_ffn_grad_x<T, GE>, row_grid(sg, d, GE::TM, split), split, st, dg, du, wg, wu, dx, sg, d, F);
 }
 template <typename T>
 int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int F, const void* w_gate, const void* w_up,
@@ -210,11 +233,11 @@ int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int 
   T* du = dg + (int64_t)sg.rows * F;
   T* h = du + (int64_t)sg.rows * F;
   const T *wg = (const T*)w_gate, *wu = (const T*)w_up, *wd = (const T*)w_down;
-  const Size zh = size_of(ceil_div(sg.rows, ST) * ceil_div(F, ST)), zx = size_of(ceil_div(sg.rows, ST) * ceil_div(d, ST));
-  auto hidden = zh == LARGE ? hidden_run<T, Large> : zh == MEDIUM ? hidden_run<T, Medium> : hidden_run<T, Small>;
-  auto dx2 = zx == LARGE ? dx2_run<T, Large> : zx == MEDIUM ? dx2_run<T, Medium> : dx2_run<T, Small>;
-  int rc = hidden((const T*)x, (const T*)dy, wg, wu, wd, dg, du, h, sg, d, F, st);
-  if (rc == CAPMOE_OK) rc = dx2(dg, du, wg, wu, (T*)dx, sg, d, F, st);
+  const Plan ph = plan_rows(sg, F, d), px = plan_rows(sg, d, F);
+  auto hidden = ph.size == LARGE ? hidden_run<T, Large> : ph.size == MEDIUM ? hidden_run<T, Medium> : hidden_run<T, Small>;
+  auto dx2 = px.size == LARGE ? dx2_run<T, Large> : px.size == MEDIUM ? dx2_run<T, Medium> : dx2_run<T, Small>;
+  int rc = hidden((const T*)x, (const T*)dy, wg, wu, wd, dg, du, h, sg, d, F, ph.split, st);
+  if (rc == CAPMOE_OK) rc = dx2(dg, du, wg, wu, (T*)dx, sg, d, F, px.split, st);
   if (rc != CAPMOE_OK) return rc;
   DwSet<T, T> s = {{dg, du, (const T*)dy}, {(const T*)x, (const T*)x, h}, {(T*)dwg, (T*)dwu, (T*)dwd}, {F, F, d}, {d, d, F}};
   return dw_simt(s, 3, sg, st);

@@ -98,6 +98,13 @@ def test_many_segments_fp32(cm):
     _check_all(cm, COUNTS["many"], 40, 72, F32)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("counts,d,n", [([1], 1021, 37), ([3, 0, 1], 64, 1001), ([2, 5], 511, 130), ([1, 40], 65, 300), ([7], 4099, 5)])
+def test_few_rows_with_long_sums(cm, counts, d, n, dtype):
+    """So few tiles that the reduction is split over a cluster's blocks, in 2, 4 and 8 parts."""
+    _check_all(cm, counts, d, n, dtype)
+
+
 @pytest.mark.parametrize("counts", [COUNTS["borders"], COUNTS["longer"]])
 def test_without_a_status_block(cm, counts):
     _check_all(cm, counts, 192, 320, BF16, status=False)
@@ -163,6 +170,11 @@ def _check_ffn_gradient(cm, counts, d, F, dtype):
                                         ([1200, 0, 33], 136, 192)])
 def test_ffn_gradient(cm, counts, d, F, dtype):
     _check_ffn_gradient(cm, counts, d, F, dtype)
+
+
+@pytest.mark.parametrize("counts,d,F", [([1], 1001, 33), ([2, 0, 5], 300, 70), ([33, 1], 515, 96), ([4], 70, 999)])
+def test_ffn_gradient_of_few_rows(cm, counts, d, F):
+    _check_ffn_gradient(cm, counts, d, F, F32)
 
 
 def test_ffn_gradient_against_differences(cm):
