@@ -136,9 +136,10 @@ struct Stager {
   }
 };
 
-// Result element (i, j) of a thread, i < R, j < 4: row and column in the tile
+// Result element (i, j) of a thread, i < R, j < 4: row and column in the tile (a store's lanes write runs of 64 bytes; four
+// columns side by side in a thread, each stored by itself as rows of odd length want it, take four times the requests)
 template <class GE> __device__ __forceinline__ int out_row(int i) { return (int)(threadIdx.x >> 4) + (GE::SN / 16) * i; }
-__device__ __forceinline__ int out_col(int j) { return (int)(threadIdx.x & 15) * 4 + j; }
+__device__ __forceinline__ int out_col(int j) { return (int)(threadIdx.x & 15) + 16 * j; }
 constexpr int CROW = ST + 8;                        // row of a partial tile
 
 // acc += A B^T over the tile; result elements at out_row / out_col
@@ -274,9 +275,9 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
   }
 #pragma unroll
   for (int i = 0; i < GE::R; ++i) {
-    const float* c0 = &sm.a[0][0] + out_row<GE>(i) * CROW + out_col(0);
-    const float4 p = *reinterpret_cast<const float4*>(c0), q = *reinterpret_cast<const float4*>(c0 + TM * CROW);
-    acc[i][0] += p.x + q.x; acc[i][1] += p.y + q.y; acc[i][2] += p.z + q.z; acc[i][3] += p.w + q.w;
+    const float* c0 = &sm.a[0][0] + out_row<GE>(i) * CROW;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] += c0[out_col(j)] + c0[TM * CROW + out_col(j)];
   }
 }
 
@@ -297,22 +298,25 @@ __device__ __forceinline__ bool join_shares(SimtTile<GE>& sm, float (&acc)[N][GE
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   const int row = out_row<GE>(0);
-  float* C = &sm.a[0][0] + row * ST + out_col(0);
+  float* C = &sm.a[0][0] + row * ST;
   __syncthreads();                                  // the last product's partial tiles have been read
 #pragma unroll
   for (int n = 0; n < N; ++n)
-    *reinterpret_cast<float4*>(C + n * GE::TM * ST) = make_float4(acc[n][0][0], acc[n][0][1], acc[n][0][2], acc[n][0][3]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) C[n * GE::TM * ST + out_col(j)] = acc[n][0][j];
   cluster.sync();
   const bool mine = row * S / GE::TM == (int)blockIdx.z;
   if (mine) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
       for (int z = 0; z < S; ++z) {
-        const float4 p = *reinterpret_cast<const float4*>(cluster.map_shared_rank(C + n * GE::TM * ST, z));
-        s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
+        const float* p = cluster.map_shared_rank(C + n * GE::TM * ST, z);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += p[out_col(j)];
       }
-      acc[n][0][0] = s.x; acc[n][0][1] = s.y; acc[n][0][2] = s.z; acc[n][0][3] = s.w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[n][0][j] = s[j];
     }
   }
   cluster.sync();                                   // nobody reads this block's memory any more
