@@ -8,8 +8,8 @@
 // warp per group, a third fewer shared-memory reads) changed nothing or cost up to 8 %, packed pairs of FMAs 30 %.
 // The fp32 layers this serves have a few hundred tiles at most.  G = 4, two blocks to an SM, hides one block's latency
 // behind the other; when the tiles do not outnumber the SMs, G = 8 gives a tile a whole SM: of 124 blocks that could
-// share an SM the hardware puts two on some and none on others.  (1034 rows, 7 experts, 250 x 515 weights: y 14.1 us
-// with G = 4, 17.5 with 8; dx, 124 tiles, 28.4 and 17.7; with 64-row tiles 24.9 and 30.7.)
+// share an SM the hardware puts two on some and none on others.  (1034 rows, 7 experts, 250 x 515 weights: y 13.9 us
+// with G = 4, 17.5 with 8; dx, 124 tiles, 28 and 17.5; with 64-row tiles 25 and 31.)
 // An operand is staged as it lies in memory: [index][k] when k is contiguous, [k][index] otherwise.  fp32 operands come
 // in by cp.async, two or three k-steps ahead, in 16-byte pieces when their rows start on 16 bytes, else in 4-byte ones;
 // other types go through registers, one k-step ahead.  TM = 32 where 64-row tiles would leave SMs without one.
