@@ -287,6 +287,9 @@ int capmoe_grouped_ffn_segments(const void* x_rows, const int32_t* seg_begin, co
  *                          dx_perm [A_max,d], dw_gate/dw_up [E,F,d], dw_down [E,d,F], all in `dtype`.
  *                          dg, du and h are rounded to `dtype` before the products that read them.
  *                          ws: capmoe_ffn_backward_workspace_bytes(A_max,E,F,dtype) bytes.
+ * Either workspace may be larger by capmoe_dw_split_bytes(rows, E, d, n, dtype, products) bytes (products: 1, for the
+ * backward pass 3 with rows = A_max, n = F): the reductions are then split into parts, summed in fp32 in a fixed order, when
+ * there are few output tiles and long segments (0 bytes when that would not help).
  * Outputs and workspace overlap neither each other nor an input.
  * bf16 with d and n (F) multiples of 8 runs on tensor cores (TMA-fed tiles, fp32 accumulators); fp32 and other
  * sizes run plain fp32-FMA kernels.  dev_status as in capmoe_grouped_ffn.  E <= 256, rows < 2^31. */
@@ -298,6 +301,7 @@ int capmoe_grouped_mm_dw_workspace_bytes(int E, size_t* bytes);
 int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, const int32_t* expert_offsets, int E, int d, int n,
                          int dtype, int out_dtype, void* dw, int64_t rows, void* ws, size_t ws_bytes, int32_t* dev_status,
                          void* stream);
+int capmoe_dw_split_bytes(int64_t rows, int E, int d, int n, int dtype, int products, size_t* bytes);
 int capmoe_ffn_backward_workspace_bytes(int64_t A_max, int E, int F, int dtype, size_t* bytes);
 int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_perm, const int32_t* expert_offsets, int E, int d, int F,
                                 int dtype, const void* w_gate, const void* w_up, const void* w_down, void* dx_perm,

@@ -7,6 +7,7 @@ no CPU or PyTorch fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from dataclasses import dataclass
@@ -32,7 +33,7 @@ EXPORTS = ["capmoe_capacity", "capmoe_max_rows", "capmoe_device_max_rows", "capm
            "capmoe_grouped_ffn_segments", "capmoe_debug_ffn_variant", "capmoe_ep_plan", "capmoe_ep_forward_dispatch", "capmoe_ep_forward_experts", "capmoe_ep_forward_combine", "capmoe_ep_segments", "capmoe_ep_dispatch",
            "capmoe_ep_combine", "capmoe_debug_read_probe", "capmoe_debug_check_indices",
            "capmoe_grouped_mm", "capmoe_grouped_mm_dx", "capmoe_grouped_mm_dw_workspace_bytes", "capmoe_grouped_mm_dw",
-           "capmoe_ffn_backward_workspace_bytes", "capmoe_grouped_ffn_backward", "capmoe_quantize_rows",
+           "capmoe_dw_split_bytes", "capmoe_ffn_backward_workspace_bytes", "capmoe_grouped_ffn_backward", "capmoe_quantize_rows",
            "capmoe_quantize_weights", "capmoe_grouped_mm_fp8", "capmoe_ffn_fp8_workspace_bytes", "capmoe_grouped_ffn_fp8"]
 
 
@@ -526,14 +527,36 @@ def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, de
     d = x_rows.shape[1]
     dw = _out(where, dw, (E, n, d), out_dtype or (dw.dtype if dw is not None else x_rows.dtype), x_rows)
     if ws is None:
-        ws = torch.empty((_bytes("capmoe_grouped_mm_dw_workspace_bytes", E),), device=x_rows.device, dtype=torch.uint8)
+        ws = x_rows.new_empty((_dw_bytes(rows, E, d, n, x_rows.dtype),), dtype=torch.uint8)
     _run(where, x_rows, dy_rows, x_rows, offsets, E, d, n, _dt(x_rows), _dt(dw), dw, rows, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return dw
 
 
+def dw_split_bytes(rows: int, E: int, d: int, n: int, dtype, products: int = 1) -> int:
+    """What to add to the workspace of grouped_mm_dw (products=1) or grouped_ffn_backward (n=F, products=3) for splitting
+    long sums when there are few output tiles; workspaces made inside those calls have it."""
+    return _bytes("capmoe_dw_split_bytes", _i64(rows), int(E), int(d), int(n), _dt(dtype), int(products))
+
+
 def ffn_backward_workspace_bytes(A_max: int, E: int, F: int, dtype) -> int:
     return _bytes("capmoe_ffn_backward_workspace_bytes", _i64(A_max), int(E), int(F), _dt(dtype))
+
+
+# sizes of the workspaces that the calls make themselves
+@functools.lru_cache(maxsize=1024)
+def _dw_bytes(rows, E, d, n, dtype):
+    return _bytes("capmoe_grouped_mm_dw_workspace_bytes", E) + dw_split_bytes(rows, E, d, n, dtype)
+
+
+@functools.lru_cache(maxsize=1024)
+def _ffn_backward_bytes(A_max, E, d, F, dtype):
+    return ffn_backward_workspace_bytes(A_max, E, F, dtype) + dw_split_bytes(A_max, E, d, F, dtype, 3)
+
+
+@functools.lru_cache(maxsize=1024)
+def _ffn_fp8_bytes(A_max, d, F):
+    return ffn_fp8_workspace_bytes(A_max, d, F)
 
 
 def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None, dw=None, ws=None, dev_status=None,
@@ -560,7 +583,7 @@ def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None
     dwu = _out(where, dwu, (E, F, d), dtype, x_perm)
     dwd = _out(where, dwd, (E, d, F), dtype, x_perm)
     if ws is None:
-        ws = torch.empty((ffn_backward_workspace_bytes(A_max, E, F, dtype),), device=x_perm.device, dtype=torch.uint8)
+        ws = x_perm.new_empty((_ffn_backward_bytes(A_max, E, d, F, dtype),), dtype=torch.uint8)
     _run(where, x_perm, x_perm, dy_perm, offsets, E, d, F, _dt(dtype), w_gate, w_up, w_down, dx, dwg, dwu, dwd, A_max, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return dx, dwg, dwu, dwd
@@ -660,7 +683,7 @@ def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None,
     _coded(where, *w_down, (E, d, F), QBLOCK)
     y_perm = _out(where, y_perm, (A_max, d), torch.bfloat16, x_perm)
     if ws is None:
-        ws = torch.empty((ffn_fp8_workspace_bytes(A_max, d, F),), device=x_perm.device, dtype=torch.uint8)
+        ws = x_perm.new_empty((_ffn_fp8_bytes(A_max, d, F),), dtype=torch.uint8)
     _run(where, x_perm, x_perm, offsets, E, d, F, *w_gate, *w_up, *w_down, y_perm, A_max, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return y_perm

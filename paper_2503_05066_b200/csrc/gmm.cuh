@@ -68,13 +68,16 @@ int gmm_hidden(const void* x, const void* dy, const Segments& sg, int d, int F, 
 int gmm_dx2(const void* dg, const void* du, const Segments& sg, int d, int F, const void* wg, const void* wu, void* dx,
             int32_t* dev_status, int32_t* sched, bool early, cudaStream_t st);
 size_t gmm_dw_map_bytes(int E, int lists);
-int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws,
-           int32_t* dev_status, int32_t* sched, cudaStream_t st);
+// into how many parts the reductions of `products` gradients are split when `parts` (16-byte aligned) has room for them
+int gmm_dw_split(int64_t rows, int E, int d, int n, int products);
+size_t gmm_dw_parts_bytes(int E, int d, int n, int products, int split);
+int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws, float* parts,
+           int split, int32_t* dev_status, int32_t* sched, cudaStream_t st);
 // the FFN's three weight gradients: the maps first (they need the addresses only, so they can be made ahead)
 int gmm_dw_ffn_maps(const void* dg, const void* du, const void* dy, const void* x, const void* h, const Segments& sg, int d, int F,
                     void* map_ws, cudaStream_t st);
-int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd, const void* map_ws, int32_t* dev_status,
-               int32_t* sched, cudaStream_t st);
+int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd, const void* map_ws, float* parts, int split,
+               int32_t* dev_status, int32_t* sched, cudaStream_t st);
 // 8-bit (gmm_rows.cu, gmm_swiglu8.cu): d and n (F) multiples of 16; xs_ld, hs_ld: bytes from one row's scales to the next's
 inline bool gmm8_supported(int d, int n) { return d % 16 == 0 && n % 16 == 0; }
 int gmm8(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wq, const uint8_t* ws, int d, int n, void* y,

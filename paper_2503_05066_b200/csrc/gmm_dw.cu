@@ -6,6 +6,9 @@
 // transposed in memory.  The rows of an expert are ragged: the tensor maps are copies, one per expert, whose row count
 // ends where the expert's rows end (made on the device by k_segment_maps, since the host does not know the offsets),
 // so TMA fills the rows behind with zeros and no other expert's row, NaN or not, enters the sum.
+// When the tiles are fewer than half the pairs (one or two experts of a rank, thousands of rows each) the reductions are
+// split into parts, each a tile of its own with an fp32 output in the workspace, and a second kernel adds the parts in
+// their order.
 // What bounds it: a tile of an expert with a few hundred rows has only a handful of k-blocks, about as long as its
 // epilogue (3200 cycles) and as its share of the HBM writes; 17,500 rows of 64 experts, 2048 x 1024: 92 us for 268 MB of
 // gradients (0.44 of the tensor pipe, 0.6 of the copy bandwidth), the three gradients of the FFN there 262 us.
@@ -21,6 +24,7 @@ struct DwArgs {
   void* out[3];                // the outputs as plain pointers, for pieces that do not fill a box
   int count, M[3], N[3];       // products, their sizes: out[p] is [E, M, N]
   int ia[3], ib[3];            // which of the per-expert map lists holds each product's operands
+  int split;                   // parts of every reduction, each with an output of its own: out[p] is [split, E, M, N]
   int wide_a, wide_b;          // a bit per product: one box per k-block (see make_mn_map)
   const CUtensorMap* maps;     // [lists][E]
   int32_t* dev_status;
@@ -53,8 +57,9 @@ constexpr int DW_TAIL = DW_STG_OFF + EPI_WARPS * WIDE_BYTES;
 constexpr int DW_SMEM = DW_TAIL + 1024 + 512 + 2 * (GMM_MAX_E + 1) * 4 + 16 + TR_BYTES;
 static_assert(DW_SMEM <= 227 * 1024, "shared memory of a thread block");
 
-// e, product p; row0, rows: output rows of the tile; n0: first output column; k0, num_kb: first row and k-blocks of the expert
-struct DTile { int e, row0, rows, n0, p, num_kb, k0; };
+// e, product p; row0, rows: output rows of the tile; n0: first output column; k0, num_kb: first row and k-blocks of the
+// reduction; oe: which of the output's [split * E] matrices
+struct DTile { int e, row0, rows, n0, p, num_kb, k0, oe; };
 
 constexpr int GMM_THREADS = TC_THREADS + 32;             // one more warp: the scheduler
 
@@ -109,12 +114,12 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
   const uint32_t tmem_base = *tmem_slot;
 
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
-  const int tile_hi = E * per_e;
+  const int tile_hi = E * per_e * ar.split;
   auto get_tile = [&](int j, bool whole_warp, DTile& t) -> bool {
     int4 a, b;
     if (!ring.get(j, whole_warp, a, b)) return false;
     t.e = a.x; t.row0 = a.y; t.rows = a.z; t.n0 = a.w;
-    t.p = b.x; t.num_kb = b.y; t.k0 = b.z;
+    t.p = b.x; t.num_kb = b.y; t.k0 = b.z; t.oe = b.w;
     return true;
   };
 
@@ -180,8 +185,8 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
     // ------------------------------------------------------------ scheduler (both CTAs)
     if (elect_one()) {
       ring.run(pair, npairs, tile_hi, ar.sched, [&](int tile, int4& a, int4& b) {
-        const int e = tile / per_e;
-        int local = tile - e * per_e, p = 0, nmb = (ar.M[0] + 255) >> 8;
+        const int part = tile / per_e, e = part / ar.split, s = part - e * ar.split;
+        int local = tile - part * per_e, p = 0, nmb = (ar.M[0] + 255) >> 8;
         while (p + 1 < ar.count) {
           const int here = nmb * ((ar.N[p] + 255) >> 8);
           if (local < here) break;
@@ -190,7 +195,8 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
         }
         const int nb = local / nmb, m0 = (local - nb * nmb) * BM2;
         a = make_int4(e, m0, min(BM2, ar.M[p] - m0), nb * 256);
-        b = make_int4(p, (ends[e] - offs[e] + BK - 1) / BK, offs[e], 0);
+        const int kbs = (ends[e] - offs[e] + BK - 1) / BK, each = (kbs + ar.split - 1) / ar.split, first = min(s * each, kbs);
+        b = make_int4(p, min(each, kbs - first), offs[e] + first * BK, s * E + e);
       });
     }
   } else {
@@ -211,7 +217,7 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
       const bool full_rows = warp_row0 + 32 <= t.rows, row_ok = warp_row0 + lane < t.rows;
       const bool empty_sum = t.num_kb == 0;                     // an expert without rows: zeros
       const int Nout = ar.N[t.p];
-      const int64_t row = (int64_t)t.e * ar.M[t.p] + t.row0 + warp_row0;
+      const int64_t row = (int64_t)t.oe * ar.M[t.p] + t.row0 + warp_row0;
       const CUtensorMap* mo = t.p == 0 ? &mp.o0 : t.p == 1 ? &mp.o1 : &mp.o2;
       TO* orow = reinterpret_cast<TO*>(ar.out[t.p]) + (row + lane) * Nout + t.n0;
       constexpr int PC = 128 / (int)sizeof(TO);               // columns of a piece
@@ -256,6 +262,32 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
   if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
 }
 
+// Sum of the parts, in their order.  out[p] [n] from parts [3][split][n], n a multiple of 4.
+template <typename TO> struct JoinSet { TO* out[3]; };
+template <typename TO>
+__global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ parts, JoinSet<TO> to, int split, int64_t n, int per_product) {
+  wait_for_previous_kernel();
+  allow_next_kernel();
+  const int p = (int)blockIdx.x / per_product;
+  const int64_t i = ((int64_t)(blockIdx.x - (unsigned)(p * per_product)) * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  const float* from = parts + (int64_t)p * split * n + i;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0; k < split; ++k) {
+    const float4 v = *reinterpret_cast<const float4*>(from + k * n);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(to.out[p] + i) = s;
+  else *reinterpret_cast<uint2*>(to.out[p] + i) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+}
+template <typename TO>
+int join_parts(const float* parts, int products, const JoinSet<TO>& to, int split, int64_t n, cudaStream_t st) {
+  const int per = (int)ceil_div(n, 1024);
+  const int rc = note_cuda(launch_chained(k_join_parts<TO>, (unsigned)(products * per), 256, 0, st, parts, to, split, n, per));
+  count_launch(1);
+  return rc;
+}
+
 template <typename TO>
 int launch(const DwMaps& mp, const DwArgs& ar, cudaStream_t st) {
   const int pairs = sm_count() / 2;
@@ -288,22 +320,43 @@ int segment_maps(const BaseMaps& base, int lists, const Segments& sg, void* ws, 
 
 }  // namespace
 
+size_t gmm_dw_parts_bytes(int E, int d, int n, int products, int split) {
+  return split > 1 ? (size_t)split * products * E * d * n * sizeof(float) : 0;
+}
+// A reduction's parts: with fewer tiles than half the pairs, as many as save most, of 8 k-blocks at least on the average of
+// the allocated rows.  A k-block takes 0.27 us; joining parts takes a launch, 3 us, and writes and reads them once (6 bytes
+// a nanosecond, 1000 times that a microsecond).  One expert, 2048 x 1024, two parts: 16,384 rows 81 us whole, 59 split,
+// 4096 rows 26.7 and 24.9, 2048 rows 17.6 and 19.8 (not split); 3 experts of 9000 rows, 104 x 88, 16 parts: 89 and 20.
+int gmm_dw_split(int64_t rows, int E, int d, int n, int products) {
+  const int64_t pairs = sm_count() / 2, tiles = ceil_div(d, 256) * ceil_div(n, 256) * E * products, kbs = rows / E / BK;
+  int best = 1;
+  double gain = 0;
+  for (int s = 2; s <= 16 && s * tiles <= pairs && kbs >= 8 * s; ++s) {
+    const double g = 0.27 * (double)kbs * (s - 1) / s - 3.0 - (double)gmm_dw_parts_bytes(E, d, n, products, s) * 2 / 6e6;
+    if (g > gain) { gain = g; best = s; }
+  }
+  return best;
+}
 size_t gmm_dw_map_bytes(int E, int lists) { return (size_t)lists * E * sizeof(CUtensorMap); }
 
-int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws,
-           int32_t* dev_status, int32_t* sched, cudaStream_t st) {
+int gmm_dw(const void* dy, const void* x, const Segments& sg, int d, int n, bool out_f32, void* dw, void* map_ws, float* parts,
+           int split, int32_t* dev_status, int32_t* sched, cudaStream_t st) {
   DwMaps mp = {};
   DwArgs ar = {};
   BaseMaps base = {};
   if (!make_mn_map(&base.m[0], dy, n, sg.rows, 0) || !make_mn_map(&base.m[1], x, d, sg.rows, 0) ||
-      !make_wide_map(&mp.o0, dw, d, (uint64_t)sg.E * n, out_f32 ? 4 : 2))
+      !make_wide_map(&mp.o0, split > 1 ? parts : dw, d, (uint64_t)split * sg.E * n, split > 1 || out_f32 ? 4 : 2))
     return note_cuda(cudaErrorInvalidValue);
-  const int rc = segment_maps(base, 2, sg, map_ws, sched, st);
+  int rc = segment_maps(base, 2, sg, map_ws, sched, st);
   if (rc != CAPMOE_OK) return rc;
-  ar.sg = sg; ar.out[0] = dw; ar.count = 1; ar.M[0] = n; ar.N[0] = d; ar.ia[0] = 0; ar.ib[0] = 1;
+  ar.sg = sg; ar.split = split; ar.out[0] = split > 1 ? parts : dw; ar.count = 1; ar.M[0] = n; ar.N[0] = d; ar.ia[0] = 0; ar.ib[0] = 1;
   ar.wide_a = mn_wide(n); ar.wide_b = mn_wide(d);
   ar.maps = (const CUtensorMap*)map_ws; ar.dev_status = dev_status; ar.sched = sched;
-  return out_f32 ? launch<float>(mp, ar, st) : launch<__nv_bfloat16>(mp, ar, st);
+  if (split == 1) return out_f32 ? launch<float>(mp, ar, st) : launch<__nv_bfloat16>(mp, ar, st);
+  if ((rc = launch<float>(mp, ar, st)) != CAPMOE_OK) return rc;
+  const int64_t size = (int64_t)sg.E * n * d;
+  if (out_f32) return join_parts<float>(parts, 1, {{(float*)dw}}, split, size, st);
+  return join_parts<__nv_bfloat16>(parts, 1, {{(__nv_bfloat16*)dw}}, split, size, st);
 }
 
 int gmm_dw_ffn_maps(const void* dg, const void* du, const void* dy, const void* x, const void* h, const Segments& sg, int d, int F,
@@ -316,15 +369,20 @@ int gmm_dw_ffn_maps(const void* dg, const void* du, const void* dy, const void* 
   return segment_maps(base, MAP_LISTS, sg, map_ws, nullptr, st);
 }
 
-int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd, const void* map_ws, int32_t* dev_status,
-               int32_t* sched, cudaStream_t st) {
+int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd, const void* map_ws, float* parts, int split,
+               int32_t* dev_status, int32_t* sched, cudaStream_t st) {
   DwMaps mp = {};
   DwArgs ar = {};
-  if (!make_wide_map(&mp.o0, dwg, d, (uint64_t)sg.E * F, 2) || !make_wide_map(&mp.o1, dwu, d, (uint64_t)sg.E * F, 2) ||
-      !make_wide_map(&mp.o2, dwd, F, (uint64_t)sg.E * d, 2))
+  const int64_t size = (int64_t)sg.E * F * d, step = split * size;
+  const bool f = split > 1;
+  void *o0 = f ? parts : dwg, *o1 = f ? parts + step : dwu, *o2 = f ? parts + 2 * step : dwd;
+  const uint64_t mats = (uint64_t)split * sg.E;
+  const int elt = f ? 4 : 2;
+  if (!make_wide_map(&mp.o0, o0, d, mats * F, elt) || !make_wide_map(&mp.o1, o1, d, mats * F, elt) ||
+      !make_wide_map(&mp.o2, o2, F, mats * d, elt))
     return note_cuda(cudaErrorInvalidValue);
-  ar.sg = sg; ar.count = 3;
-  ar.out[0] = dwg; ar.out[1] = dwu; ar.out[2] = dwd;
+  ar.sg = sg; ar.count = 3; ar.split = split;
+  ar.out[0] = o0; ar.out[1] = o1; ar.out[2] = o2;
   ar.M[0] = ar.M[1] = F; ar.M[2] = d;
   ar.N[0] = ar.N[1] = d; ar.N[2] = F;
   ar.ia[0] = 0; ar.ia[1] = 1; ar.ia[2] = 2;
@@ -332,7 +390,11 @@ int gmm_dw_ffn(const Segments& sg, int d, int F, void* dwg, void* dwu, void* dwd
   ar.wide_a = (mn_wide(F) ? 3 : 0) | (mn_wide(d) ? 4 : 0);
   ar.wide_b = (mn_wide(d) ? 3 : 0) | (mn_wide(F) ? 4 : 0);
   ar.maps = (const CUtensorMap*)map_ws; ar.dev_status = dev_status; ar.sched = sched;
-  return launch<__nv_bfloat16>(mp, ar, st);
+  if (!f) return launch<__nv_bfloat16>(mp, ar, st);
+  const int rc = launch<float>(mp, ar, st);
+  if (rc != CAPMOE_OK) return rc;
+  using B = __nv_bfloat16;
+  return join_parts<B>(parts, 3, {{(B*)dwg, (B*)dwu, (B*)dwd}}, split, size, st);
 }
 
 }  // namespace capmoe

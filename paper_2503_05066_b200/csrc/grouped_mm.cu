@@ -274,6 +274,12 @@ bool usable(P... p) {                       // every pointer there and 16-byte a
 }
 size_t align256(size_t b) { return (b + 255) / 256 * 256; }
 void* align256(void* p) { return (void*)align256((size_t)p); }
+// Parts of the weight gradients' reductions: all that pay when the workspace has room for them behind `parts`, else one.
+int split_that_fits(int64_t rows, int E, int d, int n, int products, const uint8_t* parts, const void* ws, size_t ws_bytes) {
+  const int split = gmm_dw_split(rows, E, d, n, products);
+  const size_t before = (size_t)(parts - (const uint8_t*)ws);
+  return before <= ws_bytes && gmm_dw_parts_bytes(E, d, n, products, split) <= ws_bytes - before ? split : 1;
+}
 
 }  // namespace
 }  // namespace capmoe
@@ -331,14 +337,25 @@ extern "C" int capmoe_grouped_mm_dw(const void* dy_rows, const void* x_rows, con
   if (ws_bytes < need) return CAPMOE_EWORKSPACE;
   const Segments sg{expert_offsets, E, (int)rows};
   cudaStream_t st = as_stream(stream);
-  if (gmm_supported(E, d, n, dtype))
-    return gmm_dw(dy_rows, x_rows, sg, d, n, out_dtype == CAPMOE_F32, dw, align256(ws), dev_status, counter_at(dev_status, 0), st);
+  if (gmm_supported(E, d, n, dtype)) {
+    uint8_t* maps = (uint8_t*)align256(ws);
+    uint8_t* parts = maps + align256(gmm_dw_map_bytes(E, 2));
+    return gmm_dw(dy_rows, x_rows, sg, d, n, out_dtype == CAPMOE_F32, dw, maps, (float*)parts,
+                  split_that_fits(rows, E, d, n, 1, parts, ws, ws_bytes), dev_status, counter_at(dev_status, 0), st);
+  }
   if (dtype == CAPMOE_F32)
     return dw_simt(DwSet<float, float>{{(const float*)dy_rows}, {(const float*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
   using B = __nv_bfloat16;
   if (out_dtype == CAPMOE_F32)
     return dw_simt(DwSet<B, float>{{(const B*)dy_rows}, {(const B*)x_rows}, {(float*)dw}, {n}, {d}}, 1, sg, st);
   return dw_simt(DwSet<B, B>{{(const B*)dy_rows}, {(const B*)x_rows}, {(B*)dw}, {n}, {d}}, 1, sg, st);
+}
+
+extern "C" int capmoe_dw_split_bytes(int64_t rows, int E, int d, int n, int dtype, int products, size_t* bytes) {
+  if (!bytes || rows < 0 || E < 1 || d < 1 || n < 1 || products < 1 || products > 3) return CAPMOE_EINVAL;
+  const int split = gmm_supported(E, d, n, dtype) ? gmm_dw_split(rows, E, d, n, products) : 1;
+  *bytes = split > 1 ? gmm_dw_parts_bytes(E, d, n, products, split) + 512 : 0;    // 512: to align the parts
+  return CAPMOE_OK;
 }
 
 extern "C" int capmoe_ffn_backward_workspace_bytes(int64_t A_max, int E, int F, int dtype, size_t* bytes) {
@@ -376,7 +393,9 @@ extern "C" int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_pe
       rc = gmm_hidden(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dg, du, h, dev_status, counter_at(dev_status, 0), true, st);
     if (rc == CAPMOE_OK) rc = gmm_dx2(dg, du, sg, d, F, w_gate, w_up, dx_perm, dev_status, counter_at(dev_status, 1), true, st);
     if (rc != CAPMOE_OK) return rc;
-    return gmm_dw_ffn(sg, d, F, dw_gate, dw_up, dw_down, maps, dev_status, counter_at(dev_status, 2), st);
+    uint8_t* parts = (uint8_t*)align256(h + A_max * F);
+    return gmm_dw_ffn(sg, d, F, dw_gate, dw_up, dw_down, maps, (float*)parts,
+                      split_that_fits(A_max, E, d, F, 3, parts, ws, ws_bytes), dev_status, counter_at(dev_status, 2), st);
   }
   if (dtype == CAPMOE_F32)
     return ffn_grad_simt<float>(x_perm, dy_perm, sg, d, F, w_gate, w_up, w_down, dx_perm, dw_gate, dw_up, dw_down, ws, st);

@@ -121,6 +121,32 @@ def test_weight_gradient_in_fp32(cm, d, n):
         R.close(dw[e], *R.product(dy[r].double().T, x[r].double().T, F32))
 
 
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("counts,d,n,in_parts", [([3000], 136, 72, True), ([700, 0, 5000], 264, 256, True), ([0, 9000], 512, 320, True),
+                                                 ([1, 1, 2600, 40], 64, 1032, False)])
+def test_weight_gradient_in_parts(cm, counts, d, n, in_parts, out_dtype):
+    """Few output tiles and long segments, on the average of the allocated rows: the sums are split into parts when the
+    workspace has room for them."""
+    off, A, rows, x, dy, _ = _case(counts, d, n, BF16)
+    extra = cm.dw_split_bytes(rows, len(counts), d, n, BF16)
+    assert extra >= 2 * 4 * len(counts) * d * n if in_parts else extra == 0
+    small = torch.empty(1 << 12, device="cuda", dtype=torch.uint8)
+    whole = cm.grouped_mm_dw(dy, x, off, out_dtype=out_dtype, dev_status=_block(cm), ws=small)
+    before = cm.launch_count()
+    split = cm.grouped_mm_dw(dy, x, off, out_dtype=out_dtype, dev_status=_block(cm))
+    assert cm.launch_count() - before == (3 if in_parts else 2)  # maps, products, the sum of the parts
+    assert torch.equal(split, cm.grouped_mm_dw(dy, x, off, out_dtype=out_dtype))
+    for e, r in _spans(counts):
+        want = R.product(dy[r].double().T, x[r].double().T, out_dtype)
+        R.close(split[e], *want)
+        R.close(whole[e], *want)
+
+
+def test_few_tiles_but_short_segments_are_not_split(cm):
+    assert cm.dw_split_bytes(900, 1, 256, 256, BF16) == 0 and cm.dw_split_bytes(1 << 20, 64, 2048, 1024, BF16) == 0
+    assert cm.dw_split_bytes(1 << 20, 1, 256, 256, F32) == 0
+
+
 def test_weight_gradient_with_no_rows_allocated(cm):
     x = torch.empty((0, 64), device="cuda", dtype=BF16)
     dy = torch.empty((0, 32), device="cuda", dtype=BF16)
@@ -170,6 +196,12 @@ def _check_ffn_gradient(cm, counts, d, F, dtype):
                                         ([1200, 0, 33], 136, 192)])
 def test_ffn_gradient(cm, counts, d, F, dtype):
     _check_ffn_gradient(cm, counts, d, F, dtype)
+
+
+@pytest.mark.parametrize("counts,d,F", [([2100], 136, 192), ([5, 4000], 256, 264)])
+def test_ffn_gradient_in_parts(cm, counts, d, F):
+    assert cm.dw_split_bytes(sum(counts) + 3, len(counts), d, F, BF16, products=3) > 0
+    _check_ffn_gradient(cm, counts, d, F, BF16)
 
 
 @pytest.mark.parametrize("counts,d,F", [([1], 1001, 33), ([2, 0, 5], 300, 70), ([33, 1], 515, 96), ([4], 70, 999)])
