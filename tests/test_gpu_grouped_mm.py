@@ -142,6 +142,30 @@ def test_weight_gradient_in_parts(cm, counts, d, n, in_parts, out_dtype):
         R.close(whole[e], *want)
 
 
+def test_parts_captured_and_replayed(cm):
+    """Split sums (bf16 parts in the workspace, fp32 clusters) in one graph, replayed after the offsets have moved."""
+    off, A, rows, x, dy, _ = _case([700, 0, 5000], 264, 256, BF16)
+    dy2, w2, off2 = _normal((9, 1021), 1.0, F32, 41), _normal((2, 37, 1021), 0.1, F32, 42), R.offsets_of([4, 5])
+
+    def calls():
+        return [cm.grouped_mm_dw(dy, x, off), cm.grouped_mm(dy2, off2, w2)]
+
+    calls()
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        got = calls()
+    off.copy_(R.offsets_of([2000, 3000, 700]))
+    off2.copy_(R.offsets_of([8, 1]))
+    torch.cuda.synchronize()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(got, calls()):
+        assert torch.equal(a, b)
+
+
 def test_few_tiles_but_short_segments_are_not_split(cm):
     assert cm.dw_split_bytes(900, 1, 256, 256, BF16) == 0 and cm.dw_split_bytes(1 << 20, 64, 2048, 1024, BF16) == 0
     assert cm.dw_split_bytes(1 << 20, 1, 256, 256, F32) == 0

@@ -133,3 +133,12 @@ def test_binding_checks_shapes_and_types(cm):
 def test_strided_offsets_are_refused(cm):
     with pytest.raises(AssertionError, match="contiguous"):
         cm.quantize_rows(torch.zeros((4, 64)), offsets=torch.zeros(10, dtype=torch.int32)[::2])
+
+
+def test_split_bytes_refuses_bad_sizes(cm):
+    out = ctypes.c_size_t(1)
+    good = dict(rows=I(1 << 20), E=2, d=512, n=512, dt=1, products=1)
+    for change in (dict(rows=I(-1)), dict(E=0), dict(d=0), dict(n=0), dict(products=0), dict(products=4)):
+        assert cm.lib().capmoe_dw_split_bytes(*{**good, **change}.values(), ctypes.byref(out)) == cm.EINVAL
+    assert cm.lib().capmoe_dw_split_bytes(*good.values(), None) == cm.EINVAL
+    assert cm.lib().capmoe_dw_split_bytes(*{**good, "d": 33}.values(), ctypes.byref(out)) == cm.OK and out.value == 0
