@@ -1,15 +1,17 @@
 // Plain-FMA tile product shared by the grouped products' fp32, odd-size and 8-bit fallback kernels:
-// C[TM, 64] += A[TM, K] B[64, K]^T with fp32 accumulation, operands read through small loader types that
+// C[TM, TN] += A[TM, K] B[TN, K]^T with fp32 accumulation, operands read through small loader types that
 // hide storage type, major order and block scales.
-// A block is G groups of 64 threads; a k-step is KG G long and each group multiplies its KG of it over the whole tile, a
-// thread with a TM/8 x 8 micro-tile (rows and columns 8 apart); the partial tiles are added in shared memory at the
-// end, in a fixed order.  What bounds it is latency: a k-step of two resident blocks takes about 2000 cycles, 1024 of them
+// 64-column tiles: a block is G groups of 64 threads; a k-step is KG G long and each group multiplies its KG of it over the
+// whole tile, a thread with a TM/8 x 8 micro-tile (rows and columns 8 apart); the partial tiles are added in shared memory
+// at the end, in a fixed order.  Many tiles: 128 x 128 by one group of 256 threads with 8 x 8 micro-tiles, four times the
+// FMAs between two barriers (0.52 of the FMA rate at 16,305 rows, 1000 x 1024; 0.42 with 64 x 64).
+// What bounds the small ones is latency: a k-step of two resident blocks takes about 2000 cycles, 1024 of them
 // FMA issue, in a call that lasts 8 of those and 6000 cycles around them.  Micro-tiles of 8 x 8 for 32-row tiles too (a
 // warp per group, a third fewer shared-memory reads) changed nothing or cost up to 8 %, packed pairs of FMAs 30 %.
 // The fp32 layers this serves have a few hundred tiles at most.  G = 4, two blocks to an SM, hides one block's latency
 // behind the other; when the tiles do not outnumber the SMs, G = 8 gives a tile a whole SM: of 124 blocks that could
-// share an SM the hardware puts two on some and none on others.  (1034 rows, 7 experts, 250 x 515 weights: y 13.9 us
-// with G = 4, 17.5 with 8; dx, 124 tiles, 28 and 17.5; with 64-row tiles 25 and 31.)
+// share an SM the hardware puts two on some and none on others.  (1034 rows, 7 experts, 250 x 515 weights: y 13.2 us
+// with G = 4, 17 with 8; dx, 124 tiles, 28 and 16.7; with 64-row tiles 25 and 31.)
 // An operand is staged as it lies in memory: [index][k] when k is contiguous, [k][index] otherwise.  fp32 operands come
 // in by cp.async, two or three k-steps ahead, in 16-byte pieces when their rows start on 16 bytes, else in 4-byte ones;
 // other types go through registers, one k-step ahead.  TM = 32 where 64-row tiles would leave SMs without one.
@@ -20,16 +22,21 @@
 namespace capmoe {
 namespace {
 
-constexpr int ST = 64;        // tile columns
+constexpr int ST = 64;        // columns of the smaller tiles
 // Geometry of a block: TM tile rows, G thread groups
-template <int TM_, int G_>
+template <int TM_, int G_, int TN_ = ST>
 struct Geo {
-  static constexpr int TM = TM_, G = G_;
-  static constexpr int KG = TM == 64 ? 4 : 8;       // a group's part of a k-step (eight spill the large micro-tile)
+  static constexpr int TM = TM_, TN = TN_, G = G_;
+  static constexpr int TG = TN == ST ? 64 : 256;    // threads of a group
+  static constexpr int KG = G == 1 ? 16 : TM == 64 ? 4 : 8;   // a group's part of a k-step (eight spill the large micro-tile)
   static constexpr int SK = KG * G;                 // k-step
-  static constexpr int SN = 64 * G;                 // threads
-  static constexpr int DEPTH = TM == 64 ? 4 : 3;    // k-steps in the ring
-  static constexpr int R = TM * ST / SN / 4;        // result elements of a thread: R x 4
+  static constexpr int SN = TG * G;                 // threads
+  static constexpr int BLOCKS = 512 / SN;           // resident blocks that registers are kept for
+  static constexpr int DEPTH = TM == 32 ? 3 : 4;    // k-steps in the ring
+  // a thread's micro-tile: MR rows, RS apart, by 8 columns, CS apart
+  static constexpr int RS = TN == ST ? 8 : 16, MR = TM / RS, CS = RS;
+  // result elements of a thread: R x C; with one group its micro-tile, else its share of the joined tile
+  static constexpr int C = G == 1 ? 8 : 4, R = TM * TN / SN / C;
   // floats of one k-step of an operand of W rows (columns): [W][SK + 4] or [SK][W + 4]; both row pitches are odd multiples
   // of 16 bytes
   static constexpr int staged(int W) { return W * (SK + 4) > SK * (W + 4) ? W * (SK + 4) : SK * (W + 4); }
@@ -61,7 +68,7 @@ struct Coded {
   }
 };
 
-template <class GE> struct alignas(16) SimtTile { float a[GE::DEPTH][GE::staged(GE::TM)], b[GE::DEPTH][GE::staged(ST)]; };
+template <class GE> struct alignas(16) SimtTile { float a[GE::DEPTH][GE::staged(GE::TM)], b[GE::DEPTH][GE::staged(GE::TN)]; };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const float* src, int valid) {    // valid: bytes that exist, the rest is zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
@@ -70,94 +77,102 @@ __device__ __forceinline__ void copy4(uint32_t dst, const float* src, int valid)
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
 }
 
-// A thread's share of staging an fp32 operand of W rows (columns), n of which exist: source addresses are worked out once
-// and advance by a k-step (the copies' address arithmetic cost twice the FMAs' instructions when done per copy).
+// A thread's share of staging an fp32 operand of W rows (columns), n of which exist: one address is worked out once and
+// advances by a k-step, the other copies of a step lie at equal distances from it (worked out per copy, the addresses cost
+// twice the FMAs' instructions; one held for each copy, the registers spill).
 template <class GE, int W, class L>
 struct Stager {
   static constexpr int SK = GE::SK, SN = GE::SN;
   static constexpr int N4 = W * SK / SN;           // 4-byte copies per thread and step
   static constexpr int N16 = (N4 + 3) / 4;         // 16-byte copies (of the first threads only if N4 < 4)
   static constexpr int V = SK / 4;                 // 16-byte pieces of a k-step of one row, k contiguous
-  const float* src[N4];
+  static constexpr int E16 = L::k_fast ? SN / V : SN / (W / 4), E4 = L::k_fast ? SN / SK : SN / W;   // rows (k) between two copies
+  const float *src, *base;                         // this thread's first copy of the step in hand; some valid address
+  int64_t between, step_len;
   uint32_t dst0, size;                             // size: per copy, 4-byte form a bit, 16-byte form the bytes inside (8 bits)
-  int64_t step_len;
-  int k, K;                                        // this thread's first k of the step in hand; end of the reduction
+  int left;                                        // reduction steps from this thread's first k on
   bool vec, idle;
-  __device__ __forceinline__ Stager(const L& l, int n, int K_, const float* ring) : K(K_) {
+  __device__ __forceinline__ Stager(const L& l, int n, int K, const float* ring) : base(l.p) {
     const int tid = threadIdx.x;
     vec = l.ld % 4 == 0 && ((uintptr_t)l.p & 15u) == 0;
     step_len = L::k_fast ? SK : SK * l.ld;
     size = 0;
     idle = vec && tid >= W * SK / 4;
     const int i0 = vec ? (L::k_fast ? tid / V : tid % (W / 4) * 4) : (L::k_fast ? tid / SK : tid % W);
-    k = vec ? (L::k_fast ? tid % V * 4 : tid / (W / 4)) : (L::k_fast ? tid % SK : tid / W);
+    const int k = vec ? (L::k_fast ? tid % V * 4 : tid / (W / 4)) : (L::k_fast ? tid % SK : tid / W);
     dst0 = (uint32_t)__cvta_generic_to_shared(ring) + 4u * (uint32_t)(L::k_fast ? i0 * (SK + 4) + k : k * (W + 4) + i0);
+    src = l.ptr(i0, k);                            // (used only where the element exists)
+    left = K - k;
+    between = (vec ? E16 : E4) * l.ld;
     if (vec) {
 #pragma unroll
       for (int e = 0; e < N16; ++e) {
-        const int i = L::k_fast ? i0 + e * (SN / V) : i0, kk = L::k_fast ? k : k + e * (SN / (W / 4));
+        const int i = L::k_fast ? i0 + e * E16 : i0;
         const int in = idle ? 0 : L::k_fast ? (i < n ? 4 : 0) : n - i;
-        const uint32_t bytes = in <= 0 ? 0u : in >= 4 ? 16u : 4u * (uint32_t)in;
-        size |= bytes << (8 * e);
-        src[e] = bytes ? l.ptr(i, kk) : l.p;
+        size |= (in <= 0 ? 0u : in >= 4 ? 16u : 4u * (uint32_t)in) << (8 * e);
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < N4; ++e) {
-        const int i = L::k_fast ? i0 + e * (SN / SK) : i0, kk = L::k_fast ? k : k + e * (SN / W);
-        const bool in = i < n;
-        size |= (uint32_t)in << e;
-        src[e] = in ? l.ptr(i, kk) : l.p;
-      }
+      for (int e = 0; e < N4; ++e) size |= (uint32_t)((L::k_fast ? i0 + e * E4 : i0) < n) << e;
     }
   }
   // copies the step in hand into the ring's buffer at byte offset `off` and moves on
   __device__ __forceinline__ void step(uint32_t off) {
+    const float* p = src;
     if (vec) {
       if (!idle) {
 #pragma unroll
         for (int e = 0; e < N16; ++e) {
           const uint32_t bytes = (size >> (8 * e)) & 255u;
-          const int left = K - (L::k_fast ? k : k + e * (SN / (W / 4)));
-          const uint32_t valid = L::k_fast ? (left <= 0 ? 0u : min(bytes, 4u * (uint32_t)min(left, 4))) : left > 0 ? bytes : 0u;
-          copy16(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * (SN / V) * (SK + 4) : e * (SN / (W / 4)) * (W + 4)), src[e], (int)valid);
-          if (bytes) src[e] += step_len;
+          const int l = left - (L::k_fast ? 0 : e * E16);
+          const uint32_t valid = L::k_fast ? (l <= 0 ? 0u : min(bytes, 4u * (uint32_t)min(l, 4))) : l > 0 ? bytes : 0u;
+          copy16(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * E16 * (SK + 4) : e * E16 * (W + 4)), valid ? p : base, (int)valid);
+          p += between;
         }
       }
     } else {
 #pragma unroll
       for (int e = 0; e < N4; ++e) {
-        const bool in = ((size >> e) & 1u) && k + (L::k_fast ? 0 : e * (SN / W)) < K;
-        copy4(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * (SN / SK) * (SK + 4) : e * (SN / W) * (W + 4)), src[e], in ? 4 : 0);
-        if ((size >> e) & 1u) src[e] += step_len;
+        const bool in = ((size >> e) & 1u) && left > (L::k_fast ? 0 : e * E4);
+        copy4(dst0 + off + 4u * (uint32_t)(L::k_fast ? e * E4 * (SK + 4) : e * E4 * (W + 4)), in ? p : base, in ? 4 : 0);
+        p += between;
       }
     }
-    k += SK;
+    left -= SK;
+    src += step_len;
   }
 };
 
 // Result element (i, j) of a thread, i < R, j < 4: row and column in the tile (a store's lanes write runs of 64 bytes; four
 // columns side by side in a thread, each stored by itself as rows of odd length want it, take four times the requests)
-template <class GE> __device__ __forceinline__ int out_row(int i) { return (int)(threadIdx.x >> 4) + (GE::SN / 16) * i; }
-__device__ __forceinline__ int out_col(int j) { return (int)(threadIdx.x & 15) + 16 * j; }
+template <class GE> __device__ __forceinline__ int micro_row(int tid) {       // first row (column) of a thread's micro-tile
+  return GE::TN == ST ? (tid >> 3) & 7 : (tid >> 6) * 4 + ((tid >> 3) & 3);
+}
+template <class GE> __device__ __forceinline__ int micro_col(int tid) { return GE::TN == ST ? tid & 7 : ((tid >> 5) & 1) * 8 + (tid & 7); }
+template <class GE> __device__ __forceinline__ int out_row(int i) {
+  return GE::G == 1 ? micro_row<GE>((int)threadIdx.x) + GE::RS * i : (int)(threadIdx.x >> 4) + (GE::SN / 16) * i;
+}
+template <class GE> __device__ __forceinline__ int out_col(int j) {
+  return GE::G == 1 ? micro_col<GE>((int)threadIdx.x) + GE::CS * j : (int)(threadIdx.x & 15) + 16 * j;
+}
 constexpr int CROW = ST + 8;                        // row of a partial tile
 
 // acc += A B^T over the tile; result elements at out_row / out_col
 template <class GE, class LA, class LB>
 __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int rows, int cols, int K, SimtTile<GE>& sm,
-                                             float (&acc)[GE::R][4]) {
-  constexpr int TM = GE::TM, SK = GE::SK, SN = GE::SN, SDEPTH = GE::DEPTH;
-  const int tid = threadIdx.x, tx = tid & 7, ty = (tid >> 3) & 7, group = tid >> 6;
-  constexpr int R = TM / 8;
+                                             float (&acc)[GE::R][GE::C]) {
+  constexpr int TM = GE::TM, TN = GE::TN, SK = GE::SK, SN = GE::SN, SDEPTH = GE::DEPTH;
+  const int tid = threadIdx.x, tx = micro_col<GE>(tid), ty = micro_row<GE>(tid), group = tid / GE::TG;
+  constexpr int R = GE::MR, RS = GE::RS, CS = GE::CS;
   constexpr bool ring = LA::direct && LB::direct;
-  static_assert(sizeof(SimtTile<GE>) >= 2 * TM * CROW * sizeof(float), "two partial tiles fit the staging buffers");
+  static_assert(GE::G == 1 || sizeof(SimtTile<GE>) >= 2 * TM * CROW * sizeof(float), "two partial tiles fit the staging buffers");
   if (K <= 0) return;
   const int steps = (K + SK - 1) / SK;
   float part[R][8];
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) part[i][j] = 0.f;
+    for (int j = 0; j < 8; ++j) part[i][j] = GE::G == 1 ? acc[i % GE::R][j % GE::C] : 0.f;
   auto multiply = [&](int buf) {
     const float *A = sm.a[buf], *B = sm.b[buf];
 #pragma unroll
@@ -166,24 +181,24 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
       if constexpr (LA::k_fast) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-          const float4 f = *reinterpret_cast<const float4*>(A + (ty + 8 * i) * (SK + 4) + k0);
+          const float4 f = *reinterpret_cast<const float4*>(A + (ty + RS * i) * (SK + 4) + k0);
           a[i][0] = f.x; a[i][1] = f.y; a[i][2] = f.z; a[i][3] = f.w;
         }
       } else {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-          for (int i = 0; i < R; ++i) a[i][kk] = A[(k0 + kk) * (TM + 4) + ty + 8 * i];
+          for (int i = 0; i < R; ++i) a[i][kk] = A[(k0 + kk) * (TM + 4) + ty + RS * i];
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float b[4];
         if constexpr (LB::k_fast) {
-          const float4 f = *reinterpret_cast<const float4*>(B + (tx + 8 * j) * (SK + 4) + k0);
+          const float4 f = *reinterpret_cast<const float4*>(B + (tx + CS * j) * (SK + 4) + k0);
           b[0] = f.x; b[1] = f.y; b[2] = f.z; b[3] = f.w;
         } else {
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) b[kk] = B[(k0 + kk) * (ST + 4) + tx + 8 * j];
+          for (int kk = 0; kk < 4; ++kk) b[kk] = B[(k0 + kk) * (TN + 4) + tx + CS * j];
         }
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
@@ -195,7 +210,7 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
   __syncthreads();                                  // an earlier product may still read the buffers
   if constexpr (ring) {
     Stager<GE, TM, LA> sa(la, rows, K, sm.a[0]);
-    Stager<GE, ST, LB> sb(lb, cols, K, sm.b[0]);
+    Stager<GE, TN, LB> sb(lb, cols, K, sm.b[0]);
     uint32_t buf = 0;                               // ring buffer of the next step to copy
     int left = steps;                               // steps not yet copied
     auto issue = [&]() {
@@ -217,12 +232,12 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
   } else {
-    constexpr int NA = TM * SK / SN, NB = ST * SK / SN;
+    constexpr int NA = TM * SK / SN, NB = TN * SK / SN;
     float ra[NA], rb[NB];
     auto a_k = [&](int x) { return LA::k_fast ? x % SK : x / TM; };
     auto a_i = [&](int x) { return LA::k_fast ? x / SK : x % TM; };
-    auto b_k = [&](int x) { return LB::k_fast ? x % SK : x / ST; };
-    auto b_i = [&](int x) { return LB::k_fast ? x / SK : x % ST; };
+    auto b_k = [&](int x) { return LB::k_fast ? x % SK : x / TN; };
+    auto b_i = [&](int x) { return LB::k_fast ? x / SK : x % TN; };
     auto fetch = [&](int k0) {
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
@@ -244,7 +259,7 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const int x = tid + i * SN;
-        sm.b[buf][LB::k_fast ? b_i(x) * (SK + 4) + b_k(x) : b_k(x) * (ST + 4) + b_i(x)] = rb[i];
+        sm.b[buf][LB::k_fast ? b_i(x) * (SK + 4) + b_k(x) : b_k(x) * (TN + 4) + b_i(x)] = rb[i];
       }
     };
     fetch(0);
@@ -256,6 +271,13 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
       if (step + 1 < steps) put((step + 1) & 1);    // last read two steps ago, before the previous barrier
       __syncthreads();
     }
+  }
+  if constexpr (GE::G == 1) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[i][j] = part[i][j];
+    return;
   }
   // the even and the odd groups, one after the other from the last to the first, in the staging buffers, then both sums
   __syncthreads();
@@ -277,7 +299,7 @@ __device__ __forceinline__ void tile_product(const LA& la, const LB& lb, int row
   for (int i = 0; i < GE::R; ++i) {
     const float* c0 = &sm.a[0][0] + out_row<GE>(i) * CROW;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] += c0[out_col(j)] + c0[TM * CROW + out_col(j)];
+    for (int j = 0; j < GE::C; ++j) acc[i][j] += c0[out_col<GE>(j)] + c0[TM * CROW + out_col<GE>(j)];
   }
 }
 
@@ -291,7 +313,7 @@ __device__ __forceinline__ Share share_of(int K) {
 // Joins the blocks' partial results through distributed shared memory, in the blocks' order: each block sums its part of the tile's rows from all of them.
 // False for a thread whose rows another block stores.  All threads of the cluster call it.
 template <class GE, int N>
-__device__ __forceinline__ bool join_shares(SimtTile<GE>& sm, float (&acc)[N][GE::R][4]) {
+__device__ __forceinline__ bool join_shares(SimtTile<GE>& sm, float (&acc)[N][GE::R][GE::C]) {
   const int S = (int)gridDim.z;
   if (GE::R > 1 || S == 1) return true;             // only the smallest geometry is split
   static_assert(GE::R > 1 || sizeof(SimtTile<GE>) >= N * GE::TM * ST * sizeof(float), "the partial results fit the staging buffers");
@@ -303,7 +325,7 @@ __device__ __forceinline__ bool join_shares(SimtTile<GE>& sm, float (&acc)[N][GE
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) C[n * GE::TM * ST + out_col(j)] = acc[n][0][j];
+    for (int j = 0; j < 4; ++j) C[n * GE::TM * ST + out_col<GE>(j)] = acc[n][0][j];
   cluster.sync();
   const bool mine = row * S / GE::TM == (int)blockIdx.z;
   if (mine) {
@@ -313,7 +335,7 @@ __device__ __forceinline__ bool join_shares(SimtTile<GE>& sm, float (&acc)[N][GE
       for (int z = 0; z < S; ++z) {
         const float* p = cluster.map_shared_rank(C + n * GE::TM * ST, z);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] += p[out_col(j)];
+        for (int j = 0; j < 4; ++j) s[j] += p[out_col<GE>(j)];
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[n][0][j] = s[j];
@@ -323,12 +345,12 @@ __device__ __forceinline__ bool join_shares(SimtTile<GE>& sm, float (&acc)[N][GE
   return mine;
 }
 
-template <int R>
-__device__ __forceinline__ void clear_acc(float (&acc)[R][4]) {
+template <int R, int C>
+__device__ __forceinline__ void clear_acc(float (&acc)[R][C]) {
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+    for (int j = 0; j < C; ++j) acc[i][j] = 0.f;
 }
 
 template <class GE>

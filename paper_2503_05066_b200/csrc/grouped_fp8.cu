@@ -186,7 +186,7 @@ k_mm_fp8(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, const u
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = out_row<G8>(i), c = col0 + out_col(j);
+      const int r = out_row<G8>(i), c = col0 + out_col<G8>(j);
       float v = acc[i][j];
       if (SWIGLU) v = v / (1.0f + expf(-v)) * up[i][j];
       if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<TO>(v);

@@ -15,17 +15,17 @@ namespace {
 enum { DIR_FWD = 0, DIR_DX = 1 };
 
 template <typename T, int DIR, class GE>
-__global__ void __launch_bounds__(GE::SN, 8 / GE::G)
+__global__ void __launch_bounds__(GE::SN, GE::BLOCKS)
 k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out, Segments sg, int K, int Nout) {
   wait_for_previous_kernel();
   SimtTile<GE>& sm = simt_tile<GE>();
   RowTile t;
   if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
-  const int col0 = blockIdx.y * ST;
+  const int col0 = blockIdx.y * GE::TN;
   const T* We = W + (int64_t)t.e * Nout * K;
   constexpr int R = GE::R;
   const Share k = share_of(K);
-  float acc[1][R][4];
+  float acc[1][R][GE::C];
   clear_acc(acc[0]);
   const Dense<T, true> la{A + (int64_t)t.row0 * K + k.k0, K};
   if (DIR == DIR_FWD) tile_product<GE>(la, Dense<T, true>{We + (int64_t)col0 * K + k.k0, K}, t.rows, Nout - col0, k.len, sm, acc[0]);
@@ -34,8 +34,8 @@ k_mm_rows(const T* __restrict__ A, const T* __restrict__ W, T* __restrict__ out,
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = out_row<GE>(i), c = col0 + out_col(j);
+    for (int j = 0; j < GE::C; ++j) {
+      const int r = out_row<GE>(i), c = col0 + out_col<GE>(j);
       if (r < t.rows && c < Nout) out[(int64_t)(t.row0 + r) * Nout + c] = from_float<T>(acc[0][i][j]);
     }
 }
@@ -49,29 +49,29 @@ struct DwSet { const T* P[3]; const T* Q[3]; TO* out[3]; int M[3], N[3]; };
 // experts, 512 x 512, fp32: 34 us with 1 row, 43 with 4, 58 with 8, 79 with 12; staged 60, 60, 61, 62).
 constexpr int DW_DIRECT = 8;
 template <typename T, typename TO, class GE>
-__global__ void __launch_bounds__(GE::SN, 8 / GE::G) k_mm_dw(DwSet<T, TO> s, Segments sg) {
+__global__ void __launch_bounds__(GE::SN, GE::BLOCKS) k_mm_dw(DwSet<T, TO> s, Segments sg) {
   wait_for_previous_kernel();
   SimtTile<GE>& sm = simt_tile<GE>();
   const int p = blockIdx.z / sg.E, e = blockIdx.z - p * sg.E;
   const int M = s.M[p], N = s.N[p];
-  const int r0 = blockIdx.x * GE::TM, c0 = blockIdx.y * ST;
+  const int r0 = blockIdx.x * GE::TM, c0 = blockIdx.y * GE::TN;
   if (r0 >= M || c0 >= N) return;
   const int begin = seg_at(sg, e), n = seg_at(sg, e + 1) - begin;
   constexpr int R = GE::R;
-  float acc[R][4];
+  float acc[R][GE::C];
   clear_acc(acc);
   const Dense<T, false> P{s.P[p] + (int64_t)begin * M + r0, M}, Q{s.Q[p] + (int64_t)begin * N + c0, N};
   if (n <= DW_DIRECT) {
     for (int k = 0; k < n; ++k) {
-      float a[R], b[4];
+      float a[R], b[GE::C];
 #pragma unroll
       for (int i = 0; i < R; ++i) a[i] = r0 + out_row<GE>(i) < M ? P.at(out_row<GE>(i), k) : 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[j] = c0 + out_col(j) < N ? Q.at(out_col(j), k) : 0.f;
+      for (int j = 0; j < GE::C; ++j) b[j] = c0 + out_col<GE>(j) < N ? Q.at(out_col<GE>(j), k) : 0.f;
 #pragma unroll
       for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        for (int j = 0; j < GE::C; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
     }
   } else {
     tile_product<GE>(P, Q, M - r0, N - c0, n, sm, acc);
@@ -79,15 +79,15 @@ __global__ void __launch_bounds__(GE::SN, 8 / GE::G) k_mm_dw(DwSet<T, TO> s, Seg
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = r0 + out_row<GE>(i), c = c0 + out_col(j);
+    for (int j = 0; j < GE::C; ++j) {
+      const int r = r0 + out_row<GE>(i), c = c0 + out_col<GE>(j);
       if (r < M && c < N) s.out[p][((int64_t)e * M + r) * N + c] = from_float<TO>(acc[i][j]);
     }
 }
 
 // dg, du and h of the SwiGLU backward pass: three products over d with the elementwise part in registers.
 template <typename T, class GE>
-__global__ void __launch_bounds__(GE::SN, 8 / GE::G)
+__global__ void __launch_bounds__(GE::SN, GE::BLOCKS)
 k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __restrict__ wg, const T* __restrict__ wu,
                   const T* __restrict__ wd, T* __restrict__ dg, T* __restrict__ du, T* __restrict__ h, Segments sg, int d,
                   int F) {
@@ -95,12 +95,12 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
   SimtTile<GE>& sm = simt_tile<GE>();
   RowTile t;
   if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
-  const int col0 = blockIdx.y * ST, cols = F - col0;
+  const int col0 = blockIdx.y * GE::TN, cols = F - col0;
   const int64_t we = (int64_t)t.e * F * d;
   const Share k = share_of(d);
   const int64_t at = (int64_t)t.row0 * d + k.k0, wat = we + (int64_t)col0 * d + k.k0;
   constexpr int R = GE::R;
-  float acc[3][R][4];                               // g, u, dh
+  float acc[3][R][GE::C];                               // g, u, dh
   clear_acc(acc[0]); clear_acc(acc[1]); clear_acc(acc[2]);
   tile_product<GE>(Dense<T, true>{x + at, d}, Dense<T, true>{wg + wat, d}, t.rows, cols, k.len, sm, acc[0]);
   tile_product<GE>(Dense<T, true>{x + at, d}, Dense<T, true>{wu + wat, d}, t.rows, cols, k.len, sm, acc[1]);
@@ -109,8 +109,8 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = out_row<GE>(i), c = col0 + out_col(j);
+    for (int j = 0; j < GE::C; ++j) {
+      const int r = out_row<GE>(i), c = col0 + out_col<GE>(j);
       if (r >= t.rows || c >= F) continue;
       const float gv = acc[0][i][j], uv = acc[1][i][j], dhv = acc[2][i][j];
       const float p = 1.0f / (1.0f + expf(-gv));
@@ -124,18 +124,18 @@ k_ffn_grad_hidden(const T* __restrict__ x, const T* __restrict__ dy, const T* __
 
 // dx = dg W_g + du W_u (weights [E, F, d])
 template <typename T, class GE>
-__global__ void __launch_bounds__(GE::SN, 8 / GE::G)
+__global__ void __launch_bounds__(GE::SN, GE::BLOCKS)
 k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __restrict__ wg, const T* __restrict__ wu,
              T* __restrict__ dx, Segments sg, int d, int F) {
   wait_for_previous_kernel();
   SimtTile<GE>& sm = simt_tile<GE>();
   RowTile t;
   if (!find_row_tile<GE>(sg, blockIdx.x, t)) return;
-  const int col0 = blockIdx.y * ST;
+  const int col0 = blockIdx.y * GE::TN;
   const Share k = share_of(F);
   const int64_t at = (int64_t)t.row0 * F + k.k0, we = (int64_t)t.e * F * d + (int64_t)k.k0 * d + col0;
   constexpr int R = GE::R;
-  float acc[1][R][4];
+  float acc[1][R][GE::C];
   clear_acc(acc[0]);
   tile_product<GE>(Dense<T, true>{dg + at, F}, Dense<T, false>{wg + we, d}, t.rows, d - col0, k.len, sm, acc[0]);
   tile_product<GE>(Dense<T, true>{du + at, F}, Dense<T, false>{wu + we, d}, t.rows, d - col0, k.len, sm, acc[0]);
@@ -143,8 +143,8 @@ k_ffn_grad_x(const T* __restrict__ dg, const T* __restrict__ du, const T* __rest
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = out_row<GE>(i), c = col0 + out_col(j);
+    for (int j = 0; j < GE::C; ++j) {
+      const int r = out_row<GE>(i), c = col0 + out_col<GE>(j);
       if (r < t.rows && c < d) dx[(int64_t)(t.row0 + r) * d + c] = from_float<T>(acc[0][i][j]);
     }
 }
@@ -176,13 +176,16 @@ int launch_tiles(void (*kernel)(KArgs...), dim3 grid, int split, cudaStream_t st
   return launched(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
 }
 
-dim3 row_grid(const Segments& sg, int cols, int tm, int split) {       // every segment rounds up to whole tiles
-  return dim3((unsigned)(ceil_div(sg.rows, tm) + sg.E), (unsigned)ceil_div(cols, ST), (unsigned)split);
+template <class GE>
+dim3 row_grid(const Segments& sg, int cols, int split) {       // every segment rounds up to whole tiles
+  return dim3((unsigned)(ceil_div(sg.rows, GE::TM) + sg.E), (unsigned)ceil_div(cols, GE::TN), (unsigned)split);
 }
-// Geometry by the number of tiles: from `large` 64 x 64 ones per SM on, those; else 32-row ones, whose block gets an SM to
+// Geometry by the number of tiles.  128 x 128 tiles when BIG_MIN whole ones per SM exist and the segments fill them (16,305
+// rows of 8 experts, 1000 x 1024: y 870 us, dx 885, with 64 x 64 tiles 1070 and 1111; 2919 rows of 8, 848 x 862, with 1 or 2
+// per SM: 215 us against 145).  From `large` 64 x 64 ones per SM on, those; else 32-row ones, whose block gets an SM to
 // itself when they do not outnumber the SMs (see gmm_simt.cuh; FFN gradients of 236 rows of 45 experts, 41 x 415: 74 us
 // with two blocks to an SM, 90 with one).
-enum Size { LARGE, MEDIUM, SMALL };
+enum Size { BIG, LARGE, MEDIUM, SMALL };
 Size size_of(int64_t tiles64, int64_t tiles32, int large = 2) {
   return tiles64 >= large * sm_count() ? LARGE : tiles32 > sm_count() ? MEDIUM : SMALL;
 }
@@ -191,57 +194,62 @@ Size size_of(int64_t tiles64, int64_t tiles32, int large = 2) {
 // SPLIT_MIN steps the reduction is split.
 struct Plan { Size size; int split; };
 constexpr int SPLIT_MIN = 32;
+constexpr int BIG_MIN = 2;
 Plan plan_rows(const Segments& sg, int cols, int K) {
   const int64_t used = ((sg.E < sg.rows ? sg.E : sg.rows) * 3 + 3) / 4, nc = ceil_div(cols, ST);
   const int64_t t32 = ceil_div(sg.rows, 32) + used / 2, tiles32 = (t32 > used ? t32 : used) * nc;
   Plan p = {size_of(ceil_div(sg.rows, ST) * nc, tiles32), 1};
+  if (sg.rows / sg.E >= 128 && (int64_t)(sg.rows / 128) * (cols / 128) >= BIG_MIN * sm_count()) p.size = BIG;
   if (p.size == SMALL)
     while (p.split < 8 && tiles32 * p.split * 2 <= sm_count() && K >= p.split * 2 * SPLIT_MIN) p.split *= 2;
   return p;
 }
+using Big = Geo<128, 1, 128>;
 using Large = Geo<64, 4>;
 using Medium = Geo<32, 4>;
 using Small = Geo<32, 8>;
 
 template <typename T, int DIR, class GE>
 int rows_run(const T* a, const T* w, T* out, const Segments& sg, int K, int Nout, int split, cudaStream_t st) {
-  return launch_tiles<GE>(k_mm_rows<T, DIR, GE>, row_grid(sg, Nout, GE::TM, split), split, st, a, w, out, sg, K, Nout);
+  return launch_tiles<GE>(k_mm_rows<T, DIR, GE>, row_grid<GE>(sg, Nout, split), split, st, a, w, out, sg, K, Nout);
 }
 template <typename T, int DIR>
 int rows_simt(const void* a, const void* w, void* out, const Segments& sg, int K, int Nout, cudaStream_t st) {
   const Plan p = plan_rows(sg, Nout, K);
-  auto run = p.size == LARGE ? rows_run<T, DIR, Large> : p.size == MEDIUM ? rows_run<T, DIR, Medium> : rows_run<T, DIR, Small>;
+  auto run = p.size == BIG ? rows_run<T, DIR, Big> : p.size == LARGE ? rows_run<T, DIR, Large> : p.size == MEDIUM ? rows_run<T, DIR, Medium> : rows_run<T, DIR, Small>;
   return run((const T*)a, (const T*)w, (T*)out, sg, K, Nout, p.split, st);
 }
 
 template <typename T, typename TO, class GE>
 int dw_run(const DwSet<T, TO>& s, int M, int N, unsigned z, const Segments& sg, cudaStream_t st) {
-  return launch_tiles<GE>(k_mm_dw<T, TO, GE>, dim3((unsigned)ceil_div(M, GE::TM), (unsigned)ceil_div(N, ST), z), 1, st, s, sg);
+  return launch_tiles<GE>(k_mm_dw<T, TO, GE>, dim3((unsigned)ceil_div(M, GE::TM), (unsigned)ceil_div(N, GE::TN), z), 1, st, s, sg);
 }
 template <typename T, typename TO>
 int dw_simt(const DwSet<T, TO>& s, int count, const Segments& sg, cudaStream_t st) {
   int M = 0, N = 0;
-  int64_t tiles = 0;
+  int64_t tiles = 0, big = 0;
   for (int p = 0; p < count; ++p) {
     M = s.M[p] > M ? s.M[p] : M;
     N = s.N[p] > N ? s.N[p] : N;
     tiles += ceil_div(s.M[p], ST) * ceil_div(s.N[p], ST) * sg.E;
+    big += (int64_t)(s.M[p] / 128) * (s.N[p] / 128) * sg.E;
   }
   // short sums: 64-row tiles from one per SM on (871 rows of 8 experts, 512 x 256: 12.5 us, 14.3 with 32-row tiles)
-  const Size z = size_of(tiles, 2 * tiles, 1);
-  auto run = z == LARGE ? dw_run<T, TO, Large> : z == MEDIUM ? dw_run<T, TO, Medium> : dw_run<T, TO, Small>;
+  Size z = size_of(tiles, 2 * tiles, 1);
+  if (sg.rows / sg.E >= 64 && big >= BIG_MIN * sm_count()) z = BIG;
+  auto run = z == BIG ? dw_run<T, TO, Big> : z == LARGE ? dw_run<T, TO, Large> : z == MEDIUM ? dw_run<T, TO, Medium> : dw_run<T, TO, Small>;
   return run(s, M, N, (unsigned)(count * sg.E), sg, st);
 }
 
 template <typename T, class GE>
 int hidden_run(const T* x, const T* dy, const T* wg, const T* wu, const T* wd, T* dg, T* du, T* h, const Segments& sg, int d, int F,
                int split, cudaStream_t st) {
-  return launch_tiles<GE>(k_ffn_grad_hidden<T, GE>, row_grid(sg, F, GE::TM, split), split, st, x, dy, wg, wu, wd, dg, du, h, sg, d, F);
+  return launch_tiles<GE>(k_ffn_grad_hidden<T, GE>, row_grid<GE>(sg, F, split), split, st, x, dy, wg, wu, wd, dg, du, h, sg, d, F);
 }
 template <typename T, class GE>
 int dx2_run(const T* dg, const T* du, const T* wg, const T* wu, T* dx, const Segments& sg, int d, int F, int split,
             cudaStream_t st) {
-  return launch_tiles<GE>(k_ffn_grad_x<T, GE>, row_grid(sg, d, GE::TM, split), split, st, dg, du, wg, wu, dx, sg, d, F);
+  return launch_tiles<GE>(k_ffn_grad_x<T, GE>, row_grid<GE>(sg, d, split), split, st, dg, du, wg, wu, dx, sg, d, F);
 }
 template <typename T>
 int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int F, const void* w_gate, const void* w_up,
@@ -251,8 +259,8 @@ int ffn_grad_simt(const void* x, const void* dy, const Segments& sg, int d, int 
   T* h = du + (int64_t)sg.rows * F;
   const T *wg = (const T*)w_gate, *wu = (const T*)w_up, *wd = (const T*)w_down;
   const Plan ph = plan_rows(sg, F, d), px = plan_rows(sg, d, F);
-  auto hidden = ph.size == LARGE ? hidden_run<T, Large> : ph.size == MEDIUM ? hidden_run<T, Medium> : hidden_run<T, Small>;
-  auto dx2 = px.size == LARGE ? dx2_run<T, Large> : px.size == MEDIUM ? dx2_run<T, Medium> : dx2_run<T, Small>;
+  auto hidden = ph.size <= LARGE ? hidden_run<T, Large> : ph.size == MEDIUM ? hidden_run<T, Medium> : hidden_run<T, Small>;
+  auto dx2 = px.size == BIG ? dx2_run<T, Big> : px.size == LARGE ? dx2_run<T, Large> : px.size == MEDIUM ? dx2_run<T, Medium> : dx2_run<T, Small>;
   int rc = hidden((const T*)x, (const T*)dy, wg, wu, wd, dg, du, h, sg, d, F, ph.split, st);
   if (rc == CAPMOE_OK) rc = dx2(dg, du, wg, wu, (T*)dx, sg, d, F, px.split, st);
   if (rc != CAPMOE_OK) return rc;

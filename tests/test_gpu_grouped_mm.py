@@ -98,6 +98,14 @@ def test_many_segments_fp32(cm):
     _check_all(cm, COUNTS["many"], 40, 72, F32)
 
 
+@pytest.mark.parametrize("counts,d,n,dtype", [([1300, 0, 1270, 10], 37, 1921, F32), ([1300, 0, 1270, 10], 1921, 37, F32),
+                                              ([1300, 0, 1270, 10], 64, 1924, F32), ([70, 0, 200], 1300, 1301, F32),
+                                              ([1300, 0, 1270, 10], 37, 1921, BF16), ([70, 0, 200], 1301, 1300, BF16)])
+def test_large_tiles_of_the_fma_kernels(cm, counts, d, n, dtype):
+    """So many 128 x 128 tiles that one direction's product runs on them (fp32, and bf16 of odd sizes)."""
+    _check_all(cm, counts, d, n, dtype)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("counts,d,n", [([1], 1021, 37), ([3, 0, 1], 64, 1001), ([2, 5], 511, 130), ([1, 40], 65, 300), ([7], 4099, 5)])
 def test_few_rows_with_long_sums(cm, counts, d, n, dtype):
@@ -226,6 +234,11 @@ def test_ffn_gradient(cm, counts, d, F, dtype):
 def test_ffn_gradient_in_parts(cm, counts, d, F):
     assert cm.dw_split_bytes(sum(counts) + 3, len(counts), d, F, BF16, products=3) > 0
     _check_ffn_gradient(cm, counts, d, F, BF16)
+
+
+@pytest.mark.parametrize("counts,d,F", [([1300, 0, 1270, 10], 1921, 37), ([70, 0, 200], 1285, 650)])
+def test_ffn_gradient_of_large_fp32_tiles(cm, counts, d, F):
+    _check_ffn_gradient(cm, counts, d, F, F32)
 
 
 @pytest.mark.parametrize("counts,d,F", [([1], 1001, 33), ([2, 0, 5], 300, 70), ([33, 1], 515, 96), ([4], 70, 999)])
