@@ -168,6 +168,28 @@ __device__ __forceinline__ void load_mn(uint32_t dst, const CUtensorMap* m, bool
   }
 }
 
+// ---------------------------------------------------------------- signals between the CTAs of a pair
+__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// mbar_wait for a barrier that the peer CTA arrives on with release semantics (acquire at cluster scope; a separate
+// fence on the MMA thread costs about a microsecond per scale group)
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
+}
+
 // ---------------------------------------------------------------- tile ring
 // One thread of its own warp (the scheduler) picks a CTA's tiles, works out where they lie and hands each on as a record of
 // eight ints through a ring in shared memory; the other roles only read records.  The first tile of a pair is its
@@ -225,16 +247,19 @@ struct TileRing {
         if (leader) {
           tile = npairs + claim;
           if (tile < tile_hi) claim = atomicAdd(counter, 1);
-          if (!mbar_wait(xempty(q), (use & 1u) ^ 1u, abort_flag)) return;
+          if (!mbar_wait_cluster(xempty(q), (use & 1u) ^ 1u, abort_flag)) return;
           const uint32_t pfull = peer_addr(xfull(q));
           asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(pfull), "r"(4u) : "memory");
           asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];"
                        ::"r"(peer_addr(xval(q))), "r"((uint32_t)tile), "r"(pfull)
                        : "memory");
         } else {
-          if (!mbar_wait(xfull(q), use & 1u, abort_flag)) return;
+          // Cluster scope throughout, and the value read before the slot is given back: with waits and arrivals of CTA scope
+          // (the default) a pair took different tiles once in a million hand-overs, where many tiles are empty sums.
+          if (!mbar_wait_cluster(xfull(q), use & 1u, abort_flag)) return;
           asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tile) : "r"(xval(q)) : "memory");
-          mbar_arrive_cluster(xempty(q) & PEER_MASK);
+          asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          mbar_arrive_release_cluster(xempty(q) & PEER_MASK);
         }
       }
       int4 a = make_int4(-1, 0, 0, 0), b = make_int4(0, 0, 0, 0);
@@ -298,27 +323,6 @@ __device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t saddr) {
 __device__ __forceinline__ void umma2_commit_own(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// mbar_wait for a barrier that the peer CTA arrives on with release semantics (acquire at cluster scope; a separate
-// fence on the MMA thread costs about a microsecond per scale group)
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait_cluster(bar, parity)) return true;
-  return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
-}
-
 // Scale bytes k .. k + 15 of a row of nb (four scale groups): one 16-byte load where rows start on 16 bytes, else the
 // aligned words that hold a byte of the row, shifted into place.  Bytes behind the row are whatever lies there: no k-block
 // asks for them.
