@@ -168,28 +168,6 @@ __device__ __forceinline__ void load_mn(uint32_t dst, const CUtensorMap* m, bool
   }
 }
 
-// ---------------------------------------------------------------- signals between the CTAs of a pair
-__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// mbar_wait for a barrier that the peer CTA arrives on with release semantics (acquire at cluster scope; a separate
-// fence on the MMA thread costs about a microsecond per scale group)
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait_cluster(bar, parity)) return true;
-  return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
-}
-
 // ---------------------------------------------------------------- tile ring
 // One thread of its own warp (the scheduler) picks a CTA's tiles, works out where they lie and hands each on as a record of
 // eight ints through a ring in shared memory; the other roles only read records.  The first tile of a pair is its
@@ -254,12 +232,9 @@ struct TileRing {
                        ::"r"(peer_addr(xval(q))), "r"((uint32_t)tile), "r"(pfull)
                        : "memory");
         } else {
-          // Cluster scope throughout, and the value read before the slot is given back: with waits and arrivals of CTA scope
-          // (the default) a pair took different tiles once in a million hand-overs, where many tiles are empty sums.
           if (!mbar_wait_cluster(xfull(q), use & 1u, abort_flag)) return;
           asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tile) : "r"(xval(q)) : "memory");
-          asm volatile("fence.acq_rel.cluster;" ::: "memory");
-          mbar_arrive_release_cluster(xempty(q) & PEER_MASK);
+          give_back_slot(xempty(q));
         }
       }
       int4 a = make_int4(-1, 0, 0, 0), b = make_int4(0, 0, 0, 0);

@@ -198,6 +198,34 @@ constexpr uint32_t PEER_MASK = 0xFEFFFFFFu;                // shared::cluster ad
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// mbar_wait for a barrier that the peer CTA arrives on with release semantics (acquire at cluster scope; a separate
+// fence on the MMA thread costs about a microsecond per scale group)
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
+}
+// Gives a slot that the even CTA fills by st.async back to it, after this thread (and the lanes of its warp, behind a
+// __syncwarp) have read the value: the read must be over, at cluster scope, before the next value may be sent.  With
+// arrivals of CTA scope (the default) CTAs of a pair were seen to take different tiles, about once in a million
+// hand-overs of a two-deep mailbox between tiles that are empty sums.
+__device__ __forceinline__ void give_back_slot(uint32_t bar) {
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  mbar_arrive_release_cluster(bar & PEER_MASK);
+}
 // Tile queue of a CTA or a CTA pair.  With a scheduler counter the CTAs do not walk fixed lists of
 // tiles: the (leader's) producer thread takes the next tile index from a global counter shortly
 // before it needs it and hands it to every role (of both CTAs) through a small ring in shared
@@ -224,7 +252,8 @@ struct TileQueue {
   // leader's producer thread: publish tile (or -1 = no more) as entry q; false if a wait ran out
   __device__ __forceinline__ bool put(int q, int tile) const {
     const uint32_t par = (((uint32_t)q / TQ) & 1u) ^ 1u;
-    if (!mbar_wait(empty(q), par, abort_flag)) return false;     // only the count matters here
+    // all readers of the slot's last entry are done with it, the peer's at cluster scope
+    if (!(PAIRED ? mbar_wait_cluster(empty(q), par, abort_flag) : mbar_wait(empty(q), par, abort_flag))) return false;
     asm volatile("st.shared.u32 [%0], %1;" ::"r"(val(q)), "r"((uint32_t)tile) : "memory");
     mbar_arrive(full(q));
     if constexpr (PAIRED) {
@@ -241,15 +270,16 @@ struct TileQueue {
   // any other role (one thread, or one whole warp): entry q, or -2 if the wait ran out
   __device__ __forceinline__ int get(int q, bool whole_warp) const {
     const uint32_t par = ((uint32_t)q / TQ) & 1u;
-    bool ok = mbar_wait(full(q), par, abort_flag);
+    const bool remote = PAIRED && rank != 0;                      // the entry comes from the other CTA
+    bool ok = remote ? mbar_wait_cluster(full(q), par, abort_flag) : mbar_wait(full(q), par, abort_flag);
     if (whole_warp) ok = __all_sync(0xffffffffu, ok);
     if (!ok) return -2;
     uint32_t v;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(val(q)) : "memory");
     if (whole_warp) __syncwarp();
     if (!whole_warp || (threadIdx.x & 31) == 0) {
-      if (!PAIRED || rank == 0) mbar_arrive(empty(q));
-      else mbar_arrive_cluster(empty(q) & PEER_MASK);
+      if (remote) give_back_slot(empty(q));
+      else mbar_arrive(empty(q));
     }
     return (int)v;
   }
