@@ -292,7 +292,7 @@ int capmoe_grouped_ffn_segments(const void* x_rows, const int32_t* seg_begin, co
  * there are few output tiles and long segments (0 bytes when that would not help).
  * Outputs and workspace overlap neither each other nor an input.
  * bf16 with d and n (F) multiples of 8 runs on tensor cores (TMA-fed tiles, fp32 accumulators); fp32 and other
- * sizes run plain fp32-FMA kernels.  dev_status as in capmoe_grouped_ffn.  E <= 256, rows < 2^31. */
+ * sizes run plain fp32-FMA kernels.  dev_status as in capmoe_grouped_ffn.  E <= 256, rows <= 2^31 - 512. */
 int capmoe_grouped_mm(const void* x_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n, int dtype,
                       void* y, int64_t rows, int32_t* dev_status, void* stream);
 int capmoe_grouped_mm_dx(const void* dy_rows, const int32_t* expert_offsets, const void* w, int E, int d, int n, int dtype,

@@ -5,6 +5,8 @@
 namespace capmoe {
 
 constexpr int GMM_MAX_E = 256;               // segments per call (the kernels keep their bounds in shared memory)
+// Row counts are rounded up to whole tiles (256 rows) and row numbers run up to a tile past the last row, in 32 bits.
+constexpr int64_t GMM_MAX_ROWS = ((int64_t)1 << 31) - 512;
 constexpr int QBLOCK = 128;                  // columns (and, for weights, rows) that share one scale
 constexpr int Q_NAN_SCALE = 255;             // scale code of a block that holds a NaN or an infinity
 

@@ -280,7 +280,7 @@ k_gmm_rows(const __grid_constant__ TMaps mp, const __grid_constant__ TArgs ar) {
         while (tile >= tile_start[cursor + 1]) ++cursor;
         const int local = tile - tile_start[cursor], cnt = ends[cursor] - offs[cursor];
         const int ntb = (cnt + tt - 1) / tt;
-        const int per = ((cnt + ntb - 1) / ntb + 15) & ~15;              // equal token blocks of whole MMA steps
+        const int per = (cnt / ntb + (cnt % ntb != 0) + 15) & ~15;       // equal token blocks of whole MMA steps (cnt + ntb may pass 2^31)
         const int wb = local / ntb, r0 = (local - wb * ntb) * per;
         const int rows = min(per, cnt - r0);                             // at least one: (ntb - 1) * per < cnt
         a = make_int4(cursor, offs[cursor] + r0, rows, (rows + 15) & ~15);

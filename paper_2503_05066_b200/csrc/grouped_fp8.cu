@@ -241,7 +241,7 @@ int launch_tiles(void (*kernel)(KArgs...), const Segments& sg, int cols, cudaStr
 
 int check_shape(const int32_t* offsets, int E, int d, int n, int64_t rows) {
   if (E < 1 || d < 1 || n < 1 || rows < 0 || !offsets) return CAPMOE_EINVAL;
-  if (E > GMM_MAX_E || rows >= ((int64_t)1 << 31) || ceil_div(d, ST) > 65535 || ceil_div(n, ST) > 65535)
+  if (E > GMM_MAX_E || rows > GMM_MAX_ROWS || ceil_div(d, ST) > 65535 || ceil_div(n, ST) > 65535)
     return CAPMOE_EUNSUPPORTED;
   return CAPMOE_OK;
 }

@@ -1,0 +1,80 @@
+"""Grouped products at the largest row counts that they accept: nearly all rows in one expert, a few before and behind it."""
+import pytest
+import torch
+
+import grouped_ref as R
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+ROWS = (1 << 31) - 512
+COUNTS = [5, ROWS - 12, 7]
+
+
+@pytest.fixture(scope="module")
+def cm():
+    from paper_2503_05066_b200 import capmoe
+    capmoe.lib()
+    return capmoe
+
+
+@pytest.fixture(autouse=True)
+def room():
+    def need(gigabytes):
+        torch.cuda.empty_cache()
+        if torch.cuda.mem_get_info()[0] < (gigabytes + 4) * 1e9:
+            pytest.skip("not enough free memory on this device")
+    yield need
+    torch.cuda.empty_cache()
+
+
+def _normal(shape, std, dtype, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.empty(shape, device="cuda", dtype=dtype).normal_(0, std, generator=g)
+
+
+def _sample():
+    """Row numbers next to every border and all over, and the expert of each."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    any_row = torch.randint(0, ROWS, (200_000,), device="cuda", generator=g)
+    at = torch.cat([torch.arange(600, device="cuda"), any_row, torch.arange(ROWS - 600, ROWS, device="cuda")])
+    e = (at >= 5).long() + (at >= ROWS - 7).long()
+    return [(i, at[e == i]) for i in range(3)]
+
+
+def _finite(t):
+    return all(bool(torch.isfinite(c.float()).all()) for c in t.split(1 << 26))
+
+
+@pytest.mark.parametrize("dtype,size", [(BF16, 8), (F32, 1)])
+def test_products(cm, room, dtype, size):
+    """All rows are written (the outputs start as NaN), and those at every border are right."""
+    room(2e-9 * ROWS * size * dtype.itemsize)
+    off = R.offsets_of(COUNTS)
+    x, w = _normal((ROWS, size), 1.0, dtype, 1), _normal((3, size, size), 1.0, dtype, 2)
+    y = torch.full_like(x, float("nan"))
+    cm.grouped_mm(x, off, w, y=y)
+    assert _finite(y)
+    for e, r in _sample():
+        R.close(y[r], *R.product(x[r].double(), w[e].double(), dtype))
+    x.fill_(float("nan"))
+    cm.grouped_mm_dx(y, off, w, dx=x)
+    assert _finite(x)
+    for e, r in _sample():
+        R.close(x[r], *R.product(y[r].double(), w[e].double().T, dtype))
+
+
+def test_8_bit_product(cm, room):
+    size = 16
+    room(1e-9 * ROWS * (size + 1 + 2 * size))
+    off = R.offsets_of(COUNTS)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    code = torch.empty((ROWS, size), device="cuda", dtype=torch.uint8).random_(0, 0x7f, generator=g)       # finite, positive
+    scale = torch.empty((ROWS, 1), device="cuda", dtype=torch.uint8).random_(120, 130, generator=g)
+    xq, xs = code.view(cm.FP8), scale.view(cm.SCALE)
+    wq, ws = cm.quantize_weights(_normal((3, size, size), 1.0, BF16, 4))
+    y = torch.full((ROWS, size), float("nan"), device="cuda", dtype=BF16)
+    cm.grouped_mm_fp8(xq, xs, off, wq, ws, y=y)
+    assert _finite(y)
+    for e, r in _sample():
+        at = R.decoded(code[r].view(cm.FP8), scale[r].view(cm.SCALE), 1)
+        R.close(y[r], *R.product(at, R.decoded(wq[e], ws[e], 128), BF16))

@@ -142,3 +142,13 @@ def test_split_bytes_refuses_bad_sizes(cm):
         assert cm.lib().capmoe_dw_split_bytes(*{**good, **change}.values(), ctypes.byref(out)) == cm.EINVAL
     assert cm.lib().capmoe_dw_split_bytes(*good.values(), None) == cm.EINVAL
     assert cm.lib().capmoe_dw_split_bytes(*{**good, "d": 33}.values(), ctypes.byref(out)) == cm.OK and out.value == 0
+
+
+@pytest.mark.parametrize("name", ["mm", "dx", "dw", "bwd", "mm8", "ffn8"])
+def test_rows_that_round_up_past_32_bits(cm, name):
+    """Segments are rounded up to whole tiles in 32 bits: the last 511 row counts below 2^31 are refused."""
+    fn, good = _calls(cm)[name]
+    before = cm.launch_count()
+    for rows in ((1 << 31) - 511, (1 << 31) - 1):
+        assert fn(*{**good, "rows": I(rows)}.values()) == cm.EUNSUPPORTED
+    assert cm.launch_count() == before
