@@ -84,8 +84,12 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
   auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(MAX_STAGES + s); };
   auto tfull_bar = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MAX_STAGES + b); };
   auto tempty_bar = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MAX_STAGES + 2 + b); };
+  // A tile lasts as long as its reduction, whose length the host does not know: 0.28 to 0.46 us a k-block for a pair on its
+  // own (2^25 rows of one expert, 8 x 8 to 88 x 88), so 400 million rows outlast the usual limit.  Waits for a whole tile get
+  // about 2 us more for each k-block that may be in it.
+  const long long tile_limit = WAIT_LIMIT_CYCLES + (long long)(ar.sg.rows / BK) * 4096;
   const TileRing ring{bar0 + 8u * RING_BAR, smem_u32(ends + (GMM_MAX_E + 1) + 2) /* 2 * 257 + 2 ints: 16-byte aligned */, rank,
-                      abort_flag};
+                      abort_flag, tile_limit};
 
   // set-up that touches no global memory comes before the wait for the previous kernel
   if (tid == 0) {
@@ -208,7 +212,7 @@ __global__ void __launch_bounds__(GMM_THREADS, 1) k_gmm_dw(const __grid_constant
     for (int j = 0;; ++j, ++it) {
       if (!get_tile(j, true, t)) break;
       const uint32_t b = it & 1u, use = it >> 1;
-      bool ready = mbar_wait(tfull_bar(b), use & 1u, abort_flag);
+      bool ready = mbar_wait(tfull_bar(b), use & 1u, abort_flag, tile_limit);
       ready = __all_sync(0xffffffffu, ready);
       if (!ready) break;
       tc_fence_after();

@@ -182,6 +182,7 @@ struct TileRing {
   uint32_t rec0;                     // records
   uint32_t rank;
   volatile int* abort_flag;
+  long long limit = WAIT_LIMIT_CYCLES;   // of a wait, which may last as long as a tile
   __device__ __forceinline__ uint32_t full(int j) const { return bar0 + 8u * (uint32_t)(j & (TR - 1)); }
   __device__ __forceinline__ uint32_t empty(int j) const { return bar0 + 8u * (uint32_t)(TR + (j & (TR - 1))); }
   __device__ __forceinline__ uint32_t xfull(int q) const { return bar0 + 8u * (uint32_t)(2 * TR + (q & 1)); }
@@ -193,7 +194,7 @@ struct TileRing {
   }
   // Record j for one thread or one whole warp; false when there is no further tile or a wait ran out.
   __device__ __forceinline__ bool get(int j, bool whole_warp, int4& a, int4& b) const {
-    bool ok = mbar_wait(full(j), ((uint32_t)j / TR) & 1u, abort_flag);
+    bool ok = mbar_wait(full(j), ((uint32_t)j / TR) & 1u, abort_flag, limit);
     if (whole_warp) ok = __all_sync(0xffffffffu, ok);
     if (!ok) return false;
     const uint32_t r = rec0 + 32u * (uint32_t)(j & (TR - 1));
@@ -204,7 +205,7 @@ struct TileRing {
     return a.x >= 0;
   }
   __device__ __forceinline__ bool put(int j, const int4& a, const int4& b) const {
-    if (!mbar_wait(empty(j), (((uint32_t)j / TR) & 1u) ^ 1u, abort_flag)) return false;
+    if (!mbar_wait(empty(j), (((uint32_t)j / TR) & 1u) ^ 1u, abort_flag, limit)) return false;
     const uint32_t r = rec0 + 32u * (uint32_t)(j & (TR - 1));
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(r), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(r + 16u), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
@@ -225,14 +226,14 @@ struct TileRing {
         if (leader) {
           tile = npairs + claim;
           if (tile < tile_hi) claim = atomicAdd(counter, 1);
-          if (!mbar_wait_cluster(xempty(q), (use & 1u) ^ 1u, abort_flag)) return;
+          if (!mbar_wait_cluster(xempty(q), (use & 1u) ^ 1u, abort_flag, limit)) return;
           const uint32_t pfull = peer_addr(xfull(q));
           asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(pfull), "r"(4u) : "memory");
           asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];"
                        ::"r"(peer_addr(xval(q))), "r"((uint32_t)tile), "r"(pfull)
                        : "memory");
         } else {
-          if (!mbar_wait_cluster(xfull(q), use & 1u, abort_flag)) return;
+          if (!mbar_wait_cluster(xfull(q), use & 1u, abort_flag, limit)) return;
           asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tile) : "r"(xval(q)) : "memory");
           give_back_slot(xempty(q));
         }

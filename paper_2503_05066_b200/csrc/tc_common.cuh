@@ -214,9 +214,10 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                                  long long limit_cycles = WAIT_LIMIT_CYCLES) {
   if (mbar_try_wait_cluster(bar, parity)) return true;
-  return mbar_wait(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);
+  return mbar_wait(bar, parity, abort_flag, limit_cycles) && mbar_try_wait_cluster(bar, parity);
 }
 // Gives a slot that the even CTA fills by st.async back to it, after this thread (and the lanes of its warp, behind a
 // __syncwarp) have read the value: the read must be over, at cluster scope, before the next value may be sent.  With

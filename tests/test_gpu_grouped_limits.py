@@ -78,3 +78,27 @@ def test_8_bit_product(cm, room):
     for e, r in _sample():
         at = R.decoded(code[r].view(cm.FP8), scale[r].view(cm.SCALE), 1)
         R.close(y[r], *R.product(at, R.decoded(wq[e], ws[e], 128), BF16))
+
+
+def test_weight_gradient_of_a_very_long_segment(cm, room):
+    """One of many experts has 805 million rows: its reduction, which is not split, takes about four seconds, longer than a
+    wait may usually last.  Sums of -1, 0 and 1 far below 2^24: every order gives the same."""
+    rows, E, size = 3 << 28, 40, 8
+    room(4e-9 * rows * size)
+    off = torch.full((E + 1,), rows, device="cuda", dtype=torch.int32)
+    off[:18] = 0
+    off[18:21] = rows - 5                                       # two experts without rows behind it, then one with five
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.empty((rows, size), device="cuda", dtype=BF16) for _ in range(2))
+    for t in (x, dy):
+        for c in t.split(1 << 26):
+            c.copy_(torch.empty(c.shape, device="cuda", dtype=torch.int8).random_(-1, 2, generator=g))
+    st = torch.zeros(cm.FFN_STATUS_WORDS, device="cuda", dtype=torch.int32)
+    want = torch.zeros((E, size, size), device="cuda", dtype=F32)
+    for a, b in zip(dy[:-5].split(1 << 24), x[:-5].split(1 << 24)):
+        want[17] += a.float().T @ b.float()
+    want[20] = dy[-5:].float().T @ x[-5:].float()
+    for status in (st, None):
+        dw = cm.grouped_mm_dw(dy, x, off, out_dtype=F32, dev_status=status)
+        assert torch.equal(dw, want)
+    assert int(st[0]) == 0 and float(want[17].abs().max()) < 2 ** 22
