@@ -316,7 +316,8 @@ int capmoe_grouped_ffn_backward(const void* x_perm, const void* dy_perm, const i
  *                            expert_offsets + E) only the rows below *n_rows are read and written
  *   capmoe_quantize_weights  w [E,n,d] -> q [E,n,d], scale [E, ceil(n/128), ceil(d/128)]
  * The scale is the smallest 2^e (e >= -127) with max|block| <= 448 * 2^e, 1 for a block of zeros; codes are
- * rounded to nearest even.  A block that holds a NaN or an infinity becomes NaN as a whole.
+ * rounded to nearest even.  A block that holds a NaN or an infinity becomes NaN as a whole.  rows < 2^31,
+ * n and d <= 2^31 - 1024.
  *   capmoe_grouped_mm_fp8    y[r] = W[e] x[r] from codes and scales, fp32 accumulation, y [rows,n] bf16
  *   capmoe_grouped_ffn_fp8   stage 5 with 8-bit weights: x_perm [A_max,d] bf16 is quantised, then
  *                            h = silu(W_g x) * (W_u x) in fp32, h quantised, y_perm [A_max,d] bf16 = W_d h.

@@ -13,6 +13,7 @@ namespace {
 
 using G8 = Geo<ST, 8>;                     // block of the fallback product
 constexpr int QN = 256;                    // threads of the quantisers
+constexpr int Q_MAX = 0x7fffffff - 1023;   // columns, rows of a weight: 32 bits after rounding up to eight blocks of 128
 
 // Eight consecutive elements of a row, kept as they are stored until they are used (half the registers of fp32 for bf16,
 // so more loads in flight): 16-byte loads with VEC, else the first `left` one by one.
@@ -279,7 +280,7 @@ extern "C" int capmoe_quantize_rows(const void* x, const int32_t* n_rows, int64_
                                     void* stream) {
   if (rows < 0 || d < 1) return CAPMOE_EINVAL;
   if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
-  if (rows >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
+  if (rows >= ((int64_t)1 << 31) || d > Q_MAX) return CAPMOE_EUNSUPPORTED;
   if (rows == 0) return CAPMOE_OK;
   if (!usable(x, q) || !scale) return CAPMOE_EINVAL;
   if (dtype == CAPMOE_F32) return quantize_rows_run<float>(x, n_rows, rows, d, q, scale, ceil_div(d, QBLOCK), as_stream(stream));
@@ -289,6 +290,7 @@ extern "C" int capmoe_quantize_rows(const void* x, const int32_t* n_rows, int64_
 extern "C" int capmoe_quantize_weights(const void* w, int E, int n, int d, int dtype, void* q, void* scale, void* stream) {
   if (E < 1 || n < 1 || d < 1) return CAPMOE_EINVAL;
   if (dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) return CAPMOE_EUNSUPPORTED;
+  if (n > Q_MAX || d > Q_MAX) return CAPMOE_EUNSUPPORTED;
   if (!usable(w, q) || !scale) return CAPMOE_EINVAL;
   if (dtype == CAPMOE_F32) return quantize_weights_run<float>(w, E, n, d, q, scale, as_stream(stream));
   return quantize_weights_run<__nv_bfloat16>(w, E, n, d, q, scale, as_stream(stream));

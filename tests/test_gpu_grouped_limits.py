@@ -102,3 +102,14 @@ def test_weight_gradient_of_a_very_long_segment(cm, room):
         dw = cm.grouped_mm_dw(dy, x, off, out_dtype=F32, dev_status=status)
         assert torch.equal(dw, want)
     assert int(st[0]) == 0 and float(want[17].abs().max()) < 2 ** 22
+
+
+def test_quantisers_of_the_longest_rows(cm, room):
+    """One row (one column of a weight) of 2^31 - 1024 elements has the blocks of as many rows of 128."""
+    size = (1 << 31) - 1024
+    room(2e-9 * size * 4)
+    x = _normal((1, size), 1.0, BF16, 6)
+    q, s = (t.view(torch.uint8) for t in cm.quantize_rows(x.view(-1, 128)))
+    for view, got in ((x.shape, cm.quantize_rows(x)), ((1, size, 1), cm.quantize_weights(x.view(1, size, 1)))):
+        assert got[0].shape == view
+        assert torch.equal(got[0].view(torch.uint8).view(q.shape), q) and torch.equal(got[1].view(torch.uint8).view(s.shape), s)

@@ -152,3 +152,15 @@ def test_rows_that_round_up_past_32_bits(cm, name):
     for rows in ((1 << 31) - 511, (1 << 31) - 1):
         assert fn(*{**good, "rows": I(rows)}.values()) == cm.EUNSUPPORTED
     assert cm.launch_count() == before
+
+
+def test_quantisers_refuse_sizes_that_pass_32_bits(cm):
+    """Columns (rows of a weight) are rounded up to whole warps' shares in 32 bits."""
+    L = cm.lib()
+    before = cm.launch_count()
+    for v in ((1 << 31) - 1023, (1 << 31) - 1):
+        for dt in (cm.F32, cm.BF16):
+            assert L.capmoe_quantize_rows(P, Z, I(1), v, dt, P, P, Z) == cm.EUNSUPPORTED
+            assert L.capmoe_quantize_weights(P, 1, v, 1, dt, P, P, Z) == cm.EUNSUPPORTED
+            assert L.capmoe_quantize_weights(P, 1, 1, v, dt, P, P, Z) == cm.EUNSUPPORTED
+    assert cm.launch_count() == before
