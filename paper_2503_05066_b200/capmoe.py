@@ -460,6 +460,12 @@ def _bytes(fn, *args) -> int:
     return out.value
 
 
+def _fits(where: str, *sizes):
+    """Sizes that the library takes as C ints, which ctypes would cut to 32 bits."""
+    if max(sizes) > 0x7fffffff:
+        _refuse(where, f"sizes {sizes} pass 32 bits", EUNSUPPORTED)
+
+
 def _experts(where: str, offsets) -> int:
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2:
         _refuse(where, "offsets must be int32 [E+1]")
@@ -492,6 +498,7 @@ def grouped_mm(x_rows, offsets, w, y=None, dev_status=None, stream=None):
         _refuse(where, "x_rows [rows,d] and w [E,n,d] of one dtype expected")
     rows, d = x_rows.shape
     n = w.shape[1]
+    _fits(where, E, d, n)
     y = _out(where, y, (rows, n), x_rows.dtype, x_rows)
     _run(where, x_rows, x_rows, offsets, w, E, d, n, _dt(x_rows), y, rows, _status(where, dev_status))
     return y
@@ -508,6 +515,7 @@ def grouped_mm_dx(dy_rows, offsets, w, dx=None, dev_status=None, stream=None):
         _refuse(where, "dy_rows [rows,n] and w [E,n,d] of one dtype expected")
     rows, n = dy_rows.shape
     d = w.shape[2]
+    _fits(where, E, d, n)
     dx = _out(where, dx, (rows, d), dy_rows.dtype, dy_rows)
     _run(where, dy_rows, dy_rows, offsets, w, E, d, n, _dt(dy_rows), dx, rows, _status(where, dev_status))
     return dx
@@ -525,6 +533,7 @@ def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, de
         _refuse(where, "dy_rows [rows,n] and x_rows [rows,d] of one dtype expected")
     rows, n = dy_rows.shape
     d = x_rows.shape[1]
+    _fits(where, E, d, n)
     dw = _out(where, dw, (E, n, d), out_dtype or (dw.dtype if dw is not None else x_rows.dtype), x_rows)
     if ws is None:
         ws = x_rows.new_empty((_dw_bytes(rows, E, d, n, x_rows.dtype),), dtype=torch.uint8)
@@ -577,6 +586,7 @@ def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None
         _refuse(where, "one dtype expected")
     A_max, d = x_perm.shape
     F = w_gate.shape[1]
+    _fits(where, E, d, F)
     dx = _out(where, dx, (A_max, d), dtype, x_perm)
     dwg, dwu, dwd = (None, None, None) if dw is None else dw
     dwg = _out(where, dwg, (E, F, d), dtype, x_perm)
@@ -608,6 +618,7 @@ def quantize_rows(x, offsets=None, out=None, stream=None):
     if x.dim() != 2:
         _refuse(where, "x [rows,d] expected")
     rows, d = x.shape
+    _fits(where, d)
     q, scale = (None, None) if out is None else out
     q = torch.empty_like(x, dtype=FP8) if q is None else _out(where, q, (rows, d), FP8, x)
     scale = _out(where, scale, (rows, _blocks(d)), SCALE, x)
@@ -631,6 +642,7 @@ def quantize_weights(w, out=None, stream=None):
     if w.dim() != 3:
         _refuse(where, "w [E,n,d] expected")
     E, n, d = w.shape
+    _fits(where, E, n, d)
     q, scale = (None, None) if out is None else out
     q = _out(where, q, (E, n, d), FP8, w)
     scale = _out(where, scale, (E, _blocks(n), _blocks(d)), SCALE, w)
@@ -655,6 +667,7 @@ def grouped_mm_fp8(x_q, x_scale, offsets, w_q, w_scale, y=None, dev_status=None,
         _refuse(where, "x_q [rows,d], w_q [E,n,d] expected")
     rows, d = x_q.shape
     n = w_q.shape[1]
+    _fits(where, E, d, n)
     _coded(where, x_q, x_scale, (rows, d), 1)
     _coded(where, w_q, w_scale, (E, n, d), QBLOCK)
     y = _out(where, y, (rows, n), torch.bfloat16, x_q)
@@ -678,6 +691,7 @@ def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None,
         _refuse(where, "x_perm [A_max,d] bfloat16 and (q, scale) weights expected")
     A_max, d = x_perm.shape
     F = w_gate[0].shape[1]
+    _fits(where, E, d, F)
     _coded(where, *w_gate, (E, F, d), QBLOCK)
     _coded(where, *w_up, (E, F, d), QBLOCK)
     _coded(where, *w_down, (E, d, F), QBLOCK)

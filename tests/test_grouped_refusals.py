@@ -164,3 +164,29 @@ def test_quantisers_refuse_sizes_that_pass_32_bits(cm):
             assert L.capmoe_quantize_weights(P, 1, v, 1, dt, P, P, Z) == cm.EUNSUPPORTED
             assert L.capmoe_quantize_weights(P, 1, 1, v, dt, P, P, Z) == cm.EUNSUPPORTED
     assert cm.launch_count() == before
+
+
+def test_binding_refuses_sizes_that_do_not_fit_a_c_int(cm):
+    """2^32 + 64 columns must not reach the library as 64."""
+    bf, i32, big = torch.bfloat16, torch.int32, (1 << 32) + 64
+
+    def meta(*shape, dtype=bf):
+        return torch.empty(shape, device="meta", dtype=dtype)
+
+    off = meta(3, dtype=i32)
+    w8 = (meta(2, 64, big, dtype=cm.FP8), meta(2, 1, big // 128 + 1, dtype=cm.SCALE))
+    d8 = (meta(2, big, 64, dtype=cm.FP8), meta(2, big // 128 + 1, 1, dtype=cm.SCALE))
+    calls = [
+        lambda: cm.grouped_mm(meta(4, big), off, meta(2, 64, big)), lambda: cm.grouped_mm(meta(4, 64), off, meta(2, big, 64)),
+        lambda: cm.grouped_mm_dx(meta(4, big), off, meta(2, big, 64)), lambda: cm.grouped_mm_dw(meta(4, big), meta(4, 64), off),
+        lambda: cm.grouped_ffn_backward(meta(4, 64), meta(4, 64), off, meta(2, big, 64), meta(2, big, 64), meta(2, 64, big)),
+        lambda: cm.quantize_rows(meta(4, big)), lambda: cm.quantize_weights(meta(2, big, 64)),
+        lambda: cm.quantize_weights(meta(2, 64, big)), lambda: cm.quantize_weights(meta(big, 64, 64)),
+        lambda: cm.grouped_mm_fp8(meta(4, big, dtype=cm.FP8), meta(4, big // 128 + 1, dtype=cm.SCALE), off, *w8),
+        lambda: cm.grouped_ffn_fp8(meta(4, 64), off, d8, d8, w8),
+        lambda: cm.grouped_mm(meta(4, 64), meta((1 << 32) + 3, dtype=i32), meta((1 << 32) + 2, 64, 64)),
+    ]
+    for i, call in enumerate(calls):
+        with pytest.raises(cm.CapmoeError) as err:
+            call()
+        assert err.value.status == cm.EUNSUPPORTED, i
