@@ -536,7 +536,7 @@ def grouped_mm_dw(dy_rows, x_rows, offsets, dw=None, out_dtype=None, ws=None, de
     _fits(where, E, d, n)
     dw = _out(where, dw, (E, n, d), out_dtype or (dw.dtype if dw is not None else x_rows.dtype), x_rows)
     if ws is None:
-        ws = x_rows.new_empty((_dw_bytes(rows, E, d, n, x_rows.dtype),), dtype=torch.uint8)
+        ws = x_rows.new_empty((_dw_bytes(x_rows.get_device(), rows, E, d, n, x_rows.dtype),), dtype=torch.uint8)
     _run(where, x_rows, dy_rows, x_rows, offsets, E, d, n, _dt(x_rows), _dt(dw), dw, rows, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return dw
@@ -552,14 +552,14 @@ def ffn_backward_workspace_bytes(A_max: int, E: int, F: int, dtype) -> int:
     return _bytes("capmoe_ffn_backward_workspace_bytes", _i64(A_max), int(E), int(F), _dt(dtype))
 
 
-# sizes of the workspaces that the calls make themselves
+# Sizes of the workspaces that the calls make themselves; the splits depend on the (current) device's SM count.
 @functools.lru_cache(maxsize=1024)
-def _dw_bytes(rows, E, d, n, dtype):
+def _dw_bytes(device, rows, E, d, n, dtype):
     return _bytes("capmoe_grouped_mm_dw_workspace_bytes", E) + dw_split_bytes(rows, E, d, n, dtype)
 
 
 @functools.lru_cache(maxsize=1024)
-def _ffn_backward_bytes(A_max, E, d, F, dtype):
+def _ffn_backward_bytes(device, A_max, E, d, F, dtype):
     return ffn_backward_workspace_bytes(A_max, E, F, dtype) + dw_split_bytes(A_max, E, d, F, dtype, 3)
 
 
@@ -593,7 +593,7 @@ def grouped_ffn_backward(x_perm, dy_perm, offsets, w_gate, w_up, w_down, dx=None
     dwu = _out(where, dwu, (E, F, d), dtype, x_perm)
     dwd = _out(where, dwd, (E, d, F), dtype, x_perm)
     if ws is None:
-        ws = x_perm.new_empty((_ffn_backward_bytes(A_max, E, d, F, dtype),), dtype=torch.uint8)
+        ws = x_perm.new_empty((_ffn_backward_bytes(x_perm.get_device(), A_max, E, d, F, dtype),), dtype=torch.uint8)
     _run(where, x_perm, x_perm, dy_perm, offsets, E, d, F, _dt(dtype), w_gate, w_up, w_down, dx, dwg, dwu, dwd, A_max, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return dx, dwg, dwu, dwd

@@ -190,3 +190,26 @@ def test_binding_refuses_sizes_that_do_not_fit_a_c_int(cm):
         with pytest.raises(cm.CapmoeError) as err:
             call()
         assert err.value.status == cm.EUNSUPPORTED, i
+
+
+def test_workspaces_are_sized_for_their_device(cm, monkeypatch):
+    """The size depends on the device's SM count: one device's must not serve another."""
+    class On(torch.Tensor):
+        index = 0
+
+        def get_device(self):
+            return On.index
+
+    sizes = {"capmoe_grouped_mm_dw_workspace_bytes": 512, "capmoe_ffn_backward_workspace_bytes": 512, "capmoe_dw_split_bytes": 0}
+    seen = []
+    monkeypatch.setattr(cm, "_bytes", lambda fn, *args: sizes[fn] + (On.index + 1) * 1000)
+    monkeypatch.setattr(cm, "_run", lambda name, like, *args: seen.append(next(v for v in args if isinstance(v, torch.Tensor) and
+                                                                              v.dtype == torch.uint8).numel()))
+    off = torch.zeros(4, dtype=torch.int32)
+    x, w, wd = torch.zeros((17, 24)).as_subclass(On), torch.zeros((3, 40, 24)), torch.zeros((3, 24, 40))
+    for On.index in (0, 1, 0, 1):
+        cm.grouped_mm_dw(x, x, off)
+        cm.grouped_ffn_backward(x, x, off, w, w, wd)
+    cm._dw_bytes.cache_clear()
+    cm._ffn_backward_bytes.cache_clear()
+    assert seen == [2512, 2512, 4512, 4512] * 2
