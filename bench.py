@@ -41,12 +41,12 @@ UNIT = "tokens/s"
 # key = (config, N, F, mode, gamma, straggler) -> {"gate_up": bytes, "down": bytes}
 NCU_TRAFFIC = {
     "kernel_sources": ["paper_2503_05066_b200/csrc/ffn_tc.cu", "paper_2503_05066_b200/csrc/tc_common.cuh"],
-    "sha256": "50320e18dc87454ff7b6bb78d56bdd910562c4331286dba03e2abdceefe292fe",
+    "sha256": "76fbae5d1dbd2d4074c0e4f4264d5c7236af97d2a2a81936be9b324bc9a6c1ff",
     "captures": {
         # ncu --metrics gpu__time_duration.sum,dram__bytes_read.sum,dram__bytes_write.sum (one pass),
         # means of nine launches each of the two GEMM kernels
-        ("mixtral", 8192, 14336, "expanded_drop", 1.0, True): {"gate_up": 2591500000 + 460600000,
-                                                                "down": 3039100000 + 126300000},
+        ("mixtral", 8192, 14336, "expanded_drop", 1.0, True): {"gate_up": 2321600000 + 460700000,
+                                                                "down": 4067600000 + 128500000},
     },
 }
 

@@ -220,13 +220,11 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
   return mbar_wait(bar, parity, abort_flag, limit_cycles) && mbar_try_wait_cluster(bar, parity);
 }
 // Gives a slot that the even CTA fills by st.async back to it, after this thread (and the lanes of its warp, behind a
-// __syncwarp) have read the value: the read must be over, at cluster scope, before the next value may be sent.  With
-// arrivals of CTA scope (the default) CTAs of a pair were seen to take different tiles, about once in a million
-// hand-overs of a two-deep mailbox between tiles that are empty sums.
-__device__ __forceinline__ void give_back_slot(uint32_t bar) {
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  mbar_arrive_release_cluster(bar & PEER_MASK);
-}
+// __syncwarp) have read the value: the release at cluster scope, with the acquire of the even CTA's wait, puts the read
+// before the next value.  With arrivals of CTA scope (the default) CTAs of a pair took different tiles, about once in a
+// million hand-overs of a two-deep mailbox between tiles that are empty sums; with this none in 90 million.  A fence in
+// front of the release is not needed and costs an FFN of short segments 2 to 3 %.
+__device__ __forceinline__ void give_back_slot(uint32_t bar) { mbar_arrive_release_cluster(bar & PEER_MASK); }
 // Tile queue of a CTA or a CTA pair.  With a scheduler counter the CTAs do not walk fixed lists of
 // tiles: the (leader's) producer thread takes the next tile index from a global counter shortly
 // before it needs it and hands it to every role (of both CTAs) through a small ring in shared
