@@ -10,8 +10,9 @@
 // split into parts, each a tile of its own with an fp32 output in the workspace, and a second kernel adds the parts in
 // their order.
 // What bounds it: a tile of an expert with a few hundred rows has only a handful of k-blocks, about as long as its
-// epilogue (3200 cycles) and as its share of the HBM writes; 17,500 rows of 64 experts, 2048 x 1024: 92 us for 268 MB of
-// gradients (0.44 of the tensor pipe, 0.6 of the copy bandwidth), the three gradients of the FFN there 262 us.
+// epilogue (3200 cycles) and as its share of the HBM writes; 17,500 rows of 64 experts, 2048 x 1024, 268 MB of
+// gradients: 87 us for one cold launch (0.46 of the tensor pipe, 0.44 of the peak DRAM rate), about 105 us in a loop at the
+// power limit, 84 with operands of zeros, which do not reach it; the FFN's three gradients there 240 us cold.
 #include "gmm.cuh"
 #include "gmm_tc.cuh"
 

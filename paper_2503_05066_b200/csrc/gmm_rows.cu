@@ -6,12 +6,16 @@
 // products were 2 % faster at best, at 2000 rows per expert and more, and up to half as fast below 300.)
 //   T_FWD   y^T  = W[e] x^T             T_DX  dx^T = W[e]^T dy^T         T_DX2  dx^T = W_g[e]^T dg^T + W_u[e]^T du^T
 //   T_HID   dg, du, h of the SwiGLU FFN's backward pass: g, u and dh of a tile side by side in tensor memory, the
-//           elementwise part in the epilogue, so that g, u and dh are never rounded or written
+//           elementwise part in the epilogue, so that g, u and dh are never rounded or written; dg, du and h are rounded
+//           to bf16, because the MMAs that read them multiply bf16: a third of the FFN gradients' error (0.23 % of their
+//           norm, 0.17 % with those three exact), and half the bytes of fp32 copies
 //   T_F8    8-bit T_FWD                 T_F8SW  8-bit gate/up with SwiGLU, hidden rows quantised
 // Weights whose output index is contiguous (W^T) are MN-major operands, loaded as they lie (make_mn_map).
 // One token's row of an output is one column of an accumulator.  The epilogue reads 8 x 8 fragments, which stmatrix
 // writes transposed to shared memory, so that whole 64-byte runs of a token's row leave the warp.  (Two-byte stores
 // straight from the accumulator's columns took 15,000 cycles for a 128-token tile of T_HID, half as long as its MMAs.)
+// silu is computed with __expf and __fdividef: a few units of 2^-23 while |g| is below 10, about 100 at -87, and 0 for g
+// below -87 (the exact value is under 2^-118 there); the result is then rounded to 8 bits of mantissa or fewer.
 // In T_F8SW a CTA's 128 weight rows are exactly one block of 128 hidden columns, whose maximum is taken per token over
 // the lanes (shuffles) and the four warps (shared memory).
 // A stage holds the weights of one k-block and `tb` token rows per CTA; `tb` follows the average segment so that short

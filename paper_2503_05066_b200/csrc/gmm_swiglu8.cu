@@ -6,9 +6,11 @@
 // columns side by side, which is one block of 128 hidden columns per row: its largest magnitude meets between the two
 // threads that share a row, and the hidden row leaves the kernel as codes, never as fp32.
 // Tensor memory: two accumulators of 256 columns and four groups of scales do not fit 512 columns, so the
-// accumulators overlap by 64 columns ([0,256) and [192,448)); an epilogue reads the shared columns first and lets the
-// next tile's MMAs start then, with most of its own columns still to convert.  (With the tokens on the N side, as in
-// gmm_rows.cu, gate and up would fill the 448 columns at 224 tokens, and an epilogue could not overlap the next tile.)
+// accumulators overlap by 64 columns ([0,256) and [192,448)).  The next tile's MMAs wait for the warps that read those 64
+// columns, which, like the others, hold a tile's hidden values in registers before they let go of any of its columns; they
+// do not wait for the other half of the warps, nor for anyone's quantising and storing.  (With the tokens on the N side, as
+// in gmm_rows.cu, gate and up would fill the 448 columns at 224 tokens, and an epilogue could not overlap the next tile.)
+// silu: __expf and __fdividef, as in gmm_rows.cu.
 // What bounds it: the tensor pipe; the scale copies take about 10 % of it.
 #include "gmm.cuh"
 #include "gmm_tc.cuh"
