@@ -7,7 +7,7 @@
 //   T_FWD   y^T  = W[e] x^T             T_DX  dx^T = W[e]^T dy^T         T_DX2  dx^T = W_g[e]^T dg^T + W_u[e]^T du^T
 //   T_HID   dg, du, h of the SwiGLU FFN's backward pass: g, u and dh of a tile side by side in tensor memory, the
 //           elementwise part in the epilogue, so that g, u and dh are never rounded or written; dg, du and h are rounded
-//           to bf16, because the MMAs that read them multiply bf16: a third of the FFN gradients' error (0.23 % of their
+//           to bf16, because the MMAs that read them multiply bf16: a quarter of the FFN gradients' error (0.23 % of their
 //           norm, 0.17 % with those three exact), and half the bytes of fp32 copies
 //   T_F8    8-bit T_FWD                 T_F8SW  8-bit gate/up with SwiGLU, hidden rows quantised
 // Weights whose output index is contiguous (W^T) are MN-major operands, loaded as they lie (make_mn_map).
