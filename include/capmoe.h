@@ -334,6 +334,72 @@ int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_offsets, in
                            const void* wg_scale, const void* wu_q, const void* wu_scale, const void* wd_q,
                            const void* wd_scale, void* y_perm, int64_t A_max, void* ws, size_t ws_bytes, int32_t* dev_status,
                            void* stream);
+/* capmoe_grouped_ffn_fp8 from rows that are codes already (x_q [A_max,d], x_scale [A_max, ceil(d/128)], as capmoe_quantize_rows
+ * or capmoe_permute_fp8 leave them): the same result, one pass less over the rows. */
+int capmoe_grouped_ffn_fp8_codes(const void* x_q, const void* x_scale, const int32_t* expert_offsets, int E, int d, int F,
+                                 const void* wg_q, const void* wg_scale, const void* wu_q, const void* wu_scale, const void* wd_q,
+                                 const void* wd_scale, void* y_perm, int64_t A_max, void* ws, size_t ws_bytes,
+                                 int32_t* dev_status, void* stream);
+
+/* ---------------------------------------------------------------- the norm in front of the layer
+ * Root-mean-square norm of N rows of d columns, with the residual's addition and 8-bit codes of the result:
+ *   h = x + residual, rounded to `dtype` (h = x without a residual),
+ *   rstd = 1 / sqrt(sum_c h_c^2 / d + eps),  y_c = h_c rstd w_c, rounded to `dtype`,
+ *   q, scale = what capmoe_quantize_rows makes of y: one pass for what would be three.
+ * Sums and products are fp32.  A NaN or an infinity stays in its row.
+ *   in : x, residual (or NULL) [N,d], w [d], all `dtype`; eps >= 0.
+ *   out: h [N,d] (with a residual, else NULL; may be x or residual), y [N,d] (may be x, residual where they are not h's),
+ *        rstd [N] fp32 or NULL, q [N,d] and scale [N, ceil(d/128)] or both NULL.
+ * capmoe_rms_norm_backward: gradients from dy [N,d] and, or NULL, dh [N,d], the gradient that reaches h from behind (the
+ * residual stream's).  With g = dy w:  dx = rstd (g - h rstd^2 (sum_c g_c h_c) / d) + dh, the gradient of x and of the
+ * residual alike (may be dy or dh);  dw = sum over the rows of dy h rstd [d] in out_dtype (`dtype`, or CAPMOE_F32), zeros
+ * for N = 0, summed in fp32 in a fixed order for a given N, d and device.
+ *   ws: capmoe_rms_norm_backward_workspace_bytes(N,d,dtype) bytes on the device that is current.
+ * d <= 16384.  Rows of whole 16-byte vectors are read as such, others element by element. */
+int capmoe_rms_norm(const void* x, const void* residual, const void* w, int64_t N, int d, int dtype, float eps, void* h, void* y,
+                    float* rstd, void* q, void* scale, void* stream);
+int capmoe_rms_norm_backward_workspace_bytes(int64_t N, int d, int dtype, size_t* bytes);
+int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const float* rstd, const void* dh, int64_t N, int d,
+                             int dtype, int out_dtype, void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------- stage 4 in 8 bits; gradients of stages 6, 4 and 1
+ * Over the rows that a drop stage gave out in slot_row [N,slots] (slots = k, or with D > 0 k + E/D: capmoe_permute); A_max is
+ * the allocated row count of the row matrices.  Entries of slot_row that are negative or not below A_max count as no row; every
+ * other row belongs to one slot.  Rows that no slot names are neither read nor written.
+ *   capmoe_permute_fp8       capmoe_permute of codes and scales (capmoe_quantize_rows, capmoe_rms_norm): x_q [N,d], x_scale
+ *                            [N, ceil(d/128)] -> q_perm [A_max,d], scale_perm [A_max, ceil(d/128)], perm_token, perm_weight.
+ *                            d a multiple of 16.
+ *   capmoe_combine_backward  gradients of capmoe_combine from dy [N,d]: dy_perm[r] = perm_weight[r] dy[t] (rounded to `dtype`),
+ *                            dweight[r] = sum_c dy[t,c] y_perm[r,c] (fp32) for the row r of a slot of token t.  (That of
+ *                            y_shared is dy.)
+ *   capmoe_permute_backward  gradient of capmoe_permute: dx[t] = add0[t] + add1[t] + sum over t's rows of dx_perm[r], added in
+ *                            this order, slots ascending, in fp32, rounded once.  add0, add1 [N,d] or NULL: what reaches x by
+ *                            other ways, e.g. through the router and the shared expert; dx may be one of them.
+ *   capmoe_route_backward    gradients of capmoe_route.  The loss sees the scores S through the kept pairs' weights, with
+ *                            dweight [A_max], and, or NULL, directly, with dscores: [N,E] in rows of dscores_ld >= E floats, or
+ *                            (dscores_ld = 0) [E], the same for every token, as a balance loss gives it.
+ *                              dS[t,e] = dscores[t,e] + dweight[row of (t,e)],  dlogits = S (dS - sum_f S_f dS_f) [N,E] fp32,
+ *                              dx = dlogits W_r [N,d] `dtype`,  dw = dlogits^T x [E,d] out_dtype (`dtype`, or CAPMOE_F32),
+ *                              dbias = sum_t dlogits [E] fp32.
+ *                            bf16: dlogits enter the products as the sum of two bf16 numbers each (2^-17 of them is lost).
+ *                            N = 0 leaves zeros in dw and dbias.  All sums have a fixed order for given sizes and device.
+ *                            ws: capmoe_route_backward_workspace_bytes(N,d,E,dtype) bytes on the device that is current.
+ * The first three: rows of whole 16-byte vectors, slots <= 288, N and A_max < 2^31.  route_backward: E <= 256, k <= 32,
+ * N <= 2^31 - 512, any d; d a multiple of 8 runs on tensor cores in bf16.  dev_status as in capmoe_grouped_ffn.  Outputs and
+ * workspace overlap neither each other nor an input, but for dx of capmoe_permute_backward. */
+int capmoe_permute_fp8(const void* x_q, const void* x_scale, int64_t N, int d, int E, int k, int slots, int D, int64_t A_max,
+                       const float* scores, const int32_t* topk_idx, const int32_t* token_group, const int32_t* slot_row,
+                       void* q_perm, void* scale_perm, int32_t* perm_token, float* perm_weight, void* stream);
+int capmoe_combine_backward(const void* dy, const void* y_perm, const int32_t* slot_row, const float* perm_weight, int64_t N,
+                            int d, int slots, int dtype, int64_t A_max, void* dy_perm, float* dweight, void* stream);
+int capmoe_permute_backward(const void* dx_perm, const int32_t* slot_row, int64_t N, int d, int slots, int dtype, int64_t A_max,
+                            const void* add0, const void* add1, void* dx, void* stream);
+int capmoe_route_backward_workspace_bytes(int64_t N, int d, int E, int dtype, size_t* bytes);
+int capmoe_route_backward(const void* x, const void* w_router, const float* scores, const int32_t* topk_idx,
+                          const int32_t* slot_row, const float* dweight, int64_t N, int d, int E, int k, int slots, int D,
+                          const int32_t* token_group, const float* dscores, int64_t dscores_ld, int dtype, int out_dtype,
+                          int64_t A_max, float* dlogits, void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes,
+                          int32_t* dev_status, void* stream);
 
 /* ---------------------------------------------------------------- expert parallelism
  * The paper's deployment (experimental set-up: data parallel over the tokens, expert parallel over

@@ -34,7 +34,10 @@ EXPORTS = ["capmoe_capacity", "capmoe_max_rows", "capmoe_device_max_rows", "capm
            "capmoe_ep_combine", "capmoe_debug_read_probe", "capmoe_debug_check_indices",
            "capmoe_grouped_mm", "capmoe_grouped_mm_dx", "capmoe_grouped_mm_dw_workspace_bytes", "capmoe_grouped_mm_dw",
            "capmoe_dw_split_bytes", "capmoe_ffn_backward_workspace_bytes", "capmoe_grouped_ffn_backward", "capmoe_quantize_rows",
-           "capmoe_quantize_weights", "capmoe_grouped_mm_fp8", "capmoe_ffn_fp8_workspace_bytes", "capmoe_grouped_ffn_fp8"]
+           "capmoe_quantize_weights", "capmoe_grouped_mm_fp8", "capmoe_ffn_fp8_workspace_bytes", "capmoe_grouped_ffn_fp8",
+           "capmoe_grouped_ffn_fp8_codes", "capmoe_rms_norm", "capmoe_rms_norm_backward_workspace_bytes", "capmoe_rms_norm_backward",
+           "capmoe_permute_fp8", "capmoe_combine_backward", "capmoe_permute_backward", "capmoe_route_backward_workspace_bytes",
+           "capmoe_route_backward"]
 
 
 class CapmoeError(RuntimeError):
@@ -428,6 +431,13 @@ _ARGTYPES = {
     "capmoe_quantize_weights": [_V, _I, _I, _I, _I, _V, _V, _V],
     "capmoe_grouped_mm_fp8": [_V, _V, _V, _V, _V, _I, _I, _I, _V, _L, _V, _V],
     "capmoe_grouped_ffn_fp8": [_V, _V, _I, _I, _I, _V, _V, _V, _V, _V, _V, _V, _L, _V, _S, _V, _V],
+    "capmoe_grouped_ffn_fp8_codes": [_V, _V, _V, _I, _I, _I, _V, _V, _V, _V, _V, _V, _V, _L, _V, _S, _V, _V],
+    "capmoe_rms_norm": [_V, _V, _V, _L, _I, _I, ctypes.c_float, _V, _V, _V, _V, _V, _V],
+    "capmoe_rms_norm_backward": [_V, _V, _V, _V, _V, _L, _I, _I, _I, _V, _V, _V, _S, _V],
+    "capmoe_permute_fp8": [_V, _V, _L, _I, _I, _I, _I, _I, _L, _V, _V, _V, _V, _V, _V, _V, _V, _V],
+    "capmoe_combine_backward": [_V, _V, _V, _V, _L, _I, _I, _I, _L, _V, _V, _V],
+    "capmoe_permute_backward": [_V, _V, _L, _I, _I, _I, _L, _V, _V, _V, _V],
+    "capmoe_route_backward": [_V, _V, _V, _V, _V, _V, _L, _I, _I, _I, _I, _I, _V, _V, _L, _I, _I, _L, _V, _V, _V, _V, _V, _S, _V, _V],
 }
 
 
@@ -681,26 +691,221 @@ def ffn_fp8_workspace_bytes(A_max: int, d: int, F: int) -> int:
 
 def grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm=None, ws=None, dev_status=None, stream=None):
     """grouped_ffn with 8-bit weights, each a (q, scale) pair of quantize_weights; x_perm [A_max,d] bfloat16 and the
-    hidden rows are quantised on the way -> y_perm [A_max,d] bfloat16."""
+    hidden rows are quantised on the way -> y_perm [A_max,d] bfloat16.  x_perm may be a (q, scale) pair itself, as
+    quantize_rows or permute_fp8 leave it."""
     where = "capmoe_grouped_ffn_fp8"
     if stream is not None:
         with torch.cuda.stream(stream):
             return grouped_ffn_fp8(x_perm, offsets, w_gate, w_up, w_down, y_perm, ws, dev_status)
     E = _experts(where, offsets)
-    if x_perm.dim() != 2 or x_perm.dtype != torch.bfloat16 or w_gate[0].dim() != 3:
-        _refuse(where, "x_perm [A_max,d] bfloat16 and (q, scale) weights expected")
+    x_scale = None
+    if isinstance(x_perm, (tuple, list)):
+        where = "capmoe_grouped_ffn_fp8_codes"
+        x_perm, x_scale = x_perm
+    if x_perm.dim() != 2 or (x_scale is None and x_perm.dtype != torch.bfloat16) or w_gate[0].dim() != 3:
+        _refuse(where, "x_perm [A_max,d] bfloat16 (or codes and scales) and (q, scale) weights expected")
     A_max, d = x_perm.shape
     F = w_gate[0].shape[1]
     _fits(where, E, d, F)
+    rows = (x_perm,)
+    if x_scale is not None:
+        _coded(where, x_perm, x_scale, (A_max, d), 1)
+        rows = (x_perm, x_scale)
     _coded(where, *w_gate, (E, F, d), QBLOCK)
     _coded(where, *w_up, (E, F, d), QBLOCK)
     _coded(where, *w_down, (E, d, F), QBLOCK)
     y_perm = _out(where, y_perm, (A_max, d), torch.bfloat16, x_perm)
     if ws is None:
         ws = x_perm.new_empty((_ffn_fp8_bytes(A_max, d, F),), dtype=torch.uint8)
-    _run(where, x_perm, x_perm, offsets, E, d, F, *w_gate, *w_up, *w_down, y_perm, A_max, ws,
+    _run(where, x_perm, *rows, offsets, E, d, F, *w_gate, *w_up, *w_down, y_perm, A_max, ws,
          ws.numel() * ws.element_size(), _status(where, dev_status))
     return y_perm
+
+
+# ----------------------------------------------------------------------------- the norm in front of the layer
+def _want(where: str, name: str, t, shape, dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        _refuse(where, f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None, stream=None):
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * w by rows.  x, residual [N,d], w [d] -> dict(y, h, rstd [N] float32), h
+    being x itself without a residual; with fp8 also q, scale: the codes that quantize_rows makes of y.  `out` may hand in any
+    of these buffers (h may be x's or residual's)."""
+    where = "capmoe_rms_norm"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm(x, w, residual, eps, fp8, out)
+    if x.dim() != 2 or w.shape != x.shape[1:] or w.dtype != x.dtype:
+        _refuse(where, "x [N,d] and w [d] of one dtype expected")
+    N, d = x.shape
+    _fits(where, d)
+    _want(where, "residual", residual, x.shape, x.dtype)
+    out = out or {}
+    r = dict(y=_out(where, out.get("y"), x.shape, x.dtype, x), rstd=_out(where, out.get("rstd"), (N,), torch.float32, x))
+    r["h"] = x if residual is None else _out(where, out.get("h"), x.shape, x.dtype, x)
+    if fp8:
+        r["q"] = _out(where, out.get("q"), (N, d), FP8, x)
+        r["scale"] = _out(where, out.get("scale"), (N, _blocks(d)), SCALE, x)
+    _run(where, x, x, residual, w, N, d, _dt(x), eps, None if residual is None else r["h"], r["y"], r["rstd"], r.get("q"), r.get("scale"))
+    return r
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_backward_bytes(device, N, d, dtype):
+    return _bytes("capmoe_rms_norm_backward_workspace_bytes", _i64(N), d, _dt(dtype))
+
+
+def rms_norm_backward_workspace_bytes(N: int, d: int, dtype) -> int:
+    return _bytes("capmoe_rms_norm_backward_workspace_bytes", _i64(N), int(d), _dt(dtype))
+
+
+def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, out_dtype=None, ws=None, stream=None):
+    """Gradients of rms_norm from dy, the h and rstd that it returned and dh, what reaches h from behind (or None).
+    -> (dx [N,d], the gradient of x and of the residual alike, dw [d] in the rows' dtype, or out_dtype (float32))."""
+    where = "capmoe_rms_norm_backward"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm_backward(dy, h, w, rstd, dh, dx, dw, out_dtype, ws)
+    if h.dim() != 2 or w.shape != h.shape[1:] or w.dtype != h.dtype:
+        _refuse(where, "h [N,d] and w [d] of one dtype expected")
+    N, d = h.shape
+    _fits(where, d)
+    _want(where, "dy", dy, h.shape, h.dtype)
+    _want(where, "dh", dh, h.shape, h.dtype)
+    _want(where, "rstd", rstd, (N,), torch.float32)
+    dx = _out(where, dx, h.shape, h.dtype, h)
+    dw = _out(where, dw, (d,), out_dtype or (dw.dtype if dw is not None else h.dtype), h)
+    if ws is None:
+        ws = h.new_empty((_norm_backward_bytes(h.get_device(), N, d, h.dtype),), dtype=torch.uint8)
+    _run(where, h, dy, h, w, rstd, dh, N, d, _dt(h), _dt(dw), dx, dw, ws, ws.numel() * ws.element_size())
+    return dx, dw
+
+
+# ----------------------------------------------------------------------------- permute in 8 bits; gradients of combine, permute, route
+def _slot_rows(where: str, slot_row, N: int):
+    if slot_row.dtype != torch.int32 or slot_row.dim() != 2 or slot_row.shape[0] != N:
+        _refuse(where, "slot_row must be int32 [N,slots]")
+    return slot_row.shape[1]
+
+
+def _route_lists(where: str, scores, topk_idx, slot_row, D: int, token_group):
+    """-> (N, E, k, slots) after the checks of what the route and drop stages left."""
+    if scores.dim() != 2 or scores.dtype != torch.float32 or topk_idx.dim() != 2 or topk_idx.dtype != torch.int32:
+        _refuse(where, "scores [N,E] float32 and topk_idx [N,k] int32 expected")
+    N, E = scores.shape
+    if topk_idx.shape[0] != N:
+        _refuse(where, "scores and topk_idx of one number of tokens expected")
+    _want(where, "token_group", token_group, (N,), torch.int32)
+    return N, E, topk_idx.shape[1], _slot_rows(where, slot_row, N)
+
+
+def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0, token_group=None, out=None, stream=None):
+    """permute of 8-bit rows (rms_norm(fp8=True), quantize_rows).  -> dict(x_q [A_max,d], x_scale [A_max, ceil(d/128)],
+    perm_token [A_max], perm_weight [A_max]); rows >= A are left unwritten.  `out` may hand in those buffers."""
+    where = "capmoe_permute_fp8"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max, D, token_group, out)
+    N, E, k, slots = _route_lists(where, scores, topk_idx, slot_row, D, token_group)
+    if x_q.dim() != 2 or x_q.shape[0] != N:
+        _refuse(where, "x_q [N,d] expected")
+    d = x_q.shape[1]
+    _fits(where, d, D)
+    _coded(where, x_q, x_scale, (N, d), 1)
+    out = out or {}
+    r = dict(x_q=_out(where, out.get("x_q"), (A_max, d), FP8, x_q), x_scale=_out(where, out.get("x_scale"), (A_max, _blocks(d)), SCALE, x_q),
+             perm_token=_out(where, out.get("perm_token"), (A_max,), torch.int32, x_q),
+             perm_weight=_out(where, out.get("perm_weight"), (A_max,), torch.float32, x_q))
+    _run(where, x_q, x_q, x_scale, N, d, E, k, slots, D, A_max, scores, topk_idx, token_group, slot_row, r["x_q"], r["x_scale"],
+         r["perm_token"], r["perm_weight"])
+    return r
+
+
+def combine_backward(dy, y_perm, slot_row, perm_weight, dy_perm=None, dweight=None, stream=None):
+    """Gradients of combine: dy_perm[r] = perm_weight[r] dy[t], dweight[r] = dy[t] . y_perm[r] for the row r of a slot of t.
+    dy [N,d], y_perm [A_max,d] -> (dy_perm [A_max,d], dweight [A_max] float32); rows that no slot names are left as they are
+    (undefined in buffers made here).  The gradient of y_shared is dy."""
+    where = "capmoe_combine_backward"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return combine_backward(dy, y_perm, slot_row, perm_weight, dy_perm, dweight)
+    if dy.dim() != 2 or y_perm.dim() != 2 or y_perm.shape[1] != dy.shape[1] or y_perm.dtype != dy.dtype:
+        _refuse(where, "dy [N,d] and y_perm [A_max,d] of one dtype expected")
+    N, d = dy.shape
+    A_max = y_perm.shape[0]
+    _fits(where, d)
+    slots = _slot_rows(where, slot_row, N)
+    _want(where, "perm_weight", perm_weight, (A_max,), torch.float32)
+    dy_perm = _out(where, dy_perm, (A_max, d), dy.dtype, dy)
+    dweight = _out(where, dweight, (A_max,), torch.float32, dy)
+    _run(where, dy, dy, y_perm, slot_row, perm_weight, N, d, slots, _dt(dy), A_max, dy_perm, dweight)
+    return dy_perm, dweight
+
+
+def permute_backward(dx_perm, slot_row, add=None, dx=None, stream=None):
+    """Gradient of permute: dx[t] = sum of dx_perm over t's rows, plus `add`, a tensor [N,d] or up to two of them (what reaches
+    x through the router or a shared expert).  dx_perm [A_max,d] -> dx [N,d], which may be one of `add`."""
+    where = "capmoe_permute_backward"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return permute_backward(dx_perm, slot_row, add, dx)
+    if dx_perm.dim() != 2:
+        _refuse(where, "dx_perm [A_max,d] expected")
+    A_max, d = dx_perm.shape
+    N = slot_row.shape[0]
+    _fits(where, d)
+    slots = _slot_rows(where, slot_row, N)
+    add = () if add is None else (add,) if isinstance(add, torch.Tensor) else tuple(add)
+    if len(add) > 2:
+        _refuse(where, "at most two tensors to add", EUNSUPPORTED)
+    for t in add:
+        _want(where, "add", t, (N, d), dx_perm.dtype)
+    dx = _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
+    _run(where, dx_perm, dx_perm, slot_row, N, d, slots, _dt(dx_perm), A_max, *(add + (None, None))[:2], dx)
+    return dx
+
+
+@functools.lru_cache(maxsize=1024)
+def _route_backward_bytes(device, N, d, E, dtype):
+    return route_backward_workspace_bytes(N, d, E, dtype)
+
+
+def route_backward_workspace_bytes(N: int, d: int, E: int, dtype) -> int:
+    return _bytes("capmoe_route_backward_workspace_bytes", _i64(N), int(d), int(E), _dt(dtype))
+
+
+def route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D: int = 0, token_group=None, dscores=None, out=None, out_dtype=None,
+                   ws=None, dev_status=None, stream=None):
+    """Gradients of route from dweight [A_max], the gradient of the kept pairs' weights (combine_backward), and dscores, what
+    the scores get besides: [N,E], or [E] for all tokens (a balance loss), or None.  -> dict(dlogits [N,E] float32, dx [N,d],
+    dw [E,d] in the rows' dtype, or out_dtype (float32), dbias [E] float32); `out` may hand in any of them."""
+    where = "capmoe_route_backward"
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D, token_group, dscores, out, out_dtype, ws, dev_status)
+    N, E, k, slots = _route_lists(where, scores, topk_idx, slot_row, D, token_group)
+    if x.dim() != 2 or x.shape[0] != N or w_router.shape != (E, x.shape[1]) or w_router.dtype != x.dtype:
+        _refuse(where, "x [N,d] and w_router [E,d] of one dtype expected")
+    d = x.shape[1]
+    _fits(where, d, D)
+    if dweight.dtype != torch.float32 or dweight.dim() != 1:
+        _refuse(where, "dweight must be float32 [A_max]")
+    ld = 0
+    if dscores is not None and dscores.dim() == 2:
+        ld = E
+    _want(where, "dscores", dscores, (N, E) if ld else (E,), torch.float32)
+    out = out or {}
+    dw = out.get("dw")
+    r = dict(dlogits=_out(where, out.get("dlogits"), (N, E), torch.float32, x), dx=_out(where, out.get("dx"), (N, d), x.dtype, x),
+             dw=_out(where, dw, (E, d), out_dtype or (dw.dtype if dw is not None else x.dtype), x),
+             dbias=_out(where, out.get("dbias"), (E,), torch.float32, x))
+    if ws is None:
+        ws = x.new_empty((_route_backward_bytes(x.get_device(), N, d, E, x.dtype),), dtype=torch.uint8)
+    _run(where, x, x, w_router, scores, topk_idx, slot_row, dweight, N, d, E, k, slots, D, token_group, dscores, ld, _dt(x), _dt(r["dw"]),
+         dweight.shape[0], r["dlogits"], r["dx"], r["dw"], r["dbias"], ws, ws.numel() * ws.element_size(), _status(where, dev_status))
+    return r
 
 
 # ----------------------------------------------------------------------------- expert parallelism

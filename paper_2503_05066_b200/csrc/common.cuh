@@ -50,6 +50,9 @@ int permute_impl(const void* x, int64_t N, int d, int E, int k, int slots, int D
                  const int32_t* topk_idx, const int32_t* token_group, const int32_t* slot_row, void* x_perm,
                  int32_t* perm_token, float* perm_weight, uint64_t* keep_mask_out, void* stream);
 
+// out[c] = sum over g < parts of part[g * d + c], in a fixed order (norm.cu).
+int sum_parts(const float* part, int64_t parts, int d, int out_dtype, void* out, cudaStream_t st);
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t elt_size(int dtype) { return dtype == CAPMOE_F32 ? 4 : 2; }
 inline cudaStream_t as_stream(void* s) { return reinterpret_cast<cudaStream_t>(s); }

@@ -320,37 +320,61 @@ extern "C" int capmoe_ffn_fp8_workspace_bytes(int64_t A_max, int d, int F, size_
   return CAPMOE_OK;
 }
 
+namespace {
+// The 8-bit FFN from rows (x, quantised here) or, with x NULL, from their codes and scales.
+int ffn_fp8(const void* x, const void* x_q, const void* x_scale, const int32_t* offsets, int E, int d, int F, const uint8_t* wg, const uint8_t* wgs,
+            const uint8_t* wu, const uint8_t* wus, const uint8_t* wd, const uint8_t* wds, void* y, int64_t A_max, void* ws, size_t ws_bytes,
+            int32_t* dev_status, cudaStream_t st) {
+  const FfnWs w = ffn_ws(A_max, d, F);
+  if (ws_bytes < w.total) return CAPMOE_EWORKSPACE;
+  const Segments sg{offsets, E, (int)A_max};
+  uint8_t* b = (uint8_t*)ws;
+  const bool tc = gmm8_supported(d, F);
+  int rc = CAPMOE_OK;
+  int32_t* counters = counters_of(sg, dev_status);
+  if (tc && (rc = begin_counters(counters, 2, st)) != CAPMOE_OK) return rc;
+  const uint8_t *xq = (const uint8_t*)x_q, *xs = (const uint8_t*)x_scale;
+  int64_t xs_ld = ceil_div(d, QBLOCK);
+  if (x) {
+    if ((rc = quantize_rows_run<__nv_bfloat16>(x, offsets + E, A_max, d, b + w.xq, b + w.xs, w.xs_ld, st)) != CAPMOE_OK) return rc;
+    xq = b + w.xq; xs = b + w.xs; xs_ld = w.xs_ld;
+  }
+  if (tc) {
+    // without the quantiser the gate/up product is the first kernel that is sure to wait for what came before this call, and it
+    // may let the next one start sooner than that: neither starts early then (gmm.cuh)
+    const bool early = x != nullptr;
+    rc = gmm8_swiglu(xq, xs, xs_ld, sg, wg, wgs, wu, wus, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(counters, 0), early, st);
+    if (rc != CAPMOE_OK) return rc;
+    return gmm8(b + w.hq, b + w.hs, w.hs_ld, sg, wd, wds, F, d, y, dev_status, counter_at(counters, 1), early, st);
+  }
+  float* h = (float*)(b + w.h);
+  rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, xq, xs, wg, wgs, wu, wus, h, sg, d, F);
+  if (rc != CAPMOE_OK) return rc;
+  rc = quantize_rows_run<float>(h, offsets + E, A_max, F, b + w.hq, b + w.hs, w.hs_ld, st);
+  if (rc != CAPMOE_OK) return rc;
+  const uint8_t* none = nullptr;
+  return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, d, st, b + w.hq, b + w.hs, wd, wds, none, none, (__nv_bfloat16*)y, sg, F, d);
+}
+}  // namespace
+
 extern "C" int capmoe_grouped_ffn_fp8(const void* x_perm, const int32_t* expert_offsets, int E, int d, int F, const void* wg_q,
                                       const void* wg_scale, const void* wu_q, const void* wu_scale, const void* wd_q,
                                       const void* wd_scale, void* y_perm, int64_t A_max, void* ws, size_t ws_bytes,
                                       int32_t* dev_status, void* stream) {
-  int rc = check_shape(expert_offsets, E, d, F, A_max);
+  const int rc = check_shape(expert_offsets, E, d, F, A_max);
   if (rc != CAPMOE_OK || A_max == 0) return rc;
   if (!usable(x_perm, wg_q, wu_q, wd_q, y_perm, ws) || !wg_scale || !wu_scale || !wd_scale) return CAPMOE_EINVAL;
-  const FfnWs w = ffn_ws(A_max, d, F);
-  if (ws_bytes < w.total) return CAPMOE_EWORKSPACE;
-  const Segments sg{expert_offsets, E, (int)A_max};
-  cudaStream_t st = as_stream(stream);
-  uint8_t* b = (uint8_t*)ws;
-  const bool tc = gmm8_supported(d, F);
-  int32_t* counters = counters_of(sg, dev_status);
-  if (tc && (rc = begin_counters(counters, 2, st)) != CAPMOE_OK) return rc;
-  rc = quantize_rows_run<__nv_bfloat16>(x_perm, expert_offsets + E, A_max, d, b + w.xq, b + w.xs, w.xs_ld, st);
-  if (rc != CAPMOE_OK) return rc;
-  if (tc) {
-    rc = gmm8_swiglu(b + w.xq, b + w.xs, w.xs_ld, sg, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
-                        (const uint8_t*)wu_scale, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(counters, 0), true, st);
-    if (rc != CAPMOE_OK) return rc;
-    return gmm8(b + w.hq, b + w.hs, w.hs_ld, sg, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, F, d, y_perm, dev_status,
-                counter_at(counters, 1), true, st);
-  }
-  float* h = (float*)(b + w.h);
-  rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, b + w.xq, b + w.xs, (const uint8_t*)wg_q, (const uint8_t*)wg_scale,
-                    (const uint8_t*)wu_q, (const uint8_t*)wu_scale, h, sg, d, F);
-  if (rc != CAPMOE_OK) return rc;
-  rc = quantize_rows_run<float>(h, expert_offsets + E, A_max, F, b + w.hq, b + w.hs, w.hs_ld, st);
-  if (rc != CAPMOE_OK) return rc;
-  const uint8_t* none = nullptr;
-  return launch_tiles(k_mm_fp8<__nv_bfloat16, false>, sg, d, st, b + w.hq, b + w.hs, (const uint8_t*)wd_q,
-                      (const uint8_t*)wd_scale, none, none, (__nv_bfloat16*)y_perm, sg, F, d);
+  return ffn_fp8(x_perm, nullptr, nullptr, expert_offsets, E, d, F, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
+                 (const uint8_t*)wu_scale, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, y_perm, A_max, ws, ws_bytes, dev_status, as_stream(stream));
+}
+
+extern "C" int capmoe_grouped_ffn_fp8_codes(const void* x_q, const void* x_scale, const int32_t* expert_offsets, int E, int d, int F,
+                                            const void* wg_q, const void* wg_scale, const void* wu_q, const void* wu_scale, const void* wd_q,
+                                            const void* wd_scale, void* y_perm, int64_t A_max, void* ws, size_t ws_bytes, int32_t* dev_status,
+                                            void* stream) {
+  const int rc = check_shape(expert_offsets, E, d, F, A_max);
+  if (rc != CAPMOE_OK || A_max == 0) return rc;
+  if (!usable(x_q, wg_q, wu_q, wd_q, y_perm, ws) || !x_scale || !wg_scale || !wu_scale || !wd_scale) return CAPMOE_EINVAL;
+  return ffn_fp8(nullptr, x_q, x_scale, expert_offsets, E, d, F, (const uint8_t*)wg_q, (const uint8_t*)wg_scale, (const uint8_t*)wu_q,
+                 (const uint8_t*)wu_scale, (const uint8_t*)wd_q, (const uint8_t*)wd_scale, y_perm, A_max, ws, ws_bytes, dev_status, as_stream(stream));
 }

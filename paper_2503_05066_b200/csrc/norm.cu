@@ -1,0 +1,386 @@
+// Root-mean-square norm of the rows in front of an expert layer, with the residual's addition and the 8-bit codes that the
+// expert products read, and its gradients.
+//   h = x + residual (rounded to the storage type: what the residual stream keeps)
+//   rstd = (sum_c h_c^2 / d + eps)^(-1/2),  y = h rstd w,  codes of the rounded y as capmoe_quantize_rows makes them
+//   dx = rstd (g - h rstd^2 (sum_c g_c h_c) / d) + dh with g = dy w,  dw = sum over the rows of dy h rstd
+// All of it in fp32; what is stored has one rounding (h, y, dx) or none before the last (rstd, dw).
+#include "gmm.cuh"
+#include "rowvec.cuh"
+
+namespace capmoe {
+namespace {
+
+constexpr int NW = 8;                        // warps of a block, `wpr` of them to a row (a row of 16 warps is a block of its own)
+constexpr int NT_MAX = 512;
+constexpr int NORM_MAX_D = 16384;
+
+// The NV columns from p on, as they are stored: one 16-byte access with VEC, else the first `left` one by one.
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 get_cells(const T* p, int left) {
+  if constexpr (VEC) {
+    return __ldcs(reinterpret_cast<const uint4*>(p));
+  } else {
+    float f[Vec16<T>::n];
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::n; ++i) f[i] = i < left ? to_float(p[i]) : 0.f;
+    return Vec16<T>::store(f);
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void put_cells(T* p, int left, const uint4& v) {
+  if constexpr (VEC) {
+    *reinterpret_cast<uint4*>(p) = v;
+  } else {
+    float f[Vec16<T>::n];
+    Vec16<T>::load(v, f);
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::n; ++i)
+      if (i < left) p[i] = from_float<T>(f[i]);
+  }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// Sum over the wpr warps of a row (a power of two), the same bits in all of them.  `red`: a word per warp of the block.
+__device__ __forceinline__ float row_sum(float v, int wpr, float* red) {
+  v = warp_sum(v);
+  if (wpr > 1) {
+    const int warp = threadIdx.x >> 5, first = warp & ~(wpr - 1);
+    if ((threadIdx.x & 31) == 0) red[warp] = v;
+    __syncthreads();
+    v = 0.f;
+    for (int i = 0; i < wpr; ++i) v += red[first + i];
+  }
+  return v;
+}
+
+// Codes of NV columns under the scale of their block of 128 (16 lanes of bf16, 32 of fp32), which is made here.
+template <typename T, bool VEC>
+__device__ __forceinline__ void put_codes(const uint4& v, int c, int d, uint8_t* q, uint8_t* scale) {
+  constexpr int NV = Vec16<T>::n, LANES = QBLOCK / NV;
+  float f[NV];
+  Vec16<T>::load(v, f);
+  uint32_t m = 0;                            // of non-negative floats the larger has the larger pattern; NaN is above all
+#pragma unroll
+  for (int i = 0; i < NV; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (c >= d) return;
+  const uint32_t code = scale_code(m);
+  uint32_t b[NV / 4];
+  const float inv = inv_scale(code == (uint32_t)Q_NAN_SCALE ? 127u : code);
+#pragma unroll
+  for (int i = 0; i < NV / 4; ++i)
+    b[i] = code == (uint32_t)Q_NAN_SCALE ? 0x7f7f7f7fu
+                                         : to_e4m3x2(f[4 * i] * inv, f[4 * i + 1] * inv) | to_e4m3x2(f[4 * i + 2] * inv, f[4 * i + 3] * inv) << 16;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < NV / 4; ++i) reinterpret_cast<uint32_t*>(q + c)[i] = b[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (c + i < d) q[c + i] = (uint8_t)(b[i / 4] >> (8 * (i & 3)));
+  }
+  if ((threadIdx.x & (LANES - 1)) == 0) scale[c / QBLOCK] = (uint8_t)code;
+}
+
+template <typename T>
+struct NormArgs {
+  const T *x, *res, *w;
+  int64_t N;
+  int d, wpr;
+  float eps;
+  T *h, *y;
+  float* rstd;
+  uint8_t *q, *scale;
+};
+
+// A row stays in the registers of its warps between the two uses, VPT vectors a thread: one pass over HBM.
+template <typename T, bool VEC, int VPT>
+__global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  constexpr int NV = Vec16<T>::n;
+  __shared__ float red[NT_MAX / 32];
+  const int tpr = a.wpr * 32, t = threadIdx.x & (tpr - 1), d = a.d;
+  const int64_t row = (int64_t)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr;
+  const bool live = row < a.N;
+  const int64_t at = row * d;
+  uint4 v[VPT];
+#pragma unroll
+  for (int u = 0; u < VPT; ++u) {
+    const int c = (u * tpr + t) * NV;
+    v[u] = live && c < d ? get_cells<T, VEC>(a.x + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (a.res) {
+    uint4 r[VPT];
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      const int c = (u * tpr + t) * NV;
+      r[u] = live && c < d ? get_cells<T, VEC>(a.res + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      const int c = (u * tpr + t) * NV;
+      float f[NV], g[NV];
+      Vec16<T>::load(v[u], f);
+      Vec16<T>::load(r[u], g);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f[i] += g[i];
+      v[u] = Vec16<T>::store(f);
+      if (live && c < d) put_cells<T, VEC>(a.h + at + c, d - c, v[u]);
+    }
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int u = 0; u < VPT; ++u) {
+    float f[NV];
+    Vec16<T>::load(v[u], f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) sum = fmaf(f[i], f[i], sum);
+  }
+  const float rstd = rsqrtf(row_sum(sum, a.wpr, red) / (float)d + a.eps);
+  if (!live) return;                         // whole warps; nothing below crosses a warp
+  if (a.rstd && t == 0) a.rstd[row] = rstd;
+  const int nb = (d + QBLOCK - 1) / QBLOCK;
+#pragma unroll
+  for (int u = 0; u < VPT; ++u) {
+    const int c = (u * tpr + t) * NV;
+    float f[NV], g[NV];
+    Vec16<T>::load(v[u], f);
+    Vec16<T>::load(c < d ? (VEC ? __ldg(reinterpret_cast<const uint4*>(a.w + c)) : get_cells<T, false>(a.w + c, d - c)) : make_uint4(0u, 0u, 0u, 0u), g);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f[i] = f[i] * rstd * g[i];
+    const uint4 y = Vec16<T>::store(f);
+    if (c < d) put_cells<T, VEC>(a.y + at + c, d - c, y);
+    if (a.q) put_codes<T, VEC>(y, c, d, a.q + at, a.scale + row * nb);
+  }
+}
+
+template <typename T>
+struct GradArgs {
+  const T *dy, *h, *w;
+  const float* rstd;
+  const T* dh;
+  int64_t N;
+  int d, wpr;
+  T* dx;
+  float* part;                               // [groups of warps][d]
+};
+
+// A group of wpr warps walks its rows, a thread's columns are the same in all of them: dw is summed in registers, and
+// written once per group for k_sum_parts to join in a fixed order.
+template <typename T, bool VEC, int VPT>
+__global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  constexpr int NV = Vec16<T>::n;
+  __shared__ float red[2][NT_MAX / 32];
+  const int tpr = a.wpr * 32, t = threadIdx.x & (tpr - 1), d = a.d;
+  const int64_t group = (int64_t)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr, groups = (int64_t)gridDim.x * (blockDim.x / tpr);
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  uint4 w[VPT];
+  float dw[VPT][NV];
+#pragma unroll
+  for (int u = 0; u < VPT; ++u) {
+    const int c = (u * tpr + t) * NV;
+    w[u] = c < d ? get_cells<T, VEC>(a.w + c, d - c) : zero;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) dw[u][i] = 0.f;
+  }
+  int it = 0;
+  for (int64_t row0 = 0; row0 < a.N; row0 += groups, it ^= 1) {      // the same count in all warps of the block
+    const int64_t row = row0 + group, at = row * d;
+    const bool live = row < a.N;
+    const float rstd = live ? a.rstd[row] : 0.f;
+    uint4 dy[VPT], h[VPT], dh[VPT];
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      const int c = (u * tpr + t) * NV;
+      const bool in = live && c < d;
+      dy[u] = in ? get_cells<T, VEC>(a.dy + at + c, d - c) : zero;
+      h[u] = in ? get_cells<T, VEC>(a.h + at + c, d - c) : zero;
+      dh[u] = in && a.dh ? get_cells<T, VEC>(a.dh + at + c, d - c) : zero;
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      float p[NV], q[NV], g[NV];
+      Vec16<T>::load(dy[u], p);
+      Vec16<T>::load(h[u], q);
+      Vec16<T>::load(w[u], g);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const float n = q[i] * rstd;
+        dot = fmaf(p[i] * g[i], n, dot);
+        dw[u][i] = fmaf(p[i], n, dw[u][i]);
+      }
+    }
+    const float mean = row_sum(dot, a.wpr, red[it]) / (float)d;
+    if (!live) continue;
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      const int c = (u * tpr + t) * NV;
+      float p[NV], q[NV], g[NV], e[NV];
+      Vec16<T>::load(dy[u], p);
+      Vec16<T>::load(h[u], q);
+      Vec16<T>::load(w[u], g);
+      Vec16<T>::load(dh[u], e);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) p[i] = fmaf(rstd, p[i] * g[i] - q[i] * rstd * mean, e[i]);
+      if (c < d) put_cells<T, VEC>(a.dx + at + c, d - c, Vec16<T>::store(p));
+    }
+  }
+  float* part = a.part + group * d;
+#pragma unroll
+  for (int u = 0; u < VPT; ++u) {
+    const int c = (u * tpr + t) * NV;
+#pragma unroll
+    for (int i = 0; i < NV; i += 4) {
+      if (VEC && c < d) *reinterpret_cast<float4*>(part + c + i) = make_float4(dw[u][i], dw[u][i + 1], dw[u][i + 2], dw[u][i + 3]);
+      if (!VEC) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + i + j < d) part[c + i + j] = dw[u][i + j];
+      }
+    }
+  }
+}
+
+// out[c] = sum over g of part[g][c]: a block per 32 columns, 32 threads to a column, then the 32 sums in their order.
+template <typename TO>
+__global__ void __launch_bounds__(1024) k_sum_parts(const float* __restrict__ part, int64_t parts, int d, TO* __restrict__ out) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  __shared__ float sum[32][33];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+  float s = 0.f;
+  if (c < d)
+#pragma unroll 4
+    for (int64_t g = r; g < parts; g += 32) s += part[g * d + c];
+  sum[r][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (r == 0 && c < d) {
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += sum[i][threadIdx.x & 31];
+    out[c] = from_float<TO>(s);
+  }
+}
+
+constexpr int NORM_VPT = 8;                  // vectors a thread that a row's warps are chosen for, with many rows
+constexpr int GRAD_VPT = 2;                  // the same of the gradient, whose threads also hold dw and w
+constexpr int GRAD_BLOCKS = 4;               // blocks per SM at most
+// Warps to a row: as few as hold it in `vpt` vectors a thread, more while the rows leave warps of the device without one; 16
+// where eight would have to hold more than `most` vectors a thread.
+int warps_per_row(int64_t N, int vecs, int vpt, int most) {
+  int wpr = 1;
+  while (wpr < NW && vecs > 32 * wpr && (vecs > 32 * wpr * vpt || N * wpr < (int64_t)sm_count() * NW)) wpr *= 2;
+  return vecs > 32 * NW * most ? 2 * NW : wpr;
+}
+int norm_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, NORM_VPT, 8); }
+int grad_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, GRAD_VPT, 4); }
+int rows_per_block(int wpr) { return wpr < NW ? NW / wpr : 1; }
+unsigned threads_of(int wpr) { return 32u * (unsigned)(wpr < NW ? NW : wpr); }
+int vecs_of(int d, int dtype) { return (int)ceil_div((int64_t)d * (int64_t)elt_size(dtype), 16); }
+int grad_blocks(int64_t N, int wpr) {
+  const int64_t want = ceil_div(N, rows_per_block(wpr)), most = (int64_t)sm_count() * GRAD_BLOCKS;
+  return (int)(want < most ? want : most);
+}
+
+template <typename T, bool VEC>
+int norm_run(const NormArgs<T>& a, cudaStream_t st) {
+  const int vpt = (int)ceil_div(ceil_div(a.d, Vec16<T>::n), 32 * a.wpr);
+  const int64_t blocks = ceil_div(a.N, rows_per_block(a.wpr));
+  if (blocks > 0x7fffffff) return CAPMOE_EUNSUPPORTED;
+  auto k = vpt <= 1 ? k_rms_norm<T, VEC, 1> : vpt <= 2 ? k_rms_norm<T, VEC, 2> : vpt <= 4 ? k_rms_norm<T, VEC, 4> : k_rms_norm<T, VEC, 8>;
+  const int rc = note_cuda(launch_chained(k, (unsigned)blocks, threads_of(a.wpr), 0, st, a));
+  count_launch(1);
+  return rc;
+}
+template <typename T>
+int norm(const void* x, const void* res, const void* w, int64_t N, int d, float eps, void* h, void* y, float* rstd, void* q, void* scale,
+         int dtype, cudaStream_t st) {
+  const NormArgs<T> a{(const T*)x, (const T*)res, (const T*)w, N, d, norm_warps(N, vecs_of(d, dtype)), eps, (T*)h, (T*)y, rstd,
+                      (uint8_t*)q, (uint8_t*)scale};
+  return d % Vec16<T>::n == 0 ? norm_run<T, true>(a, st) : norm_run<T, false>(a, st);
+}
+
+template <typename T, bool VEC>
+int grad_run(const GradArgs<T>& a, cudaStream_t st) {
+  const int vpt = (int)ceil_div(ceil_div(a.d, Vec16<T>::n), 32 * a.wpr);
+  auto k = vpt <= 1 ? k_rms_norm_grad<T, VEC, 1> : vpt <= 2 ? k_rms_norm_grad<T, VEC, 2> : vpt <= 4 ? k_rms_norm_grad<T, VEC, 4>
+                                                                                              : k_rms_norm_grad<T, VEC, 8>;
+  const int rc = note_cuda(launch_chained(k, (unsigned)grad_blocks(a.N, a.wpr), threads_of(a.wpr), 0, st, a));
+  count_launch(1);
+  return rc;
+}
+template <typename T>
+int norm_grad(const void* dy, const void* h, const void* w, const float* rstd, const void* dh, int64_t N, int d, int dtype, int out_dtype,
+              void* dx, void* dw, float* part, cudaStream_t st) {
+  const GradArgs<T> a{(const T*)dy, (const T*)h, (const T*)w, rstd, (const T*)dh, N, d, grad_warps(N, vecs_of(d, dtype)), (T*)dx, part};
+  const int rc = d % Vec16<T>::n == 0 ? grad_run<T, true>(a, st) : grad_run<T, false>(a, st);
+  if (rc != CAPMOE_OK) return rc;
+  return sum_parts(part, (int64_t)grad_blocks(N, a.wpr) * rows_per_block(a.wpr), d, out_dtype, dw, st);
+}
+
+int check_norm(int64_t N, int d, int dtype) {
+  if (N < 0 || d < 1) return CAPMOE_EINVAL;
+  if ((dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) || d > NORM_MAX_D) return CAPMOE_EUNSUPPORTED;
+  return CAPMOE_OK;
+}
+template <class... P>
+bool usable(P... p) {
+  return ((p != nullptr && aligned16(p)) && ...);
+}
+
+}  // namespace
+
+int sum_parts(const float* part, int64_t parts, int d, int out_dtype, void* out, cudaStream_t st) {
+  const unsigned grid = (unsigned)ceil_div(d, 32);
+  const int rc = note_cuda(out_dtype == CAPMOE_F32 ? launch_chained(k_sum_parts<float>, grid, 1024, 0, st, part, parts, d, (float*)out)
+                                                   : launch_chained(k_sum_parts<__nv_bfloat16>, grid, 1024, 0, st, part, parts, d, (__nv_bfloat16*)out));
+  count_launch(1);
+  return rc;
+}
+
+}  // namespace capmoe
+
+using namespace capmoe;
+
+extern "C" int capmoe_rms_norm(const void* x, const void* residual, const void* w, int64_t N, int d, int dtype, float eps, void* h, void* y,
+                               float* rstd, void* q, void* scale, void* stream) {
+  const int rc = check_norm(N, d, dtype);
+  if (rc != CAPMOE_OK) return rc;
+  if (!(eps >= 0.f)) return CAPMOE_EINVAL;
+  if (N == 0) return CAPMOE_OK;
+  if (!usable(x, w, y) || !aligned16(residual) || !aligned16(h) || !aligned16(q)) return CAPMOE_EINVAL;
+  if (!residual != !h || !q != !scale) return CAPMOE_EINVAL;
+  if (dtype == CAPMOE_F32) return norm<float>(x, residual, w, N, d, eps, h, y, rstd, q, scale, dtype, as_stream(stream));
+  return norm<__nv_bfloat16>(x, residual, w, N, d, eps, h, y, rstd, q, scale, dtype, as_stream(stream));
+}
+
+extern "C" int capmoe_rms_norm_backward_workspace_bytes(int64_t N, int d, int dtype, size_t* bytes) {
+  const int rc = check_norm(N, d, dtype);
+  if (!bytes) return CAPMOE_EINVAL;
+  if (rc != CAPMOE_OK) return rc;
+  const int wpr = grad_warps(N, vecs_of(d, dtype));
+  *bytes = (size_t)grad_blocks(N, wpr) * (size_t)rows_per_block(wpr) * (size_t)d * sizeof(float);
+  return CAPMOE_OK;
+}
+
+extern "C" int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const float* rstd, const void* dh, int64_t N, int d,
+                                        int dtype, int out_dtype, void* dx, void* dw, void* ws, size_t ws_bytes, void* stream) {
+  size_t need = 0;
+  const int rc = capmoe_rms_norm_backward_workspace_bytes(N, d, dtype, &need);
+  if (rc != CAPMOE_OK) return rc;
+  if (out_dtype != CAPMOE_F32 && (out_dtype != CAPMOE_BF16 || dtype != CAPMOE_BF16)) return CAPMOE_EUNSUPPORTED;
+  if (!dw) return CAPMOE_EINVAL;
+  if (N == 0) return note_cuda(cudaMemsetAsync(dw, 0, (size_t)d * elt_size(out_dtype), as_stream(stream)));
+  if (!usable(dy, h, w, dx, ws) || !rstd || !aligned16(dh)) return CAPMOE_EINVAL;
+  if (ws_bytes < need) return CAPMOE_EWORKSPACE;
+  if (dtype == CAPMOE_F32) return norm_grad<float>(dy, h, w, rstd, dh, N, d, dtype, out_dtype, dx, dw, (float*)ws, as_stream(stream));
+  return norm_grad<__nv_bfloat16>(dy, h, w, rstd, dh, N, d, dtype, out_dtype, dx, dw, (float*)ws, as_stream(stream));
+}

@@ -3,7 +3,7 @@
 // Work unit = (token, 2 KB chunk of its row): one warp per unit, four 16-byte vectors per lane,
 // so that the number of units (N * row bytes / 2 KB) is many times the number of resident warps
 // and the last wave stays full.  Each x row is read once and written to every row that keeps it.
-#include "common.cuh"
+#include "rowvec.cuh"
 
 namespace capmoe {
 namespace {
@@ -93,37 +93,6 @@ k_permute(const uint4* __restrict__ x, int64_t N, int row_vecs /* 16-byte vector
     }
   }
 }
-
-template <typename T> struct Vec16;
-template <> struct Vec16<float> {
-  static constexpr int n = 4;
-  static __device__ __forceinline__ void load(const uint4& v, float* f) {
-    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
-  }
-  static __device__ __forceinline__ uint4 store(const float* f) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-  }
-};
-template <> struct Vec16<__nv_bfloat16> {
-  static constexpr int n = 8;
-  static __device__ __forceinline__ void load(const uint4& v, float* f) {
-    const unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ uint4 store(const float* f) {
-    unsigned w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-      w[i] = *reinterpret_cast<unsigned*>(&p);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
-};
 
 // acc[u] += wgt * row[u] for the VPL vectors of one kept row
 template <typename T>
