@@ -381,7 +381,7 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  *                              dS[t,e] = dscores[t,e] + dweight[row of (t,e)],  dlogits = S (dS - sum_f S_f dS_f) [N,E] fp32,
  *                              dx = dlogits W_r [N,d] `dtype`,  dw = dlogits^T x [E,d] out_dtype (`dtype`, or CAPMOE_F32),
  *                              dbias = sum_t dlogits [E] fp32.
- *                            bf16: dlogits enter the products as the sum of two bf16 numbers each (2^-17 of them is lost).
+ *                            bf16: dlogits enter the products as the sum of two bf16 numbers each (at most 2^-16 of them is lost).
  *                            N = 0 leaves zeros in dw and dbias.  All sums have a fixed order for given sizes and device.
  *                            ws: capmoe_route_backward_workspace_bytes(N,d,E,dtype) bytes on the device that is current.
  * The first three: rows of whole 16-byte vectors, slots <= 288, N and A_max < 2^31.  route_backward: E <= 256, k <= 32,

@@ -1157,6 +1157,29 @@ class MoELayer:
                "capmoe_layer_forward_host")
         return y_host
 
+    def backward(self, dy, dscores=None, out_dtype=None):
+        """Gradients of the layer's last forward() from dy [N,d], the gradient of y, and dscores ([N,E] or [E]), what the router's
+        scores get besides (a balance loss).  The forward's buffers must be as it left them.  -> dict(dx [N,d], dw_router, dbias,
+        dw_gate, dw_up, dw_down, dlogits, and for a shared expert dws_gate, dws_up, dws_down); the router's weights' gradient in
+        out_dtype (float32) or the activations' dtype."""
+        t = self.t
+        status = t["dev_status"]
+        dy_perm, dweight = combine_backward(dy, t["y_perm"], t["slot_row"], t["perm_weight"])
+        dx_perm, dwg, dwu, dwd = grouped_ffn_backward(t["x_perm"], dy_perm, t["expert_offsets"], t["w_gate"], t["w_up"], t["w_down"],
+                                                      dev_status=status)
+        r = route_backward(t["x"], t["w_router"], t["scores"], t["topk_idx"], t["slot_row"], dweight,
+                           D=self.D if self.slots > self.k else 0, dscores=dscores, out_dtype=out_dtype, dev_status=status)
+        g = dict(dw_router=r["dw"], dbias=r["dbias"], dw_gate=dwg, dw_up=dwu, dw_down=dwd, dlogits=r["dlogits"])
+        add = (r["dx"],)
+        if "ws_gate" in t:
+            d = t["x"].shape[1]
+            wg, wu, wd = t["ws_gate"].view(1, -1, d), t["ws_up"].view(1, -1, d), t["ws_down"].view(1, d, -1)
+            dxs, dsg, dsu, dsd = grouped_ffn_backward(t["x"], dy, t["one_segment"], wg, wu, wd, dev_status=status)
+            g.update(dws_gate=dsg.view_as(t["ws_gate"]), dws_up=dsu.view_as(t["ws_up"]), dws_down=dsd.view_as(t["ws_down"]))
+            add += (dxs,)
+        g["dx"] = permute_backward(dx_perm, t["slot_row"], add=add, dx=r["dx"])
+        return g
+
     def check_device_status(self):
         s = int(self.t["dev_status"][0].item())
         if s != OK:

@@ -4,8 +4,8 @@
 //   dl[t,e] = S[t,e] (dS[t,e] - sum_f S[t,f] dS[t,f])
 //   dx = dl W_r,   dW_r = dl^T x,   dbias = sum_t dl
 // The two products run as grouped products of one expert (dx) and of ranges of tokens (dW_r, added in their order here).
-// bf16: dl is fp32, and one rounding to bf16 would cost its gradients 2^-9 each; it goes in as two bf16 numbers, its rounding
-// and the rounding of what that leaves out (2^-17 of dl), side by side as 2E columns, against W_r twice.
+// bf16: dl is fp32, and one rounding to bf16 could cost it 2^-8; it goes in as two bf16 numbers, its rounding and the
+// rounding of what that leaves out (2^-16 of dl is lost at most), side by side as 2E columns, against W_r twice.
 #include "gmm.cuh"
 #include "rowvec.cuh"
 
