@@ -737,18 +737,27 @@ def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None
     if stream is not None:
         with torch.cuda.stream(stream):
             return rms_norm(x, w, residual, eps, fp8, out)
-    if x.dim() != 2 or w.shape != x.shape[1:] or w.dtype != x.dtype:
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2 or w.dim() != 1 or w.shape[0] != shape[1] or w.dtype != dtype:
         _refuse(where, "x [N,d] and w [d] of one dtype expected")
-    N, d = x.shape
-    _fits(where, d)
-    _want(where, "residual", residual, x.shape, x.dtype)
-    out = out or {}
-    r = dict(y=_out(where, out.get("y"), x.shape, x.dtype, x), rstd=_out(where, out.get("rstd"), (N,), torch.float32, x))
-    r["h"] = x if residual is None else _out(where, out.get("h"), x.shape, x.dtype, x)
-    if fp8:
-        r["q"] = _out(where, out.get("q"), (N, d), FP8, x)
-        r["scale"] = _out(where, out.get("scale"), (N, _blocks(d)), SCALE, x)
-    _run(where, x, x, residual, w, N, d, _dt(x), eps, None if residual is None else r["h"], r["y"], r["rstd"], r.get("q"), r.get("scale"))
+    N, d = shape
+    _want(where, "residual", residual, shape, dtype)
+    r = dict(h=x)
+    if out is None:                           # (allocations are most of the call's time: the cheapest form of each)
+        r["y"] = y = torch.empty_like(x)
+        r["rstd"] = rstd = torch.empty(N, dtype=torch.float32, device=x.device)
+        if residual is not None:
+            r["h"] = torch.empty_like(x)
+        if fp8:
+            r["q"], r["scale"] = torch.empty_like(x, dtype=FP8), torch.empty(N, _blocks(d), dtype=SCALE, device=x.device)
+    else:
+        r["y"] = y = _out(where, out.get("y"), shape, dtype, x)
+        r["rstd"] = rstd = _out(where, out.get("rstd"), (N,), torch.float32, x)
+        if residual is not None:
+            r["h"] = _out(where, out.get("h"), shape, dtype, x)
+        if fp8:
+            r["q"], r["scale"] = _out(where, out.get("q"), shape, FP8, x), _out(where, out.get("scale"), (N, _blocks(d)), SCALE, x)
+    _run(where, x, x, residual, w, N, d, _dt(dtype), eps, None if residual is None else r["h"], y, rstd, r.get("q"), r.get("scale"))
     return r
 
 
@@ -768,18 +777,25 @@ def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, out_dtype=None,
     if stream is not None:
         with torch.cuda.stream(stream):
             return rms_norm_backward(dy, h, w, rstd, dh, dx, dw, out_dtype, ws)
-    if h.dim() != 2 or w.shape != h.shape[1:] or w.dtype != h.dtype:
+    shape, dtype = h.shape, h.dtype
+    if len(shape) != 2 or w.dim() != 1 or w.shape[0] != shape[1] or w.dtype != dtype:
         _refuse(where, "h [N,d] and w [d] of one dtype expected")
-    N, d = h.shape
-    _fits(where, d)
-    _want(where, "dy", dy, h.shape, h.dtype)
-    _want(where, "dh", dh, h.shape, h.dtype)
+    N, d = shape
+    _want(where, "dy", dy, shape, dtype)
+    _want(where, "dh", dh, shape, dtype)
     _want(where, "rstd", rstd, (N,), torch.float32)
-    dx = _out(where, dx, h.shape, h.dtype, h)
-    dw = _out(where, dw, (d,), out_dtype or (dw.dtype if dw is not None else h.dtype), h)
+    dx = torch.empty_like(h) if dx is None else _out(where, dx, shape, dtype, h)
+    if dw is None:
+        dw = torch.empty(d, dtype=out_dtype or dtype, device=h.device)
+    else:
+        _out(where, dw, (d,), out_dtype or dw.dtype, h)
+    code = _dt(dtype)
     if ws is None:
-        ws = h.new_empty((_norm_backward_bytes(h.get_device(), N, d, h.dtype),), dtype=torch.uint8)
-    _run(where, h, dy, h, w, rstd, dh, N, d, _dt(h), _dt(dw), dx, dw, ws, ws.numel() * ws.element_size())
+        size = _norm_backward_bytes(h.get_device(), N, d, dtype)
+        ws = torch.empty(size, dtype=torch.uint8, device=h.device)
+    else:
+        size = ws.numel() * ws.element_size()
+    _run(where, h, dy, h, w, rstd, dh, N, d, code, _dt(dw), dx, dw, ws, size)
     return dx, dw
 
 
@@ -813,11 +829,17 @@ def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0
         _refuse(where, "x_q [N,d] expected")
     d = x_q.shape[1]
     _fits(where, d, D)
-    _coded(where, x_q, x_scale, (N, d), 1)
-    out = out or {}
-    r = dict(x_q=_out(where, out.get("x_q"), (A_max, d), FP8, x_q), x_scale=_out(where, out.get("x_scale"), (A_max, _blocks(d)), SCALE, x_q),
-             perm_token=_out(where, out.get("perm_token"), (A_max,), torch.int32, x_q),
-             perm_weight=_out(where, out.get("perm_weight"), (A_max,), torch.float32, x_q))
+    nb = _blocks(d)
+    if x_q.dtype != FP8 or x_scale.dtype != SCALE or x_scale.shape != (N, nb):
+        _refuse(where, f"float8_e4m3fn [N,d] with float8_e8m0fnu scales {(N, nb)} expected")
+    if out is None:
+        dev = x_q.device
+        r = dict(x_q=torch.empty(A_max, d, dtype=FP8, device=dev), x_scale=torch.empty(A_max, nb, dtype=SCALE, device=dev),
+                 perm_token=torch.empty(A_max, dtype=torch.int32, device=dev), perm_weight=torch.empty(A_max, dtype=torch.float32, device=dev))
+    else:
+        r = dict(x_q=_out(where, out.get("x_q"), (A_max, d), FP8, x_q), x_scale=_out(where, out.get("x_scale"), (A_max, nb), SCALE, x_q),
+                 perm_token=_out(where, out.get("perm_token"), (A_max,), torch.int32, x_q),
+                 perm_weight=_out(where, out.get("perm_weight"), (A_max,), torch.float32, x_q))
     _run(where, x_q, x_q, x_scale, N, d, E, k, slots, D, A_max, scores, topk_idx, token_group, slot_row, r["x_q"], r["x_scale"],
          r["perm_token"], r["perm_weight"])
     return r
@@ -862,7 +884,7 @@ def permute_backward(dx_perm, slot_row, add=None, dx=None, stream=None):
         _refuse(where, "at most two tensors to add", EUNSUPPORTED)
     for t in add:
         _want(where, "add", t, (N, d), dx_perm.dtype)
-    dx = _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
+    dx = torch.empty(N, d, dtype=dx_perm.dtype, device=dx_perm.device) if dx is None else _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
     _run(where, dx_perm, dx_perm, slot_row, N, d, slots, _dt(dx_perm), A_max, *(add + (None, None))[:2], dx)
     return dx
 
@@ -896,15 +918,24 @@ def route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D: int = 0,
     if dscores is not None and dscores.dim() == 2:
         ld = E
     _want(where, "dscores", dscores, (N, E) if ld else (E,), torch.float32)
-    out = out or {}
-    dw = out.get("dw")
-    r = dict(dlogits=_out(where, out.get("dlogits"), (N, E), torch.float32, x), dx=_out(where, out.get("dx"), (N, d), x.dtype, x),
-             dw=_out(where, dw, (E, d), out_dtype or (dw.dtype if dw is not None else x.dtype), x),
-             dbias=_out(where, out.get("dbias"), (E,), torch.float32, x))
+    dtype, dev = x.dtype, x.device
+    code = _dt(dtype)
+    if out is None:
+        r = dict(dlogits=torch.empty_like(scores), dx=torch.empty_like(x),
+                 dw=torch.empty_like(w_router) if out_dtype is None else torch.empty_like(w_router, dtype=out_dtype),
+                 dbias=torch.empty(E, dtype=torch.float32, device=dev))
+    else:
+        dw = out.get("dw")
+        r = dict(dlogits=_out(where, out.get("dlogits"), (N, E), torch.float32, x), dx=_out(where, out.get("dx"), (N, d), dtype, x),
+                 dw=_out(where, dw, (E, d), out_dtype or (dw.dtype if dw is not None else dtype), x),
+                 dbias=_out(where, out.get("dbias"), (E,), torch.float32, x))
     if ws is None:
-        ws = x.new_empty((_route_backward_bytes(x.get_device(), N, d, E, x.dtype),), dtype=torch.uint8)
-    _run(where, x, x, w_router, scores, topk_idx, slot_row, dweight, N, d, E, k, slots, D, token_group, dscores, ld, _dt(x), _dt(r["dw"]),
-         dweight.shape[0], r["dlogits"], r["dx"], r["dw"], r["dbias"], ws, ws.numel() * ws.element_size(), _status(where, dev_status))
+        size = _route_backward_bytes(x.get_device(), N, d, E, dtype)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    else:
+        size = ws.numel() * ws.element_size()
+    _run(where, x, x, w_router, scores, topk_idx, slot_row, dweight, N, d, E, k, slots, D, token_group, dscores, ld, code, _dt(r["dw"]),
+         dweight.shape[0], r["dlogits"], r["dx"], r["dw"], r["dbias"], ws, size, _status(where, dev_status))
     return r
 
 

@@ -142,7 +142,10 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) sum = fmaf(f[i], f[i], sum);
   }
-  const float rstd = rsqrtf(row_sum(sum, a.wpr, red) / (float)d + a.eps);
+  const float ms = row_sum(sum, a.wpr, red) / (float)d + a.eps;
+  float rstd = rsqrtf(ms);
+  const float left = fmaf(-ms * rstd, rstd, 1.f);            // one Newton step: what rsqrtf leaves would be the largest error of an fp32 y
+  if (fabsf(left) < 0.5f) rstd = fmaf(0.5f * rstd, left, rstd);   // (not from an infinity or a zero)
   if (!live) return;                         // whole warps; nothing below crosses a warp
   if (a.rstd && t == 0) a.rstd[row] = rstd;
   const int nb = (d + QBLOCK - 1) / QBLOCK;
@@ -171,17 +174,33 @@ struct GradArgs {
   float* part;                               // [groups of warps][d]
 };
 
-// A group of wpr warps walks its rows, a thread's columns are the same in all of them: dw is summed in registers, and
-// written once per group for k_sum_parts to join in a fixed order.
-template <typename T, bool VEC, int VPT>
+// Per-thread ring of the rows to come: every thread copies the 16-byte vectors that it will use itself into its own places of
+// shared memory, so nothing but its own copies has to be waited for.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {        // zeros where not in
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16u : 0u) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ uint4 get_shared(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+// A group of wpr warps walks its rows, DEPTH - 1 of them in flight ahead of the one it works on; a thread's columns are the same
+// in all of them: dw is summed in registers, and written once per group for k_sum_parts to join in a fixed order.
+template <typename T, bool VEC, int VPT, int DEPTH>
 __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   allow_next_kernel();
   wait_for_previous_kernel();
   constexpr int NV = Vec16<T>::n;
   __shared__ float red[2][NT_MAX / 32];
+  extern __shared__ uint4 ring[];            // [DEPTH][dy, h, dh][VPT][threads]
   const int tpr = a.wpr * 32, t = threadIdx.x & (tpr - 1), d = a.d;
   const int64_t group = (int64_t)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr, groups = (int64_t)gridDim.x * (blockDim.x / tpr);
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring + threadIdx.x), step = blockDim.x * 16u;
   uint4 w[VPT];
   float dw[VPT][NV];
 #pragma unroll
@@ -191,23 +210,38 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) dw[u][i] = 0.f;
   }
-  int it = 0;
-  for (int64_t row0 = 0; row0 < a.N; row0 += groups, it ^= 1) {      // the same count in all warps of the block
-    const int64_t row = row0 + group, at = row * d;
-    const bool live = row < a.N;
-    const float rstd = live ? a.rstd[row] : 0.f;
-    uint4 dy[VPT], h[VPT], dh[VPT];
+  auto fetch = [&](int64_t row, int slot) {
+    const uint32_t to = mine + (uint32_t)(slot * 3 * VPT) * step;
+    const T* from[3] = {a.dy, a.h, a.dh};
 #pragma unroll
-    for (int u = 0; u < VPT; ++u) {
-      const int c = (u * tpr + t) * NV;
-      const bool in = live && c < d;
-      dy[u] = in ? get_cells<T, VEC>(a.dy + at + c, d - c) : zero;
-      h[u] = in ? get_cells<T, VEC>(a.h + at + c, d - c) : zero;
-      dh[u] = in && a.dh ? get_cells<T, VEC>(a.dh + at + c, d - c) : zero;
-    }
+    for (int m = 0; m < 3; ++m)
+#pragma unroll
+      for (int u = 0; u < VPT; ++u) {
+        const int c = (u * tpr + t) * NV;
+        const bool in = row < a.N && c < d && from[m];
+        const T* p = in ? from[m] + row * d + c : a.dy;
+        if constexpr (VEC) copy16(to + (uint32_t)(m * VPT + u) * step, p, in);
+        else ring[(size_t)((slot * 3 + m) * VPT + u) * blockDim.x + threadIdx.x] = in ? get_cells<T, false>(p, d - c) : zero;
+      }
+    if constexpr (VEC) copies_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s) fetch(group + s * groups, s);
+  float rstd = group < a.N ? a.rstd[group] : 0.f;
+  int it = 0, slot = 0;
+  for (int64_t row0 = 0; row0 < a.N; row0 += groups, it ^= 1) {      // the same count in all warps of the block
+    const int64_t row = row0 + group;
+    const bool live = row < a.N;
+    fetch(row + (DEPTH - 1) * groups, slot == 0 ? DEPTH - 1 : slot - 1);
+    const float rstd1 = row + groups < a.N ? a.rstd[row + groups] : 0.f;
+    if constexpr (VEC) copies_wait<DEPTH - 1>();
+    const uint32_t from = mine + (uint32_t)(slot * 3 * VPT) * step;
+    uint4 dy[VPT], h[VPT];
     float dot = 0.f;
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
+      dy[u] = get_shared(from + (uint32_t)u * step);
+      h[u] = get_shared(from + (uint32_t)(VPT + u) * step);
       float p[NV], q[NV], g[NV];
       Vec16<T>::load(dy[u], p);
       Vec16<T>::load(h[u], q);
@@ -219,8 +253,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
         dw[u][i] = fmaf(p[i], n, dw[u][i]);
       }
     }
-    const float mean = row_sum(dot, a.wpr, red[it]) / (float)d;
-    if (!live) continue;
+    const float k = -row_sum(dot, a.wpr, red[it]) / (float)d * rstd * rstd;
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
       const int c = (u * tpr + t) * NV;
@@ -228,11 +261,13 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
       Vec16<T>::load(dy[u], p);
       Vec16<T>::load(h[u], q);
       Vec16<T>::load(w[u], g);
-      Vec16<T>::load(dh[u], e);
+      Vec16<T>::load(get_shared(from + (uint32_t)(2 * VPT + u) * step), e);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) p[i] = fmaf(rstd, p[i] * g[i] - q[i] * rstd * mean, e[i]);
-      if (c < d) put_cells<T, VEC>(a.dx + at + c, d - c, Vec16<T>::store(p));
+      for (int i = 0; i < NV; ++i) p[i] = fmaf(q[i], k, fmaf(rstd, p[i] * g[i], e[i]));
+      if (live && c < d) put_cells<T, VEC>(a.dx + row * d + c, d - c, Vec16<T>::store(p));
     }
+    rstd = rstd1;
+    if (++slot == DEPTH) slot = 0;
   }
   float* part = a.part + group * d;
 #pragma unroll
@@ -250,29 +285,32 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   }
 }
 
-// out[c] = sum over g of part[g][c]: a block per 32 columns, 32 threads to a column, then the 32 sums in their order.
+// out[c] = sum over g of part[g][c]: a block per SUM_COLS columns (a half line), SUM_ROWS threads to a column, then their
+// sums in order.  (A block per 32 columns leaves most SMs without one.)
+constexpr int SUM_COLS = 16, SUM_ROWS = 32;
 template <typename TO>
-__global__ void __launch_bounds__(1024) k_sum_parts(const float* __restrict__ part, int64_t parts, int d, TO* __restrict__ out) {
+__global__ void __launch_bounds__(SUM_COLS * SUM_ROWS) k_sum_parts(const float* __restrict__ part, int64_t parts, int d, TO* __restrict__ out) {
   allow_next_kernel();
   wait_for_previous_kernel();
-  __shared__ float sum[32][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+  __shared__ float sum[SUM_ROWS][SUM_COLS];
+  const int i = threadIdx.x & (SUM_COLS - 1), c = blockIdx.x * SUM_COLS + i, r = threadIdx.x / SUM_COLS;
   float s = 0.f;
   if (c < d)
-#pragma unroll 4
-    for (int64_t g = r; g < parts; g += 32) s += part[g * d + c];
-  sum[r][threadIdx.x & 31] = s;
+#pragma unroll 8
+    for (int64_t g = r; g < parts; g += SUM_ROWS) s += part[g * d + c];
+  sum[r][i] = s;
   __syncthreads();
   if (r == 0 && c < d) {
-#pragma unroll
-    for (int i = 1; i < 32; ++i) s += sum[i][threadIdx.x & 31];
+#pragma unroll 8
+    for (int j = 1; j < SUM_ROWS; ++j) s += sum[j][i];
     out[c] = from_float<TO>(s);
   }
 }
 
-constexpr int NORM_VPT = 8;                  // vectors a thread that a row's warps are chosen for, with many rows
+constexpr int NORM_VPT = 2;                  // vectors a thread that a row's warps are chosen for, with many rows
 constexpr int GRAD_VPT = 2;                  // the same of the gradient, whose threads also hold dw and w
-constexpr int GRAD_BLOCKS = 4;               // blocks per SM at most
+constexpr int GRAD_BLOCKS = 2;               // blocks per SM at most
+constexpr int GRAD_DEPTH1 = 4, GRAD_DEPTH2 = 4;   // rows in the ring with one and two vectors a thread
 // Warps to a row: as few as hold it in `vpt` vectors a thread, more while the rows leave warps of the device without one; 16
 // where eight would have to hold more than `most` vectors a thread.
 int warps_per_row(int64_t N, int vecs, int vpt, int most) {
@@ -281,7 +319,7 @@ int warps_per_row(int64_t N, int vecs, int vpt, int most) {
   return vecs > 32 * NW * most ? 2 * NW : wpr;
 }
 int norm_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, NORM_VPT, 8); }
-int grad_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, GRAD_VPT, 4); }
+int grad_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, GRAD_VPT, 2); }
 int rows_per_block(int wpr) { return wpr < NW ? NW / wpr : 1; }
 unsigned threads_of(int wpr) { return 32u * (unsigned)(wpr < NW ? NW : wpr); }
 int vecs_of(int d, int dtype) { return (int)ceil_div((int64_t)d * (int64_t)elt_size(dtype), 16); }
@@ -311,9 +349,14 @@ int norm(const void* x, const void* res, const void* w, int64_t N, int d, float 
 template <typename T, bool VEC>
 int grad_run(const GradArgs<T>& a, cudaStream_t st) {
   const int vpt = (int)ceil_div(ceil_div(a.d, Vec16<T>::n), 32 * a.wpr);
-  auto k = vpt <= 1 ? k_rms_norm_grad<T, VEC, 1> : vpt <= 2 ? k_rms_norm_grad<T, VEC, 2> : vpt <= 4 ? k_rms_norm_grad<T, VEC, 4>
-                                                                                              : k_rms_norm_grad<T, VEC, 8>;
-  const int rc = note_cuda(launch_chained(k, (unsigned)grad_blocks(a.N, a.wpr), threads_of(a.wpr), 0, st, a));
+  const int room = vpt <= 1 ? 1 : vpt <= 2 ? 2 : vpt <= 4 ? 4 : 8;
+  const int depth = room == 1 ? GRAD_DEPTH1 : room == 2 ? GRAD_DEPTH2 : 8 / room;
+  auto k = room == 1 ? k_rms_norm_grad<T, VEC, 1, GRAD_DEPTH1> : room == 2 ? k_rms_norm_grad<T, VEC, 2, GRAD_DEPTH2>
+           : room == 4 ? k_rms_norm_grad<T, VEC, 4, 2> : k_rms_norm_grad<T, VEC, 8, 1>;
+  const size_t smem = (size_t)depth * 3 * (size_t)room * threads_of(a.wpr) * 16;
+  const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (err != cudaSuccess) return note_cuda(err);
+  const int rc = note_cuda(launch_chained(k, (unsigned)grad_blocks(a.N, a.wpr), threads_of(a.wpr), smem, st, a));
   count_launch(1);
   return rc;
 }
@@ -339,9 +382,9 @@ bool usable(P... p) {
 }  // namespace
 
 int sum_parts(const float* part, int64_t parts, int d, int out_dtype, void* out, cudaStream_t st) {
-  const unsigned grid = (unsigned)ceil_div(d, 32);
-  const int rc = note_cuda(out_dtype == CAPMOE_F32 ? launch_chained(k_sum_parts<float>, grid, 1024, 0, st, part, parts, d, (float*)out)
-                                                   : launch_chained(k_sum_parts<__nv_bfloat16>, grid, 1024, 0, st, part, parts, d, (__nv_bfloat16*)out));
+  const unsigned grid = (unsigned)ceil_div(d, SUM_COLS), block = SUM_COLS * SUM_ROWS;
+  const int rc = note_cuda(out_dtype == CAPMOE_F32 ? launch_chained(k_sum_parts<float>, grid, block, 0, st, part, parts, d, (float*)out)
+                                                   : launch_chained(k_sum_parts<__nv_bfloat16>, grid, block, 0, st, part, parts, d, (__nv_bfloat16*)out));
   count_launch(1);
   return rc;
 }
