@@ -3,45 +3,48 @@
 //   dS[t,e] = sum of dweight[r] over the slots of t that keep a row r of e  (+ dscores[t,e])
 //   dl[t,e] = S[t,e] (dS[t,e] - sum_f S[t,f] dS[t,f])
 //   dx = dl W_r,   dW_r = dl^T x,   dbias = sum_t dl
-// The two products run as grouped products of one expert (dx) and of ranges of tokens (dW_r, added in their order here).
-// bf16: dl is fp32, and one rounding to bf16 could cost it 2^-8; it goes in as two bf16 numbers, its rounding and the
-// rounding of what that leaves out (2^-16 of dl is lost at most), side by side as 2E columns, against W_r twice.
-#include "gmm.cuh"
+// Three forms of the products, all with fp32 accumulation and parts of dW_r and dbias over ranges of tokens that one last kernel
+// adds in their order:
+//   E <= 16       k_route_grad_few: everything in one kernel on plain FMAs, W_r and dW_r in registers
+//   bf16, E <= 128, whole 16-byte vectors   k_route_logit_grad, then both products in one pass over x (route_grad_tc.cu)
+//   other sizes   k_route_logit_grad, then the grouped products (gmm.cuh) of one expert (dx) and of ranges of tokens (dW_r)
+// bf16 products on tensor cores: dl is fp32, and one rounding to bf16 could cost it 2^-8; it goes in as two bf16 numbers, its
+// rounding and the rounding of what that leaves out (2^-16 of dl is lost at most).
+#include "route_grad.cuh"
 #include "rowvec.cuh"
 
 namespace capmoe {
 namespace {
 
 constexpr int RG_WARPS = 8;
-constexpr int RG_BLOCKS = 8;                 // blocks per SM at most (walks the tokens, so that dbias has few parts)
+constexpr int RG_BLOCKS = 4;                 // blocks per SM at most (walks the tokens, so that dbias has few parts)
 
 struct LogitArgs {
-  const float *scores, *dweight, *dscores;
-  const int32_t *topk_idx, *slot_row, *token_group;
-  int64_t N, rows, dscores_ld;
-  int E, k, slots, D;
+  ScoreGrad s;
   float *dlogits, *dbias_part;
-  __nv_bfloat16* pair;                       // bf16: [N, 2 Ep], else NULL
-  int Ep;
-  const __nv_bfloat16* w;                    // bf16: W_r [E, d] and its copy with itself [2 Ep, d]
+  __nv_bfloat16* pair;                       // bf16: [N, 2 Eq], else NULL
+  int Eq;
+  const __nv_bfloat16* w;                    // for the grouped product: W_r [E, d] and its copy with itself [2 Eq, d], else NULL
   __nv_bfloat16* w2;
   int d;
-  int32_t* offsets;                          // [0, N], then `ranges` + 1 bounds of the ranges of tokens
+  int32_t* offsets;                          // for the grouped products: [0, N], then `ranges` + 1 bounds of tokens, else NULL
   int ranges, range;
 };
 
 // One warp a token, lane + 32 i an expert.
 template <int EPL>
 __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitArgs a) {
-  allow_next_kernel();
   wait_for_previous_kernel();
+  allow_next_kernel();                       // in this order: an early successor reads what came before (gmm.cuh)
   __shared__ float ds[RG_WARPS][EPL * 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.E;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.s.E;
   const int64_t tid = (int64_t)blockIdx.x * (RG_WARPS * 32) + threadIdx.x, threads = (int64_t)gridDim.x * (RG_WARPS * 32);
-  if (tid < 2) a.offsets[tid] = tid ? (int32_t)a.N : 0;
-  if (tid <= a.ranges) a.offsets[2 + tid] = (int32_t)min(a.N, tid * (int64_t)a.range);
+  if (a.offsets) {
+    if (tid < 2) a.offsets[tid] = tid ? (int32_t)a.s.N : 0;
+    if (tid <= a.ranges) a.offsets[2 + tid] = (int32_t)min(a.s.N, tid * (int64_t)a.range);
+  }
   if (a.w2) {
-    const int64_t half = (int64_t)a.Ep * a.d;
+    const int64_t half = (int64_t)a.Eq * a.d;
     for (int64_t i = tid; i < 2 * half; i += threads) {
       const int64_t j = i < half ? i : i - half;
       a.w2[i] = j < (int64_t)E * a.d ? a.w[j] : __float2bfloat16_rn(0.f);
@@ -50,28 +53,21 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
   float bias[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) bias[i] = 0.f;
-  for (int64_t t = (int64_t)blockIdx.x * RG_WARPS + warp; t < a.N; t += (int64_t)gridDim.x * RG_WARPS) {
+  for (int64_t t = (int64_t)blockIdx.x * RG_WARPS + warp; t < a.s.N; t += (int64_t)gridDim.x * RG_WARPS) {
     float* row = ds[warp];
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = lane + 32 * i;
-      row[e] = a.dscores && e < E ? a.dscores[t * a.dscores_ld + e] : 0.f;
-    }
-    __syncwarp();
-    for (int s = lane; s < a.slots; s += 32) {
-      const int32_t r = a.slot_row[t * a.slots + s];
-      if (r >= 0 && r < a.rows) {
-        const int e = s < a.k ? a.topk_idx[t * a.k + s] : home_group(t, a.N, a.D, a.token_group) * (E / a.D) + (s - a.k);
-        if ((unsigned)e < (unsigned)E) atomicAdd(&row[e], a.dweight[r]);       // (one addition: a token has one row of an expert)
-      }
-    }
-    __syncwarp();
     float s[EPL], g[EPL], dot = 0.f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       const int e = lane + 32 * i;
-      s[i] = e < E ? a.scores[t * E + e] : 0.f;
-      g[i] = row[e];
+      s[i] = e < E ? a.s.scores[t * E + e] : 0.f;
+      row[e] = a.s.dscores && e < E ? a.s.dscores[t * a.s.dscores_ld + e] : 0.f;
+    }
+    __syncwarp();
+    add_kept(a.s, t, lane, 32, row);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      g[i] = row[lane + 32 * i];
       dot = fmaf(s[i], g[i], dot);
     }
 #pragma unroll
@@ -79,15 +75,13 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       const int e = lane + 32 * i;
-      const float dl = s[i] * (g[i] - dot);
-      if (e < E) {
-        a.dlogits[t * E + e] = dl;
-        bias[i] += dl;
-      }
-      if (a.pair && e < a.Ep) {
+      const float dl = e < E ? s[i] * (g[i] - dot) : 0.f;
+      bias[i] += dl;
+      if (e < E) a.dlogits[t * E + e] = dl;
+      if (a.pair && e < a.Eq) {
         const __nv_bfloat16 hi = __float2bfloat16_rn(dl);
-        a.pair[t * 2 * a.Ep + e] = hi;
-        a.pair[t * 2 * a.Ep + a.Ep + e] = __float2bfloat16_rn(dl - __bfloat162float(hi));
+        a.pair[t * 2 * a.Eq + e] = hi;
+        a.pair[t * 2 * a.Eq + a.Eq + e] = __float2bfloat16_rn(dl - __bfloat162float(hi));
       }
     }
     __syncwarp();                            // row is rewritten by the next token
@@ -103,50 +97,274 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
   }
 }
 
-// dw [E, d] from parts [ranges][copies * Ep][d] (copies = 2: both halves of dl), in a fixed order.
-template <typename TO>
-__global__ void __launch_bounds__(256) k_join_dw(const float* __restrict__ part, int ranges, int copies, int E, int Ep, int d, TO* __restrict__ dw) {
+// ---------------------------------------------------------------- up to 16 experts
+// A thread owns V columns: their W_r and dW_r stay in its registers, x goes by once.  A block is `tx` threads across the columns
+// by `ty` tokens at a time; it walks a range of tokens in chunks, whose dl it makes first (EM lanes a token) in shared memory.
+// 16 FMAs an element of x for E = 8: bound by HBM as long as enough loads are in flight (U tokens a thread).
+constexpr int FEW_N = 256;                   // threads
+constexpr int FEW_TOK = 64;                  // tokens of a chunk
+constexpr int V = 4;
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void few_load(const T* p, int step, int left, float* f) {      // V columns, `step` apart (1 with VEC)
+  if constexpr (VEC && sizeof(T) == 2) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    f[0] = __uint_as_float(q.x << 16); f[1] = __uint_as_float(q.x & 0xffff0000u);
+    f[2] = __uint_as_float(q.y << 16); f[3] = __uint_as_float(q.y & 0xffff0000u);
+  } else if constexpr (VEC) {
+    const float4 q = *reinterpret_cast<const float4*>(p);
+    f[0] = q.x; f[1] = q.y; f[2] = q.z; f[3] = q.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = j * step < left ? to_float(p[j * step]) : 0.f;
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void few_store(T* p, int step, int left, const float* f) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<unsigned*>(&a), *reinterpret_cast<unsigned*>(&b));
+  } else if constexpr (VEC) {
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j * step < left) p[j * step] = from_float<T>(f[j]);
+  }
+}
+
+template <typename T>
+struct FewArgs {
+  ScoreGrad s;
+  const T *x, *w;
+  int d, tx, per;                            // per: tokens of a range
+  T* dx;
+  float *dlogits, *parts, *dbias_part;       // parts [ranges][E][d], dbias_part [ranges][E]
+};
+
+template <typename T, bool VEC, int EM>
+__global__ void __launch_bounds__(FEW_N) k_route_grad_few(const FewArgs<T> a) {
   allow_next_kernel();
   wait_for_previous_kernel();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)E * d) return;
-  const int64_t half = (int64_t)Ep * d;
+  constexpr int U = EM == 8 ? 8 : 4;         // tokens in flight
+  __shared__ float dl[FEW_TOK][EM];
+  __shared__ float sum[FEW_N][V];
+  const int E = a.s.E, d = a.d, tx = a.tx, ty = FEW_N / tx, cx = threadIdx.x & (tx - 1), cy = threadIdx.x / tx;
+  const int step = VEC ? 1 : tx, c = (int)blockIdx.x * tx * V + (VEC ? cx * V : cx), left = d - c;
+  const bool cols = left > 0;
+  const int range = blockIdx.y;
+  const int64_t first = (int64_t)range * a.per, last = min(a.s.N, first + a.per);
+  float w[EM][V], dw[EM][V], bias = 0.f;
+#pragma unroll
+  for (int e = 0; e < EM; ++e) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) w[e][j] = dw[e][j] = 0.f;
+    if (e < E && cols) few_load<T, VEC>(a.w + (int64_t)e * d + c, step, left, w[e]);
+  }
+  for (int64_t t0 = first; t0 < last; t0 += FEW_TOK) {
+    const int n = (int)min((int64_t)FEW_TOK, last - t0);
+    const int e = threadIdx.x & (EM - 1);
+    __syncthreads();                         // the last chunk's dl has been read
+#pragma unroll
+    for (int i = threadIdx.x / EM; i < FEW_TOK; i += FEW_N / EM) {
+      const int64_t t = t0 + i;
+      const bool mine = i < n && e < E;
+      const float s = mine ? a.s.scores[t * E + e] : 0.f;
+      dl[i][e] = mine && a.s.dscores ? a.s.dscores[t * a.s.dscores_ld + e] : 0.f;
+      __syncwarp();
+      if (i < n) add_kept(a.s, t, e, EM, dl[i]);
+      __syncwarp();
+      const float g = dl[i][e];
+      float dot = s * g;
+#pragma unroll
+      for (int o = EM / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      const float v = mine ? s * (g - dot) : 0.f;
+      dl[i][e] = v;
+      bias += v;
+      if (mine && blockIdx.x == 0) a.dlogits[t * E + e] = v;
+    }
+    __syncthreads();
+    if (cols)
+      for (int i0 = cy; i0 < n; i0 += ty * U) {
+        float x[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u * ty;
+          if (i < n) few_load<T, VEC>(a.x + (t0 + i) * d + c, step, left, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u * ty;
+          if (i >= n) break;
+          float y[V] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e4 = 0; e4 < EM; e4 += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(&dl[i][e4]);
+            const float l[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+              for (int j = 0; j < V; ++j) {
+                y[j] = fmaf(l[m], w[e4 + m][j], y[j]);
+                dw[e4 + m][j] = fmaf(l[m], x[u][j], dw[e4 + m][j]);
+              }
+          }
+          few_store<T, VEC>(a.dx + (t0 + i) * d + c, step, left, y);
+        }
+      }
+  }
+  // the ty shares of dW_r in their order, then a part
+  float* part = a.parts + (int64_t)range * E * d;
+#pragma unroll
+  for (int e = 0; e < EM; ++e) {
+    if (ty > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[threadIdx.x][j] = dw[e][j];
+      __syncthreads();
+      if (cy == 0)
+        for (int k = 1; k < ty; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) dw[e][j] += sum[cx + k * tx][j];
+    }
+    if (cy == 0 && e < E && cols) few_store<float, false>(part + (int64_t)e * d + c, step, left, dw[e]);
+  }
+  if (blockIdx.x == 0) {
+    __syncthreads();
+    sum[threadIdx.x][0] = bias;
+    __syncthreads();
+    if (threadIdx.x < E) {
+      float b = 0.f;
+      for (int k = threadIdx.x; k < FEW_N; k += EM) b += sum[k][0];
+      a.dbias_part[(int64_t)range * E + threadIdx.x] = b;
+    }
+  }
+}
+
+// dW_r [E, d] from parts [ranges][copies][rows][d] (copies = 2: both halves of dl) and, in the blocks behind, dbias [E] from parts
+// [bias_parts][E], all in a fixed order.
+constexpr int JOIN_N = 256, JOIN_E = 8;      // threads; experts of a block for dbias
+template <typename TO, int VW>
+__global__ void __launch_bounds__(JOIN_N) k_join_route(const float* __restrict__ part, int parts, int64_t each, int64_t size, int dw_blocks,
+                                                       TO* __restrict__ dw, const float* __restrict__ bias_part, int bias_parts, int E,
+                                                       float* __restrict__ dbias) {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+  if ((int)blockIdx.x < dw_blocks) {
+    const int64_t i = ((int64_t)blockIdx.x * JOIN_N + threadIdx.x) * VW;
+    if (i >= size) return;
+    float s[VW];
+#pragma unroll
+    for (int j = 0; j < VW; ++j) s[j] = 0.f;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) {
+      if constexpr (VW == 4) {
+        const float4 v = __ldcs(reinterpret_cast<const float4*>(part + p * each + i));
+        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+      } else {
+        s[0] += part[p * each + i];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VW; ++j) dw[i + j] = from_float<TO>(s[j]);
+    return;
+  }
+  __shared__ float sum[JOIN_N];
+  const int e = (int)(blockIdx.x - dw_blocks) * JOIN_E + (threadIdx.x & (JOIN_E - 1)), r = threadIdx.x / JOIN_E;
   float s = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < ranges * copies; ++p) s += part[p * half + i];
-  dw[i] = from_float<TO>(s);
+  if (e < E)
+#pragma unroll 8
+    for (int p = r; p < bias_parts; p += JOIN_N / JOIN_E) s += bias_part[(int64_t)p * E + e];
+  sum[threadIdx.x] = s;
+  __syncthreads();
+  if (r == 0 && e < E) {
+#pragma unroll 8
+    for (int k = 1; k < JOIN_N / JOIN_E; ++k) s += sum[k * JOIN_E + threadIdx.x];
+    dbias[e] = s;
+  }
+}
+
+template <typename TO>
+int join_run(const float* part, int parts, int64_t each, int64_t size, void* dw, const float* bias_part, int bias_parts, int E, float* dbias,
+             cudaStream_t st) {
+  const bool wide = each % 4 == 0 && size % 4 == 0;
+  const int64_t dw_blocks = parts ? ceil_div(size, (int64_t)JOIN_N * (wide ? 4 : 1)) : 0, blocks = dw_blocks + ceil_div(E, JOIN_E);
+  if (blocks > 0x7fffffff) return CAPMOE_EUNSUPPORTED;
+  auto k = wide ? k_join_route<TO, 4> : k_join_route<TO, 1>;
+  const int rc = note_cuda(launch_chained(k, (unsigned)blocks, JOIN_N, 0, st, part, parts, each, size, (int)dw_blocks, (TO*)dw, bias_part, bias_parts, E,
+                                          dbias));
+  count_launch(1);
+  return rc;
 }
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
-// Ranges of tokens whose dW_r are summed apart: enough for the tiles of 256 x 256 to fill the pairs of SMs, 512 tokens each at least.
-int ranges_of(int64_t N, int d, int n) {
-  const int64_t tiles = ceil_div(d, 256) * ceil_div(n, 256), want = (sm_count() / 2) / tiles, most = N / 512;
-  int64_t r = want < most ? want : most;
-  return (int)(r < 1 ? 1 : r > 64 ? 64 : r);
-}
+enum Form { FEW, TC, GENERAL };
 struct RouteWs {
-  int copies, Ep, ranges, blocks;
+  Form form;
+  int copies, Eq, ranges, blocks;            // general form, tensor cores: blocks of the logits' kernel
   size_t offsets, bias, pair, w2, parts, dw, dw_bytes, total;
 };
+int few_tx(int d) {
+  int tx = 32;
+  while (tx < FEW_N && tx * V < d) tx *= 2;
+  return tx;
+}
 RouteWs route_ws(int64_t N, int d, int E, int dtype) {
-  RouteWs w;
-  w.copies = dtype == CAPMOE_BF16 ? 2 : 1;
-  w.Ep = dtype == CAPMOE_BF16 ? (E + 3) / 4 * 4 : E;         // rows of `pair` in whole 16-byte vectors
-  w.ranges = ranges_of(N, d, w.copies * w.Ep);
-  const int64_t want = ceil_div(N, RG_WARPS), most = (int64_t)sm_count() * RG_BLOCKS;
-  w.blocks = (int)(want < most ? want : most);
+  RouteWs w = {};
+  const bool bf16 = dtype == CAPMOE_BF16;
+  w.form = E <= 16 ? FEW : route_grad_tc_supported(d, E, dtype) ? TC : GENERAL;
+  w.copies = w.form != FEW && bf16 ? 2 : 1;
+  w.Eq = w.copies == 2 ? (E + 7) / 8 * 8 : E;                // rows of `pair` in whole 16-byte vectors
+  const int64_t sms = sm_count();
+  if (w.form == FEW) {
+    // two blocks per SM; 32 tokens each at least, or a part of dW_r would be as long as its tokens
+    const int64_t across = ceil_div(d, few_tx(d) * V), want = 2 * sms / across, most = ceil_div(N, 32);
+    int64_t r = want < most ? want : most;
+    if (r < 1) r = 1;
+    if (r > 65535) r = 65535;
+    w.ranges = (int)ceil_div(N, ceil_div(N, r));
+  } else if (w.form == TC) {
+    w.ranges = route_grad_tc_ranges(N, d, E);
+  } else {
+    // enough for the tiles of 256 x 256 to fill the pairs of SMs, 512 tokens each at least
+    const int64_t want = sms / 2 / (ceil_div(d, 256) * ceil_div(w.copies * w.Eq, 256)), most = N / 512;
+    const int64_t r = want < most ? want : most;
+    w.ranges = (int)(r < 1 ? 1 : r > 64 ? 64 : r);
+  }
+  const int64_t want = ceil_div(N, RG_WARPS), most = sms * RG_BLOCKS;
+  w.blocks = w.form == FEW ? w.ranges : (int)(want < most ? want : most);
+  if (w.ranges < 1) w.ranges = 1;
   if (w.blocks < 1) w.blocks = 1;
-  w.offsets = 0;
-  w.bias = up256((size_t)(w.ranges + 3) * 4);
+  w.bias = w.form == GENERAL ? up256((size_t)(w.ranges + 3) * 4) : 0;
   w.pair = w.bias + up256((size_t)w.blocks * E * 4);
-  w.w2 = w.pair + (w.copies == 2 ? up256((size_t)N * 2 * w.Ep * 2) : 0);
-  w.parts = w.w2 + (w.copies == 2 ? up256((size_t)2 * w.Ep * d * 2) : 0);
-  w.dw = w.parts + (w.copies * w.ranges > 1 ? up256((size_t)w.ranges * w.copies * w.Ep * d * 4) : 0);
-  w.dw_bytes = 0;
-  capmoe_grouped_mm_dw_workspace_bytes(w.ranges, &w.dw_bytes);
+  w.w2 = w.pair + (w.copies == 2 ? up256((size_t)N * 2 * w.Eq * 2) : 0);
+  w.parts = w.w2 + (w.form == GENERAL && bf16 ? up256((size_t)2 * w.Eq * d * 2) : 0);
+  const size_t rows = w.form == GENERAL ? (size_t)w.copies * w.Eq : (size_t)E;
+  w.dw = w.parts + up256((size_t)w.ranges * rows * d * 4);
+  if (w.form == GENERAL) capmoe_grouped_mm_dw_workspace_bytes(w.ranges, &w.dw_bytes);
   w.total = w.dw + up256(w.dw_bytes) + 256;                  // 256: to align all of it
   return w;
+}
+
+template <typename T>
+int few_run(const ScoreGrad& s, const void* x, const void* w, int d, const RouteWs& ws, uint8_t* b, float* dlogits, void* dx, cudaStream_t st) {
+  const FewArgs<T> a{s, (const T*)x, (const T*)w, d, few_tx(d), (int)ceil_div(s.N, ws.ranges), (T*)dx, dlogits, (float*)(b + ws.parts), (float*)(b + ws.bias)};
+  const bool vec = d % V == 0;
+  auto k = s.E <= 8 ? (vec ? k_route_grad_few<T, true, 8> : k_route_grad_few<T, false, 8>)
+                    : (vec ? k_route_grad_few<T, true, 16> : k_route_grad_few<T, false, 16>);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ceil_div(d, a.tx * V), (unsigned)ws.ranges);
+  cfg.blockDim = dim3(FEW_N);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const int rc = note_cuda(cudaLaunchKernelEx(&cfg, k, a));
+  count_launch(1);
+  return rc;
 }
 
 int check_route(int64_t N, int d, int E, int dtype) {
@@ -167,7 +385,7 @@ using namespace capmoe;
 extern "C" int capmoe_route_backward_workspace_bytes(int64_t N, int d, int E, int dtype, size_t* bytes) {
   const int rc = check_route(N, d, E, dtype);
   if (!bytes) return CAPMOE_EINVAL;
-  if (rc == CAPMOE_OK) *bytes = route_ws(N, d, E, dtype).total;
+  if (rc == CAPMOE_OK) *bytes = N ? route_ws(N, d, E, dtype).total : 0;
   return rc;
 }
 
@@ -193,39 +411,38 @@ extern "C" int capmoe_route_backward(const void* x, const void* w_router, const 
   if (ws_bytes < w.total) return CAPMOE_EWORKSPACE;
   uint8_t* b = (uint8_t*)up256((size_t)ws);
   const bool bf16 = dtype == CAPMOE_BF16;
-  const int n = w.copies * w.Ep;
-  LogitArgs a = {};
-  a.scores = scores; a.dweight = dweight; a.dscores = dscores;
-  a.topk_idx = topk_idx; a.slot_row = slot_row; a.token_group = token_group;
-  a.N = N; a.rows = A_max; a.dscores_ld = dscores_ld;
-  a.E = E; a.k = k; a.slots = slots; a.D = D;
-  a.dlogits = dlogits; a.dbias_part = (float*)(b + w.bias);
-  a.offsets = (int32_t*)(b + w.offsets); a.ranges = w.ranges; a.range = (int)ceil_div(N, w.ranges);
-  a.Ep = w.Ep; a.d = d;
-  if (bf16) {
-    a.pair = (__nv_bfloat16*)(b + w.pair);
-    a.w = (const __nv_bfloat16*)w_router;
-    a.w2 = (__nv_bfloat16*)(b + w.w2);
-  }
-  auto kernel = E <= 32 ? k_route_logit_grad<1> : E <= 64 ? k_route_logit_grad<2> : E <= 128 ? k_route_logit_grad<4> : k_route_logit_grad<8>;
-  rc = note_cuda(launch_chained(kernel, (unsigned)w.blocks, RG_WARPS * 32, 0, st, a));
-  count_launch(1);
-  if (rc != CAPMOE_OK) return rc;
-  const void* dl = bf16 ? (const void*)a.pair : dlogits;
-  const void* wr = bf16 ? (const void*)a.w2 : w_router;
-  if ((rc = capmoe_grouped_mm_dx(dl, a.offsets, wr, 1, d, n, dtype, dx, N, dev_status, stream)) != CAPMOE_OK) return rc;
-  const bool joined = w.copies * w.ranges > 1;
-  float* parts = joined ? (float*)(b + w.parts) : (float*)dw;
-  rc = capmoe_grouped_mm_dw(dl, x, a.offsets + 2, w.ranges, d, n, dtype, CAPMOE_F32, parts, N, b + w.dw, w.dw_bytes, dev_status, stream);
-  if (rc != CAPMOE_OK) return rc;
-  if (joined) {
-    const int64_t blocks = ceil_div((int64_t)E * d, 256);
-    rc = note_cuda(out_dtype == CAPMOE_F32
-                       ? launch_chained(k_join_dw<float>, (unsigned)blocks, 256, 0, st, (const float*)parts, w.ranges, w.copies, E, w.Ep, d, (float*)dw)
-                       : launch_chained(k_join_dw<__nv_bfloat16>, (unsigned)blocks, 256, 0, st, (const float*)parts, w.ranges, w.copies, E, w.Ep, d,
-                                        (__nv_bfloat16*)dw));
+  const ScoreGrad sg{scores, dweight, dscores, topk_idx, slot_row, token_group, N, A_max, dscores_ld, E, k, slots, D};
+  float *parts = (float*)(b + w.parts), *bias = (float*)(b + w.bias);
+  if (w.form == FEW) {
+    rc = bf16 ? few_run<__nv_bfloat16>(sg, x, w_router, d, w, b, dlogits, dx, st) : few_run<float>(sg, x, w_router, d, w, b, dlogits, dx, st);
+  } else {
+    LogitArgs a = {};
+    a.s = sg;
+    a.dlogits = dlogits; a.dbias_part = bias;
+    a.pair = bf16 ? (__nv_bfloat16*)(b + w.pair) : nullptr;
+    a.Eq = w.Eq; a.d = d;
+    if (w.form == GENERAL) {
+      a.offsets = (int32_t*)b; a.ranges = w.ranges; a.range = (int)ceil_div(N, w.ranges);
+      if (bf16) { a.w = (const __nv_bfloat16*)w_router; a.w2 = (__nv_bfloat16*)(b + w.w2); }
+    }
+    auto kernel = E <= 32 ? k_route_logit_grad<1> : E <= 64 ? k_route_logit_grad<2> : E <= 128 ? k_route_logit_grad<4> : k_route_logit_grad<8>;
+    rc = note_cuda(launch_chained(kernel, (unsigned)w.blocks, RG_WARPS * 32, 0, st, a));
     count_launch(1);
     if (rc != CAPMOE_OK) return rc;
+    if (w.form == TC) {
+      rc = route_grad_tc(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dx, parts, dev_status, st);
+    } else {
+      const int n = w.copies * w.Eq;
+      const void *dl = bf16 ? (const void*)a.pair : dlogits, *wr = bf16 ? (const void*)a.w2 : w_router;
+      rc = capmoe_grouped_mm_dx(dl, a.offsets, wr, 1, d, n, dtype, dx, N, dev_status, stream);
+      if (rc == CAPMOE_OK)
+        rc = capmoe_grouped_mm_dw(dl, x, a.offsets + 2, w.ranges, d, n, dtype, CAPMOE_F32, parts, N, b + w.dw, w.dw_bytes, dev_status, stream);
+    }
   }
-  return sum_parts(a.dbias_part, w.blocks, E, CAPMOE_F32, dbias, st);
+  if (rc != CAPMOE_OK) return rc;
+  // (the grouped product's parts hold a range's two halves one behind the other, of Eq rows each)
+  const int copies = w.form == GENERAL ? w.copies : 1;
+  const int64_t each = (int64_t)(w.form == GENERAL ? w.Eq : E) * d, size = (int64_t)E * d;
+  return out_dtype == CAPMOE_F32 ? join_run<float>(parts, w.ranges * copies, each, size, dw, bias, w.blocks, E, dbias, st)
+                                 : join_run<__nv_bfloat16>(parts, w.ranges * copies, each, size, dw, bias, w.blocks, E, dbias, st);
 }

@@ -1,0 +1,303 @@
+// The two products of the router's gradient on tcgen05, in one pass over x:
+//   dx[t] = sum_e dl[t,e] W_r[e],   dW_r[e] = sum_t dl[t,e] x[t]
+// dl comes as two bf16 numbers per element (route_grad.cu), each multiplied on its own into the same fp32 accumulators.
+// A CTA owns DC columns of x, W_r and dx and a range of tokens, which it walks in blocks of 128.  W_r's columns stay in shared
+// memory.  Of a block, dl (128 x E, both halves) is the A operand of dx = dl W_r (tokens are the M side, 128 columns the N side)
+// and, read along the other axis from the same bytes, the B operand of dW_r^T = x^T dl (128 columns are the M side, experts the N
+// side); x comes in stages of 64 tokens.  dW_r^T stays in tensor memory until the range ends and leaves as a part, fp32, that
+// route_grad.cu adds up in order; dx passes through three accumulators of 128 columns, so that its epilogue overlaps the MMAs.
+//   E <= 64: DC = 256, dl double-buffered, x in three stages of 32 KB;  E <= 128: DC = 128, x in two stages of 16 KB
+// What bounds it: HBM; x is read and dx written once.  Tensor pipe per 128 tokens x 256 columns, E = 64: about 2600 cycles of the
+// 5500 that the copy bandwidth allows an SM.
+#include "gmm_tc.cuh"
+#include "route_grad.cuh"
+
+namespace capmoe {
+namespace {
+
+template <int KB>                            // blocks of 64 experts
+struct RG {
+  static constexpr int DC = KB == 1 ? 256 : 128;
+  static constexpr int BOX = 64 * 64 * 2;                      // 64 columns by 64 rows, bf16
+  static constexpr int W_BYTES = KB * (DC / 64) * BOX;
+  static constexpr int DL_HALF = KB * 2 * BOX;                 // 128 tokens by KB * 64 experts
+  static constexpr int DL_BYTES = 2 * DL_HALF;
+  static constexpr int X_BYTES = (DC / 64) * BOX;
+  static constexpr int NST = KB == 1 ? 3 : 2;
+  static constexpr int DL_OFF = W_BYTES, X_OFF = DL_OFF + 2 * DL_BYTES, STG_OFF = X_OFF + NST * X_BYTES;
+  static constexpr int TAIL = STG_OFF + EPI_WARPS * WIDE_BYTES;
+  static constexpr int SMEM = TAIL + 1024 + 256;
+  static constexpr int CHUNKS = DC / 128;
+  static constexpr int SLOTS = 3;
+  static constexpr int DW_COLS = CHUNKS * KB * 64;             // tensor-memory columns of dW_r^T, then SLOTS x 128 for dx
+  static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
+  static_assert(DW_COLS + SLOTS * 128 <= 512, "tensor memory");
+};
+
+struct RGMaps { CUtensorMap hi, lo, x, w, o; };
+struct RGArgs {
+  int64_t N;
+  int d, E, slices, per;                     // per: tokens of a range, a multiple of 64
+  __nv_bfloat16* dx;
+  float* parts;
+  int32_t* dev_status;
+};
+
+// kind::f16, one CTA: D = fp32, A = B = bf16, M = 128, N = n; transpose bits for MN-major operands
+__device__ __forceinline__ uint32_t one_idesc(int n, bool a_mn, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(BM >> 4) << 24);
+}
+// MN-major operand whose boxes of 64 output indices lie `apart` bytes from each other
+__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t apart) {
+  return (umma_desc_mn(saddr) & ~((uint64_t)0x3fff << 16)) | ((uint64_t)(apart >> 4) << 16);
+}
+
+template <int KB>
+__global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_constant__ RGMaps mp, const __grid_constant__ RGArgs ar) {
+  using S = RG<KB>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (tiles - raw);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen + S::TAIL);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 24);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t bar0 = smem_u32(bars);
+  auto xfull = [&](int s) { return bar0 + 8u * (uint32_t)s; };                 // NST each
+  auto xempty = [&](int s) { return bar0 + 8u * (uint32_t)(4 + s); };
+  auto dfull = [&](int b) { return bar0 + 8u * (uint32_t)(8 + b); };           // dl
+  auto dempty = [&](int b) { return bar0 + 8u * (uint32_t)(10 + b); };
+  auto sfull = [&](int s) { return bar0 + 8u * (uint32_t)(12 + s); };          // dx accumulators
+  auto sempty = [&](int s) { return bar0 + 8u * (uint32_t)(16 + s); };
+  const uint32_t wfull = bar0 + 8u * 20u, wdone = bar0 + 8u * 21u;             // W_r has arrived; dW_r is complete
+
+  if (tid == 0) {
+    for (int s = 0; s < S::NST; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(dfull(b), 1); mbar_init(dempty(b), 1); }
+    for (int s = 0; s < S::SLOTS; ++s) { mbar_init(sfull(s), 1); mbar_init(sempty(s), EPI_WARPS * 32); }
+    mbar_init(wfull, 1);
+    mbar_init(wdone, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  allow_next_kernel();
+  const uint32_t tmem_base = *tmem_slot;
+
+  const int slice = (int)(blockIdx.x % (unsigned)ar.slices), range = (int)(blockIdx.x / (unsigned)ar.slices);
+  const int c0 = slice * S::DC;
+  const int64_t first = (int64_t)range * ar.per, last = min(ar.N, first + ar.per);      // first < last
+  const int blocks = (int)((last - first + 127) >> 7);
+  const int halves = (int)((last - first + 63) >> 6);                                   // stages of x
+  constexpr uint32_t W = 0, DL = S::DL_OFF, X = S::X_OFF;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (elect_one()) {
+      // W_r and x come from before the kernel that makes dl: they are fetched while it still runs
+      mbar_expect_tx(wfull, (uint32_t)S::W_BYTES);
+#pragma unroll
+      for (int i = 0; i < KB * (S::DC / 64); ++i)
+        tma_load_2d(tiles + W + (uint32_t)(i * S::BOX), &mp.w, c0 + i % (S::DC / 64) * 64, i / (S::DC / 64) * 64, wfull);
+      int s = 0, h = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      auto load_x = [&]() {                                      // stage h of x
+        if (!mbar_wait(xempty(s), ph ^ 1u, abort_flag)) return false;
+        mbar_expect_tx(xfull(s), (uint32_t)S::X_BYTES);
+#pragma unroll
+        for (int i = 0; i < S::DC / 64; ++i)
+          tma_load_2d(tiles + X + (uint32_t)(s * S::X_BYTES + i * S::BOX), &mp.x, c0 + i * 64, (int)first + h * 64, xfull(s));
+        ++h;
+        if (++s == S::NST) { s = 0; ph ^= 1u; }
+        return true;
+      };
+      const int ahead = min(halves, S::NST);
+      while (ok && h < ahead) ok = load_x();
+      wait_for_previous_kernel();
+      for (int b = 0; ok && b < blocks; ++b) {
+        const int buf = b & 1;
+        if (!mbar_wait(dempty(buf), (((uint32_t)b >> 1) & 1u) ^ 1u, abort_flag)) break;
+        mbar_expect_tx(dfull(buf), (uint32_t)S::DL_BYTES);
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {
+          const uint32_t to = tiles + DL + (uint32_t)(buf * S::DL_BYTES + i * 2 * S::BOX);
+          tma_load_2d(to, &mp.hi, i * 64, (int)first + b * 128, dfull(buf));
+          tma_load_2d(to + (uint32_t)S::DL_HALF, &mp.lo, i * 64, (int)first + b * 128, dfull(buf));
+        }
+        while (ok && h < min(halves, 2 * b + 2)) ok = load_x();
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    if (elect_one()) {
+      const int n_pad = (ar.E + 15) & ~15;
+      const uint32_t id_x = one_idesc(128, false, true), id_w = one_idesc(n_pad, true, true);
+      int s = 0, sl = 0, h = 0;
+      uint32_t ph = 0, slp = 0;
+      bool ok = mbar_wait(wfull, 0u, abort_flag);
+      for (int b = 0; ok && b < blocks; ++b) {
+        const int buf = b & 1;
+        const uint32_t dl = tiles + DL + (uint32_t)(buf * S::DL_BYTES);
+        if (!mbar_wait(dfull(buf), ((uint32_t)b >> 1) & 1u, abort_flag)) { ok = false; break; }
+        for (int u = 0; ok && u < S::CHUNKS; ++u) {               // dx, 128 columns at a time
+          if (!mbar_wait(sempty(sl), slp ^ 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t acc = tmem_base + (uint32_t)(S::DW_COLS + sl * 128);
+          for (int e0 = 0; e0 < ar.E; e0 += 16) {
+            const int kb = e0 >> 6, ks = (e0 >> 4) & 3;
+            const uint64_t wd = mn_desc(tiles + W + (uint32_t)((kb * (S::DC / 64) + u * 2) * S::BOX), S::BOX) + 128 * ks;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+              umma(acc, umma_desc(dl + (uint32_t)(half * S::DL_HALF + kb * 2 * S::BOX)) + 2 * ks, wd, id_x, (e0 | half) != 0 ? 1u : 0u);
+          }
+          umma_commit(sfull(sl));
+          if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
+        }
+        for (int i = 0; ok && i < 2 && h < halves; ++i, ++h) {    // dW_r^T, 64 tokens at a time
+          if (!mbar_wait(xfull(s), ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < S::CHUNKS; ++c) {
+            const uint64_t xd = mn_desc(tiles + X + (uint32_t)(s * S::X_BYTES + c * 2 * S::BOX), S::BOX);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+              for (int half = 0; half < 2; ++half)
+                umma(tmem_base + (uint32_t)(c * KB * 64), xd + 128 * ks,
+                     mn_desc(dl + (uint32_t)(half * S::DL_HALF + i * S::BOX), 2 * S::BOX) + 128 * ks, id_w, (h | ks | half) != 0 ? 1u : 0u);
+          }
+          umma_commit(xempty(s));
+          if (++s == S::NST) { s = 0; ph ^= 1u; }
+        }
+        if (ok) umma_commit(dempty(buf));
+      }
+      if (ok) umma_commit(wdone);
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue: two warps per quarter of the lanes
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    uint8_t* stg = gen + S::STG_OFF + (warp - 2) * WIDE_BYTES;
+    int sl = 0;
+    uint32_t slp = 0;
+    bool ok = true;
+    for (int b = 0; ok && b < blocks; ++b) {
+      const int64_t row = first + (int64_t)b * 128 + quarter * 32;
+      const bool full_rows = row + 32 <= last, row_ok = row + lane < last;
+      for (int u = 0; u < S::CHUNKS; ++u) {
+        ok = mbar_wait(sfull(sl), slp, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t g[64], w[32];
+        const uint32_t taddr = tmem_base + lanes + (uint32_t)(S::DW_COLS + sl * 128 + half * 64);
+        tmem_ld32(taddr, g);
+        tmem_ld32(taddr + 32u, g + 32);
+        tmem_ld_wait();
+        tc_fence_before();
+        mbar_arrive(sempty(sl));
+        if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
+        const int col = c0 + u * 128 + half * 64;
+        if (col < ar.d) put_wide(w, full_rows, row_ok, stg, &mp.o, col, (int)row, ar.dx + (row + lane) * ar.d + col, (ar.d - col) * 2);
+      }
+    }
+    if (ok) {
+      ok = mbar_wait(wdone, 0u, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+    }
+    if (ok) {                                                     // lane: a column; 16 experts at a time, the halves in turn
+      tc_fence_after();
+      float* part = ar.parts + (int64_t)range * ar.E * ar.d;
+#pragma unroll 1
+      for (int c = 0; c < S::CHUNKS; ++c) {
+        const int col = c0 + c * 128 + quarter * 32 + lane;
+#pragma unroll 1
+        for (int e0 = half * 16; e0 < ar.E; e0 += 32) {
+          uint32_t g[16];
+          tmem_ld16(tmem_base + lanes + (uint32_t)(c * KB * 64 + e0), g);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (e0 + i < ar.E && col < ar.d) part[(int64_t)(e0 + i) * ar.d + col] = __uint_as_float(g[i]);
+        }
+      }
+      tc_fence_before();
+    }
+    if (lane == 0) bulk_wait_all();                               // this lane's stores have landed before the CTA ends
+  }
+
+  // ------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {                // a wait ran out: copies may still be on their way to this shared memory (10 ms)
+    const long long t0 = clock64();
+    while (clock64() - t0 < 20000000LL) {}
+    __syncthreads();
+  }
+  if (warp == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+  if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
+}
+
+// Half of `pair`: [N, Eq] in rows of 2 Eq, boxes of 64 columns by 128 rows
+bool make_half_map(CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {cols * 4};
+  cuuint32_t box[2] = {64, 128};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int slices_of(int d, int E) { return (int)ceil_div(d, E <= 64 ? RG<1>::DC : RG<2>::DC); }
+
+template <int KB>
+int run(const RGMaps& mp, const RGArgs& ar, int ranges, cudaStream_t st) {
+  const cudaError_t err = cudaFuncSetAttribute(k_route_grad<KB>, cudaFuncAttributeMaxDynamicSharedMemorySize, RG<KB>::SMEM);
+  if (err != cudaSuccess) return note_cuda(err);
+  const int rc = note_cuda(launch_chained(k_route_grad<KB>, (unsigned)(ar.slices * ranges), TC_THREADS, RG<KB>::SMEM, st, mp, ar));
+  count_launch(1);
+  return rc;
+}
+
+}  // namespace
+
+// Ranges of whole stages of 64 tokens, none of them empty: one wave of CTAs, 128 tokens each at least.
+int route_grad_tc_ranges(int64_t N, int d, int E) {
+  const int64_t units = ceil_div(N, 64), wave = sm_count() / slices_of(d, E), most = ceil_div(units, 2);
+  int64_t r = wave < most ? wave : most;
+  if (r < 1) r = 1;
+  return (int)ceil_div(units, ceil_div(units, r));
+}
+
+int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
+                  int32_t* dev_status, cudaStream_t st) {
+  RGMaps mp = {};
+  if (!make_half_map(&mp.hi, pair, (uint64_t)Eq, (uint64_t)N) || !make_half_map(&mp.lo, (const uint8_t*)pair + 2 * Eq, (uint64_t)Eq, (uint64_t)N) ||
+      !make_map(&mp.x, x, (uint64_t)d, (uint64_t)N, 0, 64) || !make_map(&mp.w, w, (uint64_t)d, (uint64_t)E, 0, 64) ||
+      !make_wide_map(&mp.o, dx, (uint64_t)d, (uint64_t)N, 2))
+    return note_cuda(cudaErrorInvalidValue);
+  RGArgs ar = {};
+  ar.N = N; ar.d = d; ar.E = E;
+  ar.slices = slices_of(d, E);
+  ar.per = (int)(ceil_div(ceil_div(N, 64), ranges) * 64);
+  ar.dx = (__nv_bfloat16*)dx; ar.parts = parts; ar.dev_status = dev_status;
+  return E <= 64 ? run<1>(mp, ar, ranges, st) : run<2>(mp, ar, ranges, st);
+}
+
+}  // namespace capmoe
