@@ -5,9 +5,9 @@
 //   dx = dl W_r,   dW_r = dl^T x,   dbias = sum_t dl
 // Three forms of the products, all with fp32 accumulation and parts of dW_r and dbias over ranges of tokens that one last kernel
 // adds in their order:
-//   E <= 16       k_route_grad_few: everything in one kernel on plain FMAs, W_r and dW_r in registers
-//   bf16, E <= 128, whole 16-byte vectors   k_route_logit_grad, then both products in one pass over x (route_grad_tc.cu)
-//   other sizes   k_route_logit_grad, then the grouped products (gmm.cuh) of one expert (dx) and of ranges of tokens (dW_r)
+//   bf16, rows of whole 16-byte vectors   k_route_logit_grad, then both products in one pass over x (route_grad_tc.cu)
+//   others, E <= 16   k_route_grad_few: everything in one kernel on plain FMAs, W_r and dW_r in registers
+//   others            k_route_logit_grad, then the grouped products (gmm.cuh) of one expert (dx) and of ranges of tokens (dW_r)
 // bf16 products on tensor cores: dl is fp32, and one rounding to bf16 could cost it 2^-8; it goes in as two bf16 numbers, its
 // rounding and the rounding of what that leaves out (2^-16 of dl is lost at most).
 #include "route_grad.cuh"
@@ -31,12 +31,13 @@ struct LogitArgs {
   int ranges, range;
 };
 
-// One warp a token, lane + 32 i an expert.
+// A warp takes four tokens at a time (their lookups in flight together), lane + 32 i an expert of each.
+constexpr int RG_TOK = 4;
 template <int EPL>
 __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitArgs a) {
   wait_for_previous_kernel();
   allow_next_kernel();                       // in this order: an early successor reads what came before (gmm.cuh)
-  __shared__ float ds[RG_WARPS][EPL * 32];
+  __shared__ float ds[RG_WARPS][RG_TOK][EPL * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.s.E;
   const int64_t tid = (int64_t)blockIdx.x * (RG_WARPS * 32) + threadIdx.x, threads = (int64_t)gridDim.x * (RG_WARPS * 32);
   if (a.offsets) {
@@ -44,55 +45,77 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
     if (tid <= a.ranges) a.offsets[2 + tid] = (int32_t)min(a.s.N, tid * (int64_t)a.range);
   }
   if (a.w2) {
-    const int64_t half = (int64_t)a.Eq * a.d;
-    for (int64_t i = tid; i < 2 * half; i += threads) {
-      const int64_t j = i < half ? i : i - half;
-      a.w2[i] = j < (int64_t)E * a.d ? a.w[j] : __float2bfloat16_rn(0.f);
+    const int64_t half = (int64_t)a.Eq * a.d, have = (int64_t)E * a.d;       // (Eq is a multiple of 8: both in whole vectors)
+    const bool vec = have % 8 == 0;
+    for (int64_t i = tid * 8; i < half; i += threads * 8) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (vec) {
+        if (i < have) v = *reinterpret_cast<const uint4*>(a.w + i);
+      } else {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = i + j < have ? __bfloat162float(a.w[i + j]) : 0.f;
+        v = Vec16<__nv_bfloat16>::store(f);
+      }
+      *reinterpret_cast<uint4*>(a.w2 + i) = v;
+      *reinterpret_cast<uint4*>(a.w2 + half + i) = v;
     }
   }
   float bias[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) bias[i] = 0.f;
-  for (int64_t t = (int64_t)blockIdx.x * RG_WARPS + warp; t < a.s.N; t += (int64_t)gridDim.x * RG_WARPS) {
-    float* row = ds[warp];
-    float s[EPL], g[EPL], dot = 0.f;
+  for (int64_t t0 = ((int64_t)blockIdx.x * RG_WARPS + warp) * RG_TOK; t0 < a.s.N; t0 += (int64_t)gridDim.x * RG_WARPS * RG_TOK) {
+    const int n = (int)min((int64_t)RG_TOK, a.s.N - t0);
+    float s[RG_TOK][EPL];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = lane + 32 * i;
-      s[i] = e < E ? a.s.scores[t * E + e] : 0.f;
-      row[e] = a.s.dscores && e < E ? a.s.dscores[t * a.s.dscores_ld + e] : 0.f;
-    }
+    for (int j = 0; j < RG_TOK; ++j)
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        const int e = lane + 32 * i;
+        const bool in = j < n && e < E;
+        s[j][i] = in ? a.s.scores[(t0 + j) * E + e] : 0.f;
+        ds[warp][j][e] = in && a.s.dscores ? a.s.dscores[(t0 + j) * a.s.dscores_ld + e] : 0.f;
+      }
     __syncwarp();
-    add_kept(a.s, t, lane, 32, row);
+    add_kept(a.s, t0, n, lane, 32, ds[warp][0], EPL * 32);
     __syncwarp();
+    float dot[RG_TOK];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      g[i] = row[lane + 32 * i];
-      dot = fmaf(s[i], g[i], dot);
+    for (int j = 0; j < RG_TOK; ++j) {
+      dot[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) dot[j] = fmaf(s[j][i], ds[warp][j][lane + 32 * i], dot[j]);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = lane + 32 * i;
-      const float dl = e < E ? s[i] * (g[i] - dot) : 0.f;
-      bias[i] += dl;
-      if (e < E) a.dlogits[t * E + e] = dl;
-      if (a.pair && e < a.Eq) {
-        const __nv_bfloat16 hi = __float2bfloat16_rn(dl);
-        a.pair[t * 2 * a.Eq + e] = hi;
-        a.pair[t * 2 * a.Eq + a.Eq + e] = __float2bfloat16_rn(dl - __bfloat162float(hi));
+      for (int j = 0; j < RG_TOK; ++j) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
+#pragma unroll
+    for (int j = 0; j < RG_TOK; ++j) {
+      if (j >= n) break;
+      const int64_t t = t0 + j;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        const int e = lane + 32 * i;
+        const float dl = e < E ? s[j][i] * (ds[warp][j][e] - dot[j]) : 0.f;
+        bias[i] += dl;
+        if (e < E) a.dlogits[t * E + e] = dl;
+        if (a.pair && e < a.Eq) {
+          const __nv_bfloat16 hi = __float2bfloat16_rn(dl);
+          a.pair[t * 2 * a.Eq + e] = hi;
+          a.pair[t * 2 * a.Eq + a.Eq + e] = __float2bfloat16_rn(dl - __bfloat162float(hi));
+        }
       }
     }
-    __syncwarp();                            // row is rewritten by the next token
+    __syncwarp();                            // the rows are rewritten for the next tokens
   }
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) ds[warp][lane + 32 * i] = bias[i];
+  for (int i = 0; i < EPL; ++i) ds[warp][0][lane + 32 * i] = bias[i];
   __syncthreads();
   for (int e = threadIdx.x; e < E; e += RG_WARPS * 32) {
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < RG_WARPS; ++i) sum += ds[i][e];
+    for (int i = 0; i < RG_WARPS; ++i) sum += ds[i][0][e];
     a.dbias_part[(int64_t)blockIdx.x * E + e] = sum;
   }
 }
@@ -105,20 +128,31 @@ constexpr int FEW_N = 256;                   // threads
 constexpr int FEW_TOK = 64;                  // tokens of a chunk
 constexpr int V = 4;
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void few_load(const T* p, int step, int left, float* f) {      // V columns, `step` apart (1 with VEC)
-  if constexpr (VEC && sizeof(T) == 2) {
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
-    f[0] = __uint_as_float(q.x << 16); f[1] = __uint_as_float(q.x & 0xffff0000u);
-    f[2] = __uint_as_float(q.y << 16); f[3] = __uint_as_float(q.y & 0xffff0000u);
-  } else if constexpr (VEC) {
-    const float4 q = *reinterpret_cast<const float4*>(p);
-    f[0] = q.x; f[1] = q.y; f[2] = q.z; f[3] = q.w;
-  } else {
+// V columns as they are stored, `step` apart (1 with VEC); without VEC columns that do not exist repeat the last one.
+template <typename T, bool VEC> struct Few {
+  T v[V];
+  __device__ __forceinline__ void load(const T* p, int step, int left) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = j * step < left ? to_float(p[j * step]) : 0.f;
+    for (int j = 0; j < V; ++j) v[j] = p[j * step < left ? j * step : 0];
   }
-}
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = to_float(v[j]);
+  }
+};
+template <> struct Few<__nv_bfloat16, true> {
+  uint2 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int, int) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float* f) const {
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+};
+template <> struct Few<float, true> {
+  float4 v;
+  __device__ __forceinline__ void load(const float* p, int, int) { v = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void get(float* f) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+};
 template <typename T, bool VEC>
 __device__ __forceinline__ void few_store(T* p, int step, int left, const float* f) {
   if constexpr (VEC && sizeof(T) == 2) {
@@ -143,10 +177,10 @@ struct FewArgs {
 };
 
 template <typename T, bool VEC, int EM>
-__global__ void __launch_bounds__(FEW_N) k_route_grad_few(const FewArgs<T> a) {
+__global__ void __launch_bounds__(FEW_N, EM == 8 ? 2 : 1) k_route_grad_few(const FewArgs<T> a) {
   allow_next_kernel();
   wait_for_previous_kernel();
-  constexpr int U = EM == 8 ? 8 : 4;         // tokens in flight
+  constexpr int U = 8;                       // tokens in flight
   __shared__ float dl[FEW_TOK][EM];
   __shared__ float sum[FEW_N][V];
   const int E = a.s.E, d = a.d, tx = a.tx, ty = FEW_N / tx, cx = threadIdx.x & (tx - 1), cy = threadIdx.x / tx;
@@ -159,44 +193,52 @@ __global__ void __launch_bounds__(FEW_N) k_route_grad_few(const FewArgs<T> a) {
   for (int e = 0; e < EM; ++e) {
 #pragma unroll
     for (int j = 0; j < V; ++j) w[e][j] = dw[e][j] = 0.f;
-    if (e < E && cols) few_load<T, VEC>(a.w + (int64_t)e * d + c, step, left, w[e]);
+    if (e < E && cols) {
+      Few<T, VEC> q;
+      q.load(a.w + (int64_t)e * d + c, step, left);
+      q.get(w[e]);
+    }
   }
   for (int64_t t0 = first; t0 < last; t0 += FEW_TOK) {
     const int n = (int)min((int64_t)FEW_TOK, last - t0);
-    const int e = threadIdx.x & (EM - 1);
+    const int e = threadIdx.x & (EM - 1), i0 = threadIdx.x / EM;
+    constexpr int EACH = FEW_TOK * EM / FEW_N, BY = FEW_N / EM;         // tokens of a thread's expert, tokens between them
+    float s[EACH];
     __syncthreads();                         // the last chunk's dl has been read
 #pragma unroll
-    for (int i = threadIdx.x / EM; i < FEW_TOK; i += FEW_N / EM) {
-      const int64_t t = t0 + i;
+    for (int m = 0; m < EACH; ++m) {
+      const int i = i0 + m * BY;
       const bool mine = i < n && e < E;
-      const float s = mine ? a.s.scores[t * E + e] : 0.f;
-      dl[i][e] = mine && a.s.dscores ? a.s.dscores[t * a.s.dscores_ld + e] : 0.f;
-      __syncwarp();
-      if (i < n) add_kept(a.s, t, e, EM, dl[i]);
-      __syncwarp();
+      s[m] = mine ? a.s.scores[(t0 + i) * E + e] : 0.f;
+      dl[i][e] = mine && a.s.dscores ? a.s.dscores[(t0 + i) * a.s.dscores_ld + e] : 0.f;
+    }
+    __syncthreads();
+    add_kept(a.s, t0, n, threadIdx.x, FEW_N, &dl[0][0], EM);
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < EACH; ++m) {
+      const int i = i0 + m * BY;
       const float g = dl[i][e];
-      float dot = s * g;
+      float dot = s[m] * g;
 #pragma unroll
       for (int o = EM / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      const float v = mine ? s * (g - dot) : 0.f;
+      const float v = i < n && e < E ? s[m] * (g - dot) : 0.f;
       dl[i][e] = v;
       bias += v;
-      if (mine && blockIdx.x == 0) a.dlogits[t * E + e] = v;
+      if (i < n && e < E && blockIdx.x == 0) a.dlogits[(t0 + i) * E + e] = v;
     }
     __syncthreads();
     if (cols)
-      for (int i0 = cy; i0 < n; i0 += ty * U) {
-        float x[U][V];
+      for (int i1 = cy; i1 < n; i1 += ty * U) {
+        Few<T, VEC> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u].load(a.x + (t0 + min(i1 + u * ty, n - 1)) * d + c, step, left);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int i = i0 + u * ty;
-          if (i < n) few_load<T, VEC>(a.x + (t0 + i) * d + c, step, left, x[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = i0 + u * ty;
+          const int i = i1 + u * ty;
           if (i >= n) break;
-          float y[V] = {0.f, 0.f, 0.f, 0.f};
+          float f[V], y[V] = {0.f, 0.f, 0.f, 0.f};
+          x[u].get(f);
 #pragma unroll
           for (int e4 = 0; e4 < EM; e4 += 4) {
             const float4 q = *reinterpret_cast<const float4*>(&dl[i][e4]);
@@ -206,7 +248,7 @@ __global__ void __launch_bounds__(FEW_N) k_route_grad_few(const FewArgs<T> a) {
 #pragma unroll
               for (int j = 0; j < V; ++j) {
                 y[j] = fmaf(l[m], w[e4 + m][j], y[j]);
-                dw[e4 + m][j] = fmaf(l[m], x[u][j], dw[e4 + m][j]);
+                dw[e4 + m][j] = fmaf(l[m], f[j], dw[e4 + m][j]);
               }
           }
           few_store<T, VEC>(a.dx + (t0 + i) * d + c, step, left, y);
@@ -244,6 +286,7 @@ __global__ void __launch_bounds__(FEW_N) k_route_grad_few(const FewArgs<T> a) {
 // dW_r [E, d] from parts [ranges][copies][rows][d] (copies = 2: both halves of dl) and, in the blocks behind, dbias [E] from parts
 // [bias_parts][E], all in a fixed order.
 constexpr int JOIN_N = 256, JOIN_E = 8;      // threads; experts of a block for dbias
+constexpr int JOIN_G = 8;                    // threads that share an output's parts (every JOIN_G-th each, their loads in flight together)
 template <typename TO, int VW>
 __global__ void __launch_bounds__(JOIN_N) k_join_route(const float* __restrict__ part, int parts, int64_t each, int64_t size, int dw_blocks,
                                                        TO* __restrict__ dw, const float* __restrict__ bias_part, int bias_parts, int E,
@@ -251,22 +294,34 @@ __global__ void __launch_bounds__(JOIN_N) k_join_route(const float* __restrict__
   allow_next_kernel();
   wait_for_previous_kernel();
   if ((int)blockIdx.x < dw_blocks) {
-    const int64_t i = ((int64_t)blockIdx.x * JOIN_N + threadIdx.x) * VW;
-    if (i >= size) return;
+    __shared__ float share[JOIN_N][VW];
+    constexpr int COLS = JOIN_N / JOIN_G;
+    const int col = threadIdx.x & (COLS - 1), g = threadIdx.x / COLS;
+    const int64_t i = ((int64_t)blockIdx.x * COLS + col) * VW;
     float s[VW];
 #pragma unroll
     for (int j = 0; j < VW; ++j) s[j] = 0.f;
-#pragma unroll 8
-    for (int p = 0; p < parts; ++p) {
-      if constexpr (VW == 4) {
-        const float4 v = __ldcs(reinterpret_cast<const float4*>(part + p * each + i));
-        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
-      } else {
-        s[0] += part[p * each + i];
+    if (i < size)
+#pragma unroll 4
+      for (int p = g; p < parts; p += JOIN_G) {
+        if constexpr (VW == 4) {
+          const float4 v = __ldcs(reinterpret_cast<const float4*>(part + p * each + i));
+          s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+        } else {
+          s[0] += part[p * each + i];
+        }
       }
-    }
 #pragma unroll
-    for (int j = 0; j < VW; ++j) dw[i + j] = from_float<TO>(s[j]);
+    for (int j = 0; j < VW; ++j) share[threadIdx.x][j] = s[j];
+    __syncthreads();
+    if (g == 0 && i < size) {
+#pragma unroll
+      for (int k = 1; k < JOIN_G; ++k)
+#pragma unroll
+        for (int j = 0; j < VW; ++j) s[j] += share[k * COLS + col][j];
+#pragma unroll
+      for (int j = 0; j < VW; ++j) dw[i + j] = from_float<TO>(s[j]);
+    }
     return;
   }
   __shared__ float sum[JOIN_N];
@@ -288,7 +343,7 @@ template <typename TO>
 int join_run(const float* part, int parts, int64_t each, int64_t size, void* dw, const float* bias_part, int bias_parts, int E, float* dbias,
              cudaStream_t st) {
   const bool wide = each % 4 == 0 && size % 4 == 0;
-  const int64_t dw_blocks = parts ? ceil_div(size, (int64_t)JOIN_N * (wide ? 4 : 1)) : 0, blocks = dw_blocks + ceil_div(E, JOIN_E);
+  const int64_t dw_blocks = parts ? ceil_div(size, (int64_t)(JOIN_N / JOIN_G) * (wide ? 4 : 1)) : 0, blocks = dw_blocks + ceil_div(E, JOIN_E);
   if (blocks > 0x7fffffff) return CAPMOE_EUNSUPPORTED;
   auto k = wide ? k_join_route<TO, 4> : k_join_route<TO, 1>;
   const int rc = note_cuda(launch_chained(k, (unsigned)blocks, JOIN_N, 0, st, part, parts, each, size, (int)dw_blocks, (TO*)dw, bias_part, bias_parts, E,
@@ -313,7 +368,7 @@ int few_tx(int d) {
 RouteWs route_ws(int64_t N, int d, int E, int dtype) {
   RouteWs w = {};
   const bool bf16 = dtype == CAPMOE_BF16;
-  w.form = E <= 16 ? FEW : route_grad_tc_supported(d, E, dtype) ? TC : GENERAL;
+  w.form = route_grad_tc_supported(d, dtype) ? TC : E <= 16 ? FEW : GENERAL;
   w.copies = w.form != FEW && bf16 ? 2 : 1;
   w.Eq = w.copies == 2 ? (E + 7) / 8 * 8 : E;                // rows of `pair` in whole 16-byte vectors
   const int64_t sms = sm_count();
@@ -332,7 +387,7 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
     const int64_t r = want < most ? want : most;
     w.ranges = (int)(r < 1 ? 1 : r > 64 ? 64 : r);
   }
-  const int64_t want = ceil_div(N, RG_WARPS), most = sms * RG_BLOCKS;
+  const int64_t want = ceil_div(N, RG_WARPS * RG_TOK), most = sms * RG_BLOCKS;
   w.blocks = w.form == FEW ? w.ranges : (int)(want < most ? want : most);
   if (w.ranges < 1) w.ranges = 1;
   if (w.blocks < 1) w.blocks = 1;

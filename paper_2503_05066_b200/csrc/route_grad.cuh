@@ -12,22 +12,26 @@ struct ScoreGrad {
   int E, k, slots, D;
 };
 
-// Adds dweight of token t's kept rows to its row of dS (shared memory; E words, set to dscores before), the lanes lane,
-// lane + lanes .. of the slots.  A token has one row of an expert: each word has one addition, whatever the order of the lanes.
-__device__ __forceinline__ void add_kept(const ScoreGrad& a, int64_t t, int lane, int lanes, float* row) {
-  for (int s = lane; s < a.slots; s += lanes) {
-    const int32_t r = a.slot_row[t * a.slots + s];
+// Adds dweight of the kept rows of tokens t0 .. t0 + n - 1 to their rows of dS (shared memory, `ld` words apart, set to dscores
+// before), the (token, slot) pairs spread over threads `me` of `of`, so that the lookups of many tokens are in flight together.
+// A token has one row of an expert: each word has one addition, whatever the order.
+__device__ __forceinline__ void add_kept(const ScoreGrad& a, int64_t t0, int n, int me, int of, float* ds, int ld) {
+  const int pairs = n * a.slots, m = a.D > 0 ? a.E / a.D : 0;
+  for (int i = me; i < pairs; i += of) {
+    const int32_t r = a.slot_row[t0 * a.slots + i];
+    const int tok = i / a.slots, s = i - tok * a.slots;
+    const int64_t t = t0 + tok;
     if (r >= 0 && r < a.rows) {
-      const int e = s < a.k ? a.topk_idx[t * a.k + s] : home_group(t, a.N, a.D, a.token_group) * (a.E / a.D) + (s - a.k);
-      if ((unsigned)e < (unsigned)a.E) atomicAdd(&row[e], a.dweight[r]);
+      const int e = s < a.k ? a.topk_idx[t * a.k + s] : home_group(t, a.N, a.D, a.token_group) * m + (s - a.k);
+      if ((unsigned)e < (unsigned)a.E) atomicAdd(&ds[tok * ld + e], a.dweight[r]);
     }
   }
 }
 
-// dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05: bf16, d a multiple of 8, E <= 128.
+// dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05: bf16, d a multiple of 8.
 // pair [N, 2 Eq]: dl as two bf16 numbers, Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the stream
 // wrote `pair` and let its successor start only after its own wait for what came before.
-inline bool route_grad_tc_supported(int d, int E, int dtype) { return dtype == CAPMOE_BF16 && d % 8 == 0 && E > 16 && E <= 128; }
+inline bool route_grad_tc_supported(int d, int dtype) { return dtype == CAPMOE_BF16 && d % 8 == 0; }
 int route_grad_tc_ranges(int64_t N, int d, int E);
 int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
                   int32_t* dev_status, cudaStream_t st);

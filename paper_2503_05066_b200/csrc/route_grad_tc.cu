@@ -2,34 +2,36 @@
 //   dx[t] = sum_e dl[t,e] W_r[e],   dW_r[e] = sum_t dl[t,e] x[t]
 // dl comes as two bf16 numbers per element (route_grad.cu), each multiplied on its own into the same fp32 accumulators.
 // A CTA owns DC columns of x, W_r and dx and a range of tokens, which it walks in blocks of 128.  W_r's columns stay in shared
-// memory.  Of a block, dl (128 x E, both halves) is the A operand of dx = dl W_r (tokens are the M side, 128 columns the N side)
-// and, read along the other axis from the same bytes, the B operand of dW_r^T = x^T dl (128 columns are the M side, experts the N
-// side); x comes in stages of 64 tokens.  dW_r^T stays in tensor memory until the range ends and leaves as a part, fp32, that
-// route_grad.cu adds up in order; dx passes through three accumulators of 128 columns, so that its epilogue overlaps the MMAs.
-//   E <= 64: DC = 256, dl double-buffered, x in three stages of 32 KB;  E <= 128: DC = 128, x in two stages of 16 KB
+// memory.  dl of a block comes in tiles of 64 experts (128 x 64, both halves, 32 KB): a tile is the A operand of dx = dl W_r
+// (tokens are the M side, 128 columns the N side) and, read along the other axis from the same bytes, the B operand of
+// dW_r^T = x^T dl (128 columns are the M side, experts the N side); x comes in stages of 64 tokens and stays for all tiles of its
+// block.  dW_r^T stays in tensor memory until the range ends and leaves as a part, fp32, that route_grad.cu adds up in order; dx
+// passes through two or three accumulators of 128 columns, so that its epilogue overlaps the MMAs.
 // What bounds it: HBM; x is read and dx written once.  Tensor pipe per 128 tokens x 256 columns, E = 64: about 2600 cycles of the
-// 5500 that the copy bandwidth allows an SM.
+// 5500 that the copy bandwidth allows an SM; from E = 128 on the tensor pipe is the longer of the two.
 #include "gmm_tc.cuh"
 #include "route_grad.cuh"
 
 namespace capmoe {
 namespace {
 
-template <int KB>                            // blocks of 64 experts
+template <int KB>                            // tiles of 64 experts, at most: 1, 2 or 4
 struct RG {
   static constexpr int DC = KB == 1 ? 256 : 128;
   static constexpr int BOX = 64 * 64 * 2;                      // 64 columns by 64 rows, bf16
   static constexpr int W_BYTES = KB * (DC / 64) * BOX;
-  static constexpr int DL_HALF = KB * 2 * BOX;                 // 128 tokens by KB * 64 experts
-  static constexpr int DL_BYTES = 2 * DL_HALF;
+  static constexpr int DL_HALF = 2 * BOX, DL_BYTES = 2 * DL_HALF;      // a tile: 128 tokens by 64 experts, twice
+  static constexpr int RING = KB == 1 ? 2 : 3;                 // tiles of dl
   static constexpr int X_BYTES = (DC / 64) * BOX;
-  static constexpr int NST = KB == 1 ? 3 : 2;
-  static constexpr int DL_OFF = W_BYTES, X_OFF = DL_OFF + 2 * DL_BYTES, STG_OFF = X_OFF + NST * X_BYTES;
-  static constexpr int TAIL = STG_OFF + EPI_WARPS * WIDE_BYTES;
+  static constexpr int NST = KB == 2 ? 4 : 3;                  // stages of x
+  static constexpr bool WIDE = KB < 4;                         // dx leaves in pieces of 64 columns, else 32 (half the staging)
+  static constexpr int STG_BYTES = WIDE ? WIDE_BYTES : STG_WARP_BYTES;
+  static constexpr int DL_OFF = W_BYTES, X_OFF = DL_OFF + RING * DL_BYTES, STG_OFF = X_OFF + NST * X_BYTES;
+  static constexpr int TAIL = STG_OFF + EPI_WARPS * STG_BYTES;
   static constexpr int SMEM = TAIL + 1024 + 256;
   static constexpr int CHUNKS = DC / 128;
-  static constexpr int SLOTS = 3;
   static constexpr int DW_COLS = CHUNKS * KB * 64;             // tensor-memory columns of dW_r^T, then SLOTS x 128 for dx
+  static constexpr int SLOTS = KB < 4 ? 3 : 2;
   static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
   static_assert(DW_COLS + SLOTS * 128 <= 512, "tensor memory");
 };
@@ -48,11 +50,6 @@ __device__ __forceinline__ uint32_t one_idesc(int n, bool a_mn, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(BM >> 4) << 24);
 }
-// MN-major operand whose boxes of 64 output indices lie `apart` bytes from each other
-__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t apart) {
-  return (umma_desc_mn(saddr) & ~((uint64_t)0x3fff << 16)) | ((uint64_t)(apart >> 4) << 16);
-}
-
 template <int KB>
 __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_constant__ RGMaps mp, const __grid_constant__ RGArgs ar) {
   using S = RG<KB>;
@@ -65,17 +62,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bar0 = smem_u32(bars);
-  auto xfull = [&](int s) { return bar0 + 8u * (uint32_t)s; };                 // NST each
+  auto xfull = [&](int s) { return bar0 + 8u * (uint32_t)s; };                 // stages of x
   auto xempty = [&](int s) { return bar0 + 8u * (uint32_t)(4 + s); };
-  auto dfull = [&](int b) { return bar0 + 8u * (uint32_t)(8 + b); };           // dl
-  auto dempty = [&](int b) { return bar0 + 8u * (uint32_t)(10 + b); };
-  auto sfull = [&](int s) { return bar0 + 8u * (uint32_t)(12 + s); };          // dx accumulators
-  auto sempty = [&](int s) { return bar0 + 8u * (uint32_t)(16 + s); };
+  auto dfull = [&](int r) { return bar0 + 8u * (uint32_t)(8 + r); };           // tiles of dl
+  auto dempty = [&](int r) { return bar0 + 8u * (uint32_t)(11 + r); };
+  auto sfull = [&](int s) { return bar0 + 8u * (uint32_t)(14 + s); };          // dx accumulators
+  auto sempty = [&](int s) { return bar0 + 8u * (uint32_t)(17 + s); };
   const uint32_t wfull = bar0 + 8u * 20u, wdone = bar0 + 8u * 21u;             // W_r has arrived; dW_r is complete
 
   if (tid == 0) {
     for (int s = 0; s < S::NST; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(dfull(b), 1); mbar_init(dempty(b), 1); }
+    for (int r = 0; r < S::RING; ++r) { mbar_init(dfull(r), 1); mbar_init(dempty(r), 1); }
     for (int s = 0; s < S::SLOTS; ++s) { mbar_init(sfull(s), 1); mbar_init(sempty(s), EPI_WARPS * 32); }
     mbar_init(wfull, 1);
     mbar_init(wdone, 1);
@@ -97,16 +94,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
   const int64_t first = (int64_t)range * ar.per, last = min(ar.N, first + ar.per);      // first < last
   const int blocks = (int)((last - first + 127) >> 7);
   const int halves = (int)((last - first + 63) >> 6);                                   // stages of x
+  const int kbs = (ar.E + 63) >> 6;                                                     // tiles of a block
   constexpr uint32_t W = 0, DL = S::DL_OFF, X = S::X_OFF;
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (elect_one()) {
       // W_r and x come from before the kernel that makes dl: they are fetched while it still runs
-      mbar_expect_tx(wfull, (uint32_t)S::W_BYTES);
+      mbar_expect_tx(wfull, (uint32_t)(kbs * (S::DC / 64) * S::BOX));
+      for (int kb = 0; kb < kbs; ++kb)
 #pragma unroll
-      for (int i = 0; i < KB * (S::DC / 64); ++i)
-        tma_load_2d(tiles + W + (uint32_t)(i * S::BOX), &mp.w, c0 + i % (S::DC / 64) * 64, i / (S::DC / 64) * 64, wfull);
+        for (int i = 0; i < S::DC / 64; ++i)
+          tma_load_2d(tiles + W + (uint32_t)((kb * (S::DC / 64) + i) * S::BOX), &mp.w, c0 + i * 64, kb * 64, wfull);
       int s = 0, h = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -123,62 +122,69 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
       const int ahead = min(halves, S::NST);
       while (ok && h < ahead) ok = load_x();
       wait_for_previous_kernel();
-      for (int b = 0; ok && b < blocks; ++b) {
-        const int buf = b & 1;
-        if (!mbar_wait(dempty(buf), (((uint32_t)b >> 1) & 1u) ^ 1u, abort_flag)) break;
-        mbar_expect_tx(dfull(buf), (uint32_t)S::DL_BYTES);
-#pragma unroll
-        for (int i = 0; i < KB; ++i) {
-          const uint32_t to = tiles + DL + (uint32_t)(buf * S::DL_BYTES + i * 2 * S::BOX);
-          tma_load_2d(to, &mp.hi, i * 64, (int)first + b * 128, dfull(buf));
-          tma_load_2d(to + (uint32_t)S::DL_HALF, &mp.lo, i * 64, (int)first + b * 128, dfull(buf));
+      int r = 0;
+      uint32_t rph = 0;
+      for (int b = 0; ok && b < blocks; ++b)
+        for (int kb = 0; ok && kb < kbs; ++kb) {
+          if (!mbar_wait(dempty(r), rph ^ 1u, abort_flag)) { ok = false; break; }
+          mbar_expect_tx(dfull(r), (uint32_t)S::DL_BYTES);
+          const uint32_t to = tiles + DL + (uint32_t)(r * S::DL_BYTES);
+          tma_load_2d(to, &mp.hi, kb * 64, (int)first + b * 128, dfull(r));
+          tma_load_2d(to + (uint32_t)S::DL_HALF, &mp.lo, kb * 64, (int)first + b * 128, dfull(r));
+          if (++r == S::RING) { r = 0; rph ^= 1u; }
+          while (ok && h < min(halves, 2 * b + 2)) ok = load_x();    // (the first tile's MMAs are the first to need them)
         }
-        while (ok && h < min(halves, 2 * b + 2)) ok = load_x();
-      }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     if (elect_one()) {
-      const int n_pad = (ar.E + 15) & ~15;
-      const uint32_t id_x = one_idesc(128, false, true), id_w = one_idesc(n_pad, true, true);
-      int s = 0, sl = 0, h = 0;
-      uint32_t ph = 0, slp = 0;
+      const uint32_t id_x = one_idesc(128, false, true);
+      int s = 0, sl = 0, r = 0;
+      uint32_t ph = 0, slp = 0, rph = 0;
       bool ok = mbar_wait(wfull, 0u, abort_flag);
       for (int b = 0; ok && b < blocks; ++b) {
-        const int buf = b & 1;
-        const uint32_t dl = tiles + DL + (uint32_t)(buf * S::DL_BYTES);
-        if (!mbar_wait(dfull(buf), ((uint32_t)b >> 1) & 1u, abort_flag)) { ok = false; break; }
-        for (int u = 0; ok && u < S::CHUNKS; ++u) {               // dx, 128 columns at a time
-          if (!mbar_wait(sempty(sl), slp ^ 1u, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t acc = tmem_base + (uint32_t)(S::DW_COLS + sl * 128);
-          for (int e0 = 0; e0 < ar.E; e0 += 16) {
-            const int kb = e0 >> 6, ks = (e0 >> 4) & 3;
-            const uint64_t wd = mn_desc(tiles + W + (uint32_t)((kb * (S::DC / 64) + u * 2) * S::BOX), S::BOX) + 128 * ks;
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-              umma(acc, umma_desc(dl + (uint32_t)(half * S::DL_HALF + kb * 2 * S::BOX)) + 2 * ks, wd, id_x, (e0 | half) != 0 ? 1u : 0u);
-          }
-          umma_commit(sfull(sl));
-          if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
-        }
-        for (int i = 0; ok && i < 2 && h < halves; ++i, ++h) {    // dW_r^T, 64 tokens at a time
-          if (!mbar_wait(xfull(s), ph, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-#pragma unroll
-          for (int c = 0; c < S::CHUNKS; ++c) {
-            const uint64_t xd = mn_desc(tiles + X + (uint32_t)(s * S::X_BYTES + c * 2 * S::BOX), S::BOX);
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
+        const int here = min(2, halves - 2 * b);                  // stages of x in this block
+        for (int kb = 0; ok && kb < kbs; ++kb) {
+          const uint32_t dl = tiles + DL + (uint32_t)(r * S::DL_BYTES);
+          const int steps = min(4, (ar.E - kb * 64 + 15) >> 4);   // of 16 experts
+          if (!mbar_wait(dfull(r), rph, abort_flag)) { ok = false; break; }
+          for (int u = 0; ok && u < S::CHUNKS; ++u) {             // dx, 128 columns at a time (kbs == 1 where there are two)
+            if (kb == 0 && !mbar_wait(sempty(sl), slp ^ 1u, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t acc = tmem_base + (uint32_t)(S::DW_COLS + sl * 128);
+            const uint64_t wd = umma_desc_mn(tiles + W + (uint32_t)((kb * (S::DC / 64) + u * 2) * S::BOX));
+            for (int ks = 0; ks < steps; ++ks)
 #pragma unroll
               for (int half = 0; half < 2; ++half)
-                umma(tmem_base + (uint32_t)(c * KB * 64), xd + 128 * ks,
-                     mn_desc(dl + (uint32_t)(half * S::DL_HALF + i * S::BOX), 2 * S::BOX) + 128 * ks, id_w, (h | ks | half) != 0 ? 1u : 0u);
+                umma(acc, umma_desc(dl + (uint32_t)(half * S::DL_HALF)) + 2 * ks, wd + 128 * ks, id_x, (kb | ks | half) != 0 ? 1u : 0u);
+            if (kb == kbs - 1) {
+              umma_commit(sfull(sl));
+              if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
+            }
           }
-          umma_commit(xempty(s));
-          if (++s == S::NST) { s = 0; ph ^= 1u; }
+          const uint32_t id_w = one_idesc(steps * 16, true, true);
+          int xs = s;
+          uint32_t xph = ph;
+          for (int i = 0; ok && i < here; ++i) {                  // dW_r^T, 64 tokens at a time
+            if (!mbar_wait(xfull(xs), xph, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < S::CHUNKS; ++c) {
+              const uint64_t xd = umma_desc_mn(tiles + X + (uint32_t)(xs * S::X_BYTES + c * 2 * S::BOX));
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                  umma(tmem_base + (uint32_t)((c * KB + kb) * 64), xd + 128 * ks,
+                       umma_desc_mn(dl + (uint32_t)(half * S::DL_HALF + i * S::BOX)) + 128 * ks, id_w, (b | i | ks | half) != 0 ? 1u : 0u);
+            }
+            if (kb == kbs - 1) umma_commit(xempty(xs));
+            if (++xs == S::NST) { xs = 0; xph ^= 1u; }
+          }
+          if (kb == kbs - 1) { s = xs; ph = xph; }
+          if (ok) umma_commit(dempty(r));
+          if (++r == S::RING) { r = 0; rph ^= 1u; }
         }
-        if (ok) umma_commit(dempty(buf));
       }
       if (ok) umma_commit(wdone);
     }
@@ -186,7 +192,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
     // ------------------------------------------------------------ epilogue: two warps per quarter of the lanes
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    uint8_t* stg = gen + S::STG_OFF + (warp - 2) * WIDE_BYTES;
+    uint8_t* stg = gen + S::STG_OFF + (warp - 2) * S::STG_BYTES;
     int sl = 0;
     uint32_t slp = 0;
     bool ok = true;
@@ -209,7 +215,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
 #pragma unroll
         for (int i = 0; i < 32; ++i) w[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
         const int col = c0 + u * 128 + half * 64;
-        if (col < ar.d) put_wide(w, full_rows, row_ok, stg, &mp.o, col, (int)row, ar.dx + (row + lane) * ar.d + col, (ar.d - col) * 2);
+        __nv_bfloat16* out = ar.dx + (row + lane) * ar.d + col;
+        if constexpr (S::WIDE) {
+          if (col < ar.d) put_wide(w, full_rows, row_ok, stg, &mp.o, col, (int)row, out, (ar.d - col) * 2);
+        } else {
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            if (col + p * 32 < ar.d) store_piece(w + p * 16, full_rows, row_ok, stg, &mp.o, col + p * 32, (int)row, out + p * 32, ar.d - col - p * 32);
+        }
       }
     }
     if (ok) {
@@ -290,14 +303,14 @@ int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int
   RGMaps mp = {};
   if (!make_half_map(&mp.hi, pair, (uint64_t)Eq, (uint64_t)N) || !make_half_map(&mp.lo, (const uint8_t*)pair + 2 * Eq, (uint64_t)Eq, (uint64_t)N) ||
       !make_map(&mp.x, x, (uint64_t)d, (uint64_t)N, 0, 64) || !make_map(&mp.w, w, (uint64_t)d, (uint64_t)E, 0, 64) ||
-      !make_wide_map(&mp.o, dx, (uint64_t)d, (uint64_t)N, 2))
+      !(E <= 128 ? make_wide_map(&mp.o, dx, (uint64_t)d, (uint64_t)N, 2) : make_store_map(&mp.o, dx, (uint64_t)d, (uint64_t)N)))
     return note_cuda(cudaErrorInvalidValue);
   RGArgs ar = {};
   ar.N = N; ar.d = d; ar.E = E;
   ar.slices = slices_of(d, E);
   ar.per = (int)(ceil_div(ceil_div(N, 64), ranges) * 64);
   ar.dx = (__nv_bfloat16*)dx; ar.parts = parts; ar.dev_status = dev_status;
-  return E <= 64 ? run<1>(mp, ar, ranges, st) : run<2>(mp, ar, ranges, st);
+  return E <= 64 ? run<1>(mp, ar, ranges, st) : E <= 128 ? run<2>(mp, ar, ranges, st) : run<4>(mp, ar, ranges, st);
 }
 
 }  // namespace capmoe
