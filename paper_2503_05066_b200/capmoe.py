@@ -445,21 +445,27 @@ def _refuse(where: str, what: str, status: int = EINVAL):
     raise CapmoeError(status, f"{where}: {what}")
 
 
+_fns = {}                   # entry points by name, once the library is loaded
+
+
 def _run(name: str, like, *args):
     """Calls entry point `name` with `args` and the current stream; tensors among the arguments pass as their addresses."""
     here = like.get_device()
-    raw = []
+    raw, tensor = [], torch.Tensor
     for v in args:
-        if isinstance(v, torch.Tensor):
+        if isinstance(v, tensor):
             if v.get_device() != here or here < 0:
                 _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
             assert v.is_contiguous(), "capmoe tensors must be contiguous"
-            raw.append(v.data_ptr())
-        else:
-            raw.append(v)
-    if here != torch._C._cuda_getDevice():
+            v = v.data_ptr()
+        raw.append(v)
+    cuda = torch._C
+    if here != cuda._cuda_getDevice():
         _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
-    rc = getattr(_lib or lib(), name)(*raw, torch._C._cuda_getCurrentRawStream(here))
+    fn = _fns.get(name)
+    if fn is None:
+        fn = _fns[name] = getattr(lib(), name)
+    rc = fn(*raw, cuda._cuda_getCurrentRawStream(here))
     if rc != OK:
         raise CapmoeError(rc, name)
 
@@ -741,15 +747,17 @@ def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None
     if len(shape) != 2 or w.dim() != 1 or w.shape[0] != shape[1] or w.dtype != dtype:
         _refuse(where, "x [N,d] and w [d] of one dtype expected")
     N, d = shape
-    _want(where, "residual", residual, shape, dtype)
+    if residual is not None and (residual.shape != shape or residual.dtype != dtype):
+        _want(where, "residual", residual, shape, dtype)
     r = dict(h=x)
     if out is None:                           # (allocations are most of the call's time: the cheapest form of each)
-        r["y"] = y = torch.empty_like(x)
-        r["rstd"] = rstd = torch.empty(N, dtype=torch.float32, device=x.device)
+        empty, like, dev = torch.empty, torch.empty_like, x.device
+        r["y"] = y = like(x)
+        r["rstd"] = rstd = empty(N, dtype=torch.float32, device=dev)
         if residual is not None:
-            r["h"] = torch.empty_like(x)
+            r["h"] = like(x)
         if fp8:
-            r["q"], r["scale"] = torch.empty_like(x, dtype=FP8), torch.empty(N, _blocks(d), dtype=SCALE, device=x.device)
+            r["q"], r["scale"] = like(x, dtype=FP8), empty(N, _blocks(d), dtype=SCALE, device=dev)
     else:
         r["y"] = y = _out(where, out.get("y"), shape, dtype, x)
         r["rstd"] = rstd = _out(where, out.get("rstd"), (N,), torch.float32, x)

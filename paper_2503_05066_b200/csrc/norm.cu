@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(SUM_COLS * SUM_ROWS) k_sum_parts(const float* 
 constexpr int NORM_VPT = 2;                  // vectors a thread that a row's warps are chosen for, with many rows
 constexpr int GRAD_VPT = 2;                  // the same of the gradient, whose threads also hold dw and w
 constexpr int GRAD_BLOCKS = 2;               // blocks per SM at most
-constexpr int GRAD_DEPTH1 = 4, GRAD_DEPTH2 = 4;   // rows in the ring with one and two vectors a thread
+constexpr int GRAD_DEPTH1 = 3, GRAD_DEPTH2 = 4;   // rows in the ring with one and two vectors a thread
 // Warps to a row: as few as hold it in `vpt` vectors a thread, more while the rows leave warps of the device without one; 16
 // where eight would have to hold more than `most` vectors a thread.
 int warps_per_row(int64_t N, int vecs, int vpt, int most) {
@@ -354,8 +354,10 @@ int grad_run(const GradArgs<T>& a, cudaStream_t st) {
   auto k = room == 1 ? k_rms_norm_grad<T, VEC, 1, GRAD_DEPTH1> : room == 2 ? k_rms_norm_grad<T, VEC, 2, GRAD_DEPTH2>
            : room == 4 ? k_rms_norm_grad<T, VEC, 4, 2> : k_rms_norm_grad<T, VEC, 8, 1>;
   const size_t smem = (size_t)depth * 3 * (size_t)room * threads_of(a.wpr) * 16;
-  const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (err != cudaSuccess) return note_cuda(err);
+  if (smem > 40 * 1024) {                    // (the default limit is 48 KB, what the kernel declares included)
+    const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (err != cudaSuccess) return note_cuda(err);
+  }
   const int rc = note_cuda(launch_chained(k, (unsigned)grad_blocks(a.N, a.wpr), threads_of(a.wpr), smem, st, a));
   count_launch(1);
   return rc;
