@@ -389,7 +389,7 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  * workspace overlap neither each other nor an input, but for dx of capmoe_permute_backward. */
 int capmoe_permute_fp8(const void* x_q, const void* x_scale, int64_t N, int d, int E, int k, int slots, int D, int64_t A_max,
                        const float* scores, const int32_t* topk_idx, const int32_t* token_group, const int32_t* slot_row,
-                       void* q_perm, void* scale_perm, int32_t* perm_token, float* perm_weight, void* stream);
+                       void* q_perm, void* scale_perm, int32_t* perm_token, float* perm_weight, int32_t* dev_status, void* stream);
 int capmoe_combine_backward(const void* dy, const void* y_perm, const int32_t* slot_row, const float* perm_weight, int64_t N,
                             int d, int slots, int dtype, int64_t A_max, void* dy_perm, float* dweight, void* stream);
 int capmoe_permute_backward(const void* dx_perm, const int32_t* slot_row, int64_t N, int d, int slots, int dtype, int64_t A_max,

@@ -434,7 +434,7 @@ _ARGTYPES = {
     "capmoe_grouped_ffn_fp8_codes": [_V, _V, _V, _I, _I, _I, _V, _V, _V, _V, _V, _V, _V, _L, _V, _S, _V, _V],
     "capmoe_rms_norm": [_V, _V, _V, _L, _I, _I, ctypes.c_float, _V, _V, _V, _V, _V, _V],
     "capmoe_rms_norm_backward": [_V, _V, _V, _V, _V, _L, _I, _I, _I, _V, _V, _V, _S, _V],
-    "capmoe_permute_fp8": [_V, _V, _L, _I, _I, _I, _I, _I, _L, _V, _V, _V, _V, _V, _V, _V, _V, _V],
+    "capmoe_permute_fp8": [_V, _V, _L, _I, _I, _I, _I, _I, _L, _V, _V, _V, _V, _V, _V, _V, _V, _V, _V],
     "capmoe_combine_backward": [_V, _V, _V, _V, _L, _I, _I, _I, _L, _V, _V, _V],
     "capmoe_permute_backward": [_V, _V, _L, _I, _I, _I, _L, _V, _V, _V, _V],
     "capmoe_route_backward": [_V, _V, _V, _V, _V, _V, _L, _I, _I, _I, _I, _I, _V, _V, _L, _I, _I, _L, _V, _V, _V, _V, _V, _S, _V, _V],
@@ -825,13 +825,13 @@ def _route_lists(where: str, scores, topk_idx, slot_row, D: int, token_group):
     return N, E, topk_idx.shape[1], _slot_rows(where, slot_row, N)
 
 
-def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0, token_group=None, out=None, stream=None):
+def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0, token_group=None, out=None, dev_status=None, stream=None):
     """permute of 8-bit rows (rms_norm(fp8=True), quantize_rows).  -> dict(x_q [A_max,d], x_scale [A_max, ceil(d/128)],
     perm_token [A_max], perm_weight [A_max]); rows >= A are left unwritten.  `out` may hand in those buffers."""
     where = "capmoe_permute_fp8"
     if stream is not None:
         with torch.cuda.stream(stream):
-            return permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max, D, token_group, out)
+            return permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max, D, token_group, out, dev_status)
     N, E, k, slots = _route_lists(where, scores, topk_idx, slot_row, D, token_group)
     if x_q.dim() != 2 or x_q.shape[0] != N:
         _refuse(where, "x_q [N,d] expected")
@@ -849,7 +849,7 @@ def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0
                  perm_token=_out(where, out.get("perm_token"), (A_max,), torch.int32, x_q),
                  perm_weight=_out(where, out.get("perm_weight"), (A_max,), torch.float32, x_q))
     _run(where, x_q, x_q, x_scale, N, d, E, k, slots, D, A_max, scores, topk_idx, token_group, slot_row, r["x_q"], r["x_scale"],
-         r["perm_token"], r["perm_weight"])
+         r["perm_token"], r["perm_weight"], _status(where, dev_status))
     return r
 
 

@@ -41,7 +41,7 @@ def _slots(N, slots, spare, seed, keep=0.7):
     return slot_row, rows, t, s, r
 
 
-SHAPES = [(1, 1, 8), (1, 4, 64), (3, 2, 136), (33, 8, 256), (200, 3, 1024), (517, 6, 2048), (40, 2, 8192), (64, 33, 264), (20, 288, 128), (300, 1, 4104)]
+SHAPES = [(1, 1, 8), (1, 4, 64), (3, 2, 136), (33, 8, 256), (200, 3, 1024), (517, 6, 2048), (40, 2, 8192), (64, 33, 264), (20, 288, 128), (300, 1, 4104), (30, 70, 4096), (2, 3, 16384), (5, 40, 1032)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -104,7 +104,8 @@ def _expert_of(r, dr, E, D):
 
 
 @pytest.mark.parametrize("N,E,k,D,d", [(1, 2, 1, 0, 16), (7, 8, 2, 0, 128), (130, 60, 4, 0, 2048), (1000, 64, 6, 0, 272), (500, 8, 2, 4, 4096),
-                                       (300, 256, 8, 32, 2064), (900, 130, 6, 10, 48), (100, 64, 2, 1, 160)])
+                                       (300, 256, 8, 32, 2064), (900, 130, 6, 10, 48), (100, 64, 2, 1, 160),
+                                       (70, 8, 2, 0, 16400), (3000, 16, 4, 0, 512), (40, 4, 1, 0, 40000)])
 def test_permute_fp8(cm, N, E, k, D, d):
     r, dr, rows = _routing(cm, N, E, k, D, N)
     rows += 3

@@ -29,7 +29,7 @@ def _calls(cm):
         "norm": (L.capmoe_rms_norm, dict(x=P, res=P, w=P, N=I(8), d=64, dt=1, eps=f(1e-6), h=P, y=P, rstd=P, q=P, sc=P, s=Z)),
         "norm_bwd": (L.capmoe_rms_norm_backward, dict(dy=P, h=P, w=P, rstd=P, dh=P, N=I(8), d=64, dt=1, odt=1, dx=P, dw=P, ws=P, wsb=BIG, s=Z)),
         "perm8": (L.capmoe_permute_fp8, dict(x=P, xs=P, N=I(8), d=64, E=4, k=2, slots=2, D=0, rows=I(16), sc=P, idx=P, tg=Z, sr=P, q=P, qs=P,
-                                             pt=P, pw=P, s=Z)),
+                                             pt=P, pw=P, st=Z, s=Z)),
         "comb_bwd": (L.capmoe_combine_backward, dict(dy=P, yp=P, sr=P, pw=P, N=I(8), d=64, slots=2, dt=1, rows=I(16), dyp=P, dwt=P, s=Z)),
         "perm_bwd": (L.capmoe_permute_backward, dict(dxp=P, sr=P, N=I(8), d=64, slots=2, dt=1, rows=I(16), a=P, b=P, dx=P, s=Z)),
         "route_bwd": (L.capmoe_route_backward, dict(x=P, w=P, sc=P, idx=P, sr=P, dwt=P, N=I(8), d=64, E=4, k=2, slots=2, D=0, tg=Z, ds=Z, ld=I(0), dt=1,
