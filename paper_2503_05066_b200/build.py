@@ -1,4 +1,4 @@
-"""Builds libcapmoe.so (sm_100a only) in-tree with nvcc.  `python -m paper_2503_05066_b200.build`."""
+"""Builds libcapmoe.so (sm_100a only, nvcc) and the Python binding _bind.so (g++) in-tree.  `python -m paper_2503_05066_b200.build`."""
 from __future__ import annotations
 
 import os
@@ -10,6 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcapmoe.so")
+BIND_SRC, BIND = os.path.join(CSRC, "bind.cpp"), os.path.join(PKG, "_bind.so")
 SOURCES = ["api.cu", "route.cu", "drop.cu", "drop_cluster.cu", "drop_parallel.cu", "variants.cu", "permute_combine.cu", "ffn_simt.cu", "ffn_tc.cu", "ffn_tc_t.cu",
            "grouped_mm.cu", "grouped_fp8.cu", "gmm_rows.cu", "gmm_dw.cu", "gmm_swiglu8.cu",
            "norm.cu", "token_grad.cu", "route_grad.cu", "route_grad_tc.cu"]
@@ -24,6 +25,19 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def _bind_cmd() -> list:
+    """The binding against the running interpreter and torch, and the library beside it."""
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"),
+           sysconfig.get_paths()["include"]]
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+            *[a for p in inc for a in ("-isystem", p)], BIND_SRC, "-o", BIND, "-L", PKG, "-l:libcapmoe.so", "-Wl,-rpath,$ORIGIN",
+            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
 def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
@@ -34,9 +48,12 @@ def _stale(obj: str, src: str) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "capmoe.h"), __file__]
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= max(os.path.getmtime(p) for p in deps):
-        return LIB                       # up to date (object files need not exist: only the .so travels)
+    header = os.path.join(ROOT, "include", "capmoe.h")
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))] + [header, __file__]
+    fresh = lambda out, of: not force and os.path.exists(out) and os.path.getmtime(out) >= max(os.path.getmtime(p) for p in of)  # noqa: E731
+    bound = fresh(BIND, [BIND_SRC, header, __file__])
+    if fresh(LIB, deps) and bound:
+        return LIB                       # up to date (object files need not exist: only the .so travel)
     objdir = os.path.join(PKG, "build")
     os.makedirs(objdir, exist_ok=True)
     nvcc = _nvcc()
@@ -53,13 +70,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if r.returncode != 0:
             raise RuntimeError("nvcc failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
         return r.stderr
-    with ThreadPoolExecutor(max_workers=8) as ex:
-        logs = list(ex.map(run, jobs))
-    if verbose:
-        print("\n".join(logs))
-    objs = [os.path.join(objdir, s.replace(".cu", ".o")) for s in SOURCES]
-    if jobs or not os.path.exists(LIB):
-        run([nvcc, "-shared", "-o", LIB, *objs, "-lcudart"])
+    if not fresh(LIB, deps):
+        with ThreadPoolExecutor(max_workers=8) as ex:
+            logs = list(ex.map(run, jobs))
+        if verbose:
+            print("\n".join(logs))
+        run([nvcc, "-shared", "-o", LIB, *[os.path.join(objdir, s.replace(".cu", ".o")) for s in SOURCES], "-lcudart"])
+    if not bound:
+        run(_bind_cmd())
     return LIB
 
 

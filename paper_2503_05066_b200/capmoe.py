@@ -1,4 +1,5 @@
-"""ctypes binding of libcapmoe.so: same names as the C ABI, argument marshalling only.
+"""Binding of libcapmoe.so: same names as the C ABI, argument marshalling only (ctypes, and for the calls of a training or
+decode step, which come every few microseconds, a compiled one: csrc/bind.cpp).
 
 torch is used for device memory and streams; every step of the layer runs inside the CUDA
 library.  If the shared library is missing or cannot be loaded, every call raises: there is
@@ -8,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib
 import math
 import os
 from dataclasses import dataclass
@@ -445,29 +447,31 @@ def _refuse(where: str, what: str, status: int = EINVAL):
     raise CapmoeError(status, f"{where}: {what}")
 
 
-_fns = {}                   # entry points by name, once the library is loaded
+_call = None                # run() of the compiled binding (csrc/bind.cpp), loaded with the library
+
+
+def _load_call():
+    global _call
+    lib()
+    if not os.path.exists(os.path.join(_PKG, "_bind.so")):
+        raise RuntimeError(f"{_PKG}/_bind.so is missing: build it with `python -m paper_2503_05066_b200.build`")
+    _call = importlib.import_module("paper_2503_05066_b200._bind").run
+    return _call
 
 
 def _run(name: str, like, *args):
     """Calls entry point `name` with `args` and the current stream; tensors among the arguments pass as their addresses."""
-    here = like.get_device()
-    raw, tensor = [], torch.Tensor
-    for v in args:
-        if isinstance(v, tensor):
-            if v.get_device() != here or here < 0:
-                _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
-            assert v.is_contiguous(), "capmoe tensors must be contiguous"
-            v = v.data_ptr()
-        raw.append(v)
-    cuda = torch._C
-    if here != cuda._cuda_getDevice():
-        _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
-    fn = _fns.get(name)
-    if fn is None:
-        fn = _fns[name] = getattr(lib(), name)
-    rc = fn(*raw, cuda._cuda_getCurrentRawStream(here))
-    if rc != OK:
+    rc = (_call or _load_call())(name, like, *args)
+    if rc:
         raise CapmoeError(rc, name)
+    if rc is None:                         # nothing was called
+        here = like.get_device()
+        for v in args:
+            if isinstance(v, torch.Tensor):
+                if v.get_device() != here or here < 0:
+                    _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
+                assert v.is_contiguous(), "capmoe tensors must be contiguous"
+        _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
 
 
 def _bytes(fn, *args) -> int:

@@ -1,0 +1,110 @@
+// What a call from Python costs besides its launch: the arguments of a C entry point taken from Python objects, tensors as their
+// addresses on the current stream.  Every conversion goes by the entry point's own parameter types (capmoe.h).  With ctypes the
+// same takes about 3 us of a call, as much as a launch.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <string_view>
+#include <unordered_map>
+#include <utility>
+
+#include "capmoe.h"
+
+namespace {
+
+struct Slot { int64_t i; double f; };            // an argument as an integer or address, and as a number
+constexpr int MAX_ARGS = 32;
+
+template <class T>
+T as(const Slot& s) {
+  if constexpr (std::is_pointer_v<T>) return reinterpret_cast<T>(s.i);
+  else if constexpr (std::is_floating_point_v<T>) return static_cast<T>(s.f);
+  else return static_cast<T>(s.i);
+}
+template <auto Fn> struct Entry;
+template <class... P, int (*Fn)(P...)>
+struct Entry<Fn> {
+  static constexpr int params = sizeof...(P);
+  template <size_t... I>
+  static int call(const Slot* s, std::index_sequence<I...>) { return Fn(as<P>(s[I])...); }
+  static int run(const Slot* s) { return call(s, std::make_index_sequence<sizeof...(P)>{}); }
+};
+struct Call { int (*run)(const Slot*); int params; };
+template <auto Fn> constexpr Call entry() { return {&Entry<Fn>::run, Entry<Fn>::params}; }
+
+const std::unordered_map<std::string_view, Call>& entries() {
+  static const std::unordered_map<std::string_view, Call> table = {
+#define CAPMOE_ENTRY(name) {#name, entry<&name>()}
+      CAPMOE_ENTRY(capmoe_grouped_mm), CAPMOE_ENTRY(capmoe_grouped_mm_dx), CAPMOE_ENTRY(capmoe_grouped_mm_dw),
+      CAPMOE_ENTRY(capmoe_grouped_ffn_backward), CAPMOE_ENTRY(capmoe_quantize_rows), CAPMOE_ENTRY(capmoe_quantize_weights),
+      CAPMOE_ENTRY(capmoe_grouped_mm_fp8), CAPMOE_ENTRY(capmoe_grouped_ffn_fp8), CAPMOE_ENTRY(capmoe_grouped_ffn_fp8_codes),
+      CAPMOE_ENTRY(capmoe_rms_norm), CAPMOE_ENTRY(capmoe_rms_norm_backward), CAPMOE_ENTRY(capmoe_permute_fp8),
+      CAPMOE_ENTRY(capmoe_combine_backward), CAPMOE_ENTRY(capmoe_permute_backward), CAPMOE_ENTRY(capmoe_route_backward),
+#undef CAPMOE_ENTRY
+  };
+  return table;
+}
+
+// run(name, like, *args): the entry point's status, the current stream as its last argument; None where an argument is not what
+// the caller may pass (a tensor that is not on like's device or not contiguous, like's device not the current one), which the
+// caller turns into its message.
+PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n < 2 || !PyUnicode_Check(args[0]) || !THPVariable_Check(args[1])) {
+    PyErr_SetString(PyExc_TypeError, "run(name, like, *args)");
+    return nullptr;
+  }
+  Py_ssize_t length = 0;
+  const char* name = PyUnicode_AsUTF8AndSize(args[0], &length);
+  if (!name) return nullptr;
+  const auto it = entries().find(std::string_view(name, (size_t)length));
+  if (it == entries().end() || n - 1 != it->second.params || n - 1 > MAX_ARGS) {
+    PyErr_Format(PyExc_TypeError, "%s: no such entry point, or %zd arguments are not what it takes", name, n - 2);
+    return nullptr;
+  }
+  const at::Tensor& like = THPVariable_Unpack(args[1]);
+  if (!like.is_cuda()) Py_RETURN_NONE;
+  const auto here = like.get_device();
+  Slot slots[MAX_ARGS];
+  int k = 0;
+  for (Py_ssize_t i = 2; i < n; ++i, ++k) {
+    PyObject* o = args[i];
+    Slot& s = slots[k];
+    if (o == Py_None) {
+      s = {0, 0.0};
+    } else if (THPVariable_Check(o)) {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      if (!t.is_cuda() || t.get_device() != here || !t.is_contiguous()) Py_RETURN_NONE;
+      s = {reinterpret_cast<int64_t>(t.data_ptr()), 0.0};
+    } else if (PyLong_Check(o)) {
+      const long long v = PyLong_AsLongLong(o);
+      if (v == -1 && PyErr_Occurred()) return nullptr;
+      s = {(int64_t)v, (double)v};
+    } else {
+      const double v = PyFloat_AsDouble(o);
+      if (v == -1.0 && PyErr_Occurred()) return nullptr;
+      s = {0, v};
+    }
+  }
+  try {
+    if (c10::cuda::current_device() != here) Py_RETURN_NONE;
+    slots[k] = {reinterpret_cast<int64_t>(c10::cuda::getCurrentCUDAStream(here).stream()), 0.0};
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = it->second.run(slots);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+PyMethodDef methods[] = {{"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, "Calls an entry point of libcapmoe.so."}, {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__bind() { return PyModule_Create(&module); }
