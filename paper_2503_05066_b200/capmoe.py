@@ -447,21 +447,21 @@ def _refuse(where: str, what: str, status: int = EINVAL):
     raise CapmoeError(status, f"{where}: {what}")
 
 
-_call = None                # run() of the compiled binding (csrc/bind.cpp), loaded with the library
+_bind = None                # the compiled binding (csrc/bind.cpp), loaded with the library
 
 
-def _load_call():
-    global _call
+def _binding():
+    global _bind
     lib()
     if not os.path.exists(os.path.join(_PKG, "_bind.so")):
         raise RuntimeError(f"{_PKG}/_bind.so is missing: build it with `python -m paper_2503_05066_b200.build`")
-    _call = importlib.import_module("paper_2503_05066_b200._bind").run
-    return _call
+    _bind = importlib.import_module("paper_2503_05066_b200._bind")
+    return _bind
 
 
 def _run(name: str, like, *args):
     """Calls entry point `name` with `args` and the current stream; tensors among the arguments pass as their addresses."""
-    rc = (_call or _load_call())(name, like, *args)
+    rc = (_bind or _binding()).run(name, like, *args)
     if rc:
         raise CapmoeError(rc, name)
     if rc is None:                         # nothing was called
@@ -755,13 +755,13 @@ def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None
         _want(where, "residual", residual, shape, dtype)
     r = dict(h=x)
     if out is None:                           # (allocations are most of the call's time: the cheapest form of each)
-        empty, like, dev = torch.empty, torch.empty_like, x.device
-        r["y"] = y = like(x)
-        r["rstd"] = rstd = empty(N, dtype=torch.float32, device=dev)
+        new = (_bind or _binding()).new
+        r["y"] = y = new(x, None)
+        r["rstd"] = rstd = new(x, torch.float32, N)
         if residual is not None:
-            r["h"] = like(x)
+            r["h"] = new(x, None)
         if fp8:
-            r["q"], r["scale"] = like(x, dtype=FP8), empty(N, _blocks(d), dtype=SCALE, device=dev)
+            r["q"], r["scale"] = new(x, FP8), new(x, SCALE, N, _blocks(d))
     else:
         r["y"] = y = _out(where, out.get("y"), shape, dtype, x)
         r["rstd"] = rstd = _out(where, out.get("rstd"), (N,), torch.float32, x)
@@ -796,15 +796,16 @@ def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, out_dtype=None,
     _want(where, "dy", dy, shape, dtype)
     _want(where, "dh", dh, shape, dtype)
     _want(where, "rstd", rstd, (N,), torch.float32)
-    dx = torch.empty_like(h) if dx is None else _out(where, dx, shape, dtype, h)
+    new = (_bind or _binding()).new
+    dx = new(h, None) if dx is None else _out(where, dx, shape, dtype, h)
     if dw is None:
-        dw = torch.empty(d, dtype=out_dtype or dtype, device=h.device)
+        dw = new(h, out_dtype, d)
     else:
         _out(where, dw, (d,), out_dtype or dw.dtype, h)
     code = _dt(dtype)
     if ws is None:
         size = _norm_backward_bytes(h.get_device(), N, d, dtype)
-        ws = torch.empty(size, dtype=torch.uint8, device=h.device)
+        ws = new(h, torch.uint8, size)
     else:
         size = ws.numel() * ws.element_size()
     _run(where, h, dy, h, w, rstd, dh, N, d, code, _dt(dw), dx, dw, ws, size)
@@ -845,9 +846,9 @@ def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0
     if x_q.dtype != FP8 or x_scale.dtype != SCALE or x_scale.shape != (N, nb):
         _refuse(where, f"float8_e4m3fn [N,d] with float8_e8m0fnu scales {(N, nb)} expected")
     if out is None:
-        dev = x_q.device
-        r = dict(x_q=torch.empty(A_max, d, dtype=FP8, device=dev), x_scale=torch.empty(A_max, nb, dtype=SCALE, device=dev),
-                 perm_token=torch.empty(A_max, dtype=torch.int32, device=dev), perm_weight=torch.empty(A_max, dtype=torch.float32, device=dev))
+        new = (_bind or _binding()).new
+        r = dict(x_q=new(x_q, FP8, A_max, d), x_scale=new(x_q, SCALE, A_max, nb), perm_token=new(x_q, torch.int32, A_max),
+                 perm_weight=new(x_q, torch.float32, A_max))
     else:
         r = dict(x_q=_out(where, out.get("x_q"), (A_max, d), FP8, x_q), x_scale=_out(where, out.get("x_scale"), (A_max, nb), SCALE, x_q),
                  perm_token=_out(where, out.get("perm_token"), (A_max,), torch.int32, x_q),
@@ -896,7 +897,7 @@ def permute_backward(dx_perm, slot_row, add=None, dx=None, stream=None):
         _refuse(where, "at most two tensors to add", EUNSUPPORTED)
     for t in add:
         _want(where, "add", t, (N, d), dx_perm.dtype)
-    dx = torch.empty(N, d, dtype=dx_perm.dtype, device=dx_perm.device) if dx is None else _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
+    dx = (_bind or _binding()).new(dx_perm, None, N, d) if dx is None else _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
     _run(where, dx_perm, dx_perm, slot_row, N, d, slots, _dt(dx_perm), A_max, *(add + (None, None))[:2], dx)
     return dx
 
@@ -930,12 +931,11 @@ def route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D: int = 0,
     if dscores is not None and dscores.dim() == 2:
         ld = E
     _want(where, "dscores", dscores, (N, E) if ld else (E,), torch.float32)
-    dtype, dev = x.dtype, x.device
+    dtype = x.dtype
     code = _dt(dtype)
+    new = (_bind or _binding()).new
     if out is None:
-        r = dict(dlogits=torch.empty_like(scores), dx=torch.empty_like(x),
-                 dw=torch.empty_like(w_router) if out_dtype is None else torch.empty_like(w_router, dtype=out_dtype),
-                 dbias=torch.empty(E, dtype=torch.float32, device=dev))
+        r = dict(dlogits=new(scores, None), dx=new(x, None), dw=new(w_router, out_dtype), dbias=new(x, torch.float32, E))
     else:
         dw = out.get("dw")
         r = dict(dlogits=_out(where, out.get("dlogits"), (N, E), torch.float32, x), dx=_out(where, out.get("dx"), (N, d), dtype, x),
@@ -943,7 +943,7 @@ def route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D: int = 0,
                  dbias=_out(where, out.get("dbias"), (E,), torch.float32, x))
     if ws is None:
         size = _route_backward_bytes(x.get_device(), N, d, E, dtype)
-        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        ws = new(x, torch.uint8, size)
     else:
         size = ws.numel() * ws.element_size()
     _run(where, x, x, w_router, scores, topk_idx, slot_row, dweight, N, d, E, k, slots, D, token_group, dscores, ld, code, _dt(r["dw"]),

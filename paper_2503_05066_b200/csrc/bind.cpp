@@ -5,6 +5,9 @@
 #include <Python.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <ATen/Functions.h>
+#include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string_view>
@@ -52,6 +55,7 @@ const std::unordered_map<std::string_view, Call>& entries() {
 // the caller may pass (a tensor that is not on like's device or not contiguous, like's device not the current one), which the
 // caller turns into its message.
 PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
   if (n < 2 || !PyUnicode_Check(args[0]) || !THPVariable_Check(args[1])) {
     PyErr_SetString(PyExc_TypeError, "run(name, like, *args)");
     return nullptr;
@@ -88,21 +92,38 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
       s = {0, v};
     }
   }
-  try {
-    if (c10::cuda::current_device() != here) Py_RETURN_NONE;
-    slots[k] = {reinterpret_cast<int64_t>(c10::cuda::getCurrentCUDAStream(here).stream()), 0.0};
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
-  }
+  if (c10::cuda::current_device() != here) Py_RETURN_NONE;
+  slots[k] = {reinterpret_cast<int64_t>(c10::cuda::getCurrentCUDAStream(here).stream()), 0.0};
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = it->second.run(slots);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, "Calls an entry point of libcapmoe.so."}, {nullptr, nullptr, 0, nullptr}};
+// new(like, dtype, *sizes): an uninitialised tensor on like's device, of like's type where dtype is None, and its sizes where there
+// are none: torch.empty without the parsing of its arguments, half of its time.
+PyObject* make(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS                               // torch's exceptions as their Python types, out of memory among them
+  if (n < 2 || n > 6 || !THPVariable_Check(args[0]) || !(args[1] == Py_None || THPDtype_Check(args[1]))) {
+    PyErr_SetString(PyExc_TypeError, "new(like, dtype, *sizes)");
+    return nullptr;
+  }
+  const at::Tensor& like = THPVariable_Unpack(args[0]);
+  int64_t sizes[4];
+  for (Py_ssize_t i = 2; i < n; ++i) {
+    sizes[i - 2] = PyLong_AsLongLong(args[i]);
+    if (sizes[i - 2] == -1 && PyErr_Occurred()) return nullptr;
+  }
+  const auto options = at::TensorOptions().device(like.device()).dtype(
+      args[1] == Py_None ? like.scalar_type() : reinterpret_cast<THPDtype*>(args[1])->scalar_type);
+  return THPVariable_Wrap(at::empty(n == 2 ? like.sizes() : at::IntArrayRef(sizes, (size_t)(n - 2)), options));
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, "Calls an entry point of libcapmoe.so."},
+                         {"new", (PyCFunction)(void (*)(void))make, METH_FASTCALL, "An uninitialised tensor."}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
