@@ -14,7 +14,14 @@ constexpr int NW = 8;                        // warps of a block, `wpr` of them 
 constexpr int NT_MAX = 512;
 constexpr int NORM_MAX_D = 16384;
 
-// The NV columns from p on, as they are stored: one 16-byte access with VEC, else the first `left` one by one.
+// A thread's NV columns of a vector's place u: with VEC (rows that start on 16 bytes) NV in a row, one 16-byte access; else the lanes
+// of a warp take turns, so that their accesses of single elements lie side by side, and a thread's columns are 32 apart.  Both ways
+// a warp has the same 32 NV columns, whole blocks of 128 of them.
+template <bool VEC, int NV>
+__device__ __forceinline__ int column(int u, int tpr, int t) {
+  return VEC ? (u * tpr + t) * NV : (u * tpr + (t & ~31)) * NV + (t & 31);
+}
+// The columns from p on, as they are stored; `left`: columns from there to the end of the row.
 template <typename T, bool VEC>
 __device__ __forceinline__ uint4 get_cells(const T* p, int left) {
   if constexpr (VEC) {
@@ -22,7 +29,7 @@ __device__ __forceinline__ uint4 get_cells(const T* p, int left) {
   } else {
     float f[Vec16<T>::n];
 #pragma unroll
-    for (int i = 0; i < Vec16<T>::n; ++i) f[i] = i < left ? to_float(p[i]) : 0.f;
+    for (int i = 0; i < Vec16<T>::n; ++i) f[i] = i * 32 < left ? to_float(p[i * 32]) : 0.f;
     return Vec16<T>::store(f);
   }
 }
@@ -35,7 +42,7 @@ __device__ __forceinline__ void put_cells(T* p, int left, const uint4& v) {
     Vec16<T>::load(v, f);
 #pragma unroll
     for (int i = 0; i < Vec16<T>::n; ++i)
-      if (i < left) p[i] = from_float<T>(f[i]);
+      if (i * 32 < left) p[i * 32] = from_float<T>(f[i]);
   }
 }
 
@@ -57,34 +64,40 @@ __device__ __forceinline__ float row_sum(float v, int wpr, float* red) {
   return v;
 }
 
-// Codes of NV columns under the scale of their block of 128 (16 lanes of bf16, 32 of fp32), which is made here.
+__device__ __forceinline__ uint32_t two_codes(float a, float b, uint32_t code) {
+  const float inv = inv_scale(code);
+  return code == (uint32_t)Q_NAN_SCALE ? 0x7f7fu : to_e4m3x2(a * inv, b * inv);
+}
+// Codes of a thread's columns under the scales of their blocks of 128, which are made here.
 template <typename T, bool VEC>
 __device__ __forceinline__ void put_codes(const uint4& v, int c, int d, uint8_t* q, uint8_t* scale) {
-  constexpr int NV = Vec16<T>::n, LANES = QBLOCK / NV;
+  // a block: all NV columns of LANES lanes, or, lanes taking turns, PER columns of all lanes
+  constexpr int NV = Vec16<T>::n, LANES = VEC ? QBLOCK / NV : 32, PER = VEC ? NV : QBLOCK / 32;
   float f[NV];
   Vec16<T>::load(v, f);
-  uint32_t m = 0;                            // of non-negative floats the larger has the larger pattern; NaN is above all
 #pragma unroll
-  for (int i = 0; i < NV; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+  for (int b = 0; b < NV; b += PER) {
+    uint32_t m = 0;                          // of non-negative floats the larger has the larger pattern; NaN is above all
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (c >= d) return;
-  const uint32_t code = scale_code(m);
-  uint32_t b[NV / 4];
-  const float inv = inv_scale(code == (uint32_t)Q_NAN_SCALE ? 127u : code);
+    for (int i = 0; i < PER; ++i) m = max(m, __float_as_uint(f[b + i]) & 0x7fffffffu);
 #pragma unroll
-  for (int i = 0; i < NV / 4; ++i)
-    b[i] = code == (uint32_t)Q_NAN_SCALE ? 0x7f7f7f7fu
-                                         : to_e4m3x2(f[4 * i] * inv, f[4 * i + 1] * inv) | to_e4m3x2(f[4 * i + 2] * inv, f[4 * i + 3] * inv) << 16;
-  if constexpr (VEC) {
+    for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const uint32_t code = scale_code(m);
+    const int at = VEC ? c : c + b * 32;     // first of the thread's columns in the block
+    if (at >= d) continue;
 #pragma unroll
-    for (int i = 0; i < NV / 4; ++i) reinterpret_cast<uint32_t*>(q + c)[i] = b[i];
-  } else {
+    for (int i = 0; i < PER; i += 4) {
+      const uint32_t w = two_codes(f[b + i], f[b + i + 1], code) | two_codes(f[b + i + 2], f[b + i + 3], code) << 16;
+      if constexpr (VEC) {
+        *reinterpret_cast<uint32_t*>(q + at + i) = w;
+      } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (c + i < d) q[c + i] = (uint8_t)(b[i / 4] >> (8 * (i & 3)));
+        for (int j = 0; j < 4; ++j)
+          if (at + 32 * (i + j) < d) q[at + 32 * (i + j)] = (uint8_t)(w >> (8 * j));
+      }
+    }
+    if ((threadIdx.x & (LANES - 1)) == 0) scale[at / QBLOCK] = (uint8_t)code;
   }
-  if ((threadIdx.x & (LANES - 1)) == 0) scale[c / QBLOCK] = (uint8_t)code;
 }
 
 template <typename T>
@@ -112,19 +125,19 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
   uint4 v[VPT];
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = (u * tpr + t) * NV;
+    const int c = column<VEC, NV>(u, tpr, t);
     v[u] = live && c < d ? get_cells<T, VEC>(a.x + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
   }
   if (a.res) {
     uint4 r[VPT];
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
-      const int c = (u * tpr + t) * NV;
+      const int c = column<VEC, NV>(u, tpr, t);
       r[u] = live && c < d ? get_cells<T, VEC>(a.res + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
-      const int c = (u * tpr + t) * NV;
+      const int c = column<VEC, NV>(u, tpr, t);
       float f[NV], g[NV];
       Vec16<T>::load(v[u], f);
       Vec16<T>::load(r[u], g);
@@ -151,7 +164,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
   const int nb = (d + QBLOCK - 1) / QBLOCK;
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = (u * tpr + t) * NV;
+    const int c = column<VEC, NV>(u, tpr, t);
     float f[NV], g[NV];
     Vec16<T>::load(v[u], f);
     Vec16<T>::load(c < d ? (VEC ? __ldg(reinterpret_cast<const uint4*>(a.w + c)) : get_cells<T, false>(a.w + c, d - c)) : make_uint4(0u, 0u, 0u, 0u), g);
@@ -196,7 +209,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   wait_for_previous_kernel();
   constexpr int NV = Vec16<T>::n;
   __shared__ float red[2][NT_MAX / 32];
-  extern __shared__ uint4 ring[];            // [DEPTH][dy, h, dh][VPT][threads]
+  extern __shared__ uint4 ring[];            // [PLACES][dy, h, dh][VPT][threads]
   const int tpr = a.wpr * 32, t = threadIdx.x & (tpr - 1), d = a.d;
   const int64_t group = (int64_t)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr, groups = (int64_t)gridDim.x * (blockDim.x / tpr);
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -205,36 +218,59 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   float dw[VPT][NV];
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = (u * tpr + t) * NV;
+    const int c = column<VEC, NV>(u, tpr, t);
     w[u] = c < d ? get_cells<T, VEC>(a.w + c, d - c) : zero;
 #pragma unroll
     for (int i = 0; i < NV; ++i) dw[u][i] = 0.f;
   }
+  // Rows of whole vectors: asynchronous copies, DEPTH - 1 rows ahead.  Others: the next row's elements wait in registers while this
+  // row is worked on (copies of less than four bytes do not exist), and take its place afterwards.
+  constexpr int PLACES = VEC ? DEPTH : 1;
+  T raw[VEC ? 1 : 3][VEC ? 1 : VPT][VEC ? 1 : NV];
+  const T* const from3[3] = {a.dy, a.h, a.dh};
   auto fetch = [&](int64_t row, int slot) {
-    const uint32_t to = mine + (uint32_t)(slot * 3 * VPT) * step;
-    const T* from[3] = {a.dy, a.h, a.dh};
 #pragma unroll
     for (int m = 0; m < 3; ++m)
 #pragma unroll
       for (int u = 0; u < VPT; ++u) {
-        const int c = (u * tpr + t) * NV;
-        const bool in = row < a.N && c < d && from[m];
-        const T* p = in ? from[m] + row * d + c : a.dy;
-        if constexpr (VEC) copy16(to + (uint32_t)(m * VPT + u) * step, p, in);
-        else ring[(size_t)((slot * 3 + m) * VPT + u) * blockDim.x + threadIdx.x] = in ? get_cells<T, false>(p, d - c) : zero;
+        const int c = column<VEC, NV>(u, tpr, t);
+        const bool in = row < a.N && from3[m];
+        const T* p = in ? from3[m] + row * d : a.w;
+        if constexpr (VEC) {
+          copy16(mine + (uint32_t)((slot * 3 + m) * VPT + u) * step, p + (c < d ? c : 0), in && c < d);
+        } else {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) raw[m][u][i] = p[c + i * 32 < d ? c + i * 32 : 0];
+        }
       }
     if constexpr (VEC) copies_commit();
   };
+  auto place = [&](int64_t row, int slot) {  // what fetch left in registers, zeros where there is nothing
+    if constexpr (!VEC) {
 #pragma unroll
-  for (int s = 0; s < DEPTH - 1; ++s) fetch(group + s * groups, s);
+      for (int m = 0; m < 3; ++m)
+#pragma unroll
+        for (int u = 0; u < VPT; ++u) {
+          const int c = column<VEC, NV>(u, tpr, t);
+          float f[NV];
+#pragma unroll
+          for (int i = 0; i < NV; ++i) f[i] = row < a.N && from3[m] && c + i * 32 < d ? to_float(raw[m][u][i]) : 0.f;
+          ring[(size_t)((slot * 3 + m) * VPT + u) * blockDim.x + threadIdx.x] = Vec16<T>::store(f);
+        }
+    }
+  };
+  constexpr int AHEAD = VEC ? DEPTH - 1 : 1;
+#pragma unroll
+  for (int s = 0; s < AHEAD; ++s) fetch(group + s * groups, s);
+  place(group, 0);
   float rstd = group < a.N ? a.rstd[group] : 0.f;
   int it = 0, slot = 0;
   for (int64_t row0 = 0; row0 < a.N; row0 += groups, it ^= 1) {      // the same count in all warps of the block
     const int64_t row = row0 + group;
     const bool live = row < a.N;
-    fetch(row + (DEPTH - 1) * groups, slot == 0 ? DEPTH - 1 : slot - 1);
+    fetch(row + AHEAD * groups, slot == 0 ? PLACES - 1 : slot - 1);
     const float rstd1 = row + groups < a.N ? a.rstd[row + groups] : 0.f;
-    if constexpr (VEC) copies_wait<DEPTH - 1>();
+    if constexpr (VEC) copies_wait<AHEAD>();
     const uint32_t from = mine + (uint32_t)(slot * 3 * VPT) * step;
     uint4 dy[VPT], h[VPT];
     float dot = 0.f;
@@ -256,7 +292,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
     const float k = -row_sum(dot, a.wpr, red[it]) / (float)d * rstd * rstd;
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
-      const int c = (u * tpr + t) * NV;
+      const int c = column<VEC, NV>(u, tpr, t);
       float p[NV], q[NV], g[NV], e[NV];
       Vec16<T>::load(dy[u], p);
       Vec16<T>::load(h[u], q);
@@ -267,20 +303,17 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
       if (live && c < d) put_cells<T, VEC>(a.dx + row * d + c, d - c, Vec16<T>::store(p));
     }
     rstd = rstd1;
-    if (++slot == DEPTH) slot = 0;
+    if (++slot == PLACES) slot = 0;
+    place(row + groups, slot);
   }
   float* part = a.part + group * d;
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = (u * tpr + t) * NV;
+    const int c = column<VEC, NV>(u, tpr, t);
 #pragma unroll
-    for (int i = 0; i < NV; i += 4) {
-      if (VEC && c < d) *reinterpret_cast<float4*>(part + c + i) = make_float4(dw[u][i], dw[u][i + 1], dw[u][i + 2], dw[u][i + 3]);
-      if (!VEC) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (c + i + j < d) part[c + i + j] = dw[u][i + j];
-      }
+    for (int i = 0; i < NV; ++i) {
+      if (VEC && i % 4 == 0 && c < d) *reinterpret_cast<float4*>(part + c + i) = make_float4(dw[u][i], dw[u][i + 1], dw[u][i + 2], dw[u][i + 3]);
+      if (!VEC && c + i * 32 < d) part[c + i * 32] = dw[u][i];
     }
   }
 }
@@ -350,7 +383,7 @@ template <typename T, bool VEC>
 int grad_run(const GradArgs<T>& a, cudaStream_t st) {
   const int vpt = (int)ceil_div(ceil_div(a.d, Vec16<T>::n), 32 * a.wpr);
   const int room = vpt <= 1 ? 1 : vpt <= 2 ? 2 : vpt <= 4 ? 4 : 8;
-  const int depth = room == 1 ? GRAD_DEPTH1 : room == 2 ? GRAD_DEPTH2 : 8 / room;
+  const int depth = !VEC ? 1 : room == 1 ? GRAD_DEPTH1 : room == 2 ? GRAD_DEPTH2 : 8 / room;
   auto k = room == 1 ? k_rms_norm_grad<T, VEC, 1, GRAD_DEPTH1> : room == 2 ? k_rms_norm_grad<T, VEC, 2, GRAD_DEPTH2>
            : room == 4 ? k_rms_norm_grad<T, VEC, 4, 2> : k_rms_norm_grad<T, VEC, 8, 1>;
   const size_t smem = (size_t)depth * 3 * (size_t)room * threads_of(a.wpr) * 16;
