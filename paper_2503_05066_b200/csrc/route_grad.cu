@@ -6,7 +6,7 @@
 // Three forms of the products, all with fp32 accumulation and parts of dW_r and dbias over ranges of tokens that one last kernel
 // adds in their order:
 //   bf16, rows of whole 16-byte vectors   k_route_logit_grad, then both products in one pass over x (route_grad_tc.cu)
-//   others, E <= 16   k_route_grad_few: everything in one kernel on plain FMAs, W_r and dW_r in registers
+//   others, E <= 32   k_route_grad_few: everything in one kernel on plain FMAs, W_r and dW_r in registers
 //   others            k_route_logit_grad, then the grouped products (gmm.cuh) of one expert (dx) and of ranges of tokens (dW_r)
 // bf16 products on tensor cores: dl is fp32, and one rounding to bf16 could cost it 2^-8; it goes in as two bf16 numbers, its
 // rounding and the rounding of what that leaves out (2^-16 of dl is lost at most).
@@ -120,52 +120,54 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
   }
 }
 
-// ---------------------------------------------------------------- up to 16 experts
-// A thread owns V columns: their W_r and dW_r stay in its registers, x goes by once.  A block is `tx` threads across the columns
-// by `ty` tokens at a time; it walks a range of tokens in chunks, whose dl it makes first (EM lanes a token) in shared memory.
-// 16 FMAs an element of x for E = 8: bound by HBM as long as enough loads are in flight (U tokens a thread).
+// ---------------------------------------------------------------- up to 32 experts, plain FMAs
+// A thread owns V columns: their W_r and dW_r (EM >= E experts each, 128 registers at most) stay in its registers, x goes by once.  A
+// block is `tx` threads across the columns by `ty` tokens at a time; it walks a range of tokens in chunks, whose dl it makes first
+// in shared memory.  4 E FMAs an element of x and dx: bound by HBM up to 8 experts or so as long as enough loads are in flight (U
+// tokens a thread), by the FMAs beyond.
 constexpr int FEW_N = 256;                   // threads
 constexpr int FEW_TOK = 64;                  // tokens of a chunk
-constexpr int V = 4;
+constexpr int FEW_MAX_E = 32;
+template <int EM> constexpr int few_v = EM <= 16 ? 4 : 2;
 
-// V columns as they are stored, `step` apart (1 with VEC); without VEC columns that do not exist repeat the last one.
-template <typename T, bool VEC> struct Few {
+template <int BYTES> struct Word;
+template <> struct Word<16> { using type = uint4; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<4> { using type = uint32_t; };
+// V columns as they are stored, `step` apart (1 with VEC, which takes them in one access); without VEC columns that do not exist
+// repeat the first.
+template <typename T, bool VEC, int V> struct Few {
+  using W = typename Word<V * (int)sizeof(T)>::type;
   T v[V];
   __device__ __forceinline__ void load(const T* p, int step, int left) {
+    if constexpr (VEC) {
+      const W w = *reinterpret_cast<const W*>(p);
+      memcpy(v, &w, sizeof(W));
+    } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = p[j * step < left ? j * step : 0];
+      for (int j = 0; j < V; ++j) v[j] = p[j * step < left ? j * step : 0];
+    }
   }
   __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
     for (int j = 0; j < V; ++j) f[j] = to_float(v[j]);
   }
-};
-template <> struct Few<__nv_bfloat16, true> {
-  uint2 v;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p, int, int) { v = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void get(float* f) const {
-    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
-  }
-};
-template <> struct Few<float, true> {
-  float4 v;
-  __device__ __forceinline__ void load(const float* p, int, int) { v = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void get(float* f) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
-};
-template <typename T, bool VEC>
-__device__ __forceinline__ void few_store(T* p, int step, int left, const float* f) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<unsigned*>(&a), *reinterpret_cast<unsigned*>(&b));
-  } else if constexpr (VEC) {
-    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  } else {
+  __device__ __forceinline__ void set(const float* f) {
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j * step < left) p[j * step] = from_float<T>(f[j]);
+    for (int j = 0; j < V; ++j) v[j] = from_float<T>(f[j]);
   }
-}
+  __device__ __forceinline__ void store(T* p, int step, int left) const {
+    if constexpr (VEC) {
+      W w;
+      memcpy(&w, v, sizeof(W));
+      *reinterpret_cast<W*>(p) = w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j * step < left) p[j * step] = v[j];
+    }
+  }
+};
 
 template <typename T>
 struct FewArgs {
@@ -180,80 +182,123 @@ template <typename T, bool VEC, int EM>
 __global__ void __launch_bounds__(FEW_N, EM == 8 ? 2 : 1) k_route_grad_few(const FewArgs<T> a) {
   allow_next_kernel();
   wait_for_previous_kernel();
+  constexpr int V = few_v<EM>;
   constexpr int U = 8;                       // tokens in flight
-  __shared__ float dl[FEW_TOK][EM];
-  __shared__ float sum[FEW_N][V];
+  constexpr int P = 4 / V;                   // sums of dx that run side by side: four chains of FMAs whatever V
+  constexpr int G = EM < 32 ? EM : 32, EPL = EM / G;                    // lanes of a token's dl, experts of a lane
+  constexpr int BY = FEW_N / G, EACH = FEW_TOK / BY;                    // tokens at a time, and of a thread
+  __shared__ __align__(16) float dl[FEW_TOK][EM];
+  __shared__ float sum[FEW_N][V > EPL ? V : EPL];
   const int E = a.s.E, d = a.d, tx = a.tx, ty = FEW_N / tx, cx = threadIdx.x & (tx - 1), cy = threadIdx.x / tx;
   const int step = VEC ? 1 : tx, c = (int)blockIdx.x * tx * V + (VEC ? cx * V : cx), left = d - c;
   const bool cols = left > 0;
   const int range = blockIdx.y;
   const int64_t first = (int64_t)range * a.per, last = min(a.s.N, first + a.per);
-  float w[EM][V], dw[EM][V], bias = 0.f;
+  const int e0 = threadIdx.x & (G - 1), i0 = threadIdx.x / G;
+  float w[EM][V], dw[EM][V], bias[EPL];
+#pragma unroll
+  for (int m = 0; m < EPL; ++m) bias[m] = 0.f;
 #pragma unroll
   for (int e = 0; e < EM; ++e) {
 #pragma unroll
     for (int j = 0; j < V; ++j) w[e][j] = dw[e][j] = 0.f;
     if (e < E && cols) {
-      Few<T, VEC> q;
+      Few<T, VEC, V> q;
       q.load(a.w + (int64_t)e * d + c, step, left);
       q.get(w[e]);
     }
   }
   for (int64_t t0 = first; t0 < last; t0 += FEW_TOK) {
     const int n = (int)min((int64_t)FEW_TOK, last - t0);
-    const int e = threadIdx.x & (EM - 1), i0 = threadIdx.x / EM;
-    constexpr int EACH = FEW_TOK * EM / FEW_N, BY = FEW_N / EM;         // tokens of a thread's expert, tokens between them
-    float s[EACH];
+    float s[EACH][EPL];
     __syncthreads();                         // the last chunk's dl has been read
 #pragma unroll
-    for (int m = 0; m < EACH; ++m) {
-      const int i = i0 + m * BY;
-      const bool mine = i < n && e < E;
-      s[m] = mine ? a.s.scores[(t0 + i) * E + e] : 0.f;
-      dl[i][e] = mine && a.s.dscores ? a.s.dscores[(t0 + i) * a.s.dscores_ld + e] : 0.f;
-    }
+    for (int k = 0; k < EACH; ++k)
+#pragma unroll
+      for (int m = 0; m < EPL; ++m) {
+        const int i = i0 + k * BY, e = e0 + m * G;
+        const bool mine = i < n && e < E;
+        s[k][m] = mine ? a.s.scores[(t0 + i) * E + e] : 0.f;
+        dl[i][e] = mine && a.s.dscores ? a.s.dscores[(t0 + i) * a.s.dscores_ld + e] : 0.f;
+      }
     __syncthreads();
     add_kept(a.s, t0, n, threadIdx.x, FEW_N, &dl[0][0], EM);
     __syncthreads();
 #pragma unroll
-    for (int m = 0; m < EACH; ++m) {
-      const int i = i0 + m * BY;
-      const float g = dl[i][e];
-      float dot = s[m] * g;
+    for (int k = 0; k < EACH; ++k) {
+      const int i = i0 + k * BY;
+      float g[EPL], dot = 0.f;
 #pragma unroll
-      for (int o = EM / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      const float v = i < n && e < E ? s[m] * (g - dot) : 0.f;
-      dl[i][e] = v;
-      bias += v;
-      if (i < n && e < E && blockIdx.x == 0) a.dlogits[(t0 + i) * E + e] = v;
+      for (int m = 0; m < EPL; ++m) {
+        g[m] = dl[i][e0 + m * G];
+        dot = fmaf(s[k][m], g[m], dot);
+      }
+#pragma unroll
+      for (int o = G / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+#pragma unroll
+      for (int m = 0; m < EPL; ++m) {
+        const int e = e0 + m * G;
+        const bool mine = i < n && e < E;
+        const float v = mine ? s[k][m] * (g[m] - dot) : 0.f;
+        dl[i][e] = v;
+        bias[m] += v;
+        if (mine && blockIdx.x == 0) a.dlogits[(t0 + i) * E + e] = v;
+      }
     }
     __syncthreads();
-    if (cols)
-      for (int i1 = cy; i1 < n; i1 += ty * U) {
-        Few<T, VEC> x[U];
+    auto fetch = [&](Few<T, VEC, V>& x, int i) { x.load(a.x + (t0 + min(i, n - 1)) * d + c, step, left); };
+    auto work = [&](int i, const Few<T, VEC, V>& x) {
+      float f[V], y[P][V];
+      x.get(f);
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u].load(a.x + (t0 + min(i1 + u * ty, n - 1)) * d + c, step, left);
+      for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = i1 + u * ty;
-          if (i >= n) break;
-          float f[V], y[V] = {0.f, 0.f, 0.f, 0.f};
-          x[u].get(f);
+        for (int j = 0; j < V; ++j) y[p][j] = 0.f;
 #pragma unroll
-          for (int e4 = 0; e4 < EM; e4 += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(&dl[i][e4]);
-            const float l[4] = {q.x, q.y, q.z, q.w};
+      for (int e4 = 0; e4 < EM; e4 += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(&dl[i][e4]);
+        const float l[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
-              for (int j = 0; j < V; ++j) {
-                y[j] = fmaf(l[m], w[e4 + m][j], y[j]);
-                dw[e4 + m][j] = fmaf(l[m], f[j], dw[e4 + m][j]);
-              }
+          for (int j = 0; j < V; ++j) {
+            y[m % P][j] = fmaf(l[m], w[e4 + m][j], y[m % P][j]);
+            dw[e4 + m][j] = fmaf(l[m], f[j], dw[e4 + m][j]);
           }
-          few_store<T, VEC>(a.dx + (t0 + i) * d + c, step, left, y);
+      }
+#pragma unroll
+      for (int p = 1; p < P; ++p)
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[0][j] += y[p][j];
+      Few<T, VEC, V> out;
+      out.set(y[0]);
+      out.store(a.dx + (t0 + i) * d + c, step, left);
+    };
+    if (cols) {
+      if constexpr (EM <= 16) {
+        for (int i1 = cy; i1 < n; i1 += ty * U) {
+          Few<T, VEC, V> x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) fetch(x[u], i1 + u * ty);
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (i1 + u * ty >= n) break;
+            work(i1 + u * ty, x[u]);
+          }
+        }
+      } else {                               // a token is hundreds of instructions: eight of them side by side would miss the instruction cache
+        Few<T, VEC, V> x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) fetch(x[u], cy + u * ty);
+#pragma unroll 1
+        for (int i = cy; i < n; i += ty) {
+          const Few<T, VEC, V> now = x[0];
+          x[0] = x[1]; x[1] = x[2]; x[2] = x[3];
+          fetch(x[3], i + 4 * ty);
+          work(i, now);
         }
       }
+    }
   }
   // the ty shares of dW_r in their order, then a part
   float* part = a.parts + (int64_t)range * E * d;
@@ -269,15 +314,20 @@ __global__ void __launch_bounds__(FEW_N, EM == 8 ? 2 : 1) k_route_grad_few(const
 #pragma unroll
           for (int j = 0; j < V; ++j) dw[e][j] += sum[cx + k * tx][j];
     }
-    if (cy == 0 && e < E && cols) few_store<float, false>(part + (int64_t)e * d + c, step, left, dw[e]);
+    if (cy == 0 && e < E && cols) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j * step < left) part[(int64_t)e * d + c + j * step] = dw[e][j];
+    }
   }
   if (blockIdx.x == 0) {
     __syncthreads();
-    sum[threadIdx.x][0] = bias;
+#pragma unroll
+    for (int m = 0; m < EPL; ++m) sum[threadIdx.x][m] = bias[m];
     __syncthreads();
     if (threadIdx.x < E) {
       float b = 0.f;
-      for (int k = threadIdx.x; k < FEW_N; k += EM) b += sum[k][0];
+      for (int k = threadIdx.x & (G - 1); k < FEW_N; k += G) b += sum[k][threadIdx.x / G];
       a.dbias_part[(int64_t)range * E + threadIdx.x] = b;
     }
   }
@@ -360,21 +410,22 @@ struct RouteWs {
   int copies, Eq, ranges, blocks;            // general form, tensor cores: blocks of the logits' kernel
   size_t offsets, bias, pair, w2, parts, dw, dw_bytes, total;
 };
-int few_tx(int d) {
+int few_columns(int E) { return E <= 16 ? few_v<16> : few_v<32>; }                               // of a thread
+int few_tx(int d, int E) {
   int tx = 32;
-  while (tx < FEW_N && tx * V < d) tx *= 2;
+  while (tx < FEW_N && tx * few_columns(E) < d) tx *= 2;
   return tx;
 }
 RouteWs route_ws(int64_t N, int d, int E, int dtype) {
   RouteWs w = {};
   const bool bf16 = dtype == CAPMOE_BF16;
-  w.form = route_grad_tc_supported(d, dtype) ? TC : E <= 16 ? FEW : GENERAL;
+  w.form = route_grad_tc_supported(d, dtype) ? TC : E <= FEW_MAX_E ? FEW : GENERAL;
   w.copies = w.form != FEW && bf16 ? 2 : 1;
   w.Eq = w.copies == 2 ? (E + 7) / 8 * 8 : E;                // rows of `pair` in whole 16-byte vectors
   const int64_t sms = sm_count();
   if (w.form == FEW) {
     // two blocks per SM; 32 tokens each at least, or a part of dW_r would be as long as its tokens
-    const int64_t across = ceil_div(d, few_tx(d) * V), want = 2 * sms / across, most = ceil_div(N, 32);
+    const int64_t across = ceil_div(d, few_tx(d, E) * few_columns(E)), want = 2 * sms / across, most = ceil_div(N, 32);
     int64_t r = want < most ? want : most;
     if (r < 1) r = 1;
     if (r > 65535) r = 65535;
@@ -382,8 +433,9 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
   } else if (w.form == TC) {
     w.ranges = route_grad_tc_ranges(N, d, E);
   } else {
-    // enough for the tiles of 256 x 256 to fill the pairs of SMs, 512 tokens each at least
-    const int64_t want = sms / 2 / (ceil_div(d, 256) * ceil_div(w.copies * w.Eq, 256)), most = N / 512;
+    // plain FMAs: tiles of 32 x 64 for four blocks per SM, 128 tokens each at least (fp32, 64 experts: 4096 tokens of 1024 columns
+    // 55.7 us, 58.0 with twice the ranges; 21,900 tokens of 96 columns 43, 50 with 512 tokens each at least)
+    const int64_t want = sms * 4 / (ceil_div(d, 64) * ceil_div(w.copies * w.Eq, 32)), most = N / 128;
     const int64_t r = want < most ? want : most;
     w.ranges = (int)(r < 1 ? 1 : r > 64 ? 64 : r);
   }
@@ -404,10 +456,12 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
 
 template <typename T>
 int few_run(const ScoreGrad& s, const void* x, const void* w, int d, const RouteWs& ws, uint8_t* b, float* dlogits, void* dx, cudaStream_t st) {
-  const FewArgs<T> a{s, (const T*)x, (const T*)w, d, few_tx(d), (int)ceil_div(s.N, ws.ranges), (T*)dx, dlogits, (float*)(b + ws.parts), (float*)(b + ws.bias)};
+  const FewArgs<T> a{s, (const T*)x, (const T*)w, d, few_tx(d, s.E), (int)ceil_div(s.N, ws.ranges), (T*)dx, dlogits, (float*)(b + ws.parts), (float*)(b + ws.bias)};
+  const int V = few_columns(s.E);
   const bool vec = d % V == 0;
-  auto k = s.E <= 8 ? (vec ? k_route_grad_few<T, true, 8> : k_route_grad_few<T, false, 8>)
-                    : (vec ? k_route_grad_few<T, true, 16> : k_route_grad_few<T, false, 16>);
+  auto k = s.E <= 8    ? (vec ? k_route_grad_few<T, true, 8> : k_route_grad_few<T, false, 8>)
+           : s.E <= 16 ? (vec ? k_route_grad_few<T, true, 16> : k_route_grad_few<T, false, 16>)
+                       : (vec ? k_route_grad_few<T, true, 32> : k_route_grad_few<T, false, 32>);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ceil_div(d, a.tx * V), (unsigned)ws.ranges);
   cfg.blockDim = dim3(FEW_N);
