@@ -367,8 +367,8 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  * the allocated row count of the row matrices.  Entries of slot_row that are negative or not below A_max count as no row; every
  * other row belongs to one slot.  Rows that no slot names are neither read nor written.
  *   capmoe_permute_fp8       capmoe_permute of codes and scales (capmoe_quantize_rows, capmoe_rms_norm): x_q [N,d], x_scale
- *                            [N, ceil(d/128)] -> q_perm [A_max,d], scale_perm [A_max, ceil(d/128)], perm_token, perm_weight.
- *                            d a multiple of 16.
+ *                            [N, ceil(d/128)] -> q_perm [A_max,d], scale_perm [A_max, ceil(d/128)], perm_token, perm_weight
+ *                            [A_max].  d a multiple of 16.
  *   capmoe_combine_backward  gradients of capmoe_combine from dy [N,d]: dy_perm[r] = perm_weight[r] dy[t] (rounded to `dtype`),
  *                            dweight[r] = sum_c dy[t,c] y_perm[r,c] (fp32) for the row r of a slot of token t.  (That of
  *                            y_shared is dy.)
@@ -385,8 +385,9 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  *                            N = 0 leaves zeros in dw and dbias.  All sums have a fixed order for given sizes and device.
  *                            ws: capmoe_route_backward_workspace_bytes(N,d,E,dtype) bytes on the device that is current.
  * The first three: rows of whole 16-byte vectors, slots <= 288, N and A_max < 2^31.  route_backward: E <= 256, k <= 32,
- * N <= 2^31 - 512, any d; d a multiple of 8 runs on tensor cores in bf16.  dev_status as in capmoe_grouped_ffn.  Outputs and
- * workspace overlap neither each other nor an input, but for dx of capmoe_permute_backward. */
+ * N <= 2^31 - 512, any d; d a multiple of 8 runs on tensor cores in bf16.  dev_status: NULL, or as in capmoe_grouped_ffn (word 0
+ * says whether a bounded wait ran out).  Outputs and workspace overlap neither each other nor an input, but for dx of
+ * capmoe_permute_backward. */
 int capmoe_permute_fp8(const void* x_q, const void* x_scale, int64_t N, int d, int E, int k, int slots, int D, int64_t A_max,
                        const float* scores, const int32_t* topk_idx, const int32_t* token_group, const int32_t* slot_row,
                        void* q_perm, void* scale_perm, int32_t* perm_token, float* perm_weight, int32_t* dev_status, void* stream);

@@ -1200,11 +1200,14 @@ class MoELayer:
                "capmoe_layer_forward_host")
         return y_host
 
-    def backward(self, dy, dscores=None, out_dtype=None):
+    def backward(self, dy, dscores=None, out_dtype=None, stream=None):
         """Gradients of the layer's last forward() from dy [N,d], the gradient of y, and dscores ([N,E] or [E]), what the router's
         scores get besides (a balance loss).  The forward's buffers must be as it left them.  -> dict(dx [N,d], dw_router, dbias,
         dw_gate, dw_up, dw_down, dlogits, and for a shared expert dws_gate, dws_up, dws_down); the router's weights' gradient in
         out_dtype (float32) or the activations' dtype."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.backward(dy, dscores, out_dtype)
         t = self.t
         status = t["dev_status"]
         dy_perm, dweight = combine_backward(dy, t["y_perm"], t["slot_row"], t["perm_weight"])

@@ -21,6 +21,11 @@ namespace {
 struct Slot { int64_t i; double f; };            // an argument as an integer or address, and as a number
 constexpr int MAX_ARGS = 32;
 
+enum Kind : uint8_t { ADDRESS, WIDE, INT, REAL };            // pointer, 64-bit integer, int, number
+template <class T>
+constexpr Kind kind_of() {
+  return std::is_pointer_v<T> ? ADDRESS : std::is_floating_point_v<T> ? REAL : sizeof(T) == 8 ? WIDE : INT;
+}
 template <class T>
 T as(const Slot& s) {
   if constexpr (std::is_pointer_v<T>) return reinterpret_cast<T>(s.i);
@@ -31,12 +36,13 @@ template <auto Fn> struct Entry;
 template <class... P, int (*Fn)(P...)>
 struct Entry<Fn> {
   static constexpr int params = sizeof...(P);
+  static constexpr Kind kinds[] = {kind_of<P>()...};
   template <size_t... I>
   static int call(const Slot* s, std::index_sequence<I...>) { return Fn(as<P>(s[I])...); }
   static int run(const Slot* s) { return call(s, std::make_index_sequence<sizeof...(P)>{}); }
 };
-struct Call { int (*run)(const Slot*); int params; };
-template <auto Fn> constexpr Call entry() { return {&Entry<Fn>::run, Entry<Fn>::params}; }
+struct Call { int (*run)(const Slot*); int params; const Kind* kinds; };
+template <auto Fn> constexpr Call entry() { return {&Entry<Fn>::run, Entry<Fn>::params, Entry<Fn>::kinds}; }
 
 const std::unordered_map<std::string_view, Call>& entries() {
   static const std::unordered_map<std::string_view, Call> table = {
@@ -51,9 +57,10 @@ const std::unordered_map<std::string_view, Call>& entries() {
   return table;
 }
 
-// run(name, like, *args): the entry point's status, the current stream as its last argument; None where an argument is not what
-// the caller may pass (a tensor that is not on like's device or not contiguous, like's device not the current one), which the
-// caller turns into its message.
+// run(name, like, *args): the entry point's status, the current stream as its last argument, CAPMOE_EUNSUPPORTED for a size that
+// does not fit the int it is passed as; None where a tensor may not be passed (it is not on like's device or not contiguous, or
+// like's device is not the current one), which the caller turns into its message.  Other types than the entry point's are a
+// TypeError.
 PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n < 2 || !PyUnicode_Check(args[0]) || !THPVariable_Check(args[1])) {
@@ -76,20 +83,29 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
   for (Py_ssize_t i = 2; i < n; ++i, ++k) {
     PyObject* o = args[i];
     Slot& s = slots[k];
-    if (o == Py_None) {
-      s = {0, 0.0};
-    } else if (THPVariable_Check(o)) {
-      const at::Tensor& t = THPVariable_Unpack(o);
-      if (!t.is_cuda() || t.get_device() != here || !t.is_contiguous()) Py_RETURN_NONE;
-      s = {reinterpret_cast<int64_t>(t.data_ptr()), 0.0};
-    } else if (PyLong_Check(o)) {
-      const long long v = PyLong_AsLongLong(o);
-      if (v == -1 && PyErr_Occurred()) return nullptr;
-      s = {(int64_t)v, (double)v};
-    } else {
+    const Kind kind = it->second.kinds[k];
+    if (kind == REAL) {
       const double v = PyFloat_AsDouble(o);
       if (v == -1.0 && PyErr_Occurred()) return nullptr;
       s = {0, v};
+    } else if (o == Py_None && kind == ADDRESS) {
+      s = {0, 0.0};
+    } else if (kind == ADDRESS && THPVariable_Check(o)) {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      if (!t.is_cuda() || t.get_device() != here || !t.is_contiguous()) Py_RETURN_NONE;
+      s = {reinterpret_cast<int64_t>(t.data_ptr()), 0.0};
+    } else {
+      if (!PyLong_Check(o) && (!PyIndex_Check(o) || THPVariable_Check(o))) {
+        PyErr_Format(PyExc_TypeError, "%s: argument %d is a %s", name, k, Py_TYPE(o)->tp_name);
+        return nullptr;
+      }
+      PyObject* index = PyLong_Check(o) ? Py_NewRef(o) : PyNumber_Index(o);      // (a NumPy integer)
+      if (!index) return nullptr;
+      const long long v = PyLong_AsLongLong(index);
+      Py_DECREF(index);
+      if (v == -1 && PyErr_Occurred()) return nullptr;
+      if (kind == INT && v != (int)v) return PyLong_FromLong(CAPMOE_EUNSUPPORTED);
+      s = {(int64_t)v, 0.0};
     }
   }
   if (c10::cuda::current_device() != here) Py_RETURN_NONE;

@@ -107,7 +107,7 @@ k_permute8(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, int
       const int64_t t = t0 + tok;
       const int e = s < k ? topk_idx[t * k + s] : home_group(t, N, D, token_group) * m + (s - k);
       perm_token[r] = (int32_t)t;
-      perm_weight[r] = scores[t * E + e];
+      perm_weight[r] = (unsigned)e < (unsigned)E ? scores[t * E + e] : 0.f;
       copy_bytes(scale_perm + (int64_t)r * nb, scale + t * nb, nb, width);
     }
   }
@@ -373,7 +373,7 @@ extern "C" int capmoe_permute_fp8(const void* x_q, const void* x_scale, int64_t 
   if (D > 0 ? E % D != 0 || slots != k + E / D : slots != k) return CAPMOE_EINVAL;
   const int rc = check_rows(N, d, slots, A_max, 1);
   if (rc != CAPMOE_OK) return rc;
-  if (N == 0) return CAPMOE_OK;
+  if (N == 0 || A_max == 0) return CAPMOE_OK;
   if (!usable(x_q, q_perm) || !x_scale || !scale_perm || !scores || !topk_idx || !slot_row || !perm_token || !perm_weight) return CAPMOE_EINVAL;
   const int nb = (int)ceil_div(d, QBLOCK);
   const uintptr_t all = (uintptr_t)nb | (uintptr_t)x_scale | (uintptr_t)scale_perm;

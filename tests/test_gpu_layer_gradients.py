@@ -123,6 +123,34 @@ def test_permute_fp8(cm, N, E, k, D, d):
     assert bool((got["x_q"][A:].float() == 2).all()) and bool((got["x_scale"][A:].float() == 4).all())
 
 
+def test_permute_fp8_without_rows(cm):
+    """Capacity zero: nobody keeps anything, no buffer is touched."""
+    r = cm.route(None, None, None, 2, logits_in=_normal((40, 8), 1.0, F32, 2))
+    q, sc = cm.quantize_rows(_normal((40, 64), 1.0, BF16, 1))
+    none = torch.full((40, 2), -1, device="cuda", dtype=torch.int32)
+    got = cm.permute_fp8(q, sc, r["scores"], r["topk_idx"], none, 0)
+    assert got["x_q"].shape == (0, 64) and got["perm_token"].shape == (0,)
+
+
+def test_sizes_of_other_types(cm):
+    """NumPy integers are sizes, floats are not; a size past 32 bits is refused, not cut."""
+    import numpy as np
+    N, E = 40, 8
+    r, dr, rows = _routing(cm, N, E, 2, 0, 1)
+    q, sc = cm.quantize_rows(_normal((N, 64), 1.0, BF16, 1))
+    args = (q, sc, r["scores"], r["topk_idx"], dr["slot_row"])
+    want = cm.permute_fp8(*args, rows)
+    A = int(dr["offsets"][-1])
+    assert torch.equal(cm.permute_fp8(*args, np.int64(rows))["x_q"][:A].view(torch.uint8), want["x_q"][:A].view(torch.uint8))
+    run = cm._binding().run
+    y = torch.empty((N, 64), device="cuda")
+    good = [y, None, y[0], N, 64, 0, 1e-6, None, y, None, None, None]
+    assert run("capmoe_rms_norm", y, *good[:3], N, (1 << 32) + 64, *good[5:]) == cm.EUNSUPPORTED
+    for at, bad in ((3, 4.0), (4, "64"), (4, None), (5, y), (6, None)):
+        with pytest.raises(TypeError):
+            run("capmoe_rms_norm", y, *good[:at], bad, *good[at + 1:])
+
+
 @pytest.mark.parametrize("N,E,k,d,F", [(1, 8, 2, 2048, 1408), (128, 60, 4, 2048, 1408), (2000, 8, 2, 256, 512), (300, 8, 2, 264, 136), (3000, 4, 2, 1424, 256)])
 def test_ffn_from_codes_is_the_ffn_from_rows(cm, N, E, k, d, F):
     """Norm with codes, codes sorted by expert, FFN from codes: the bits of norm, permute, FFN that quantises its rows."""
@@ -451,8 +479,13 @@ def test_layer_gradients(cm, mode, kw):
 def test_layer_gradients_are_those_of_the_stages_in_bf16(cm):
     layer, dy = _layer(cm, 900, 256, 128, 64, 6, 8, "expanded_drop", BF16, shared=False)
     t = layer.t
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = layer.backward(dy, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
     g = layer.backward(dy)
     layer.check_device_status()
+    assert all(torch.equal(g[k], other[k]) for k in g)
     dyp, dwt = cm.combine_backward(dy, t["y_perm"], t["slot_row"], t["perm_weight"])
     dxp, dwg, dwu, dwd = cm.grouped_ffn_backward(t["x_perm"], dyp, t["expert_offsets"], t["w_gate"], t["w_up"], t["w_down"])
     r = cm.route_backward(t["x"], t["w_router"], t["scores"], t["topk_idx"], t["slot_row"], dwt, D=8)

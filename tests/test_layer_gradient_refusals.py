@@ -142,3 +142,16 @@ def test_the_binding_refuses_before_the_library(cm):
     refused(cm.EINVAL, cm.route_backward, x, t(8, 64), *lists, t(8), token_group=i(3))
     refused(cm.EINVAL, cm.permute_fp8, x, t(4, 1), *lists, 8)
     refused(cm.EINVAL, cm.grouped_ffn_fp8, (x, x), i(5), (t(4, 8, 64), x), (x, x), (x, x))
+
+
+def test_the_compiled_binding_takes_what_the_entry_points_take(cm):
+    """Types and ranges of its arguments, on calls that end in a check of the library or before it."""
+    run = cm._binding().run
+    x = torch.zeros((4, 64))
+    with pytest.raises(TypeError):
+        run("capmoe_rms_norm")
+    with pytest.raises(TypeError):
+        run("capmoe_nothing", x)
+    with pytest.raises(TypeError):
+        run("capmoe_rms_norm", x, x)                                     # too few
+    assert run("capmoe_rms_norm", x, *([None] * 12)) is None             # not on a GPU: nothing is looked at
