@@ -87,6 +87,8 @@ int gmm8(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg
 int gmm8_swiglu(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                 const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
                 int32_t* sched, bool early, cudaStream_t st);
+// Whether gmm8_swiglu's kernel lets its successor start only after its own wait for what came before: its short form does.
+bool gmm8_swiglu_waits_first(const Segments& sg);
 int gmm8_swiglu_short(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                       const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
                       int32_t* sched, bool early, cudaStream_t st);

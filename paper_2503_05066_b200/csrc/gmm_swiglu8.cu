@@ -349,6 +349,8 @@ int launch(const F8Maps& mp, const F8Args& ar, cudaStream_t st) {
 
 }  // namespace
 
+bool gmm8_swiglu_waits_first(const Segments& sg) { return use_short(sg, SHORT_LIMIT); }
+
 int gmm8_swiglu(const uint8_t* xq, const uint8_t* xs, int64_t xs_ld, const Segments& sg, const uint8_t* wg, const uint8_t* wgs,
                    const uint8_t* wu, const uint8_t* wus, int d, int F, uint8_t* hq, uint8_t* hs, int64_t hs_ld, int32_t* dev_status,
                    int32_t* sched, bool early, cudaStream_t st) {

@@ -340,12 +340,11 @@ int ffn_fp8(const void* x, const void* x_q, const void* x_scale, const int32_t* 
     xq = b + w.xq; xs = b + w.xs; xs_ld = w.xs_ld;
   }
   if (tc) {
-    // without the quantiser the gate/up product is the first kernel that is sure to wait for what came before this call, and it
-    // may let the next one start sooner than that: neither starts early then (gmm.cuh)
-    const bool early = x != nullptr;
-    rc = gmm8_swiglu(xq, xs, xs_ld, sg, wg, wgs, wu, wus, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(counters, 0), early, st);
+    // without the quantiser the gate/up product is the first kernel of the call that is sure to wait for what came before: it cannot
+    // start early, and the down product only where it does not let that start sooner than its own wait (gmm.cuh)
+    rc = gmm8_swiglu(xq, xs, xs_ld, sg, wg, wgs, wu, wus, d, F, b + w.hq, b + w.hs, w.hs_ld, dev_status, counter_at(counters, 0), x != nullptr, st);
     if (rc != CAPMOE_OK) return rc;
-    return gmm8(b + w.hq, b + w.hs, w.hs_ld, sg, wd, wds, F, d, y, dev_status, counter_at(counters, 1), early, st);
+    return gmm8(b + w.hq, b + w.hs, w.hs_ld, sg, wd, wds, F, d, y, dev_status, counter_at(counters, 1), x != nullptr || gmm8_swiglu_waits_first(sg), st);
   }
   float* h = (float*)(b + w.h);
   rc = launch_tiles(k_mm_fp8<float, true>, sg, F, st, xq, xs, wg, wgs, wu, wus, h, sg, d, F);

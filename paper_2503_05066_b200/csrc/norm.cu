@@ -111,7 +111,9 @@ struct NormArgs {
   uint8_t *q, *scale;
 };
 
-// A row stays in the registers of its warps between the two uses, VPT vectors a thread: one pass over HBM.
+// A row stays in the registers of its warps between the two uses, VPT vectors a thread: one pass over HBM, which bounds it
+// (16,384 rows of 2048 bf16 columns with residual and codes: 47.8 us, 0.97 of the copy bandwidth).  Few vectors a thread and many
+// warps mix reads and writes: with eight vectors a thread, a warp to a row, the same took 59.9 us, with one 51.2.
 template <typename T, bool VEC, int VPT>
 __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
   allow_next_kernel();
@@ -202,7 +204,10 @@ __device__ __forceinline__ uint4 get_shared(uint32_t at) {
 }
 
 // A group of wpr warps walks its rows, DEPTH - 1 of them in flight ahead of the one it works on; a thread's columns are the same
-// in all of them: dw is summed in registers, and written once per group for k_sum_parts to join in a fixed order.
+// in all of them: dw is summed in registers, and written once per group for k_sum_parts to join in a fixed order.  Bound by HBM
+// (16,384 rows of 4096 bf16 columns with dh: 83.6 us with the sum of the parts, 0.98 of the copy bandwidth; 108 with each row's loads
+// waited for, 88 with the next row's in registers); narrower rows also by the row's sum, a barrier a row (16,384 of 2048 without
+// dh: 40 us, 0.76).
 template <typename T, bool VEC, int VPT, int DEPTH>
 __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   allow_next_kernel();

@@ -91,8 +91,13 @@ k_permute8(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, int
   wait_for_previous_kernel();
   const int32_t* sr = slot_row + (t0 + lane) * slots;
   bool any = false;
-  if (lane < n)
-    for (int s = 0; s < slots; ++s) any = any || (sr[s] >= 0 && sr[s] < rows);
+  if (lane < n) {
+#pragma unroll 8
+    for (int s = 0; s < slots; ++s) {        // (all look-ups at once: no early end)
+      const int32_t r = sr[s];
+      any |= (r >= 0) & (r < rows);
+    }
+  }
   if (any) {                                 // a token nobody keeps is never read
     mbar_expect_tx(bar, (uint32_t)bytes);
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
