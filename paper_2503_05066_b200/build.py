@@ -35,7 +35,7 @@ def _bind_cmd() -> list:
            sysconfig.get_paths()["include"]]
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
             *[a for p in inc for a in ("-isystem", p)], BIND_SRC, "-o", BIND, "-L", PKG, "-l:libcapmoe.so", "-Wl,-rpath,$ORIGIN",
-            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
 
 
 def _stale(obj: str, src: str) -> bool:

@@ -6,6 +6,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <ATen/Functions.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -132,9 +133,10 @@ PyObject* make(PyObject*, PyObject* const* args, Py_ssize_t n) {
     sizes[i - 2] = PyLong_AsLongLong(args[i]);
     if (sizes[i - 2] == -1 && PyErr_Occurred()) return nullptr;
   }
-  const auto options = at::TensorOptions().device(like.device()).dtype(
-      args[1] == Py_None ? like.scalar_type() : reinterpret_cast<THPDtype*>(args[1])->scalar_type);
-  return THPVariable_Wrap(at::empty(n == 2 ? like.sizes() : at::IntArrayRef(sizes, (size_t)(n - 2)), options));
+  const auto shape = n == 2 ? like.sizes() : at::IntArrayRef(sizes, (size_t)(n - 2));
+  const auto dtype = args[1] == Py_None ? like.scalar_type() : reinterpret_cast<THPDtype*>(args[1])->scalar_type;
+  if (!like.is_cuda()) return THPVariable_Wrap(at::empty(shape, at::TensorOptions().device(like.device()).dtype(dtype)));   // (run refuses it)
+  return THPVariable_Wrap(at::detail::empty_cuda(shape, dtype, like.device(), c10::nullopt));
   END_HANDLE_TH_ERRORS
 }
 
