@@ -382,10 +382,12 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  *                              dx = dlogits W_r [N,d] `dtype`,  dw = dlogits^T x [E,d] out_dtype (`dtype`, or CAPMOE_F32),
  *                              dbias = sum_t dlogits [E] fp32.
  *                            bf16: dlogits enter the products as the sum of two bf16 numbers each (at most 2^-16 of them is lost).
+ *                            fp32: beyond eight experts on tensor cores, every factor as the sum of three bf16 numbers that it is
+ *                            (at most 2^-30 of each term is lost).
  *                            N = 0 leaves zeros in dw and dbias.  All sums have a fixed order for given sizes and device.
  *                            ws: capmoe_route_backward_workspace_bytes(N,d,E,dtype) bytes on the device that is current.
  * The first three: rows of whole 16-byte vectors, slots <= 288, N and A_max < 2^31.  route_backward: E <= 256, k <= 32,
- * N <= 2^31 - 512, any d; d a multiple of 8 runs on tensor cores in bf16.  dev_status: NULL, or as in capmoe_grouped_ffn (word 0
+ * N <= 2^31 - 512, any d (bf16 is fastest with d a multiple of 8).  dev_status: NULL, or as in capmoe_grouped_ffn (word 0
  * says whether a bounded wait ran out).  Outputs and workspace overlap neither each other nor an input, but for dx of
  * capmoe_permute_backward. */
 int capmoe_permute_fp8(const void* x_q, const void* x_scale, int64_t N, int d, int E, int k, int slots, int D, int64_t A_max,

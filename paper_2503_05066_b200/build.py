@@ -13,7 +13,7 @@ LIB = os.path.join(PKG, "libcapmoe.so")
 BIND_SRC, BIND = os.path.join(CSRC, "bind.cpp"), os.path.join(PKG, "_bind.so")
 SOURCES = ["api.cu", "route.cu", "drop.cu", "drop_cluster.cu", "drop_parallel.cu", "variants.cu", "permute_combine.cu", "ffn_simt.cu", "ffn_tc.cu", "ffn_tc_t.cu",
            "grouped_mm.cu", "grouped_fp8.cu", "gmm_rows.cu", "gmm_dw.cu", "gmm_swiglu8.cu",
-           "norm.cu", "token_grad.cu", "route_grad.cu", "route_grad_tc.cu"]
+           "norm.cu", "token_grad.cu", "route_grad.cu", "route_grad_tc.cu", "route_grad_any.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

@@ -24,6 +24,11 @@ __device__ __forceinline__ uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
          ((uint32_t)((2 * BM) >> 4) << 24);
 }
 
+// kind::f16, one CTA: D = fp32, A = B = bf16, M = 128, N = n; transpose bits for MN-major operands
+__device__ __forceinline__ uint32_t one_idesc(int n, bool a_mn, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(BM >> 4) << 24);
+}
 // A wide piece of an output: 32 rows of 128 bytes (64 bf16 or 32 fp32 columns), lane r holding row r as 32 words.  With all
 // 32 rows inside the segment it goes out as one TMA box (128-byte swizzle) from a 4 KB buffer of the warp, else row by
 // row.  `bytes_left`: of the output row from this piece on, a multiple of 16.  Against 64-byte pieces this halves the
@@ -342,6 +347,19 @@ bool make_store_map_u8(CUtensorMap* m, const void* base, uint64_t cols, uint64_t
   cuuint32_t estr[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Part i of n of a matrix [rows, n cols] of bf16: boxes of 64 columns by 128 rows
+inline bool make_part_map(CUtensorMap* m, const void* base, int i, int n, uint64_t cols, uint64_t rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {cols * 2 * (uint64_t)n};
+  cuuint32_t box[2] = {64, 128};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<uint8_t*>((const uint8_t*)base + cols * 2 * (uint64_t)i), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -28,12 +28,18 @@ __device__ __forceinline__ void add_kept(const ScoreGrad& a, int64_t t0, int n, 
   }
 }
 
-// dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05: bf16, d a multiple of 8.
-// pair [N, 2 Eq]: dl as two bf16 numbers, Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the stream
-// wrote `pair` and let its successor start only after its own wait for what came before.
+// dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05.
+// pair [N, n Eq]: dl as n bf16 numbers (route_parts), Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the
+// stream wrote `pair` and let its successor start only after its own wait for what came before.
+inline int route_parts(int dtype) { return dtype == CAPMOE_BF16 ? 2 : 3; }
+//   bf16, d a multiple of 8
 inline bool route_grad_tc_supported(int d, int dtype) { return dtype == CAPMOE_BF16 && d % 8 == 0; }
 int route_grad_tc_ranges(int64_t N, int d, int E);
 int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
                   int32_t* dev_status, cudaStream_t st);
+//   any
+int route_grad_any_ranges(int64_t N, int d);
+int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx, float* parts,
+                   int32_t* dev_status, cudaStream_t st);
 
 }  // namespace capmoe

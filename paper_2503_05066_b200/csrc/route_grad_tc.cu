@@ -8,7 +8,9 @@
 // block.  dW_r^T stays in tensor memory until the range ends and leaves as a part, fp32, that route_grad.cu adds up in order; dx
 // passes through two or three accumulators of 128 columns, so that its epilogue overlaps the MMAs.
 // What bounds it: HBM; x is read and dx written once.  Tensor pipe per 128 tokens x 256 columns, E = 64: about 2600 cycles of the
-// 5500 that the copy bandwidth allows an SM; from E = 128 on the tensor pipe is the longer of the two.
+// 5500 that the copy bandwidth allows an SM; from E = 128 on the tensor pipe is the longer of the two.  16,384 tokens of 2048 columns,
+// E = 64: 28 us, 5.2 TB/s of x, dx and parts (18 us without the stores of dx, the same without the MMAs, with two stages of x, with
+// two CTAs of 128 columns on an SM or with ranges of 16 tokens' multiples).
 #include "gmm_tc.cuh"
 #include "route_grad.cuh"
 
@@ -45,11 +47,6 @@ struct RGArgs {
   int32_t* dev_status;
 };
 
-// kind::f16, one CTA: D = fp32, A = B = bf16, M = 128, N = n; transpose bits for MN-major operands
-__device__ __forceinline__ uint32_t one_idesc(int n, bool a_mn, bool b_mn) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
-         ((uint32_t)(BM >> 4) << 24);
-}
 template <int KB>
 __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_constant__ RGMaps mp, const __grid_constant__ RGArgs ar) {
   using S = RG<KB>;
@@ -73,7 +70,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
   if (tid == 0) {
     for (int s = 0; s < S::NST; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), 1); }
     for (int r = 0; r < S::RING; ++r) { mbar_init(dfull(r), 1); mbar_init(dempty(r), 1); }
-    for (int s = 0; s < S::SLOTS; ++s) { mbar_init(sfull(s), 1); mbar_init(sempty(s), EPI_WARPS * 32); }
+    for (int s = 0; s < S::SLOTS; ++s) { mbar_init(sfull(s), 1); mbar_init(sempty(s), EPI_WARPS); }
     mbar_init(wfull, 1);
     mbar_init(wdone, 1);
     *abort_flag = 0;
@@ -210,7 +207,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
         tmem_ld32(taddr + 32u, g + 32);
         tmem_ld_wait();
         tc_fence_before();
-        mbar_arrive(sempty(sl));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sempty(sl));
         if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
 #pragma unroll
         for (int i = 0; i < 32; ++i) w[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
@@ -265,18 +263,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
   if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
 }
 
-// Half of `pair`: [N, Eq] in rows of 2 Eq, boxes of 64 columns by 128 rows
-bool make_half_map(CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[2] = {cols, rows};
-  cuuint64_t strides[1] = {cols * 4};
-  cuuint32_t box[2] = {64, 128};
-  cuuint32_t estr[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int slices_of(int d, int E) { return (int)ceil_div(d, E <= 64 ? RG<1>::DC : RG<2>::DC); }
 
 template <int KB>
@@ -301,7 +287,7 @@ int route_grad_tc_ranges(int64_t N, int d, int E) {
 int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
                   int32_t* dev_status, cudaStream_t st) {
   RGMaps mp = {};
-  if (!make_half_map(&mp.hi, pair, (uint64_t)Eq, (uint64_t)N) || !make_half_map(&mp.lo, (const uint8_t*)pair + 2 * Eq, (uint64_t)Eq, (uint64_t)N) ||
+  if (!make_part_map(&mp.hi, pair, 0, 2, (uint64_t)Eq, (uint64_t)N) || !make_part_map(&mp.lo, pair, 1, 2, (uint64_t)Eq, (uint64_t)N) ||
       !make_map(&mp.x, x, (uint64_t)d, (uint64_t)N, 0, 64) || !make_map(&mp.w, w, (uint64_t)d, (uint64_t)E, 0, 64) ||
       !(E <= 128 ? make_wide_map(&mp.o, dx, (uint64_t)d, (uint64_t)N, 2) : make_store_map(&mp.o, dx, (uint64_t)d, (uint64_t)N)))
     return note_cuda(cudaErrorInvalidValue);

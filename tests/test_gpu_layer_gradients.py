@@ -232,6 +232,26 @@ def test_route_backward_of_many_tokens(cm, N, E, k, D, d, dtype):
     _check_route(cm, N, E, k, D, d, dtype, "all", None, seed=N)
 
 
+@pytest.mark.parametrize("N,E,k,D,d,dtype", [(5001, 256, 8, 0, 130, F32), (3000, 200, 4, 0, 257, F32), (4100, 65, 3, 0, 1032, F32), (9001, 256, 8, 0, 259, BF16),
+                                             (300, 9, 2, 0, 4099, F32), (300, 3, 1, 0, 4098, BF16), (129, 17, 2, 0, 127, BF16), (65, 129, 2, 0, 1, F32),
+                                             (193, 70, 2, 0, 2, BF16), (257, 33, 2, 0, 63, BF16)])
+def test_route_backward_of_rows_that_warps_lay_out(cm, N, E, k, D, d, dtype):
+    """fp32 in passes of 64 experts; bf16 rows that start between words of four bytes; column slices of one and two columns."""
+    _check_route(cm, N, E, k, D, d, dtype, "each", None, seed=N)
+
+
+def test_route_backward_of_large_and_small_numbers(cm):
+    """Three bf16 numbers hold an fp32 number of any size: tokens near the largest, W_r far below one."""
+    N, E, d = 300, 24, 96
+    r, dr, rows = _routing(cm, N, E, 2, 0, 5, 4.0)
+    x, w = _normal((N, d), 1.0, F32, 6) * 2.0 ** 121, _normal((E, d), 1.0, F32, 7) * 2.0 ** -90
+    dweight = _normal((rows,), 2.0 ** -20, F32, 8)
+    got = cm.route_backward(x, w, r["scores"], r["topk_idx"], dr["slot_row"], dweight)
+    ref = _route_ref(x, w, r["scores"], _expert_of(r, dr, E, 0), dr["slot_row"], dweight, None, F32)
+    close(got["dx"], ref[1][0], rounded(*ref[1], F32))
+    close(got["dw"], ref[2][0], rounded(*ref[2], F32))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_route_backward_without_tokens_and_without_rows(cm, dtype):
     E, d = 8, 64
