@@ -350,7 +350,7 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
     if (r > 65535) r = 65535;
     w.ranges = (int)ceil_div(N, ceil_div(N, r));
   } else {
-    w.ranges = w.form == TC ? route_grad_tc_ranges(N, d, E) : route_grad_any_ranges(N, d);
+    w.ranges = w.form == TC ? route_grad_tc_ranges(N, d, E) : route_grad_any_ranges(N, d, dtype);
   }
   const int64_t want = ceil_div(N, RG_WARPS * RG_TOK), most = sms * RG_BLOCKS;
   w.blocks = w.form == FEW ? w.ranges : (int)(want < most ? want : most);

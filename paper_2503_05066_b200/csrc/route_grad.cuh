@@ -28,6 +28,17 @@ __device__ __forceinline__ void add_kept(const ScoreGrad& a, int64_t t0, int n, 
   }
 }
 
+// Ranges of whole stages of 64 tokens, none of them empty: one wave of CTAs, 128 tokens each at least, or as many waves as keep a range
+// within `most` tokens.  The MMAs cut their sums off where fp32 ends, and a long sum loses with each of them (dW_r of bf16 products, two
+// MMAs per 16 tokens: 1.9 10^-5 after ROUTE_CHAIN tokens, where dl's two numbers alone may leave out 1.5 10^-5).
+constexpr int64_t ROUTE_CHAIN = 8192;
+inline int route_ranges(int64_t N, int64_t slices, int64_t most) {
+  const int64_t units = ceil_div(N, 64), wave = sm_count() / slices > 1 ? sm_count() / slices : 1;
+  int64_t r = wave * ceil_div(N, wave * most);
+  if (r > ceil_div(units, 2)) r = ceil_div(units, 2);
+  return (int)ceil_div(units, ceil_div(units, r));
+}
+
 // dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05.
 // pair [N, n Eq]: dl as n bf16 numbers (route_parts), Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the
 // stream wrote `pair` and let its successor start only after its own wait for what came before.
@@ -38,7 +49,7 @@ int route_grad_tc_ranges(int64_t N, int d, int E);
 int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
                   int32_t* dev_status, cudaStream_t st);
 //   any
-int route_grad_any_ranges(int64_t N, int d);
+int route_grad_any_ranges(int64_t N, int d, int dtype);
 int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx, float* parts,
                    int32_t* dev_status, cudaStream_t st);
 

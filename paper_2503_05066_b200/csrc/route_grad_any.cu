@@ -7,7 +7,9 @@
 // fp32 goes in exactly: the top 16 bits of a number are a bf16 number, so are those of the rest, and what that leaves has 8
 // bits: three numbers whose sum it is.  Of the nine products of two such sums all but the last (2^-30 of the product at most) are
 // added up in fp32, the smallest first (with the six largest, which leave out up to 2^-21, 3 % less time).  Three numbers of W_r, x
-// and dl fill the shared memory with 64 experts; more come in passes of 64, the later ones adding to dx.
+// and dl fill the shared memory with 64 experts; more come in passes of 64, the later ones adding to dx.  The MMAs cut their sums off where
+// fp32 ends: the largest products have an accumulator of dW_r^T to themselves, and both are added up in registers every 256 tokens (the
+// error of dW_r over 4096 tokens a CTA is 3 10^-7 of it like this, 3 10^-5 with one accumulator to the end; the time is the same).
 // fp32, 16,384 tokens of 4096 columns, 64 experts: 179 us (plain FMAs 556), bound by the loading warps (two parts of three go
 // through subtractions) and by shared memory, which the MMAs read at its full rate; bf16, 16,384 of 2047, 32 experts: 56 us, bound by
 // instructions (two loads of two bytes for a word).  Left out: two stages of x ahead in registers (17 % slower, spilled).
@@ -36,12 +38,15 @@ struct RA {
   static constexpr int DL_OFF = W_BYTES, X_OFF = DL_OFF + RING * DL_BYTES, STG_OFF = X_OFF + NST * X_BYTES;
   static constexpr int TAIL = STG_OFF + EPI_WARPS * STG_BYTES;
   static constexpr int SMEM = TAIL + 1024 + 256;
-  static constexpr int DW_COLS = KB * 64;                      // tensor-memory columns of dW_r^T, then SLOTS x 128 for dx
+  static constexpr int SUMS = F32 ? 2 : 1;                     // accumulators of dW_r^T: fp32 two, of the large products and the others
+  static constexpr int GROUP = F32 ? 2 : 1 << 30;              // blocks that a set of them takes, two sets in turn
+  static constexpr int DW_COLS = F32 ? 2 * SUMS * 64 : KB * 64;        // tensor-memory columns of dW_r^T, then SLOTS x 128 for dx
   static constexpr int SLOTS = 2;
   static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
   static_assert(DW_COLS + SLOTS * 128 <= 512, "tensor memory");
 };
-// The products of part i of one factor with part j of the other, the smallest first; w: part of W_r or x, l: part of dl.
+// The products of part i of one factor with part j of the other, the smallest first; w: part of W_r or x, l: part of dl.  (The MMAs cut
+// their sums off where fp32 ends: sums should be large late, and not often.)
 template <typename T> struct Pairs;
 template <> struct Pairs<float> {
   static constexpr int n = 8;
@@ -119,40 +124,33 @@ struct Rows {
   }
 };
 
-// 64 columns of dx, lane r holding row r: `cols` of them of the first `rows` rows go to `out`, whose rows are `ld` apart, with `add`
-// onto what is there.  stg: 32 x 33 words of the warp.
-template <typename T>
-__device__ __forceinline__ void put_sums(const uint32_t* g, uint32_t* stg, T* out, int ld, int rows, int cols, bool add);
-// fp32: rows of 32 columns through shared memory (sectors of eight columns straight from registers: 173 -> 181 us for 16,384 tokens,
-// 64 experts, 4096 columns, six products).
-template <>
-__device__ __forceinline__ void put_sums<float>(const uint32_t* g, uint32_t* stg, float* out, int ld, int rows, int cols, bool add) {
+// Columns of dx, lane r holding row r: `cols` of them of the first `rows` rows go to `out`, whose rows are `ld` apart.  stg: 32 x 33
+// words of the warp.
+// fp32: 32 columns, with `add` onto what is there (sectors of eight columns straight from registers: 173 -> 181 us for 16,384
+// tokens, 64 experts, 4096 columns).
+__device__ __forceinline__ void put_sums(const uint32_t* g, uint32_t* stg, float* out, int ld, int rows, int cols, bool add) {
   const int lane = threadIdx.x & 31;
+  __syncwarp();
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    __syncwarp();
+  for (int i = 0; i < 32; ++i) stg[lane * 33 + i] = g[i];
+  __syncwarp();
+  if (lane < cols) {
+    float* to = out + lane;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) stg[lane * 33 + i] = g[p * 32 + i];
-    __syncwarp();
-    if (p * 32 + lane < cols) {
-      float* to = out + p * 32 + lane;
+    for (int r0 = 0; r0 < 32; r0 += 8, to += 8 * (int64_t)ld) {
+      float v[8];
 #pragma unroll
-      for (int r0 = 0; r0 < 32; r0 += 8, to += 8 * (int64_t)ld) {
-        float v[8];
+      for (int j = 0; j < 8; ++j) v[j] = add && r0 + j < rows ? to[j * (int64_t)ld] : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = add && r0 + j < rows ? to[j * (int64_t)ld] : 0.f;
+      for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(stg[(r0 + j) * 33 + lane]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(stg[(r0 + j) * 33 + lane]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (r0 + j < rows) to[j * (int64_t)ld] = v[j];
-      }
+      for (int j = 0; j < 8; ++j)
+        if (r0 + j < rows) to[j * (int64_t)ld] = v[j];
     }
   }
 }
 // bf16: a row of 64 columns in words that lie on four bytes, the element in front of them and behind them by itself.
-template <>
-__device__ __forceinline__ void put_sums<__nv_bfloat16>(const uint32_t* g, uint32_t* stg, __nv_bfloat16* out, int ld, int rows, int cols, bool) {
+__device__ __forceinline__ void put_sums(const uint32_t* g, uint32_t* stg, __nv_bfloat16* out, int ld, int rows, int cols) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
 #pragma unroll
@@ -202,14 +200,16 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
   auto dempty = [&](int r) { return bar0 + 8u * (uint32_t)(10 + r); };
   auto sfull = [&](int s) { return bar0 + 8u * (uint32_t)(12 + s); };          // dx accumulators
   auto sempty = [&](int s) { return bar0 + 8u * (uint32_t)(14 + s); };
-  const uint32_t wfull = bar0 + 8u * 16u, wdone = bar0 + 8u * 17u;             // W_r has arrived; dW_r is complete
+  const uint32_t wfull = bar0 + 8u * 16u;                                      // W_r has arrived
+  auto gfull = [&](int g) { return bar0 + 8u * (uint32_t)(17 + g); };          // accumulators of dW_r
+  auto gempty = [&](int g) { return bar0 + 8u * (uint32_t)(19 + g); };
 
   if (tid == 0) {
     for (int s = 0; s < S::NST; ++s) { mbar_init(xfull(s), LOAD_WARPS); mbar_init(xempty(s), 1); }
     for (int r = 0; r < S::RING; ++r) { mbar_init(dfull(r), 1); mbar_init(dempty(r), 1); }
     for (int s = 0; s < S::SLOTS; ++s) { mbar_init(sfull(s), 1); mbar_init(sempty(s), EPI_WARPS); }
     mbar_init(wfull, LOAD_WARPS);
-    mbar_init(wdone, 1);
+    for (int g = 0; g < 2; ++g) { mbar_init(gfull(g), 1); mbar_init(gempty(g), EPI_WARPS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -290,6 +290,8 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
       bool ok = mbar_wait(wfull, 0u, abort_flag);
       for (int b = 0; ok && b < blocks; ++b) {
         const int here = min(2, halves - 2 * b);                  // stages of x in this block
+        const int in = b % S::GROUP, set = b / S::GROUP & 1;      // (bf16: one group)
+        if (S::F32 && in == 0 && !mbar_wait(gempty(set), (uint32_t)(b / S::GROUP >> 1 & 1) ^ 1u, abort_flag)) { ok = false; break; }
         for (int kb = 0; ok && kb < kbs; ++kb) {
           const uint32_t dl = tiles + DL + (uint32_t)(r * S::DL_BYTES);
           const int steps = min(4, (ar.n - kb * 64 + 15) >> 4);   // of 16 experts
@@ -318,8 +320,11 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
               const uint64_t a = umma_desc_mn(tiles + X + (uint32_t)(xs * S::X_BYTES + Pairs<T>::w(p) * TILE));
               const uint64_t l = umma_desc_mn(dl + (uint32_t)(Pairs<T>::l(p) * TILE + i * BOX));
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks)
-                umma(tmem_base + (uint32_t)(kb * 64), a + 128 * ks, l + 128 * ks, id_w, (b | i | ks | p) != 0 ? 1u : 0u);
+              for (int ks = 0; ks < 4; ++ks) {
+                const bool large = S::F32 && p == Pairs<T>::n - 1;
+                umma(tmem_base + (uint32_t)(S::F32 ? set * S::SUMS * 64 + (large ? 64 : 0) : kb * 64), a + 128 * ks, l + 128 * ks, id_w,
+                     (in | i | ks | (large ? 0 : p)) != 0 ? 1u : 0u);
+              }
             }
             if (kb == kbs - 1) umma_commit(xempty(xs));
             if (++xs == S::NST) { xs = 0; xph ^= 1u; }
@@ -328,8 +333,8 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
           if (ok) umma_commit(dempty(r));
           if (++r == S::RING) { r = 0; rph ^= 1u; }
         }
+        if (ok && (in == S::GROUP - 1 || b == blocks - 1)) umma_commit(gfull(set));
       }
-      if (ok) umma_commit(wdone);
     }
   } else {
     // ------------------------------------------------------------ epilogue: two warps per quarter of the lanes
@@ -339,6 +344,9 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
     int sl = 0;
     uint32_t slp = 0;
     bool ok = true;
+    float sum[S::F32 ? 32 : 1];
+#pragma unroll
+    for (int i = 0; i < (S::F32 ? 32 : 1); ++i) sum[i] = 0.f;
     if (ar.e0) wait_for_previous_kernel();                        // it made the dx that this one adds to
     for (int b = 0; ok && b < blocks; ++b) {
       const int64_t row = first + (int64_t)b * 128 + quarter * 32;
@@ -347,37 +355,76 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      uint32_t g[64];
       const uint32_t taddr = tmem_base + lanes + (uint32_t)(S::DW_COLS + sl * 128 + half * 64);
-      tmem_ld32(taddr, g);
-      tmem_ld32(taddr + 32u, g + 32);
-      tmem_ld_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(sempty(sl));
-      if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
       const int col0 = c0 + half * 64, cols = min(64, ar.d - col0);
       T* out = ar.dx + row * ar.d + col0;
-      if (cols > 0) put_sums<T>(g, stg, out, ar.d, rows, cols, ar.e0 != 0);
-    }
-    if (ok) {
-      ok = mbar_wait(wdone, 0u, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
-    }
-    if (ok) {                                                     // lane: a column; 16 experts at a time, the halves in turn
-      tc_fence_after();
-      float* part = ar.parts + ((int64_t)range * ar.E + ar.e0) * ar.d;
-      const int col = c0 + quarter * 32 + lane;
+      auto drained = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sempty(sl));
+      };
+      if constexpr (S::F32) {                                     // 32 columns at a time: `sum` holds registers
+        uint32_t g[32];
 #pragma unroll 1
-      for (int e = half * 16; e < ar.n; e += 32) {
-        uint32_t g[16];
-        tmem_ld16(tmem_base + lanes + (uint32_t)e, g);
+        for (int p = 0; p < 2; ++p) {
+          tmem_ld32(taddr + (uint32_t)(p * 32), g);
+          tmem_ld_wait();
+          if (p) drained();
+          put_sums(g, stg, out + p * 32, ar.d, rows, cols - p * 32, ar.e0 != 0);
+        }
+      } else {
+        uint32_t g[64];
+        tmem_ld32(taddr, g);
+        tmem_ld32(taddr + 32u, g + 32);
         tmem_ld_wait();
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (e + i < ar.n && col < ar.d) part[(int64_t)(e + i) * ar.d + col] = __uint_as_float(g[i]);
+        drained();
+        if (cols > 0) put_sums(g, stg, out, ar.d, rows, cols);
       }
-      tc_fence_before();
+      if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
+      if constexpr (S::F32) {
+        const int set = b / S::GROUP & 1;
+        if (b % S::GROUP == S::GROUP - 1 || b == blocks - 1) {    // experts half * 32 on, of this lane's column
+          ok = mbar_wait(gfull(set), (uint32_t)(b / S::GROUP >> 1 & 1), abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t g[32];
+#pragma unroll
+          for (int q = 0; q < S::SUMS; ++q) {
+            tmem_ld32(tmem_base + lanes + (uint32_t)((set * S::SUMS + q) * 64 + half * 32), g);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sum[i] += __uint_as_float(g[i]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(gempty(set));
+        }
+      }
+    }
+    float* part = ar.parts + ((int64_t)range * ar.E + ar.e0) * ar.d;
+    const int col = c0 + quarter * 32 + lane;
+    if constexpr (S::F32) {
+      if (ok && col < ar.d)
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (half * 32 + i < ar.n) part[(int64_t)(half * 32 + i) * ar.d + col] = sum[i];
+    } else if (ok) {
+      ok = mbar_wait(gfull(0), 0u, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) {                                                   // lane: a column; 16 experts at a time, the halves in turn
+        tc_fence_after();
+#pragma unroll 1
+        for (int e = half * 16; e < ar.n; e += 32) {
+          uint32_t g[16];
+          tmem_ld16(tmem_base + lanes + (uint32_t)e, g);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (e + i < ar.n && col < ar.d) part[(int64_t)(e + i) * ar.d + col] = __uint_as_float(g[i]);
+        }
+        tc_fence_before();
+      }
     }
   }
 
@@ -423,13 +470,7 @@ int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E,
 
 }  // namespace
 
-// Ranges of whole stages of 64 tokens, none of them empty: one wave of CTAs, 128 tokens each at least.
-int route_grad_any_ranges(int64_t N, int d) {
-  const int64_t units = ceil_div(N, 64), wave = sm_count() / ceil_div(d, DC), most = ceil_div(units, 2);
-  int64_t r = wave < most ? wave : most;
-  if (r < 1) r = 1;
-  return (int)ceil_div(units, ceil_div(units, r));
-}
+int route_grad_any_ranges(int64_t N, int d, int dtype) { return route_ranges(N, ceil_div(d, DC), dtype == CAPMOE_F32 ? N : ROUTE_CHAIN); }
 
 int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx, float* parts,
                    int32_t* dev_status, cudaStream_t st) {

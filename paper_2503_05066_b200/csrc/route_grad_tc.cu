@@ -276,13 +276,7 @@ int run(const RGMaps& mp, const RGArgs& ar, int ranges, cudaStream_t st) {
 
 }  // namespace
 
-// Ranges of whole stages of 64 tokens, none of them empty: one wave of CTAs, 128 tokens each at least.
-int route_grad_tc_ranges(int64_t N, int d, int E) {
-  const int64_t units = ceil_div(N, 64), wave = sm_count() / slices_of(d, E), most = ceil_div(units, 2);
-  int64_t r = wave < most ? wave : most;
-  if (r < 1) r = 1;
-  return (int)ceil_div(units, ceil_div(units, r));
-}
+int route_grad_tc_ranges(int64_t N, int d, int E) { return route_ranges(N, slices_of(d, E), ROUTE_CHAIN); }
 
 int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
                   int32_t* dev_status, cudaStream_t st) {

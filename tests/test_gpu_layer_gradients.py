@@ -240,6 +240,19 @@ def test_route_backward_of_rows_that_warps_lay_out(cm, N, E, k, D, d, dtype):
     _check_route(cm, N, E, k, D, d, dtype, "each", None, seed=N)
 
 
+def test_long_fp32_sums_of_dw_keep_their_precision(cm):
+    """Sums of 9000 terms of one sign, 2300 of them in one thread block.  Sixteen additions a group of 256 tokens that cut off what
+    fp32 does not hold (2^-23 of the sum, and as much where terms are aligned), then rounded ones: 9 groups, 4 ranges."""
+    N, E, d = 9000, 20, 4096
+    r, dr, rows = _routing(cm, N, E, 2, 0, 5, 4.0)
+    x, w = _normal((N, d), 1.0, F32, 6).abs() + 0.1, _normal((E, d), 0.1, F32, 7)
+    dscores = torch.zeros((E,), device="cuda")
+    dscores[3] = 1.0                                                  # one expert's dlogits are positive, the others' negative
+    got = cm.route_backward(x, w, r["scores"], r["topk_idx"], dr["slot_row"], torch.zeros((rows,), device="cuda"), dscores=dscores)
+    want = got["dlogits"].double().T @ x.double()
+    close(got["dw"], want, (2 * 16 + 9 + 4 + 1) * U2 * want.abs())
+
+
 def test_route_backward_of_large_and_small_numbers(cm):
     """Three bf16 numbers hold an fp32 number of any size: tokens near the largest, W_r far below one."""
     N, E, d = 300, 24, 96
