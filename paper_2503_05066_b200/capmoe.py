@@ -739,6 +739,12 @@ def _want(where: str, name: str, t, shape, dtype):
     return t
 
 
+def _no_fit(where: str, x):
+    """The last refusal of arguments that do not fit together: the rows' type, or else the sizes."""
+    _dt(x.dtype)
+    _refuse(where, "types or sizes of the arguments do not fit together")
+
+
 def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None, stream=None):
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * w by rows.  x, residual [N,d], w [d] -> dict(y, h, rstd [N] float32), h
     being x itself without a residual; with fp8 also q, scale: the codes that quantize_rows makes of y.  `out` may hand in any
@@ -747,15 +753,17 @@ def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None
     if stream is not None:
         with torch.cuda.stream(stream):
             return rms_norm(x, w, residual, eps, fp8, out)
-    shape, dtype = x.shape, x.dtype
-    if len(shape) != 2 or w.dim() != 1 or w.shape[0] != shape[1] or w.dtype != dtype:
-        _refuse(where, "x [N,d] and w [d] of one dtype expected")
-    N, d = shape
-    if residual is not None and (residual.shape != shape or residual.dtype != dtype):
-        _want(where, "residual", residual, shape, dtype)
+    bind = _bind or _binding()
+    fit = bind.match("T[N,d] T[d] T?[N,d]", x, w, residual)
+    if fit is None:
+        if x.dim() != 2 or w.dim() != 1 or w.shape[0] != x.shape[1] or w.dtype != x.dtype:
+            _refuse(where, "x [N,d] and w [d] of one dtype expected")
+        _want(where, "residual", residual, x.shape, x.dtype)
+        _no_fit(where, x)
+    code, N, d = fit
     r = dict(h=x)
     if out is None:                           # (allocations are most of the call's time: the cheapest form of each)
-        new = (_bind or _binding()).new
+        new = bind.new
         r["y"] = y = new(x, None)
         r["rstd"] = rstd = new(x, torch.float32, N)
         if residual is not None:
@@ -763,19 +771,21 @@ def rms_norm(x, w, residual=None, eps: float = 1e-6, fp8: bool = False, out=None
         if fp8:
             r["q"], r["scale"] = new(x, FP8), new(x, SCALE, N, _blocks(d))
     else:
+        shape, dtype = x.shape, x.dtype
         r["y"] = y = _out(where, out.get("y"), shape, dtype, x)
         r["rstd"] = rstd = _out(where, out.get("rstd"), (N,), torch.float32, x)
         if residual is not None:
             r["h"] = _out(where, out.get("h"), shape, dtype, x)
         if fp8:
             r["q"], r["scale"] = _out(where, out.get("q"), shape, FP8, x), _out(where, out.get("scale"), (N, _blocks(d)), SCALE, x)
-    _run(where, x, x, residual, w, N, d, _dt(dtype), eps, None if residual is None else r["h"], y, rstd, r.get("q"), r.get("scale"))
+    _run(where, x, x, residual, w, N, d, code, eps, None if residual is None else r["h"], y, rstd, r.get("q"), r.get("scale"))
     return r
 
 
 @functools.lru_cache(maxsize=1024)
-def _norm_backward_bytes(device, N, d, dtype):
-    return _bytes("capmoe_rms_norm_backward_workspace_bytes", _i64(N), d, _dt(dtype))
+def _norm_backward_bytes(device, N, d, code):
+    _fits("capmoe_rms_norm_backward", d)
+    return _bytes("capmoe_rms_norm_backward_workspace_bytes", _i64(N), d, code)
 
 
 def rms_norm_backward_workspace_bytes(N: int, d: int, dtype) -> int:
@@ -789,26 +799,27 @@ def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, out_dtype=None,
     if stream is not None:
         with torch.cuda.stream(stream):
             return rms_norm_backward(dy, h, w, rstd, dh, dx, dw, out_dtype, ws)
-    shape, dtype = h.shape, h.dtype
-    if len(shape) != 2 or w.dim() != 1 or w.shape[0] != shape[1] or w.dtype != dtype:
-        _refuse(where, "h [N,d] and w [d] of one dtype expected")
-    N, d = shape
-    _want(where, "dy", dy, shape, dtype)
-    _want(where, "dh", dh, shape, dtype)
-    _want(where, "rstd", rstd, (N,), torch.float32)
-    new = (_bind or _binding()).new
-    dx = new(h, None) if dx is None else _out(where, dx, shape, dtype, h)
+    bind = _bind or _binding()
+    fit = bind.match("T[N,d] T[d] T[N,d] f[N] T?[N,d]", h, w, dy, rstd, dh)
+    if fit is None:
+        if h.dim() != 2 or w.dim() != 1 or w.shape[0] != h.shape[1] or w.dtype != h.dtype:
+            _refuse(where, "h [N,d] and w [d] of one dtype expected")
+        _want(where, "dy", dy, h.shape, h.dtype)
+        _want(where, "dh", dh, h.shape, h.dtype)
+        _want(where, "rstd", rstd, h.shape[:1], torch.float32)
+        _no_fit(where, h)
+    code, N, d = fit
+    dx = bind.new(h, None) if dx is None else _out(where, dx, h.shape, h.dtype, h)
     if dw is None:
-        dw = new(h, out_dtype, d)
+        dw = bind.new(w, out_dtype)
     else:
         _out(where, dw, (d,), out_dtype or dw.dtype, h)
-    code = _dt(dtype)
     if ws is None:
-        size = _norm_backward_bytes(h.get_device(), N, d, dtype)
-        ws = new(h, torch.uint8, size)
+        size = _norm_backward_bytes(h.get_device(), N, d, code)
+        ws = bind.new(h, torch.uint8, size)
     else:
         size = ws.numel() * ws.element_size()
-    _run(where, h, dy, h, w, rstd, dh, N, d, code, _dt(dw), dx, dw, ws, size)
+    _run(where, h, dy, h, w, rstd, dh, N, d, code, _dt(dw) if out_dtype or dw.dtype != h.dtype else code, dx, dw, ws, size)
     return dx, dw
 
 
@@ -816,18 +827,18 @@ def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, out_dtype=None,
 def _slot_rows(where: str, slot_row, N: int):
     if slot_row.dtype != torch.int32 or slot_row.dim() != 2 or slot_row.shape[0] != N:
         _refuse(where, "slot_row must be int32 [N,slots]")
-    return slot_row.shape[1]
 
 
-def _route_lists(where: str, scores, topk_idx, slot_row, D: int, token_group):
-    """-> (N, E, k, slots) after the checks of what the route and drop stages left."""
+def _route_lists(where: str, scores, topk_idx, slot_row, token_group):
+    """Refuses what the route and drop stages do not leave; -> N."""
     if scores.dim() != 2 or scores.dtype != torch.float32 or topk_idx.dim() != 2 or topk_idx.dtype != torch.int32:
         _refuse(where, "scores [N,E] float32 and topk_idx [N,k] int32 expected")
-    N, E = scores.shape
+    N = scores.shape[0]
     if topk_idx.shape[0] != N:
         _refuse(where, "scores and topk_idx of one number of tokens expected")
     _want(where, "token_group", token_group, (N,), torch.int32)
-    return N, E, topk_idx.shape[1], _slot_rows(where, slot_row, N)
+    _slot_rows(where, slot_row, N)
+    return N
 
 
 def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0, token_group=None, out=None, dev_status=None, stream=None):
@@ -837,16 +848,17 @@ def permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max: int, D: int = 0
     if stream is not None:
         with torch.cuda.stream(stream):
             return permute_fp8(x_q, x_scale, scores, topk_idx, slot_row, A_max, D, token_group, out, dev_status)
-    N, E, k, slots = _route_lists(where, scores, topk_idx, slot_row, D, token_group)
-    if x_q.dim() != 2 or x_q.shape[0] != N:
-        _refuse(where, "x_q [N,d] expected")
-    d = x_q.shape[1]
-    _fits(where, d, D)
+    bind = _bind or _binding()
+    fit = bind.match("q[N,d] s[N,B] f[N,E] i[N,k] i[N,s] i?[N]", x_q, x_scale, scores, topk_idx, slot_row, token_group)
+    if fit is None:
+        N = _route_lists(where, scores, topk_idx, slot_row, token_group)
+        if x_q.dim() != 2 or x_q.shape[0] != N:
+            _refuse(where, "x_q [N,d] expected")
+        _refuse(where, f"float8_e4m3fn [N,d] with float8_e8m0fnu scales {(N, _blocks(x_q.shape[1]))} expected")
+    _, N, d, E, k, slots = fit
     nb = _blocks(d)
-    if x_q.dtype != FP8 or x_scale.dtype != SCALE or x_scale.shape != (N, nb):
-        _refuse(where, f"float8_e4m3fn [N,d] with float8_e8m0fnu scales {(N, nb)} expected")
     if out is None:
-        new = (_bind or _binding()).new
+        new = bind.new
         r = dict(x_q=new(x_q, FP8, A_max, d), x_scale=new(x_q, SCALE, A_max, nb), perm_token=new(x_q, torch.int32, A_max),
                  perm_weight=new(x_q, torch.float32, A_max))
     else:
@@ -866,16 +878,18 @@ def combine_backward(dy, y_perm, slot_row, perm_weight, dy_perm=None, dweight=No
     if stream is not None:
         with torch.cuda.stream(stream):
             return combine_backward(dy, y_perm, slot_row, perm_weight, dy_perm, dweight)
-    if dy.dim() != 2 or y_perm.dim() != 2 or y_perm.shape[1] != dy.shape[1] or y_perm.dtype != dy.dtype:
-        _refuse(where, "dy [N,d] and y_perm [A_max,d] of one dtype expected")
-    N, d = dy.shape
-    A_max = y_perm.shape[0]
-    _fits(where, d)
-    slots = _slot_rows(where, slot_row, N)
-    _want(where, "perm_weight", perm_weight, (A_max,), torch.float32)
-    dy_perm = _out(where, dy_perm, (A_max, d), dy.dtype, dy)
-    dweight = _out(where, dweight, (A_max,), torch.float32, dy)
-    _run(where, dy, dy, y_perm, slot_row, perm_weight, N, d, slots, _dt(dy), A_max, dy_perm, dweight)
+    bind = _bind or _binding()
+    fit = bind.match("T[N,d] T[A,d] i[N,s] f[A]", dy, y_perm, slot_row, perm_weight)
+    if fit is None:
+        if dy.dim() != 2 or y_perm.dim() != 2 or y_perm.shape[1] != dy.shape[1] or y_perm.dtype != dy.dtype:
+            _refuse(where, "dy [N,d] and y_perm [A_max,d] of one dtype expected")
+        _slot_rows(where, slot_row, dy.shape[0])
+        _want(where, "perm_weight", perm_weight, y_perm.shape[:1], torch.float32)
+        _no_fit(where, dy)
+    code, N, d, A_max, slots = fit
+    dy_perm = bind.new(y_perm, None) if dy_perm is None else _out(where, dy_perm, y_perm.shape, dy.dtype, dy)
+    dweight = bind.new(perm_weight, None) if dweight is None else _out(where, dweight, (A_max,), torch.float32, dy)
+    _run(where, dy, dy, y_perm, slot_row, perm_weight, N, d, slots, code, A_max, dy_perm, dweight)
     return dy_perm, dweight
 
 
@@ -886,25 +900,32 @@ def permute_backward(dx_perm, slot_row, add=None, dx=None, stream=None):
     if stream is not None:
         with torch.cuda.stream(stream):
             return permute_backward(dx_perm, slot_row, add, dx)
-    if dx_perm.dim() != 2:
-        _refuse(where, "dx_perm [A_max,d] expected")
-    A_max, d = dx_perm.shape
-    N = slot_row.shape[0]
-    _fits(where, d)
-    slots = _slot_rows(where, slot_row, N)
-    add = () if add is None else (add,) if isinstance(add, torch.Tensor) else tuple(add)
-    if len(add) > 2:
-        _refuse(where, "at most two tensors to add", EUNSUPPORTED)
-    for t in add:
-        _want(where, "add", t, (N, d), dx_perm.dtype)
-    dx = (_bind or _binding()).new(dx_perm, None, N, d) if dx is None else _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
-    _run(where, dx_perm, dx_perm, slot_row, N, d, slots, _dt(dx_perm), A_max, *(add + (None, None))[:2], dx)
+    bind = _bind or _binding()
+    add0 = add1 = None
+    if add is not None:
+        add = (add,) if isinstance(add, torch.Tensor) else tuple(add)
+        if len(add) > 2:
+            _refuse(where, "at most two tensors to add", EUNSUPPORTED)
+        add0, add1 = (add + (None, None))[:2]
+    fit = bind.match("T[A,d] i[N,s] T?[N,d] T?[N,d]", dx_perm, slot_row, add0, add1)
+    if fit is None:
+        if dx_perm.dim() != 2:
+            _refuse(where, "dx_perm [A_max,d] expected")
+        N = slot_row.shape[0] if slot_row.dim() else 0
+        _slot_rows(where, slot_row, N)
+        for t in (add0, add1):
+            _want(where, "add", t, (N, dx_perm.shape[1]), dx_perm.dtype)
+        _no_fit(where, dx_perm)
+    code, A_max, d, N, slots = fit
+    dx = bind.new(dx_perm, None, N, d) if dx is None else _out(where, dx, (N, d), dx_perm.dtype, dx_perm)
+    _run(where, dx_perm, dx_perm, slot_row, N, d, slots, code, A_max, add0, add1, dx)
     return dx
 
 
 @functools.lru_cache(maxsize=1024)
-def _route_backward_bytes(device, N, d, E, dtype):
-    return route_backward_workspace_bytes(N, d, E, dtype)
+def _route_backward_bytes(device, N, d, E, code):
+    _fits("capmoe_route_backward", d, E)
+    return _bytes("capmoe_route_backward_workspace_bytes", _i64(N), d, E, code)
 
 
 def route_backward_workspace_bytes(N: int, d: int, E: int, dtype) -> int:
@@ -920,34 +941,36 @@ def route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D: int = 0,
     if stream is not None:
         with torch.cuda.stream(stream):
             return route_backward(x, w_router, scores, topk_idx, slot_row, dweight, D, token_group, dscores, out, out_dtype, ws, dev_status)
-    N, E, k, slots = _route_lists(where, scores, topk_idx, slot_row, D, token_group)
-    if x.dim() != 2 or x.shape[0] != N or w_router.shape != (E, x.shape[1]) or w_router.dtype != x.dtype:
-        _refuse(where, "x [N,d] and w_router [E,d] of one dtype expected")
-    d = x.shape[1]
-    _fits(where, d, D)
-    if dweight.dtype != torch.float32 or dweight.dim() != 1:
-        _refuse(where, "dweight must be float32 [A_max]")
+    bind = _bind or _binding()
+    fit = bind.match("T[N,d] T[E,d] f[N,E] i[N,k] i[N,s] f[A] i?[N]", x, w_router, scores, topk_idx, slot_row, dweight, token_group)
+    if fit is None:
+        N = _route_lists(where, scores, topk_idx, slot_row, token_group)
+        if x.dim() != 2 or x.shape[0] != N or w_router.shape != (scores.shape[1], x.shape[1]) or w_router.dtype != x.dtype:
+            _refuse(where, "x [N,d] and w_router [E,d] of one dtype expected")
+        if dweight.dtype != torch.float32 or dweight.dim() != 1:
+            _refuse(where, "dweight must be float32 [A_max]")
+        _no_fit(where, x)
+    code, N, d, E, k, slots, A_max = fit
     ld = 0
-    if dscores is not None and dscores.dim() == 2:
-        ld = E
-    _want(where, "dscores", dscores, (N, E) if ld else (E,), torch.float32)
-    dtype = x.dtype
-    code = _dt(dtype)
-    new = (_bind or _binding()).new
+    if dscores is not None:
+        if dscores.dim() == 2:
+            ld = E
+        _want(where, "dscores", dscores, (N, E) if ld else (E,), torch.float32)
+    new = bind.new
     if out is None:
         r = dict(dlogits=new(scores, None), dx=new(x, None), dw=new(w_router, out_dtype), dbias=new(x, torch.float32, E))
     else:
-        dw = out.get("dw")
+        dw, dtype = out.get("dw"), x.dtype
         r = dict(dlogits=_out(where, out.get("dlogits"), (N, E), torch.float32, x), dx=_out(where, out.get("dx"), (N, d), dtype, x),
                  dw=_out(where, dw, (E, d), out_dtype or (dw.dtype if dw is not None else dtype), x),
                  dbias=_out(where, out.get("dbias"), (E,), torch.float32, x))
     if ws is None:
-        size = _route_backward_bytes(x.get_device(), N, d, E, dtype)
+        size = _route_backward_bytes(x.get_device(), N, d, E, code)
         ws = new(x, torch.uint8, size)
     else:
         size = ws.numel() * ws.element_size()
-    _run(where, x, x, w_router, scores, topk_idx, slot_row, dweight, N, d, E, k, slots, D, token_group, dscores, ld, code, _dt(r["dw"]),
-         dweight.shape[0], r["dlogits"], r["dx"], r["dw"], r["dbias"], ws, size, _status(where, dev_status))
+    _run(where, x, x, w_router, scores, topk_idx, slot_row, dweight, N, d, E, k, slots, D, token_group, dscores, ld, code, code if out_dtype is None and out is None else _dt(r["dw"]),
+         A_max, r["dlogits"], r["dx"], r["dw"], r["dbias"], ws, size, _status(where, dev_status))
     return r
 
 

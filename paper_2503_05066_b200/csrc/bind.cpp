@@ -11,9 +11,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <string>
 #include <string_view>
 #include <unordered_map>
 #include <utility>
+#include <vector>
 
 #include "capmoe.h"
 
@@ -140,7 +142,97 @@ PyObject* make(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, "Calls an entry point of libcapmoe.so."},
+// What match() knows of an argument: its type (T: float32 or bfloat16, one type for all T; f float32, i int32, q and s the 8-bit codes
+// and their scales), whether it may be None, and its sizes, letters that mean the same number wherever they stand (B: blocks of 128 of d).
+struct Shape {
+  char type;
+  bool optional;
+  int dims;
+  char size[4];
+};
+struct Pattern {
+  std::vector<Shape> args;
+  std::string letters;                           // in the order of their first place
+};
+// "T[N,d] T?[d]": a shape per argument
+Pattern parse(const char* p) {
+  Pattern out;
+  while (*p) {
+    Shape a = {*p++, false, 0, {}};
+    if (*p == '?') { a.optional = true; ++p; }
+    for (++p; *p && *p != ']'; ++p)
+      if (*p != ',' && a.dims < 4) {
+        a.size[a.dims++] = *p;
+        if (*p != 'B' && out.letters.find(*p) == std::string::npos) out.letters += *p;
+      }
+    if (*p) ++p;
+    if (*p) ++p;
+    out.args.push_back(a);
+  }
+  return out;
+}
+bool is_type(char type, at::ScalarType t, at::ScalarType& bound) {
+  switch (type) {
+    case 'f': return t == at::kFloat;
+    case 'i': return t == at::kInt;
+    case 'q': return t == at::kFloat8_e4m3fn;
+    case 's': return t == at::kFloat8_e8m0fnu;
+    default:
+      if (bound == at::ScalarType::Undefined && (t == at::kFloat || t == at::kBFloat16)) bound = t;
+      return t == bound;
+  }
+}
+
+// match(pattern, *tensors): (dtype code of the T's, or -1, and the letters' numbers), None where an argument does not fit; the caller
+// then finds out why.  One call for what takes 2 to 4 us of attribute look-ups.
+PyObject* match(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  static std::unordered_map<std::string, Pattern> known;
+  Py_ssize_t length = 0;
+  const char* text = n > 0 && PyUnicode_Check(args[0]) ? PyUnicode_AsUTF8AndSize(args[0], &length) : nullptr;
+  if (!text) {
+    PyErr_SetString(PyExc_TypeError, "match(pattern, *tensors)");
+    return nullptr;
+  }
+  std::string key(text, (size_t)length);
+  auto it = known.find(key);
+  if (it == known.end()) it = known.emplace(key, parse(text)).first;
+  const Pattern& pattern = it->second;
+  if ((size_t)(n - 1) != pattern.args.size()) {
+    PyErr_Format(PyExc_TypeError, "match: %zd tensors expected", (Py_ssize_t)pattern.args.size());
+    return nullptr;
+  }
+  int64_t size[128];
+  for (char c : pattern.letters) size[(int)c] = -1;
+  at::ScalarType bound = at::ScalarType::Undefined;
+  for (Py_ssize_t i = 1; i < n; ++i) {
+    const Shape& a = pattern.args[(size_t)i - 1];
+    if (args[i] == Py_None && a.optional) continue;
+    if (!THPVariable_Check(args[i])) Py_RETURN_NONE;
+    const at::Tensor& t = THPVariable_Unpack(args[i]);
+    if (t.dim() != a.dims || !is_type(a.type, t.scalar_type(), bound)) Py_RETURN_NONE;
+    for (int j = 0; j < a.dims; ++j) {
+      const int64_t have = t.size(j);
+      const char c = a.size[j];
+      if (c == 'B') {
+        if (have != (size['d'] + 127) / 128) Py_RETURN_NONE;
+      } else {
+        int64_t& want = size[(int)c];
+        if (want < 0) want = have;
+        if (want != have) Py_RETURN_NONE;
+      }
+    }
+  }
+  PyObject* out = PyTuple_New(1 + (Py_ssize_t)pattern.letters.size());
+  if (!out) return nullptr;
+  PyTuple_SET_ITEM(out, 0, PyLong_FromLong(bound == at::kFloat ? CAPMOE_F32 : bound == at::kBFloat16 ? CAPMOE_BF16 : -1));
+  for (size_t i = 0; i < pattern.letters.size(); ++i) PyTuple_SET_ITEM(out, (Py_ssize_t)i + 1, PyLong_FromLongLong(size[(int)pattern.letters[i]]));
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"match", (PyCFunction)(void (*)(void))match, METH_FASTCALL, "Types and sizes of arguments."},
+                         {"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, "Calls an entry point of libcapmoe.so."},
                          {"new", (PyCFunction)(void (*)(void))make, METH_FASTCALL, "An uninitialised tensor."}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
