@@ -20,7 +20,7 @@ constexpr int RG_BLOCKS = 4;                 // blocks per SM at most (walks the
 
 struct LogitArgs {
   ScoreGrad s;
-  float *dlogits, *dbias_part;
+  float *dlogits, *dbias_part;               // dbias_part may be NULL
   __nv_bfloat16* pair;                       // [N, parts Eq]
   int Eq, parts;                             // two: rounded; three: cut off
 };
@@ -92,6 +92,7 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
     }
     __syncwarp();                            // the rows are rewritten for the next tokens
   }
+  if (!a.dbias_part) return;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) ds[warp][0][lane + 32 * i] = bias[i];
   __syncthreads();
@@ -362,10 +363,10 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
   return w;
 }
 
-int few_run(const ScoreGrad& s, const void* x, const void* w, int d, const RouteWs& ws, uint8_t* b, float* dlogits, void* dx, cudaStream_t st) {
-  const FewArgs a{s, (const float*)x, (const float*)w, d, few_tx(d), (int)ceil_div(s.N, ws.ranges), (float*)dx, dlogits, (float*)(b + ws.parts), (float*)(b + ws.bias)};
+int few_run(const ScoreGrad& s, const void* x, const void* w, int d, int ranges, float* dlogits, void* dx, float* parts, float* bias, cudaStream_t st) {
+  const FewArgs a{s, (const float*)x, (const float*)w, d, few_tx(d), (int)ceil_div(s.N, ranges), (float*)dx, dlogits, parts, bias};
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ceil_div(d, a.tx * FEW_V), (unsigned)ws.ranges);
+  cfg.gridDim = dim3((unsigned)ceil_div(d, a.tx * FEW_V), (unsigned)ranges);
   cfg.blockDim = dim3(FEW_N);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -422,23 +423,27 @@ extern "C" int capmoe_route_backward(const void* x, const void* w_router, const 
   if (ws_bytes < w.total) return CAPMOE_EWORKSPACE;
   uint8_t* b = (uint8_t*)up256((size_t)ws);
   const ScoreGrad sg{scores, dweight, dscores, topk_idx, slot_row, token_group, N, A_max, dscores_ld, E, k, slots, D};
-  float *parts = (float*)(b + w.parts), *bias = (float*)(b + w.bias);
+  // nothing to join: a launch less for up to 128 tokens (32 of FEW; dbias is then the sum of one thread an expert: not of many tokens)
+  const bool single = w.ranges == 1 && (w.form == FEW || N <= 256);
+  const bool whole = single && out_dtype == CAPMOE_F32;
+  float *parts = whole ? (float*)dw : (float*)(b + w.parts), *bias = single ? dbias : (float*)(b + w.bias);
   if (w.form == FEW) {
-    rc = few_run(sg, x, w_router, d, w, b, dlogits, dx, st);
+    rc = few_run(sg, x, w_router, d, w.ranges, dlogits, dx, parts, bias, st);
   } else {
     LogitArgs a = {};
     a.s = sg;
-    a.dlogits = dlogits; a.dbias_part = bias;
+    a.dlogits = dlogits; a.dbias_part = single ? nullptr : bias;
     a.pair = (__nv_bfloat16*)(b + w.pair);
     a.Eq = w.Eq; a.parts = route_parts(dtype);
     auto kernel = E <= 32 ? k_route_logit_grad<1> : E <= 64 ? k_route_logit_grad<2> : E <= 128 ? k_route_logit_grad<4> : k_route_logit_grad<8>;
     rc = note_cuda(launch_chained(kernel, (unsigned)w.blocks, RG_WARPS * 32, 0, st, a));
     count_launch(1);
     if (rc != CAPMOE_OK) return rc;
-    rc = w.form == TC ? route_grad_tc(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dx, parts, dev_status, st)
-                      : route_grad_any(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dtype, dx, parts, dev_status, st);
+    const RouteOut out{parts, single && !whole ? (__nv_bfloat16*)dw : nullptr, dlogits, single ? dbias : nullptr};
+    rc = w.form == TC ? route_grad_tc(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dx, out, dev_status, st)
+                      : route_grad_any(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dtype, dx, out, dev_status, st);
   }
-  if (rc != CAPMOE_OK) return rc;
+  if (rc != CAPMOE_OK || single) return rc;
   const int64_t size = (int64_t)E * d;
   return out_dtype == CAPMOE_F32 ? join_run<float>(parts, w.ranges, size, dw, bias, w.blocks, E, dbias, st)
                                  : join_run<__nv_bfloat16>(parts, w.ranges, size, dw, bias, w.blocks, E, dbias, st);

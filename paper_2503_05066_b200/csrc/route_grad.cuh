@@ -42,15 +42,31 @@ inline int route_ranges(int64_t N, int64_t slices, int64_t most) {
 // dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05.
 // pair [N, n Eq]: dl as n bf16 numbers (route_parts), Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the
 // stream wrote `pair` and let its successor start only after its own wait for what came before.
+// With one range dW_r is final: it goes to `parts`, or as bf16 to dw16, and dbias is made too, from dl [N, E].
+struct RouteOut {
+  float* parts;
+  __nv_bfloat16* dw16;                       // else NULL, as the other two
+  const float* dl;
+  float* dbias;
+};
+// Sums of the columns of dl [n, E], threads `me` of `of`.
+__device__ __forceinline__ void sum_bias(const RouteOut& o, int64_t n, int E, int me, int of) {
+  for (int e = me; e < E; e += of) {
+    float s = 0.f;
+#pragma unroll 16
+    for (int64_t t = 0; t < n; ++t) s += o.dl[t * E + e];
+    o.dbias[e] = s;
+  }
+}
 inline int route_parts(int dtype) { return dtype == CAPMOE_BF16 ? 2 : 3; }
 //   bf16, d a multiple of 8
 inline bool route_grad_tc_supported(int d, int dtype) { return dtype == CAPMOE_BF16 && d % 8 == 0; }
 int route_grad_tc_ranges(int64_t N, int d, int E);
-int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
+int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out,
                   int32_t* dev_status, cudaStream_t st);
 //   any
 int route_grad_any_ranges(int64_t N, int d, int dtype);
-int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx, float* parts,
-                   int32_t* dev_status, cudaStream_t st);
+int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx,
+                   const RouteOut& out, int32_t* dev_status, cudaStream_t st);
 
 }  // namespace capmoe

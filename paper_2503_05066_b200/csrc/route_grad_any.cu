@@ -66,7 +66,7 @@ struct RAArgs {
   int64_t N;
   int d, E, e0, n, slices, per;              // experts e0 .. e0 + n - 1 of E; per: tokens of a range, a multiple of 64
   T* dx;                                     // is added to from the second pass on
-  float* parts;
+  RouteOut out;
   int32_t* dev_status;
 };
 
@@ -348,6 +348,10 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
 #pragma unroll
     for (int i = 0; i < (S::F32 ? 32 : 1); ++i) sum[i] = 0.f;
     if (ar.e0) wait_for_previous_kernel();                        // it made the dx that this one adds to
+    if (ar.out.dbias && slice == 0) {
+      wait_for_previous_kernel();
+      sum_bias(ar.out, ar.N, ar.E, tid - 64, EPI_WARPS * 32);
+    }
     for (int b = 0; ok && b < blocks; ++b) {
       const int64_t row = first + (int64_t)b * 128 + quarter * 32;
       const int rows = (int)max((int64_t)0, min((int64_t)32, last - row));
@@ -402,13 +406,13 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
         }
       }
     }
-    float* part = ar.parts + ((int64_t)range * ar.E + ar.e0) * ar.d;
+    const int64_t part = ((int64_t)range * ar.E + ar.e0) * ar.d;
     const int col = c0 + quarter * 32 + lane;
     if constexpr (S::F32) {
       if (ok && col < ar.d)
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (half * 32 + i < ar.n) part[(int64_t)(half * 32 + i) * ar.d + col] = sum[i];
+          if (half * 32 + i < ar.n) ar.out.parts[part + (int64_t)(half * 32 + i) * ar.d + col] = sum[i];
     } else if (ok) {
       ok = mbar_wait(gfull(0), 0u, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
@@ -421,7 +425,11 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (e + i < ar.n && col < ar.d) part[(int64_t)(e + i) * ar.d + col] = __uint_as_float(g[i]);
+            if (e + i < ar.n && col < ar.d) {
+              const int64_t at = part + (int64_t)(e + i) * ar.d + col;
+              if (ar.out.dw16) ar.out.dw16[at] = __float2bfloat16_rn(__uint_as_float(g[i]));
+              else ar.out.parts[at] = __uint_as_float(g[i]);
+            }
         }
         tc_fence_before();
       }
@@ -444,7 +452,7 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
 }
 
 template <typename T>
-int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts, int32_t* dev_status,
+int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out, int32_t* dev_status,
         cudaStream_t st) {
   using S = RA<T>;
   RAMaps mp = {};
@@ -457,13 +465,14 @@ int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E,
   ar.x = (const T*)x; ar.w = (const T*)w; ar.N = N; ar.d = d; ar.E = E;
   ar.slices = (int)ceil_div(d, DC);
   ar.per = (int)(ceil_div(ceil_div(N, 64), ranges) * 64);
-  ar.dx = (T*)dx; ar.parts = parts; ar.dev_status = dev_status;
+  ar.dx = (T*)dx; ar.out = out; ar.dev_status = dev_status;
   for (int e0 = 0; e0 < E; e0 += S::KB * 64) {
     ar.e0 = e0;
     ar.n = E - e0 < S::KB * 64 ? E - e0 : S::KB * 64;
     const int rc = note_cuda(launch_chained(k, (unsigned)(ar.slices * ranges), ANY_THREADS, S::SMEM, st, mp, ar));
     count_launch(1);
     if (rc != CAPMOE_OK) return rc;
+    ar.out.dbias = nullptr;                    // the first pass makes it
   }
   return CAPMOE_OK;
 }
@@ -472,10 +481,10 @@ int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E,
 
 int route_grad_any_ranges(int64_t N, int d, int dtype) { return route_ranges(N, ceil_div(d, DC), dtype == CAPMOE_F32 ? N : ROUTE_CHAIN); }
 
-int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx, float* parts,
-                   int32_t* dev_status, cudaStream_t st) {
-  return dtype == CAPMOE_F32 ? run<float>(pair, x, w, N, d, E, Eq, ranges, dx, parts, dev_status, st)
-                             : run<__nv_bfloat16>(pair, x, w, N, d, E, Eq, ranges, dx, parts, dev_status, st);
+int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx,
+                   const RouteOut& out, int32_t* dev_status, cudaStream_t st) {
+  return dtype == CAPMOE_F32 ? run<float>(pair, x, w, N, d, E, Eq, ranges, dx, out, dev_status, st)
+                             : run<__nv_bfloat16>(pair, x, w, N, d, E, Eq, ranges, dx, out, dev_status, st);
 }
 
 }  // namespace capmoe

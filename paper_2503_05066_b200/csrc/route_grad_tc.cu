@@ -43,7 +43,7 @@ struct RGArgs {
   int64_t N;
   int d, E, slices, per;                     // per: tokens of a range, a multiple of 64
   __nv_bfloat16* dx;
-  float* parts;
+  RouteOut out;
   int32_t* dev_status;
 };
 
@@ -193,6 +193,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
     int sl = 0;
     uint32_t slp = 0;
     bool ok = true;
+    if (ar.out.dbias && slice == 0) {
+      wait_for_previous_kernel();
+      sum_bias(ar.out, ar.N, ar.E, tid - 64, EPI_WARPS * 32);
+    }
     for (int b = 0; ok && b < blocks; ++b) {
       const int64_t row = first + (int64_t)b * 128 + quarter * 32;
       const bool full_rows = row + 32 <= last, row_ok = row + lane < last;
@@ -229,7 +233,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
     }
     if (ok) {                                                     // lane: a column; 16 experts at a time, the halves in turn
       tc_fence_after();
-      float* part = ar.parts + (int64_t)range * ar.E * ar.d;
+      const int64_t part = (int64_t)range * ar.E * ar.d;
 #pragma unroll 1
       for (int c = 0; c < S::CHUNKS; ++c) {
         const int col = c0 + c * 128 + quarter * 32 + lane;
@@ -240,7 +244,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_route_grad(const __grid_const
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (e0 + i < ar.E && col < ar.d) part[(int64_t)(e0 + i) * ar.d + col] = __uint_as_float(g[i]);
+            if (e0 + i < ar.E && col < ar.d) {
+              const int64_t at = part + (int64_t)(e0 + i) * ar.d + col;
+              if (ar.out.dw16) ar.out.dw16[at] = __float2bfloat16_rn(__uint_as_float(g[i]));
+              else ar.out.parts[at] = __uint_as_float(g[i]);
+            }
         }
       }
       tc_fence_before();
@@ -278,7 +286,7 @@ int run(const RGMaps& mp, const RGArgs& ar, int ranges, cudaStream_t st) {
 
 int route_grad_tc_ranges(int64_t N, int d, int E) { return route_ranges(N, slices_of(d, E), ROUTE_CHAIN); }
 
-int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, float* parts,
+int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out,
                   int32_t* dev_status, cudaStream_t st) {
   RGMaps mp = {};
   if (!make_part_map(&mp.hi, pair, 0, 2, (uint64_t)Eq, (uint64_t)N) || !make_part_map(&mp.lo, pair, 1, 2, (uint64_t)Eq, (uint64_t)N) ||
@@ -289,7 +297,7 @@ int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int
   ar.N = N; ar.d = d; ar.E = E;
   ar.slices = slices_of(d, E);
   ar.per = (int)(ceil_div(ceil_div(N, 64), ranges) * 64);
-  ar.dx = (__nv_bfloat16*)dx; ar.parts = parts; ar.dev_status = dev_status;
+  ar.dx = (__nv_bfloat16*)dx; ar.out = out; ar.dev_status = dev_status;
   return E <= 64 ? run<1>(mp, ar, ranges, st) : E <= 128 ? run<2>(mp, ar, ranges, st) : run<4>(mp, ar, ranges, st);
 }
 

@@ -240,6 +240,14 @@ def test_route_backward_of_rows_that_warps_lay_out(cm, N, E, k, D, d, dtype):
     _check_route(cm, N, E, k, D, d, dtype, "each", None, seed=N)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,E,d", [(1, 3, 40), (32, 8, 520), (33, 8, 520), (64, 60, 2048), (100, 256, 136), (128, 70, 131), (128, 16, 1032), (129, 16, 1032)])
+def test_route_backward_of_few_tokens(cm, N, E, d, dtype):
+    """Up to 128 tokens dW and dbias have no parts to join."""
+    for out in (None, F32):
+        _check_route(cm, N, E, min(E, 4), 0, d, dtype, "each", out, seed=N + d, gamma=4.0)
+
+
 def test_long_fp32_sums_of_dw_keep_their_precision(cm):
     """Sums of 9000 terms of one sign, 2300 of them in one thread block.  Sixteen additions a group of 256 tokens that cut off what
     fp32 does not hold (2^-23 of the sum, and as much where terms are aligned), then rounded ones: 9 groups, 4 ranges."""
