@@ -248,6 +248,30 @@ def test_route_backward_of_few_tokens(cm, N, E, d, dtype):
         _check_route(cm, N, E, min(E, 4), 0, d, dtype, "each", out, seed=N + d, gamma=4.0)
 
 
+def test_route_backward_captured_and_on_two_streams(cm):
+    """Every form of the products, twice in one graph with workspaces of its own, replayed while the same calls run on another stream."""
+    calls = []
+    for N, E, d, dtype in ((700, 200, 260, F32), (700, 30, 131, BF16), (900, 64, 512, BF16), (600, 6, 100, F32), (100, 70, 96, F32), (90, 70, 96, BF16)):
+        args, kw, want = _check_route(cm, N, E, 2, 0, d, dtype, "all", None, seed=N)
+        calls.append((args, kw, want))
+    torch.cuda.synchronize()
+    g, got = torch.cuda.CUDAGraph(), []
+    with torch.cuda.graph(g):
+        for _ in range(2):
+            got += [cm.route_backward(*args, **kw) for args, kw, _ in calls]
+    side, eager = torch.cuda.Stream(), []
+    for _ in range(3):
+        for r in got:
+            for v in r.values():
+                v.fill_(float("nan"))
+        side.wait_stream(torch.cuda.current_stream())
+        g.replay()
+        eager = [cm.route_backward(*args, stream=side, **kw) for args, kw, _ in calls]
+        torch.cuda.synchronize()
+        for r, (_, _, want) in zip(got + eager, calls * 3):
+            assert all(torch.equal(r[key], want[key]) for key in want)
+
+
 def test_long_fp32_sums_of_dw_keep_their_precision(cm):
     """Sums of 9000 terms of one sign, 2300 of them in one thread block.  Sixteen additions a group of 256 tokens that cut off what
     fp32 does not hold (2^-23 of the sum, and as much where terms are aligned), then rounded ones: 9 groups, 4 ranges."""
