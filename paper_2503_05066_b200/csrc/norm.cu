@@ -14,35 +14,48 @@ constexpr int NW = 8;                        // warps of a block, `wpr` of them 
 constexpr int NT_MAX = 512;
 constexpr int NORM_MAX_D = 16384;
 
-// A thread's NV columns of a vector's place u: with VEC (rows that start on 16 bytes) NV in a row, one 16-byte access; else the lanes
-// of a warp take turns, so that their accesses of single elements lie side by side, and a thread's columns are 32 apart.  Both ways
-// a warp has the same 32 NV columns, whole blocks of 128 of them.
-template <bool VEC, int NV>
-__device__ __forceinline__ int column(int u, int tpr, int t) {
-  return VEC ? (u * tpr + t) * NV : (u * tpr + (t & ~31)) * NV + (t & 31);
+// A thread's NV columns of a vector's place u are NV / W accesses of W neighbouring columns: with W = NV (rows that start on 16 bytes)
+// one; else four bytes (or, bf16 rows that do not start on four, one column) at a time, and the lanes of a warp take turns, so that
+// their accesses lie side by side.  Either way a warp has the same 32 NV columns, whole blocks of 128 of them.  (16,384 bf16 rows with
+// residual: 2048 columns 41 us, 2046 46, 2047 62, and 76 for both of the latter with accesses of one column converted on the way; the
+// gradient with dh 46, 52, 94, and 91.)
+template <int W, int NV>
+__device__ __forceinline__ int column(int u, int tpr, int t) {           // the first
+  return W == NV ? (u * tpr + t) * NV : (u * tpr + (t & ~31)) * NV + (t & 31) * W;
 }
+template <int W, int NV>
+__device__ __forceinline__ constexpr int other(int i) {                  // from there to the i-th
+  return W == NV ? i : i / W * 32 * W + i % W;
+}
+template <int BYTES> struct Access;
+template <> struct Access<4> { using type = uint32_t; };
+template <> struct Access<2> { using type = uint16_t; };
 // The columns from p on, as they are stored; `left`: columns from there to the end of the row.
-template <typename T, bool VEC>
+template <typename T, int W>
 __device__ __forceinline__ uint4 get_cells(const T* p, int left) {
-  if constexpr (VEC) {
+  constexpr int NV = Vec16<T>::n;
+  if constexpr (W == NV) {
     return __ldcs(reinterpret_cast<const uint4*>(p));
   } else {
-    float f[Vec16<T>::n];
+    using A = typename Access<W * (int)sizeof(T)>::type;
+    union { uint4 v; A a[NV / W]; } x;
 #pragma unroll
-    for (int i = 0; i < Vec16<T>::n; ++i) f[i] = i * 32 < left ? to_float(p[i * 32]) : 0.f;
-    return Vec16<T>::store(f);
+    for (int i = 0; i < NV / W; ++i) x.a[i] = i * 32 * W < left ? *reinterpret_cast<const A*>(p + i * 32 * W) : A(0);
+    return x.v;
   }
 }
-template <typename T, bool VEC>
+template <typename T, int W>
 __device__ __forceinline__ void put_cells(T* p, int left, const uint4& v) {
-  if constexpr (VEC) {
+  constexpr int NV = Vec16<T>::n;
+  if constexpr (W == NV) {
     *reinterpret_cast<uint4*>(p) = v;
   } else {
-    float f[Vec16<T>::n];
-    Vec16<T>::load(v, f);
+    using A = typename Access<W * (int)sizeof(T)>::type;
+    union { uint4 v; A a[NV / W]; } x;
+    x.v = v;
 #pragma unroll
-    for (int i = 0; i < Vec16<T>::n; ++i)
-      if (i * 32 < left) p[i * 32] = from_float<T>(f[i]);
+    for (int i = 0; i < NV / W; ++i)
+      if (i * 32 * W < left) *reinterpret_cast<A*>(p + i * 32 * W) = x.a[i];
   }
 }
 
@@ -69,10 +82,10 @@ __device__ __forceinline__ uint32_t two_codes(float a, float b, uint32_t code) {
   return code == (uint32_t)Q_NAN_SCALE ? 0x7f7fu : to_e4m3x2(a * inv, b * inv);
 }
 // Codes of a thread's columns under the scales of their blocks of 128, which are made here.
-template <typename T, bool VEC>
+template <typename T, int W>
 __device__ __forceinline__ void put_codes(const uint4& v, int c, int d, uint8_t* q, uint8_t* scale) {
   // a block: all NV columns of LANES lanes, or, lanes taking turns, PER columns of all lanes
-  constexpr int NV = Vec16<T>::n, LANES = VEC ? QBLOCK / NV : 32, PER = VEC ? NV : QBLOCK / 32;
+  constexpr int NV = Vec16<T>::n, LANES = W == NV ? QBLOCK / NV : 32, PER = W == NV ? NV : QBLOCK / 32;
   float f[NV];
   Vec16<T>::load(v, f);
 #pragma unroll
@@ -83,17 +96,17 @@ __device__ __forceinline__ void put_codes(const uint4& v, int c, int d, uint8_t*
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
     const uint32_t code = scale_code(m);
-    const int at = VEC ? c : c + b * 32;     // first of the thread's columns in the block
+    const int at = c + other<W, NV>(b);      // first of the thread's columns in the block
     if (at >= d) continue;
 #pragma unroll
     for (int i = 0; i < PER; i += 4) {
       const uint32_t w = two_codes(f[b + i], f[b + i + 1], code) | two_codes(f[b + i + 2], f[b + i + 3], code) << 16;
-      if constexpr (VEC) {
+      if constexpr (W == NV) {
         *reinterpret_cast<uint32_t*>(q + at + i) = w;
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (at + 32 * (i + j) < d) q[at + 32 * (i + j)] = (uint8_t)(w >> (8 * j));
+          if (at + other<W, NV>(i + j) < d) q[at + other<W, NV>(i + j)] = (uint8_t)(w >> (8 * j));
       }
     }
     if ((threadIdx.x & (LANES - 1)) == 0) scale[at / QBLOCK] = (uint8_t)code;
@@ -114,7 +127,7 @@ struct NormArgs {
 // A row stays in the registers of its warps between the two uses, VPT vectors a thread: one pass over HBM, which bounds it
 // (16,384 rows of 2048 bf16 columns with residual and codes: 47.8 us, 0.97 of the copy bandwidth).  Few vectors a thread and many
 // warps mix reads and writes: with eight vectors a thread, a warp to a row, the same took 59.9 us, with one 51.2.
-template <typename T, bool VEC, int VPT>
+template <typename T, int W, int VPT>
 __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
   allow_next_kernel();
   wait_for_previous_kernel();
@@ -127,26 +140,26 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
   uint4 v[VPT];
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = column<VEC, NV>(u, tpr, t);
-    v[u] = live && c < d ? get_cells<T, VEC>(a.x + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
+    const int c = column<W, NV>(u, tpr, t);
+    v[u] = live && c < d ? get_cells<T, W>(a.x + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
   }
   if (a.res) {
     uint4 r[VPT];
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
-      const int c = column<VEC, NV>(u, tpr, t);
-      r[u] = live && c < d ? get_cells<T, VEC>(a.res + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
+      const int c = column<W, NV>(u, tpr, t);
+      r[u] = live && c < d ? get_cells<T, W>(a.res + at + c, d - c) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
-      const int c = column<VEC, NV>(u, tpr, t);
+      const int c = column<W, NV>(u, tpr, t);
       float f[NV], g[NV];
       Vec16<T>::load(v[u], f);
       Vec16<T>::load(r[u], g);
 #pragma unroll
       for (int i = 0; i < NV; ++i) f[i] += g[i];
       v[u] = Vec16<T>::store(f);
-      if (live && c < d) put_cells<T, VEC>(a.h + at + c, d - c, v[u]);
+      if (live && c < d) put_cells<T, W>(a.h + at + c, d - c, v[u]);
     }
   }
   float sum = 0.f;
@@ -166,15 +179,15 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm(const NormArgs<T> a) {
   const int nb = (d + QBLOCK - 1) / QBLOCK;
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = column<VEC, NV>(u, tpr, t);
+    const int c = column<W, NV>(u, tpr, t);
     float f[NV], g[NV];
     Vec16<T>::load(v[u], f);
-    Vec16<T>::load(c < d ? (VEC ? __ldg(reinterpret_cast<const uint4*>(a.w + c)) : get_cells<T, false>(a.w + c, d - c)) : make_uint4(0u, 0u, 0u, 0u), g);
+    Vec16<T>::load(c < d ? (W == NV ? __ldg(reinterpret_cast<const uint4*>(a.w + c)) : get_cells<T, W>(a.w + c, d - c)) : make_uint4(0u, 0u, 0u, 0u), g);
 #pragma unroll
     for (int i = 0; i < NV; ++i) f[i] = f[i] * rstd * g[i];
     const uint4 y = Vec16<T>::store(f);
-    if (c < d) put_cells<T, VEC>(a.y + at + c, d - c, y);
-    if (a.q) put_codes<T, VEC>(y, c, d, a.q + at, a.scale + row * nb);
+    if (c < d) put_cells<T, W>(a.y + at + c, d - c, y);
+    if (a.q) put_codes<T, W>(y, c, d, a.q + at, a.scale + row * nb);
   }
 }
 
@@ -186,8 +199,14 @@ struct GradArgs {
   int64_t N;
   int d, wpr;
   T* dx;
-  float* part;                               // [groups of warps][d]
+  float* part;                               // [blocks][d]
+  __nv_bfloat16* dw16;                       // one block: dw itself, as bf16; else NULL
 };
+
+__device__ __forceinline__ uint4 together(const uint32_t* a) { return make_uint4(a[0], a[1], a[2], a[3]); }
+__device__ __forceinline__ uint4 together(const uint16_t* a) {
+  return make_uint4(a[0] | (uint32_t)a[1] << 16, a[2] | (uint32_t)a[3] << 16, a[4] | (uint32_t)a[5] << 16, a[6] | (uint32_t)a[7] << 16);
+}
 
 // Per-thread ring of the rows to come: every thread copies the 16-byte vectors that it will use itself into its own places of
 // shared memory, so nothing but its own copies has to be waited for.
@@ -204,15 +223,18 @@ __device__ __forceinline__ uint4 get_shared(uint32_t at) {
 }
 
 // A group of wpr warps walks its rows, DEPTH - 1 of them in flight ahead of the one it works on; a thread's columns are the same
-// in all of them: dw is summed in registers, and written once per group for k_sum_parts to join in a fixed order.  Bound by HBM
+// in all of them: dw is summed in registers, over a block's groups in shared memory, and written once per block for k_sum_parts to
+// join, all in a fixed order.  (A part per group: 12,247 rows of 192 bf16 columns 14.2 us,
+// like this 11.9.)  So few rows that a block walks four at most have the block to themselves, and no parts.  Bound by HBM
 // (16,384 rows of 4096 bf16 columns with dh: 83.6 us with the sum of the parts, 0.98 of the copy bandwidth; 108 with each row's loads
 // waited for, 88 with the next row's in registers); narrower rows also by the row's sum, a barrier a row (16,384 of 2048 without
 // dh: 40 us, 0.76).
-template <typename T, bool VEC, int VPT, int DEPTH>
+template <typename T, int W, int VPT, int DEPTH>
 __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   allow_next_kernel();
   wait_for_previous_kernel();
   constexpr int NV = Vec16<T>::n;
+  constexpr bool ASYNC = W == NV;
   __shared__ float red[2][NT_MAX / 32];
   extern __shared__ uint4 ring[];            // [PLACES][dy, h, dh][VPT][threads]
   const int tpr = a.wpr * 32, t = threadIdx.x & (tpr - 1), d = a.d;
@@ -223,48 +245,50 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
   float dw[VPT][NV];
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = column<VEC, NV>(u, tpr, t);
-    w[u] = c < d ? get_cells<T, VEC>(a.w + c, d - c) : zero;
+    const int c = column<W, NV>(u, tpr, t);
+    w[u] = c < d ? get_cells<T, W>(a.w + c, d - c) : zero;
 #pragma unroll
     for (int i = 0; i < NV; ++i) dw[u][i] = 0.f;
   }
-  // Rows of whole vectors: asynchronous copies, DEPTH - 1 rows ahead.  Others: the next row's elements wait in registers while this
-  // row is worked on (copies of less than four bytes do not exist), and take its place afterwards.
-  constexpr int PLACES = VEC ? DEPTH : 1;
-  T raw[VEC ? 1 : 3][VEC ? 1 : VPT][VEC ? 1 : NV];
+  // Rows of whole vectors: asynchronous copies, DEPTH - 1 rows ahead.  Others: the next row's columns wait in registers while this
+  // row is worked on, and take its place afterwards (asynchronous copies of four bytes: 8192 rows of 2049 fp32 columns 79 -> 152 us).
+  constexpr int PLACES = ASYNC ? DEPTH : 1;
+  using A = typename Access<ASYNC ? 4 : W * (int)sizeof(T)>::type;
+  A raw[ASYNC ? 1 : 3][ASYNC ? 1 : VPT][ASYNC ? 1 : NV / W];
   const T* const from3[3] = {a.dy, a.h, a.dh};
   auto fetch = [&](int64_t row, int slot) {
 #pragma unroll
     for (int m = 0; m < 3; ++m)
 #pragma unroll
       for (int u = 0; u < VPT; ++u) {
-        const int c = column<VEC, NV>(u, tpr, t);
+        const int c = column<W, NV>(u, tpr, t);
         const bool in = row < a.N && from3[m];
         const T* p = in ? from3[m] + row * d : a.w;
-        if constexpr (VEC) {
-          copy16(mine + (uint32_t)((slot * 3 + m) * VPT + u) * step, p + (c < d ? c : 0), in && c < d);
+        const uint32_t to = mine + (uint32_t)((slot * 3 + m) * VPT + u) * step;
+        if constexpr (W == NV) {
+          copy16(to, p + (c < d ? c : 0), in && c < d);
         } else {
 #pragma unroll
-          for (int i = 0; i < NV; ++i) raw[m][u][i] = p[c + i * 32 < d ? c + i * 32 : 0];
+          for (int i = 0; i < NV / W; ++i) raw[m][u][i] = *reinterpret_cast<const A*>(p + (c + i * 32 * W < d ? c + i * 32 * W : 0));
         }
       }
-    if constexpr (VEC) copies_commit();
+    if constexpr (ASYNC) copies_commit();
   };
   auto place = [&](int64_t row, int slot) {  // what fetch left in registers, zeros where there is nothing
-    if constexpr (!VEC) {
+    if constexpr (!ASYNC) {
 #pragma unroll
       for (int m = 0; m < 3; ++m)
 #pragma unroll
         for (int u = 0; u < VPT; ++u) {
-          const int c = column<VEC, NV>(u, tpr, t);
-          float f[NV];
+          const int c = column<W, NV>(u, tpr, t);
+          A cells[NV / W];
 #pragma unroll
-          for (int i = 0; i < NV; ++i) f[i] = row < a.N && from3[m] && c + i * 32 < d ? to_float(raw[m][u][i]) : 0.f;
-          ring[(size_t)((slot * 3 + m) * VPT + u) * blockDim.x + threadIdx.x] = Vec16<T>::store(f);
+          for (int i = 0; i < NV / W; ++i) cells[i] = row < a.N && from3[m] && c + i * 32 * W < d ? raw[m][u][i] : A(0);
+          ring[(size_t)((slot * 3 + m) * VPT + u) * blockDim.x + threadIdx.x] = together(cells);
         }
     }
   };
-  constexpr int AHEAD = VEC ? DEPTH - 1 : 1;
+  constexpr int AHEAD = ASYNC ? DEPTH - 1 : 1;
 #pragma unroll
   for (int s = 0; s < AHEAD; ++s) fetch(group + s * groups, s);
   place(group, 0);
@@ -275,7 +299,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
     const bool live = row < a.N;
     fetch(row + AHEAD * groups, slot == 0 ? PLACES - 1 : slot - 1);
     const float rstd1 = row + groups < a.N ? a.rstd[row + groups] : 0.f;
-    if constexpr (VEC) copies_wait<AHEAD>();
+    if constexpr (ASYNC) copies_wait<AHEAD>();
     const uint32_t from = mine + (uint32_t)(slot * 3 * VPT) * step;
     uint4 dy[VPT], h[VPT];
     float dot = 0.f;
@@ -297,7 +321,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
     const float k = -row_sum(dot, a.wpr, red[it]) / (float)d * rstd * rstd;
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
-      const int c = column<VEC, NV>(u, tpr, t);
+      const int c = column<W, NV>(u, tpr, t);
       float p[NV], q[NV], g[NV], e[NV];
       Vec16<T>::load(dy[u], p);
       Vec16<T>::load(h[u], q);
@@ -305,20 +329,36 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
       Vec16<T>::load(get_shared(from + (uint32_t)(2 * VPT + u) * step), e);
 #pragma unroll
       for (int i = 0; i < NV; ++i) p[i] = fmaf(q[i], k, fmaf(rstd, p[i] * g[i], e[i]));
-      if (live && c < d) put_cells<T, VEC>(a.dx + row * d + c, d - c, Vec16<T>::store(p));
+      if (live && c < d) put_cells<T, W>(a.dx + row * d + c, d - c, Vec16<T>::store(p));
     }
     rstd = rstd1;
     if (++slot == PLACES) slot = 0;
     place(row + groups, slot);
   }
-  float* part = a.part + group * d;
+  float* to = a.part + (int64_t)blockIdx.x * d;                // the block's part, of its groups' sums in their order
+  const bool staged = tpr < (int)blockDim.x || a.dw16 || (reinterpret_cast<uintptr_t>(a.part) & 15);
+  if (staged) {
+    if constexpr (ASYNC) copies_wait<0>();
+    __syncthreads();                         // the ring is free
+    to = reinterpret_cast<float*>(ring) + (threadIdx.x / tpr) * d;
+  }
 #pragma unroll
   for (int u = 0; u < VPT; ++u) {
-    const int c = column<VEC, NV>(u, tpr, t);
+    const int c = column<W, NV>(u, tpr, t);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (VEC && i % 4 == 0 && c < d) *reinterpret_cast<float4*>(part + c + i) = make_float4(dw[u][i], dw[u][i + 1], dw[u][i + 2], dw[u][i + 3]);
-      if (!VEC && c + i * 32 < d) part[c + i * 32] = dw[u][i];
+      if (W == NV && i % 4 == 0 && c < d) *reinterpret_cast<float4*>(to + c + i) = make_float4(dw[u][i], dw[u][i + 1], dw[u][i + 2], dw[u][i + 3]);
+      if (W < NV && c + other<W, NV>(i) < d) to[c + other<W, NV>(i)] = dw[u][i];
+    }
+  }
+  if (staged) {
+    __syncthreads();
+    const float* sums = reinterpret_cast<const float*>(ring);
+    for (int c = threadIdx.x; c < d; c += blockDim.x) {
+      float v = sums[c];
+      for (int g = 1; g < (int)blockDim.x / tpr; ++g) v += sums[g * d + c];
+      if (a.dw16) a.dw16[c] = __float2bfloat16_rn(v);
+      else a.part[(int64_t)blockIdx.x * d + c] = v;
     }
   }
 }
@@ -357,21 +397,25 @@ int warps_per_row(int64_t N, int vecs, int vpt, int most) {
   return vecs > 32 * NW * most ? 2 * NW : wpr;
 }
 int norm_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, NORM_VPT, 8); }
-int grad_warps(int64_t N, int vecs) { return warps_per_row(N, vecs, GRAD_VPT, 2); }
 int rows_per_block(int wpr) { return wpr < NW ? NW / wpr : 1; }
+constexpr int ALONE = 4;                     // rows that a group of the gradient's only block walks at most (of rows that eight warps hold)
+int grad_warps(int64_t N, int vecs) {
+  const int few = warps_per_row((int64_t)1 << 40, vecs, GRAD_VPT, 2);
+  return few <= NW && N <= ALONE * rows_per_block(few) ? few : warps_per_row(N, vecs, GRAD_VPT, 2);
+}
 unsigned threads_of(int wpr) { return 32u * (unsigned)(wpr < NW ? NW : wpr); }
 int vecs_of(int d, int dtype) { return (int)ceil_div((int64_t)d * (int64_t)elt_size(dtype), 16); }
 int grad_blocks(int64_t N, int wpr) {
   const int64_t want = ceil_div(N, rows_per_block(wpr)), most = (int64_t)sm_count() * GRAD_BLOCKS;
-  return (int)(want < most ? want : most);
+  return wpr <= NW && want <= ALONE ? 1 : (int)(want < most ? want : most);
 }
 
-template <typename T, bool VEC>
+template <typename T, int W>
 int norm_run(const NormArgs<T>& a, cudaStream_t st) {
   const int vpt = (int)ceil_div(ceil_div(a.d, Vec16<T>::n), 32 * a.wpr);
   const int64_t blocks = ceil_div(a.N, rows_per_block(a.wpr));
   if (blocks > 0x7fffffff) return CAPMOE_EUNSUPPORTED;
-  auto k = vpt <= 1 ? k_rms_norm<T, VEC, 1> : vpt <= 2 ? k_rms_norm<T, VEC, 2> : vpt <= 4 ? k_rms_norm<T, VEC, 4> : k_rms_norm<T, VEC, 8>;
+  auto k = vpt <= 1 ? k_rms_norm<T, W, 1> : vpt <= 2 ? k_rms_norm<T, W, 2> : vpt <= 4 ? k_rms_norm<T, W, 4> : k_rms_norm<T, W, 8>;
   const int rc = note_cuda(launch_chained(k, (unsigned)blocks, threads_of(a.wpr), 0, st, a));
   count_launch(1);
   return rc;
@@ -381,16 +425,17 @@ int norm(const void* x, const void* res, const void* w, int64_t N, int d, float 
          int dtype, cudaStream_t st) {
   const NormArgs<T> a{(const T*)x, (const T*)res, (const T*)w, N, d, norm_warps(N, vecs_of(d, dtype)), eps, (T*)h, (T*)y, rstd,
                       (uint8_t*)q, (uint8_t*)scale};
-  return d % Vec16<T>::n == 0 ? norm_run<T, true>(a, st) : norm_run<T, false>(a, st);
+  constexpr int NV = Vec16<T>::n, W = 4 / sizeof(T);
+  return d % NV == 0 ? norm_run<T, NV>(a, st) : d % W == 0 ? norm_run<T, W>(a, st) : norm_run<T, 1>(a, st);
 }
 
-template <typename T, bool VEC>
+template <typename T, int W>
 int grad_run(const GradArgs<T>& a, cudaStream_t st) {
   const int vpt = (int)ceil_div(ceil_div(a.d, Vec16<T>::n), 32 * a.wpr);
   const int room = vpt <= 1 ? 1 : vpt <= 2 ? 2 : vpt <= 4 ? 4 : 8;
-  const int depth = !VEC ? 1 : room == 1 ? GRAD_DEPTH1 : room == 2 ? GRAD_DEPTH2 : 8 / room;
-  auto k = room == 1 ? k_rms_norm_grad<T, VEC, 1, GRAD_DEPTH1> : room == 2 ? k_rms_norm_grad<T, VEC, 2, GRAD_DEPTH2>
-           : room == 4 ? k_rms_norm_grad<T, VEC, 4, 2> : k_rms_norm_grad<T, VEC, 8, 1>;
+  const int depth = W < Vec16<T>::n ? 1 : room == 1 ? GRAD_DEPTH1 : room == 2 ? GRAD_DEPTH2 : 8 / room;
+  auto k = room == 1 ? k_rms_norm_grad<T, W, 1, GRAD_DEPTH1> : room == 2 ? k_rms_norm_grad<T, W, 2, GRAD_DEPTH2>
+           : room == 4 ? k_rms_norm_grad<T, W, 4, 2> : k_rms_norm_grad<T, W, 8, 1>;
   const size_t smem = (size_t)depth * 3 * (size_t)room * threads_of(a.wpr) * 16;
   if (smem > 40 * 1024) {                    // (the default limit is 48 KB, what the kernel declares included)
     const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -403,10 +448,14 @@ int grad_run(const GradArgs<T>& a, cudaStream_t st) {
 template <typename T>
 int norm_grad(const void* dy, const void* h, const void* w, const float* rstd, const void* dh, int64_t N, int d, int dtype, int out_dtype,
               void* dx, void* dw, float* part, cudaStream_t st) {
-  const GradArgs<T> a{(const T*)dy, (const T*)h, (const T*)w, rstd, (const T*)dh, N, d, grad_warps(N, vecs_of(d, dtype)), (T*)dx, part};
-  const int rc = d % Vec16<T>::n == 0 ? grad_run<T, true>(a, st) : grad_run<T, false>(a, st);
-  if (rc != CAPMOE_OK) return rc;
-  return sum_parts(part, (int64_t)grad_blocks(N, a.wpr) * rows_per_block(a.wpr), d, out_dtype, dw, st);
+  GradArgs<T> a{(const T*)dy, (const T*)h, (const T*)w, rstd, (const T*)dh, N, d, grad_warps(N, vecs_of(d, dtype)), (T*)dx, part, nullptr};
+  const int blocks = grad_blocks(N, a.wpr);
+  if (blocks == 1 && out_dtype == CAPMOE_F32) a.part = (float*)dw;
+  if (blocks == 1 && out_dtype == CAPMOE_BF16) a.dw16 = (__nv_bfloat16*)dw;
+  constexpr int NV = Vec16<T>::n, W = 4 / sizeof(T);
+  const int rc = d % NV == 0 ? grad_run<T, NV>(a, st) : d % W == 0 ? grad_run<T, W>(a, st) : grad_run<T, 1>(a, st);
+  if (rc != CAPMOE_OK || blocks == 1) return rc;
+  return sum_parts(part, blocks, d, out_dtype, dw, st);
 }
 
 int check_norm(int64_t N, int d, int dtype) {
@@ -450,7 +499,7 @@ extern "C" int capmoe_rms_norm_backward_workspace_bytes(int64_t N, int d, int dt
   if (!bytes) return CAPMOE_EINVAL;
   if (rc != CAPMOE_OK) return rc;
   const int wpr = grad_warps(N, vecs_of(d, dtype));
-  *bytes = (size_t)grad_blocks(N, wpr) * (size_t)rows_per_block(wpr) * (size_t)d * sizeof(float);
+  *bytes = N ? (size_t)grad_blocks(N, wpr) * (size_t)d * sizeof(float) : 0;
   return CAPMOE_OK;
 }
 

@@ -173,6 +173,17 @@ def test_gradients_of_many_rows(cm, N, d, dtype):
     _check_grad(cm, N, d, dtype, True, None, seed=N)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,d", [(32, 60), (33, 60), (31, 512), (16, 520), (17, 1024), (4, 4096), (5, 4096), (4, 16384), (2, 8193), (9, 1001), (3000, 24), (2500, 130)])
+def test_gradients_of_one_block_and_of_narrow_rows(cm, N, d, dtype):
+    for out in (None, F32):
+        args = _check_grad(cm, N, d, dtype, True, out, seed=N + d)
+    h, w, dy, dh, rstd, gx, gw = args
+    room = torch.full((d + 4,), float("nan"), device="cuda")          # dw anywhere on four bytes, and nothing beside it
+    x2, w2 = cm.rms_norm_backward(dy, h, w, rstd, dh=dh, dw=room[1:d + 1])
+    assert torch.equal(x2, gx) and torch.equal(w2, gw) and bool(room[0].isnan()) and bool(room[d + 1:].isnan().all())
+
+
 def test_gradients_against_differences(cm):
     """Along random directions: (f(p + s v) - f(p - s v)) / 2s of f = <dy, y> + <dh, h> in 64 bits, whose own error is s^2 and
     rounding / s; the gradient's is its elementwise bound times the direction."""
