@@ -355,7 +355,7 @@ int capmoe_grouped_ffn_fp8_codes(const void* x_q, const void* x_scale, const int
  * residual alike (may be dy or dh);  dw = sum over the rows of dy h rstd [d] in out_dtype (`dtype`, or CAPMOE_F32), zeros
  * for N = 0, summed in fp32 in a fixed order for a given N, d and device.
  *   ws: capmoe_rms_norm_backward_workspace_bytes(N,d,dtype) bytes on the device that is current.
- * d <= 16384.  Rows of whole 16-byte vectors are read as such, others element by element. */
+ * d <= 16384.  Rows of whole 16-byte vectors are the fastest, then those of whole words of four bytes. */
 int capmoe_rms_norm(const void* x, const void* residual, const void* w, int64_t N, int d, int dtype, float eps, void* h, void* y,
                     float* rstd, void* q, void* scale, void* stream);
 int capmoe_rms_norm_backward_workspace_bytes(int64_t N, int d, int dtype, size_t* bytes);
