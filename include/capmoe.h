@@ -381,9 +381,8 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  *                              dS[t,e] = dscores[t,e] + dweight[row of (t,e)],  dlogits = S (dS - sum_f S_f dS_f) [N,E] fp32,
  *                              dx = dlogits W_r [N,d] `dtype`,  dw = dlogits^T x [E,d] out_dtype (`dtype`, or CAPMOE_F32),
  *                              dbias = sum_t dlogits [E] fp32.
- *                            bf16: dlogits enter the products as the sum of two bf16 numbers each (at most 2^-16 of them is lost).
- *                            fp32: beyond eight experts on tensor cores, every factor as the sum of three bf16 numbers that it is
- *                            (at most 2^-30 of each term is lost).
+ *                            On tensor cores (bf16, and fp32 beyond eight experts) every fp32 factor enters the products as the sum
+ *                            of three bf16 numbers that it is: nothing of dlogits is lost, of fp32 terms at most 2^-30 each.
  *                            N = 0 leaves zeros in dw and dbias.  All sums have a fixed order for given sizes and device.
  *                            ws: capmoe_route_backward_workspace_bytes(N,d,E,dtype) bytes on the device that is current.
  * The first three: rows of whole 16-byte vectors, slots <= 288, N and A_max < 2^31.  route_backward: E <= 256, k <= 32,

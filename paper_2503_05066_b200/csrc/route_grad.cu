@@ -8,8 +8,8 @@
 //   fp32, up to eight experts             k_route_grad_few: everything in one kernel on plain FMAs, W_r and dW_r in registers
 //   bf16, rows of whole 16-byte vectors   k_route_logit_grad, then both products in one pass over x (route_grad_tc.cu)
 //   others                                the same with x read and laid out by warps (route_grad_any.cu)
-// Tensor cores take dl, which is fp32, as a sum of bf16 numbers.  One rounding could cost it 2^-8: for bf16 products it goes in as
-// its rounding and the rounding of what that leaves out (2^-16 of dl is lost at most), for fp32 as three that lose nothing.
+// Tensor cores take dl, which is fp32, as three bf16 numbers whose sum it is: the top 16 bits of an fp32 number are a bf16 number, so are
+// those of the rest, and what that leaves has 8 bits.
 #include "route_grad.cuh"
 
 namespace capmoe {
@@ -21,8 +21,8 @@ constexpr int RG_BLOCKS = 4;                 // blocks per SM at most (walks the
 struct LogitArgs {
   ScoreGrad s;
   float *dlogits, *dbias_part;               // dbias_part may be NULL
-  __nv_bfloat16* pair;                       // [N, parts Eq]
-  int Eq, parts;                             // two: rounded; three: cut off
+  __nv_bfloat16* split;                      // [N, ROUTE_PARTS Eq]
+  int Eq;
 };
 
 // A warp takes four tokens at a time (their lookups in flight together), lane + 32 i an expert of each.
@@ -73,19 +73,13 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
         bias[i] += dl;
         if (e < E) a.dlogits[t * E + e] = dl;
         if (e < a.Eq) {
-          __nv_bfloat16* p = a.pair + t * a.parts * a.Eq + e;
-          if (a.parts == 2) {
-            const __nv_bfloat16 hi = __float2bfloat16_rn(dl);
-            p[0] = hi;
-            p[a.Eq] = __float2bfloat16_rn(dl - __bfloat162float(hi));
-          } else {
-            float rest = dl;
+          __nv_bfloat16* p = a.split + t * ROUTE_PARTS * a.Eq + e;
+          float rest = dl;
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {
-              const uint32_t top = __float_as_uint(rest) & 0xffff0000u;
-              p[q * a.Eq] = __ushort_as_bfloat16((unsigned short)(top >> 16));
-              rest = rest == __uint_as_float(top) ? 0.f : rest - __uint_as_float(top);       // (an infinity leaves nothing)
-            }
+          for (int q = 0; q < ROUTE_PARTS; ++q) {
+            const uint32_t top = __float_as_uint(rest) & 0xffff0000u;
+            p[q * a.Eq] = __ushort_as_bfloat16((unsigned short)(top >> 16));
+            rest = rest == __uint_as_float(top) ? 0.f : rest - __uint_as_float(top);         // (an infinity leaves nothing)
           }
         }
       }
@@ -331,7 +325,7 @@ enum Form { FEW, TC, ANY };
 struct RouteWs {
   Form form;
   int Eq, ranges, blocks;                    // blocks of the logits' kernel (FEW: ranges)
-  size_t bias, pair, parts, total;
+  size_t bias, split, parts, total;
 };
 int few_tx(int d) {
   int tx = 32;
@@ -341,7 +335,7 @@ int few_tx(int d) {
 RouteWs route_ws(int64_t N, int d, int E, int dtype) {
   RouteWs w = {};
   w.form = route_grad_tc_supported(d, dtype) ? TC : dtype == CAPMOE_F32 && E <= FEW_E ? FEW : ANY;
-  w.Eq = (E + 7) / 8 * 8;                    // rows of `pair` in whole 16-byte vectors
+  w.Eq = (E + 7) / 8 * 8;                    // rows of `split` in whole 16-byte vectors
   const int64_t sms = sm_count();
   if (w.form == FEW) {
     // two blocks per SM; 32 tokens each at least, or a part of dW_r would be as long as its tokens
@@ -351,14 +345,14 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
     if (r > 65535) r = 65535;
     w.ranges = (int)ceil_div(N, ceil_div(N, r));
   } else {
-    w.ranges = w.form == TC ? route_grad_tc_ranges(N, d, E) : route_grad_any_ranges(N, d, dtype);
+    w.ranges = w.form == TC ? route_grad_tc_ranges(N, d, E) : route_grad_any_ranges(N, d, E, dtype);
   }
   const int64_t want = ceil_div(N, RG_WARPS * RG_TOK), most = sms * RG_BLOCKS;
   w.blocks = w.form == FEW ? w.ranges : (int)(want < most ? want : most);
   if (w.ranges < 1) w.ranges = 1;
   if (w.blocks < 1) w.blocks = 1;
-  w.pair = up256((size_t)w.blocks * E * 4);
-  w.parts = w.pair + (w.form == FEW ? 0 : up256((size_t)N * route_parts(dtype) * w.Eq * 2));
+  w.split = up256((size_t)w.blocks * E * 4);
+  w.parts = w.split + (w.form == FEW ? 0 : up256((size_t)N * ROUTE_PARTS * w.Eq * 2));
   w.total = w.parts + up256((size_t)w.ranges * E * d * 4) + 256;         // 256: to align all of it
   return w;
 }
@@ -433,15 +427,15 @@ extern "C" int capmoe_route_backward(const void* x, const void* w_router, const 
     LogitArgs a = {};
     a.s = sg;
     a.dlogits = dlogits; a.dbias_part = single ? nullptr : bias;
-    a.pair = (__nv_bfloat16*)(b + w.pair);
-    a.Eq = w.Eq; a.parts = route_parts(dtype);
+    a.split = (__nv_bfloat16*)(b + w.split);
+    a.Eq = w.Eq;
     auto kernel = E <= 32 ? k_route_logit_grad<1> : E <= 64 ? k_route_logit_grad<2> : E <= 128 ? k_route_logit_grad<4> : k_route_logit_grad<8>;
     rc = note_cuda(launch_chained(kernel, (unsigned)w.blocks, RG_WARPS * 32, 0, st, a));
     count_launch(1);
     if (rc != CAPMOE_OK) return rc;
     const RouteOut out{parts, single && !whole ? (__nv_bfloat16*)dw : nullptr, dlogits, single ? dbias : nullptr};
-    rc = w.form == TC ? route_grad_tc(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dx, out, dev_status, st)
-                      : route_grad_any(a.pair, x, w_router, N, d, E, w.Eq, w.ranges, dtype, dx, out, dev_status, st);
+    rc = w.form == TC ? route_grad_tc(a.split, x, w_router, N, d, E, w.Eq, w.ranges, dx, out, dev_status, st)
+                      : route_grad_any(a.split, x, w_router, N, d, E, w.Eq, w.ranges, dtype, dx, out, dev_status, st);
   }
   if (rc != CAPMOE_OK || single) return rc;
   const int64_t size = (int64_t)E * d;

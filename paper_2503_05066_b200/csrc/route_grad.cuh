@@ -29,9 +29,7 @@ __device__ __forceinline__ void add_kept(const ScoreGrad& a, int64_t t0, int n, 
 }
 
 // Ranges of whole stages of 64 tokens, none of them empty: one wave of CTAs, 128 tokens each at least, or as many waves as keep a range
-// within `most` tokens.  The MMAs cut their sums off where fp32 ends, and a long sum loses with each of them (dW_r of bf16 products, two
-// MMAs per 16 tokens: 1.9 10^-5 after ROUTE_CHAIN tokens, where dl's two numbers alone may leave out 1.5 10^-5).
-constexpr int64_t ROUTE_CHAIN = 8192;
+// within `most` tokens.
 inline int route_ranges(int64_t N, int64_t slices, int64_t most) {
   const int64_t units = ceil_div(N, 64), wave = sm_count() / slices > 1 ? sm_count() / slices : 1;
   int64_t r = wave * ceil_div(N, wave * most);
@@ -40,8 +38,8 @@ inline int route_ranges(int64_t N, int64_t slices, int64_t most) {
 }
 
 // dx = dl W_r and the parts of dW_r = dl^T x over `ranges` ranges of tokens on tcgen05.
-// pair [N, n Eq]: dl as n bf16 numbers (route_parts), Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the
-// stream wrote `pair` and let its successor start only after its own wait for what came before.
+// split [N, ROUTE_PARTS Eq]: dl as bf16 numbers, Eq a multiple of 8 >= E; parts [ranges][E][d].  The kernel before it on the
+// stream wrote `split` and let its successor start only after its own wait for what came before.
 // With one range dW_r is final: it goes to `parts`, or as bf16 to dw16, and dbias is made too, from dl [N, E].
 struct RouteOut {
   float* parts;
@@ -58,15 +56,15 @@ __device__ __forceinline__ void sum_bias(const RouteOut& o, int64_t n, int E, in
     o.dbias[e] = s;
   }
 }
-inline int route_parts(int dtype) { return dtype == CAPMOE_BF16 ? 2 : 3; }
+constexpr int ROUTE_PARTS = 3;
 //   bf16, d a multiple of 8
 inline bool route_grad_tc_supported(int d, int dtype) { return dtype == CAPMOE_BF16 && d % 8 == 0; }
 int route_grad_tc_ranges(int64_t N, int d, int E);
-int route_grad_tc(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out,
+int route_grad_tc(const void* split, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out,
                   int32_t* dev_status, cudaStream_t st);
 //   any
-int route_grad_any_ranges(int64_t N, int d, int dtype);
-int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx,
+int route_grad_any_ranges(int64_t N, int d, int E, int dtype);
+int route_grad_any(const void* split, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx,
                    const RouteOut& out, int32_t* dev_status, cudaStream_t st);
 
 }  // namespace capmoe

@@ -4,14 +4,15 @@
 // memory, dl comes in tiles of 64 experts by TMA, dW_r^T stays in tensor memory until the range ends.  But x and W_r are read by
 // eight warps of their own, element by element or in pairs, neighbouring columns on neighbouring lanes, and laid out for the MMAs
 // on the way (rows of 128 bytes, their 16-byte pieces swapped by the row's last three bits).
-// fp32 goes in exactly: the top 16 bits of a number are a bf16 number, so are those of the rest, and what that leaves has 8
-// bits: three numbers whose sum it is.  Of the nine products of two such sums all but the last (2^-30 of the product at most) are
-// added up in fp32, the smallest first (with the six largest, which leave out up to 2^-21, 3 % less time).  Three numbers of W_r, x
-// and dl fill the shared memory with 64 experts; more come in passes of 64, the later ones adding to dx.  The MMAs cut their sums off where
-// fp32 ends: the largest products have an accumulator of dW_r^T to themselves, and both are added up in registers every 256 tokens (the
-// error of dW_r over 4096 tokens a CTA is 3 10^-7 of it like this, 3 10^-5 with one accumulator to the end; the time is the same).
+// fp32 goes in exactly, as three bf16 numbers whose sum it is (route_grad.cu).  Of the nine products of two such sums all but the last
+// (2^-30 of the product at most) are added up in fp32, the smallest first (with the six largest, which leave out up to 2^-21, 3 % less
+// time).  Three numbers of W_r, x and dl fill the shared memory with 64 experts; more come in passes of 64, the later ones adding to dx.
+// The MMAs cut their sums off where fp32 ends.  With up to 64 experts the largest products have an accumulator of dW_r^T to
+// themselves, and both are added up in registers every 256 tokens (the error of fp32's dW_r over 4096 tokens a CTA is 3 10^-7 of it like
+// this, 3 10^-5 with one accumulator to the end; the time is the same).  bf16 tokens of more experts have one accumulator, registers
+// for no more, and ranges of ROUTE_CHAIN tokens at most.
 // fp32, 16,384 tokens of 4096 columns, 64 experts: 179 us (plain FMAs 556), bound by the loading warps (two parts of three go
-// through subtractions) and by shared memory, which the MMAs read at its full rate; bf16, 16,384 of 2047, 32 experts: 56 us, bound by
+// through subtractions) and by shared memory, which the MMAs read at its full rate; bf16, 16,384 of 2047, 32 experts: 57 us, bound by
 // instructions (two loads of two bytes for a word).  Left out: two stages of x ahead in registers (17 % slower, spilled).
 #include "gmm_tc.cuh"
 #include "route_grad.cuh"
@@ -25,22 +26,20 @@ constexpr int DC = 128;                      // columns of a CTA
 constexpr int BOX = 64 * 128;                // 64 rows of 64 columns
 constexpr int TILE = 2 * BOX;                // 64 rows of 128 columns of x or W_r; 128 tokens of 64 experts of dl
 
-template <typename T>
+template <typename T, int KB>                // KB: tiles of 64 experts, at most: 1, or of bf16 also 2 or 4
 struct RA {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr int P = F32 ? 3 : 1;                        // bf16 numbers of an element of x and W_r
-  static constexpr int Q = F32 ? 3 : 2;                        // and of dl
-  static constexpr int KB = F32 ? 1 : 4;                       // tiles of 64 experts, at most
-  static constexpr int W_BYTES = KB * P * TILE, DL_BYTES = Q * TILE, X_BYTES = P * TILE;
+  static constexpr int W_BYTES = KB * P * TILE, DL_BYTES = ROUTE_PARTS * TILE, X_BYTES = P * TILE;
   static constexpr int RING = F32 ? 1 : 2;                     // tiles of dl
-  static constexpr int NST = F32 ? 2 : 4;                      // stages of x, 64 tokens each
+  static constexpr int NST = F32 || KB == 4 ? 2 : 4;           // stages of x, 64 tokens each
   static constexpr int STG_BYTES = 32 * 33 * 4;                // an epilogue warp's 32 x 32 sums of dx
   static constexpr int DL_OFF = W_BYTES, X_OFF = DL_OFF + RING * DL_BYTES, STG_OFF = X_OFF + NST * X_BYTES;
   static constexpr int TAIL = STG_OFF + EPI_WARPS * STG_BYTES;
   static constexpr int SMEM = TAIL + 1024 + 256;
-  static constexpr int SUMS = F32 ? 2 : 1;                     // accumulators of dW_r^T: fp32 two, of the large products and the others
-  static constexpr int GROUP = F32 ? 2 : 1 << 30;              // blocks that a set of them takes, two sets in turn
-  static constexpr int DW_COLS = F32 ? 2 * SUMS * 64 : KB * 64;        // tensor-memory columns of dW_r^T, then SLOTS x 128 for dx
+  static constexpr bool FLUSH = KB == 1;                       // accumulators of dW_r^T: two, of the large products and the others; else one
+  static constexpr int GROUP = FLUSH ? 2 : 1 << 30;            // blocks that a set of two takes, two sets in turn
+  static constexpr int DW_COLS = FLUSH ? 4 * 64 : KB * 64;     // tensor-memory columns of dW_r^T, then SLOTS x 128 for dx
   static constexpr int SLOTS = 2;
   static_assert(SMEM <= 227 * 1024, "shared memory of a thread block");
   static_assert(DW_COLS + SLOTS * 128 <= 512, "tensor memory");
@@ -54,12 +53,12 @@ template <> struct Pairs<float> {
   __device__ static constexpr int w(int i) { constexpr int v[n] = {2, 1, 2, 1, 0, 1, 0, 0}; return v[i]; }
 };
 template <> struct Pairs<__nv_bfloat16> {
-  static constexpr int n = 2;
-  __device__ static constexpr int l(int i) { return 1 - i; }
+  static constexpr int n = ROUTE_PARTS;
+  __device__ static constexpr int l(int i) { return n - 1 - i; }
   __device__ static constexpr int w(int) { return 0; }
 };
 
-struct RAMaps { CUtensorMap dl[3]; };
+struct RAMaps { CUtensorMap dl[ROUTE_PARTS]; };
 template <typename T>
 struct RAArgs {
   const T *x, *w;
@@ -149,13 +148,10 @@ __device__ __forceinline__ void put_sums(const uint32_t* g, uint32_t* stg, float
     }
   }
 }
-// bf16: a row of 64 columns in words that lie on four bytes, the element in front of them and behind them by itself.
-__device__ __forceinline__ void put_sums(const uint32_t* g, uint32_t* stg, __nv_bfloat16* out, int ld, int rows, int cols) {
+// bf16: a row of 64 columns, which the warp has packed into stg, in words that lie on four bytes, the element in front of them and
+// behind them by itself.
+__device__ __forceinline__ void put_packed(const uint32_t* stg, __nv_bfloat16* out, int ld, int rows, int cols) {
   const int lane = threadIdx.x & 31;
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 32; ++i) stg[lane * 33 + i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
-  __syncwarp();
   const int odd0 = (int)((reinterpret_cast<uintptr_t>(out) >> 1) & 1), odd1 = odd0 ^ (ld & 1);       // rows that start between words
   const int col0 = 2 * lane - odd0, col1 = 2 * lane - odd1;
   const bool in0 = col0 >= 0 && col0 + 1 < cols, in1 = col1 >= 0 && col1 + 1 < cols;
@@ -182,9 +178,9 @@ __device__ __forceinline__ void put_sums(const uint32_t* g, uint32_t* stg, __nv_
   }
 }
 
-template <typename T, bool PAIR>
+template <typename T, int KB, bool PAIR>
 __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_constant__ RAMaps mp, const __grid_constant__ RAArgs<T> ar) {
-  using S = RA<T>;
+  using S = RA<T, KB>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t tiles = (raw + 1023u) & ~1023u;
@@ -276,7 +272,7 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
           if (!ok) break;
           mbar_expect_tx(dfull(r), (uint32_t)S::DL_BYTES);
 #pragma unroll
-          for (int q = 0; q < S::Q; ++q)
+          for (int q = 0; q < ROUTE_PARTS; ++q)
             tma_load_2d(tiles + DL + (uint32_t)(r * S::DL_BYTES + q * TILE), &mp.dl[q], ar.e0 + kb * 64, (int)first + b * 128, dfull(r));
           if (++r == S::RING) { r = 0; rph ^= 1u; }
         }
@@ -290,8 +286,8 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
       bool ok = mbar_wait(wfull, 0u, abort_flag);
       for (int b = 0; ok && b < blocks; ++b) {
         const int here = min(2, halves - 2 * b);                  // stages of x in this block
-        const int in = b % S::GROUP, set = b / S::GROUP & 1;      // (bf16: one group)
-        if (S::F32 && in == 0 && !mbar_wait(gempty(set), (uint32_t)(b / S::GROUP >> 1 & 1) ^ 1u, abort_flag)) { ok = false; break; }
+        const int in = b % S::GROUP, set = b / S::GROUP & 1;      // (without FLUSH one group)
+        if (S::FLUSH && in == 0 && !mbar_wait(gempty(set), (uint32_t)(b / S::GROUP >> 1 & 1) ^ 1u, abort_flag)) { ok = false; break; }
         for (int kb = 0; ok && kb < kbs; ++kb) {
           const uint32_t dl = tiles + DL + (uint32_t)(r * S::DL_BYTES);
           const int steps = min(4, (ar.n - kb * 64 + 15) >> 4);   // of 16 experts
@@ -321,8 +317,8 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
               const uint64_t l = umma_desc_mn(dl + (uint32_t)(Pairs<T>::l(p) * TILE + i * BOX));
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks) {
-                const bool large = S::F32 && p == Pairs<T>::n - 1;
-                umma(tmem_base + (uint32_t)(S::F32 ? set * S::SUMS * 64 + (large ? 64 : 0) : kb * 64), a + 128 * ks, l + 128 * ks, id_w,
+                const bool large = S::FLUSH && p == Pairs<T>::n - 1;
+                umma(tmem_base + (uint32_t)(S::FLUSH ? set * 128 + (large ? 64 : 0) : kb * 64), a + 128 * ks, l + 128 * ks, id_w,
                      (in | i | ks | (large ? 0 : p)) != 0 ? 1u : 0u);
               }
             }
@@ -344,9 +340,9 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
     int sl = 0;
     uint32_t slp = 0;
     bool ok = true;
-    float sum[S::F32 ? 32 : 1];
+    float sum[S::FLUSH ? 32 : 1];
 #pragma unroll
-    for (int i = 0; i < (S::F32 ? 32 : 1); ++i) sum[i] = 0.f;
+    for (int i = 0; i < (S::FLUSH ? 32 : 1); ++i) sum[i] = 0.f;
     if (ar.e0) wait_for_previous_kernel();                        // it made the dx that this one adds to
     if (ar.out.dbias && slice == 0) {
       wait_for_previous_kernel();
@@ -367,25 +363,26 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
         __syncwarp();
         if (lane == 0) mbar_arrive(sempty(sl));
       };
-      if constexpr (S::F32) {                                     // 32 columns at a time: `sum` holds registers
-        uint32_t g[32];
+      if constexpr (!S::F32) __syncwarp();                        // the last block's columns have left the staging buffer
 #pragma unroll 1
-        for (int p = 0; p < 2; ++p) {
-          tmem_ld32(taddr + (uint32_t)(p * 32), g);
-          tmem_ld_wait();
-          if (p) drained();
-          put_sums(g, stg, out + p * 32, ar.d, rows, cols - p * 32, ar.e0 != 0);
-        }
-      } else {
-        uint32_t g[64];
-        tmem_ld32(taddr, g);
-        tmem_ld32(taddr + 32u, g + 32);
+      for (int p = 0; p < 2; ++p) {                               // 32 columns at a time: `sum` holds registers
+        uint32_t g[32];
+        tmem_ld32(taddr + (uint32_t)(p * 32), g);
         tmem_ld_wait();
-        drained();
-        if (cols > 0) put_sums(g, stg, out, ar.d, rows, cols);
+        if (p) drained();
+        if constexpr (S::F32) {
+          put_sums(g, stg, out + p * 32, ar.d, rows, cols - p * 32, ar.e0 != 0);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) stg[lane * 33 + p * 16 + i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
+        }
+      }
+      if constexpr (!S::F32) {
+        __syncwarp();
+        if (cols > 0) put_packed(stg, out, ar.d, rows, cols);
       }
       if (++sl == S::SLOTS) { sl = 0; slp ^= 1u; }
-      if constexpr (S::F32) {
+      if constexpr (S::FLUSH) {
         const int set = b / S::GROUP & 1;
         if (b % S::GROUP == S::GROUP - 1 || b == blocks - 1) {    // experts half * 32 on, of this lane's column
           ok = mbar_wait(gfull(set), (uint32_t)(b / S::GROUP >> 1 & 1), abort_flag);
@@ -394,8 +391,8 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
           tc_fence_after();
           uint32_t g[32];
 #pragma unroll
-          for (int q = 0; q < S::SUMS; ++q) {
-            tmem_ld32(tmem_base + lanes + (uint32_t)((set * S::SUMS + q) * 64 + half * 32), g);
+          for (int q = 0; q < 2; ++q) {
+            tmem_ld32(tmem_base + lanes + (uint32_t)((set * 2 + q) * 64 + half * 32), g);
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 32; ++i) sum[i] += __uint_as_float(g[i]);
@@ -408,11 +405,15 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
     }
     const int64_t part = ((int64_t)range * ar.E + ar.e0) * ar.d;
     const int col = c0 + quarter * 32 + lane;
-    if constexpr (S::F32) {
+    if constexpr (S::FLUSH) {
       if (ok && col < ar.d)
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (half * 32 + i < ar.n) ar.out.parts[part + (int64_t)(half * 32 + i) * ar.d + col] = sum[i];
+          if (half * 32 + i < ar.n) {
+            const int64_t at = part + (int64_t)(half * 32 + i) * ar.d + col;
+            if (ar.out.dw16) ar.out.dw16[at] = __float2bfloat16_rn(sum[i]);
+            else ar.out.parts[at] = sum[i];
+          }
     } else if (ok) {
       ok = mbar_wait(gfull(0), 0u, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
@@ -451,14 +452,14 @@ __global__ void __launch_bounds__(ANY_THREADS, 1) k_route_grad_any(const __grid_
   if (tid == 0 && *abort_flag && ar.dev_status) atomicExch(ar.dev_status, (int)CAPMOE_ETIMEOUT);
 }
 
-template <typename T>
-int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out, int32_t* dev_status,
+template <typename T, int KB>
+int run(const void* split, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, void* dx, const RouteOut& out, int32_t* dev_status,
         cudaStream_t st) {
-  using S = RA<T>;
+  using S = RA<T, KB>;
   RAMaps mp = {};
-  for (int q = 0; q < S::Q; ++q)
-    if (!make_part_map(&mp.dl[q], pair, q, S::Q, (uint64_t)Eq, (uint64_t)N)) return note_cuda(cudaErrorInvalidValue);
-  auto k = d % 2 == 0 ? k_route_grad_any<T, true> : k_route_grad_any<T, false>;
+  for (int q = 0; q < ROUTE_PARTS; ++q)
+    if (!make_part_map(&mp.dl[q], split, q, ROUTE_PARTS, (uint64_t)Eq, (uint64_t)N)) return note_cuda(cudaErrorInvalidValue);
+  auto k = d % 2 == 0 ? k_route_grad_any<T, KB, true> : k_route_grad_any<T, KB, false>;
   const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
   if (err != cudaSuccess) return note_cuda(err);
   RAArgs<T> ar = {};
@@ -466,9 +467,9 @@ int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E,
   ar.slices = (int)ceil_div(d, DC);
   ar.per = (int)(ceil_div(ceil_div(N, 64), ranges) * 64);
   ar.dx = (T*)dx; ar.out = out; ar.dev_status = dev_status;
-  for (int e0 = 0; e0 < E; e0 += S::KB * 64) {
+  for (int e0 = 0; e0 < E; e0 += KB * 64) {
     ar.e0 = e0;
-    ar.n = E - e0 < S::KB * 64 ? E - e0 : S::KB * 64;
+    ar.n = E - e0 < KB * 64 ? E - e0 : KB * 64;
     const int rc = note_cuda(launch_chained(k, (unsigned)(ar.slices * ranges), ANY_THREADS, S::SMEM, st, mp, ar));
     count_launch(1);
     if (rc != CAPMOE_OK) return rc;
@@ -479,12 +480,18 @@ int run(const void* pair, const void* x, const void* w, int64_t N, int d, int E,
 
 }  // namespace
 
-int route_grad_any_ranges(int64_t N, int d, int dtype) { return route_ranges(N, ceil_div(d, DC), dtype == CAPMOE_F32 ? N : ROUTE_CHAIN); }
+// The longest sum of bf16 tokens with more than 64 experts that one accumulator takes (64 groups of 16 tokens, three MMAs each:
+// dW_r is off by 4 10^-6 of it, 2.8 10^-5 after 8192 tokens).
+constexpr int64_t ROUTE_CHAIN = 1024;
+int route_grad_any_ranges(int64_t N, int d, int E, int dtype) {
+  return route_ranges(N, ceil_div(d, DC), dtype == CAPMOE_F32 || E <= 64 ? N : ROUTE_CHAIN);
+}
 
-int route_grad_any(const void* pair, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx,
+int route_grad_any(const void* split, const void* x, const void* w, int64_t N, int d, int E, int Eq, int ranges, int dtype, void* dx,
                    const RouteOut& out, int32_t* dev_status, cudaStream_t st) {
-  return dtype == CAPMOE_F32 ? run<float>(pair, x, w, N, d, E, Eq, ranges, dx, out, dev_status, st)
-                             : run<__nv_bfloat16>(pair, x, w, N, d, E, Eq, ranges, dx, out, dev_status, st);
+  if (dtype == CAPMOE_F32) return run<float, 1>(split, x, w, N, d, E, Eq, ranges, dx, out, dev_status, st);
+  auto of = E <= 64 ? run<__nv_bfloat16, 1> : E <= 128 ? run<__nv_bfloat16, 2> : run<__nv_bfloat16, 4>;
+  return of(split, x, w, N, d, E, Eq, ranges, dx, out, dev_status, st);
 }
 
 }  // namespace capmoe
