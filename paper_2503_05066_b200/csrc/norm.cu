@@ -2,7 +2,7 @@
 // expert products read, and its gradients.
 //   h = x + residual (rounded to the storage type: what the residual stream keeps)
 //   rstd = (sum_c h_c^2 / d + eps)^(-1/2),  y = h rstd w,  codes of the rounded y as capmoe_quantize_rows makes them
-//   dx = rstd (g - h rstd^2 (sum_c g_c h_c) / d) + dh with g = dy w,  dw = sum over the rows of dy h rstd
+//   dx = rstd (g - n (sum_c g_c n_c) / d) + dh with g = dy w and n = h rstd,  dw = sum over the rows of dy n
 // All of it in fp32; what is stored has one rounding (h, y, dx) or none before the last (rstd, dw).
 #include "gmm.cuh"
 #include "rowvec.cuh"
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
         dw[u][i] = fmaf(p[i], n, dw[u][i]);
       }
     }
-    const float k = -row_sum(dot, a.wpr, red[it]) / (float)d * rstd * rstd;
+    const float mean = row_sum(dot, a.wpr, red[it]) / (float)d;
 #pragma unroll
     for (int u = 0; u < VPT; ++u) {
       const int c = column<W, NV>(u, tpr, t);
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(NT_MAX) k_rms_norm_grad(const GradArgs<T> a) {
       Vec16<T>::load(w[u], g);
       Vec16<T>::load(get_shared(from + (uint32_t)(2 * VPT + u) * step), e);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) p[i] = fmaf(q[i], k, fmaf(rstd, p[i] * g[i], e[i]));
+      for (int i = 0; i < NV; ++i) p[i] = fmaf(rstd, fmaf(-q[i] * rstd, mean, p[i] * g[i]), e[i]);      // (rstd^2 alone may pass fp32)
       if (live && c < d) put_cells<T, W>(a.dx + row * d + c, d - c, Vec16<T>::store(p));
     }
     rstd = rstd1;
