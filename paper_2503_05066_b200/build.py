@@ -1,4 +1,4 @@
-"""Builds libcapmoe.so (sm_100a only, nvcc) and the Python binding _bind.so (g++) in-tree.  `python -m paper_2503_05066_b200.build`."""
+"""Builds libcapmoe.so (sm_100a only, nvcc) and the Python binding _bind.*.so (g++) in-tree.  `python -m paper_2503_05066_b200.build`."""
 from __future__ import annotations
 
 import os
@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcapmoe.so")
-BIND_SRC, BIND = os.path.join(CSRC, "bind.cpp"), os.path.join(PKG, "_bind.so")
+BIND_SRC = os.path.join(CSRC, "bind.cpp")
 SOURCES = ["api.cu", "route.cu", "drop.cu", "drop_cluster.cu", "drop_parallel.cu", "variants.cu", "permute_combine.cu", "ffn_simt.cu", "ffn_tc.cu", "ffn_tc_t.cu",
            "grouped_mm.cu", "grouped_fp8.cu", "gmm_rows.cu", "gmm_dw.cu", "gmm_swiglu8.cu",
            "norm.cu", "token_grad.cu", "route_grad.cu", "route_grad_tc.cu", "route_grad_any.cu"]
@@ -25,6 +25,13 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def bind_path() -> str:
+    """The binding's file for the running interpreter and torch: it is linked against both, so each pair has a file of its own."""
+    import sysconfig
+    import torch
+    return os.path.join(PKG, f"_bind.{sysconfig.get_config_var('SOABI')}-torch-{torch.__version__}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}.so")
+
+
 def _bind_cmd() -> list:
     """The binding against the running interpreter and torch, and the library beside it."""
     import sysconfig
@@ -34,7 +41,7 @@ def _bind_cmd() -> list:
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"),
            sysconfig.get_paths()["include"]]
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
-            *[a for p in inc for a in ("-isystem", p)], BIND_SRC, "-o", BIND, "-L", PKG, "-l:libcapmoe.so", "-Wl,-rpath,$ORIGIN",
+            *[a for p in inc for a in ("-isystem", p)], BIND_SRC, "-o", bind_path(), "-L", PKG, "-l:libcapmoe.so", "-Wl,-rpath,$ORIGIN",
             "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
 
 
@@ -51,7 +58,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     header = os.path.join(ROOT, "include", "capmoe.h")
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))] + [header, __file__]
     fresh = lambda out, of: not force and os.path.exists(out) and os.path.getmtime(out) >= max(os.path.getmtime(p) for p in of)  # noqa: E731
-    bound = fresh(BIND, [BIND_SRC, header, __file__])
+    bound = fresh(bind_path(), [BIND_SRC, header, __file__])
     if fresh(LIB, deps) and bound:
         return LIB                       # up to date (object files need not exist: only the .so travel)
     objdir = os.path.join(PKG, "build")
@@ -68,7 +75,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError("nvcc failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
+            raise RuntimeError("failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
         return r.stderr
     if not fresh(LIB, deps):
         with ThreadPoolExecutor(max_workers=8) as ex:

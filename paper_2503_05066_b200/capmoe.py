@@ -9,13 +9,15 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import importlib
+import importlib.util
 import math
 import os
 from dataclasses import dataclass
 from typing import Optional
 
 import torch
+
+from .build import bind_path
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libcapmoe.so")
@@ -451,17 +453,42 @@ _bind = None                # the compiled binding (csrc/bind.cpp), loaded with 
 
 
 def _binding():
+    """The compiled binding for this interpreter and torch; the operators that match their arguments with it need it."""
     global _bind
     lib()
-    if not os.path.exists(os.path.join(_PKG, "_bind.so")):
-        raise RuntimeError(f"{_PKG}/_bind.so is missing: build it with `python -m paper_2503_05066_b200.build`")
-    _bind = importlib.import_module("paper_2503_05066_b200._bind")
+    path = bind_path()
+    if not os.path.exists(path):
+        raise RuntimeError(f"{path} is missing: build it with `python -m paper_2503_05066_b200.build`")
+    spec = importlib.util.spec_from_file_location("paper_2503_05066_b200._bind", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    _bind = module
     return _bind
+
+
+def _run_unbound(name: str, like, *args):
+    """_run by ctypes, for the grouped products where the binding has not been built for this interpreter and torch."""
+    here = like.get_device()
+    raw = []
+    for v in args:
+        if isinstance(v, torch.Tensor):
+            if v.get_device() != here or here < 0:
+                _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
+            assert v.is_contiguous(), "capmoe tensors must be contiguous"
+            raw.append(v.data_ptr())
+        else:
+            raw.append(v)
+    if here != torch.cuda.current_device():
+        _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
+    return getattr(lib(), name)(*raw, torch.cuda.current_stream(here).cuda_stream)
 
 
 def _run(name: str, like, *args):
     """Calls entry point `name` with `args` and the current stream; tensors among the arguments pass as their addresses."""
-    rc = (_bind or _binding()).run(name, like, *args)
+    if _bind is None and not os.path.exists(bind_path()):
+        rc = _run_unbound(name, like, *args)
+    else:
+        rc = (_bind or _binding()).run(name, like, *args)
     if rc:
         raise CapmoeError(rc, name)
     if rc is None:                         # nothing was called
