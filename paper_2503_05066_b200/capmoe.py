@@ -467,20 +467,13 @@ def _binding():
 
 
 def _run_unbound(name: str, like, *args):
-    """_run by ctypes, for the grouped products where the binding has not been built for this interpreter and torch."""
+    """The binding's run() by ctypes, for the grouped products where it has not been built for this interpreter and torch."""
     here = like.get_device()
-    raw = []
-    for v in args:
-        if isinstance(v, torch.Tensor):
-            if v.get_device() != here or here < 0:
-                _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
-            assert v.is_contiguous(), "capmoe tensors must be contiguous"
-            raw.append(v.data_ptr())
-        else:
-            raw.append(v)
+    if any(isinstance(v, torch.Tensor) and (v.get_device() != here or not v.is_contiguous()) for v in args) or here < 0:
+        return None
     if here != torch.cuda.current_device():
-        _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
-    return getattr(lib(), name)(*raw, torch.cuda.current_stream(here).cuda_stream)
+        return None
+    return getattr(lib(), name)(*[v.data_ptr() if isinstance(v, torch.Tensor) else v for v in args], torch.cuda.current_stream(here).cuda_stream)
 
 
 def _run(name: str, like, *args):
@@ -498,6 +491,8 @@ def _run(name: str, like, *args):
                 if v.get_device() != here or here < 0:
                     _refuse(name, f"CUDA tensors on one device expected, got {v.device} next to {like.device}")
                 assert v.is_contiguous(), "capmoe tensors must be contiguous"
+        for sizes in (_dw_bytes, _ffn_backward_bytes, _norm_backward_bytes, _route_backward_bytes):
+            sizes.cache_clear()            # the library sized a workspace for the current device, but it is remembered for `here`
         _refuse(name, f"tensors on cuda:{here}, but cuda:{torch.cuda.current_device()} is the current device")
 
 

@@ -72,3 +72,44 @@ def test_grouped_products_without_a_binding_on_a_gpu(cm, monkeypatch, tmp_path):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(cm.CapmoeError, match="CUDA tensors on one device expected"):
         cm.grouped_mm(x, off, w.cpu())
+
+
+def test_a_refused_call_leaves_no_size_for_its_device(cm, monkeypatch):
+    """Sizes come from the current device's SM count and are remembered for the tensors' device: a call that is refused because the two
+    differ must not leave one behind."""
+    class On1(torch.Tensor):
+        def get_device(self):
+            return 1
+
+    current, seen = [0], []
+
+    class Bind:
+        match = staticmethod(lambda pattern, *tensors: cm_match(pattern, *tensors))
+
+        @staticmethod
+        def new(like, dtype, *sizes):
+            t = torch.empty(sizes or like.shape, dtype=dtype or like.dtype)
+            if dtype == torch.uint8:
+                seen.append(t.numel())
+            return t.as_subclass(On1)
+
+        @staticmethod
+        def run(name, like, *args):
+            return None if current[0] != like.get_device() else 0
+
+    cm_match = cm._binding().match
+    monkeypatch.setattr(cm, "_bind", Bind)
+    monkeypatch.setattr(cm, "_bytes", lambda fn, *args: 512 + 1000 * current[0])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    f, i = (lambda *s: torch.zeros(s).as_subclass(On1)), (lambda *s: torch.zeros(s, dtype=torch.int32).as_subclass(On1))
+    calls = [lambda: cm.rms_norm_backward(f(4, 64), f(4, 64), f(64), f(4)),
+             lambda: cm.route_backward(f(4, 64), f(8, 64), f(4, 8), i(4, 2), i(4, 2), f(8))]
+    for call in calls:
+        current[0] = 0
+        with pytest.raises(cm.CapmoeError, match="tensors on cuda:1, but cuda:0 is the current device"):
+            call()
+        current[0] = 1
+        call()
+    cm._norm_backward_bytes.cache_clear()
+    cm._route_backward_bytes.cache_clear()
+    assert seen == [512, 1512, 512, 1512]
