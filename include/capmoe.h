@@ -383,6 +383,8 @@ int capmoe_rms_norm_backward(const void* dy, const void* h, const void* w, const
  *                              dbias = sum_t dlogits [E] fp32.
  *                            On tensor cores (bf16, and fp32 beyond eight experts) every fp32 factor enters the products as the sum
  *                            of three bf16 numbers that it is: nothing of dlogits is lost, of fp32 terms at most 2^-30 each.
+ *                            A NaN or an infinity among x, w_router and dS reaches the sums that hold it and no others; on tensor
+ *                            cores, where it meets zeros among the three numbers, it may come out of them as a NaN.
  *                            N = 0 leaves zeros in dw and dbias.  All sums have a fixed order for given sizes and device.
  *                            ws: capmoe_route_backward_workspace_bytes(N,d,E,dtype) bytes on the device that is current.
  * The first three: rows of whole 16-byte vectors, slots <= 288, N and A_max < 2^31.  route_backward: E <= 256, k <= 32,

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(RG_WARPS * 32) k_route_logit_grad(const LogitA
           for (int q = 0; q < ROUTE_PARTS; ++q) {
             const uint32_t top = __float_as_uint(rest) & 0xffff0000u;
             p[q * a.Eq] = __ushort_as_bfloat16((unsigned short)(top >> 16));
-            rest = rest == __uint_as_float(top) ? 0.f : rest - __uint_as_float(top);         // (an infinity leaves nothing)
+            rest = rest == __uint_as_float(top) ? 0.f : rest - __uint_as_float(top);         // (an infinity: zeros, not inf - inf)
           }
         }
       }

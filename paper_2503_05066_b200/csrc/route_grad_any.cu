@@ -111,7 +111,7 @@ struct Rows {
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
           *reinterpret_cast<uint32_t*>(at + p * TILE) = __byte_perm(a, b, 0x7632);
-          const uint32_t ta = a & 0xffff0000u, tb = b & 0xffff0000u;           // (an infinity leaves nothing)
+          const uint32_t ta = a & 0xffff0000u, tb = b & 0xffff0000u;           // (an infinity: zeros, not inf - inf)
           a = a == ta ? 0u : __float_as_uint(__uint_as_float(a) - __uint_as_float(ta));
           b = b == tb ? 0u : __float_as_uint(__uint_as_float(b) - __uint_as_float(tb));
         }
