@@ -54,6 +54,10 @@ int permute_impl(const void* x, int64_t N, int d, int E, int k, int slots, int D
 int sum_parts(const float* part, int64_t parts, int d, int out_dtype, void* out, cudaStream_t st);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+template <class... P>
+inline bool usable(P... p) {                // every pointer there and 16-byte aligned
+  return ((p != nullptr && aligned16(p)) && ...);
+}
 inline size_t elt_size(int dtype) { return dtype == CAPMOE_F32 ? 4 : 2; }
 inline cudaStream_t as_stream(void* s) { return reinterpret_cast<cudaStream_t>(s); }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -77,10 +81,10 @@ __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("gridd
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_chained(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem,
+inline cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem,
                                   cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -90,6 +94,12 @@ inline cudaError_t launch_chained(void (*kernel)(KArgs...), unsigned grid, unsig
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+// Lets a kernel have this much dynamic shared memory (the default limit is 48 KB, what the kernel declares included).
+template <typename... KArgs>
+inline cudaError_t allow_smem(void (*kernel)(KArgs...), size_t smem) {
+  return smem > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
 }
 
 // Which tensor-core FFN kernel serves a call: chosen from the shape (FFN_AUTO), or forced through

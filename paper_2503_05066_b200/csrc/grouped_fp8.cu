@@ -246,10 +246,6 @@ int check_shape(const int32_t* offsets, int E, int d, int n, int64_t rows) {
     return CAPMOE_EUNSUPPORTED;
   return CAPMOE_OK;
 }
-template <class... P>
-bool usable(P... p) {
-  return ((p != nullptr && aligned16(p)) && ...);
-}
 
 // Workspace of the 8-bit FFN: codes and scales of x and of the hidden rows, and (sizes without a
 // tensor-core kernel) the hidden rows in fp32.  Rows of scales start on 16 bytes (one load for 16 of them: with packed rows

@@ -276,10 +276,6 @@ int check_shape(const int32_t* offsets, int E, int d, int n, int dtype, int64_t 
     return CAPMOE_EUNSUPPORTED;
   return CAPMOE_OK;
 }
-template <class... P>
-bool usable(P... p) {                       // every pointer there and 16-byte aligned
-  return ((p != nullptr && aligned16(p)) && ...);
-}
 size_t align256(size_t b) { return (b + 255) / 256 * 256; }
 void* align256(void* p) { return (void*)align256((size_t)p); }
 // Parts of the weight gradients' reductions: all that pay when the workspace has room for them behind `parts`, else one.

@@ -210,12 +210,6 @@ __device__ __forceinline__ uint4 together(const uint16_t* a) {
 
 // Per-thread ring of the rows to come: every thread copies the 16-byte vectors that it will use itself into its own places of
 // shared memory, so nothing but its own copies has to be waited for.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {        // zeros where not in
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16u : 0u) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 __device__ __forceinline__ uint4 get_shared(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
@@ -437,10 +431,8 @@ int grad_run(const GradArgs<T>& a, cudaStream_t st) {
   auto k = room == 1 ? k_rms_norm_grad<T, W, 1, GRAD_DEPTH1> : room == 2 ? k_rms_norm_grad<T, W, 2, GRAD_DEPTH2>
            : room == 4 ? k_rms_norm_grad<T, W, 4, 2> : k_rms_norm_grad<T, W, 8, 1>;
   const size_t smem = (size_t)depth * 3 * (size_t)room * threads_of(a.wpr) * 16;
-  if (smem > 40 * 1024) {                    // (the default limit is 48 KB, what the kernel declares included)
-    const cudaError_t err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (err != cudaSuccess) return note_cuda(err);
-  }
+  const cudaError_t err = allow_smem(k, smem);
+  if (err != cudaSuccess) return note_cuda(err);
   const int rc = note_cuda(launch_chained(k, (unsigned)grad_blocks(a.N, a.wpr), threads_of(a.wpr), smem, st, a));
   count_launch(1);
   return rc;
@@ -462,10 +454,6 @@ int check_norm(int64_t N, int d, int dtype) {
   if (N < 0 || d < 1) return CAPMOE_EINVAL;
   if ((dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) || d > NORM_MAX_D) return CAPMOE_EUNSUPPORTED;
   return CAPMOE_OK;
-}
-template <class... P>
-bool usable(P... p) {
-  return ((p != nullptr && aligned16(p)) && ...);
 }
 
 }  // namespace

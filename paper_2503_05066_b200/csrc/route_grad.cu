@@ -359,16 +359,8 @@ RouteWs route_ws(int64_t N, int d, int E, int dtype) {
 
 int few_run(const ScoreGrad& s, const void* x, const void* w, int d, int ranges, float* dlogits, void* dx, float* parts, float* bias, cudaStream_t st) {
   const FewArgs a{s, (const float*)x, (const float*)w, d, few_tx(d), (int)ceil_div(s.N, ranges), (float*)dx, dlogits, parts, bias};
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ceil_div(d, a.tx * FEW_V), (unsigned)ranges);
-  cfg.blockDim = dim3(FEW_N);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const int rc = note_cuda(cudaLaunchKernelEx(&cfg, d % FEW_V == 0 ? k_route_grad_few<true> : k_route_grad_few<false>, a));
+  const int rc = note_cuda(launch_chained(d % FEW_V == 0 ? k_route_grad_few<true> : k_route_grad_few<false>,
+                                          dim3((unsigned)ceil_div(d, a.tx * FEW_V), (unsigned)ranges), FEW_N, 0, st, a));
   count_launch(1);
   return rc;
 }
@@ -377,10 +369,6 @@ int check_route(int64_t N, int d, int E, int dtype) {
   if (N < 0 || d < 1 || E < 1) return CAPMOE_EINVAL;
   if ((dtype != CAPMOE_F32 && dtype != CAPMOE_BF16) || E > 256 || N > GMM_MAX_ROWS || ceil_div(d, 64) > 65535) return CAPMOE_EUNSUPPORTED;
   return CAPMOE_OK;
-}
-template <class... P>
-bool usable(P... p) {
-  return ((p != nullptr && aligned16(p)) && ...);
 }
 
 }  // namespace

@@ -1,9 +1,17 @@
-// 16-byte vectors of a row: what is stored, as fp32, and back (one rounding to the storage type).
+// 16-byte vectors of a row: what is stored, as fp32, and back (one rounding to the storage type), and their asynchronous copies.
 #pragma once
 #include "common.cuh"
 
 namespace capmoe {
 namespace {
+
+// Asynchronous copies of 16 bytes into shared memory (zeros where not `in`), in groups that their own thread waits for.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in = true) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16u : 0u) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 template <typename T> struct Vec16;
 template <> struct Vec16<float> {

@@ -25,21 +25,14 @@ __device__ __forceinline__ int32_t slot_at(const int32_t* slot_row, int64_t t, i
   const int32_t r = t < N && s < slots ? slot_row[t * slots + s] : -1;
   return r < rows ? r : -1;
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// What a stage holds: `n` row chunks (below zero: there are no further stages), of token `t`, vectors from `v0` on; `first` and
-// `last` of the sums that they belong to; the rows, and their weights.
+// What a stage holds: `n` row chunks (below zero: there are no further stages), vectors from `v0` on; `first` and `last` of the sums
+// that they belong to; the rows, and their weights.
 struct Stage {
   int n, v0, first, last;
-  long long t;
   int32_t row[ROWS];
   float w[ROWS];
 };
@@ -328,21 +321,9 @@ static_assert(CG_SPLIT * sizeof(RingC) + sizeof(float) * MAX_SLOTS * (CG_SPLIT +
 
 template <class... KArgs, class... Args>
 int launch_wide(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, Args... args) {
-  if (smem > 40 * 1024) {                    // (the default limit is 48 KB, what the kernel declares included)
-    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (err != cudaSuccess) return note_cuda(err);
-  }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const int rc = note_cuda(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
+  const cudaError_t err = allow_smem(kernel, smem);
+  if (err != cudaSuccess) return note_cuda(err);
+  const int rc = note_cuda(launch_chained(kernel, grid, block, smem, st, args...));
   count_launch(1);
   return rc;
 }
@@ -360,10 +341,6 @@ int check_rows(int64_t N, int d, int slots, int64_t rows, size_t elt) {
   if (N < 0 || d < 1 || slots < 1 || rows < 0) return CAPMOE_EINVAL;
   if (slots > MAX_SLOTS || ((size_t)d * elt) % 16 != 0 || rows >= ((int64_t)1 << 31) || N >= ((int64_t)1 << 31)) return CAPMOE_EUNSUPPORTED;
   return CAPMOE_OK;
-}
-template <class... P>
-bool usable(P... p) {
-  return ((p != nullptr && aligned16(p)) && ...);
 }
 
 }  // namespace
