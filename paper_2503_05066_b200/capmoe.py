@@ -1249,7 +1249,8 @@ class MoELayer:
         """Gradients of the layer's last forward() from dy [N,d], the gradient of y, and dscores ([N,E] or [E]), what the router's
         scores get besides (a balance loss).  The forward's buffers must be as it left them.  -> dict(dx [N,d], dw_router, dbias,
         dw_gate, dw_up, dw_down, dlogits, and for a shared expert dws_gate, dws_up, dws_down); the router's weights' gradient in
-        out_dtype (float32) or the activations' dtype."""
+        out_dtype (float32) or the activations' dtype.  The parts of dx that come through the router and the shared expert are rounded to
+        the activations' dtype before they are added up with the experts' (in fp32): half a step of each part."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.backward(dy, dscores, out_dtype)

@@ -9,9 +9,10 @@
 // block.  The MMAs cut their sums off where fp32 ends, so dW_r^T stays in tensor memory for GROUP blocks only; the epilogue adds the
 // groups up in registers, and the range's sum leaves as a part, fp32, that route_grad.cu adds up in order.  dx passes through two
 // accumulators of 128 columns, so that its epilogue overlaps the MMAs.
-// What bounds it: up to 64 experts HBM, x is read and dx written once; from 128 on the tensor pipe.  16,384 tokens of 2048 columns:
-// 64 experts 41.5 us with the other two launches, 128 experts 74, 256 experts 125 (dl as two numbers, which lose 2^-18 of it, and one
-// accumulator for a range, which loses up to 2 10^-5 of dW_r: 41.8, 51, 93).
+// What bounds it: up to 64 experts HBM, x is read and dx written once; beyond, dl's way from L2, which every slice of columns reads
+// again (256 experts, 2048 columns: 400 MB), and the MMAs.  16,384 tokens of 2048 columns, with the other two launches: 64 experts
+// 41.5 us (37.6 without the MMAs), 128 experts 67 to 74 (54), 256 experts 125 (93).  dl as two numbers, which lose 2^-18 of it, and one
+// accumulator for a range, which loses up to 2 10^-5 of dW_r: 41.8, 51, 93.
 #include "gmm_tc.cuh"
 #include "route_grad.cuh"
 
